@@ -384,6 +384,76 @@ int a2cid2_graph_chi(int32_t n, int64_t n_edges, const int32_t* ei, const int32_
  * alpha~ = 1/2 sqrt(chi1/chi2); accelerated == 0: eta = 0, alpha = alpha~ = 1/2. */
 int a2cid2_prescribe(double chi1, double chi2, int32_t accelerated, double* eta, double* alpha, double* alpha_tilde);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators of a language model's gradient event
+ *
+ * The engine applies gradients that the user's model writes into rows of the gradient buffer. When the
+ * rows are the parameters of a language model, these calls make such a row: the embedding lookup and
+ * its gradient, the loss over the vocabulary with its gradients, and the orthogonalisation of a
+ * matrix's gradient or momentum for all workers at once. They need no handle.
+ *
+ *   - All buffers are device memory of the current device, of the storage type (A2_F32 or A2_BF16;
+ *     sums, softmax statistics and norms are held in fp32 or more) unless stated otherwise. A matrix is
+ *     row-major; its pitch counts elements from one row to the next and is at least its width. A matrix
+ *     may start anywhere inside a worker's row (element alignment suffices; matrices whose start and pitch
+ *     are multiples of 16 bytes take faster accesses). Buffers of one call must not overlap
+ *     unless stated otherwise.
+ *   - Work is queued on cuda_stream (a cudaStream_t, NULL = default stream) and not waited for. Nothing is
+ *     allocated: workspace is device memory of at least the size that the operator's _workspace call
+ *     gives for the same sizes, 256-byte aligned, used by the queued work only. Calls whose work may
+ *     overlap need workspaces of their own.
+ *   - Token ids and targets are int32; an id outside [0, vocab) means "no token" (padding, a masked prompt).
+ *   - Results do not depend on the order in which the GPU happens to work: the same call gives the same bits.
+ *   - Errors: A2_EINVAL (NULL, size, pitch, alignment, type, non-finite parameter, workspace too small),
+ *     A2_ERANGE (a size beyond what the kernels index), A2_ECUDA; text from a2cid2_last_error(NULL).
+ *     Nothing is queued by a call that fails with one of the first two.
+ * ------------------------------------------------------------------------------------------ */
+
+/* out[t] = scale * table[ids[t]], a row of zeros where ids[t] is no token. table [vocab, width],
+ * ids [n_ids], out [n_ids, width]. n_ids = 0 does nothing. */
+int a2cid2_embed(const void* table, int64_t vocab, int64_t width, int64_t table_pitch, const int32_t* ids, int64_t n_ids,
+                 double scale, void* out, int64_t out_pitch, int32_t storage_dtype, void* cuda_stream);
+
+int a2cid2_embed_grad_workspace(int64_t vocab, int64_t width, int64_t n_ids, int64_t* bytes);
+
+/* grad_table[v] = scale * sum over t with ids[t] = v of grad_out[t]: the positions are sorted by id, each row's sum
+ * is taken in fp32 and rounded once. accumulate != 0 adds to grad_table instead (for a
+ * table tied to the vocabulary's matrix) and leaves rows without a token untouched; else those become zeros.
+ * A row of grad_out whose id is no token is not read. grad_out [n_ids, width], grad_table [vocab, width]. */
+int a2cid2_embed_grad(const void* grad_out, int64_t grad_out_pitch, const int32_t* ids, int64_t n_ids, int64_t vocab,
+                      int64_t width, double scale, int32_t accumulate, void* grad_table, int64_t grad_table_pitch,
+                      int32_t storage_dtype, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+int a2cid2_vocab_loss_workspace(int64_t n_tokens, int64_t width, int64_t vocab, int32_t with_grad, int32_t storage_dtype,
+                                int64_t* bytes);
+
+/* Softmax cross entropy of hidden [n_tokens, width] against the vocabulary's matrix head [vocab, width]:
+ *   z_tv = <hidden_t, head_v>,  lse[t] = log sum_v exp z_tv,  loss[t] = lse[t] - z_{t, targets[t]}
+ * (0 where targets[t] is no token), both float [n_tokens]. The logits are made in pieces and never kept.
+ * With grad_hidden [n_tokens, width] and/or grad_head [vocab, width] not NULL the same call gives the gradients of
+ * sum_t scale * weights[t] * loss[t] (weights: float [n_tokens] or NULL for ones):
+ *   P_tv = scale * weights[t] * (exp(z_tv - lse[t]) - [v = targets[t]]), 0 where targets[t] is no token,
+ *   grad_hidden_t = sum_v P_tv head_v,  grad_head_v = sum_t P_tv hidden_t.
+ * A token without a target adds nothing to grad_head and has a zero row in grad_hidden, whatever its hidden row and weight
+ * hold. With fp32 rows the products are formed from two 11-bit words an operand (22 bits, about what an fp32 sum keeps); with
+ * bf16 rows P is rounded to bf16 before its products. n_tokens = 0 zeroes grad_head. */
+int a2cid2_vocab_loss(const void* hidden, int64_t hidden_pitch, const void* head, int64_t head_pitch, const int32_t* targets,
+                      int64_t n_tokens, int64_t width, int64_t vocab, const float* weights, double scale, float* loss,
+                      float* lse, void* grad_hidden, int64_t grad_hidden_pitch, void* grad_head, int64_t grad_head_pitch,
+                      int32_t storage_dtype, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+int a2cid2_orthogonalize_workspace(int64_t n_mats, int64_t rows, int64_t cols, int32_t storage_dtype, int64_t* bytes);
+
+/* Pushes the singular values of every matrix towards one: X = G / (|G|_F + eps), then `steps` times
+ * X <- a X + (b A + c A^2) X with A = X X^T (for rows > cols on the transposed matrix, which is the same polynomial),
+ * out = scale * X. Matrix k of the batch starts at in + k * in_stride elements: with one matrix per worker's row, the stride is
+ * the row pitch. out == in with the same stride and pitch is allowed. eps >= 0; a zero matrix gives zeros (also with eps = 0).
+ * n_mats = 0 does nothing; steps = 0 normalises. */
+int a2cid2_orthogonalize(const void* in, int64_t in_stride, int64_t in_pitch, int64_t n_mats, int64_t rows, int64_t cols,
+                         int32_t steps, double a, double b, double c, double eps, double scale, void* out, int64_t out_stride,
+                         int64_t out_pitch, int32_t storage_dtype, void* workspace, int64_t workspace_bytes,
+                         void* cuda_stream);
+
 /* Library version string. */
 const char* a2cid2_version(void);
 

@@ -61,6 +61,7 @@ _dp = C.POINTER(C.c_double)
 _ip = C.POINTER(C.c_int32)
 _lp = C.POINTER(C.c_int64)
 _vp = C.c_void_p
+_i64 = C.c_int64
 
 # name -> (restype, argtypes); mirrors include/a2cid2.h one to one
 SIGNATURES = {
@@ -99,6 +100,15 @@ SIGNATURES = {
     "a2cid2_sched_destroy": (None, [_vp]),
     "a2cid2_graph_chi": (C.c_int, [C.c_int32, C.c_int64, _ip, _ip, _dp, _dp, _dp]),
     "a2cid2_prescribe": (C.c_int, [C.c_double, C.c_double, C.c_int32, _dp, _dp, _dp]),
+    "a2cid2_embed": (C.c_int, [_vp, _i64, _i64, _i64, _vp, _i64, C.c_double, _vp, _i64, C.c_int32, _vp]),
+    "a2cid2_embed_grad_workspace": (C.c_int, [_i64, _i64, _i64, _lp]),
+    "a2cid2_embed_grad": (C.c_int, [_vp, _i64, _vp, _i64, _i64, _i64, C.c_double, C.c_int32, _vp, _i64, C.c_int32, _vp, _i64, _vp]),
+    "a2cid2_vocab_loss_workspace": (C.c_int, [_i64, _i64, _i64, C.c_int32, C.c_int32, _lp]),
+    "a2cid2_vocab_loss": (C.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _vp, C.c_double, _vp, _vp, _vp, _i64, _vp, _i64,
+                                    C.c_int32, _vp, _i64, _vp]),
+    "a2cid2_orthogonalize_workspace": (C.c_int, [_i64, _i64, _i64, C.c_int32, _lp]),
+    "a2cid2_orthogonalize": (C.c_int, [_vp, _i64, _i64, _i64, _i64, _i64, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double,
+                                       C.c_double, _vp, _i64, _i64, C.c_int32, _vp, _i64, _vp]),
     "a2cid2_version": (C.c_char_p, []),
 }
 

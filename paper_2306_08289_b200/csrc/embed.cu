@@ -1,0 +1,440 @@
+// Embedding lookup y_t = s E[id_t] and its gradient dE_v (+)= s sum_{t: id_t = v} dy_t.
+#include "lm_ops.h"
+
+namespace a2 {
+
+namespace {
+
+constexpr int kThreads = 128;
+
+// Threads that share a row's columns: enough for one vector each, at most a CTA, a power of two.
+int group_threads(int64_t width, int vec) {
+    int g = 8;
+    while (g < kThreads && (int64_t)g * vec < width) g *= 2;
+    return g;
+}
+
+bool aligned16(const void* p, int64_t pitch, int64_t elem) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (pitch * elem) % 16 == 0;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Lookup. Bound by memory: a token's row is read once and written once. A group of threads owns kRows
+// tokens, so that every thread has that many loads of 16 bytes in flight.
+// ---------------------------------------------------------------------------------------------
+constexpr int kRows = 4;
+
+template <class T, int VEC>
+__global__ void __launch_bounds__(kThreads) k_embed(const T* __restrict__ table, int64_t vocab, int64_t width, int64_t table_pitch,
+                                                    const int32_t* __restrict__ ids, int64_t n_ids, float scale,
+                                                    T* __restrict__ out, int64_t out_pitch, int group) {
+    const int lane = threadIdx.x % group;
+    const int64_t first = ((int64_t)blockIdx.x * (kThreads / group) + threadIdx.x / group) * kRows;
+    int64_t id[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const int64_t v = first + r < n_ids ? ids[first + r] : -1;
+        id[r] = v < vocab ? v : -1;
+    }
+    for (int64_t c = (int64_t)lane * VEC; c < width; c += (int64_t)group * VEC) {
+        Pack<T, VEC> row[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+            if (id[r] >= 0) row[r] = *reinterpret_cast<const Pack<T, VEC>*>(table + id[r] * table_pitch + c);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (first + r >= n_ids) break;
+            Pack<T, VEC> o;
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) o.v[k] = narrow<T>(id[r] >= 0 ? widen(row[r].v[k]) * scale : 0.0f);
+            *reinterpret_cast<Pack<T, VEC>*>(out + (first + r) * out_pitch + c) = o;
+        }
+    }
+}
+
+template <class T>
+cudaError_t embed_typed(const EmbedArgs& a, cudaStream_t s) {
+    constexpr int kVec = 16 / sizeof(T);
+    const bool wide = a.width % kVec == 0 && aligned16(a.table, a.table_pitch, sizeof(T)) && aligned16(a.out, a.out_pitch, sizeof(T));
+    const int group = group_threads(a.width, wide ? kVec : 1);
+    const int64_t grid = ceil_div(a.n_ids, (int64_t)(kThreads / group) * kRows);
+    auto* table = static_cast<const T*>(a.table);
+    auto* out = static_cast<T*>(a.out);
+    if (wide)
+        k_embed<T, kVec><<<(unsigned)grid, kThreads, 0, s>>>(table, a.vocab, a.width, a.table_pitch, a.ids, a.n_ids, a.scale, out,
+                                                             a.out_pitch, group);
+    else
+        k_embed<T, 1><<<(unsigned)grid, kThreads, 0, s>>>(table, a.vocab, a.width, a.table_pitch, a.ids, a.n_ids, a.scale, out,
+                                                          a.out_pitch, group);
+    return cudaGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------------
+// Stable sort of the positions 0 .. n-1 by their id (an id outside the table sorts last, as `vocab`), least
+// significant digit first, kDigitBits a pass. Stable and without floating atomics, so the gradient's sums have
+// one fixed order: positions ascending.
+// ---------------------------------------------------------------------------------------------
+constexpr int kDigitBits = 9;
+constexpr int kDigits = 1 << kDigitBits;
+constexpr int kSortThreads = kDigits;  // thread d of a sorting CTA owns digit d
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kTileItems = 4;                          // items a thread holds in the many-CTA sort
+constexpr int kTile = kSortThreads * kTileItems;       // 2048 positions a CTA
+constexpr int kOneItems = 8;                           // items a thread holds when one CTA sorts all
+constexpr int kOneTile = kSortThreads * kOneItems;     // 4096 positions
+
+struct Pair {
+    uint32_t key;
+    uint32_t pos;
+};
+
+__device__ __forceinline__ uint32_t sort_key(int32_t id, int64_t vocab) {
+    return id >= 0 && id < vocab ? (uint32_t)id : (uint32_t)vocab;
+}
+__device__ __forceinline__ int digit_of(uint32_t key, int pass) { return (key >> (pass * kDigitBits)) & (kDigits - 1); }
+
+// Rank of every item among the tile's items of the same digit, in tile order (warp w holds items
+// w * 32 * ITEMS .. , round by round), and the tile's count of digit threadIdx.x. count: [kSortWarps][kDigits].
+template <int ITEMS>
+__device__ __forceinline__ int tile_ranks(const Pair (&item)[ITEMS], const bool (&live)[ITEMS], int pass, int* count, int (&rank)[ITEMS]) {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    for (int w = 0; w < kSortWarps; ++w) count[w * kDigits + threadIdx.x] = 0;
+    __syncthreads();
+    int* mine = count + warp * kDigits;
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        const int d = live[k] ? digit_of(item[k].key, pass) : kDigits + lane;  // an absent item matches none
+        const unsigned same = __match_any_sync(0xffffffffu, d);
+        int before = 0;
+        if (live[k]) before = mine[d];
+        __syncwarp();
+        rank[k] = before + __popc(same & ((1u << lane) - 1));
+        if (live[k] && lane == 31 - __clz(same)) mine[d] = before + __popc(same);
+        __syncwarp();
+    }
+    __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) {
+        const int c = count[w * kDigits + threadIdx.x];
+        count[w * kDigits + threadIdx.x] = total;
+        total += c;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k)
+        if (live[k]) rank[k] += mine[digit_of(item[k].key, pass)];
+    return total;
+}
+
+// Exclusive sum over the CTA's kSortThreads threads.
+__device__ __forceinline__ int block_exclusive(int v, int* warp_sums) {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    int inc = v;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const int up = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += up;
+    }
+    if (lane == 31) warp_sums[warp] = inc;
+    __syncthreads();
+    int base = 0;
+    for (int w = 0; w < warp; ++w) base += warp_sums[w];
+    __syncthreads();
+    return base + inc - v;
+}
+
+// Up to kOneTile positions: all passes in the shared memory of one CTA.
+__global__ void __launch_bounds__(kSortThreads) k_sort_one(const int32_t* __restrict__ ids, int n, int64_t vocab, int passes, Pair* __restrict__ out) {
+    static_assert(sizeof(Pair) * kOneTile <= sizeof(int) * kSortWarps * kDigits, "the pairs reuse the counters' space");
+    __shared__ __align__(16) int count[kSortWarps * kDigits];
+    Pair* pairs = reinterpret_cast<Pair*>(count);  // the counters are done with when the pairs move
+    __shared__ int base[kDigits];
+    __shared__ int warp_sums[kSortWarps];
+    const int first = (threadIdx.x / 32) * 32 * kOneItems + threadIdx.x % 32;
+    Pair item[kOneItems];
+    bool live[kOneItems];
+#pragma unroll
+    for (int k = 0; k < kOneItems; ++k) {
+        const int i = first + 32 * k;
+        live[k] = i < n;
+        item[k] = live[k] ? Pair{sort_key(ids[i], vocab), (uint32_t)i} : Pair{0, 0};
+    }
+    for (int pass = 0; pass < passes; ++pass) {
+        int rank[kOneItems];
+        const int total = tile_ranks<kOneItems>(item, live, pass, count, rank);
+        base[threadIdx.x] = block_exclusive(total, warp_sums);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kOneItems; ++k)
+            if (live[k]) pairs[base[digit_of(item[k].key, pass)] + rank[k]] = item[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kOneItems; ++k)
+            if (live[k]) item[k] = pairs[first + 32 * k];
+        __syncthreads();
+    }
+#pragma unroll
+    for (int k = 0; k < kOneItems; ++k)
+        if (live[k]) out[first + 32 * k] = item[k];
+}
+
+// Counts of the first digit, per tile of kTile positions.
+__global__ void __launch_bounds__(kSortThreads) k_sort_count(const int32_t* __restrict__ ids, int64_t n, int64_t vocab, int* __restrict__ counts) {
+    __shared__ int c[kDigits];
+    c[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t first = (int64_t)blockIdx.x * kTile;
+    for (int64_t i = first + threadIdx.x; i < min(first + kTile, n); i += kSortThreads) atomicAdd(&c[digit_of(sort_key(ids[i], vocab), 0)], 1);
+    __syncthreads();
+    counts[(int64_t)blockIdx.x * kDigits + threadIdx.x] = c[threadIdx.x];
+}
+
+// One pass: every tile adds up where its items go from the counts of all tiles, moves them, and counts the next
+// digit of the tiles they land in (integer sums: the order of the atomics does not show).
+__global__ void __launch_bounds__(kSortThreads) k_sort_pass(const int32_t* __restrict__ ids, const Pair* __restrict__ in, int64_t n, int64_t vocab,
+                                                            int pass, bool last, const int* __restrict__ counts, int n_tiles,
+                                                            Pair* __restrict__ out, int* __restrict__ next_counts) {
+    __shared__ int count[kSortWarps * kDigits];
+    __shared__ int base[kDigits];
+    __shared__ int warp_sums[kSortWarps];
+    const int64_t first = (int64_t)blockIdx.x * kTile + (threadIdx.x / 32) * 32 * kTileItems + threadIdx.x % 32;
+    Pair item[kTileItems];
+    bool live[kTileItems];
+#pragma unroll
+    for (int k = 0; k < kTileItems; ++k) {
+        const int64_t i = first + 32 * k;
+        live[k] = i < n;
+        item[k] = Pair{0, 0};
+        if (live[k]) item[k] = in ? in[i] : Pair{sort_key(ids[i], vocab), (uint32_t)i};
+    }
+    int before = 0, all = 0;
+#pragma unroll 8
+    for (int t = 0; t < n_tiles; ++t) {
+        const int c = counts[(int64_t)t * kDigits + threadIdx.x];
+        all += c;
+        before += t < (int)blockIdx.x ? c : 0;
+    }
+    base[threadIdx.x] = block_exclusive(all, warp_sums) + before;
+    int rank[kTileItems];
+    tile_ranks<kTileItems>(item, live, pass, count, rank);  // its barriers also publish base
+#pragma unroll
+    for (int k = 0; k < kTileItems; ++k) {
+        if (!live[k]) continue;
+        const int64_t to = (int64_t)base[digit_of(item[k].key, pass)] + rank[k];
+        out[to] = item[k];
+        if (!last) atomicAdd(&next_counts[(to / kTile) * kDigits + digit_of(item[k].key, pass + 1)], 1);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Sums over the sorted positions. A group of threads takes a block of `span` sorted positions and a range of
+// columns; an id whose positions all lie in the block is finished there. What an id has in a block that it
+// enters or leaves half-way goes to `partial` ([block][2][width]: the id the block begins with, the id it ends
+// with), and k_join adds those up, block by block. Further CTAs of the same launch write the rows of ids that
+// have no position.
+// ---------------------------------------------------------------------------------------------
+constexpr int kAhead = 8;  // rows in flight a thread
+
+template <class T, int VEC>
+__device__ __forceinline__ void finish_row(T* row, const float (&sum)[VEC], float scale, bool accumulate) {
+    Pack<T, VEC> o;
+    if (accumulate) o = *reinterpret_cast<Pack<T, VEC>*>(row);
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) o.v[k] = narrow<T>(accumulate ? widen(o.v[k]) + scale * sum[k] : scale * sum[k]);
+    *reinterpret_cast<Pack<T, VEC>*>(row) = o;
+}
+
+constexpr int kZeroRows = 64;  // ids a CTA looks through for ones without a position
+
+template <class T, int VEC>
+__global__ void __launch_bounds__(kThreads) k_segments(const T* __restrict__ grad_out, int64_t grad_pitch, const Pair* __restrict__ sorted, int64_t n,
+                                                       int64_t vocab, int64_t width, float scale, bool accumulate, T* __restrict__ table,
+                                                       int64_t table_pitch, float* __restrict__ partial, int span, int group, int64_t sum_ctas) {
+    const int64_t c = ((int64_t)blockIdx.y * group + threadIdx.x % group) * VEC;
+    if ((int64_t)blockIdx.x >= sum_ctas) {  // rows without a position
+        __shared__ unsigned char used[kZeroRows];
+        const int64_t v0 = ((int64_t)blockIdx.x - sum_ctas) * kZeroRows;
+        const int64_t v1 = min(v0 + kZeroRows, vocab);
+        if (threadIdx.x < v1 - v0) {  // every thread looks one id up
+            const uint32_t v = (uint32_t)(v0 + threadIdx.x);
+            int64_t a = 0, b = n;
+            while (a < b) {
+                const int64_t mid = (a + b) / 2;
+                if (sorted[mid].key < v) a = mid + 1;
+                else b = mid;
+            }
+            used[threadIdx.x] = a < n && sorted[a].key == v;
+        }
+        __syncthreads();
+        Pack<T, VEC> zero;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) zero.v[k] = narrow<T>(0.0f);
+        if (c < width)
+            for (int64_t v = v0 + threadIdx.x / group; v < v1; v += kThreads / group)
+                if (!used[v - v0]) *reinterpret_cast<Pack<T, VEC>*>(table + v * table_pitch + c) = zero;
+        return;
+    }
+    const int64_t block = (int64_t)blockIdx.x * (kThreads / group) + threadIdx.x / group;
+    const int64_t p0 = block * span, p1 = min(p0 + span, n);
+    if (p0 >= n || c >= width) return;
+    const uint32_t head = p0 > 0 ? sorted[p0 - 1].key : 0xffffffffu;  // an id equal to it began in an earlier block
+    const uint32_t tail = p1 < n ? sorted[p1].key : 0xffffffffu;      // an id equal to it goes on in the next block
+    float sum[VEC] = {};
+    uint32_t key = sorted[p0].key;
+    auto flush = [&]() {
+        if (key >= (uint32_t)vocab) return;  // no token
+        const bool enters = key == head, leaves = key == tail;
+        if (!enters && !leaves) {
+            finish_row<T, VEC>(table + (int64_t)key * table_pitch + c, sum, scale, accumulate);
+        } else {
+            float* to = partial + (block * 2 + (enters ? 0 : 1)) * width + c;
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) to[k] = sum[k];
+        }
+    };
+    for (int64_t p = p0; p < p1; p += kAhead) {
+        Pair at[kAhead];
+        Pack<T, VEC> row[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (p + k < p1) at[k] = sorted[p + k];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (p + k < p1 && at[k].key < (uint32_t)vocab)
+                row[k] = *reinterpret_cast<const Pack<T, VEC>*>(grad_out + (int64_t)at[k].pos * grad_pitch + c);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (p + k >= p1) break;
+            if (at[k].key != key) {
+                flush();
+                key = at[k].key;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
+            }
+            if (key >= (uint32_t)vocab) continue;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum[e] += widen(row[k].v[e]);
+        }
+    }
+    flush();
+}
+
+// The ids that lie in more than one block: the group of the block where such an id begins adds up its parts in
+// block order.
+template <class T, int VEC>
+__global__ void __launch_bounds__(kThreads) k_join(const Pair* __restrict__ sorted, int64_t n, int64_t vocab, int64_t width, float scale,
+                                                   bool accumulate, T* __restrict__ table, int64_t table_pitch,
+                                                   const float* __restrict__ partial, int span, int group) {
+    const int64_t block = (int64_t)blockIdx.x * (kThreads / group) + threadIdx.x / group;
+    const int64_t c = ((int64_t)blockIdx.y * group + threadIdx.x % group) * VEC;
+    const int64_t p0 = block * span, p1 = p0 + span;
+    if (p1 >= n || c >= width) return;  // the last block's ids end in it
+    const uint32_t key = sorted[p1 - 1].key;
+    if (key >= (uint32_t)vocab || sorted[p1].key != key) return;  // ends here
+    if (p0 > 0 && sorted[p0 - 1].key == key) return;              // began earlier
+    float sum[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) sum[k] = partial[(block * 2 + 1) * width + c + k];
+    for (int64_t b = block + 1; b * span < n && sorted[b * span].key == key; ++b)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) sum[k] += partial[b * 2 * width + c + k];
+    finish_row<T, VEC>(table + (int64_t)key * table_pitch + c, sum, scale, accumulate);
+}
+
+int sort_passes(int64_t vocab) {  // keys are 0 .. vocab
+    int passes = 1;
+    while (passes * kDigitBits < 32 && (vocab >> (passes * kDigitBits)) != 0) ++passes;
+    return passes;
+}
+
+// Sorted positions one group sums up: small, so that short inputs still fill the GPU.
+int segment_span(int64_t n_ids) { return n_ids <= 16384 ? 16 : 64; }
+
+struct GradPlan {
+    Pair* sorted;
+    Pair* other;
+    int* counts;
+    float* partial;
+    int64_t n_tiles;
+    int passes;
+};
+
+int64_t grad_layout(int64_t vocab, int64_t width, int64_t n_ids, void* workspace, GradPlan* out) {
+    GradPlan p{};
+    Carver w(workspace);
+    p.passes = sort_passes(vocab);
+    p.n_tiles = ceil_div(n_ids, kTile);
+    p.sorted = w.take<Pair>(n_ids);
+    if (n_ids > kOneTile) {
+        p.other = w.take<Pair>(n_ids);
+        p.counts = w.take<int>(p.passes * p.n_tiles * kDigits);
+    }
+    p.partial = w.take<float>(ceil_div(n_ids, segment_span(n_ids)) * 2 * width);
+    if (out) *out = p;
+    return w.used;
+}
+
+template <class T, int VEC>
+cudaError_t segments_typed(const EmbedGradArgs& a, const GradPlan& p, cudaStream_t s) {
+    const int span = segment_span(a.n_ids);
+    const int group = group_threads(a.width, VEC);
+    const int64_t per_cta = kThreads / group;
+    const int64_t blocks = ceil_div(a.n_ids, span);
+    const int64_t col_ctas = ceil_div(a.width, (int64_t)group * VEC);
+    auto* g = static_cast<const T*>(a.grad_out);
+    auto* table = static_cast<T*>(a.grad_table);
+    const int64_t sum_ctas = ceil_div(blocks, per_cta);
+    const int64_t zero_ctas = a.accumulate ? 0 : ceil_div(a.vocab, kZeroRows);
+    if (sum_ctas + zero_ctas > 0)
+        k_segments<T, VEC><<<dim3((unsigned)(sum_ctas + zero_ctas), (unsigned)col_ctas), kThreads, 0, s>>>(
+            g, a.grad_out_pitch, p.sorted, a.n_ids, a.vocab, a.width, a.scale, a.accumulate, table, a.grad_table_pitch, p.partial, span,
+            group, sum_ctas);
+    if (blocks > 1)
+        k_join<T, VEC><<<dim3((unsigned)sum_ctas, (unsigned)col_ctas), kThreads, 0, s>>>(p.sorted, a.n_ids, a.vocab, a.width, a.scale,
+                                                                                         a.accumulate, table, a.grad_table_pitch, p.partial,
+                                                                                         span, group);
+    return cudaGetLastError();
+}
+
+template <class T>
+cudaError_t grad_typed(const EmbedGradArgs& a, const GradPlan& p, cudaStream_t s) {
+    constexpr int kVec = 16 / sizeof(T);
+    const bool wide =
+        a.width % kVec == 0 && aligned16(a.grad_out, a.grad_out_pitch, sizeof(T)) && aligned16(a.grad_table, a.grad_table_pitch, sizeof(T));
+    return wide ? segments_typed<T, kVec>(a, p, s) : segments_typed<T, 1>(a, p, s);
+}
+
+}  // namespace
+
+cudaError_t run_embed(const EmbedArgs& a, cudaStream_t s) {
+    if (a.n_ids == 0) return cudaSuccess;
+    return a.dtype == A2_BF16 ? embed_typed<__nv_bfloat16>(a, s) : embed_typed<float>(a, s);
+}
+
+int64_t embed_grad_workspace(int64_t vocab, int64_t width, int64_t n_ids) { return grad_layout(vocab, width, n_ids, nullptr, nullptr); }
+
+cudaError_t run_embed_grad(const EmbedGradArgs& a, void* workspace, cudaStream_t s) {
+    GradPlan p;
+    grad_layout(a.vocab, a.width, a.n_ids, workspace, &p);
+    if (a.n_ids > kOneTile) {
+        cudaError_t e = cudaMemsetAsync(p.counts, 0, sizeof(int) * (size_t)(p.passes * p.n_tiles * kDigits), s);
+        if (e != cudaSuccess) return e;
+        k_sort_count<<<(unsigned)p.n_tiles, kSortThreads, 0, s>>>(a.ids, a.n_ids, a.vocab, p.counts);
+        // the passes go back and forth between the two buffers and end in p.sorted
+        Pair* from = nullptr;
+        for (int pass = 0; pass < p.passes; ++pass) {
+            Pair* to = (p.passes - pass) % 2 == 1 ? p.sorted : p.other;
+            const int* counts = p.counts + (int64_t)pass * p.n_tiles * kDigits;
+            const bool last = pass + 1 == p.passes;
+            k_sort_pass<<<(unsigned)p.n_tiles, kSortThreads, 0, s>>>(a.ids, from, a.n_ids, a.vocab, pass, last, counts, (int)p.n_tiles, to,
+                                                                     last ? nullptr : p.counts + (int64_t)(pass + 1) * p.n_tiles * kDigits);
+            from = to;
+        }
+    } else if (a.n_ids > 0) {
+        k_sort_one<<<1, kSortThreads, 0, s>>>(a.ids, (int)a.n_ids, a.vocab, p.passes, p.sorted);
+    }
+    return a.dtype == A2_BF16 ? grad_typed<__nv_bfloat16>(a, p, s) : grad_typed<float>(a, p, s);
+}
+
+}  // namespace a2
