@@ -109,6 +109,7 @@ SIGNATURES = {
     "a2cid2_orthogonalize_workspace": (C.c_int, [_i64, _i64, _i64, C.c_int32, _lp]),
     "a2cid2_orthogonalize": (C.c_int, [_vp, _i64, _i64, _i64, _i64, _i64, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double,
                                        C.c_double, _vp, _i64, _i64, C.c_int32, _vp, _i64, _vp]),
+    "a2cid2_operators_check": (C.c_int, [_vp]),
     "a2cid2_version": (C.c_char_p, []),
 }
 

@@ -1,0 +1,91 @@
+// Host side of the tensor-core products: tensor maps, launch shape, the flag of kernels that gave up a wait.
+#include "gemm_sm100.cuh"
+
+namespace a2 {
+
+namespace {
+
+__device__ int g_gave_up;
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encoder() {
+    static const EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+
+// Boxes of 64 x `box_rows` (128 bytes a row) of a [mats][rows][inner] array of 16-bit elements.
+cudaError_t make_map(const void* p, bool bf16, int64_t inner, int64_t rows, int64_t pitch, int64_t mats, int64_t stride, int box_rows, CUtensorMap* out) {
+    const EncodeTiled encode = encoder();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)mats};
+    const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)(mats > 1 ? stride : pitch * rows) * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, one[3] = {1, 1, 1};
+    const CUresult r = encode(out, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(p), dims, strides,
+                              box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+cudaError_t operand_maps(const Operand& o, bool bf16, int64_t mats, CUtensorMap (&out)[2]) {
+    const int64_t inner = o.mn ? o.rows : o.k, rows = o.mn ? o.k : o.rows;
+    for (int w = 0; w < 2; ++w) {
+        const void* p = w && o.lo ? o.lo : o.p;
+        const cudaError_t e = make_map(p, bf16, inner, rows, o.pitch, mats, o.stride, o.mn ? kBlockK : 128, &out[w]);
+        if (e != cudaSuccess) return e;
+        if (!o.lo) {
+            out[1] = out[0];
+            break;
+        }
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
+int gemm_clusters() {
+    int device = 0, sms = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 1;
+    return sms >= 2 ? sms / 2 : 1;
+}
+
+cudaError_t make_gemm(const Operand& a, const Operand& b, int64_t mats, bool bf16, bool lower, int flush, GemmArgs* g) {
+    cudaError_t e = operand_maps(a, bf16, mats, g->a);
+    if (e == cudaSuccess) e = operand_maps(b, bf16, mats, g->b);
+    if (e != cudaSuccess) return e;
+    void* flag = nullptr;
+    e = cudaGetSymbolAddress(&flag, g_gave_up);
+    if (e != cudaSuccess) return e;
+    g->gave_up = static_cast<int*>(flag);
+    g->tiles_m = (int32_t)ceil_div(a.rows, kTileM);
+    g->tiles_n = (int32_t)ceil_div(b.rows, kTileN);
+    g->batch = (int32_t)mats;
+    g->k_blocks = (int32_t)ceil_div(a.k, kBlockK);
+    g->passes = a.lo ? 3 : 1;
+    g->flush = flush > 0 ? flush : g->k_blocks * g->passes;
+    // fp32 sums; fp16 (0) or bf16 (1) operands; MN-major bits; N / 8 and M / 16
+    g->idesc = 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (a.mn ? 1u : 0u) << 15 | (b.mn ? 1u : 0u) << 16 |
+               (uint32_t)(kTileN / 8) << 17 | (uint32_t)(kTileM / 16) << 24;
+    g->a_mn = a.mn;
+    g->b_mn = b.mn;
+    g->lower = lower;
+    return cudaSuccess;
+}
+
+cudaError_t products_gave_up(cudaStream_t s, bool* out) {
+    int v = 0;
+    cudaError_t e = cudaStreamSynchronize(s);
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&v, g_gave_up, sizeof v);
+    *out = v != 0;
+    return e;
+}
+
+}  // namespace a2

@@ -183,6 +183,8 @@ int a2cid2_orthogonalize(const void* in, int64_t in_stride, int64_t in_pitch, in
     A2_TRY(check_number("c", c));
     A2_TRY(check_number("scale", scale));
     A2_CHECK(std::isfinite(eps) && eps >= 0, A2_EINVAL, "need eps >= 0");
+    double center;
+    A2_CHECK(a2::orthogonalize_range(a, b, c, steps, &center), A2_EINVAL, "the coefficients take singular values of [0, 1] beyond 1.95");
     A2_TRY(check_matrix("in", in, n_mats, cols, in_pitch, storage_dtype));
     A2_TRY(check_matrix("out", out, n_mats, cols, out_pitch, storage_dtype));
     // matrices of a batch may not share elements: a matrix takes (rows - 1) * pitch + cols of them
@@ -193,9 +195,16 @@ int a2cid2_orthogonalize(const void* in, int64_t in_stride, int64_t in_pitch, in
              "in place needs the same stride and pitch on both sides");
     A2_TRY(check_workspace(workspace, workspace_bytes, a2::orthogonalize_workspace(n_mats, rows, cols, storage_dtype)));
     if (n_mats == 0) return A2_OK;
-    const a2::OrthogonalizeArgs args{in, in_stride, in_pitch, n_mats, rows, cols, steps, (float)a, (float)b, (float)c, eps, (float)scale, out,
+    const a2::OrthogonalizeArgs args{in, in_stride, in_pitch, n_mats, rows, cols, steps, (float)a, (float)b, (float)c, (float)center, eps, (float)scale, out,
                                      out_stride, out_pitch, storage_dtype};
     return status(a2::run_orthogonalize(args, workspace, (cudaStream_t)cuda_stream), "orthogonalisation");
+}
+
+int a2cid2_operators_check(void* cuda_stream) {
+    bool gave_up = false;
+    A2_TRY(status(a2::products_gave_up((cudaStream_t)cuda_stream, &gave_up), "operators check"));
+    A2_CHECK(!gave_up, A2_ECUDA, "a product gave up waiting for its operands: results since the start of the process may be incomplete");
+    return A2_OK;
 }
 
 }  // extern "C"

@@ -79,14 +79,20 @@ struct OrthogonalizeArgs {
     int64_t n_mats, rows, cols;
     int32_t steps;
     float ca, cb, cc;
+    float center;  // of orthogonalize_range
     double eps;
     float scale;
     void* out;
     int64_t out_stride, out_pitch;
     int32_t dtype;
 };
+// Whether the steps keep singular values of [0, 1], and the polynomial, inside what the fp16 intermediates hold; the
+// polynomial's middle.
+bool orthogonalize_range(double a, double b, double c, int steps, double* center);
 int64_t orthogonalize_workspace(int64_t n_mats, int64_t rows, int64_t cols, int32_t dtype);
 cudaError_t run_orthogonalize(const OrthogonalizeArgs& a, void* workspace, cudaStream_t s);
+
+cudaError_t products_gave_up(cudaStream_t s, bool* out);  // waits for the stream; whether a product ever gave up on this device
 
 #ifdef __CUDACC__
 __device__ __forceinline__ float widen(float v) { return v; }

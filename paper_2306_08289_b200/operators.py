@@ -151,3 +151,9 @@ def orthogonalize(mats, steps=5, coeffs=NEWTON_SCHULZ, eps=1e-7, scale=1.0, out=
         B._check(B.lib().a2cid2_orthogonalize(mats.data_ptr(), mats.stride(0), pitch, n, rows, cols, steps, *coeffs, eps, scale, out.data_ptr(),
                                               out.stride(0), out_pitch, dtype, ws.data_ptr(), size, s))
     return out
+
+
+def check(stream=None):
+    """Waits for the stream (torch's current one if None) and raises `binding.A2Error` if a kernel of the products ever gave up a wait
+    on the current device."""
+    B._check(B.lib().a2cid2_operators_check((torch.cuda.current_stream() if stream is None else stream).cuda_stream))

@@ -424,6 +424,7 @@ def test_refusals():
                  lambda: ops.vocab_loss_grad(t, t, ids, weights=torch.ones(10, device=DEV, dtype=torch.float64)),
                  lambda: ops.vocab_loss_grad(t, t, ids, grad_head=t[:5]), lambda: ops.vocab_loss_grad(t, t, ids, scale=math.inf),
                  lambda: ops.orthogonalize(t, steps=-1), lambda: ops.orthogonalize(t, eps=-1.0), lambda: ops.orthogonalize(t, coeffs=(1, math.nan, 0)),
+                 lambda: ops.orthogonalize(t, coeffs=(3.0, 0.0, 0.0)), lambda: ops.orthogonalize(t, coeffs=(1.0, -9.0, 1.0)),
                  lambda: ops.orthogonalize(t[None].expand(3, 10, 8)), lambda: ops.orthogonalize(t[None, None]), lambda: ops.orthogonalize(t.T)):
         with pytest.raises(B.A2Error) as e:
             call()
@@ -452,3 +453,4 @@ def test_rows_of_an_engine_train_a_language_model():
         trace, entropy = language_model.train(n=4, vocab=64, width=32, T=40.0, storage=storage, sequences=8, length=16, samples=2)
         assert trace[0][1] > 0.9 * math.log(64) and trace[-1][1] < 0.5 * (entropy + math.log(64)), (trace, entropy)
         assert all(math.isfinite(v) for row in trace for v in row)
+    ops.check()
