@@ -449,7 +449,7 @@ int a2cid2_orthogonalize_workspace(int64_t n_mats, int64_t rows, int64_t cols, i
  * out = scale * X. Matrix k of the batch starts at in + k * in_stride elements: with one matrix per worker's row, the stride is
  * the row pitch. out == in with the same stride and pitch is allowed. eps >= 0; a zero matrix gives zeros (also with eps = 0).
  * n_mats = 0 does nothing; steps = 0 normalises. The coefficients must keep singular values of [0, 1] below 1.95 over the steps
- * and b s + c s^2 within a range of 7.8 there (A2_EINVAL otherwise): the intermediates are fp16 words, one with bf16 rows
+ * and |a + b s^2 + c s^4| below 3.9 there (A2_EINVAL otherwise): the intermediates are fp16 words, one with bf16 rows
  * (11 bits), two with fp32 rows (22 bits). A matrix that holds a NaN or an infinity becomes all NaN, the others of the batch are not
  * touched by it. */
 int a2cid2_orthogonalize(const void* in, int64_t in_stride, int64_t in_pitch, int64_t n_mats, int64_t rows, int64_t cols,

@@ -28,6 +28,7 @@ template <class T, int VEC>
 __global__ void __launch_bounds__(kThreads) k_embed(const T* __restrict__ table, int64_t vocab, int64_t width, int64_t table_pitch,
                                                     const int32_t* __restrict__ ids, int64_t n_ids, float scale,
                                                     T* __restrict__ out, int64_t out_pitch, int group) {
+    ptx::chained();
     const int lane = threadIdx.x % group;
     const int64_t first = ((int64_t)blockIdx.x * (kThreads / group) + threadIdx.x / group) * kRows;
     int64_t id[kRows];
@@ -61,10 +62,10 @@ cudaError_t embed_typed(const EmbedArgs& a, cudaStream_t s) {
     auto* table = static_cast<const T*>(a.table);
     auto* out = static_cast<T*>(a.out);
     if (wide)
-        k_embed<T, kVec><<<(unsigned)grid, kThreads, 0, s>>>(table, a.vocab, a.width, a.table_pitch, a.ids, a.n_ids, a.scale, out,
+        launch_chained(k_embed<T, kVec>, dim3((unsigned)grid), kThreads, 0, s, table, a.vocab, a.width, a.table_pitch, a.ids, a.n_ids, a.scale, out,
                                                              a.out_pitch, group);
     else
-        k_embed<T, 1><<<(unsigned)grid, kThreads, 0, s>>>(table, a.vocab, a.width, a.table_pitch, a.ids, a.n_ids, a.scale, out,
+        launch_chained(k_embed<T, 1>, dim3((unsigned)grid), kThreads, 0, s, table, a.vocab, a.width, a.table_pitch, a.ids, a.n_ids, a.scale, out,
                                                           a.out_pitch, group);
     return cudaGetLastError();
 }
@@ -78,10 +79,8 @@ constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kSortThreads = kDigits;  // thread d of a sorting CTA owns digit d
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kTileItems = 4;                          // items a thread holds in the many-CTA sort
-constexpr int kTile = kSortThreads * kTileItems;       // 2048 positions a CTA
-constexpr int kOneItems = 8;                           // items a thread holds when one CTA sorts all
-constexpr int kOneTile = kSortThreads * kOneItems;     // 4096 positions
+constexpr int kTileItems = 4;                     // items a thread holds
+constexpr int kTile = kSortThreads * kTileItems;  // 2048 positions a CTA
 
 struct Pair {
     uint32_t key;
@@ -144,50 +143,17 @@ __device__ __forceinline__ int block_exclusive(int v, int* warp_sums) {
     return base + inc - v;
 }
 
-// Up to kOneTile positions: all passes in the shared memory of one CTA.
-__global__ void __launch_bounds__(kSortThreads) k_sort_one(const int32_t* __restrict__ ids, int n, int64_t vocab, int passes, Pair* __restrict__ out) {
-    static_assert(sizeof(Pair) * kOneTile <= sizeof(int) * kSortWarps * kDigits, "the pairs reuse the counters' space");
-    __shared__ __align__(16) int count[kSortWarps * kDigits];
-    Pair* pairs = reinterpret_cast<Pair*>(count);  // the counters are done with when the pairs move
-    __shared__ int base[kDigits];
-    __shared__ int warp_sums[kSortWarps];
-    const int first = (threadIdx.x / 32) * 32 * kOneItems + threadIdx.x % 32;
-    Pair item[kOneItems];
-    bool live[kOneItems];
-#pragma unroll
-    for (int k = 0; k < kOneItems; ++k) {
-        const int i = first + 32 * k;
-        live[k] = i < n;
-        item[k] = live[k] ? Pair{sort_key(ids[i], vocab), (uint32_t)i} : Pair{0, 0};
-    }
-    for (int pass = 0; pass < passes; ++pass) {
-        int rank[kOneItems];
-        const int total = tile_ranks<kOneItems>(item, live, pass, count, rank);
-        base[threadIdx.x] = block_exclusive(total, warp_sums);
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kOneItems; ++k)
-            if (live[k]) pairs[base[digit_of(item[k].key, pass)] + rank[k]] = item[k];
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kOneItems; ++k)
-            if (live[k]) item[k] = pairs[first + 32 * k];
-        __syncthreads();
-    }
-#pragma unroll
-    for (int k = 0; k < kOneItems; ++k)
-        if (live[k]) out[first + 32 * k] = item[k];
-}
-
 // Counts of the first digit, per tile of kTile positions.
-__global__ void __launch_bounds__(kSortThreads) k_sort_count(const int32_t* __restrict__ ids, int64_t n, int64_t vocab, int* __restrict__ counts) {
+__global__ void __launch_bounds__(kSortThreads) k_sort_count(const int32_t* __restrict__ ids, int64_t n, int64_t vocab, int passes, int* __restrict__ counts) {
+    ptx::chained();
     __shared__ int c[kDigits];
     c[threadIdx.x] = 0;
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * kTile;
     for (int64_t i = first + threadIdx.x; i < min(first + kTile, n); i += kSortThreads) atomicAdd(&c[digit_of(sort_key(ids[i], vocab), 0)], 1);
     __syncthreads();
-    counts[(int64_t)blockIdx.x * kDigits + threadIdx.x] = c[threadIdx.x];
+    for (int p = 0; p < passes; ++p)  // the later passes' counts are added up by the pass before
+        counts[((int64_t)p * gridDim.x + blockIdx.x) * kDigits + threadIdx.x] = p == 0 ? c[threadIdx.x] : 0;
 }
 
 // One pass: every tile adds up where its items go from the counts of all tiles, moves them, and counts the next
@@ -195,6 +161,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(const int32_t* __re
 __global__ void __launch_bounds__(kSortThreads) k_sort_pass(const int32_t* __restrict__ ids, const Pair* __restrict__ in, int64_t n, int64_t vocab,
                                                             int pass, bool last, const int* __restrict__ counts, int n_tiles,
                                                             Pair* __restrict__ out, int* __restrict__ next_counts) {
+    ptx::chained();
     __shared__ int count[kSortWarps * kDigits];
     __shared__ int base[kDigits];
     __shared__ int warp_sums[kSortWarps];
@@ -251,6 +218,7 @@ template <class T, int VEC>
 __global__ void __launch_bounds__(kThreads) k_segments(const T* __restrict__ grad_out, int64_t grad_pitch, const Pair* __restrict__ sorted, int64_t n,
                                                        int64_t vocab, int64_t width, float scale, bool accumulate, T* __restrict__ table,
                                                        int64_t table_pitch, float* __restrict__ partial, int span, int group, int64_t sum_ctas) {
+    ptx::chained();
     const int64_t c = ((int64_t)blockIdx.y * group + threadIdx.x % group) * VEC;
     if ((int64_t)blockIdx.x >= sum_ctas) {  // rows without a position
         __shared__ unsigned char used[kZeroRows];
@@ -326,6 +294,7 @@ template <class T, int VEC>
 __global__ void __launch_bounds__(kThreads) k_join(const Pair* __restrict__ sorted, int64_t n, int64_t vocab, int64_t width, float scale,
                                                    bool accumulate, T* __restrict__ table, int64_t table_pitch,
                                                    const float* __restrict__ partial, int span, int group) {
+    ptx::chained();
     const int64_t block = (int64_t)blockIdx.x * (kThreads / group) + threadIdx.x / group;
     const int64_t c = ((int64_t)blockIdx.y * group + threadIdx.x % group) * VEC;
     const int64_t p0 = block * span, p1 = p0 + span;
@@ -333,13 +302,140 @@ __global__ void __launch_bounds__(kThreads) k_join(const Pair* __restrict__ sort
     const uint32_t key = sorted[p1 - 1].key;
     if (key >= (uint32_t)vocab || sorted[p1].key != key) return;  // ends here
     if (p0 > 0 && sorted[p0 - 1].key == key) return;              // began earlier
+    // the blocks that begin with this id follow one another; eight loads at a time, first of keys, then of sums
+    int64_t end = block + 1;
+    for (bool more = true; more;) {
+        uint32_t k[8];
+#pragma unroll
+        for (int a = 0; a < 8; ++a) k[a] = (end + a) * span < n ? sorted[(end + a) * span].key : 0xffffffffu;
+#pragma unroll
+        for (int a = 0; a < 8; ++a) {
+            more = more && k[a] == key;
+            end += more;
+        }
+    }
     float sum[VEC];
 #pragma unroll
     for (int k = 0; k < VEC; ++k) sum[k] = partial[(block * 2 + 1) * width + c + k];
-    for (int64_t b = block + 1; b * span < n && sorted[b * span].key == key; ++b)
+#pragma unroll 8
+    for (int64_t b = block + 1; b < end; ++b)
 #pragma unroll
         for (int k = 0; k < VEC; ++k) sum[k] += partial[b * 2 * width + c + k];
     finish_row<T, VEC>(table + (int64_t)key * table_pitch + c, sum, scale, accumulate);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Few positions: no sort. A CTA a position looks through all ids for its own: if the position is the first of its id, the
+// CTA lists the others in order and adds their rows up. n * n comparisons are less work than the launches of a sort up to a few
+// thousand positions. Further CTAs write the rows of ids that have none.
+// ---------------------------------------------------------------------------------------------
+constexpr int kDirectMost = 4096;
+constexpr int kDirectThreads = 256;
+constexpr int kDirectRounds = kDirectMost / kDirectThreads;
+
+template <class T, int VEC>
+__global__ void __launch_bounds__(kDirectThreads) k_direct(const T* __restrict__ grad_out, int64_t grad_pitch, const int32_t* __restrict__ ids, int n,
+                                                           int64_t vocab, int64_t width, float scale, bool accumulate, T* __restrict__ table,
+                                                           int64_t table_pitch, int group) {
+    ptx::chained();
+    __shared__ uint16_t list[kDirectMost];
+    __shared__ int counts[129];
+    __shared__ float joined[kDirectThreads * VEC];
+    const int tid = threadIdx.x, lane = tid % group, slot = tid / group, slots = kDirectThreads / group;
+    if ((int)blockIdx.x >= n) {  // rows without a position: flags of kZeroRows ids, in the list's space
+        const int64_t v0 = ((int64_t)blockIdx.x - n) * kZeroRows;
+        if (tid < kZeroRows) list[tid] = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += kDirectThreads) {
+            const int64_t v = ids[i] - v0;
+            if (v >= 0 && v < kZeroRows) list[v] = 1;
+        }
+        __syncthreads();
+        Pack<T, VEC> zero;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) zero.v[k] = narrow<T>(0.0f);
+        for (int64_t v = slot; v < kZeroRows && v0 + v < vocab; v += slots)
+            if (!list[v])
+                for (int64_t c = (int64_t)lane * VEC; c < width; c += (int64_t)group * VEC)
+                    *reinterpret_cast<Pack<T, VEC>*>(table + (v0 + v) * table_pitch + c) = zero;
+        return;
+    }
+    const int me = blockIdx.x;
+    const int32_t id = ids[me];
+    if (id < 0 || id >= vocab) return;
+    // round k of a thread is position k * kDirectThreads + tid
+    uint32_t found = 0;
+    bool earlier = false;
+#pragma unroll
+    for (int k = 0; k < kDirectRounds; ++k) {
+        const int p = k * kDirectThreads + tid;
+        const bool hit = p < n && ids[p] == id;
+        found |= (hit ? 1u : 0u) << k;
+        earlier |= hit && p < me;
+    }
+    if (__syncthreads_or(earlier)) return;  // an earlier position does this id
+    // list them in order: counts by round and warp, their prefix sums, the place among the warp's
+#pragma unroll
+    for (int k = 0; k < kDirectRounds; ++k) {
+        const unsigned hits = __ballot_sync(0xffffffffu, found >> k & 1);
+        if (tid % 32 == 0) counts[k * (kDirectThreads / 32) + tid / 32] = __popc(hits);
+    }
+    __syncthreads();
+    if (tid < 32) {  // 128 counts, four a lane
+        static_assert(kDirectRounds * kDirectThreads / 32 == 128, "four counts a lane");
+        int c[4], sum = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            c[q] = sum;
+            sum += counts[tid * 4 + q];
+        }
+        int inc = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int up = __shfl_up_sync(0xffffffffu, inc, o);
+            if (tid >= o) inc += up;
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) counts[tid * 4 + q] = inc - sum + c[q];
+        if (tid == 31) counts[128] = inc;
+    }
+    __syncthreads();
+    const int total = counts[128];
+#pragma unroll
+    for (int k = 0; k < kDirectRounds; ++k) {
+        const bool hit = found >> k & 1;
+        const unsigned hits = __ballot_sync(0xffffffffu, hit);
+        if (hit) list[counts[k * (kDirectThreads / 32) + tid / 32] + __popc(hits & ((1u << (tid % 32)) - 1))] = (uint16_t)(k * kDirectThreads + tid);
+    }
+    __syncthreads();
+    T* row = table + (int64_t)id * table_pitch;
+    for (int64_t c0 = 0; c0 < width; c0 += (int64_t)group * VEC) {
+        const int64_t c = c0 + (int64_t)lane * VEC;
+        float sum[VEC] = {};
+        if (c < width)  // a slot takes every slots-th row
+            for (int k = slot; k < total; k += slots * kAhead) {
+                Pack<T, VEC> r[kAhead];
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a)
+                    if (k + a * slots < total) r[a] = *reinterpret_cast<const Pack<T, VEC>*>(grad_out + (int64_t)list[k + a * slots] * grad_pitch + c);
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a)
+                    if (k + a * slots < total)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) sum[e] += widen(r[a].v[e]);
+            }
+        if (slots > 1 && total > 1) {  // the slots' sums, in their order
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) joined[e * kDirectThreads + tid] = sum[e];
+            __syncthreads();
+            if (slot == 0)
+                for (int o = 1; o < slots; ++o)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[e] += joined[e * kDirectThreads + o * group + lane];
+        }
+        if (slot == 0 && c < width) finish_row<T, VEC>(row + c, sum, scale, accumulate);
+    }
 }
 
 int sort_passes(int64_t vocab) {  // keys are 0 .. vocab
@@ -363,13 +459,15 @@ struct GradPlan {
 int64_t grad_layout(int64_t vocab, int64_t width, int64_t n_ids, void* workspace, GradPlan* out) {
     GradPlan p{};
     Carver w(workspace);
+    if (n_ids <= kDirectMost) {
+        if (out) *out = p;
+        return 0;
+    }
     p.passes = sort_passes(vocab);
     p.n_tiles = ceil_div(n_ids, kTile);
     p.sorted = w.take<Pair>(n_ids);
-    if (n_ids > kOneTile) {
-        p.other = w.take<Pair>(n_ids);
-        p.counts = w.take<int>(p.passes * p.n_tiles * kDigits);
-    }
+    p.other = w.take<Pair>(n_ids);
+    p.counts = w.take<int>(p.passes * p.n_tiles * kDigits);
     p.partial = w.take<float>(ceil_div(n_ids, segment_span(n_ids)) * 2 * width);
     if (out) *out = p;
     return w.used;
@@ -386,15 +484,39 @@ cudaError_t segments_typed(const EmbedGradArgs& a, const GradPlan& p, cudaStream
     auto* table = static_cast<T*>(a.grad_table);
     const int64_t sum_ctas = ceil_div(blocks, per_cta);
     const int64_t zero_ctas = a.accumulate ? 0 : ceil_div(a.vocab, kZeroRows);
-    if (sum_ctas + zero_ctas > 0)
-        k_segments<T, VEC><<<dim3((unsigned)(sum_ctas + zero_ctas), (unsigned)col_ctas), kThreads, 0, s>>>(
+    launch_chained(k_segments<T, VEC>, dim3((unsigned)(sum_ctas + zero_ctas), (unsigned)col_ctas), kThreads, 0, s, 
             g, a.grad_out_pitch, p.sorted, a.n_ids, a.vocab, a.width, a.scale, a.accumulate, table, a.grad_table_pitch, p.partial, span,
             group, sum_ctas);
-    if (blocks > 1)
-        k_join<T, VEC><<<dim3((unsigned)sum_ctas, (unsigned)col_ctas), kThreads, 0, s>>>(p.sorted, a.n_ids, a.vocab, a.width, a.scale,
+    launch_chained(k_join<T, VEC>, dim3((unsigned)sum_ctas, (unsigned)col_ctas), kThreads, 0, s, p.sorted, a.n_ids, a.vocab, a.width, a.scale,
                                                                                          a.accumulate, table, a.grad_table_pitch, p.partial,
                                                                                          span, group);
     return cudaGetLastError();
+}
+
+template <class T, int VEC>
+cudaError_t direct_typed(const EmbedGradArgs& a, cudaStream_t s) {
+    int group = group_threads(a.width, VEC);
+    const int64_t ctas = a.n_ids + (a.accumulate ? 0 : ceil_div(a.vocab, kZeroRows));
+    if (ctas == 0) return cudaSuccess;
+    return launch_chained(k_direct<T, VEC>, dim3((unsigned)ctas), kDirectThreads, 0, s, static_cast<const T*>(a.grad_out), a.grad_out_pitch, a.ids,
+                          (int)a.n_ids, a.vocab, a.width, a.scale, a.accumulate, static_cast<T*>(a.grad_table), a.grad_table_pitch, group);
+}
+
+// Sorts the positions into p.sorted, then sums.
+template <class T, int VEC>
+cudaError_t sorted_typed(const EmbedGradArgs& a, const GradPlan& p, cudaStream_t s) {
+    launch_chained(k_sort_count, dim3((unsigned)p.n_tiles), kSortThreads, 0, s, a.ids, a.n_ids, a.vocab, p.passes, p.counts);
+    // the passes go back and forth between the two buffers and end in p.sorted
+    const Pair* from = nullptr;
+    for (int pass = 0; pass < p.passes; ++pass) {
+        Pair* to = (p.passes - pass) % 2 == 1 ? p.sorted : p.other;
+        const int* counts = p.counts + (int64_t)pass * p.n_tiles * kDigits;
+        const bool last = pass + 1 == p.passes;
+        launch_chained(k_sort_pass, dim3((unsigned)p.n_tiles), kSortThreads, 0, s, a.ids, from, a.n_ids, a.vocab, pass, last, counts, (int)p.n_tiles, to,
+                       last ? nullptr : p.counts + (int64_t)(pass + 1) * p.n_tiles * kDigits);
+        from = to;
+    }
+    return segments_typed<T, VEC>(a, p, s);
 }
 
 template <class T>
@@ -402,7 +524,8 @@ cudaError_t grad_typed(const EmbedGradArgs& a, const GradPlan& p, cudaStream_t s
     constexpr int kVec = 16 / sizeof(T);
     const bool wide =
         a.width % kVec == 0 && aligned16(a.grad_out, a.grad_out_pitch, sizeof(T)) && aligned16(a.grad_table, a.grad_table_pitch, sizeof(T));
-    return wide ? segments_typed<T, kVec>(a, p, s) : segments_typed<T, 1>(a, p, s);
+    if (a.n_ids <= kDirectMost) return wide ? direct_typed<T, kVec>(a, s) : direct_typed<T, 1>(a, s);
+    return wide ? sorted_typed<T, kVec>(a, p, s) : sorted_typed<T, 1>(a, p, s);
 }
 
 }  // namespace
@@ -417,23 +540,6 @@ int64_t embed_grad_workspace(int64_t vocab, int64_t width, int64_t n_ids) { retu
 cudaError_t run_embed_grad(const EmbedGradArgs& a, void* workspace, cudaStream_t s) {
     GradPlan p;
     grad_layout(a.vocab, a.width, a.n_ids, workspace, &p);
-    if (a.n_ids > kOneTile) {
-        cudaError_t e = cudaMemsetAsync(p.counts, 0, sizeof(int) * (size_t)(p.passes * p.n_tiles * kDigits), s);
-        if (e != cudaSuccess) return e;
-        k_sort_count<<<(unsigned)p.n_tiles, kSortThreads, 0, s>>>(a.ids, a.n_ids, a.vocab, p.counts);
-        // the passes go back and forth between the two buffers and end in p.sorted
-        Pair* from = nullptr;
-        for (int pass = 0; pass < p.passes; ++pass) {
-            Pair* to = (p.passes - pass) % 2 == 1 ? p.sorted : p.other;
-            const int* counts = p.counts + (int64_t)pass * p.n_tiles * kDigits;
-            const bool last = pass + 1 == p.passes;
-            k_sort_pass<<<(unsigned)p.n_tiles, kSortThreads, 0, s>>>(a.ids, from, a.n_ids, a.vocab, pass, last, counts, (int)p.n_tiles, to,
-                                                                     last ? nullptr : p.counts + (int64_t)(pass + 1) * p.n_tiles * kDigits);
-            from = to;
-        }
-    } else if (a.n_ids > 0) {
-        k_sort_one<<<1, kSortThreads, 0, s>>>(a.ids, (int)a.n_ids, a.vocab, p.passes, p.sorted);
-    }
     return a.dtype == A2_BF16 ? grad_typed<__nv_bfloat16>(a, p, s) : grad_typed<float>(a, p, s);
 }
 

@@ -51,31 +51,39 @@ cudaError_t operand_maps(const Operand& o, bool bf16, int64_t mats, CUtensorMap 
 
 }  // namespace
 
+cudaError_t gave_up_flag(int** out) { return cudaGetSymbolAddress(reinterpret_cast<void**>(out), g_gave_up); }
+
 int gemm_clusters() {
     int device = 0, sms = 0;
     if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 1;
     return sms >= 2 ? sms / 2 : 1;
 }
 
-cudaError_t make_gemm(const Operand& a, const Operand& b, int64_t mats, bool bf16, bool lower, int flush, GemmArgs* g) {
+cudaError_t make_gemm(const Operand& a, const Operand& b, int64_t mats, bool bf16, bool lower, int flush, int splits, GemmArgs* g) {
     cudaError_t e = operand_maps(a, bf16, mats, g->a);
     if (e == cudaSuccess) e = operand_maps(b, bf16, mats, g->b);
+    auto mirror = [&](Operand o, CUtensorMap(&out)[2]) {
+        if (e != cudaSuccess || !o.symmetric) return;
+        o.mn = true;
+        e = operand_maps(o, bf16, mats, out);
+    };
+    mirror(a, g->a_mirror);
+    mirror(b, g->b_mirror);
     if (e != cudaSuccess) return e;
-    void* flag = nullptr;
-    e = cudaGetSymbolAddress(&flag, g_gave_up);
+    e = gave_up_flag(&g->gave_up);
     if (e != cudaSuccess) return e;
-    g->gave_up = static_cast<int*>(flag);
     g->tiles_m = (int32_t)ceil_div(a.rows, kTileM);
     g->tiles_n = (int32_t)ceil_div(b.rows, kTileN);
     g->batch = (int32_t)mats;
     g->k_blocks = (int32_t)ceil_div(a.k, kBlockK);
+    g->splits = splits;
     g->passes = a.lo ? 3 : 1;
     g->flush = flush > 0 ? flush : g->k_blocks * g->passes;
-    // fp32 sums; fp16 (0) or bf16 (1) operands; MN-major bits; N / 8 and M / 16
-    g->idesc = 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (a.mn ? 1u : 0u) << 15 | (b.mn ? 1u : 0u) << 16 |
-               (uint32_t)(kTileN / 8) << 17 | (uint32_t)(kTileM / 16) << 24;
+    g->idesc = instruction_desc(bf16, false, false, kTileM, kTileN);  // the kernel adds the MN-major bits
     g->a_mn = a.mn;
     g->b_mn = b.mn;
+    g->a_sym = a.symmetric;
+    g->b_sym = b.symmetric;
     g->lower = lower;
     return cudaSuccess;
 }

@@ -80,6 +80,12 @@ int check_table_sizes(int64_t vocab, int64_t width, int64_t n_ids) {
     return A2_OK;
 }
 
+// The products count their tiles in 32 bits.
+int check_products(int64_t n_tokens, int64_t vocab) {
+    A2_CHECK(a2::ceil_div(n_tokens, 256) * a2::ceil_div(vocab, 256) < (int64_t(1) << 30), A2_ERANGE, "n_tokens * vocab beyond 2^46");
+    return A2_OK;
+}
+
 int check_batch_sizes(int64_t n_mats, int64_t rows, int64_t cols) {
     A2_CHECK(n_mats >= 0 && rows >= 1 && cols >= 1, A2_EINVAL, "need rows >= 1, cols >= 1 and no negative count");
     A2_CHECK(n_mats <= kMaxMats, A2_ERANGE, "more than %lld matrices", (long long)kMaxMats);
@@ -136,6 +142,7 @@ int a2cid2_vocab_loss_workspace(int64_t n_tokens, int64_t width, int64_t vocab, 
     A2_CHECK(bytes, A2_EINVAL, "bytes is NULL");
     A2_TRY(check_type(storage_dtype));
     A2_TRY(check_table_sizes(vocab, width, n_tokens));
+    A2_TRY(check_products(n_tokens, vocab));
     *bytes = a2::vocab_loss_workspace(n_tokens, width, vocab, with_grad != 0, storage_dtype);
     return A2_OK;
 }
@@ -146,6 +153,7 @@ int a2cid2_vocab_loss(const void* hidden, int64_t hidden_pitch, const void* head
                       int32_t storage_dtype, void* workspace, int64_t workspace_bytes, void* cuda_stream) {
     A2_TRY(check_type(storage_dtype));
     A2_TRY(check_table_sizes(vocab, width, n_tokens));
+    A2_TRY(check_products(n_tokens, vocab));
     A2_TRY(check_number("scale", scale));
     A2_TRY(check_matrix("hidden", hidden, n_tokens, width, hidden_pitch, storage_dtype));
     A2_TRY(check_matrix("head", head, vocab, width, head_pitch, storage_dtype));
@@ -183,8 +191,8 @@ int a2cid2_orthogonalize(const void* in, int64_t in_stride, int64_t in_pitch, in
     A2_TRY(check_number("c", c));
     A2_TRY(check_number("scale", scale));
     A2_CHECK(std::isfinite(eps) && eps >= 0, A2_EINVAL, "need eps >= 0");
-    double center;
-    A2_CHECK(a2::orthogonalize_range(a, b, c, steps, &center), A2_EINVAL, "the coefficients take singular values of [0, 1] beyond 1.95");
+    A2_CHECK(a2::orthogonalize_range(a, b, c, steps), A2_EINVAL,
+             "the coefficients take singular values of [0, 1] beyond 1.95 or the polynomial beyond 3.9");
     A2_TRY(check_matrix("in", in, n_mats, cols, in_pitch, storage_dtype));
     A2_TRY(check_matrix("out", out, n_mats, cols, out_pitch, storage_dtype));
     // matrices of a batch may not share elements: a matrix takes (rows - 1) * pitch + cols of them
@@ -195,7 +203,7 @@ int a2cid2_orthogonalize(const void* in, int64_t in_stride, int64_t in_pitch, in
              "in place needs the same stride and pitch on both sides");
     A2_TRY(check_workspace(workspace, workspace_bytes, a2::orthogonalize_workspace(n_mats, rows, cols, storage_dtype)));
     if (n_mats == 0) return A2_OK;
-    const a2::OrthogonalizeArgs args{in, in_stride, in_pitch, n_mats, rows, cols, steps, (float)a, (float)b, (float)c, (float)center, eps, (float)scale, out,
+    const a2::OrthogonalizeArgs args{in, in_stride, in_pitch, n_mats, rows, cols, steps, (float)a, (float)b, (float)c, eps, (float)scale, out,
                                      out_stride, out_pitch, storage_dtype};
     return status(a2::run_orthogonalize(args, workspace, (cudaStream_t)cuda_stream), "orthogonalisation");
 }

@@ -79,16 +79,14 @@ struct OrthogonalizeArgs {
     int64_t n_mats, rows, cols;
     int32_t steps;
     float ca, cb, cc;
-    float center;  // of orthogonalize_range
     double eps;
     float scale;
     void* out;
     int64_t out_stride, out_pitch;
     int32_t dtype;
 };
-// Whether the steps keep singular values of [0, 1], and the polynomial, inside what the fp16 intermediates hold; the
-// polynomial's middle.
-bool orthogonalize_range(double a, double b, double c, int steps, double* center);
+// Whether the steps keep singular values of [0, 1], and the polynomial there, inside what the fp16 intermediates hold.
+bool orthogonalize_range(double a, double b, double c, int steps);
 int64_t orthogonalize_workspace(int64_t n_mats, int64_t rows, int64_t cols, int32_t dtype);
 cudaError_t run_orthogonalize(const OrthogonalizeArgs& a, void* workspace, cudaStream_t s);
 
@@ -103,6 +101,34 @@ template <>
 __device__ __forceinline__ float narrow<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// Starts a kernel that may begin before its predecessor in the stream has ended; the kernel itself calls wait_previous() before it
+// touches memory.
+template <class... P, class... A>
+cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, A&&... args) {
+    cudaLaunchConfig_t config{};
+    config.gridDim = grid;
+    config.blockDim = dim3(threads);
+    config.dynamicSmemBytes = smem;
+    config.stream = s;
+    cudaLaunchAttribute attribute{};
+    attribute.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attribute.val.programmaticStreamSerializationAllowed = 1;
+    config.attrs = &attribute;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, static_cast<P>(args)...);
+}
+
+namespace ptx {
+// Kernels of one operator are launched so that one may start while its predecessor ends: it sets itself up, lets its own
+// successor do the same, and waits until everything before it is done and visible.
+__device__ __forceinline__ void release_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void chained() {
+    release_next();
+    wait_previous();
+}
+}  // namespace ptx
 
 template <class T, int VEC>
 struct alignas(sizeof(T) * VEC) Pack {

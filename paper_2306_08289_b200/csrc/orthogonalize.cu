@@ -1,8 +1,8 @@
 // Orthogonalisation of a batch of matrices by Newton-Schulz products: X = G / (|G|_F + eps), then
-//   A = X X^T,  B = (a - q) I + b A + c A^2,  X <- q X + B X
-// (the same for any q; one in the middle of the polynomial's range makes B, and so its rounding, smallest) on the smaller side m <= n. All three products run on the tensor cores; A and B are symmetric, so only tiles on and below
-// the diagonal are computed and the others are written as their transposes: 3 m^2 n + m^3 operations a step instead of
-// 4 m^2 n + 2 m^3. A tall matrix (rows > cols) stays as it lies: Y = X^T, A = Y^T Y, Y <- q Y + Y B.
+//   A = X X^T,  B = a I + b A + c A^2,  X <- B X
+// on the smaller side m <= n. All three products run on the tensor cores; A and B are symmetric, so only tiles on and below
+// the diagonal are computed and stored, and a product reads the others as the transposes of those: 3 m^2 n + m^3 operations a
+// step instead of 4 m^2 n + 2 m^3. A tall matrix (rows > cols) stays as it lies: Y = X^T, A = Y^T Y, Y <- Y B.
 //
 // The intermediates are fp16 words at power-of-two scales: one word with bf16 rows (11 bits; bf16 words would lose 8 times as
 // much per rounding, and the roundings of small singular values grow up to a^steps), two with fp32 rows. X's elements are bounded by
@@ -38,7 +38,7 @@ __device__ __forceinline__ int next_bound(int r, float a, float b, float c) {
 }
 
 struct Poly {
-    float a, b, c, q;
+    float a, b, c;
     int step;  // 0 .. steps - 1
 };
 
@@ -56,6 +56,7 @@ constexpr int kNormThreads = 256;
 template <class T>
 __global__ void __launch_bounds__(kNormThreads) k_norm(const T* __restrict__ in, int64_t stride, int64_t pitch, int64_t rows, int64_t cols,
                                                        double* __restrict__ partial) {
+    ptx::chained();
     __shared__ double part[kNormThreads / 32];
     const T* g = in + blockIdx.y * stride;
     double sum = 0.0;
@@ -77,44 +78,52 @@ __global__ void __launch_bounds__(kNormThreads) k_norm(const T* __restrict__ in,
     }
 }
 
-__device__ __forceinline__ void split_words(float x, __half& hi, __half& lo) {
-    hi = __float2half_rn(x);
-    const float back = __half2float(hi);
-    lo = __float2half_rn(isfinite(back) ? x - back : 0.0f);
-}
-
-__device__ __forceinline__ MatScale mat_scale(const double* partial, int parts, double eps) {
-    double all = 0.0;
-    for (int p = 0; p < parts; ++p) all += partial[p];
-    const double norm = sqrt(all), by = norm + eps;
+__device__ __forceinline__ MatScale mat_scale(double squares, double eps) {
+    const double norm = sqrt(squares), by = norm + eps;
     if (!(norm <= 1e300)) return {NAN, 0, 0};
     if (norm == 0.0) return {0.0f, 0, 0};
     const int e = 13 - ilogb(norm);  // norm * 2^e in [2^13, 2^14)
     return {(float)(1.0 / (ldexp(by, e))), e, min(0, ilogb(norm / by) + 1)};
 }
 
-// Words of G 2^e, [rows, ld].
+// Words of G 2^e, [rows, ld]. Two columns a lane, so that a warp's stores are 128 bytes; `aligned`: G's pairs can be read at once.
 template <class T>
 __global__ void __launch_bounds__(kNormThreads) k_first_words(const T* __restrict__ in, int64_t stride, int64_t pitch, int64_t rows, int64_t cols,
-                                                              const double* __restrict__ partial, int parts, double eps, __half* __restrict__ hi,
-                                                              __half* __restrict__ lo, int64_t ld, MatScale* __restrict__ scales) {
+                                                              const double* __restrict__ partial, int parts, double eps, bool aligned,
+                                                              __half* __restrict__ hi, __half* __restrict__ lo, int64_t ld,
+                                                              MatScale* __restrict__ scales) {
+    ptx::chained();
     __shared__ MatScale shared;
-    if (threadIdx.x == 0) {
-        shared = mat_scale(partial + (int64_t)blockIdx.y * parts, parts, eps);
-        if (blockIdx.x == 0) scales[blockIdx.y] = shared;
+    if (threadIdx.x < 32) {
+        double sum = 0.0;
+        for (int p = threadIdx.x; p < parts; p += 32) sum += partial[(int64_t)blockIdx.y * parts + p];
+        for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (threadIdx.x == 0) {
+            shared = mat_scale(sum, eps);
+            if (blockIdx.x == 0) scales[blockIdx.y] = shared;
+        }
     }
     __syncthreads();
-    const int e = shared.e;
+    const PowerOfTwo up(shared.e);
     const T* g = in + blockIdx.y * stride;
     const int64_t base = (int64_t)blockIdx.y * rows * ld;
     const int64_t warp = (int64_t)blockIdx.x * (kNormThreads / 32) + threadIdx.x / 32, warps = (int64_t)gridDim.x * (kNormThreads / 32);
     for (int64_t i = warp; i < rows; i += warps)
 #pragma unroll 4
-        for (int64_t j = threadIdx.x % 32; j < cols; j += 32) {
-            __half h, l;
-            split_words(scalbnf(widen(g[i * pitch + j]), e), h, l);
-            hi[base + i * ld + j] = h;
-            if (lo) lo[base + i * ld + j] = l;
+        for (int64_t j = threadIdx.x % 32 * 2; j < cols; j += 64) {
+            Pack<T, 2> x;
+            const T* at = g + i * pitch + j;
+            if (aligned && j + 1 < cols) {
+                x = *reinterpret_cast<const Pack<T, 2>*>(at);
+            } else {
+                x.v[0] = at[0];
+                x.v[1] = j + 1 < cols ? at[1] : narrow<T>(0.0f);
+            }
+            Pack<__half, 2> h, l;
+            split_words(up(widen(x.v[0])), h.v[0], l.v[0]);
+            split_words(up(widen(x.v[1])), h.v[1], l.v[1]);
+            *reinterpret_cast<Pack<__half, 2>*>(hi + base + i * ld + j) = h;  // ld is even: the second one may be padding
+            if (lo) *reinterpret_cast<Pack<__half, 2>*>(lo + base + i * ld + j) = l;
         }
 }
 
@@ -122,6 +131,7 @@ __global__ void __launch_bounds__(kNormThreads) k_first_words(const T* __restric
 template <class T>
 __global__ void __launch_bounds__(kNormThreads) k_normalized(const __half* hi, const __half* lo, int64_t ld, int64_t rows, int64_t cols,
                                                              const MatScale* scales, float scale, T* out, int64_t stride, int64_t pitch) {
+    ptx::chained();
     const float by = scales[blockIdx.y].u * scale;
     const int64_t base = (int64_t)blockIdx.y * rows * ld;
     const int64_t warp = (int64_t)blockIdx.x * (kNormThreads / 32) + threadIdx.x / 32, warps = (int64_t)gridDim.x * (kNormThreads / 32);
@@ -140,31 +150,18 @@ struct Words {
     int64_t ld, stride;
 };
 
-__device__ __forceinline__ void read_words(const Words& w, int64_t at, float (&x)[32]) {
+// Words of 32 x 32 values, a row a lane (staging: 4 KB).
+__device__ __forceinline__ void write_words(const Words& w, int64_t at, const float (&x)[32], int rows, int lane, float* staging) {
+    __half h[32], l[32];
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-        const Pack<__half, 16> h = *reinterpret_cast<const Pack<__half, 16>*>(w.hi + at + g * 16);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) x[g * 16 + k] = __half2float(h.v[k]);
-        if (w.lo) {
-            const Pack<__half, 16> l = *reinterpret_cast<const Pack<__half, 16>*>(w.lo + at + g * 16);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) x[g * 16 + k] += __half2float(l.v[k]);
-        }
-    }
-}
-__device__ __forceinline__ void write_words(const Words& w, int64_t at, const float (&x)[32]) {
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-        Pack<__half, 16> h, l;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) split_words(x[g * 16 + k], h.v[k], l.v[k]);
-        *reinterpret_cast<Pack<__half, 16>*>(w.hi + at + g * 16) = h;
-        if (w.lo) *reinterpret_cast<Pack<__half, 16>*>(w.lo + at + g * 16) = l;
-    }
+    for (int k = 0; k < 32; k += 2) split_pair(x[k], x[k + 1], h[k], h[k + 1], l[k], l[k + 1]);
+    char* s = reinterpret_cast<char*>(staging);
+    store_rows16(s, h, w.hi + at, w.ld, rows, lane);
+    if (w.lo) store_rows16(s + 2048, l, w.lo + at, w.ld, rows, lane);
 }
 
-// A = X X^T (kQuadratic false) or B = (a - q) I + b A + c A^2 (true), symmetric: tiles below the diagonal are written twice.
+// A = X X^T (kQuadratic false) or B = a I + b A + c A^2 (true), symmetric: tiles above the diagonal are
+// neither computed nor stored.
 template <bool kQuadratic>
 struct SymmetricEpi {
     struct Args {
@@ -176,51 +173,48 @@ struct SymmetricEpi {
     const Args& a;
     int64_t row0, col0, mat;
     int lane;
-    bool mirror;
+    float* staging;
     float factor;
-    __device__ __forceinline__ SymmetricEpi(const Args& args, int b, int row, int col, int lane_, float*)
-        : a(args), row0(row), col0(col), mat(b), lane(lane_), mirror(row / kTileM != col / kTileN) {
+    __device__ __forceinline__ SymmetricEpi(const Args& args, const Tile& t, int row, int col, int lane_, float* staging_)
+        : a(args), row0(row), col0(col), mat(t.b), lane(lane_), staging(staging_) {
         if (kQuadratic) {
             factor = a.poly.c / kScale;
         } else {
             float now, next;
-            units(a.scales[b], a.poly, &now, &next);
+            units(a.scales[mat], a.poly, &now, &next);
             factor = kScale * now * now;
         }
     }
     __device__ __forceinline__ void chunk(int c, float (&v)[32]) {
-        const int64_t col = col0 + c * 32, row = row0 + lane;
-        if (row >= a.m || col >= a.m) return;
-        const int64_t at = mat * a.to.stride + row * a.to.ld + col;
+        const int64_t col = col0 + c * 32;
+        if (row0 >= a.m || col >= a.m) return;  // rows of `to` are padded to 64 columns: only rows need care
+        const int rows = (int)min((int64_t)32, a.m - row0);
+        const int64_t at = mat * a.to.stride + row0 * a.to.ld + col;
         if (kQuadratic) {
-            float x[32];
-            read_words(a.from, at, x);
+            __half x[32];
+            load_rows16(staging, x, a.from.hi + at, a.from.ld, rows, lane);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] = a.poly.b * x[k] + factor * v[k] + (row == col + k ? (a.poly.a - a.poly.q) * kScale : 0.0f);
+            for (int k = 0; k < 32; ++k)
+                v[k] = a.poly.b * __half2float(x[k]) + factor * v[k] + (row0 + lane == col + k ? a.poly.a * kScale : 0.0f);
+            if (a.from.lo) {
+                load_rows16(staging, x, a.from.lo + at, a.from.ld, rows, lane);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] += a.poly.b * __half2float(x[k]);
+            }
         } else {
 #pragma unroll
             for (int k = 0; k < 32; ++k) v[k] *= factor;
         }
-        write_words(a.to, at, v);
-        if (mirror) {  // col < row0: all 32 columns lie inside the matrix
-            const int64_t turned = mat * a.to.stride + col * a.to.ld + row;
-#pragma unroll
-            for (int k = 0; k < 32; ++k) {
-                __half h, l;
-                split_words(v[k], h, l);
-                a.to.hi[turned + k * a.to.ld] = h;
-                if (a.to.lo) a.to.lo[turned + k * a.to.ld] = l;
-            }
-        }
+        write_words(a.to, at, v, rows, lane, staging);
     }
     __device__ __forceinline__ void finish() {}
 };
 
-// X <- q X + B X; the last step writes the caller's matrix.
+// X <- B X; the last step writes the caller's matrix.
 template <class T>
 struct UpdateEpi {
     struct Args {
-        Words from, to;
+        Words to;
         int64_t rows, cols;
         const MatScale* scales;
         Poly poly;
@@ -233,40 +227,35 @@ struct UpdateEpi {
     int lane;
     float* staging;
     float factor;
-    __device__ __forceinline__ UpdateEpi(const Args& args, int b, int row, int col, int lane_, float* staging_)
-        : a(args), row0(row), col0(col), mat(b), lane(lane_), staging(staging_) {
+    __device__ __forceinline__ UpdateEpi(const Args& args, const Tile& t, int row, int col, int lane_, float* staging_)
+        : a(args), row0(row), col0(col), mat(t.b), lane(lane_), staging(staging_) {
         float now, next;
-        units(a.scales[b], a.poly, &now, &next);
-        factor = a.out ? a.scale * now : now / next;
+        units(a.scales[mat], a.poly, &now, &next);
+        factor = (a.out ? a.scale * now : now / next) / kScale;
     }
     __device__ __forceinline__ void chunk(int c, float (&v)[32]) {
-        const int64_t col = col0 + c * 32, row = row0 + lane;
-        if (col >= a.cols) return;
-        if (row < a.rows) {
-            const int64_t at = mat * a.from.stride + row * a.from.ld + col;
-            float x[32];
-            read_words(a.from, at, x);
+        const int64_t col = col0 + c * 32;
+        if (row0 >= a.rows || col >= a.cols) return;
+        const int rows = (int)min((int64_t)32, a.rows - row0);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] = (a.poly.q * x[k] + v[k] / kScale) * factor;
-            if (!a.out) write_words(a.to, at, v);
+        for (int k = 0; k < 32; ++k) v[k] *= factor;
+        if (!a.out) {
+            write_words(a.to, mat * a.to.stride + row0 * a.to.ld + col, v, rows, lane, staging);
+            return;
         }
-        if (!a.out) return;
-#pragma unroll
-        for (int k = 0; k < 32; ++k) staging[lane * kStagePitch + k] = v[k];
-        __syncwarp();
+        turn_columns(staging, v, lane);
         if (col + lane < a.cols) {
             T* to = a.out + mat * a.stride + row0 * a.pitch + col + lane;
-            const int rows = (int)min((int64_t)32, a.rows - row0);
-#pragma unroll 8
-            for (int r = 0; r < rows; ++r) to[r * a.pitch] = narrow<T>(staging[r * kStagePitch + lane]);
+#pragma unroll
+            for (int r = 0; r < 32; ++r)
+                if (r < rows) to[r * a.pitch] = narrow<T>(v[r]);
         }
-        __syncwarp();
     }
     __device__ __forceinline__ void finish() {}
 };
 
 // ---- layout and launches ---------------------------------------------------------------------------
-constexpr int kFlush = 4;  // K blocks a sum stays in tensor memory with fp32 rows: 16 steps of the tensor core
+constexpr int kFlush = 2;  // K blocks a sum stays in tensor memory with fp32 rows: 8 steps of the tensor core
 
 struct Layout {
     double* partial;
@@ -305,57 +294,279 @@ cudaError_t typed(const OrthogonalizeArgs& a, Layout l, cudaStream_t s) {
     const bool tall = a.rows > a.cols;
     const int64_t m = std::min(a.rows, a.cols), n = std::max(a.rows, a.cols);
     const dim3 grid((unsigned)l.parts, (unsigned)a.n_mats);
-    k_norm<T><<<grid, kNormThreads, 0, s>>>(static_cast<const T*>(a.in), a.in_stride, a.in_pitch, a.rows, a.cols, l.partial);
-    k_first_words<T><<<grid, kNormThreads, 0, s>>>(static_cast<const T*>(a.in), a.in_stride, a.in_pitch, a.rows, a.cols, l.partial, (int)l.parts,
-                                                   a.eps, l.x.hi, l.x.lo, l.x.ld, l.scales);
+    const bool aligned = reinterpret_cast<uintptr_t>(a.in) % (2 * sizeof(T)) == 0 && a.in_pitch % 2 == 0 && (a.n_mats == 1 || a.in_stride % 2 == 0);
+    launch_chained(k_norm<T>, grid, kNormThreads, 0, s, static_cast<const T*>(a.in), a.in_stride, a.in_pitch, a.rows, a.cols, l.partial);
+    launch_chained(k_first_words<T>, grid, kNormThreads, 0, s, static_cast<const T*>(a.in), a.in_stride, a.in_pitch, a.rows, a.cols, l.partial, (int)l.parts,
+                                                   a.eps, aligned, l.x.hi, l.x.lo, l.x.ld, l.scales);
     if (a.steps == 0)
-        k_normalized<T><<<grid, kNormThreads, 0, s>>>(l.x.hi, l.x.lo, l.x.ld, a.rows, a.cols, l.scales, a.scale, static_cast<T*>(a.out), a.out_stride,
+        launch_chained(k_normalized<T>, grid, kNormThreads, 0, s, l.x.hi, l.x.lo, l.x.ld, a.rows, a.cols, l.scales, a.scale, static_cast<T*>(a.out), a.out_stride,
                                                       a.out_pitch);
     auto operand = [](const Words& w, int64_t rows, int64_t k, bool mn) { return Operand{w.hi, w.lo, rows, k, w.ld, w.stride, mn}; };
     Words x = l.x, y = l.y;
     for (int step = 0; step < a.steps; ++step) {
-        const Poly poly{a.ca, a.cb, a.cc, a.center, step};
+        const Poly poly{a.ca, a.cb, a.cc, step};
         GemmArgs g;
         const Operand side = operand(x, m, n, tall);
-        cudaError_t e = make_gemm(side, side, a.n_mats, false, true, flush, &g);
+        cudaError_t e = make_gemm(side, side, a.n_mats, false, true, flush, 1, &g);
         if (e != cudaSuccess) return e;
         e = launch_gemm<SymmetricEpi<false>, kWords>(g, {l.gram, l.gram, m, l.scales, poly}, s);
         if (e != cudaSuccess) return e;
-        const Operand gram = operand(l.gram, m, m, false);
-        e = make_gemm(gram, gram, a.n_mats, false, true, flush, &g);
+        Operand gram = operand(l.gram, m, m, false), b = operand(l.poly, m, m, false);
+        gram.symmetric = b.symmetric = true;
+        e = make_gemm(gram, gram, a.n_mats, false, true, flush, 1, &g);
         if (e != cudaSuccess) return e;
         e = launch_gemm<SymmetricEpi<true>, kWords>(g, {l.gram, l.poly, m, l.scales, poly}, s);
         if (e != cudaSuccess) return e;
-        const Operand b = operand(l.poly, m, m, false);
-        e = tall ? make_gemm(operand(x, a.rows, m, false), b, a.n_mats, false, false, flush, &g)
-                 : make_gemm(b, operand(x, n, m, true), a.n_mats, false, false, flush, &g);
+        e = tall ? make_gemm(operand(x, a.rows, m, false), b, a.n_mats, false, false, flush, 1, &g)
+                 : make_gemm(b, operand(x, n, m, true), a.n_mats, false, false, flush, 1, &g);
         if (e != cudaSuccess) return e;
         const bool last = step + 1 == a.steps;
         e = launch_gemm<UpdateEpi<T>, kWords>(
-            g, {x, y, a.rows, a.cols, l.scales, poly, last ? static_cast<T*>(a.out) : nullptr, a.out_stride, a.out_pitch, a.scale}, s);
+            g, {y, a.rows, a.cols, l.scales, poly, last ? static_cast<T*>(a.out) : nullptr, a.out_stride, a.out_pitch, a.scale}, s);
         if (e != cudaSuccess) return e;
         std::swap(x, y);
     }
     return cudaGetLastError();
 }
 
+// ---- small matrices: all steps in one CTA ------------------------------------------------------------
+// m <= 128 and n <= 256: X, A and B stay in shared memory as the two-word operands of the tensor core (with either storage
+// type: the products cost nothing here), the sums in tensor memory; one launch, one read and one write of the matrix. Bound by the
+// chain of three products and their epilogues a step. X is kept [m, n] in 64-column blocks of 128-byte swizzled rows, which the tensor
+// core reads K-major for X X^T and MN-major for B X.
+constexpr int kSmallM = 128, kSmallN = 256;
+constexpr int kSmallThreads = 256;
+constexpr int kBlockBytes = kSmallM * 128;  // 128 rows of 64 fp16 columns
+constexpr int kSmallSmem = 2 * (kSmallN / 64) * kBlockBytes + 2 * (kSmallM / 64) * kBlockBytes + 1024;
+
+// Byte offset of columns col .. col + 7 of a row.
+__device__ __forceinline__ uint32_t swizzled(int row, int col) {
+    return (uint32_t)(col / 64) * kBlockBytes + row * 128 + ((((col % 64) / 8) ^ (row % 8)) * 16);
+}
+
+struct SmallArgs {
+    int64_t in_stride, in_pitch, out_stride, out_pitch;
+    int rows, cols, steps;
+    bool tall;
+    Poly poly;
+    double eps;
+    float scale;
+    int* gave_up;
+};
+
+// D = A B^T or A B over K = 16 * k_steps in the three passes of two-word operands; one thread.
+__device__ __forceinline__ void small_product(uint32_t d, const uint32_t (&a)[2], const uint32_t (&b)[2], bool b_mn, int k_steps, uint32_t idesc) {
+    for (int pass = 0; pass < 3; ++pass) {
+        const uint32_t pa = a[pass == 0], pb = b[pass == 1];  // lo hi, hi lo, hi hi
+        for (int k = 0; k < k_steps; ++k) {
+            const uint32_t along = (uint32_t)(k / 4) * kBlockBytes + (k % 4) * 32;  // K-major: 32 bytes, then the next block
+            const uint64_t da = operand_desc(pa + along, false);
+            const uint64_t db = b_mn ? operand_desc(pb + k * 2048, true, kBlockBytes) : operand_desc(pb + along, false);
+            ptx::mma_one(d, da, db, idesc, pass > 0 || k > 0);
+        }
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* __restrict__ in, T* out, const SmallArgs g) {
+    ptx::chained();
+    extern __shared__ char raw[];
+    __shared__ double part[kSmallThreads / 32];
+    __shared__ uint64_t bar_word;
+    __shared__ uint32_t tmem_slot;
+    __shared__ MatScale scale;
+    char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int m = g.tall ? g.cols : g.rows, n = g.tall ? g.rows : g.cols;
+    const int m16 = (m + 15) / 16 * 16, n16 = (n + 15) / 16 * 16, blocks = (n + 63) / 64;
+    char* xw[2] = {smem, smem + (kSmallN / 64) * kBlockBytes};
+    char* aw[2] = {smem + 2 * (kSmallN / 64) * kBlockBytes, smem + 2 * (kSmallN / 64) * kBlockBytes + (kSmallM / 64) * kBlockBytes};
+    const uint32_t xs[2] = {ptx::smem_addr(xw[0]), ptx::smem_addr(xw[1])}, as[2] = {ptx::smem_addr(aw[0]), ptx::smem_addr(aw[1])};
+    const uint32_t bar = ptx::smem_addr(&bar_word);
+    const T* from = in + blockIdx.x * g.in_stride;
+
+    if (threadIdx.x == 0) {
+        ptx::bar_init(bar, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(ptx::smem_addr(&tmem_slot)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        ptx::fence_before();
+    }
+    // the norm
+    double sum = 0.0;
+    for (int i = warp; i < g.rows; i += kSmallThreads / 32)
+        for (int j = lane; j < g.cols; j += 32) {
+            const double v = widen(from[i * g.in_pitch + j]);
+            sum += v * v;
+        }
+    for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) part[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double all = 0.0;
+        for (int w = 0; w < kSmallThreads / 32; ++w) all += part[w];
+        scale = mat_scale(all, g.eps);
+    }
+    __syncthreads();
+    ptx::fence_after();
+    const uint32_t tmem = tmem_slot;
+    // first words, zeros around the matrix: rows to a multiple of 16, columns to a multiple of 64. Eight columns a thread; the tall
+    // matrix is read along its rows, which are X's columns
+    const PowerOfTwo up(scale.e);
+    for (int k = threadIdx.x; k < m16 * blocks * 8; k += kSmallThreads) {
+        const int i = g.tall ? k % m16 : k / (blocks * 8), j = (g.tall ? k / m16 : k % (blocks * 8)) * 8;
+        Pack<__half, 8> hi, lo;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const bool inside = i < m && j + q < n;
+            const float v = inside ? widen(g.tall ? from[(j + q) * g.in_pitch + i] : from[i * g.in_pitch + j + q]) : 0.0f;
+            split_words(up(v), hi.v[q], lo.v[q]);
+        }
+        const uint32_t at = swizzled(i, j);
+        *reinterpret_cast<Pack<__half, 8>*>(xw[0] + at) = hi;
+        *reinterpret_cast<Pack<__half, 8>*>(xw[1] + at) = lo;
+    }
+
+    const int quad = warp % 4, half = warp / 4;
+    const int row = quad * 32 + lane;
+    const bool mine = quad * 32 < m;  // warps of padding rows have nothing to write
+    const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
+    const uint32_t square = instruction_desc(false, false, false, 128, m16), wide = instruction_desc(false, false, true, 128, n16);
+    uint32_t phase = 0;
+    bool ok = true;
+    // one product: operands written by everybody, MMAs by one thread, everybody waits
+    auto product = [&](uint32_t d, const uint32_t (&a)[2], const uint32_t (&b)[2], bool b_mn, int k_steps, uint32_t idesc) {
+        ptx::fence_before();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            ptx::fence_after();
+            small_product(d, a, b, b_mn, k_steps, idesc);
+            ptx::commit_one(bar);
+        }
+        __syncwarp();
+        ok = ptx::bar_wait(bar, phase & 1, g.gave_up);
+        ++phase;
+        ptx::fence_after();
+        return __syncthreads_or(!ok) == 0;
+    };
+    auto write8 = [&](char* const (&to)[2], int col, const float* v) {
+        Pack<__half, 8> hi, lo;
+#pragma unroll
+        for (int q = 0; q < 8; q += 2) split_pair(v[q], v[q + 1], hi.v[q], hi.v[q + 1], lo.v[q], lo.v[q + 1]);
+        const uint32_t at = swizzled(row, col);
+        *reinterpret_cast<Pack<__half, 8>*>(to[0] + at) = hi;
+        *reinterpret_cast<Pack<__half, 8>*>(to[1] + at) = lo;
+    };
+    T* to = out + blockIdx.x * g.out_stride;
+    Poly poly = g.poly;
+    for (poly.step = 0; poly.step < g.steps; ++poly.step) {
+        float now, next;
+        units(scale, poly, &now, &next);
+        const bool last = poly.step + 1 == g.steps;
+        if (!product(tmem, xs, xs, false, n16 / 16, square)) break;
+        const float gram = kScale * now * now;
+        for (int col = half * 32; mine && col < m16; col += 64) {
+            float v[32];
+            ptx::tmem_load32(v, lanes + col);
+            ptx::tmem_load_wait();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) v[k] *= gram;
+#pragma unroll
+            for (int k = 0; k < 32; k += 8)
+                if (col + k < m16) write8(aw, col + k, v + k);
+        }
+        if (!product(tmem + 128, as, as, false, m16 / 16, square)) break;
+        for (int col = half * 32; mine && col < m16; col += 64) {
+            float v[32], w[32];
+            ptx::tmem_load32(v, lanes + col);
+            ptx::tmem_load32(w, lanes + 128 + col);
+            ptx::tmem_load_wait();
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+                v[k] = poly.b * (gram * v[k]) + poly.c / kScale * w[k] + (row == col + k && row < m ? poly.a * kScale : 0.0f);
+#pragma unroll
+            for (int k = 0; k < 32; k += 8)
+                if (col + k < m16) write8(aw, col + k, v + k);
+        }
+        if (!product(tmem + 256, as, xs, true, m16 / 16, wide)) break;
+        const float factor = (last ? g.scale * now : now / next) / kScale;
+        for (int col = half * 32; mine && col < n16; col += 64) {
+            float v[32];
+            ptx::tmem_load32(v, lanes + 256 + col);
+            ptx::tmem_load_wait();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) v[k] *= factor;
+            if (!last) {  // rows of padding keep their zeros: what they hold in tensor memory is not a product of anything
+#pragma unroll
+                for (int k = 0; k < 32; k += 8)
+                    if (row < m && col + k < n16) write8(xw, col + k, v + k);
+                continue;
+            }
+            if (g.tall) {  // lanes lie along the caller's columns
+                if (row < m)
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (col + k < n) to[(col + k) * g.out_pitch + row] = narrow<T>(v[k]);
+            } else {  // through shared memory (B is done with), so that a row's columns are written side by side
+                float* staging = reinterpret_cast<float*>(aw[0]) + warp * 32 * kStagePitch;
+#pragma unroll
+                for (int k = 0; k < 32; ++k) staging[lane * kStagePitch + k] = v[k];
+                __syncwarp();
+                if (col + lane < n)
+                    for (int r = 0; r < 32 && quad * 32 + r < m; ++r) to[(quad * 32 + r) * g.out_pitch + col + lane] = narrow<T>(staging[r * kStagePitch + lane]);
+                __syncwarp();
+            }
+        }
+    }
+    if (g.steps == 0) {
+        for (int i = warp; i < g.rows; i += kSmallThreads / 32)
+            for (int j = lane; j < g.cols; j += 32)
+                to[i * g.out_pitch + j] = narrow<T>(up(widen(from[i * g.in_pitch + j])) * (scale.u * g.scale));
+    }
+    ptx::fence_before();
+    __syncthreads();
+    if (warp == 0) {
+        ptx::fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    }
+}
+
+template <class T>
+cudaError_t small_typed(const OrthogonalizeArgs& a, cudaStream_t s) {
+    SmallArgs g{a.in_stride, a.in_pitch, a.out_stride, a.out_pitch, (int)a.rows, (int)a.cols, a.steps, a.rows > a.cols, {a.ca, a.cb, a.cc, 0},
+                a.eps, a.scale, nullptr};
+    cudaError_t e = gave_up_flag(&g.gave_up);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_small<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
+    if (e != cudaSuccess) return e;
+    launch_chained(k_small<T>, dim3((unsigned)a.n_mats), kSmallThreads, kSmallSmem, s, static_cast<const T*>(a.in), static_cast<T*>(a.out), g);
+    return cudaGetLastError();
+}
+
+bool is_small(int64_t rows, int64_t cols) { return std::min(rows, cols) <= kSmallM && std::max(rows, cols) <= kSmallN; }
+
 }  // namespace
 
-bool orthogonalize_range(double a, double b, double c, int steps, double* center) {
-    // singular values start in [0, 1]; how far each step's polynomial takes them, on a grid
-    double reach = 1.0, low = 0.0, high = 0.0;
-    *center = a;
+bool orthogonalize_range(double a, double b, double c, int steps) {
+    // singular values start in [0, 1]; x p(x^2), p(s) = a + b s + c s^2, takes them step by step to at most its extremes: at the end
+    // of the interval and where a + 3 b s + 5 c s^2 = 0. p's own extremes: at both ends and at s = -b / 2c.
+    auto p = [&](double s) { return std::abs(a + b * s + c * s * s); };
+    double reach = 1.0;
     for (int step = 0; step < steps; ++step) {
-        double next = reach;
-        low = high = 0.0;
-        for (int k = 0; k <= 4096; ++k) {
-            const double x = reach * k / 4096, s = x * x, p = b * s + c * s * s;
-            low = std::min(low, p);
-            high = std::max(high, p);
-            next = std::max(next, std::abs(x * (a + p)));
+        const double end = reach * reach, turn = c != 0.0 ? -b / (2 * c) : -1.0;
+        if (!(p(0.0) <= kMostPoly && p(end) <= kMostPoly && !(turn > 0.0 && turn < end && p(turn) > kMostPoly))) return false;
+        double roots[2] = {b != 0.0 ? -a / (3 * b) : -1.0, -1.0};
+        const double disc = 9 * b * b - 20 * a * c;
+        if (c != 0.0) {
+            roots[0] = disc >= 0.0 ? (-3 * b + std::sqrt(disc)) / (10 * c) : -1.0;
+            roots[1] = disc >= 0.0 ? (-3 * b - std::sqrt(disc)) / (10 * c) : -1.0;
         }
-        *center = a + (low + high) / 2;
-        if (!(next <= kMostSingular) || !((high - low) / 2 <= kMostPoly)) return false;
+        double next = std::max(reach, reach * p(end));
+        for (double s : roots)
+            if (s > 0.0 && s < end) next = std::max(next, std::sqrt(s) * p(s));
+        if (!(next <= kMostSingular)) return false;
         if (next == reach) break;
         reach = next;
     }
@@ -363,10 +574,11 @@ bool orthogonalize_range(double a, double b, double c, int steps, double* center
 }
 
 int64_t orthogonalize_workspace(int64_t n_mats, int64_t rows, int64_t cols, int32_t dtype) {
-    return layout(n_mats, rows, cols, dtype, nullptr, nullptr);
+    return is_small(rows, cols) ? 0 : layout(n_mats, rows, cols, dtype, nullptr, nullptr);
 }
 
 cudaError_t run_orthogonalize(const OrthogonalizeArgs& a, void* workspace, cudaStream_t s) {
+    if (is_small(a.rows, a.cols)) return a.dtype == A2_BF16 ? small_typed<__nv_bfloat16>(a, s) : small_typed<float>(a, s);
     Layout l;
     layout(a.n_mats, a.rows, a.cols, a.dtype, workspace, &l);
     return a.dtype == A2_BF16 ? typed<__nv_bfloat16>(a, l, s) : typed<float>(a, l, s);

@@ -22,24 +22,14 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return y;
 }
 
-// Scalars found by k_scan, as bits of non-negative floats (their order is that of the bits).
+// Largest finite magnitudes, as bits of non-negative floats (their order is that of the bits): of a CTA of k_scan, or of all.
 struct Scan {
-    uint32_t hidden, head, weight;  // largest finite magnitude of each
+    uint32_t hidden, head, weight, unused;
 };
+constexpr int kScanCtas = 148, kScanThreads = 1024;
 
 // The power of two that puts `amax` into [2^14, 2^15).
 __device__ __forceinline__ int word_exponent(uint32_t amax_bits) { return amax_bits ? 14 - ilogbf(__uint_as_float(amax_bits)) : 0; }
-
-// v * 2^e in two factors, so that no intermediate leaves the range unless the result does.
-struct PowerOfTwo {
-    float a, b;
-    __device__ __forceinline__ explicit PowerOfTwo(int e) {
-        e = max(-250, min(250, e));
-        a = ldexpf(1.0f, e / 2);
-        b = ldexpf(1.0f, e - e / 2);
-    }
-    __device__ __forceinline__ float operator()(float v) const { return v * a * b; }
-};
 
 __device__ __forceinline__ bool is_token(int32_t y, int64_t vocab) { return y >= 0 && y < vocab; }
 
@@ -51,10 +41,12 @@ struct PrepareArgs {
     const float* weights;
     int64_t n, width, vocab, hidden_pitch, head_pitch;
     Scan* scan;          // NULL: neither fp32 rows nor weights
+    Scan* scan_parts;    // [kScanCtas]
     void *h0, *h1;       // hidden's words [n, ld] (h1 NULL with bf16 rows), or NULL: not wanted
     void *w0, *w1;       // head's words [vocab, ld], or NULL
     int64_t ld;
     float* rate;         // g_t / max |g|, 0 for tokens without a target; NULL without gradients
+    bool hidden_pairs, head_pairs;  // pairs of columns can be read at once
     int32_t* poisoned;   // tokens without a target whose hidden row is not finite: the row is taken as zero, its lse as NaN
 };
 
@@ -62,6 +54,7 @@ template <class T>
 __device__ __forceinline__ uint32_t scan_rows(const T* p, int64_t rows, int64_t width, int64_t pitch, int64_t warp, int64_t warps) {
     uint32_t most = 0;
     for (int64_t r = warp; r < rows; r += warps)
+#pragma unroll 8
         for (int64_t c = threadIdx.x % 32; c < width; c += 32) {
             const uint32_t bits = __float_as_uint(fabsf(widen(p[r * pitch + c])));
             if (bits < 0x7f800000u) most = max(most, bits);
@@ -69,48 +62,81 @@ __device__ __forceinline__ uint32_t scan_rows(const T* p, int64_t rows, int64_t 
     return most;
 }
 
-__device__ __forceinline__ void publish(uint32_t most, uint32_t* to) {
-    most = __reduce_max_sync(0xffffffffu, most);
-    if (threadIdx.x % 32 == 0 && most) atomicMax(to, most);
-}
-
-// Largest finite magnitudes. The head's and hidden's are needed for fp32 rows alone.
+// The head's and hidden's are needed for fp32 rows alone.
 template <class T>
-__global__ void __launch_bounds__(256) k_scan(PrepareArgs a) {
-    const int64_t warp = (int64_t)blockIdx.x * 8 + threadIdx.x / 32, warps = (int64_t)gridDim.x * 8;
+__global__ void __launch_bounds__(kScanThreads) k_scan(PrepareArgs a) {
+    ptx::chained();
+    __shared__ Scan warps_found[kScanThreads / 32];
+    const int64_t warp = (int64_t)blockIdx.x * (kScanThreads / 32) + threadIdx.x / 32, warps = (int64_t)gridDim.x * (kScanThreads / 32);
+    Scan most{};
     if (sizeof(T) == 4) {
-        publish(scan_rows(static_cast<const T*>(a.hidden), a.n, a.width, a.hidden_pitch, warp, warps), &a.scan->hidden);
-        publish(scan_rows(static_cast<const T*>(a.head), a.vocab, a.width, a.head_pitch, warp, warps), &a.scan->head);
+        most.hidden = scan_rows(static_cast<const T*>(a.hidden), a.n, a.width, a.hidden_pitch, warp, warps);
+        most.head = scan_rows(static_cast<const T*>(a.head), a.vocab, a.width, a.head_pitch, warp, warps);
     }
-    if (a.weights) {
-        uint32_t most = 0;
+    if (a.weights)
         for (int64_t t = warp * 32 + threadIdx.x % 32; t < a.n; t += warps * 32) {
             const uint32_t bits = __float_as_uint(fabsf(a.weights[t]));
-            if (is_token(a.targets[t], a.vocab) && bits < 0x7f800000u) most = max(most, bits);
+            if (is_token(a.targets[t], a.vocab) && bits < 0x7f800000u) most.weight = max(most.weight, bits);
         }
-        publish(most, &a.scan->weight);
+    auto reduce = [](Scan& m) {
+        m.hidden = __reduce_max_sync(0xffffffffu, m.hidden);
+        m.head = __reduce_max_sync(0xffffffffu, m.head);
+        m.weight = __reduce_max_sync(0xffffffffu, m.weight);
+    };
+    reduce(most);
+    if (threadIdx.x % 32 == 0) warps_found[threadIdx.x / 32] = most;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        most = threadIdx.x < kScanThreads / 32 ? warps_found[threadIdx.x] : Scan{};
+        reduce(most);
+        if (threadIdx.x == 0) a.scan_parts[blockIdx.x] = most;
     }
 }
 
-__device__ __forceinline__ void split_words(float x, __half& hi, __half& lo) {
-    hi = __float2half_rn(x);
-    const float back = __half2float(hi);
-    lo = __float2half_rn(isfinite(back) ? x - back : 0.0f);
+// The largest of the parts, by every warp for itself.
+__device__ __forceinline__ Scan join_scan(const Scan* parts) {
+    Scan most{};
+    for (int p = threadIdx.x % 32; p < kScanCtas; p += 32) {
+        const Scan s = parts[p];
+        most.hidden = max(most.hidden, s.hidden);
+        most.head = max(most.head, s.head);
+        most.weight = max(most.weight, s.weight);
+    }
+    most.hidden = __reduce_max_sync(0xffffffffu, most.hidden);
+    most.head = __reduce_max_sync(0xffffffffu, most.head);
+    most.weight = __reduce_max_sync(0xffffffffu, most.weight);
+    return most;
+}
+
+// Two columns a lane, so that a warp's stores are 128 bytes; `aligned`: the pairs can be read at once.
+template <class T>
+__device__ __forceinline__ void pack_row(const T* from, bool aligned, void* to0, void* to1, int64_t at, int64_t width, int64_t ld, int e, bool zero) {
+    const PowerOfTwo up(e);
+#pragma unroll 4
+    for (int64_t c = threadIdx.x % 32 * 2; c < width; c += 64) {
+        Pack<T, 2> x;
+        if (aligned && c + 1 < width) {
+            x = *reinterpret_cast<const Pack<T, 2>*>(from + c);
+        } else {
+            x.v[0] = from[c];
+            x.v[1] = c + 1 < width ? from[c + 1] : narrow<T>(0.0f);
+        }
+        if (zero) x.v[0] = x.v[1] = narrow<T>(0.0f);
+        if constexpr (sizeof(T) == 4) {
+            Pack<__half, 2> h, l;
+            split_words(up(x.v[0]), h.v[0], l.v[0]);
+            split_words(up(x.v[1]), h.v[1], l.v[1]);
+            *reinterpret_cast<Pack<__half, 2>*>(static_cast<__half*>(to0) + at * ld + c) = h;  // ld is even: the second one may be padding
+            *reinterpret_cast<Pack<__half, 2>*>(static_cast<__half*>(to1) + at * ld + c) = l;
+        } else {
+            *reinterpret_cast<Pack<T, 2>*>(static_cast<T*>(to0) + at * ld + c) = x;
+        }
+    }
 }
 
 template <class T>
-__device__ __forceinline__ void pack_row(const T* from, void* to0, void* to1, int64_t at, int64_t width, int64_t ld, int e, bool zero) {
-    for (int64_t c = threadIdx.x % 32; c < width; c += 32) {
-        const float x = zero ? 0.0f : widen(from[c]);
-        if constexpr (sizeof(T) == 4) {
-            __half hi, lo;
-            split_words(scalbnf(x, e), hi, lo);
-            static_cast<__half*>(to0)[at * ld + c] = hi;
-            static_cast<__half*>(to1)[at * ld + c] = lo;
-        } else {
-            static_cast<__nv_bfloat16*>(to0)[at * ld + c] = narrow<__nv_bfloat16>(x);
-        }
-    }
+bool pairs_aligned(const void* p, int64_t pitch) {
+    return reinterpret_cast<uintptr_t>(p) % (2 * sizeof(T)) == 0 && pitch % 2 == 0;
 }
 
 // The operands of the products in the workspace, a warp a row: two words of fp32 rows, a copy of bf16 ones where
@@ -118,25 +144,35 @@ __device__ __forceinline__ void pack_row(const T* from, void* to0, void* to1, in
 // becomes zero when it holds anything that is not finite.
 template <class T>
 __global__ void __launch_bounds__(256) k_pack(PrepareArgs a) {
+    ptx::chained();
     const int64_t warp = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
-    if (warp < a.n) {
-        const bool live = is_token(a.targets[warp], a.vocab);
-        if (a.rate && threadIdx.x % 32 == 0) {
-            const float most = a.weights ? __uint_as_float(a.scan->weight) : 1.0f;
-            a.rate[warp] = !live ? 0.0f : !a.weights ? 1.0f : most > 0.0f ? a.weights[warp] / most : a.weights[warp];
+    Scan scan{};
+    if (a.scan) {
+        scan = join_scan(a.scan_parts);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.scan = scan;  // for the epilogues
+    }
+    const int64_t rows = a.n + (a.w0 ? a.vocab : 0);
+    for (int64_t r = warp; r < rows; r += (int64_t)gridDim.x * 8) {
+        if (r >= a.n) {
+            const int64_t v = r - a.n;
+            pack_row(static_cast<const T*>(a.head) + v * a.head_pitch, a.head_pairs, a.w0, a.w1, v, a.width, a.ld, a.w1 ? word_exponent(scan.head) : 0,
+                     false);
+            continue;
         }
-        if (!a.h0) return;
-        const T* from = static_cast<const T*>(a.hidden) + warp * a.hidden_pitch;
+        const bool live = is_token(a.targets[r], a.vocab);
+        if (a.rate && threadIdx.x % 32 == 0) {
+            const float most = a.weights ? __uint_as_float(scan.weight) : 1.0f;
+            a.rate[r] = !live ? 0.0f : !a.weights ? 1.0f : most > 0.0f ? a.weights[r] / most : a.weights[r];
+        }
+        if (!a.h0) continue;
+        const T* from = static_cast<const T*>(a.hidden) + r * a.hidden_pitch;
         bool bad = false;
         if (!live) {
             for (int64_t c = threadIdx.x % 32; c < a.width; c += 32) bad |= !isfinite(widen(from[c]));
             bad = __any_sync(0xffffffffu, bad);
         }
-        if (threadIdx.x % 32 == 0) a.poisoned[warp] = bad;
-        pack_row(from, a.h0, a.h1, warp, a.width, a.ld, a.h1 ? word_exponent(a.scan->hidden) : 0, bad);
-    } else if (a.w0 && warp - a.n < a.vocab) {
-        const int64_t v = warp - a.n;
-        pack_row(static_cast<const T*>(a.head) + v * a.head_pitch, a.w0, a.w1, v, a.width, a.ld, a.w1 ? word_exponent(a.scan->head) : 0, false);
+        if (threadIdx.x % 32 == 0) a.poisoned[r] = bad;
+        pack_row(from, a.hidden_pairs, a.h0, a.h1, r, a.width, a.ld, a.h1 ? word_exponent(scan.hidden) : 0, bad);
     }
 }
 
@@ -156,7 +192,7 @@ struct StatisticsEpi {
     int64_t target;
     float top = -INFINITY, sum = 0.0f;
     PowerOfTwo unscale;
-    __device__ __forceinline__ StatisticsEpi(const Args& args, int, int row0, int col, int lane, float*)
+    __device__ __forceinline__ StatisticsEpi(const Args& args, const Tile& t, int row0, int col, int lane, float*)
         : a(args), row((int64_t)row0 + lane), col0(col), unscale(kWords ? -(word_exponent(args.scan->hidden) + word_exponent(args.scan->head)) : 0) {
         target = row < a.n ? a.targets[row] : -1;
     }
@@ -205,12 +241,20 @@ struct ProbabilityEpi {
         int64_t n, vocab, v0;
     };
     const Args& a;
-    int64_t row, col0;
+    int64_t row0, row, col0;
     int64_t target;
+    int lane;
+    float* staging;
     float lse = 0.0f, rate = 0.0f;
     PowerOfTwo unscale;
-    __device__ __forceinline__ ProbabilityEpi(const Args& args, int, int row0, int col, int lane, float*)
-        : a(args), row((int64_t)row0 + lane), col0(col), unscale(kWords ? -(word_exponent(args.scan->hidden) + word_exponent(args.scan->head)) : 0) {
+    __device__ __forceinline__ ProbabilityEpi(const Args& args, const Tile& t, int row_, int col, int lane_, float* staging_)
+        : a(args),
+          row0(row_),
+          row((int64_t)row_ + lane_),
+          col0(col),
+          lane(lane_),
+          staging(staging_),
+          unscale(kWords ? -(word_exponent(args.scan->hidden) + word_exponent(args.scan->head)) : 0) {
         target = -1;
         if (row < a.n) {
             lse = a.lse[row];
@@ -221,7 +265,7 @@ struct ProbabilityEpi {
         }
     }
     __device__ __forceinline__ void chunk(int c, float (&v)[32]) {
-        if (row >= a.n) return;
+        if (row0 >= a.n) return;
         const int64_t col = col0 + c * 32;
         const bool live = target >= 0 || rate != 0.0f;
 #pragma unroll
@@ -231,109 +275,137 @@ struct ProbabilityEpi {
             p = rate * (target == col + k ? p - 1.0f : p);
             v[k] = live ? p : 0.0f;
         }
-        const int64_t at = row * a.ld + col;
+        const int64_t at = row0 * a.ld + col;
+        const int rows = (int)min((int64_t)32, a.n - row0);
         if constexpr (kWords) {
-            Pack<__half, 16> hi, lo;
+            __half hi[32], lo[32];
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-#pragma unroll
-                for (int k = 0; k < 16; ++k) split_words(v[g * 16 + k] * (float)(1 << kPScale), hi.v[k], lo.v[k]);
-                *reinterpret_cast<Pack<__half, 16>*>(static_cast<__half*>(a.p0) + at + g * 16) = hi;
-                *reinterpret_cast<Pack<__half, 16>*>(static_cast<__half*>(a.p1) + at + g * 16) = lo;
-            }
+            for (int k = 0; k < 32; k += 2)
+                split_pair(v[k] * (float)(1 << kPScale), v[k + 1] * (float)(1 << kPScale), hi[k], hi[k + 1], lo[k], lo[k + 1]);
+            store_rows16(staging, hi, static_cast<__half*>(a.p0) + at, a.ld, rows, lane);
+            store_rows16(reinterpret_cast<char*>(staging) + 2048, lo, static_cast<__half*>(a.p1) + at, a.ld, rows, lane);
         } else {
-            Pack<__nv_bfloat16, 16> o;
+            __nv_bfloat16 o[32];
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-#pragma unroll
-                for (int k = 0; k < 16; ++k) o.v[k] = narrow<__nv_bfloat16>(v[g * 16 + k]);
-                *reinterpret_cast<Pack<__nv_bfloat16, 16>*>(static_cast<__nv_bfloat16*>(a.p0) + at + g * 16) = o;
-            }
+            for (int k = 0; k < 32; ++k) o[k] = narrow<__nv_bfloat16>(v[k]);
+            store_rows16(staging, o, static_cast<__nv_bfloat16*>(a.p0) + at, a.ld, rows, lane);
         }
     }
     __device__ __forceinline__ void finish() {}
 };
 
-// A gradient's tile: out = factor * (sums of the earlier pieces + this one), or those sums kept for the next piece.
+// What turns a gradient's sums into the gradient: the words' scales, the caller's, and the largest weight.
+struct GradientScale {
+    const Scan* scan;
+    bool of_hidden;  // the other operand is head (grad_hidden) or hidden (grad_head)
+    bool weighted;
+    float scale;
+};
+template <class T>
+struct GradientFactor {
+    PowerOfTwo unscale;
+    float last;
+    static __device__ __forceinline__ int exponent(const GradientScale& s) {
+        return sizeof(T) == 4 ? -(kPScale + word_exponent(s.of_hidden ? s.scan->head : s.scan->hidden)) : 0;
+    }
+    __device__ __forceinline__ explicit GradientFactor(const GradientScale& s) : unscale(exponent(s)) {
+        const float most = s.weighted ? __uint_as_float(s.scan->weight) : 1.0f;
+        last = s.scale * (most > 0.0f ? most : 1.0f);
+    }
+    __device__ __forceinline__ T operator()(float v) const { return narrow<T>((sizeof(T) == 4 ? unscale(v) : v) * last); }
+};
+
+// A gradient's tile: out = factor * (sums of the earlier pieces + this one), or those sums kept for later.
 template <class T>
 struct GradientEpi {
     struct Args {
         T* out;  // NULL: keep
         int64_t pitch, rows, cols;
-        float* kept;  // [rows, kept_ld], or NULL with a single piece
+        float* kept;  // [parts of K][rows][kept_ld], or NULL with a single piece in one part
         int64_t kept_ld;
         bool add;  // kept holds earlier pieces
-        const Scan* scan;
-        bool of_hidden;  // which word scale the other operand has: grad_hidden's is head's
-        bool weighted;
-        float scale;
+        GradientScale scale;
     };
     const Args& a;
     int64_t row0, col0;
     int lane;
     float* staging;
-    float last;
-    PowerOfTwo unscale;
-    static __device__ __forceinline__ int exponent(const Args& a) {
-        if (sizeof(T) != 4) return 0;
-        return -(kPScale + word_exponent(a.of_hidden ? a.scan->head : a.scan->hidden));
-    }
-    __device__ __forceinline__ GradientEpi(const Args& args, int, int row, int col, int lane_, float* staging_)
-        : a(args), row0(row), col0(col), lane(lane_), staging(staging_), unscale(exponent(args)) {
-        const float most = a.weighted ? __uint_as_float(a.scan->weight) : 1.0f;
-        last = a.scale * (most > 0.0f ? most : 1.0f);
-    }
+    float* kept;
+    GradientFactor<T> factor;
+    __device__ __forceinline__ GradientEpi(const Args& args, const Tile& t, int row, int col, int lane_, float* staging_)
+        : a(args), row0(row), col0(col), lane(lane_), staging(staging_), kept(a.kept ? a.kept + t.split * a.rows * a.kept_ld : nullptr), factor(a.scale) {}
     __device__ __forceinline__ void chunk(int c, float (&v)[32]) {
-        const int64_t col = col0 + c * 32, row = row0 + lane;
-        if (a.kept && row < a.rows) {  // kept_ld is a multiple of 256: no column check
-            float* k = a.kept + row * a.kept_ld + col;
+        const int64_t col = col0 + c * 32 + lane;
+        if (row0 >= a.rows || col0 + c * 32 >= a.cols) return;
+        turn_columns(staging, v, lane);
+        if (col >= a.cols) return;
+        const int rows = (int)min((int64_t)32, a.rows - row0);
+        float* keep = kept + row0 * a.kept_ld + col;
+        if (a.add) {  // all loads before the first store
+            float before[32];
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                Pack<float, 8>* at = reinterpret_cast<Pack<float, 8>*>(k + g * 8);
-                Pack<float, 8> o;
-                if (a.add) o = *at;
+            for (int r = 0; r < 32; ++r) before[r] = r < rows ? keep[r * a.kept_ld] : 0.0f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o.v[e] = v[g * 8 + e] = a.add ? o.v[e] + v[g * 8 + e] : v[g * 8 + e];
-                if (!a.out) *at = o;
+            for (int r = 0; r < 32; ++r) v[r] += before[r];
+        }
+        T* to = a.out + row0 * a.pitch + col;
+#pragma unroll
+        for (int r = 0; r < 32; ++r)
+            if (r < rows) {
+                if (a.out) to[r * a.pitch] = factor(v[r]);
+                else keep[r * a.kept_ld] = v[r];
             }
-        }
-        if (!a.out) return;
-        // through shared memory, so that a row's 32 columns are written side by side whatever the alignment
-#pragma unroll
-        for (int k = 0; k < 32; ++k) staging[lane * kStagePitch + k] = sizeof(T) == 4 ? unscale(v[k]) * last : v[k] * last;
-        __syncwarp();
-        if (col + lane < a.cols) {
-            T* to = a.out + row0 * a.pitch + col + lane;
-            const int rows = (int)min((int64_t)32, a.rows - row0);
-#pragma unroll 8
-            for (int r = 0; r < rows; ++r) to[r * a.pitch] = narrow<T>(staging[r * kStagePitch + lane]);
-        }
-        __syncwarp();
     }
     __device__ __forceinline__ void finish() {}
 };
 
-// Joins the statistics of the parts: 32 tokens a CTA, eight warps over the parts.
-__global__ void __launch_bounds__(256) k_finish(const float2* __restrict__ partial, int parts, const float* __restrict__ at_target,
+// Adds up the parts of K of a gradient, in order.
+template <class T>
+__global__ void __launch_bounds__(256) k_join_parts(const float* __restrict__ kept, int parts, int64_t kept_ld, int64_t some, int64_t rows, int64_t cols, T* __restrict__ out,
+                                                    int64_t pitch, GradientScale scale) {
+    ptx::chained();
+    const GradientFactor<T> factor(scale);
+    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x, r = blockIdx.y;
+    if (c >= cols || r >= some) return;
+    float sum = 0.0f;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) sum += kept[(p * rows + r) * kept_ld + c];
+    out[r * pitch + c] = factor(sum);
+}
+
+// Joins the statistics of the parts: 32 tokens a CTA, its warps over the parts.
+constexpr int kFinishWarps = 16;
+__global__ void __launch_bounds__(kFinishWarps * 32) k_finish(const float2* __restrict__ partial, int parts, const float* __restrict__ at_target,
                                                 const int32_t* __restrict__ targets, const int32_t* __restrict__ poisoned, int64_t n, int64_t vocab,
                                                 float* __restrict__ loss, float* __restrict__ lse) {
-    __shared__ float2 joined[8][32];
+    ptx::chained();
+    __shared__ float2 joined[kFinishWarps][32];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int64_t t = (int64_t)blockIdx.x * 32 + lane;
     float top = -INFINITY, sum = 0.0f;
-    auto join = [&](float2 p) {
-        const float next = fmaxf(top, p.x);
+    // eight parts at a time: their loads and exponentials do not wait for one another
+    for (int p0 = warp; t < n && p0 < parts; p0 += 8 * kFinishWarps) {
+        float2 p[8];
+        float next = top;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int at = p0 + k * kFinishWarps;
+            p[k] = at < parts ? partial[(int64_t)at * n + t] : make_float2(-INFINITY, 0.0f);
+            next = fmaxf(next, p[k].x);
+        }
         const float base = next == -INFINITY ? 0.0f : next;
-        sum = sum * exp2_fast((top - base) * kLog2E) + p.y * exp2_fast((p.x - base) * kLog2E);
+        sum *= exp2_fast((top - base) * kLog2E);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += p[k].y * exp2_fast((p[k].x - base) * kLog2E);
         top = next;
-    };
-    if (t < n)
-#pragma unroll 4
-        for (int p = warp; p < parts; p += 8) join(partial[(int64_t)p * n + t]);
+    }
     joined[warp][lane] = make_float2(top, sum);
     __syncthreads();
     if (warp == 0 && t < n) {
-        for (int w = 1; w < 8; ++w) join(joined[w][lane]);
+        for (int w = 1; w < kFinishWarps; ++w) top = fmaxf(top, joined[w][lane].x);
+        const float base = top == -INFINITY ? 0.0f : top;
+        sum = 0.0f;
+        for (int w = 0; w < kFinishWarps; ++w) sum += joined[w][lane].y * exp2_fast((joined[w][lane].x - base) * kLog2E);
         const float l = poisoned && poisoned[t] ? NAN : top + logf(sum);
         lse[t] = l;
         loss[t] = is_token(targets[t], vocab) ? l - at_target[t] : 0.0f;
@@ -341,21 +413,24 @@ __global__ void __launch_bounds__(256) k_finish(const float2* __restrict__ parti
 }
 
 // ---- layout and launches ------------------------------------------------------------------------
-constexpr int kFlush = 8;  // K blocks a promoted sum stays in tensor memory: 32 steps of the tensor core
+// K blocks a promoted sum stays in tensor memory: 16 steps of the tensor core with fp32 rows, 64 for the loss of bf16 rows
+constexpr int kFlush = 4, kFlushLoss = 16;
 
 struct Layout {
-    Scan* scan;
+    Scan *scan, *scan_parts;
     void *h0, *h1, *w0, *w1, *p0, *p1;
     float2* partial;
-    float *at_target, *rate, *kept;
+    float *at_target, *rate, *kept, *head_kept;
     int32_t* poisoned;
     int64_t ld, p_ld, kept_ld, piece;
+    int hidden_parts, head_parts;  // of K, in the gradients' products
 };
 
 // Vocabulary rows of a piece: as many as keep P within kPieceBytes, fewer where that fills the pairs of CTAs better.
 // Cost in units of (tile of 256 x 256) x (K of 256) a pair.
 constexpr int64_t kPieceBytes = 160ll << 20;
 constexpr int64_t kPairs = 74;
+constexpr int64_t kLeastBlocks = 8;  // of K in a part: less would leave its tile mostly epilogue
 int64_t piece_rows(int64_t n, int64_t width, int64_t vocab, int64_t words) {
     const int64_t tm = std::max<int64_t>(1, ceil_div(n, kTileM)), tw = ceil_div(width, kTileN), tv = ceil_div(vocab, kTileN);
     const int64_t most = std::min(tv, std::max<int64_t>(1, kPieceBytes / (tm * kTileM * kTileN * 2 * words)));
@@ -374,6 +449,7 @@ int64_t layout(int64_t n, int64_t width, int64_t vocab, bool with_grad, int32_t 
     Layout l{};
     l.ld = round_up(width, 64);
     l.scan = w.take<Scan>(1);
+    l.scan_parts = w.take<Scan>(kScanCtas);
     l.h0 = w.take<uint16_t>(n * l.ld);
     l.w0 = w.take<uint16_t>(vocab * l.ld);
     if (words == 2) {
@@ -390,7 +466,12 @@ int64_t layout(int64_t n, int64_t width, int64_t vocab, bool with_grad, int32_t 
         l.p0 = w.take<uint16_t>(n * l.p_ld);
         if (words == 2) l.p1 = w.take<uint16_t>(n * l.p_ld);
         l.kept_ld = round_up(width, kTileN);
-        if (l.piece < vocab) l.kept = w.take<float>(n * l.kept_ld);
+        const int64_t rows = std::min(l.piece, vocab), across = ceil_div(width, kTileN);
+        l.hidden_parts = split_parts(ceil_div(n, kTileM) * across, ceil_div(rows, kBlockK), kPairs, kLeastBlocks);
+        l.head_parts = split_parts(ceil_div(rows, kTileM) * across, ceil_div(n, kBlockK), kPairs, kLeastBlocks);
+        const int64_t keep = l.piece < vocab || l.hidden_parts > 1 ? n * l.hidden_parts : 0;
+        l.kept = w.take<float>(keep * l.kept_ld);
+        l.head_kept = w.take<float>(l.head_parts > 1 ? rows * l.head_parts * l.kept_ld : 0);
     }
     if (out) *out = l;
     return w.used;
@@ -410,20 +491,19 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
     auto in_place = [](const void* p, int64_t pitch) { return !kWords && reinterpret_cast<uintptr_t>(p) % 16 == 0 && pitch % 8 == 0; };
     const bool hidden_in_place = in_place(a.hidden, a.hidden_pitch) && !a.grad_head;
     const bool head_in_place = in_place(a.head, a.head_pitch);
-    PrepareArgs prep{a.hidden, a.head, a.targets, a.weights, n, a.width, a.vocab, a.hidden_pitch, a.head_pitch, nullptr, nullptr, nullptr,
-                     nullptr,  nullptr, l.ld, with_grad ? l.rate : nullptr, l.poisoned};
+    PrepareArgs prep{a.hidden, a.head, a.targets, a.weights, n, a.width, a.vocab, a.hidden_pitch, a.head_pitch, nullptr, l.scan_parts, nullptr, nullptr,
+                     nullptr, nullptr, l.ld, with_grad ? l.rate : nullptr, pairs_aligned<T>(a.hidden, a.hidden_pitch), pairs_aligned<T>(a.head, a.head_pitch),
+                     l.poisoned};
     const bool weighted = with_grad && a.weights;
     if (!with_grad) prep.weights = nullptr;
     if (kWords || weighted) prep.scan = l.scan;
     if (!hidden_in_place) prep.h0 = l.h0, prep.h1 = l.h1;
     if (!head_in_place) prep.w0 = l.w0, prep.w1 = l.w1;
     if (prep.scan) {
-        e = cudaMemsetAsync(l.scan, 0, sizeof(Scan), s);
-        if (e != cudaSuccess) return e;
-        const int64_t rows = kWords ? n + a.vocab : ceil_div(n, 32);
-        k_scan<T><<<(unsigned)std::min<int64_t>(ceil_div(rows, 8), 148 * 8), 256, 0, s>>>(prep);
+        launch_chained(k_scan<T>, dim3(kScanCtas), kScanThreads, 0, s, prep);
     }
-    if (prep.h0 || prep.w0 || prep.rate) k_pack<T><<<(unsigned)ceil_div(n + (prep.w0 ? a.vocab : 0), 8), 256, 0, s>>>(prep);
+    if (prep.h0 || prep.w0 || prep.rate)
+        launch_chained(k_pack<T>, dim3((unsigned)std::min<int64_t>(ceil_div(n + (prep.w0 ? a.vocab : 0), 8), 148 * 8)), 256, 0, s, prep);
 
     auto words = [&](const void* mine, void* w0, void* w1, bool here, int64_t pitch, int64_t row0, int64_t rows, int64_t cols, bool mn) {
         // rows x cols from row0 on; K-major: rows are M or N and columns K; MN-major: the other way round
@@ -438,40 +518,55 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
 
     GemmArgs g;
     // the loss is fp32 with either storage type, so its sums are promoted with both
-    e = make_gemm(hidden(false), head(0, a.vocab, false), 1, !kWords, false, kFlush, &g);
+    e = make_gemm(hidden(false), head(0, a.vocab, false), 1, !kWords, false, kWords ? kFlush : kFlushLoss, 1, &g);
     if (e != cudaSuccess) return e;
     const typename StatisticsEpi<kWords>::Args stats{l.partial, l.at_target, a.targets, l.scan, n, a.vocab};
     e = launch_gemm<StatisticsEpi<kWords>, true>(g, stats, s);
     if (e != cudaSuccess) return e;
-    k_finish<<<(unsigned)ceil_div(n, 32), 256, 0, s>>>(l.partial, (int)(2 * ceil_div(a.vocab, kTileN)), l.at_target, a.targets,
+    launch_chained(k_finish, dim3((unsigned)ceil_div(n, 32)), kFinishWarps * 32, 0, s, l.partial, (int)(2 * ceil_div(a.vocab, kTileN)), l.at_target, a.targets,
                                                       hidden_in_place ? nullptr : l.poisoned, n, a.vocab, a.loss, a.lse);
     if (!with_grad) return cudaGetLastError();
 
+    auto join = [&](const float* kept, int parts, int64_t rows, T* out, int64_t pitch, const GradientScale& scale) {
+        for (int64_t r = 0; r < rows; r += 65535) {  // the grid's second dimension ends there
+            const int64_t some = std::min<int64_t>(65535, rows - r);
+            launch_chained(k_join_parts<T>, dim3((unsigned)ceil_div(a.width, 256), (unsigned)some), 256, 0, s, kept + r * l.kept_ld, parts, l.kept_ld, some, rows, a.width,
+                                                                                                  out + r * pitch, pitch, scale);
+        }
+    };
     for (int64_t v0 = 0; v0 < a.vocab; v0 += l.piece) {
         const int64_t rows = std::min(l.piece, a.vocab - v0);
         const bool first = v0 == 0, final = v0 + rows == a.vocab;
-        e = make_gemm(hidden(false), head(v0, rows, false), 1, !kWords, false, flush, &g);
+        e = make_gemm(hidden(false), head(v0, rows, false), 1, !kWords, false, flush, 1, &g);
         if (e != cudaSuccess) return e;
         const typename ProbabilityEpi<kWords>::Args prob{l.p0, l.p1, l.p_ld, a.targets, a.lse, l.rate, l.scan, n, a.vocab, v0};
         e = launch_gemm<ProbabilityEpi<kWords>, kWords>(g, prob, s);
         if (e != cudaSuccess) return e;
         if (a.grad_head) {
             const Operand p{l.p0, l.p1, rows, n, l.p_ld, 0, true};
-            e = make_gemm(p, hidden(true), 1, !kWords, false, flush, &g);
+            const GradientScale scale{l.scan, false, weighted, a.scale};
+            T* out = static_cast<T*>(a.grad_head) + v0 * a.grad_head_pitch;
+            const bool parts = l.head_parts > 1;
+            e = make_gemm(p, hidden(true), 1, !kWords, false, flush, l.head_parts, &g);
             if (e != cudaSuccess) return e;
-            const typename GradientEpi<T>::Args grad{static_cast<T*>(a.grad_head) + v0 * a.grad_head_pitch, a.grad_head_pitch, rows, a.width, nullptr,
-                                                     0, false, l.scan, false, weighted, a.scale};
-            e = launch_gemm<GradientEpi<T>, kWords>(g, grad, s);
+            e = launch_gemm<GradientEpi<T>, kWords>(
+                g, {parts ? nullptr : out, a.grad_head_pitch, rows, a.width, l.head_kept, l.kept_ld, false, scale}, s);
             if (e != cudaSuccess) return e;
+            if (parts) join(l.head_kept, l.head_parts, rows, out, a.grad_head_pitch, scale);
         }
         if (a.grad_hidden) {
             const Operand p{l.p0, l.p1, n, rows, l.p_ld, 0, false};
-            e = make_gemm(p, head(v0, rows, true), 1, !kWords, false, flush, &g);
+            const GradientScale scale{l.scan, true, weighted, a.scale};
+            T* out = static_cast<T*>(a.grad_hidden);
+            const bool parts = l.hidden_parts > 1;
+            // part p of every piece adds to the sums of part p; a short last piece may have fewer parts, but none without a block
+            const int here = (int)std::min<int64_t>(l.hidden_parts, ceil_div(rows, kBlockK));
+            e = make_gemm(p, head(v0, rows, true), 1, !kWords, false, flush, here, &g);
             if (e != cudaSuccess) return e;
-            const typename GradientEpi<T>::Args grad{final ? static_cast<T*>(a.grad_hidden) : nullptr, a.grad_hidden_pitch, n, a.width,
-                                                     first && final ? nullptr : l.kept, l.kept_ld, !first, l.scan, true, weighted, a.scale};
-            e = launch_gemm<GradientEpi<T>, kWords>(g, grad, s);
+            e = launch_gemm<GradientEpi<T>, kWords>(
+                g, {final && !parts ? out : nullptr, a.grad_hidden_pitch, n, a.width, l.kept, l.kept_ld, !first, scale}, s);
             if (e != cudaSuccess) return e;
+            if (final && parts) join(l.kept, l.hidden_parts, n, out, a.grad_hidden_pitch, scale);
         }
     }
     return cudaGetLastError();

@@ -436,8 +436,8 @@ def test_refusals():
     assert L.a2cid2_embed(p, 10, 8, 8, i, 1 << 31, 1.0, p, 8, B.A2_F32, s) == B.A2_ERANGE
     assert L.a2cid2_embed(p, 10, 1 << 21, 1 << 21, i, 1, 1.0, p, 1 << 21, B.A2_F32, s) == B.A2_ERANGE
     assert L.a2cid2_embed(p + 2, 10, 8, 8, i, 1, 1.0, p, 8, B.A2_F32, s) == B.A2_EINVAL
-    assert L.a2cid2_embed_grad(p, 8, i, 10, 10, 8, 1.0, 0, p, 8, B.A2_F32, w, 16, s) == B.A2_EINVAL and b"needed" in L.a2cid2_last_error(None)
-    assert L.a2cid2_embed_grad(p, 8, i, 10, 10, 8, 1.0, 0, p, 8, B.A2_F32, w + 8, 1 << 19, s) == B.A2_EINVAL
+    assert L.a2cid2_embed_grad(p, 8, i, 9000, 10, 8, 1.0, 0, p, 8, B.A2_F32, w, 16, s) == B.A2_EINVAL and b"needed" in L.a2cid2_last_error(None)
+    assert L.a2cid2_embed_grad(p, 8, i, 9000, 10, 8, 1.0, 0, p, 8, B.A2_F32, w + 8, 1 << 30, s) == B.A2_EINVAL
     assert L.a2cid2_vocab_loss(p, 8, p, 8, i, 10, 8, 10, None, 1.0, None, None, None, 0, None, 0, B.A2_F32, w, 1 << 20, s) == B.A2_EINVAL
     assert L.a2cid2_vocab_loss(p, 8, p, 8, i, 10, 8, 10, None, 1.0, p, p, None, 0, None, 0, 5, w, 1 << 20, s) == B.A2_EINVAL
     assert L.a2cid2_orthogonalize(p, 80, 8, 70000, 1, 1, 5, 1.0, 1.0, 1.0, 0.0, 1.0, p, 80, 8, B.A2_F32, w, 1 << 20, s) == B.A2_ERANGE
