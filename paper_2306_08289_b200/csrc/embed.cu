@@ -1,4 +1,6 @@
 // Embedding lookup y_t = s E[id_t] and its gradient dE_v (+)= s sum_{t: id_t = v} dy_t.
+#include <algorithm>
+
 #include "lm_ops.h"
 
 namespace a2 {
@@ -143,9 +145,30 @@ __device__ __forceinline__ int block_exclusive(int v, int* warp_sums) {
     return base + inc - v;
 }
 
+// Rows [first, last) of a table become zeros: the sort leaves most of the GPU idle, so each of its launches clears kZeroBytes of the
+// table in further CTAs, with or without positions (the sums overwrite those); the rest waits for k_segments, which knows which rows
+// have none.
+struct ZeroFill {
+    char* table;
+    int64_t first, last, row_bytes, pitch_bytes;
+    bool wide;  // 16-byte stores
+};
+__device__ __forceinline__ void zero_rows(const ZeroFill& z, int64_t cta, int64_t ctas) {
+    const int64_t warp = cta * kSortWarps + threadIdx.x / 32, warps = ctas * kSortWarps;
+    for (int64_t r = z.first + warp; r < z.last; r += warps) {
+        char* row = z.table + r * z.pitch_bytes;
+        if (z.wide)
+            for (int64_t b = threadIdx.x % 32 * 16; b < z.row_bytes; b += 512) *reinterpret_cast<uint4*>(row + b) = make_uint4(0, 0, 0, 0);
+        else
+            for (int64_t b = threadIdx.x % 32 * 2; b < z.row_bytes; b += 64) *reinterpret_cast<uint16_t*>(row + b) = 0;
+    }
+}
+
 // Counts of the first digit, per tile of kTile positions.
-__global__ void __launch_bounds__(kSortThreads) k_sort_count(const int32_t* __restrict__ ids, int64_t n, int64_t vocab, int passes, int* __restrict__ counts) {
+__global__ void __launch_bounds__(kSortThreads) k_sort_count(const int32_t* __restrict__ ids, int64_t n, int64_t vocab, int passes, int n_tiles, int* __restrict__ counts,
+                                                             const ZeroFill zero) {
     ptx::chained();
+    if ((int)blockIdx.x >= n_tiles) return zero_rows(zero, blockIdx.x - n_tiles, gridDim.x - n_tiles);
     __shared__ int c[kDigits];
     c[threadIdx.x] = 0;
     __syncthreads();
@@ -153,15 +176,16 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(const int32_t* __re
     for (int64_t i = first + threadIdx.x; i < min(first + kTile, n); i += kSortThreads) atomicAdd(&c[digit_of(sort_key(ids[i], vocab), 0)], 1);
     __syncthreads();
     for (int p = 0; p < passes; ++p)  // the later passes' counts are added up by the pass before
-        counts[((int64_t)p * gridDim.x + blockIdx.x) * kDigits + threadIdx.x] = p == 0 ? c[threadIdx.x] : 0;
+        counts[((int64_t)p * n_tiles + blockIdx.x) * kDigits + threadIdx.x] = p == 0 ? c[threadIdx.x] : 0;
 }
 
 // One pass: every tile adds up where its items go from the counts of all tiles, moves them, and counts the next
 // digit of the tiles they land in (integer sums: the order of the atomics does not show).
 __global__ void __launch_bounds__(kSortThreads) k_sort_pass(const int32_t* __restrict__ ids, const Pair* __restrict__ in, int64_t n, int64_t vocab,
                                                             int pass, bool last, const int* __restrict__ counts, int n_tiles,
-                                                            Pair* __restrict__ out, int* __restrict__ next_counts) {
+                                                            Pair* __restrict__ out, int* __restrict__ next_counts, const ZeroFill zero) {
     ptx::chained();
+    if ((int)blockIdx.x >= n_tiles) return zero_rows(zero, blockIdx.x - n_tiles, gridDim.x - n_tiles);
     __shared__ int count[kSortWarps * kDigits];
     __shared__ int base[kDigits];
     __shared__ int warp_sums[kSortWarps];
@@ -198,8 +222,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_pass(const int32_t* __res
 // Sums over the sorted positions. A group of threads takes a block of `span` sorted positions and a range of
 // columns; an id whose positions all lie in the block is finished there. What an id has in a block that it
 // enters or leaves half-way goes to `partial` ([block][2][width]: the id the block begins with, the id it ends
-// with), and k_join adds those up, block by block. Further CTAs of the same launch write the rows of ids that
-// have no position.
+// with), and k_join adds those up, block by block.
 // ---------------------------------------------------------------------------------------------
 constexpr int kAhead = 8;  // rows in flight a thread
 
@@ -212,17 +235,19 @@ __device__ __forceinline__ void finish_row(T* row, const float (&sum)[VEC], floa
     *reinterpret_cast<Pack<T, VEC>*>(row) = o;
 }
 
-constexpr int kZeroRows = 64;  // ids a CTA looks through for ones without a position
+constexpr int kZeroRows = 64;   // ids a CTA looks through for ones without a position
+constexpr unsigned kZeroCtas = 148 * 2;
+constexpr int64_t kZeroBytes = 32 << 20;  // about what a launch of the sort has time for
 
 template <class T, int VEC>
 __global__ void __launch_bounds__(kThreads) k_segments(const T* __restrict__ grad_out, int64_t grad_pitch, const Pair* __restrict__ sorted, int64_t n,
                                                        int64_t vocab, int64_t width, float scale, bool accumulate, T* __restrict__ table,
-                                                       int64_t table_pitch, float* __restrict__ partial, int span, int group, int64_t sum_ctas) {
+                                                       int64_t table_pitch, float* __restrict__ partial, int span, int group, int64_t sum_ctas, int64_t zero_first) {
     ptx::chained();
     const int64_t c = ((int64_t)blockIdx.y * group + threadIdx.x % group) * VEC;
     if ((int64_t)blockIdx.x >= sum_ctas) {  // rows without a position
         __shared__ unsigned char used[kZeroRows];
-        const int64_t v0 = ((int64_t)blockIdx.x - sum_ctas) * kZeroRows;
+        const int64_t v0 = zero_first + ((int64_t)blockIdx.x - sum_ctas) * kZeroRows;
         const int64_t v1 = min(v0 + kZeroRows, vocab);
         if (threadIdx.x < v1 - v0) {  // every thread looks one id up
             const uint32_t v = (uint32_t)(v0 + threadIdx.x);
@@ -325,117 +350,109 @@ __global__ void __launch_bounds__(kThreads) k_join(const Pair* __restrict__ sort
 }
 
 // ---------------------------------------------------------------------------------------------
-// Few positions: no sort. A CTA a position looks through all ids for its own: if the position is the first of its id, the
-// CTA lists the others in order and adds their rows up. n * n comparisons are less work than the launches of a sort up to a few
-// thousand positions. Further CTAs write the rows of ids that have none.
+// Few positions: no sort. A warp takes a position (and a range of columns), looks through all ids for its own, stops if an
+// earlier position has it, else adds up the rows of all positions that have it, in order, as it finds them. n * n comparisons, 128
+// at a time, are less work than the launches of a sort up to a few thousand positions. Further CTAs write the rows of ids that have
+// no position.
 // ---------------------------------------------------------------------------------------------
-constexpr int kDirectMost = 4096;
+constexpr int64_t kDirectMost = 8192;        // positions
+constexpr int64_t kDirectSearch = 60000000;  // comparisons: positions squared times the ranges of columns
 constexpr int kDirectThreads = 256;
-constexpr int kDirectRounds = kDirectMost / kDirectThreads;
+constexpr int kDirectWarps = kDirectThreads / 32;
+constexpr int kFound = 128 + 32;  // positions a warp holds before it adds their rows up: one round of 128 ids, and a remainder
 
 template <class T, int VEC>
-__global__ void __launch_bounds__(kDirectThreads) k_direct(const T* __restrict__ grad_out, int64_t grad_pitch, const int32_t* __restrict__ ids, int n,
+__global__ void __launch_bounds__(kDirectThreads, 4) k_direct(const T* __restrict__ grad_out, int64_t grad_pitch, const int32_t* __restrict__ ids, int n,
                                                            int64_t vocab, int64_t width, float scale, bool accumulate, T* __restrict__ table,
-                                                           int64_t table_pitch, int group) {
+                                                           int64_t table_pitch, int64_t sum_ctas) {
     ptx::chained();
-    __shared__ uint16_t list[kDirectMost];
-    __shared__ int counts[129];
-    __shared__ float joined[kDirectThreads * VEC];
-    const int tid = threadIdx.x, lane = tid % group, slot = tid / group, slots = kDirectThreads / group;
-    if ((int)blockIdx.x >= n) {  // rows without a position: flags of kZeroRows ids, in the list's space
-        const int64_t v0 = ((int64_t)blockIdx.x - n) * kZeroRows;
-        if (tid < kZeroRows) list[tid] = 0;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    constexpr int64_t kColumns = 32 * VEC;  // columns of a warp
+    if ((int64_t)blockIdx.x >= sum_ctas) {        // rows without a position
+        __shared__ unsigned char used[kZeroRows];
+        const int64_t v0 = ((int64_t)blockIdx.x - sum_ctas) * kZeroRows;
+        if (tid < kZeroRows) used[tid] = 0;
         __syncthreads();
+#pragma unroll 4
         for (int i = tid; i < n; i += kDirectThreads) {
             const int64_t v = ids[i] - v0;
-            if (v >= 0 && v < kZeroRows) list[v] = 1;
+            if (v >= 0 && v < kZeroRows) used[v] = 1;
         }
         __syncthreads();
         Pack<T, VEC> zero;
 #pragma unroll
         for (int k = 0; k < VEC; ++k) zero.v[k] = narrow<T>(0.0f);
-        for (int64_t v = slot; v < kZeroRows && v0 + v < vocab; v += slots)
-            if (!list[v])
-                for (int64_t c = (int64_t)lane * VEC; c < width; c += (int64_t)group * VEC)
-                    *reinterpret_cast<Pack<T, VEC>*>(table + (v0 + v) * table_pitch + c) = zero;
+        for (int v = warp; v < kZeroRows && v0 + v < vocab; v += kDirectWarps)
+            if (!used[v])
+                for (int64_t c = (int64_t)lane * VEC; c < width; c += 32 * VEC) *reinterpret_cast<Pack<T, VEC>*>(table + (v0 + v) * table_pitch + c) = zero;
         return;
     }
-    const int me = blockIdx.x;
+    __shared__ uint16_t found[kDirectWarps][kFound];
+    const int64_t ranges = (width + kColumns - 1) / kColumns;
+    const int64_t unit = (int64_t)blockIdx.x * kDirectWarps + warp;
+    if (unit >= n * ranges) return;
+    const int me = (int)(unit / ranges);
+    const int64_t c0 = unit % ranges * kColumns + (int64_t)lane * VEC;
     const int32_t id = ids[me];
     if (id < 0 || id >= vocab) return;
-    // round k of a thread is position k * kDirectThreads + tid
-    uint32_t found = 0;
-    bool earlier = false;
+    float sum[VEC] = {};
+    int held = 0;
+    const bool inside = c0 < width;
+    auto add = [&](int from, int count) {  // rows found[from .. from + count), count <= kAhead
+        Pack<T, VEC> r[kAhead];
 #pragma unroll
-    for (int k = 0; k < kDirectRounds; ++k) {
-        const int p = k * kDirectThreads + tid;
-        const bool hit = p < n && ids[p] == id;
-        found |= (hit ? 1u : 0u) << k;
-        earlier |= hit && p < me;
-    }
-    if (__syncthreads_or(earlier)) return;  // an earlier position does this id
-    // list them in order: counts by round and warp, their prefix sums, the place among the warp's
+        for (int a = 0; a < kAhead; ++a)
+            if (a < count && inside) r[a] = *reinterpret_cast<const Pack<T, VEC>*>(grad_out + (int64_t)found[warp][from + a] * grad_pitch + c0);
 #pragma unroll
-    for (int k = 0; k < kDirectRounds; ++k) {
-        const unsigned hits = __ballot_sync(0xffffffffu, found >> k & 1);
-        if (tid % 32 == 0) counts[k * (kDirectThreads / 32) + tid / 32] = __popc(hits);
+        for (int a = 0; a < kAhead; ++a)
+            if (a < count && inside)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum[e] += widen(r[a].v[e]);
+    };
+    // earlier positions: any hit, and this warp has nothing to do
+    for (int p0 = 0; p0 < me; p0 += 512) {
+        bool hit = false;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const int p = p0 + q * 32 + lane;
+            hit |= p < me && ids[p] == id;
+        }
+        if (__any_sync(0xffffffffu, hit)) return;
     }
-    __syncthreads();
-    if (tid < 32) {  // 128 counts, four a lane
-        static_assert(kDirectRounds * kDirectThreads / 32 == 128, "four counts a lane");
-        int c[4], sum = 0;
+    for (int p0 = me; p0 < n; p0 += 128) {
+        unsigned hits[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            c[q] = sum;
-            sum += counts[tid * 4 + q];
+            const int p = p0 + q * 32 + lane;
+            hits[q] = __ballot_sync(0xffffffffu, p < n && ids[p] == id);
         }
-        int inc = sum;
+        if (!(hits[0] | hits[1] | hits[2] | hits[3])) continue;
 #pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const int up = __shfl_up_sync(0xffffffffu, inc, o);
-            if (tid >= o) inc += up;
+        for (int q = 0; q < 4; ++q) {
+            if (hits[q] >> lane & 1) found[warp][held + __popc(hits[q] & ((1u << lane) - 1))] = (uint16_t)(p0 + q * 32 + lane);
+            held += __popc(hits[q]);
         }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) counts[tid * 4 + q] = inc - sum + c[q];
-        if (tid == 31) counts[128] = inc;
+        __syncwarp();
+        int done = 0;
+        for (; held - done >= kAhead; done += kAhead) add(done, kAhead);
+        const uint16_t rest = lane < held - done ? found[warp][done + lane] : (uint16_t)0;
+        __syncwarp();
+        if (lane < held - done) found[warp][lane] = rest;
+        held -= done;
     }
-    __syncthreads();
-    const int total = counts[128];
-#pragma unroll
-    for (int k = 0; k < kDirectRounds; ++k) {
-        const bool hit = found >> k & 1;
-        const unsigned hits = __ballot_sync(0xffffffffu, hit);
-        if (hit) list[counts[k * (kDirectThreads / 32) + tid / 32] + __popc(hits & ((1u << (tid % 32)) - 1))] = (uint16_t)(k * kDirectThreads + tid);
-    }
-    __syncthreads();
-    T* row = table + (int64_t)id * table_pitch;
-    for (int64_t c0 = 0; c0 < width; c0 += (int64_t)group * VEC) {
-        const int64_t c = c0 + (int64_t)lane * VEC;
-        float sum[VEC] = {};
-        if (c < width)  // a slot takes every slots-th row
-            for (int k = slot; k < total; k += slots * kAhead) {
-                Pack<T, VEC> r[kAhead];
-#pragma unroll
-                for (int a = 0; a < kAhead; ++a)
-                    if (k + a * slots < total) r[a] = *reinterpret_cast<const Pack<T, VEC>*>(grad_out + (int64_t)list[k + a * slots] * grad_pitch + c);
-#pragma unroll
-                for (int a = 0; a < kAhead; ++a)
-                    if (k + a * slots < total)
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) sum[e] += widen(r[a].v[e]);
-            }
-        if (slots > 1 && total > 1) {  // the slots' sums, in their order
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) joined[e * kDirectThreads + tid] = sum[e];
-            __syncthreads();
-            if (slot == 0)
-                for (int o = 1; o < slots; ++o)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) sum[e] += joined[e * kDirectThreads + o * group + lane];
-        }
-        if (slot == 0 && c < width) finish_row<T, VEC>(row + c, sum, scale, accumulate);
-    }
+    __syncwarp();
+    if (held > 0) add(0, held);
+    if (inside) finish_row<T, VEC>(table + (int64_t)id * table_pitch + c0, sum, scale, accumulate);
+}
+
+// Columns one thread takes at once: 16 bytes where the rows allow it.
+template <class T>
+int columns_a_thread(const EmbedGradArgs& a) {
+    constexpr int kVec = 16 / sizeof(T);
+    return a.width % kVec == 0 && aligned16(a.grad_out, a.grad_out_pitch, sizeof(T)) && aligned16(a.grad_table, a.grad_table_pitch, sizeof(T)) ? kVec : 1;
+}
+bool is_direct(int64_t n_ids, int64_t width, int vec) {
+    return n_ids <= kDirectMost && n_ids * n_ids * ceil_div(width, 32 * vec) <= kDirectSearch;
 }
 
 int sort_passes(int64_t vocab) {  // keys are 0 .. vocab
@@ -459,7 +476,7 @@ struct GradPlan {
 int64_t grad_layout(int64_t vocab, int64_t width, int64_t n_ids, void* workspace, GradPlan* out) {
     GradPlan p{};
     Carver w(workspace);
-    if (n_ids <= kDirectMost) {
+    if (is_direct(n_ids, width, 1)) {  // whatever the alignment
         if (out) *out = p;
         return 0;
     }
@@ -474,7 +491,7 @@ int64_t grad_layout(int64_t vocab, int64_t width, int64_t n_ids, void* workspace
 }
 
 template <class T, int VEC>
-cudaError_t segments_typed(const EmbedGradArgs& a, const GradPlan& p, cudaStream_t s) {
+cudaError_t segments_typed(const EmbedGradArgs& a, const GradPlan& p, int64_t zero_first, cudaStream_t s) {
     const int span = segment_span(a.n_ids);
     const int group = group_threads(a.width, VEC);
     const int64_t per_cta = kThreads / group;
@@ -483,10 +500,9 @@ cudaError_t segments_typed(const EmbedGradArgs& a, const GradPlan& p, cudaStream
     auto* g = static_cast<const T*>(a.grad_out);
     auto* table = static_cast<T*>(a.grad_table);
     const int64_t sum_ctas = ceil_div(blocks, per_cta);
-    const int64_t zero_ctas = a.accumulate ? 0 : ceil_div(a.vocab, kZeroRows);
-    launch_chained(k_segments<T, VEC>, dim3((unsigned)(sum_ctas + zero_ctas), (unsigned)col_ctas), kThreads, 0, s, 
-            g, a.grad_out_pitch, p.sorted, a.n_ids, a.vocab, a.width, a.scale, a.accumulate, table, a.grad_table_pitch, p.partial, span,
-            group, sum_ctas);
+    const int64_t zero_ctas = a.accumulate ? 0 : ceil_div(a.vocab - zero_first, kZeroRows);
+    launch_chained(k_segments<T, VEC>, dim3((unsigned)(sum_ctas + zero_ctas), (unsigned)col_ctas), kThreads, 0, s, g, a.grad_out_pitch, p.sorted, a.n_ids,
+                   a.vocab, a.width, a.scale, a.accumulate, table, a.grad_table_pitch, p.partial, span, group, sum_ctas, zero_first);
     launch_chained(k_join<T, VEC>, dim3((unsigned)sum_ctas, (unsigned)col_ctas), kThreads, 0, s, p.sorted, a.n_ids, a.vocab, a.width, a.scale,
                                                                                          a.accumulate, table, a.grad_table_pitch, p.partial,
                                                                                          span, group);
@@ -495,37 +511,44 @@ cudaError_t segments_typed(const EmbedGradArgs& a, const GradPlan& p, cudaStream
 
 template <class T, int VEC>
 cudaError_t direct_typed(const EmbedGradArgs& a, cudaStream_t s) {
-    int group = group_threads(a.width, VEC);
-    const int64_t ctas = a.n_ids + (a.accumulate ? 0 : ceil_div(a.vocab, kZeroRows));
+    const int64_t sum_ctas = ceil_div(a.n_ids * ceil_div(a.width, 32 * VEC), kDirectWarps);
+    const int64_t ctas = sum_ctas + (a.accumulate ? 0 : ceil_div(a.vocab, kZeroRows));
     if (ctas == 0) return cudaSuccess;
     return launch_chained(k_direct<T, VEC>, dim3((unsigned)ctas), kDirectThreads, 0, s, static_cast<const T*>(a.grad_out), a.grad_out_pitch, a.ids,
-                          (int)a.n_ids, a.vocab, a.width, a.scale, a.accumulate, static_cast<T*>(a.grad_table), a.grad_table_pitch, group);
+                          (int)a.n_ids, a.vocab, a.width, a.scale, a.accumulate, static_cast<T*>(a.grad_table), a.grad_table_pitch, sum_ctas);
 }
 
 // Sorts the positions into p.sorted, then sums.
 template <class T, int VEC>
 cudaError_t sorted_typed(const EmbedGradArgs& a, const GradPlan& p, cudaStream_t s) {
-    launch_chained(k_sort_count, dim3((unsigned)p.n_tiles), kSortThreads, 0, s, a.ids, a.n_ids, a.vocab, p.passes, p.counts);
+    const int launches = p.passes + 1;
+    const unsigned zero_ctas = a.accumulate ? 0 : kZeroCtas;
+    const int64_t cleared = std::min(a.vocab, launches * std::max<int64_t>(1, kZeroBytes / (a.width * (int64_t)sizeof(T))));
+    auto share = [&](int k) {
+        return ZeroFill{static_cast<char*>(a.grad_table), cleared * k / launches, cleared * (k + 1) / launches, a.width * (int64_t)sizeof(T),
+                        a.grad_table_pitch * (int64_t)sizeof(T), VEC * sizeof(T) == 16};
+    };
+    launch_chained(k_sort_count, dim3((unsigned)p.n_tiles + zero_ctas), kSortThreads, 0, s, a.ids, a.n_ids, a.vocab, p.passes, (int)p.n_tiles, p.counts,
+                   share(0));
     // the passes go back and forth between the two buffers and end in p.sorted
     const Pair* from = nullptr;
     for (int pass = 0; pass < p.passes; ++pass) {
         Pair* to = (p.passes - pass) % 2 == 1 ? p.sorted : p.other;
         const int* counts = p.counts + (int64_t)pass * p.n_tiles * kDigits;
         const bool last = pass + 1 == p.passes;
-        launch_chained(k_sort_pass, dim3((unsigned)p.n_tiles), kSortThreads, 0, s, a.ids, from, a.n_ids, a.vocab, pass, last, counts, (int)p.n_tiles, to,
-                       last ? nullptr : p.counts + (int64_t)(pass + 1) * p.n_tiles * kDigits);
+        launch_chained(k_sort_pass, dim3((unsigned)p.n_tiles + zero_ctas), kSortThreads, 0, s, a.ids, from, a.n_ids, a.vocab, pass, last, counts,
+                       (int)p.n_tiles, to, last ? nullptr : p.counts + (int64_t)(pass + 1) * p.n_tiles * kDigits, share(pass + 1));
         from = to;
     }
-    return segments_typed<T, VEC>(a, p, s);
+    return segments_typed<T, VEC>(a, p, cleared, s);
 }
 
 template <class T>
 cudaError_t grad_typed(const EmbedGradArgs& a, const GradPlan& p, cudaStream_t s) {
     constexpr int kVec = 16 / sizeof(T);
-    const bool wide =
-        a.width % kVec == 0 && aligned16(a.grad_out, a.grad_out_pitch, sizeof(T)) && aligned16(a.grad_table, a.grad_table_pitch, sizeof(T));
-    if (a.n_ids <= kDirectMost) return wide ? direct_typed<T, kVec>(a, s) : direct_typed<T, 1>(a, s);
-    return wide ? sorted_typed<T, kVec>(a, p, s) : sorted_typed<T, 1>(a, p, s);
+    const int vec = columns_a_thread<T>(a);
+    if (is_direct(a.n_ids, a.width, vec)) return vec == kVec ? direct_typed<T, kVec>(a, s) : direct_typed<T, 1>(a, s);
+    return vec == kVec ? sorted_typed<T, kVec>(a, p, s) : sorted_typed<T, 1>(a, p, s);
 }
 
 }  // namespace

@@ -51,12 +51,43 @@ cudaError_t operand_maps(const Operand& o, bool bf16, int64_t mats, CUtensorMap 
 
 }  // namespace
 
-cudaError_t gave_up_flag(int** out) { return cudaGetSymbolAddress(reinterpret_cast<void**>(out), g_gave_up); }
+// What the launches ask of a device, looked up at its first product.
+namespace {
+constexpr int kMaxDevices = 64;
+std::atomic<int*> g_flags[kMaxDevices];
+std::atomic<int> g_clusters[kMaxDevices];
+}  // namespace
+
+cudaError_t gave_up_flag(int** out) {
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    *out = device < kMaxDevices ? g_flags[device].load() : nullptr;
+    if (*out) return cudaSuccess;
+    e = cudaGetSymbolAddress(reinterpret_cast<void**>(out), g_gave_up);
+    if (e == cudaSuccess && device < kMaxDevices) g_flags[device].store(*out);
+    return e;
+}
 
 int gemm_clusters() {
     int device = 0, sms = 0;
-    if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 1;
-    return sms >= 2 ? sms / 2 : 1;
+    if (cudaGetDevice(&device) != cudaSuccess) return 1;
+    if (device < kMaxDevices && g_clusters[device].load() > 0) return g_clusters[device].load();
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 1;
+    const int clusters = sms >= 2 ? sms / 2 : 1;
+    if (device < kMaxDevices) g_clusters[device].store(clusters);
+    return clusters;
+}
+
+cudaError_t allow_shared_memory(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = device < kMaxDevices ? uint64_t(1) << device : 0;
+    if (done.load() & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done.fetch_or(bit);
+    return e;
 }
 
 cudaError_t make_gemm(const Operand& a, const Operand& b, int64_t mats, bool bf16, bool lower, int flush, int splits, GemmArgs* g) {

@@ -27,6 +27,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "lm_ops.h"
 
@@ -72,6 +73,8 @@ struct Operand {  // a 16-bit matrix, K-major [rows, k] or MN-major [k, rows], `
 };
 cudaError_t make_gemm(const Operand& a, const Operand& b, int64_t mats, bool bf16, bool lower, int flush, int splits, GemmArgs* out);
 cudaError_t gave_up_flag(int** out);  // where kernels note a wait that ran out, on the current device
+// Lets a kernel use `bytes` of dynamic shared memory on the current device; `done` remembers the devices it was asked on.
+cudaError_t allow_shared_memory(const void* kernel, int bytes, std::atomic<uint64_t>& done);
 int gemm_clusters();  // CTA pairs that run at once on the current device
 
 #ifdef __CUDACC__
@@ -580,9 +583,10 @@ template <class Epi, bool kPromote>
 cudaError_t launch_gemm(const GemmArgs& g, const typename Epi::Args& args, cudaStream_t s) {
     const int64_t tiles = (int64_t)g.batch * g.splits * (g.lower ? (int64_t)g.tiles_m * (g.tiles_m + 1) / 2 : (int64_t)g.tiles_m * g.tiles_n);
     if (tiles == 0) return cudaSuccess;
-    cudaError_t e = cudaFuncSetAttribute(k_gemm<Epi, kPromote>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
+    static std::atomic<uint64_t> allowed;
+    const cudaError_t e = allow_shared_memory(reinterpret_cast<const void*>(k_gemm<Epi, kPromote>), kGemmSmem, allowed);
     if (e != cudaSuccess) return e;
-    const int64_t clusters = tiles < gemm_clusters() ? tiles : gemm_clusters();
+    const int64_t clusters = std::min<int64_t>(tiles, gemm_clusters());
     return launch_chained(k_gemm<Epi, kPromote>, dim3((unsigned)(2 * clusters)), kGemmThreads, kGemmSmem, s, g, args);
 }
 #endif

@@ -539,7 +539,8 @@ cudaError_t small_typed(const OrthogonalizeArgs& a, cudaStream_t s) {
     SmallArgs g{a.in_stride, a.in_pitch, a.out_stride, a.out_pitch, (int)a.rows, (int)a.cols, a.steps, a.rows > a.cols, {a.ca, a.cb, a.cc, 0},
                 a.eps, a.scale, nullptr};
     cudaError_t e = gave_up_flag(&g.gave_up);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_small<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
+    static std::atomic<uint64_t> allowed;
+    if (e == cudaSuccess) e = allow_shared_memory(reinterpret_cast<const void*>(k_small<T>), kSmallSmem, allowed);
     if (e != cudaSuccess) return e;
     launch_chained(k_small<T>, dim3((unsigned)a.n_mats), kSmallThreads, kSmallSmem, s, static_cast<const T*>(a.in), static_cast<T*>(a.out), g);
     return cudaGetLastError();

@@ -34,11 +34,12 @@ def _matrix(name, t, like=None, shape=None, ndim=2):
         _refuse(f"{name} must be float32 or bfloat16")
     if like is not None and (t.dtype != like.dtype or t.device != like.device):
         _refuse(f"{name} must have the type and device of the other matrices")
-    if t.dim() != ndim or (shape is not None and tuple(t.shape) != tuple(shape)):
-        _refuse(f"{name} has shape {tuple(t.shape)}" + (f", {tuple(shape)} needed" if shape is not None else f", {ndim} dimensions needed"))
-    if t.shape[-1] != 1 and t.stride(-1) != 1:
+    dims, strides = t.shape, t.stride()
+    if len(dims) != ndim or (shape is not None and dims != shape):
+        _refuse(f"{name} has shape {tuple(dims)}" + (f", {tuple(shape)} needed" if shape is not None else f", {ndim} dimensions needed"))
+    if dims[-1] != 1 and strides[-1] != 1:
         _refuse(f"the last dimension of {name} must be contiguous")
-    return t.stride(-2) if t.shape[-2] > 1 else max(t.shape[-1], 1)
+    return strides[-2] if dims[-2] > 1 else max(dims[-1], 1)
 
 
 def _vector(name, t, n, dtype, device):
@@ -47,36 +48,51 @@ def _vector(name, t, n, dtype, device):
     return t.data_ptr()
 
 
-@contextlib.contextmanager
-def _on(device, stream):
-    with torch.cuda.device(device), torch.cuda.stream(stream):
-        yield stream.cuda_stream
+class _Queue:
+    """The context in which a call allocates and queues: the tensors' device and the stream. Entering it gives the raw stream."""
+
+    __slots__ = ("device", "stream", "inner")
+
+    def __init__(self, device, stream):
+        self.device, self.stream, self.inner = device, stream, None
+
+    def __enter__(self):
+        if self.stream is None and torch._C._cuda_getDevice() == self.device.index:
+            return torch._C._cuda_getCurrentRawStream(self.device.index)  # nothing to switch: the usual case, kept short
+        self.inner = contextlib.ExitStack()
+        self.inner.enter_context(torch.cuda.device(self.device))
+        stream = torch.cuda.current_stream(self.device) if self.stream is None else self.stream
+        self.inner.enter_context(torch.cuda.stream(stream))
+        return stream.cuda_stream
+
+    def __exit__(self, *exc):
+        if self.inner is not None:
+            return self.inner.__exit__(*exc)
+        return False
 
 
-def _queue(device, stream):
-    """The context in which a call allocates and queues; entering it gives the raw stream."""
-    if stream is None and torch.cuda.current_device() == device.index:
-        return contextlib.nullcontext(torch.cuda.current_stream(device).cuda_stream)
-    return _on(device, torch.cuda.current_stream(device) if stream is None else stream)
-
-
-def _workspace(device, size_of, *args):
+def _workspace(like, size_of, *args):
+    """A workspace of the size the library asks for: (tensor or None, address, bytes)."""
     need = C.c_int64()
     B._check(size_of(*args, C.byref(need)))
-    return torch.empty(need.value, dtype=torch.uint8, device=device), need.value
+    if need.value == 0:
+        return None, None, 0
+    ws = torch.empty(need.value, dtype=torch.uint8, device=like.device)
+    return ws, ws.data_ptr(), need.value
 
 
 def embed(table, ids, scale=1.0, out=None, stream=None):
     """out[t] = scale * table[ids[t]]; a row of zeros where ids[t] lies outside the table. table [vocab, width], ids int32 [n]."""
     pitch = _matrix("table", table)
-    n = ids.numel()
+    n, (vocab, width) = ids.numel(), table.shape
     ids_p = _vector("ids", ids, n, torch.int32, table.device)
-    with _queue(table.device, stream) as s:
+    with _Queue(table.device, stream) as s:
         if out is None:
-            out = torch.empty(n, table.shape[1], dtype=table.dtype, device=table.device)
-        out_pitch = _matrix("out", out, table, (n, table.shape[1]))
-        B._check(B.lib().a2cid2_embed(table.data_ptr(), table.shape[0], table.shape[1], pitch, ids_p, n, scale, out.data_ptr(),
-                                      out_pitch, _DTYPES[table.dtype], s))
+            out, out_pitch = torch.empty(n, width, dtype=table.dtype, device=table.device), width
+        else:
+            out_pitch = _matrix("out", out, table, (n, width))
+        B._check(B.lib().a2cid2_embed(table.data_ptr(), vocab, width, pitch, ids_p, n, scale, out.data_ptr(), out_pitch,
+                                      _DTYPES[table.dtype], s))
     return out
 
 
@@ -88,13 +104,13 @@ def embed_grad(grad_out, ids, vocab, scale=1.0, out=None, accumulate=False, stre
     ids_p = _vector("ids", ids, n, torch.int32, grad_out.device)
     if accumulate and out is None:
         _refuse("accumulate needs out")
-    with _queue(grad_out.device, stream) as s:
+    with _Queue(grad_out.device, stream) as s:
         if out is None:
             out = torch.empty(int(vocab), width, dtype=grad_out.dtype, device=grad_out.device)
         out_pitch = _matrix("out", out, grad_out, (int(vocab), width))
-        ws, size = _workspace(grad_out.device, B.lib().a2cid2_embed_grad_workspace, vocab, width, n)
+        ws, ws_p, size = _workspace(grad_out, B.lib().a2cid2_embed_grad_workspace, vocab, width, n)
         B._check(B.lib().a2cid2_embed_grad(grad_out.data_ptr(), pitch, ids_p, n, vocab, width, scale, int(accumulate), out.data_ptr(),
-                                           out_pitch, _DTYPES[grad_out.dtype], ws.data_ptr(), size, s))
+                                           out_pitch, _DTYPES[grad_out.dtype], ws_p, size, s))
     return out
 
 
@@ -106,7 +122,7 @@ def _vocab_loss(hidden, head, targets, weights, scale, grad_hidden, grad_head, s
         _refuse(f"hidden has {width} columns, head {head.shape[1]}")
     targets_p = _vector("targets", targets, n, torch.int32, device)
     weights_p = None if weights is None else _vector("weights", weights, n, torch.float32, device)
-    with _queue(device, stream) as s:
+    with _Queue(device, stream) as s:
         grads = []
         for name, g, like in (("grad_hidden", grad_hidden, hidden), ("grad_head", grad_head, head)):
             if g is True:
@@ -116,10 +132,10 @@ def _vocab_loss(hidden, head, targets, weights, scale, grad_hidden, grad_head, s
         loss = torch.empty(n, dtype=torch.float32, device=device)
         lse = torch.empty(n, dtype=torch.float32, device=device)
         dtype = _DTYPES[hidden.dtype]
-        ws, size = _workspace(device, B.lib().a2cid2_vocab_loss_workspace, n, width, vocab, int(gh is not None or gw is not None), dtype)
+        ws, ws_p, size = _workspace(hidden, B.lib().a2cid2_vocab_loss_workspace, n, width, vocab, int(gh is not None or gw is not None), dtype)
         B._check(B.lib().a2cid2_vocab_loss(hidden.data_ptr(), hidden_pitch, head.data_ptr(), head_pitch, targets_p, n, width, vocab,
                                            weights_p, scale, loss.data_ptr(), lse.data_ptr(), gh_p, gh_pitch, gw_p, gw_pitch, dtype,
-                                           ws.data_ptr(), size, s))
+                                           ws_p, size, s))
     return loss, lse, gh, gw
 
 
@@ -142,14 +158,14 @@ def orthogonalize(mats, steps=5, coeffs=NEWTON_SCHULZ, eps=1e-7, scale=1.0, out=
         return orthogonalize(mats[None], steps, coeffs, eps, scale, None if out is None else out[None], stream)[0]
     pitch = _matrix("mats", mats, ndim=3)
     n, rows, cols = mats.shape
-    with _queue(mats.device, stream) as s:
+    with _Queue(mats.device, stream) as s:
         if out is None:
             out = torch.empty(mats.shape, dtype=mats.dtype, device=mats.device)
         out_pitch = _matrix("out", out, mats, mats.shape, ndim=3)
         dtype = _DTYPES[mats.dtype]
-        ws, size = _workspace(mats.device, B.lib().a2cid2_orthogonalize_workspace, n, rows, cols, dtype)
+        ws, ws_p, size = _workspace(mats, B.lib().a2cid2_orthogonalize_workspace, n, rows, cols, dtype)
         B._check(B.lib().a2cid2_orthogonalize(mats.data_ptr(), mats.stride(0), pitch, n, rows, cols, steps, *coeffs, eps, scale, out.data_ptr(),
-                                              out.stride(0), out_pitch, dtype, ws.data_ptr(), size, s))
+                                              out.stride(0), out_pitch, dtype, ws_p, size, s))
     return out
 
 
