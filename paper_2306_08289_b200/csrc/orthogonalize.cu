@@ -169,14 +169,16 @@ struct SymmetricEpi {
         int64_t m;
         const MatScale* scales;
         Poly poly;
+        float* parts;  // A alone: sums of the parts of K, [parts][matrix][m][ld], or NULL when K is whole
+        int64_t part_stride;
     };
     const Args& a;
-    int64_t row0, col0, mat;
+    int64_t row0, col0, mat, split;
     int lane;
     float* staging;
     float factor;
     __device__ __forceinline__ SymmetricEpi(const Args& args, const Tile& t, int row, int col, int lane_, float* staging_)
-        : a(args), row0(row), col0(col), mat(t.b), lane(lane_), staging(staging_) {
+        : a(args), row0(row), col0(col), mat(t.b), split(t.split), lane(lane_), staging(staging_) {
         if (kQuadratic) {
             factor = a.poly.c / kScale;
         } else {
@@ -190,6 +192,14 @@ struct SymmetricEpi {
         if (row0 >= a.m || col >= a.m) return;  // rows of `to` are padded to 64 columns: only rows need care
         const int rows = (int)min((int64_t)32, a.m - row0);
         const int64_t at = mat * a.to.stride + row0 * a.to.ld + col;
+        if (!kQuadratic && a.parts) {
+            turn_columns(staging, v, lane);
+            float* to = a.parts + split * a.part_stride + at + lane;
+#pragma unroll
+            for (int r = 0; r < 32; ++r)
+                if (r < rows) to[r * a.to.ld] = v[r];
+            return;
+        }
         if (kQuadratic) {
             __half x[32];
             load_rows16(staging, x, a.from.hi + at, a.from.ld, rows, lane);
@@ -209,6 +219,29 @@ struct SymmetricEpi {
     }
     __device__ __forceinline__ void finish() {}
 };
+
+// Adds up the parts of A = X X^T, in order, on and below the diagonal tiles. Two columns a thread.
+__global__ void __launch_bounds__(256) k_join_gram(const float* __restrict__ parts, int n_parts, int64_t part_stride, Words to, int64_t m,
+                                                   const MatScale* __restrict__ scales, Poly poly) {
+    ptx::chained();
+    const int64_t row = blockIdx.y, mat = blockIdx.z, col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 2;
+    if (col >= m || col / kTileN > row / kTileM) return;
+    float now, next;
+    units(scales[mat], poly, &now, &next);
+    const float factor = kScale * now * now;
+    const int64_t at = mat * to.stride + row * to.ld + col;  // ld is even: the second column may be padding
+    float x = 0.0f, y = 0.0f;
+#pragma unroll 4
+    for (int p = 0; p < n_parts; ++p) {
+        const float2 v = *reinterpret_cast<const float2*>(parts + p * part_stride + at);
+        x += v.x;
+        y += v.y;
+    }
+    Pack<__half, 2> h, l;
+    split_pair(x * factor, y * factor, h.v[0], h.v[1], l.v[0], l.v[1]);
+    *reinterpret_cast<Pack<__half, 2>*>(to.hi + at) = h;
+    if (to.lo) *reinterpret_cast<Pack<__half, 2>*>(to.lo + at) = l;
+}
 
 // X <- B X; the last step writes the caller's matrix.
 template <class T>
@@ -255,6 +288,7 @@ struct UpdateEpi {
 };
 
 // ---- layout and launches ---------------------------------------------------------------------------
+constexpr int64_t kPairs = 74, kLeastBlocks = 6;  // pairs of CTAs; fewest blocks of K worth a part (of three passes; four times that of one)
 constexpr int kFlush = 2;  // K blocks a sum stays in tensor memory with fp32 rows: 8 steps of the tensor core
 
 struct Layout {
@@ -262,6 +296,8 @@ struct Layout {
     MatScale* scales;
     Words x, y, gram, poly;
     int64_t parts;
+    int gram_parts;  // of K = n in A = X X^T, so that few matrices fill the GPU
+    float* gram_sums;
 };
 
 int64_t layout(int64_t mats, int64_t rows, int64_t cols, int32_t dtype, void* ws, Layout* out) {
@@ -283,6 +319,9 @@ int64_t layout(int64_t mats, int64_t rows, int64_t cols, int32_t dtype, void* ws
     l.y = take(rows, cols);
     l.gram = take(m, m);
     l.poly = take(m, m);
+    const int64_t side = ceil_div(m, kTileM);
+    l.gram_parts = split_parts(mats * side * (side + 1) / 2, ceil_div(std::max(rows, cols), kBlockK), kPairs, dtype == A2_F32 ? kLeastBlocks : 4 * kLeastBlocks);
+    if (l.gram_parts > 1) l.gram_sums = w.take<float>(l.gram_parts * mats * l.gram.stride);
     if (out) *out = l;
     return w.used;
 }
@@ -301,31 +340,37 @@ cudaError_t typed(const OrthogonalizeArgs& a, Layout l, cudaStream_t s) {
     if (a.steps == 0)
         launch_chained(k_normalized<T>, grid, kNormThreads, 0, s, l.x.hi, l.x.lo, l.x.ld, a.rows, a.cols, l.scales, a.scale, static_cast<T*>(a.out), a.out_stride,
                                                       a.out_pitch);
+    if (a.steps == 0) return cudaGetLastError();
+    // X goes back and forth between two buffers: two of each product that reads it
     auto operand = [](const Words& w, int64_t rows, int64_t k, bool mn) { return Operand{w.hi, w.lo, rows, k, w.ld, w.stride, mn}; };
-    Words x = l.x, y = l.y;
-    for (int step = 0; step < a.steps; ++step) {
-        const Poly poly{a.ca, a.cb, a.cc, step};
-        GemmArgs g;
-        const Operand side = operand(x, m, n, tall);
-        cudaError_t e = make_gemm(side, side, a.n_mats, false, true, flush, 1, &g);
-        if (e != cudaSuccess) return e;
-        e = launch_gemm<SymmetricEpi<false>, kWords>(g, {l.gram, l.gram, m, l.scales, poly}, s);
-        if (e != cudaSuccess) return e;
-        Operand gram = operand(l.gram, m, m, false), b = operand(l.poly, m, m, false);
-        gram.symmetric = b.symmetric = true;
-        e = make_gemm(gram, gram, a.n_mats, false, true, flush, 1, &g);
-        if (e != cudaSuccess) return e;
-        e = launch_gemm<SymmetricEpi<true>, kWords>(g, {l.gram, l.poly, m, l.scales, poly}, s);
-        if (e != cudaSuccess) return e;
-        e = tall ? make_gemm(operand(x, a.rows, m, false), b, a.n_mats, false, false, flush, 1, &g)
-                 : make_gemm(b, operand(x, n, m, true), a.n_mats, false, false, flush, 1, &g);
-        if (e != cudaSuccess) return e;
-        const bool last = step + 1 == a.steps;
-        e = launch_gemm<UpdateEpi<T>, kWords>(
-            g, {y, a.rows, a.cols, l.scales, poly, last ? static_cast<T*>(a.out) : nullptr, a.out_stride, a.out_pitch, a.scale}, s);
-        if (e != cudaSuccess) return e;
-        std::swap(x, y);
+    Operand gram = operand(l.gram, m, m, false), b = operand(l.poly, m, m, false);
+    gram.symmetric = b.symmetric = true;
+    const Words x[2] = {l.x, l.y};
+    GemmArgs make_gram[2], make_poly, update[2];
+    cudaError_t e = make_gemm(gram, gram, a.n_mats, false, true, flush, 1, &make_poly);
+    for (int k = 0; k < 2 && k < a.steps; ++k) {
+        const Operand side = operand(x[k], m, n, tall);
+        if (e == cudaSuccess) e = make_gemm(side, side, a.n_mats, false, true, flush, l.gram_parts, &make_gram[k]);
+        if (e == cudaSuccess)
+            e = tall ? make_gemm(operand(x[k], a.rows, m, false), b, a.n_mats, false, false, flush, 1, &update[k])
+                     : make_gemm(b, operand(x[k], n, m, true), a.n_mats, false, false, flush, 1, &update[k]);
     }
+    const int64_t part_stride = a.n_mats * l.gram.stride;
+    for (int step = 0; step < a.steps && e == cudaSuccess; ++step) {
+        const Poly poly{a.ca, a.cb, a.cc, step};
+        const bool last = step + 1 == a.steps;
+        e = launch_gemm<SymmetricEpi<false>, kWords>(make_gram[step % 2],
+                                                     {l.gram, l.gram, m, l.scales, poly, l.gram_parts > 1 ? l.gram_sums : nullptr, part_stride}, s);
+        if (e == cudaSuccess && l.gram_parts > 1)  // only with fewer tiles than pairs, so m and the matrices fit a grid
+            e = launch_chained(k_join_gram, dim3((unsigned)ceil_div(m, 512), (unsigned)m, (unsigned)a.n_mats), 256, 0, s, l.gram_sums, l.gram_parts,
+                               part_stride, l.gram, m, l.scales, poly);
+        if (e == cudaSuccess) e = launch_gemm<SymmetricEpi<true>, kWords>(make_poly, {l.gram, l.poly, m, l.scales, poly, nullptr, 0}, s);
+        if (e == cudaSuccess)
+            e = launch_gemm<UpdateEpi<T>, kWords>(
+                update[step % 2],
+                {x[1 - step % 2], a.rows, a.cols, l.scales, poly, last ? static_cast<T*>(a.out) : nullptr, a.out_stride, a.out_pitch, a.scale}, s);
+    }
+    if (e != cudaSuccess) return e;
     return cudaGetLastError();
 }
 
