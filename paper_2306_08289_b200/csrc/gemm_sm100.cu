@@ -79,15 +79,24 @@ int gemm_clusters() {
     return clusters;
 }
 
-cudaError_t allow_shared_memory(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+namespace {
+cudaError_t set_once(const void* kernel, cudaFuncAttribute attribute, int value, std::atomic<uint64_t>& done) {
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
     const uint64_t bit = device < kMaxDevices ? uint64_t(1) << device : 0;
     if (done.load() & bit) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    e = cudaFuncSetAttribute(kernel, attribute, value);
     if (e == cudaSuccess) done.fetch_or(bit);
     return e;
+}
+}  // namespace
+
+cudaError_t allow_shared_memory(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+    return set_once(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes, done);
+}
+cudaError_t allow_large_clusters(const void* kernel, std::atomic<uint64_t>& done) {
+    return set_once(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1, done);
 }
 
 cudaError_t make_gemm(const Operand& a, const Operand& b, int64_t mats, bool bf16, bool lower, int flush, int splits, GemmArgs* g) {

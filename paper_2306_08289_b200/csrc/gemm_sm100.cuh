@@ -74,6 +74,7 @@ struct Operand {  // a 16-bit matrix, K-major [rows, k] or MN-major [k, rows], `
 cudaError_t make_gemm(const Operand& a, const Operand& b, int64_t mats, bool bf16, bool lower, int flush, int splits, GemmArgs* out);
 cudaError_t gave_up_flag(int** out);  // where kernels note a wait that ran out, on the current device
 // Lets a kernel use `bytes` of dynamic shared memory on the current device; `done` remembers the devices it was asked on.
+cudaError_t allow_large_clusters(const void* kernel, std::atomic<uint64_t>& done);  // more than 8 CTAs
 cudaError_t allow_shared_memory(const void* kernel, int bytes, std::atomic<uint64_t>& done);
 int gemm_clusters();  // CTA pairs that run at once on the current device
 
@@ -121,6 +122,7 @@ __device__ __forceinline__ unsigned long long now_ns() {
     return t;
 }
 __device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, int* gave_up) {
+    if (bar_try(bar, parity)) return true;  // a try sleeps until the phase ends or kTryNs are over: seldom more than two
     const unsigned long long start = now_ns();
     while (!bar_try(bar, parity))
         if (now_ns() - start > kWaitNs) {

@@ -374,24 +374,46 @@ cudaError_t typed(const OrthogonalizeArgs& a, Layout l, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-// ---- small matrices: all steps in one CTA ------------------------------------------------------------
-// m <= 128 and n <= 256: X, A and B stay in shared memory as the two-word operands of the tensor core (with either storage
-// type: the products cost nothing here), the sums in tensor memory; one launch, one read and one write of the matrix. Bound by the
-// chain of three products and their epilogues a step. X is kept [m, n] in 64-column blocks of 128-byte swizzled rows, which the tensor
-// core reads K-major for X X^T and MN-major for B X.
-constexpr int kSmallM = 128, kSmallN = 256;
-constexpr int kSmallThreads = 256;
-constexpr int kBlockBytes = kSmallM * 128;  // 128 rows of 64 fp16 columns
-constexpr int kSmallSmem = 2 * (kSmallN / 64) * kBlockBytes + 2 * (kSmallM / 64) * kBlockBytes + 1024;
+// ---- narrow matrices: all steps in one cluster -------------------------------------------------------
+// m <= 128: a cluster of up to 16 CTAs holds a matrix, 256 columns of X a CTA, and runs all steps in one launch. X, A and B stay in
+// shared memory as the two-word operands of the tensor core (with either storage type: the products cost little here), the sums in
+// tensor memory. X is kept [m, 256] in 64-column blocks of 128-byte swizzled rows, which the tensor core reads K-major for X X^T and
+// MN-major for B X. Every CTA makes its columns' part of A = X X^T; the parts are added up in CTA order, a share of the rows by each
+// CTA, and every CTA takes the whole of A from the shares and forms B by itself. Bound by that chain: three products, their
+// epilogues and two exchanges a step.
+constexpr int kNarrowM = 128, kNarrowN = 256, kNarrowCtas = 16;
+constexpr int kNarrowThreads = 256;
+constexpr int kBlockBytes = kNarrowM * 128;  // 128 rows of 64 fp16 columns
+constexpr int kWordBytes = (kNarrowM / 64) * kBlockBytes;         // a word of A or B
+constexpr int kSquareBytes = kNarrowM * (kNarrowM + 4) * 4 + 64;  // two of them, or a part of A as floats (and what a last load reads past it)
+static_assert(2 * kWordBytes <= kSquareBytes, "A's words and its part share their place");
+constexpr int kNarrowSmem = 2 * (kNarrowN / 64) * kBlockBytes + kSquareBytes + 1024;
+static_assert(kNarrowSmem <= 227 * 1024 - 512, "shared memory of one CTA, with room for the static part");
 
 // Byte offset of columns col .. col + 7 of a row.
 __device__ __forceinline__ uint32_t swizzled(int row, int col) {
     return (uint32_t)(col / 64) * kBlockBytes + row * 128 + ((((col % 64) / 8) ^ (row % 8)) * 16);
 }
 
-struct SmallArgs {
+__device__ __forceinline__ float4 load_remote(uint32_t addr, int cta) {
+    uint32_t remote;
+    float4 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(cta));
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote) : "memory");
+    return v;
+}
+__device__ __forceinline__ double load_remote_double(uint32_t addr, int cta) {
+    uint32_t remote;
+    double v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(cta));
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(remote) : "memory");
+    return v;
+}
+
+struct NarrowArgs {
     int64_t in_stride, in_pitch, out_stride, out_pitch;
     int rows, cols, steps;
+    int ctas, chunk;  // of a matrix; columns of X a CTA, a multiple of 64
     bool tall;
     Poly poly;
     double eps;
@@ -400,7 +422,7 @@ struct SmallArgs {
 };
 
 // D = A B^T or A B over K = 16 * k_steps in the three passes of two-word operands; one thread.
-__device__ __forceinline__ void small_product(uint32_t d, const uint32_t (&a)[2], const uint32_t (&b)[2], bool b_mn, int k_steps, uint32_t idesc) {
+__device__ __forceinline__ void narrow_product(uint32_t d, const uint32_t (&a)[2], const uint32_t (&b)[2], bool b_mn, int k_steps, uint32_t idesc) {
     for (int pass = 0; pass < 3; ++pass) {
         const uint32_t pa = a[pass == 0], pb = b[pass == 1];  // lo hi, hi lo, hi hi
         for (int k = 0; k < k_steps; ++k) {
@@ -413,22 +435,31 @@ __device__ __forceinline__ void small_product(uint32_t d, const uint32_t (&a)[2]
 }
 
 template <class T>
-__global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* __restrict__ in, T* out, const SmallArgs g) {
-    ptx::chained();
+__global__ void __launch_bounds__(kNarrowThreads, 1) k_narrow(const T* __restrict__ in, T* out, const NarrowArgs g) {
     extern __shared__ char raw[];
-    __shared__ double part[kSmallThreads / 32];
+    __shared__ double part[kNarrowThreads / 32];
+    __shared__ double squares;
     __shared__ uint64_t bar_word;
     __shared__ uint32_t tmem_slot;
     __shared__ MatScale scale;
     char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int m = g.tall ? g.cols : g.rows, n = g.tall ? g.rows : g.cols;
+    const int rank = g.ctas > 1 ? (int)ptx::cta_rank() : 0, mat = blockIdx.x / g.ctas;
+    const int m = g.tall ? g.cols : g.rows;
+    const int first = rank * g.chunk, n = min(g.chunk, (g.tall ? g.rows : g.cols) - first);  // this CTA's columns of X
     const int m16 = (m + 15) / 16 * 16, n16 = (n + 15) / 16 * 16, blocks = (n + 63) / 64;
-    char* xw[2] = {smem, smem + (kSmallN / 64) * kBlockBytes};
-    char* aw[2] = {smem + 2 * (kSmallN / 64) * kBlockBytes, smem + 2 * (kSmallN / 64) * kBlockBytes + (kSmallM / 64) * kBlockBytes};
+    char* xw[2] = {smem, smem + (kNarrowN / 64) * kBlockBytes};
+    char* square = smem + 2 * (kNarrowN / 64) * kBlockBytes;
+    char* aw[2] = {square, square + kWordBytes};
+    // [m16][m16 + 4] in A's place while it is made: rows 16 bytes apart modulo 128, so that eight lanes' rows are free of conflicts
+    float* gram_part = reinterpret_cast<float*>(square);
+    const int pitch = m16 + 4, share = (m + g.ctas - 1) / g.ctas;
     const uint32_t xs[2] = {ptx::smem_addr(xw[0]), ptx::smem_addr(xw[1])}, as[2] = {ptx::smem_addr(aw[0]), ptx::smem_addr(aw[1])};
     const uint32_t bar = ptx::smem_addr(&bar_word);
-    const T* from = in + blockIdx.x * g.in_stride;
+    auto sync_matrix = [&] {  // all CTAs of the matrix
+        if (g.ctas > 1) ptx::cluster_sync();
+        else __syncthreads();
+    };
 
     if (threadIdx.x == 0) {
         ptx::bar_init(bar, 1);
@@ -439,10 +470,15 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* __restrict_
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
         ptx::fence_before();
     }
+    ptx::chained();
+    // element (i, j) of this CTA's columns of X
+    const T* from = in + mat * g.in_stride + (g.tall ? first * g.in_pitch : first);
+    T* to = out + mat * g.out_stride + (g.tall ? first * g.out_pitch : first);
+    const int my_rows = g.tall ? n : g.rows, my_cols = g.tall ? g.cols : n;
     // the norm
     double sum = 0.0;
-    for (int i = warp; i < g.rows; i += kSmallThreads / 32)
-        for (int j = lane; j < g.cols; j += 32) {
+    for (int i = warp; i < my_rows; i += kNarrowThreads / 32)
+        for (int j = lane; j < my_cols; j += 32) {
             const double v = widen(from[i * g.in_pitch + j]);
             sum += v * v;
         }
@@ -451,7 +487,13 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* __restrict_
     __syncthreads();
     if (threadIdx.x == 0) {
         double all = 0.0;
-        for (int w = 0; w < kSmallThreads / 32; ++w) all += part[w];
+        for (int w = 0; w < kNarrowThreads / 32; ++w) all += part[w];
+        squares = all;
+    }
+    sync_matrix();
+    if (threadIdx.x == 0) {
+        double all = 0.0;
+        for (int c = 0; c < g.ctas; ++c) all += g.ctas > 1 ? load_remote_double(ptx::smem_addr(&squares), c) : squares;
         scale = mat_scale(all, g.eps);
     }
     __syncthreads();
@@ -460,7 +502,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* __restrict_
     // first words, zeros around the matrix: rows to a multiple of 16, columns to a multiple of 64. Eight columns a thread; the tall
     // matrix is read along its rows, which are X's columns
     const PowerOfTwo up(scale.e);
-    for (int k = threadIdx.x; k < m16 * blocks * 8; k += kSmallThreads) {
+    for (int k = threadIdx.x; k < m16 * blocks * 8; k += kNarrowThreads) {
         const int i = g.tall ? k % m16 : k / (blocks * 8), j = (g.tall ? k / m16 : k % (blocks * 8)) * 8;
         Pack<__half, 8> hi, lo;
 #pragma unroll
@@ -478,24 +520,24 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* __restrict_
     const int row = quad * 32 + lane;
     const bool mine = quad * 32 < m;  // warps of padding rows have nothing to write
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
-    const uint32_t square = instruction_desc(false, false, false, 128, m16), wide = instruction_desc(false, false, true, 128, n16);
+    const uint32_t to_square = instruction_desc(false, false, false, 128, m16), to_wide = instruction_desc(false, false, true, 128, n16);
     uint32_t phase = 0;
-    bool ok = true;
+    bool ok = true;  // once a wait has run out no further product is made, but every CTA still comes to every barrier
     // one product: operands written by everybody, MMAs by one thread, everybody waits
     auto product = [&](uint32_t d, const uint32_t (&a)[2], const uint32_t (&b)[2], bool b_mn, int k_steps, uint32_t idesc) {
         ptx::fence_before();
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
-        if (threadIdx.x == 0) {
+        if (threadIdx.x == 0 && ok) {
             ptx::fence_after();
-            small_product(d, a, b, b_mn, k_steps, idesc);
+            narrow_product(d, a, b, b_mn, k_steps, idesc);
             ptx::commit_one(bar);
         }
         __syncwarp();
-        ok = ptx::bar_wait(bar, phase & 1, g.gave_up);
+        if (ok) ok = ptx::bar_wait(bar, phase & 1, g.gave_up);
         ++phase;
         ptx::fence_after();
-        return __syncthreads_or(!ok) == 0;
+        ok = __syncthreads_or(!ok) == 0;
     };
     auto write8 = [&](char* const (&to)[2], int col, const float* v) {
         Pack<__half, 8> hi, lo;
@@ -505,25 +547,80 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* __restrict_
         *reinterpret_cast<Pack<__half, 8>*>(to[0] + at) = hi;
         *reinterpret_cast<Pack<__half, 8>*>(to[1] + at) = lo;
     };
-    T* to = out + blockIdx.x * g.out_stride;
     Poly poly = g.poly;
     for (poly.step = 0; poly.step < g.steps; ++poly.step) {
         float now, next;
         units(scale, poly, &now, &next);
         const bool last = poly.step + 1 == g.steps;
-        if (!product(tmem, xs, xs, false, n16 / 16, square)) break;
         const float gram = kScale * now * now;
-        for (int col = half * 32; mine && col < m16; col += 64) {
+        product(tmem, xs, xs, false, n16 / 16, to_square);
+        float total[2][32];  // of A, this thread's columns half * 32 .. and half * 32 + 64 ..
+        if (g.ctas > 1) {
+            for (int col = half * 32; mine && col < m16; col += 64) {
+                float v[32];
+                ptx::tmem_load32(v, lanes + col);
+                ptx::tmem_load_wait();
+#pragma unroll
+                for (int k = 0; k < 32; k += 4)
+                    if (row < m16 && col + k < m16) *reinterpret_cast<float4*>(gram_part + row * pitch + col + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+            }
+            sync_matrix();
+            // this CTA's rows, in place: nobody else reads its part of them
+            for (int k = threadIdx.x; k < share * (m16 / 4); k += kNarrowThreads) {
+                const int r = rank * share + k / (m16 / 4), c = k % (m16 / 4) * 4;
+                if (r >= m) break;
+                const uint32_t at = ptx::smem_addr(gram_part + r * pitch + c);
+                float4 all = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+                for (int q = 0; q < g.ctas; ++q) {
+                    const float4 v = load_remote(at, q);
+                    all.x += v.x;
+                    all.y += v.y;
+                    all.z += v.z;
+                    all.w += v.w;
+                }
+                *reinterpret_cast<float4*>(gram_part + r * pitch + c) = all;
+            }
+            sync_matrix();
+            const int r = min(row, m - 1);
+            const uint32_t at = ptx::smem_addr(gram_part + r * pitch);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                if (mine && half * 32 + c * 64 < m16)
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4) {
+                        const float4 v = load_remote(at + (half * 32 + c * 64 + k) * 4, r / share);
+                        total[c][k] = row < m ? v.x : 0.0f;
+                        total[c][k + 1] = row < m ? v.y : 0.0f;
+                        total[c][k + 2] = row < m ? v.z : 0.0f;
+                        total[c][k + 3] = row < m ? v.w : 0.0f;
+                    }
+            sync_matrix();  // A's words go where its parts lie
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int col = half * 32 + c * 64;
+            if (!mine || col >= m16) continue;
             float v[32];
-            ptx::tmem_load32(v, lanes + col);
-            ptx::tmem_load_wait();
+            if (g.ctas > 1) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] = total[c][k];
+            } else {
+                ptx::tmem_load32(v, lanes + col);
+                ptx::tmem_load_wait();
+            }
 #pragma unroll
             for (int k = 0; k < 32; ++k) v[k] *= gram;
+            uint64_t keep[16];  // A itself, for B
+#pragma unroll
+            for (int k = 0; k < 16; ++k) asm volatile("mov.b64 %0, {%1, %2};" : "=l"(keep[k]) : "f"(v[2 * k]), "f"(v[2 * k + 1]));
+            ptx::tmem_store_pairs(lanes + col, keep);
 #pragma unroll
             for (int k = 0; k < 32; k += 8)
                 if (col + k < m16) write8(aw, col + k, v + k);
         }
-        if (!product(tmem + 128, as, as, false, m16 / 16, square)) break;
+        ptx::tmem_store_wait();
+        product(tmem + 128, as, as, false, m16 / 16, to_square);
         for (int col = half * 32; mine && col < m16; col += 64) {
             float v[32], w[32];
             ptx::tmem_load32(v, lanes + col);
@@ -531,12 +628,12 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* __restrict_
             ptx::tmem_load_wait();
 #pragma unroll
             for (int k = 0; k < 32; ++k)
-                v[k] = poly.b * (gram * v[k]) + poly.c / kScale * w[k] + (row == col + k && row < m ? poly.a * kScale : 0.0f);
+                v[k] = poly.b * v[k] + poly.c / kScale * w[k] + (row == col + k && row < m ? poly.a * kScale : 0.0f);
 #pragma unroll
             for (int k = 0; k < 32; k += 8)
                 if (col + k < m16) write8(aw, col + k, v + k);
         }
-        if (!product(tmem + 256, as, xs, true, m16 / 16, wide)) break;
+        product(tmem + 256, as, xs, true, m16 / 16, to_wide);
         const float factor = (last ? g.scale * now : now / next) / kScale;
         for (int col = half * 32; mine && col < n16; col += 64) {
             float v[32];
@@ -556,23 +653,21 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* __restrict_
                     for (int k = 0; k < 32; ++k)
                         if (col + k < n) to[(col + k) * g.out_pitch + row] = narrow<T>(v[k]);
             } else {  // through shared memory (B is done with), so that a row's columns are written side by side
-                float* staging = reinterpret_cast<float*>(aw[0]) + warp * 32 * kStagePitch;
-#pragma unroll
-                for (int k = 0; k < 32; ++k) staging[lane * kStagePitch + k] = v[k];
-                __syncwarp();
+                turn_columns(reinterpret_cast<float*>(aw[0]) + warp * 32 * kStagePitch, v, lane);
                 if (col + lane < n)
-                    for (int r = 0; r < 32 && quad * 32 + r < m; ++r) to[(quad * 32 + r) * g.out_pitch + col + lane] = narrow<T>(staging[r * kStagePitch + lane]);
-                __syncwarp();
+#pragma unroll
+                    for (int r = 0; r < 32; ++r)
+                        if (quad * 32 + r < m) to[(quad * 32 + r) * g.out_pitch + col + lane] = narrow<T>(v[r]);
             }
         }
     }
     if (g.steps == 0) {
-        for (int i = warp; i < g.rows; i += kSmallThreads / 32)
-            for (int j = lane; j < g.cols; j += 32)
+        for (int i = warp; i < my_rows; i += kNarrowThreads / 32)
+            for (int j = lane; j < my_cols; j += 32)
                 to[i * g.out_pitch + j] = narrow<T>(up(widen(from[i * g.in_pitch + j])) * (scale.u * g.scale));
     }
     ptx::fence_before();
-    __syncthreads();
+    sync_matrix();  // no CTA leaves while another may read its shared memory
     if (warp == 0) {
         ptx::fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
@@ -580,18 +675,22 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* __restrict_
 }
 
 template <class T>
-cudaError_t small_typed(const OrthogonalizeArgs& a, cudaStream_t s) {
-    SmallArgs g{a.in_stride, a.in_pitch, a.out_stride, a.out_pitch, (int)a.rows, (int)a.cols, a.steps, a.rows > a.cols, {a.ca, a.cb, a.cc, 0},
-                a.eps, a.scale, nullptr};
+cudaError_t narrow_typed(const OrthogonalizeArgs& a, cudaStream_t s) {
+    const int64_t n = std::max(a.rows, a.cols);
+    const int ctas = (int)ceil_div(n, kNarrowN);
+    NarrowArgs g{a.in_stride, a.in_pitch, a.out_stride, a.out_pitch, (int)a.rows, (int)a.cols, a.steps, ctas, (int)round_up(ceil_div(n, ctas), 64),
+                 a.rows > a.cols, {a.ca, a.cb, a.cc, 0}, a.eps, a.scale, nullptr};
+    g.ctas = (int)ceil_div(n, g.chunk);
+    static std::atomic<uint64_t> allowed, clusters;
     cudaError_t e = gave_up_flag(&g.gave_up);
-    static std::atomic<uint64_t> allowed;
-    if (e == cudaSuccess) e = allow_shared_memory(reinterpret_cast<const void*>(k_small<T>), kSmallSmem, allowed);
+    if (e == cudaSuccess) e = allow_shared_memory(reinterpret_cast<const void*>(k_narrow<T>), kNarrowSmem, allowed);
+    if (e == cudaSuccess) e = allow_large_clusters(reinterpret_cast<const void*>(k_narrow<T>), clusters);
     if (e != cudaSuccess) return e;
-    launch_chained(k_small<T>, dim3((unsigned)a.n_mats), kSmallThreads, kSmallSmem, s, static_cast<const T*>(a.in), static_cast<T*>(a.out), g);
-    return cudaGetLastError();
+    return launch_clusters(k_narrow<T>, dim3((unsigned)(a.n_mats * g.ctas)), kNarrowThreads, kNarrowSmem, (unsigned)g.ctas, s, static_cast<const T*>(a.in),
+                           static_cast<T*>(a.out), g);
 }
 
-bool is_small(int64_t rows, int64_t cols) { return std::min(rows, cols) <= kSmallM && std::max(rows, cols) <= kSmallN; }
+bool is_narrow(int64_t rows, int64_t cols) { return std::min(rows, cols) <= kNarrowM && std::max(rows, cols) <= kNarrowN * kNarrowCtas; }
 
 }  // namespace
 
@@ -620,11 +719,11 @@ bool orthogonalize_range(double a, double b, double c, int steps) {
 }
 
 int64_t orthogonalize_workspace(int64_t n_mats, int64_t rows, int64_t cols, int32_t dtype) {
-    return is_small(rows, cols) ? 0 : layout(n_mats, rows, cols, dtype, nullptr, nullptr);
+    return is_narrow(rows, cols) ? 0 : layout(n_mats, rows, cols, dtype, nullptr, nullptr);
 }
 
 cudaError_t run_orthogonalize(const OrthogonalizeArgs& a, void* workspace, cudaStream_t s) {
-    if (is_small(a.rows, a.cols)) return a.dtype == A2_BF16 ? small_typed<__nv_bfloat16>(a, s) : small_typed<float>(a, s);
+    if (is_narrow(a.rows, a.cols)) return a.dtype == A2_BF16 ? narrow_typed<__nv_bfloat16>(a, s) : narrow_typed<float>(a, s);
     Layout l;
     layout(a.n_mats, a.rows, a.cols, a.dtype, workspace, &l);
     return a.dtype == A2_BF16 ? typed<__nv_bfloat16>(a, l, s) : typed<float>(a, l, s);
