@@ -17,7 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "liba2cid2.so")
 SOURCES = ["api.cu", "kernels.cu", "scheduler.cpp", "spectral.cpp",
-           "lm_api.cu", "embed.cu", "gemm_sm100.cu", "vocab_loss.cu", "orthogonalize.cu"]
+           "lm_api.cu", "embed.cu", "gemm_sm100.cu", "vocab_loss.cu", "vocab_loss_few.cu", "orthogonalize.cu"]
 
 
 def _nvcc() -> str:

@@ -8,19 +8,13 @@
 #include <algorithm>
 
 #include "gemm_sm100.cuh"
+#include "vocab_loss.cuh"
 
 namespace a2 {
 
 namespace {
 
-constexpr float kLog2E = 1.4426950408889634f;
 constexpr int kPScale = 14;  // P / max |P| <= 1 is held at this power of two with fp32 rows
-
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 
 // Largest finite magnitudes, as bits of non-negative floats (their order is that of the bits): of a CTA of k_scan, or of all.
 struct Scan {
@@ -30,8 +24,6 @@ constexpr int kScanCtas = 148, kScanThreads = 1024;
 
 // The power of two that puts `amax` into [2^14, 2^15).
 __device__ __forceinline__ int word_exponent(uint32_t amax_bits) { return amax_bits ? 14 - ilogbf(__uint_as_float(amax_bits)) : 0; }
-
-__device__ __forceinline__ bool is_token(int32_t y, int64_t vocab) { return y >= 0 && y < vocab; }
 
 // ---- operands -----------------------------------------------------------------------------------
 struct PrepareArgs {
@@ -373,45 +365,6 @@ __global__ void __launch_bounds__(256) k_join_parts(const float* __restrict__ ke
     out[r * pitch + c] = factor(sum);
 }
 
-// Joins the statistics of the parts: 32 tokens a CTA, its warps over the parts.
-constexpr int kFinishWarps = 16;
-__global__ void __launch_bounds__(kFinishWarps * 32) k_finish(const float2* __restrict__ partial, int parts, const float* __restrict__ at_target,
-                                                const int32_t* __restrict__ targets, const int32_t* __restrict__ poisoned, int64_t n, int64_t vocab,
-                                                float* __restrict__ loss, float* __restrict__ lse) {
-    ptx::chained();
-    __shared__ float2 joined[kFinishWarps][32];
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int64_t t = (int64_t)blockIdx.x * 32 + lane;
-    float top = -INFINITY, sum = 0.0f;
-    // eight parts at a time: their loads and exponentials do not wait for one another
-    for (int p0 = warp; t < n && p0 < parts; p0 += 8 * kFinishWarps) {
-        float2 p[8];
-        float next = top;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int at = p0 + k * kFinishWarps;
-            p[k] = at < parts ? partial[(int64_t)at * n + t] : make_float2(-INFINITY, 0.0f);
-            next = fmaxf(next, p[k].x);
-        }
-        const float base = next == -INFINITY ? 0.0f : next;
-        sum *= exp2_fast((top - base) * kLog2E);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum += p[k].y * exp2_fast((p[k].x - base) * kLog2E);
-        top = next;
-    }
-    joined[warp][lane] = make_float2(top, sum);
-    __syncthreads();
-    if (warp == 0 && t < n) {
-        for (int w = 1; w < kFinishWarps; ++w) top = fmaxf(top, joined[w][lane].x);
-        const float base = top == -INFINITY ? 0.0f : top;
-        sum = 0.0f;
-        for (int w = 0; w < kFinishWarps; ++w) sum += joined[w][lane].y * exp2_fast((joined[w][lane].x - base) * kLog2E);
-        const float l = poisoned && poisoned[t] ? NAN : top + logf(sum);
-        lse[t] = l;
-        loss[t] = is_token(targets[t], vocab) ? l - at_target[t] : 0.0f;
-    }
-}
-
 // ---- layout and launches ------------------------------------------------------------------------
 // K blocks a promoted sum stays in tensor memory: 16 steps of the tensor core with fp32 rows, 64 for the loss of bf16 rows
 constexpr int kFlush = 4, kFlushLoss = 16;
@@ -575,10 +528,12 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
 }  // namespace
 
 int64_t vocab_loss_workspace(int64_t n_tokens, int64_t width, int64_t vocab, bool with_grad, int32_t dtype) {
+    if (vocab_loss_is_few(n_tokens, width, vocab, dtype)) return vocab_loss_few_workspace(n_tokens, width, vocab, with_grad);
     return layout(n_tokens, width, vocab, with_grad, dtype, nullptr, nullptr);
 }
 
 cudaError_t run_vocab_loss(const VocabLossArgs& a, void* workspace, cudaStream_t s) {
+    if (vocab_loss_is_few(a.n_tokens, a.width, a.vocab, a.dtype)) return run_vocab_loss_few(a, workspace, s);
     Layout l;
     layout(a.n_tokens, a.width, a.vocab, a.grad_hidden || a.grad_head, a.dtype, workspace, &l);
     return a.dtype == A2_BF16 ? typed<__nv_bfloat16>(a, l, s) : typed<float>(a, l, s);

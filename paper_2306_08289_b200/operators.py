@@ -19,6 +19,7 @@ from . import binding as B
 
 NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)  # a quintic whose iterates send every singular value into about [0.7, 1.2]
 
+_sizes: dict = {}
 _DTYPES = {torch.float32: B.A2_F32, torch.bfloat16: B.A2_BF16}
 
 
@@ -72,13 +73,19 @@ class _Queue:
 
 
 def _workspace(like, size_of, *args):
-    """A workspace of the size the library asks for: (tensor or None, address, bytes)."""
-    need = C.c_int64()
-    B._check(size_of(*args, C.byref(need)))
-    if need.value == 0:
+    """A workspace of the size the library asks for: (tensor or None, address, bytes). The size depends on the arguments alone, so the
+    library is asked once for each."""
+    size = _sizes.get((size_of, args))
+    if size is None:
+        need = C.c_int64()
+        B._check(size_of(*args, C.byref(need)))
+        if len(_sizes) >= 4096:
+            _sizes.clear()
+        size = _sizes[size_of, args] = need.value
+    if size == 0:
         return None, None, 0
-    ws = torch.empty(need.value, dtype=torch.uint8, device=like.device)
-    return ws, ws.data_ptr(), need.value
+    ws = torch.empty(size, dtype=torch.uint8, device=like.device)
+    return ws, ws.data_ptr(), size
 
 
 def embed(table, ids, scale=1.0, out=None, stream=None):
