@@ -78,7 +78,7 @@ def _workspace(like, size_of, *args):
     size = _sizes.get((size_of, args))
     if size is None:
         need = C.c_int64()
-        B._check(size_of(*args, C.byref(need)))
+        B._check(getattr(B.lib(), size_of)(*args, C.byref(need)))
         if len(_sizes) >= 4096:
             _sizes.clear()
         size = _sizes[size_of, args] = need.value
@@ -115,7 +115,7 @@ def embed_grad(grad_out, ids, vocab, scale=1.0, out=None, accumulate=False, stre
         if out is None:
             out = torch.empty(int(vocab), width, dtype=grad_out.dtype, device=grad_out.device)
         out_pitch = _matrix("out", out, grad_out, (int(vocab), width))
-        ws, ws_p, size = _workspace(grad_out, B.lib().a2cid2_embed_grad_workspace, vocab, width, n)
+        ws, ws_p, size = _workspace(grad_out, "a2cid2_embed_grad_workspace", vocab, width, n)
         B._check(B.lib().a2cid2_embed_grad(grad_out.data_ptr(), pitch, ids_p, n, vocab, width, scale, int(accumulate), out.data_ptr(),
                                            out_pitch, _DTYPES[grad_out.dtype], ws_p, size, s))
     return out
@@ -139,7 +139,7 @@ def _vocab_loss(hidden, head, targets, weights, scale, grad_hidden, grad_head, s
         loss = torch.empty(n, dtype=torch.float32, device=device)
         lse = torch.empty(n, dtype=torch.float32, device=device)
         dtype = _DTYPES[hidden.dtype]
-        ws, ws_p, size = _workspace(hidden, B.lib().a2cid2_vocab_loss_workspace, n, width, vocab, int(gh is not None or gw is not None), dtype)
+        ws, ws_p, size = _workspace(hidden, "a2cid2_vocab_loss_workspace", n, width, vocab, int(gh is not None or gw is not None), dtype)
         B._check(B.lib().a2cid2_vocab_loss(hidden.data_ptr(), hidden_pitch, head.data_ptr(), head_pitch, targets_p, n, width, vocab,
                                            weights_p, scale, loss.data_ptr(), lse.data_ptr(), gh_p, gh_pitch, gw_p, gw_pitch, dtype,
                                            ws_p, size, s))
@@ -170,7 +170,7 @@ def orthogonalize(mats, steps=5, coeffs=NEWTON_SCHULZ, eps=1e-7, scale=1.0, out=
             out = torch.empty(mats.shape, dtype=mats.dtype, device=mats.device)
         out_pitch = _matrix("out", out, mats, mats.shape, ndim=3)
         dtype = _DTYPES[mats.dtype]
-        ws, ws_p, size = _workspace(mats, B.lib().a2cid2_orthogonalize_workspace, n, rows, cols, dtype)
+        ws, ws_p, size = _workspace(mats, "a2cid2_orthogonalize_workspace", n, rows, cols, dtype)
         B._check(B.lib().a2cid2_orthogonalize(mats.data_ptr(), mats.stride(0), pitch, n, rows, cols, steps, *coeffs, eps, scale, out.data_ptr(),
                                               out.stride(0), out_pitch, dtype, ws_p, size, s))
     return out
