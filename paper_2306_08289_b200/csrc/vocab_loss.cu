@@ -38,19 +38,33 @@ struct PrepareArgs {
     void *w0, *w1;       // head's words [vocab, ld], or NULL
     int64_t ld;
     float* rate;         // g_t / max |g|, 0 for tokens without a target; NULL without gradients
-    bool hidden_pairs, head_pairs;  // pairs of columns can be read at once
+    bool hidden_fours, head_fours;  // four columns can be read at once
     int32_t* poisoned;   // tokens without a target whose hidden row is not finite: the row is taken as zero, its lse as NaN
 };
 
 template <class T>
-__device__ __forceinline__ uint32_t scan_rows(const T* p, int64_t rows, int64_t width, int64_t pitch, int64_t warp, int64_t warps) {
+__device__ __forceinline__ uint32_t scan_rows(const T* p, bool aligned, int64_t rows, int64_t width, int64_t pitch, int64_t warp, int64_t warps) {
     uint32_t most = 0;
-    for (int64_t r = warp; r < rows; r += warps)
+    auto see = [&](T x) {
+        const uint32_t bits = __float_as_uint(fabsf(widen(x)));
+        if (bits < 0x7f800000u) most = max(most, bits);
+    };
+    for (int64_t r = warp; r < rows; r += warps) {
+        const T* row = p + r * pitch;
+        if (aligned) {
+            int64_t c = threadIdx.x % 32 * 4;
+#pragma unroll 4
+            for (; c + 4 <= width; c += 128) {
+                const Pack<T, 4> x = *reinterpret_cast<const Pack<T, 4>*>(row + c);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) see(x.v[k]);
+            }
+            for (int k = 0; k < 4 && c + k < width; ++k) see(row[c + k]);
+        } else {
 #pragma unroll 8
-        for (int64_t c = threadIdx.x % 32; c < width; c += 32) {
-            const uint32_t bits = __float_as_uint(fabsf(widen(p[r * pitch + c])));
-            if (bits < 0x7f800000u) most = max(most, bits);
+            for (int64_t c = threadIdx.x % 32; c < width; c += 32) see(row[c]);
         }
+    }
     return most;
 }
 
@@ -62,8 +76,8 @@ __global__ void __launch_bounds__(kScanThreads) k_scan(PrepareArgs a) {
     const int64_t warp = (int64_t)blockIdx.x * (kScanThreads / 32) + threadIdx.x / 32, warps = (int64_t)gridDim.x * (kScanThreads / 32);
     Scan most{};
     if (sizeof(T) == 4) {
-        most.hidden = scan_rows(static_cast<const T*>(a.hidden), a.n, a.width, a.hidden_pitch, warp, warps);
-        most.head = scan_rows(static_cast<const T*>(a.head), a.vocab, a.width, a.head_pitch, warp, warps);
+        most.hidden = scan_rows(static_cast<const T*>(a.hidden), a.hidden_fours, a.n, a.width, a.hidden_pitch, warp, warps);
+        most.head = scan_rows(static_cast<const T*>(a.head), a.head_fours, a.vocab, a.width, a.head_pitch, warp, warps);
     }
     if (a.weights)
         for (int64_t t = warp * 32 + threadIdx.x % 32; t < a.n; t += warps * 32) {
@@ -100,35 +114,37 @@ __device__ __forceinline__ Scan join_scan(const Scan* parts) {
     return most;
 }
 
-// Two columns a lane, so that a warp's stores are 128 bytes; `aligned`: the pairs can be read at once.
+// Four columns a lane; `aligned`: they can be read at once. ld is a multiple of 64: what a lane writes past the width is padding.
 template <class T>
 __device__ __forceinline__ void pack_row(const T* from, bool aligned, void* to0, void* to1, int64_t at, int64_t width, int64_t ld, int e, bool zero) {
     const PowerOfTwo up(e);
 #pragma unroll 4
-    for (int64_t c = threadIdx.x % 32 * 2; c < width; c += 64) {
-        Pack<T, 2> x;
-        if (aligned && c + 1 < width) {
-            x = *reinterpret_cast<const Pack<T, 2>*>(from + c);
+    for (int64_t c = threadIdx.x % 32 * 4; c < width; c += 128) {
+        Pack<T, 4> x;
+        if (aligned && c + 4 <= width) {
+            x = *reinterpret_cast<const Pack<T, 4>*>(from + c);
         } else {
-            x.v[0] = from[c];
-            x.v[1] = c + 1 < width ? from[c + 1] : narrow<T>(0.0f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x.v[k] = c + k < width ? from[c + k] : narrow<T>(0.0f);
         }
-        if (zero) x.v[0] = x.v[1] = narrow<T>(0.0f);
+        if (zero)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x.v[k] = narrow<T>(0.0f);
         if constexpr (sizeof(T) == 4) {
-            Pack<__half, 2> h, l;
-            split_words(up(x.v[0]), h.v[0], l.v[0]);
-            split_words(up(x.v[1]), h.v[1], l.v[1]);
-            *reinterpret_cast<Pack<__half, 2>*>(static_cast<__half*>(to0) + at * ld + c) = h;  // ld is even: the second one may be padding
-            *reinterpret_cast<Pack<__half, 2>*>(static_cast<__half*>(to1) + at * ld + c) = l;
+            Pack<__half, 4> h, l;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) split_words(up(x.v[k]), h.v[k], l.v[k]);
+            *reinterpret_cast<Pack<__half, 4>*>(static_cast<__half*>(to0) + at * ld + c) = h;
+            *reinterpret_cast<Pack<__half, 4>*>(static_cast<__half*>(to1) + at * ld + c) = l;
         } else {
-            *reinterpret_cast<Pack<T, 2>*>(static_cast<T*>(to0) + at * ld + c) = x;
+            *reinterpret_cast<Pack<T, 4>*>(static_cast<T*>(to0) + at * ld + c) = x;
         }
     }
 }
 
 template <class T>
-bool pairs_aligned(const void* p, int64_t pitch) {
-    return reinterpret_cast<uintptr_t>(p) % (2 * sizeof(T)) == 0 && pitch % 2 == 0;
+bool fours_aligned(const void* p, int64_t pitch) {
+    return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0 && pitch % 4 == 0;
 }
 
 // The operands of the products in the workspace, a warp a row: two words of fp32 rows, a copy of bf16 ones where
@@ -147,7 +163,7 @@ __global__ void __launch_bounds__(256) k_pack(PrepareArgs a) {
     for (int64_t r = warp; r < rows; r += (int64_t)gridDim.x * 8) {
         if (r >= a.n) {
             const int64_t v = r - a.n;
-            pack_row(static_cast<const T*>(a.head) + v * a.head_pitch, a.head_pairs, a.w0, a.w1, v, a.width, a.ld, a.w1 ? word_exponent(scan.head) : 0,
+            pack_row(static_cast<const T*>(a.head) + v * a.head_pitch, a.head_fours, a.w0, a.w1, v, a.width, a.ld, a.w1 ? word_exponent(scan.head) : 0,
                      false);
             continue;
         }
@@ -164,7 +180,7 @@ __global__ void __launch_bounds__(256) k_pack(PrepareArgs a) {
             bad = __any_sync(0xffffffffu, bad);
         }
         if (threadIdx.x % 32 == 0) a.poisoned[r] = bad;
-        pack_row(from, a.hidden_pairs, a.h0, a.h1, r, a.width, a.ld, a.h1 ? word_exponent(scan.hidden) : 0, bad);
+        pack_row(from, a.hidden_fours, a.h0, a.h1, r, a.width, a.ld, a.h1 ? word_exponent(scan.hidden) : 0, bad);
     }
 }
 
@@ -445,7 +461,7 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
     const bool hidden_in_place = in_place(a.hidden, a.hidden_pitch) && !a.grad_head;
     const bool head_in_place = in_place(a.head, a.head_pitch);
     PrepareArgs prep{a.hidden, a.head, a.targets, a.weights, n, a.width, a.vocab, a.hidden_pitch, a.head_pitch, nullptr, l.scan_parts, nullptr, nullptr,
-                     nullptr, nullptr, l.ld, with_grad ? l.rate : nullptr, pairs_aligned<T>(a.hidden, a.hidden_pitch), pairs_aligned<T>(a.head, a.head_pitch),
+                     nullptr, nullptr, l.ld, with_grad ? l.rate : nullptr, fours_aligned<T>(a.hidden, a.hidden_pitch), fours_aligned<T>(a.head, a.head_pitch),
                      l.poisoned};
     const bool weighted = with_grad && a.weights;
     if (!with_grad) prep.weights = nullptr;
