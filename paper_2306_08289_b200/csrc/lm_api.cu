@@ -26,7 +26,8 @@ int status(cudaError_t e, const char* what) {
     return e == cudaSuccess ? A2_OK : fail(A2_ECUDA, "%s: %s (%s)", what, cudaGetErrorName(e), cudaGetErrorString(e));
 }
 
-constexpr int64_t kMaxRows = (int64_t(1) << 31) - 2;  // ids, tokens, vocabulary rows
+constexpr int64_t kMaxRows = int64_t(1) << 30;        // ids, tokens, vocabulary rows
+constexpr int64_t kMaxSorted = int64_t(1) << 26;      // ids of a gradient: every tile of the sort reads the counts of all tiles
 constexpr int64_t kMaxWidth = int64_t(1) << 20;       // columns of a matrix
 constexpr int64_t kMaxMats = 65535;                   // matrices of a batch
 constexpr int64_t kMaxPitch = int64_t(1) << 40;       // elements; keeps row * pitch inside 64 bits with room
@@ -118,6 +119,7 @@ int a2cid2_embed(const void* table, int64_t vocab, int64_t width, int64_t table_
 int a2cid2_embed_grad_workspace(int64_t vocab, int64_t width, int64_t n_ids, int64_t* bytes) {
     A2_CHECK(bytes, A2_EINVAL, "bytes is NULL");
     A2_TRY(check_table_sizes(vocab, width, n_ids));
+    A2_CHECK(n_ids <= kMaxSorted, A2_ERANGE, "more than %lld ids in a gradient", (long long)kMaxSorted);
     *bytes = a2::embed_grad_workspace(vocab, width, n_ids);
     return A2_OK;
 }
@@ -127,6 +129,7 @@ int a2cid2_embed_grad(const void* grad_out, int64_t grad_out_pitch, const int32_
                       int32_t storage_dtype, void* workspace, int64_t workspace_bytes, void* cuda_stream) {
     A2_TRY(check_type(storage_dtype));
     A2_TRY(check_table_sizes(vocab, width, n_ids));
+    A2_CHECK(n_ids <= kMaxSorted, A2_ERANGE, "more than %lld ids in a gradient", (long long)kMaxSorted);
     A2_TRY(check_number("scale", scale));
     A2_TRY(check_matrix("grad_out", grad_out, n_ids, width, grad_out_pitch, storage_dtype));
     A2_TRY(check_ids("ids", ids, n_ids));

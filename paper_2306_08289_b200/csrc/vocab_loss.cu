@@ -18,7 +18,7 @@ constexpr int kPScale = 14;  // P / max |P| <= 1 is held at this power of two wi
 
 // Largest finite magnitudes, as bits of non-negative floats (their order is that of the bits): of a CTA of k_scan, or of all.
 struct Scan {
-    uint32_t hidden, head, weight, unused;
+    uint32_t hidden, head, weight, unused;  // hidden: of the tokens with a target
 };
 constexpr int kScanCtas = 148, kScanThreads = 1024;
 
@@ -39,17 +39,20 @@ struct PrepareArgs {
     int64_t ld;
     float* rate;         // g_t / max |g|, 0 for tokens without a target; NULL without gradients
     bool hidden_fours, head_fours;  // four columns can be read at once
+    int32_t* exponents;  // of the words of each row of hidden
     int32_t* poisoned;   // tokens without a target whose hidden row is not finite: the row is taken as zero, its lse as NaN
 };
 
 template <class T>
-__device__ __forceinline__ uint32_t scan_rows(const T* p, bool aligned, int64_t rows, int64_t width, int64_t pitch, int64_t warp, int64_t warps) {
+__device__ __forceinline__ uint32_t scan_rows(const T* p, bool aligned, int64_t rows, int64_t width, int64_t pitch, int64_t warp, int64_t warps,
+                                              const int32_t* targets, int64_t vocab) {
     uint32_t most = 0;
     auto see = [&](T x) {
         const uint32_t bits = __float_as_uint(fabsf(widen(x)));
         if (bits < 0x7f800000u) most = max(most, bits);
     };
     for (int64_t r = warp; r < rows; r += warps) {
+        if (targets && !is_token(targets[r], vocab)) continue;
         const T* row = p + r * pitch;
         if (aligned) {
             int64_t c = threadIdx.x % 32 * 4;
@@ -76,8 +79,9 @@ __global__ void __launch_bounds__(kScanThreads) k_scan(PrepareArgs a) {
     const int64_t warp = (int64_t)blockIdx.x * (kScanThreads / 32) + threadIdx.x / 32, warps = (int64_t)gridDim.x * (kScanThreads / 32);
     Scan most{};
     if (sizeof(T) == 4) {
-        most.hidden = scan_rows(static_cast<const T*>(a.hidden), a.hidden_fours, a.n, a.width, a.hidden_pitch, warp, warps);
-        most.head = scan_rows(static_cast<const T*>(a.head), a.head_fours, a.vocab, a.width, a.head_pitch, warp, warps);
+        most.hidden = scan_rows(static_cast<const T*>(a.hidden), a.hidden_fours, a.n, a.width, a.hidden_pitch, warp, warps,
+                                a.targets, a.vocab);
+        most.head = scan_rows(static_cast<const T*>(a.head), a.head_fours, a.vocab, a.width, a.head_pitch, warp, warps, nullptr, 0);
     }
     if (a.weights)
         for (int64_t t = warp * 32 + threadIdx.x % 32; t < a.n; t += warps * 32) {
@@ -149,7 +153,8 @@ bool fours_aligned(const void* p, int64_t pitch) {
 
 // The operands of the products in the workspace, a warp a row: two words of fp32 rows, a copy of bf16 ones where
 // TMA cannot read them in place. A token without a target must add nothing to dW = P^T h: 0 * NaN would, so such a row of hidden
-// becomes zero when it holds anything that is not finite.
+// becomes zero when it holds anything that is not finite. Nor may it weigh on the others' precision: all tokens with a target share
+// one power of two (dW adds them up), one without has its own.
 template <class T>
 __global__ void __launch_bounds__(256) k_pack(PrepareArgs a) {
     ptx::chained();
@@ -174,13 +179,20 @@ __global__ void __launch_bounds__(256) k_pack(PrepareArgs a) {
         }
         if (!a.h0) continue;
         const T* from = static_cast<const T*>(a.hidden) + r * a.hidden_pitch;
+        uint32_t most = scan.hidden;
         bool bad = false;
         if (!live) {
-            for (int64_t c = threadIdx.x % 32; c < a.width; c += 32) bad |= !isfinite(widen(from[c]));
-            bad = __any_sync(0xffffffffu, bad);
+            most = 0;
+            for (int64_t c = threadIdx.x % 32; c < a.width; c += 32) most = max(most, __float_as_uint(fabsf(widen(from[c]))));
+            most = __reduce_max_sync(0xffffffffu, most);
+            bad = most >= 0x7f800000u;
         }
-        if (threadIdx.x % 32 == 0) a.poisoned[r] = bad;
-        pack_row(from, a.hidden_fours, a.h0, a.h1, r, a.width, a.ld, a.h1 ? word_exponent(scan.hidden) : 0, bad);
+        const int e = a.h1 && !bad ? word_exponent(most) : 0;
+        if (threadIdx.x % 32 == 0) {
+            a.poisoned[r] = bad;
+            if (a.h1) a.exponents[r] = e;
+        }
+        pack_row(from, a.hidden_fours, a.h0, a.h1, r, a.width, a.ld, e, bad);
     }
 }
 
@@ -193,6 +205,7 @@ struct StatisticsEpi {
         float* at_target;
         const int32_t* targets;
         const Scan* scan;
+        const int32_t* exponents;
         int64_t n, vocab;
     };
     const Args& a;
@@ -201,7 +214,7 @@ struct StatisticsEpi {
     float top = -INFINITY, sum = 0.0f;
     PowerOfTwo unscale;
     __device__ __forceinline__ StatisticsEpi(const Args& args, const Tile& t, int row0, int col, int lane, float*)
-        : a(args), row((int64_t)row0 + lane), col0(col), unscale(kWords ? -(word_exponent(args.scan->hidden) + word_exponent(args.scan->head)) : 0) {
+        : a(args), row((int64_t)row0 + lane), col0(col), unscale(kWords && row < args.n ? -(args.exponents[row] + word_exponent(args.scan->head)) : 0) {
         target = row < a.n ? a.targets[row] : -1;
     }
     __device__ __forceinline__ void chunk(int c, float (&v)[32]) {
@@ -246,6 +259,7 @@ struct ProbabilityEpi {
         const float* lse;
         const float* rate;
         const Scan* scan;
+        const int32_t* exponents;
         int64_t n, vocab, v0;
     };
     const Args& a;
@@ -262,7 +276,7 @@ struct ProbabilityEpi {
           col0(col),
           lane(lane_),
           staging(staging_),
-          unscale(kWords ? -(word_exponent(args.scan->hidden) + word_exponent(args.scan->head)) : 0) {
+          unscale(kWords && row < args.n ? -(args.exponents[row] + word_exponent(args.scan->head)) : 0) {
         target = -1;
         if (row < a.n) {
             lse = a.lse[row];
@@ -390,7 +404,7 @@ struct Layout {
     void *h0, *h1, *w0, *w1, *p0, *p1;
     float2* partial;
     float *at_target, *rate, *kept, *head_kept;
-    int32_t* poisoned;
+    int32_t *exponents, *poisoned;
     int64_t ld, p_ld, kept_ld, piece;
     int hidden_parts, head_parts;  // of K, in the gradients' products
 };
@@ -427,6 +441,7 @@ int64_t layout(int64_t n, int64_t width, int64_t vocab, bool with_grad, int32_t 
     }
     l.partial = w.take<float2>(2 * ceil_div(vocab, kTileN) * n);
     l.at_target = w.take<float>(n);
+    l.exponents = w.take<int32_t>(n);
     l.poisoned = w.take<int32_t>(n);
     if (with_grad) {
         l.piece = piece_rows(n, width, vocab, words);
@@ -457,12 +472,12 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
         return cudaMemset2DAsync(a.grad_head, a.grad_head_pitch * sizeof(T), 0, a.width * sizeof(T), a.vocab, s);
     }
     // operands: in place where TMA can read them (bf16, 16-byte rows), else from the workspace
-    auto in_place = [](const void* p, int64_t pitch) { return !kWords && reinterpret_cast<uintptr_t>(p) % 16 == 0 && pitch % 8 == 0; };
+    auto in_place = [](const void* p, int64_t pitch) { return !kWords && reinterpret_cast<uintptr_t>(p) % 16 == 0 && pitch % 8 == 0 && pitch < (int64_t(1) << 38); };
     const bool hidden_in_place = in_place(a.hidden, a.hidden_pitch) && !a.grad_head;
     const bool head_in_place = in_place(a.head, a.head_pitch);
     PrepareArgs prep{a.hidden, a.head, a.targets, a.weights, n, a.width, a.vocab, a.hidden_pitch, a.head_pitch, nullptr, l.scan_parts, nullptr, nullptr,
                      nullptr, nullptr, l.ld, with_grad ? l.rate : nullptr, fours_aligned<T>(a.hidden, a.hidden_pitch), fours_aligned<T>(a.head, a.head_pitch),
-                     l.poisoned};
+                     l.exponents, l.poisoned};
     const bool weighted = with_grad && a.weights;
     if (!with_grad) prep.weights = nullptr;
     if (kWords || weighted) prep.scan = l.scan;
@@ -489,7 +504,7 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
     // the loss is fp32 with either storage type, so its sums are promoted with both
     e = make_gemm(hidden(false), head(0, a.vocab, false), 1, !kWords, false, kWords ? kFlush : kFlushLoss, 1, &g);
     if (e != cudaSuccess) return e;
-    const typename StatisticsEpi<kWords>::Args stats{l.partial, l.at_target, a.targets, l.scan, n, a.vocab};
+    const typename StatisticsEpi<kWords>::Args stats{l.partial, l.at_target, a.targets, l.scan, l.exponents, n, a.vocab};
     e = launch_gemm<StatisticsEpi<kWords>, true>(g, stats, s);
     if (e != cudaSuccess) return e;
     launch_chained(k_finish, dim3((unsigned)ceil_div(n, 32)), kFinishWarps * 32, 0, s, l.partial, (int)(2 * ceil_div(a.vocab, kTileN)), l.at_target, a.targets,
@@ -508,7 +523,7 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
         const bool first = v0 == 0, final = v0 + rows == a.vocab;
         e = make_gemm(hidden(false), head(v0, rows, false), 1, !kWords, false, flush, 1, &g);
         if (e != cudaSuccess) return e;
-        const typename ProbabilityEpi<kWords>::Args prob{l.p0, l.p1, l.p_ld, a.targets, a.lse, l.rate, l.scan, n, a.vocab, v0};
+        const typename ProbabilityEpi<kWords>::Args prob{l.p0, l.p1, l.p_ld, a.targets, a.lse, l.rate, l.scan, l.exponents, n, a.vocab, v0};
         e = launch_gemm<ProbabilityEpi<kWords>, kWords>(g, prob, s);
         if (e != cudaSuccess) return e;
         if (a.grad_head) {

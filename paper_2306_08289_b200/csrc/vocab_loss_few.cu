@@ -71,7 +71,8 @@ __global__ void __launch_bounds__(kFewThreads) k_few_logits(const VocabLossArgs 
     ptx::chained();
     const T* hidden = static_cast<const T*>(a.hidden);
     const T* head = static_cast<const T*>(a.head);
-    const int64_t t0 = (int64_t)blockIdx.y * kM, v0 = (int64_t)blockIdx.x * kN;
+    const int64_t parts = (a.vocab + kN - 1) / kN, part = blockIdx.x % parts;  // along the vocabulary first
+    const int64_t t0 = blockIdx.x / parts * kM, v0 = part * kN;
     float sums[4][4] = {};
     tile_product<true, true>(
         sums, a.width, [&](int m, int64_t k) { return t0 + m < a.n_tokens && k < a.width ? widen(hidden[(t0 + m) * a.hidden_pitch + k]) : 0.0f; },
@@ -100,7 +101,7 @@ __global__ void __launch_bounds__(kFewThreads) k_few_logits(const VocabLossArgs 
 #pragma unroll
         for (int v = 0; v < 4; ++v) sum += exp2_fast((sums[u][v] - base) * kLog2E);
         for (int o = 8; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (tx == 0 && row) partial[t * gridDim.x + blockIdx.x] = make_float2(most, sum);
+        if (tx == 0 && row) partial[t * parts + part] = make_float2(most, sum);
     }
 }
 
@@ -253,7 +254,7 @@ template <class T>
 cudaError_t typed(const VocabLossArgs& a, const Layout& l, cudaStream_t s) {
     const int64_t n = a.n_tokens, parts = ceil_div(a.vocab, kN);
     const bool with_grad = a.grad_hidden || a.grad_head;
-    launch_chained(k_few_logits<T>, dim3((unsigned)parts, (unsigned)ceil_div(n, kM)), kFewThreads, 0, s, a, l.z, l.z_ld, l.partial, l.at_target);
+    launch_chained(k_few_logits<T>, dim3((unsigned)(parts * ceil_div(n, kM))), kFewThreads, 0, s, a, l.z, l.z_ld, l.partial, l.at_target);
     launch_chained(k_few_rows, dim3((unsigned)n, with_grad ? (unsigned)ceil_div(a.vocab, kRowColumns) : 1u), kFewThreads, 0, s, a, l.partial, (int)parts,
                    l.at_target, with_grad, l.z, l.z_ld);
     if (!with_grad) return cudaGetLastError();

@@ -83,7 +83,7 @@ def grad_reference(dy, ids, vocab, scale):
 @pytest.mark.parametrize("n,vocab,width,kind", [
     (0, 7, 16, "uniform"), (1, 1, 1, "uniform"), (1, 700, 64, "uniform"), (31, 3, 40, "uniform"), (500, 1, 33, "uniform"),
     (511, 600, 136, "one"), (4096, 513, 64, "skewed"), (4097, 511, 24, "skewed"), (6000, 262145, 8, "skewed"), (9000, 40, 260, "one"),
-    (20000, 9000, 72, "skewed"), (20000, 5, 17, "uniform"), (300, 300, 2056, "skewed"), (64, 90, 16, "none")])
+    (20000, 9000, 72, "skewed"), (20000, 5, 17, "uniform"), (300, 300, 2056, "skewed"), (64, 90, 16, "none"), (8192, 3000, 24, "skewed"), (8000, 70000, 40, "uniform"), (70000, 20000, 20, "skewed")])
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_embed_grad(storage, n, vocab, width, kind, accumulate):
     g, dt = gen(n + vocab), DT[storage]
@@ -170,7 +170,7 @@ def loss_bounds(hidden, head, targets, g, lse, P, clean, live, storage):
 
 
 SIZES = [(1, 8, 5), (1, 64, 1), (3, 1, 17), (5, 16, 257), (33, 40, 256), (128, 64, 129), (129, 201, 1003), (200, 72, 5003), (260, 328, 511),
-         (64, 24, 9000)]
+         (64, 24, 9000), (700, 520, 1300), (513, 88, 5000)]
 
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
@@ -231,6 +231,25 @@ def test_vocab_loss_edges(storage):
     zeroed = torch.where(fine[:, None], hidden, torch.zeros_like(hidden))
     b = ops.vocab_loss_grad(zeroed, head, some, scale=0.5)
     assert torch.equal(a[0], b[0]) and torch.equal(a[2], b[2]) and torch.equal(a[3], b[3])
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("n,width,vocab", [(70, 48, 300), (700, 264, 2000)])
+def test_rows_without_a_target_do_not_weigh_on_the_others(storage, n, width, vocab):
+    """Finite garbage of any size in rows without a target: the other rows keep every bit, and the garbage rows have their own lse."""
+    g, dt = gen(n), DT[storage]
+    hidden = torch.randn(n, width, generator=g, device=DEV).to(dt)
+    head = (torch.randn(vocab, width, generator=g, device=DEV) / math.sqrt(width)).to(dt)
+    targets = torch.randint(0, vocab, (n,), generator=g, device=DEV, dtype=torch.int32)
+    off = torch.arange(n, device=DEV) % 5 == 2
+    targets[off] = -1
+    a = ops.vocab_loss_grad(torch.where(off[:, None], 0.0, hidden).to(dt), head, targets, scale=0.5)
+    garbage = hidden * torch.exp2(torch.randint(-60, 90, (n, 1), generator=g, device=DEV).float()).to(dt)
+    b = ops.vocab_loss_grad(torch.where(off[:, None], garbage, hidden), head, targets, scale=0.5)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[2], b[2]) and torch.equal(a[3], b[3]) and torch.equal(a[1][~off], b[1][~off])
+    z = garbage[off].double() @ head.double().T
+    tol = (garbage[off].double().abs() @ head.double().abs().T).amax(1) * (2.0**-21 + width * 2.0**-23) + 2.0**-14
+    assert ((b[1][off].double() - torch.logsumexp(z, 1)).abs() <= tol).all()
 
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
@@ -327,7 +346,8 @@ def check_orthogonalize(mats, got, storage, steps=5, coeffs=ops.NEWTON_SCHULZ, e
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
 @pytest.mark.parametrize("mats,rows,cols", [(1, 1, 1), (2, 1, 40), (2, 40, 1), (3, 8, 8), (2, 17, 33), (5, 64, 64), (2, 100, 65), (2, 128, 128),
-                                            (2, 129, 140), (3, 256, 200), (1, 300, 1000), (2, 513, 257), (1, 640, 640)])
+                                            (2, 129, 140), (3, 256, 200), (1, 300, 1000), (2, 513, 257), (1, 640, 640), (2, 21, 1030), (3, 2577, 19), (2, 97, 282), (1, 128, 4096),
+                                            (2, 4000, 128), (1, 40, 4500), (5, 200, 700)])
 def test_orthogonalize(storage, mats, rows, cols):
     g, dt = gen(rows * 3 + cols), DT[storage]
     pad, shift = SHIFTS[(rows + cols) % 3]
