@@ -53,7 +53,17 @@ __device__ __forceinline__ void units(const MatScale& s, const Poly& p, float* n
 // ---- norm and first words ------------------------------------------------------------------------
 constexpr int kNormThreads = 256;
 
-template <class T>
+// Columns j .. j + VEC - 1 of a row, 0 past its end. Only whole groups are read at once, and those only where rows allow it (VEC = 1 else).
+template <class T, int VEC>
+__device__ __forceinline__ Pack<T, VEC> read_columns(const T* row, int64_t j, int64_t cols) {
+    if (j + VEC <= cols) return *reinterpret_cast<const Pack<T, VEC>*>(row + j);
+    Pack<T, VEC> x;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) x.v[k] = j + k < cols ? row[j + k] : narrow<T>(0.0f);
+    return x;
+}
+
+template <class T, int VEC>
 __global__ void __launch_bounds__(kNormThreads) k_norm(const T* __restrict__ in, int64_t stride, int64_t pitch, int64_t rows, int64_t cols,
                                                        double* __restrict__ partial) {
     ptx::chained();
@@ -63,9 +73,13 @@ __global__ void __launch_bounds__(kNormThreads) k_norm(const T* __restrict__ in,
     const int64_t warp = (int64_t)blockIdx.x * (kNormThreads / 32) + threadIdx.x / 32, warps = (int64_t)gridDim.x * (kNormThreads / 32);
     for (int64_t i = warp; i < rows; i += warps) {
 #pragma unroll 4
-        for (int64_t j = threadIdx.x % 32; j < cols; j += 32) {
-            const double v = widen(g[i * pitch + j]);  // the squares of fp32 values may leave fp32
-            sum += v * v;
+        for (int64_t j = threadIdx.x % 32 * VEC; j < cols; j += 32 * VEC) {
+            const Pack<T, VEC> x = read_columns<T, VEC>(g + i * pitch, j, cols);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                const double v = widen(x.v[k]);  // the squares of fp32 values may leave fp32
+                sum += v * v;
+            }
         }
     }
     for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -86,11 +100,10 @@ __device__ __forceinline__ MatScale mat_scale(double squares, double eps) {
     return {(float)(1.0 / (ldexp(by, e))), e, min(0, ilogb(norm / by) + 1)};
 }
 
-// Words of G 2^e, [rows, ld]. Two columns a lane, so that a warp's stores are 128 bytes; `aligned`: G's pairs can be read at once.
-template <class T>
+// Words of G 2^e, [rows, ld].
+template <class T, int VEC>
 __global__ void __launch_bounds__(kNormThreads) k_first_words(const T* __restrict__ in, int64_t stride, int64_t pitch, int64_t rows, int64_t cols,
-                                                              const double* __restrict__ partial, int parts, double eps, bool aligned,
-                                                              __half* __restrict__ hi, __half* __restrict__ lo, int64_t ld,
+                                                              const double* __restrict__ partial, int parts, double eps, __half* __restrict__ hi, __half* __restrict__ lo, int64_t ld,
                                                               MatScale* __restrict__ scales) {
     ptx::chained();
     __shared__ MatScale shared;
@@ -110,20 +123,13 @@ __global__ void __launch_bounds__(kNormThreads) k_first_words(const T* __restric
     const int64_t warp = (int64_t)blockIdx.x * (kNormThreads / 32) + threadIdx.x / 32, warps = (int64_t)gridDim.x * (kNormThreads / 32);
     for (int64_t i = warp; i < rows; i += warps)
 #pragma unroll 4
-        for (int64_t j = threadIdx.x % 32 * 2; j < cols; j += 64) {
-            Pack<T, 2> x;
-            const T* at = g + i * pitch + j;
-            if (aligned && j + 1 < cols) {
-                x = *reinterpret_cast<const Pack<T, 2>*>(at);
-            } else {
-                x.v[0] = at[0];
-                x.v[1] = j + 1 < cols ? at[1] : narrow<T>(0.0f);
-            }
-            Pack<__half, 2> h, l;
-            split_words(up(widen(x.v[0])), h.v[0], l.v[0]);
-            split_words(up(widen(x.v[1])), h.v[1], l.v[1]);
-            *reinterpret_cast<Pack<__half, 2>*>(hi + base + i * ld + j) = h;  // ld is even: the second one may be padding
-            if (lo) *reinterpret_cast<Pack<__half, 2>*>(lo + base + i * ld + j) = l;
+        for (int64_t j = threadIdx.x % 32 * VEC; j < cols; j += 32 * VEC) {
+            const Pack<T, VEC> x = read_columns<T, VEC>(g + i * pitch, j, cols);
+            Pack<__half, VEC> h, l;
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) split_words(up(widen(x.v[k])), h.v[k], l.v[k]);
+            *reinterpret_cast<Pack<__half, VEC>*>(hi + base + i * ld + j) = h;  // ld is a multiple of 64: the last ones may be padding
+            if (lo) *reinterpret_cast<Pack<__half, VEC>*>(lo + base + i * ld + j) = l;
         }
 }
 
@@ -333,10 +339,15 @@ cudaError_t typed(const OrthogonalizeArgs& a, Layout l, cudaStream_t s) {
     const bool tall = a.rows > a.cols;
     const int64_t m = std::min(a.rows, a.cols), n = std::max(a.rows, a.cols);
     const dim3 grid((unsigned)l.parts, (unsigned)a.n_mats);
-    const bool aligned = reinterpret_cast<uintptr_t>(a.in) % (2 * sizeof(T)) == 0 && a.in_pitch % 2 == 0 && (a.n_mats == 1 || a.in_stride % 2 == 0);
-    launch_chained(k_norm<T>, grid, kNormThreads, 0, s, static_cast<const T*>(a.in), a.in_stride, a.in_pitch, a.rows, a.cols, l.partial);
-    launch_chained(k_first_words<T>, grid, kNormThreads, 0, s, static_cast<const T*>(a.in), a.in_stride, a.in_pitch, a.rows, a.cols, l.partial, (int)l.parts,
-                                                   a.eps, aligned, l.x.hi, l.x.lo, l.x.ld, l.scales);
+    constexpr int kVec = 16 / sizeof(T);
+    const bool aligned = reinterpret_cast<uintptr_t>(a.in) % 16 == 0 && a.in_pitch % kVec == 0 && (a.n_mats == 1 || a.in_stride % kVec == 0);
+    auto first = [&](auto norm, auto words) {
+        launch_chained(norm, grid, kNormThreads, 0, s, static_cast<const T*>(a.in), a.in_stride, a.in_pitch, a.rows, a.cols, l.partial);
+        launch_chained(words, grid, kNormThreads, 0, s, static_cast<const T*>(a.in), a.in_stride, a.in_pitch, a.rows, a.cols, l.partial, (int)l.parts, a.eps,
+                       l.x.hi, l.x.lo, l.x.ld, l.scales);
+    };
+    if (aligned) first(k_norm<T, kVec>, k_first_words<T, kVec>);
+    else first(k_norm<T, 1>, k_first_words<T, 1>);
     if (a.steps == 0)
         launch_chained(k_normalized<T>, grid, kNormThreads, 0, s, l.x.hi, l.x.lo, l.x.ld, a.rows, a.cols, l.scales, a.scale, static_cast<T*>(a.out), a.out_stride,
                                                       a.out_pitch);
