@@ -429,7 +429,8 @@ int a2cid2_vocab_loss_workspace(int64_t n_tokens, int64_t width, int64_t vocab, 
 
 /* Softmax cross entropy of hidden [n_tokens, width] against the vocabulary's matrix head [vocab, width]:
  *   z_tv = <hidden_t, head_v>,  lse[t] = log sum_v exp z_tv,  loss[t] = lse[t] - z_{t, targets[t]}
- * (0 where targets[t] is no token), both float [n_tokens]. The logits are made in pieces and never kept.
+ * (0 where targets[t] is no token), both float [n_tokens]. The logits are made in pieces and not kept (of small
+ * problems up to 64 MB of them are, in the workspace).
  * With grad_hidden [n_tokens, width] and/or grad_head [vocab, width] not NULL the same call gives the gradients of
  * sum_t scale * weights[t] * loss[t] (weights: float [n_tokens] or NULL for ones):
  *   P_tv = scale * weights[t] * (exp(z_tv - lse[t]) - [v = targets[t]]), 0 where targets[t] is no token,

@@ -377,9 +377,17 @@ __device__ __forceinline__ void load_operand(const CUtensorMap* map, bool turned
 // Epilogue: constructed per tile by every thread of the eight warps as
 //   Epi(args, tile, row of lane 0 of the warp, first column of the thread's 128, lane, staging of the warp)
 // then chunk(c, v) for c = 0 .. 3 with the sums of row (row0 + lane), columns col0 + 32 c .., then finish().
-template <class Epi, bool kPromote>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
-    k_gemm(const __grid_constant__ GemmArgs g, const __grid_constant__ typename Epi::Args args) {
+//
+// A launch takes one product or two independent ones (kJobs), whose tiles it hands out one after the other: two that would each
+// leave CTAs idle fill the GPU together.
+template <class Epi, int kJobs>
+struct Jobs {
+    GemmArgs g[kJobs];
+    typename Epi::Args args[kJobs];
+};
+
+template <class Epi, bool kPromote, int kJobs>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_gemm(const __grid_constant__ Jobs<Epi, kJobs> jobs) {
     extern __shared__ char raw[];
     char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     float* staging = reinterpret_cast<float*>(smem + kStages * kStageBytes);
@@ -390,9 +398,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
     const uint32_t rank = ptx::cta_rank();
 
     if (warp == kEpilogueWarps + 1 && lane == 0)
-        for (int w = 0; w < (g.passes == 1 ? 1 : 2); ++w) {
-            asm volatile("prefetch.tensormap [%0];" ::"l"(&g.a[w]) : "memory");
-            asm volatile("prefetch.tensormap [%0];" ::"l"(&g.b[w]) : "memory");
+        for (int w = 0; w < (jobs.g[0].passes == 1 ? 1 : 2); ++w) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&jobs.g[0].a[w]) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&jobs.g[0].b[w]) : "memory");
         }
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
@@ -417,8 +425,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
     ptx::release_next();
     ptx::wait_previous();
 
-    const int n_tiles = tiles_of(g);
+    const int first_tiles = tiles_of(jobs.g[0]), n_tiles = first_tiles + (kJobs > 1 ? tiles_of(jobs.g[kJobs - 1]) : 0);
     const int first = blockIdx.x / 2, step = gridDim.x / 2;
+    int* const gave_up = jobs.g[0].gave_up;
+    auto job_of = [&](int t) { return kJobs > 1 && t >= first_tiles ? 1 : 0; };
     const uint32_t ring = ptx::smem_addr(smem);
 
     // 384 threads start with 168 registers each (64,512). The sums kept in registers need more than that in the epilogue's eight
@@ -432,7 +442,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
             bool ok = true;
             const uint32_t leader_full = ptx::on_leader(full);
             for (int t = first; t < n_tiles && ok; t += step) {
-                const Tile at = tile_at(g, t);
+                const GemmArgs& g = jobs.g[job_of(t)];
+                const Tile at = tile_at(g, t - job_of(t) * first_tiles);
                 const int row_a = at.m * kTileM + rank * 128, row_b = at.n * kTileN + rank * 128;
                 const int from_a = turned_from(g.a_mn, g.a_sym, at.m, at), from_b = turned_from(g.b_mn, g.b_sym, at.n, at);
                 for (int pass = 0; pass < g.passes && ok; ++pass) {
@@ -444,7 +455,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
                         const CUtensorMap* mb = turn_b && !g.b_mn ? &g.b_mirror[wb] : &g.b[wb];
                         const int end = run_end(kb, from_a, from_b, at.k1);
                         for (; kb < end; ++kb) {
-                            if (!(ok = ptx::bar_wait(empty + 8 * s, parity, g.gave_up))) break;
+                            if (!(ok = ptx::bar_wait(empty + 8 * s, parity, gave_up))) break;
                             const uint32_t sa = ring + s * kStageBytes;
                             if (rank == 0) ptx::bar_expect(full + 8 * s, 2 * kStageBytes);
                             load_operand(ma, turn_a, sa, leader_full + 8 * s, row_a, kb * kBlockK, at.b);
@@ -456,7 +467,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
             }
             // the last products' signals to this CTA: all of them have arrived once the whole ring is free again
             for (int k = 0; k < kStages && ok; ++k) {
-                ok = ptx::bar_wait(empty + 8 * s, parity, g.gave_up);
+                ok = ptx::bar_wait(empty + 8 * s, parity, gave_up);
                 if (++s == kStages) s = 0, parity ^= 1;
             }
             if (!ok) {  // gave up: leave the copies in flight time to land before the CTA goes
@@ -469,13 +480,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
             uint32_t s = 0, parity = 0, buf = 0, acc_parity = 1;
             bool ok = true;
             for (int t = first; t < n_tiles && ok; t += step) {
-                const Tile at = tile_at(g, t);
+                const GemmArgs& g = jobs.g[job_of(t)];
+                const Tile at = tile_at(g, t - job_of(t) * first_tiles);
                 const int from_a = turned_from(g.a_mn, g.a_sym, at.m, at), from_b = turned_from(g.b_mn, g.b_sym, at.n, at);
                 const int blocks = (at.k1 - at.k0) * g.passes;
                 int kb = at.k0;
                 for (int done = 0; done < blocks && ok;) {
                     const int end = stay_end<kPromote>(g, done, blocks);
-                    if (!(ok = ptx::bar_wait(acc_empty + 8 * buf, acc_parity, g.gave_up))) break;
+                    if (!(ok = ptx::bar_wait(acc_empty + 8 * buf, acc_parity, gave_up))) break;
                     ptx::fence_after();
                     const uint32_t d = tmem + buf * kTileN;
                     uint32_t add = 0;
@@ -487,7 +499,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
                         const uint32_t step_a = turn_a ? 2048 >> 4 : 32 >> 4, step_b = turn_b ? 2048 >> 4 : 32 >> 4;  // 16 along K
                         const uint64_t base_a = operand_desc(ring, turn_a), base_b = operand_desc(ring + kOperandBytes, turn_b);
                         for (int k = 0; k < run; ++k) {
-                            if (!(ok = ptx::bar_wait(full + 8 * s, parity, g.gave_up))) break;
+                            if (!(ok = ptx::bar_wait(full + 8 * s, parity, gave_up))) break;
                             ptx::fence_after();
                             const uint64_t da = base_a + s * (kStageBytes >> 4), db = base_b + s * (kStageBytes >> 4);
                             ptx::mma(d, da, db, idesc, add);
@@ -516,8 +528,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
         uint32_t chunk = 0;
         bool ok = true;
         for (int t = first; t < n_tiles && ok; t += step) {
-            const Tile at = tile_at(g, t);
-            Epi epi(args, at, at.m * kTileM + rank * 128 + quad * 32, at.n * kTileN + half * 128, lane, mine);
+            const GemmArgs& g = jobs.g[job_of(t)];
+            const Tile at = tile_at(g, t - job_of(t) * first_tiles);
+            Epi epi(jobs.args[job_of(t)], at, at.m * kTileM + rank * 128 + quad * 32, at.n * kTileN + half * 128, lane, mine);
             uint32_t buf = chunk & 1;
             if constexpr (kPromote) {
                 const int blocks = (at.k1 - at.k0) * g.passes;
@@ -528,7 +541,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 #pragma unroll 1
                     for (int done = 0;;) {
                         buf = chunk & 1;
-                        if (!(ok = ptx::bar_wait(acc_full + 8 * buf, (chunk >> 1) & 1, g.gave_up))) break;
+                        if (!(ok = ptx::bar_wait(acc_full + 8 * buf, (chunk >> 1) & 1, gave_up))) break;
                         ptx::fence_after();
 #pragma unroll
                         for (int c = 0; c < 4; c += 2) {
@@ -551,10 +564,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) ptx::tmem_store_pairs(lanes + buf * kTileN + c * 32, sum + c * 16);
                     ptx::tmem_store_wait();
-                } else if (!(ok = ptx::bar_wait(acc_full + 8 * buf, (chunk >> 1) & 1, g.gave_up))) {
+                } else if (!(ok = ptx::bar_wait(acc_full + 8 * buf, (chunk >> 1) & 1, gave_up))) {
                     break;
                 }
-            } else if (!(ok = ptx::bar_wait(acc_full + 8 * buf, (chunk >> 1) & 1, g.gave_up))) {
+            } else if (!(ok = ptx::bar_wait(acc_full + 8 * buf, (chunk >> 1) & 1, gave_up))) {
                 break;
             }
             ++chunk;
@@ -581,15 +594,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
     if (warp == kEpilogueWarps) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
-template <class Epi, bool kPromote>
-cudaError_t launch_gemm(const GemmArgs& g, const typename Epi::Args& args, cudaStream_t s) {
-    const int64_t tiles = (int64_t)g.batch * g.splits * (g.lower ? (int64_t)g.tiles_m * (g.tiles_m + 1) / 2 : (int64_t)g.tiles_m * g.tiles_n);
+template <class Epi, bool kPromote, int kJobs>
+cudaError_t launch_jobs(const Jobs<Epi, kJobs>& jobs, cudaStream_t s) {
+    int64_t tiles = 0;
+    for (const GemmArgs& g : jobs.g)
+        tiles += (int64_t)g.batch * g.splits * (g.lower ? (int64_t)g.tiles_m * (g.tiles_m + 1) / 2 : (int64_t)g.tiles_m * g.tiles_n);
     if (tiles == 0) return cudaSuccess;
     static std::atomic<uint64_t> allowed;
-    const cudaError_t e = allow_shared_memory(reinterpret_cast<const void*>(k_gemm<Epi, kPromote>), kGemmSmem, allowed);
+    const cudaError_t e = allow_shared_memory(reinterpret_cast<const void*>(k_gemm<Epi, kPromote, kJobs>), kGemmSmem, allowed);
     if (e != cudaSuccess) return e;
     const int64_t clusters = std::min<int64_t>(tiles, gemm_clusters());
-    return launch_chained(k_gemm<Epi, kPromote>, dim3((unsigned)(2 * clusters)), kGemmThreads, kGemmSmem, s, g, args);
+    return launch_chained(k_gemm<Epi, kPromote, kJobs>, dim3((unsigned)(2 * clusters)), kGemmThreads, kGemmSmem, s, jobs);
+}
+template <class Epi, bool kPromote>
+cudaError_t launch_gemm(const GemmArgs& g, const typename Epi::Args& args, cudaStream_t s) {
+    return launch_jobs<Epi, kPromote, 1>(Jobs<Epi, 1>{{g}, {args}}, s);
+}
+// Two independent products of one kind.
+template <class Epi, bool kPromote>
+cudaError_t launch_gemms(const GemmArgs& g, const typename Epi::Args& args, const GemmArgs& h, const typename Epi::Args& more, cudaStream_t s) {
+    return launch_jobs<Epi, kPromote, 2>(Jobs<Epi, 2>{{g, h}, {args, more}}, s);
 }
 #endif
 

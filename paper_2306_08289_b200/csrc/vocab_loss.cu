@@ -2,10 +2,11 @@
 //   z_tv = <h_t, W_v>, lse_t = log sum_v exp z_tv, loss_t = lse_t - z_ty,
 //   P_tv = g_t (exp(z_tv - lse_t) - [v = y_t]), dh = P W, dW = P^T h.
 // Four products of 2 T V H operations (three without the recomputed logits), all on the tensor cores; the logits
-// live in tensor memory only. The first product's epilogue keeps each token's maximum and sum of exponentials of 128 columns;
+// live in tensor memory only (a few of them, 64 MB at most, are kept where that is faster). The first product's epilogue keeps each token's maximum and sum of exponentials of 128 columns;
 // k_finish joins them. The gradient goes through the vocabulary in pieces: logits again, P of the piece into the workspace as
 // the 16-bit operand of the other two products.
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_sm100.cuh"
 #include "vocab_loss.cuh"
@@ -198,10 +199,13 @@ __global__ void __launch_bounds__(256) k_pack(PrepareArgs a) {
 
 // ---- epilogues ----------------------------------------------------------------------------------
 // Statistics of 128 columns of one token, by one thread.
-template <bool kWords>
+template <bool kWords, bool kKeep>
 struct StatisticsEpi {
     struct Args {
-        float2* partial;  // [2 * tile columns][n]: maximum, sum of exp(z - maximum)
+        float2* partial;  // maximum, sum of exp(z - maximum) of each token and part (128 columns)
+        int64_t row_stride, part_stride;
+        float* z;         // [n, z_ld], where the logits are kept
+        int64_t z_ld;
         float* at_target;
         const int32_t* targets;
         const Scan* scan;
@@ -209,12 +213,14 @@ struct StatisticsEpi {
         int64_t n, vocab;
     };
     const Args& a;
-    int64_t row, col0;
+    int64_t row0, row, col0;
     int64_t target;
+    int lane;
+    float* staging;
     float top = -INFINITY, sum = 0.0f;
     PowerOfTwo unscale;
-    __device__ __forceinline__ StatisticsEpi(const Args& args, const Tile& t, int row0, int col, int lane, float*)
-        : a(args), row((int64_t)row0 + lane), col0(col), unscale(kWords && row < args.n ? -(args.exponents[row] + word_exponent(args.scan->head)) : 0) {
+    __device__ __forceinline__ StatisticsEpi(const Args& args, const Tile& t, int row_, int col, int lane_, float* staging_)
+        : a(args), row0(row_), row((int64_t)row_ + lane_), col0(col), lane(lane_), staging(staging_), unscale(kWords && row < args.n ? -(args.exponents[row] + word_exponent(args.scan->head)) : 0) {
         target = row < a.n ? a.targets[row] : -1;
     }
     __device__ __forceinline__ void chunk(int c, float (&v)[32]) {
@@ -242,9 +248,17 @@ struct StatisticsEpi {
         for (int k = 0; k < 32; ++k) part[k % 4] += exp2_fast((v[k] - base) * kLog2E);
         sum = sum * exp2_fast((top - base) * kLog2E) + ((part[0] + part[1]) + (part[2] + part[3]));
         top = next;
+        if (kKeep && row0 < a.n && col < a.vocab) {
+            turn_columns(staging, v, lane);
+            float* to = a.z + row0 * a.z_ld + col + lane;
+            if (col + lane < a.vocab)
+#pragma unroll
+                for (int r = 0; r < 32; ++r)
+                    if (row0 + r < a.n) to[r * a.z_ld] = v[r];
+        }
     }
     __device__ __forceinline__ void finish() {
-        if (row < a.n) a.partial[(col0 / 128) * a.n + row] = make_float2(top, sum);
+        if (row < a.n) a.partial[col0 / 128 * a.part_stride + row * a.row_stride] = make_float2(top, sum);
     }
 };
 
@@ -337,6 +351,35 @@ struct GradientFactor {
     __device__ __forceinline__ T operator()(float v) const { return narrow<T>((sizeof(T) == 4 ? unscale(v) : v) * last); }
 };
 
+// P from kept logits.
+template <bool kWords>
+struct WordSink {
+    void *p0, *p1;
+    int64_t ld;
+    const float* rate;
+    struct Row {
+        void *p0, *p1;
+        float rate;
+        __device__ __forceinline__ void operator()(int64_t c, float p, float q) const {
+            if constexpr (kWords) {
+                Pack<__half, 2> h, l;
+                split_pair(rate * p * (float)(1 << kPScale), rate * q * (float)(1 << kPScale), h.v[0], h.v[1], l.v[0], l.v[1]);
+                *reinterpret_cast<Pack<__half, 2>*>(static_cast<__half*>(p0) + c) = h;
+                *reinterpret_cast<Pack<__half, 2>*>(static_cast<__half*>(p1) + c) = l;
+            } else {
+                *reinterpret_cast<Pack<__nv_bfloat16, 2>*>(static_cast<__nv_bfloat16*>(p0) + c) = {narrow<__nv_bfloat16>(rate * p), narrow<__nv_bfloat16>(rate * q)};
+            }
+        }
+        __device__ __forceinline__ void none(int64_t c) const {
+            *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p0) + c) = 0;
+            if (kWords) *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p1) + c) = 0;
+        }
+    };
+    __device__ __forceinline__ Row row(int64_t t) const {
+        return {static_cast<uint16_t*>(p0) + t * ld, kWords ? static_cast<uint16_t*>(p1) + t * ld : nullptr, rate[t]};
+    }
+};
+
 // A gradient's tile: out = factor * (sums of the earlier pieces + this one), or those sums kept for later.
 template <class T>
 struct GradientEpi {
@@ -403,16 +446,24 @@ struct Layout {
     Scan *scan, *scan_parts;
     void *h0, *h1, *w0, *w1, *p0, *p1;
     float2* partial;
-    float *at_target, *rate, *kept, *head_kept;
+    float *at_target, *rate, *kept, *head_kept, *z;
     int32_t *exponents, *poisoned;
-    int64_t ld, p_ld, kept_ld, piece;
+    int64_t ld, p_ld, kept_ld, piece, z_ld;
+    bool keep;  // the logits, from the statistics to P
     int hidden_parts, head_parts;  // of K, in the gradients' products
+    bool together;                 // both in one launch
 };
 
 // Vocabulary rows of a piece: as many as keep P within kPieceBytes, fewer where that fills the pairs of CTAs better.
 // Cost in units of (tile of 256 x 256) x (K of 256) a pair.
 constexpr int64_t kPieceBytes = 160ll << 20;
 constexpr int64_t kPairs = 74;
+// Few logits (64 MB as floats, half of that with bf16 rows, whose products cost a third) are kept: P then costs a pass over them and not
+// another product. Loss and gradients, us, kept / made again: fp32 rows, tokens x vocabulary x width: 333 x 5,003 x 201 71 / 97; 2,000 x 4,000 x
+// 512 139 / 179; 1,000 x 16,000 x 1,024 375 / 426; 200 x 60,000 x 80 199 / 192. bf16: 333 x 5,003 x 201 47 / 58; 2,000 x 4,000 x 512 78 / 92;
+// 128 x 50,000 x 512 149 / 143; 1,024 x 10,000 x 768 120 / 116; 200 x 60,000 x 80 127 / 102. (Part of the gain is the gradients' common launch.)
+// A vocabulary of a few tiles would leave the pass mostly launch.
+constexpr int64_t kKeepLogits = int64_t(1) << 24, kKeepVocab = 512;
 constexpr int64_t kLeastBlocks = 8;  // of K in a part: less would leave its tile mostly epilogue
 int64_t piece_rows(int64_t n, int64_t width, int64_t vocab, int64_t words) {
     const int64_t tm = std::max<int64_t>(1, ceil_div(n, kTileM)), tw = ceil_div(width, kTileN), tv = ceil_div(vocab, kTileN);
@@ -441,6 +492,9 @@ int64_t layout(int64_t n, int64_t width, int64_t vocab, bool with_grad, int32_t 
     }
     l.partial = w.take<float2>(2 * ceil_div(vocab, kTileN) * n);
     l.at_target = w.take<float>(n);
+    l.keep = n * vocab <= kKeepLogits / (words == 2 ? 1 : 2) && vocab >= kKeepVocab;
+    l.z_ld = round_up(vocab, 32);
+    if (l.keep && with_grad) l.z = w.take<float>(n * l.z_ld);
     l.exponents = w.take<int32_t>(n);
     l.poisoned = w.take<int32_t>(n);
     if (with_grad) {
@@ -451,10 +505,19 @@ int64_t layout(int64_t n, int64_t width, int64_t vocab, bool with_grad, int32_t 
         if (words == 2) l.p1 = w.take<uint16_t>(n * l.p_ld);
         l.kept_ld = round_up(width, kTileN);
         const int64_t rows = std::min(l.piece, vocab), across = ceil_div(width, kTileN);
-        l.hidden_parts = split_parts(ceil_div(n, kTileM) * across, ceil_div(rows, kBlockK), kPairs, kLeastBlocks);
-        l.head_parts = split_parts(ceil_div(rows, kTileM) * across, ceil_div(n, kBlockK), kPairs, kLeastBlocks);
-        const int64_t keep = l.piece < vocab || l.hidden_parts > 1 ? n * l.hidden_parts : 0;
-        l.kept = w.take<float>(keep * l.kept_ld);
+        const int64_t hidden_tiles = ceil_div(n, kTileM) * across, hidden_blocks = ceil_div(rows, kBlockK);
+        const int64_t head_tiles = ceil_div(rows, kTileM) * across, head_blocks = ceil_div(n, kBlockK);
+        l.together = l.piece >= vocab && hidden_tiles + head_tiles <= kPairs;
+        if (l.together) {  // one launch: a part's share of the blocks of K is what a pair of CTAs gets of all of them
+            const int64_t target = std::max(kLeastBlocks, ceil_div(hidden_tiles * hidden_blocks + head_tiles * head_blocks, kPairs));
+            l.hidden_parts = (int)std::max<int64_t>(1, hidden_blocks / target);
+            l.head_parts = (int)std::max<int64_t>(1, head_blocks / target);
+        } else {
+            l.hidden_parts = split_parts(hidden_tiles, hidden_blocks, kPairs, kLeastBlocks);
+            l.head_parts = split_parts(head_tiles, head_blocks, kPairs, kLeastBlocks);
+        }
+        const int64_t kept_rows = l.piece < vocab || l.hidden_parts > 1 ? n * l.hidden_parts : 0;
+        l.kept = w.take<float>(kept_rows * l.kept_ld);
         l.head_kept = w.take<float>(l.head_parts > 1 ? rows * l.head_parts * l.kept_ld : 0);
     }
     if (out) *out = l;
@@ -504,12 +567,22 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
     // the loss is fp32 with either storage type, so its sums are promoted with both
     e = make_gemm(hidden(false), head(0, a.vocab, false), 1, !kWords, false, kWords ? kFlush : kFlushLoss, 1, &g);
     if (e != cudaSuccess) return e;
-    const typename StatisticsEpi<kWords>::Args stats{l.partial, l.at_target, a.targets, l.scan, l.exponents, n, a.vocab};
-    e = launch_gemm<StatisticsEpi<kWords>, true>(g, stats, s);
+    const int parts = (int)(2 * ceil_div(a.vocab, kTileN));
+    auto statistics = [&](auto keep) {
+        using Epi = StatisticsEpi<kWords, decltype(keep)::value>;
+        return launch_gemm<Epi, true>(
+            g, typename Epi::Args{l.partial, l.keep ? parts : 1, l.keep ? 1 : n, l.z, l.z_ld, l.at_target, a.targets, l.scan, l.exponents, n, a.vocab}, s);
+    };
+    e = l.z ? statistics(std::true_type{}) : statistics(std::false_type{});
     if (e != cudaSuccess) return e;
-    launch_chained(k_finish, dim3((unsigned)ceil_div(n, 32)), kFinishWarps * 32, 0, s, l.partial, (int)(2 * ceil_div(a.vocab, kTileN)), l.at_target, a.targets,
-                                                      hidden_in_place ? nullptr : l.poisoned, n, a.vocab, a.loss, a.lse);
-    if (!with_grad) return cudaGetLastError();
+    const int32_t* poisoned = hidden_in_place ? nullptr : l.poisoned;
+    if (l.keep) {
+        e = launch_rows(a, l.partial, parts, l.at_target, poisoned, l.z, l.z_ld, with_grad, WordSink<kWords>{l.p0, l.p1, l.p_ld, l.rate}, s);
+    } else {
+        e = launch_chained(k_finish, dim3((unsigned)ceil_div(n, 32)), kFinishWarps * 32, 0, s, l.partial, parts, l.at_target, a.targets, poisoned, n, a.vocab,
+                           a.loss, a.lse);
+    }
+    if (e != cudaSuccess || !with_grad) return e;
 
     auto join = [&](const float* kept, int parts, int64_t rows, T* out, int64_t pitch, const GradientScale& scale) {
         for (int64_t r = 0; r < rows; r += 65535) {  // the grid's second dimension ends there
@@ -521,37 +594,39 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
     for (int64_t v0 = 0; v0 < a.vocab; v0 += l.piece) {
         const int64_t rows = std::min(l.piece, a.vocab - v0);
         const bool first = v0 == 0, final = v0 + rows == a.vocab;
-        e = make_gemm(hidden(false), head(v0, rows, false), 1, !kWords, false, flush, 1, &g);
-        if (e != cudaSuccess) return e;
-        const typename ProbabilityEpi<kWords>::Args prob{l.p0, l.p1, l.p_ld, a.targets, a.lse, l.rate, l.scan, l.exponents, n, a.vocab, v0};
-        e = launch_gemm<ProbabilityEpi<kWords>, kWords>(g, prob, s);
-        if (e != cudaSuccess) return e;
-        if (a.grad_head) {
-            const Operand p{l.p0, l.p1, rows, n, l.p_ld, 0, true};
-            const GradientScale scale{l.scan, false, weighted, a.scale};
-            T* out = static_cast<T*>(a.grad_head) + v0 * a.grad_head_pitch;
-            const bool parts = l.head_parts > 1;
-            e = make_gemm(p, hidden(true), 1, !kWords, false, flush, l.head_parts, &g);
+        if (!l.keep) {
+            e = make_gemm(hidden(false), head(v0, rows, false), 1, !kWords, false, flush, 1, &g);
             if (e != cudaSuccess) return e;
-            e = launch_gemm<GradientEpi<T>, kWords>(
-                g, {parts ? nullptr : out, a.grad_head_pitch, rows, a.width, l.head_kept, l.kept_ld, false, scale}, s);
+            const typename ProbabilityEpi<kWords>::Args prob{l.p0, l.p1, l.p_ld, a.targets, a.lse, l.rate, l.scan, l.exponents, n, a.vocab, v0};
+            e = launch_gemm<ProbabilityEpi<kWords>, kWords>(g, prob, s);
             if (e != cudaSuccess) return e;
-            if (parts) join(l.head_kept, l.head_parts, rows, out, a.grad_head_pitch, scale);
         }
-        if (a.grad_hidden) {
-            const Operand p{l.p0, l.p1, n, rows, l.p_ld, 0, false};
-            const GradientScale scale{l.scan, true, weighted, a.scale};
-            T* out = static_cast<T*>(a.grad_hidden);
-            const bool parts = l.hidden_parts > 1;
+        using Grad = GradientEpi<T>;
+        GemmArgs of_head, of_hidden;
+        const GradientScale head_scale{l.scan, false, weighted, a.scale}, hidden_scale{l.scan, true, weighted, a.scale};
+        T* head_out = a.grad_head ? static_cast<T*>(a.grad_head) + v0 * a.grad_head_pitch : nullptr;
+        T* hidden_out = static_cast<T*>(a.grad_hidden);
+        const bool head_parts = l.head_parts > 1, hidden_parts = l.hidden_parts > 1;
+        const typename Grad::Args head_args{head_parts ? nullptr : head_out, a.grad_head_pitch, rows, a.width, l.head_kept, l.kept_ld, false, head_scale};
+        const typename Grad::Args hidden_args{final && !hidden_parts ? hidden_out : nullptr, a.grad_hidden_pitch, n, a.width, l.kept, l.kept_ld, !first,
+                                              hidden_scale};
+        if (a.grad_head) e = make_gemm(Operand{l.p0, l.p1, rows, n, l.p_ld, 0, true}, hidden(true), 1, !kWords, false, flush, l.head_parts, &of_head);
+        if (a.grad_hidden && e == cudaSuccess) {
             // part p of every piece adds to the sums of part p; a short last piece may have fewer parts, but none without a block
             const int here = (int)std::min<int64_t>(l.hidden_parts, ceil_div(rows, kBlockK));
-            e = make_gemm(p, head(v0, rows, true), 1, !kWords, false, flush, here, &g);
-            if (e != cudaSuccess) return e;
-            e = launch_gemm<GradientEpi<T>, kWords>(
-                g, {final && !parts ? out : nullptr, a.grad_hidden_pitch, n, a.width, l.kept, l.kept_ld, !first, scale}, s);
-            if (e != cudaSuccess) return e;
-            if (final && parts) join(l.kept, l.hidden_parts, n, out, a.grad_hidden_pitch, scale);
+            e = make_gemm(Operand{l.p0, l.p1, n, rows, l.p_ld, 0, false}, head(v0, rows, true), 1, !kWords, false, flush, here, &of_hidden);
         }
+        if (e != cudaSuccess) return e;
+        if (l.together && a.grad_head && a.grad_hidden) {  // the longer sums first
+            e = rows >= n ? launch_gemms<Grad, kWords>(of_hidden, hidden_args, of_head, head_args, s)
+                          : launch_gemms<Grad, kWords>(of_head, head_args, of_hidden, hidden_args, s);
+        } else {
+            if (a.grad_head) e = launch_gemm<Grad, kWords>(of_head, head_args, s);
+            if (a.grad_hidden && e == cudaSuccess) e = launch_gemm<Grad, kWords>(of_hidden, hidden_args, s);
+        }
+        if (e != cudaSuccess) return e;
+        if (a.grad_head && head_parts) join(l.head_kept, l.head_parts, rows, head_out, a.grad_head_pitch, head_scale);
+        if (a.grad_hidden && hidden_parts && final) join(l.kept, l.hidden_parts, n, hidden_out, a.grad_hidden_pitch, hidden_scale);
     }
     return cudaGetLastError();
 }

@@ -105,50 +105,20 @@ __global__ void __launch_bounds__(kFewThreads) k_few_logits(const VocabLossArgs 
     }
 }
 
-// Joins a token's statistics into its loss; with gradients also turns its logits into P. A CTA a token and kRowColumns columns.
-constexpr int kRowColumns = 2048;
-
-__device__ __forceinline__ float block_reduce(float v, bool sum, float* shared) {
-    for (int o = 16; o; o /= 2) {
-        const float w = __shfl_xor_sync(0xffffffffu, v, o);
-        v = sum ? v + w : fmaxf(v, w);
-    }
-    __syncthreads();
-    if (threadIdx.x % 32 == 0) shared[threadIdx.x / 32] = v;
-    __syncthreads();
-    v = shared[0];
-    for (int w = 1; w < kFewThreads / 32; ++w) v = sum ? v + shared[w] : fmaxf(v, shared[w]);
-    return v;
-}
-
-__global__ void __launch_bounds__(kFewThreads) k_few_rows(const VocabLossArgs a, const float2* __restrict__ partial, int parts,
-                                                          const float* __restrict__ at_target, bool probabilities, float* __restrict__ z, int64_t z_ld) {
-    ptx::chained();
-    __shared__ float shared[kFewThreads / 32];
-    const int64_t t = blockIdx.x;
-    const float2* mine = partial + t * parts;
-    float top = -INFINITY, sum = 0.0f;
-    for (int p = threadIdx.x; p < parts; p += kFewThreads) top = fmaxf(top, mine[p].x);
-    top = block_reduce(top, false, shared);
-    const float base = top == -INFINITY ? 0.0f : top;
-    for (int p = threadIdx.x; p < parts; p += kFewThreads) sum += mine[p].y * exp2_fast((mine[p].x - base) * kLog2E);
-    sum = block_reduce(sum, true, shared);
-    const float lse = top + logf(sum);
-    const int64_t y = a.targets[t];
-    const bool live = is_token((int32_t)y, a.vocab);
-    if (threadIdx.x == 0 && blockIdx.y == 0) {
-        a.lse[t] = lse;
-        a.loss[t] = live ? lse - at_target[t] : 0.0f;
-    }
-    if (!probabilities) return;
-    const float g = live ? a.scale * (a.weights ? a.weights[t] : 1.0f) : 0.0f;
-    const int64_t c0 = (int64_t)blockIdx.y * kRowColumns;
-#pragma unroll 4
-    for (int64_t c = c0 + threadIdx.x; c < min(c0 + kRowColumns, a.vocab); c += kFewThreads) {
-        const float p = exp2_fast((z[t * z_ld + c] - lse) * kLog2E);
-        z[t * z_ld + c] = live ? g * (c == y ? p - 1.0f : p) : 0.0f;
-    }
-}
+// P in place of the logits, with the gradients' factor in it.
+struct FewSink {
+    float* z;
+    int64_t z_ld;
+    float scale;
+    const float* weights;
+    struct Row {
+        float* z;
+        float g;
+        __device__ __forceinline__ void operator()(int64_t c, float p, float q) const { *reinterpret_cast<float2*>(z + c) = make_float2(g * p, g * q); }
+        __device__ __forceinline__ void none(int64_t c) const { *reinterpret_cast<float2*>(z + c) = make_float2(0.0f, 0.0f); }
+    };
+    __device__ __forceinline__ Row row(int64_t t) const { return {z + t * z_ld, scale * (weights ? weights[t] : 1.0f)}; }
+};
 
 // Both gradients: CTAs 0 .. head_ctas - 1 make tiles of grad_head (32 vocabulary rows x 64 columns over a part of the tokens), the others
 // tiles of grad_hidden (32 tokens x 64 columns over a part of the vocabulary).
@@ -255,9 +225,8 @@ cudaError_t typed(const VocabLossArgs& a, const Layout& l, cudaStream_t s) {
     const int64_t n = a.n_tokens, parts = ceil_div(a.vocab, kN);
     const bool with_grad = a.grad_hidden || a.grad_head;
     launch_chained(k_few_logits<T>, dim3((unsigned)(parts * ceil_div(n, kM))), kFewThreads, 0, s, a, l.z, l.z_ld, l.partial, l.at_target);
-    launch_chained(k_few_rows, dim3((unsigned)n, with_grad ? (unsigned)ceil_div(a.vocab, kRowColumns) : 1u), kFewThreads, 0, s, a, l.partial, (int)parts,
-                   l.at_target, with_grad, l.z, l.z_ld);
-    if (!with_grad) return cudaGetLastError();
+    const cudaError_t e = launch_rows(a, l.partial, (int)parts, l.at_target, nullptr, l.z, l.z_ld, with_grad, FewSink{l.z, l.z_ld, a.scale, a.weights}, s);
+    if (e != cudaSuccess || !with_grad) return e;
     FewGradArgs g{a, l.z, l.z_ld, ceil_div(a.width, kN), l.head, l.hidden};
     if (!a.grad_head) g.head.parts = 0;
     if (!a.grad_hidden) g.hidden.parts = 0;
