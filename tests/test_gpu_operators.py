@@ -83,7 +83,7 @@ def grad_reference(dy, ids, vocab, scale):
 @pytest.mark.parametrize("n,vocab,width,kind", [
     (0, 7, 16, "uniform"), (1, 1, 1, "uniform"), (1, 700, 64, "uniform"), (31, 3, 40, "uniform"), (500, 1, 33, "uniform"),
     (511, 600, 136, "one"), (4096, 513, 64, "skewed"), (4097, 511, 24, "skewed"), (6000, 262145, 8, "skewed"), (9000, 40, 260, "one"),
-    (20000, 9000, 72, "skewed"), (20000, 5, 17, "uniform"), (300, 300, 2056, "skewed"), (64, 90, 16, "none"), (8192, 3000, 24, "skewed"), (8000, 70000, 40, "uniform"), (70000, 20000, 20, "skewed")])
+    (20000, 9000, 72, "skewed"), (20000, 5, 17, "uniform"), (300, 300, 2056, "skewed"), (64, 90, 16, "none"), (8192, 3000, 24, "skewed"), (8000, 70000, 40, "uniform"), (70000, 20000, 20, "skewed"), (4096, 17000, 40, "skewed"), (2000, 257, 136, "skewed")])
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_embed_grad(storage, n, vocab, width, kind, accumulate):
     g, dt = gen(n + vocab), DT[storage]
