@@ -498,7 +498,8 @@ int64_t layout(int64_t n, int64_t width, int64_t vocab, bool with_grad, int32_t 
     l.exponents = w.take<int32_t>(n);
     l.poisoned = w.take<int32_t>(n);
     if (with_grad) {
-        l.piece = piece_rows(n, width, vocab, words);
+        // kept logits become P in one launch, so then a piece is the whole vocabulary: at most as many elements as logits
+        l.piece = l.keep ? round_up(vocab, kTileN) : piece_rows(n, width, vocab, words);
         l.p_ld = l.piece;
         l.rate = w.take<float>(n);
         l.p0 = w.take<uint16_t>(n * l.p_ld);

@@ -206,6 +206,14 @@ def test_vocab_loss_and_gradients(storage, n, width, vocab, weighted):
     assert none is None and torch.equal(only_w, gw)
 
 
+@pytest.mark.parametrize("weighted", [False, True])
+@pytest.mark.parametrize("storage,n,width,vocab", [("f32", 100, 16, 163841), ("f32", 64, 72, 200064), ("bf16", 25, 264, 327681),
+                                                   ("bf16", 16, 64, 400003), ("bf16", 1, 300, 262144)])
+def test_few_tokens_of_a_large_vocabulary(storage, n, width, vocab, weighted):
+    """Kept logits whose P is longer than a piece of large problems would be."""
+    test_vocab_loss_and_gradients(storage, n, width, vocab, weighted)
+
+
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
 def test_vocab_loss_edges(storage):
     g, dt = gen(1), DT[storage]

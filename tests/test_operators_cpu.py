@@ -49,6 +49,23 @@ def test_workspace_sizes():
     assert B.lib().a2cid2_embed_grad_workspace(8, 8, 8, None) == B.A2_EINVAL
 
 
+@pytest.mark.parametrize("storage,words,most", [(B.A2_F32, 2, 1 << 24), (B.A2_BF16, 1, 1 << 23)])
+def test_workspace_holds_the_whole_of_kept_logits_and_P(storage, words, most):
+    """Few logits are kept and turned into P at once, so the gradients' part of the workspace holds every column of both, for any vocabulary."""
+    seen = 0
+    for n in (1, 2, 3, 8, 16, 25, 64, 102, 255, 256, 257, 700, 4000, 16384):
+        for vocab in (512, 5003, 65537, 163840, 163841, 200064, 262144, 327680, 327681, 400000, 1 << 20, 1 << 22, (1 << 23) - 1, 1 << 23, 1 << 24):
+            if n * vocab > most:
+                continue
+            for width in ((1 << 27) // (n * vocab) + 1, 257, 768):
+                if storage == B.A2_F32 and n * vocab * width <= 1 << 27 or storage == B.A2_BF16 and width <= 256:
+                    continue  # the form without tensor cores
+                forward, grad = (size("a2cid2_vocab_loss_workspace", n, width, vocab, g, storage)[1] for g in (0, 1))
+                assert grad - forward >= n * vocab * (4 + 2 * words), (n, width, vocab)
+                seen += 1
+    assert seen > 60
+
+
 EMBED = dict(table=P, vocab=10, width=8, pitch=8, ids=P, n=4, scale=1.0, out=P, out_pitch=8, dtype=B.A2_F32, stream=None)
 
 
