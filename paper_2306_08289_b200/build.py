@@ -41,6 +41,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
            "-Xcompiler", "-fPIC,-O2,-Wall", "-shared", "-cudart", "static",
+           "--diag-error", "2809",  # a launch whose status is dropped ([[nodiscard]])
            "-I", INCLUDE, "-I", CSRC, "-o", tmp]
     cmd += os.environ.get("A2CID2_NVCC_FLAGS", "").split()  # extra flags for experiments, e.g. -DA2_EVENT_THREADS=512
     if verbose:

@@ -64,13 +64,8 @@ cudaError_t embed_typed(const EmbedArgs& a, cudaStream_t s) {
     const int64_t grid = ceil_div(a.n_ids, (int64_t)(kThreads / group) * kRows);
     auto* table = static_cast<const T*>(a.table);
     auto* out = static_cast<T*>(a.out);
-    if (wide)
-        launch_chained(k_embed<T, kVec>, dim3((unsigned)grid), kThreads, 0, s, table, a.vocab, a.width, a.table_pitch, a.ids, a.n_ids, a.scale, out,
-                                                             a.out_pitch, group);
-    else
-        launch_chained(k_embed<T, 1>, dim3((unsigned)grid), kThreads, 0, s, table, a.vocab, a.width, a.table_pitch, a.ids, a.n_ids, a.scale, out,
-                                                          a.out_pitch, group);
-    return cudaGetLastError();
+    return launch_chained(wide ? k_embed<T, kVec> : k_embed<T, 1>, dim3((unsigned)grid), kThreads, 0, s, table, a.vocab, a.width, a.table_pitch, a.ids,
+                          a.n_ids, a.scale, out, a.out_pitch, group);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -508,12 +503,10 @@ cudaError_t segments_typed(const EmbedGradArgs& a, const GradPlan& p, int64_t ze
     auto* table = static_cast<T*>(a.grad_table);
     const int64_t sum_ctas = ceil_div(blocks, per_cta);
     const int64_t zero_ctas = a.accumulate ? 0 : ceil_div(a.vocab - zero_first, kZeroRows);
-    launch_chained(k_segments<T, VEC>, dim3((unsigned)(sum_ctas + zero_ctas), (unsigned)col_ctas), kThreads, 0, s, g, a.grad_out_pitch, p.sorted, a.n_ids,
-                   a.vocab, a.width, a.scale, a.accumulate, table, a.grad_table_pitch, p.partial, span, group, sum_ctas, zero_first);
-    launch_chained(k_join<T, VEC>, dim3((unsigned)sum_ctas, (unsigned)col_ctas), kThreads, 0, s, p.sorted, a.n_ids, a.vocab, a.width, a.scale,
-                                                                                         a.accumulate, table, a.grad_table_pitch, p.partial,
-                                                                                         span, group);
-    return cudaGetLastError();
+    A2_CUDA_TRY(launch_chained(k_segments<T, VEC>, dim3((unsigned)(sum_ctas + zero_ctas), (unsigned)col_ctas), kThreads, 0, s, g, a.grad_out_pitch, p.sorted,
+                           a.n_ids, a.vocab, a.width, a.scale, a.accumulate, table, a.grad_table_pitch, p.partial, span, group, sum_ctas, zero_first));
+    return launch_chained(k_join<T, VEC>, dim3((unsigned)sum_ctas, (unsigned)col_ctas), kThreads, 0, s, p.sorted, a.n_ids, a.vocab, a.width, a.scale,
+                          a.accumulate, table, a.grad_table_pitch, p.partial, span, group);
 }
 
 template <class T, int VEC>
@@ -535,16 +528,16 @@ cudaError_t sorted_typed(const EmbedGradArgs& a, const GradPlan& p, cudaStream_t
         return ZeroFill{static_cast<char*>(a.grad_table), cleared * k / launches, cleared * (k + 1) / launches, a.width * (int64_t)sizeof(T),
                         a.grad_table_pitch * (int64_t)sizeof(T), VEC * sizeof(T) == 16};
     };
-    launch_chained(k_sort_count, dim3((unsigned)p.n_tiles + zero_ctas), kSortThreads, 0, s, a.ids, a.n_ids, a.vocab, p.passes, (int)p.n_tiles, p.counts,
-                   share(0));
+    A2_CUDA_TRY(launch_chained(k_sort_count, dim3((unsigned)p.n_tiles + zero_ctas), kSortThreads, 0, s, a.ids, a.n_ids, a.vocab, p.passes, (int)p.n_tiles,
+                           p.counts, share(0)));
     // the passes go back and forth between the two buffers and end in p.sorted
     const Pair* from = nullptr;
     for (int pass = 0; pass < p.passes; ++pass) {
         Pair* to = (p.passes - pass) % 2 == 1 ? p.sorted : p.other;
         const int* counts = p.counts + (int64_t)pass * p.n_tiles * kDigits;
         const bool last = pass + 1 == p.passes;
-        launch_chained(k_sort_pass, dim3((unsigned)p.n_tiles + zero_ctas), kSortThreads, 0, s, a.ids, from, a.n_ids, a.vocab, pass, last, counts,
-                       (int)p.n_tiles, to, last ? nullptr : p.counts + (int64_t)(pass + 1) * p.n_tiles * kDigits, share(pass + 1));
+        A2_CUDA_TRY(launch_chained(k_sort_pass, dim3((unsigned)p.n_tiles + zero_ctas), kSortThreads, 0, s, a.ids, from, a.n_ids, a.vocab, pass, last, counts,
+                               (int)p.n_tiles, to, last ? nullptr : p.counts + (int64_t)(pass + 1) * p.n_tiles * kDigits, share(pass + 1)));
         from = to;
     }
     return segments_typed<T, VEC>(a, p, cleared, s);

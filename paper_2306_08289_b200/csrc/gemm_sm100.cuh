@@ -75,11 +75,11 @@ struct Operand {  // a 16-bit matrix, K-major [rows, k] or MN-major [k, rows], `
     bool mn;
     bool symmetric = false;  // rows == k, K-major
 };
-cudaError_t make_gemm(const Operand& a, const Operand& b, int64_t mats, bool bf16, bool lower, int flush, int splits, GemmArgs* out);
-cudaError_t gave_up_flag(int** out);  // where kernels note a wait that ran out, on the current device
+[[nodiscard]] cudaError_t make_gemm(const Operand& a, const Operand& b, int64_t mats, bool bf16, bool lower, int flush, int splits, GemmArgs* out);
+[[nodiscard]] cudaError_t gave_up_flag(int** out);  // where kernels note a wait that ran out, on the current device
 // Lets a kernel use `bytes` of dynamic shared memory on the current device; `done` remembers the devices it was asked on.
-cudaError_t allow_large_clusters(const void* kernel, std::atomic<uint64_t>& done);  // more than 8 CTAs
-cudaError_t allow_shared_memory(const void* kernel, int bytes, std::atomic<uint64_t>& done);
+[[nodiscard]] cudaError_t allow_large_clusters(const void* kernel, std::atomic<uint64_t>& done);  // more than 8 CTAs
+[[nodiscard]] cudaError_t allow_shared_memory(const void* kernel, int bytes, std::atomic<uint64_t>& done);
 int gemm_clusters();  // CTA pairs that run at once on the current device
 
 #ifdef __CUDACC__
@@ -599,7 +599,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
 }
 
 template <class Epi, bool kPromote, int kJobs>
-cudaError_t launch_jobs(const Jobs<Epi, kJobs>& jobs, cudaStream_t s) {
+[[nodiscard]] cudaError_t launch_jobs(const Jobs<Epi, kJobs>& jobs, cudaStream_t s) {
     int64_t tiles = 0;
     for (const GemmArgs& g : jobs.g)
         tiles += (int64_t)g.batch * g.splits * (g.lower ? (int64_t)g.tiles_m * (g.tiles_m + 1) / 2 : (int64_t)g.tiles_m * g.tiles_n);
@@ -611,12 +611,12 @@ cudaError_t launch_jobs(const Jobs<Epi, kJobs>& jobs, cudaStream_t s) {
     return launch_chained(k_gemm<Epi, kPromote, kJobs>, dim3((unsigned)(2 * clusters)), kGemmThreads, kGemmSmem, s, jobs);
 }
 template <class Epi, bool kPromote>
-cudaError_t launch_gemm(const GemmArgs& g, const typename Epi::Args& args, cudaStream_t s) {
+[[nodiscard]] cudaError_t launch_gemm(const GemmArgs& g, const typename Epi::Args& args, cudaStream_t s) {
     return launch_jobs<Epi, kPromote, 1>(Jobs<Epi, 1>{{g}, {args}}, s);
 }
 // Two independent products of one kind.
 template <class Epi, bool kPromote>
-cudaError_t launch_gemms(const GemmArgs& g, const typename Epi::Args& args, const GemmArgs& h, const typename Epi::Args& more, cudaStream_t s) {
+[[nodiscard]] cudaError_t launch_gemms(const GemmArgs& g, const typename Epi::Args& args, const GemmArgs& h, const typename Epi::Args& more, cudaStream_t s) {
     return launch_jobs<Epi, kPromote, 2>(Jobs<Epi, 2>{{g, h}, {args, more}}, s);
 }
 #endif

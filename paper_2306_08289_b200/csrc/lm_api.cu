@@ -23,7 +23,9 @@ int fail(int code, const char* format, ...) {
 }
 
 int status(cudaError_t e, const char* what) {
-    return e == cudaSuccess ? A2_OK : fail(A2_ECUDA, "%s: %s (%s)", what, cudaGetErrorName(e), cudaGetErrorString(e));
+    if (e == cudaSuccess) return A2_OK;
+    (void)cudaGetLastError();  // reported here, and not once more by whoever asks next
+    return fail(A2_ECUDA, "%s: %s (%s)", what, cudaGetErrorName(e), cudaGetErrorString(e));
 }
 
 constexpr int64_t kMaxRows = int64_t(1) << 30;        // ids, tokens, vocabulary rows

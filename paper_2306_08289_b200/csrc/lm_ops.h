@@ -91,6 +91,13 @@ bool orthogonalize_range(double a, double b, double c, int steps);
 int64_t orthogonalize_workspace(int64_t n_mats, int64_t rows, int64_t cols, int32_t dtype);
 cudaError_t run_orthogonalize(const OrthogonalizeArgs& a, void* workspace, cudaStream_t s);
 
+// Ends a function at the first launch that fails: what would follow reads what that launch was to write.
+#define A2_CUDA_TRY(call)                            \
+    do {                                             \
+        const cudaError_t e__ = (call);              \
+        if (e__ != cudaSuccess) return e__;          \
+    } while (0)
+
 cudaError_t products_gave_up(cudaStream_t s, bool* out);  // waits for the stream; whether a product ever gave up on this device
 
 #ifdef __CUDACC__
@@ -106,7 +113,7 @@ __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return
 // Starts a kernel that may begin before its predecessor in the stream has ended; the kernel itself calls wait_previous() before it
 // touches memory.
 template <class... P, class... A>
-cudaError_t launch_clusters(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, unsigned cluster, cudaStream_t s, A&&... args) {
+[[nodiscard]] cudaError_t launch_clusters(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, unsigned cluster, cudaStream_t s, A&&... args) {
     cudaLaunchConfig_t config{};
     config.gridDim = grid;
     config.blockDim = dim3(threads);
@@ -123,7 +130,7 @@ cudaError_t launch_clusters(void (*kernel)(P...), dim3 grid, unsigned threads, s
     return cudaLaunchKernelEx(&config, kernel, static_cast<P>(args)...);
 }
 template <class... P, class... A>
-cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, A&&... args) {
+[[nodiscard]] cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, A&&... args) {
     return launch_clusters(kernel, grid, threads, smem, 1, s, std::forward<A>(args)...);
 }
 

@@ -343,48 +343,41 @@ cudaError_t typed(const OrthogonalizeArgs& a, Layout l, cudaStream_t s) {
     const dim3 grid((unsigned)l.parts, (unsigned)a.n_mats);
     constexpr int kVec = 16 / sizeof(T);
     const bool aligned = reinterpret_cast<uintptr_t>(a.in) % 16 == 0 && a.in_pitch % kVec == 0 && (a.n_mats == 1 || a.in_stride % kVec == 0);
-    auto first = [&](auto norm, auto words) {
-        launch_chained(norm, grid, kNormThreads, 0, s, static_cast<const T*>(a.in), a.in_stride, a.in_pitch, a.rows, a.cols, l.partial);
-        launch_chained(words, grid, kNormThreads, 0, s, static_cast<const T*>(a.in), a.in_stride, a.in_pitch, a.rows, a.cols, l.partial, (int)l.parts, a.eps,
-                       l.x.hi, l.x.lo, l.x.ld, l.scales);
-    };
-    if (aligned) first(k_norm<T, kVec>, k_first_words<T, kVec>);
-    else first(k_norm<T, 1>, k_first_words<T, 1>);
+    A2_CUDA_TRY(launch_chained(aligned ? k_norm<T, kVec> : k_norm<T, 1>, grid, kNormThreads, 0, s, static_cast<const T*>(a.in), a.in_stride, a.in_pitch, a.rows,
+                           a.cols, l.partial));
+    A2_CUDA_TRY(launch_chained(aligned ? k_first_words<T, kVec> : k_first_words<T, 1>, grid, kNormThreads, 0, s, static_cast<const T*>(a.in), a.in_stride,
+                           a.in_pitch, a.rows, a.cols, l.partial, (int)l.parts, a.eps, l.x.hi, l.x.lo, l.x.ld, l.scales));
     if (a.steps == 0)
-        launch_chained(k_normalized<T>, grid, kNormThreads, 0, s, l.x.hi, l.x.lo, l.x.ld, a.rows, a.cols, l.scales, a.scale, static_cast<T*>(a.out), a.out_stride,
-                                                      a.out_pitch);
-    if (a.steps == 0) return cudaGetLastError();
+        return launch_chained(k_normalized<T>, grid, kNormThreads, 0, s, l.x.hi, l.x.lo, l.x.ld, a.rows, a.cols, l.scales, a.scale, static_cast<T*>(a.out),
+                              a.out_stride, a.out_pitch);
     // X goes back and forth between two buffers: two of each product that reads it
     auto operand = [](const Words& w, int64_t rows, int64_t k, bool mn) { return Operand{w.hi, w.lo, rows, k, w.ld, w.stride, mn}; };
     Operand gram = operand(l.gram, m, m, false), b = operand(l.poly, m, m, false);
     gram.symmetric = b.symmetric = true;
     const Words x[2] = {l.x, l.y};
     GemmArgs make_gram[2], make_poly, update[2];
-    cudaError_t e = make_gemm(gram, gram, a.n_mats, false, true, flush, 1, &make_poly);
+    A2_CUDA_TRY(make_gemm(gram, gram, a.n_mats, false, true, flush, 1, &make_poly));
     for (int k = 0; k < 2 && k < a.steps; ++k) {
         const Operand side = operand(x[k], m, n, tall);
-        if (e == cudaSuccess) e = make_gemm(side, side, a.n_mats, false, true, flush, l.gram_parts, &make_gram[k]);
-        if (e == cudaSuccess)
-            e = tall ? make_gemm(operand(x[k], a.rows, m, false), b, a.n_mats, false, false, flush, 1, &update[k])
-                     : make_gemm(b, operand(x[k], n, m, true), a.n_mats, false, false, flush, 1, &update[k]);
+        A2_CUDA_TRY(make_gemm(side, side, a.n_mats, false, true, flush, l.gram_parts, &make_gram[k]));
+        A2_CUDA_TRY(tall ? make_gemm(operand(x[k], a.rows, m, false), b, a.n_mats, false, false, flush, 1, &update[k])
+                     : make_gemm(b, operand(x[k], n, m, true), a.n_mats, false, false, flush, 1, &update[k]));
     }
     const int64_t part_stride = a.n_mats * l.gram.stride;
-    for (int step = 0; step < a.steps && e == cudaSuccess; ++step) {
+    for (int step = 0; step < a.steps; ++step) {
         const Poly poly{a.ca, a.cb, a.cc, step};
         const bool last = step + 1 == a.steps;
-        e = launch_gemm<SymmetricEpi<false>, kWords>(make_gram[step % 2],
-                                                     {l.gram, l.gram, m, l.scales, poly, l.gram_parts > 1 ? l.gram_sums : nullptr, part_stride}, s);
-        if (e == cudaSuccess && l.gram_parts > 1)  // only with fewer tiles than pairs, so m and the matrices fit a grid
-            e = launch_chained(k_join_gram, dim3((unsigned)ceil_div(m, 512), (unsigned)m, (unsigned)a.n_mats), 256, 0, s, l.gram_sums, l.gram_parts,
-                               part_stride, l.gram, m, l.scales, poly);
-        if (e == cudaSuccess) e = launch_gemm<SymmetricEpi<true>, kWords>(make_poly, {l.gram, l.poly, m, l.scales, poly, nullptr, 0}, s);
-        if (e == cudaSuccess)
-            e = launch_gemm<UpdateEpi<T>, kWords>(
-                update[step % 2],
-                {x[1 - step % 2], a.rows, a.cols, l.scales, poly, last ? static_cast<T*>(a.out) : nullptr, a.out_stride, a.out_pitch, a.scale}, s);
+        A2_CUDA_TRY((launch_gemm<SymmetricEpi<false>, kWords>(
+            make_gram[step % 2], {l.gram, l.gram, m, l.scales, poly, l.gram_parts > 1 ? l.gram_sums : nullptr, part_stride}, s)));
+        if (l.gram_parts > 1)  // only with fewer tiles than pairs, so m and the matrices fit a grid
+            A2_CUDA_TRY(launch_chained(k_join_gram, dim3((unsigned)ceil_div(m, 512), (unsigned)m, (unsigned)a.n_mats), 256, 0, s, l.gram_sums, l.gram_parts,
+                                   part_stride, l.gram, m, l.scales, poly));
+        A2_CUDA_TRY((launch_gemm<SymmetricEpi<true>, kWords>(make_poly, {l.gram, l.poly, m, l.scales, poly, nullptr, 0}, s)));
+        A2_CUDA_TRY((launch_gemm<UpdateEpi<T>, kWords>(
+            update[step % 2],
+            {x[1 - step % 2], a.rows, a.cols, l.scales, poly, last ? static_cast<T*>(a.out) : nullptr, a.out_stride, a.out_pitch, a.scale}, s)));
     }
-    if (e != cudaSuccess) return e;
-    return cudaGetLastError();
+    return cudaSuccess;
 }
 
 // ---- narrow matrices: all steps in one cluster -------------------------------------------------------
@@ -696,10 +689,9 @@ cudaError_t narrow_typed(const OrthogonalizeArgs& a, cudaStream_t s) {
                  a.rows > a.cols, {a.ca, a.cb, a.cc, 0}, a.eps, a.scale, nullptr};
     g.ctas = (int)ceil_div(n, g.chunk);
     static std::atomic<uint64_t> allowed, clusters;
-    cudaError_t e = gave_up_flag(&g.gave_up);
-    if (e == cudaSuccess) e = allow_shared_memory(reinterpret_cast<const void*>(k_narrow<T>), kNarrowSmem, allowed);
-    if (e == cudaSuccess) e = allow_large_clusters(reinterpret_cast<const void*>(k_narrow<T>), clusters);
-    if (e != cudaSuccess) return e;
+    A2_CUDA_TRY(gave_up_flag(&g.gave_up));
+    A2_CUDA_TRY(allow_shared_memory(reinterpret_cast<const void*>(k_narrow<T>), kNarrowSmem, allowed));
+    A2_CUDA_TRY(allow_large_clusters(reinterpret_cast<const void*>(k_narrow<T>), clusters));
     return launch_clusters(k_narrow<T>, dim3((unsigned)(a.n_mats * g.ctas)), kNarrowThreads, kNarrowSmem, (unsigned)g.ctas, s, static_cast<const T*>(a.in),
                            static_cast<T*>(a.out), g);
 }

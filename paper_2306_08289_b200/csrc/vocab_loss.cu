@@ -530,7 +530,6 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
     constexpr bool kWords = sizeof(T) == 4;
     const int64_t n = a.n_tokens;
     const bool with_grad = a.grad_hidden || a.grad_head;
-    cudaError_t e = cudaSuccess;
     if (n == 0) {
         if (!a.grad_head) return cudaSuccess;
         return cudaMemset2DAsync(a.grad_head, a.grad_head_pitch * sizeof(T), 0, a.width * sizeof(T), a.vocab, s);
@@ -547,11 +546,9 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
     if (kWords || weighted) prep.scan = l.scan;
     if (!hidden_in_place) prep.h0 = l.h0, prep.h1 = l.h1;
     if (!head_in_place) prep.w0 = l.w0, prep.w1 = l.w1;
-    if (prep.scan) {
-        launch_chained(k_scan<T>, dim3(kScanCtas), kScanThreads, 0, s, prep);
-    }
+    if (prep.scan) A2_CUDA_TRY(launch_chained(k_scan<T>, dim3(kScanCtas), kScanThreads, 0, s, prep));
     if (prep.h0 || prep.w0 || prep.rate)
-        launch_chained(k_pack<T>, dim3((unsigned)std::min<int64_t>(ceil_div(n + (prep.w0 ? a.vocab : 0), 8), 148 * 8)), 256, 0, s, prep);
+        A2_CUDA_TRY(launch_chained(k_pack<T>, dim3((unsigned)std::min<int64_t>(ceil_div(n + (prep.w0 ? a.vocab : 0), 8), 148 * 8)), 256, 0, s, prep));
 
     auto words = [&](const void* mine, void* w0, void* w1, bool here, int64_t pitch, int64_t row0, int64_t rows, int64_t cols, bool mn) {
         // rows x cols from row0 on; K-major: rows are M or N and columns K; MN-major: the other way round
@@ -566,41 +563,38 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
 
     GemmArgs g;
     // the loss is fp32 with either storage type, so its sums are promoted with both
-    e = make_gemm(hidden(false), head(0, a.vocab, false), 1, !kWords, false, kWords ? kFlush : kFlushLoss, 1, &g);
-    if (e != cudaSuccess) return e;
+    A2_CUDA_TRY(make_gemm(hidden(false), head(0, a.vocab, false), 1, !kWords, false, kWords ? kFlush : kFlushLoss, 1, &g));
     const int parts = (int)(2 * ceil_div(a.vocab, kTileN));
     auto statistics = [&](auto keep) {
         using Epi = StatisticsEpi<kWords, decltype(keep)::value>;
         return launch_gemm<Epi, true>(
             g, typename Epi::Args{l.partial, l.keep ? parts : 1, l.keep ? 1 : n, l.z, l.z_ld, l.at_target, a.targets, l.scan, l.exponents, n, a.vocab}, s);
     };
-    e = l.z ? statistics(std::true_type{}) : statistics(std::false_type{});
-    if (e != cudaSuccess) return e;
+    A2_CUDA_TRY(l.z ? statistics(std::true_type{}) : statistics(std::false_type{}));
     const int32_t* poisoned = hidden_in_place ? nullptr : l.poisoned;
     if (l.keep) {
-        e = launch_rows(a, l.partial, parts, l.at_target, poisoned, l.z, l.z_ld, with_grad, WordSink<kWords>{l.p0, l.p1, l.p_ld, l.rate}, s);
+        A2_CUDA_TRY(launch_rows(a, l.partial, parts, l.at_target, poisoned, l.z, l.z_ld, with_grad, WordSink<kWords>{l.p0, l.p1, l.p_ld, l.rate}, s));
     } else {
-        e = launch_chained(k_finish, dim3((unsigned)ceil_div(n, 32)), kFinishWarps * 32, 0, s, l.partial, parts, l.at_target, a.targets, poisoned, n, a.vocab,
-                           a.loss, a.lse);
+        A2_CUDA_TRY(launch_chained(k_finish, dim3((unsigned)ceil_div(n, 32)), kFinishWarps * 32, 0, s, l.partial, parts, l.at_target, a.targets, poisoned, n,
+                               a.vocab, a.loss, a.lse));
     }
-    if (e != cudaSuccess || !with_grad) return e;
+    if (!with_grad) return cudaSuccess;
 
     auto join = [&](const float* kept, int parts, int64_t rows, T* out, int64_t pitch, const GradientScale& scale) {
         for (int64_t r = 0; r < rows; r += 65535) {  // the grid's second dimension ends there
             const int64_t some = std::min<int64_t>(65535, rows - r);
-            launch_chained(k_join_parts<T>, dim3((unsigned)ceil_div(a.width, 256), (unsigned)some), 256, 0, s, kept + r * l.kept_ld, parts, l.kept_ld, some, rows, a.width,
-                                                                                                  out + r * pitch, pitch, scale);
+            A2_CUDA_TRY(launch_chained(k_join_parts<T>, dim3((unsigned)ceil_div(a.width, 256), (unsigned)some), 256, 0, s, kept + r * l.kept_ld, parts,
+                                   l.kept_ld, some, rows, a.width, out + r * pitch, pitch, scale));
         }
+        return cudaSuccess;
     };
     for (int64_t v0 = 0; v0 < a.vocab; v0 += l.piece) {
         const int64_t rows = std::min(l.piece, a.vocab - v0);
         const bool first = v0 == 0, final = v0 + rows == a.vocab;
         if (!l.keep) {
-            e = make_gemm(hidden(false), head(v0, rows, false), 1, !kWords, false, flush, 1, &g);
-            if (e != cudaSuccess) return e;
+            A2_CUDA_TRY(make_gemm(hidden(false), head(v0, rows, false), 1, !kWords, false, flush, 1, &g));
             const typename ProbabilityEpi<kWords>::Args prob{l.p0, l.p1, l.p_ld, a.targets, a.lse, l.rate, l.scan, l.exponents, n, a.vocab, v0};
-            e = launch_gemm<ProbabilityEpi<kWords>, kWords>(g, prob, s);
-            if (e != cudaSuccess) return e;
+            A2_CUDA_TRY((launch_gemm<ProbabilityEpi<kWords>, kWords>(g, prob, s)));
         }
         using Grad = GradientEpi<T>;
         GemmArgs of_head, of_hidden;
@@ -611,25 +605,23 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
         const typename Grad::Args head_args{head_parts ? nullptr : head_out, a.grad_head_pitch, rows, a.width, l.head_kept, l.kept_ld, false, head_scale};
         const typename Grad::Args hidden_args{final && !hidden_parts ? hidden_out : nullptr, a.grad_hidden_pitch, n, a.width, l.kept, l.kept_ld, !first,
                                               hidden_scale};
-        if (a.grad_head) e = make_gemm(Operand{l.p0, l.p1, rows, n, l.p_ld, 0, true}, hidden(true), 1, !kWords, false, flush, l.head_parts, &of_head);
-        if (a.grad_hidden && e == cudaSuccess) {
+        if (a.grad_head) A2_CUDA_TRY(make_gemm(Operand{l.p0, l.p1, rows, n, l.p_ld, 0, true}, hidden(true), 1, !kWords, false, flush, l.head_parts, &of_head));
+        if (a.grad_hidden) {
             // part p of every piece adds to the sums of part p; a short last piece may have fewer parts, but none without a block
             const int here = (int)std::min<int64_t>(l.hidden_parts, ceil_div(rows, kBlockK));
-            e = make_gemm(Operand{l.p0, l.p1, n, rows, l.p_ld, 0, false}, head(v0, rows, true), 1, !kWords, false, flush, here, &of_hidden);
+            A2_CUDA_TRY(make_gemm(Operand{l.p0, l.p1, n, rows, l.p_ld, 0, false}, head(v0, rows, true), 1, !kWords, false, flush, here, &of_hidden));
         }
-        if (e != cudaSuccess) return e;
         if (l.together && a.grad_head && a.grad_hidden) {  // the longer sums first
-            e = rows >= n ? launch_gemms<Grad, kWords>(of_hidden, hidden_args, of_head, head_args, s)
-                          : launch_gemms<Grad, kWords>(of_head, head_args, of_hidden, hidden_args, s);
+            A2_CUDA_TRY((rows >= n ? launch_gemms<Grad, kWords>(of_hidden, hidden_args, of_head, head_args, s)
+                               : launch_gemms<Grad, kWords>(of_head, head_args, of_hidden, hidden_args, s)));
         } else {
-            if (a.grad_head) e = launch_gemm<Grad, kWords>(of_head, head_args, s);
-            if (a.grad_hidden && e == cudaSuccess) e = launch_gemm<Grad, kWords>(of_hidden, hidden_args, s);
+            if (a.grad_head) A2_CUDA_TRY((launch_gemm<Grad, kWords>(of_head, head_args, s)));
+            if (a.grad_hidden) A2_CUDA_TRY((launch_gemm<Grad, kWords>(of_hidden, hidden_args, s)));
         }
-        if (e != cudaSuccess) return e;
-        if (a.grad_head && head_parts) join(l.head_kept, l.head_parts, rows, head_out, a.grad_head_pitch, head_scale);
-        if (a.grad_hidden && hidden_parts && final) join(l.kept, l.hidden_parts, n, hidden_out, a.grad_hidden_pitch, hidden_scale);
+        if (a.grad_head && head_parts) A2_CUDA_TRY(join(l.head_kept, l.head_parts, rows, head_out, a.grad_head_pitch, head_scale));
+        if (a.grad_hidden && hidden_parts && final) A2_CUDA_TRY(join(l.kept, l.hidden_parts, n, hidden_out, a.grad_hidden_pitch, hidden_scale));
     }
-    return cudaGetLastError();
+    return cudaSuccess;
 }
 
 }  // namespace

@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(kRowThreads) k_rows(const VocabLossArgs a, con
 }
 
 template <class Sink>
-cudaError_t launch_rows(const VocabLossArgs& a, const float2* partial, int parts, const float* at_target, const int32_t* poisoned, const float* z, int64_t z_ld,
+[[nodiscard]] cudaError_t launch_rows(const VocabLossArgs& a, const float2* partial, int parts, const float* at_target, const int32_t* poisoned, const float* z, int64_t z_ld,
                         bool with_grad, const Sink& sink, cudaStream_t s) {
     return launch_chained(k_rows<Sink>, dim3((unsigned)a.n_tokens, with_grad ? (unsigned)ceil_div(a.vocab, kRowColumns) : 1u), kRowThreads, 0, s, a, partial,
                           parts, at_target, poisoned, with_grad, z, z_ld, sink);

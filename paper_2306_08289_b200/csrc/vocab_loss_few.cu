@@ -224,21 +224,20 @@ template <class T>
 cudaError_t typed(const VocabLossArgs& a, const Layout& l, cudaStream_t s) {
     const int64_t n = a.n_tokens, parts = ceil_div(a.vocab, kN);
     const bool with_grad = a.grad_hidden || a.grad_head;
-    launch_chained(k_few_logits<T>, dim3((unsigned)(parts * ceil_div(n, kM))), kFewThreads, 0, s, a, l.z, l.z_ld, l.partial, l.at_target);
-    const cudaError_t e = launch_rows(a, l.partial, (int)parts, l.at_target, nullptr, l.z, l.z_ld, with_grad, FewSink{l.z, l.z_ld, a.scale, a.weights}, s);
-    if (e != cudaSuccess || !with_grad) return e;
+    A2_CUDA_TRY(launch_chained(k_few_logits<T>, dim3((unsigned)(parts * ceil_div(n, kM))), kFewThreads, 0, s, a, l.z, l.z_ld, l.partial, l.at_target));
+    A2_CUDA_TRY(launch_rows(a, l.partial, (int)parts, l.at_target, nullptr, l.z, l.z_ld, with_grad, FewSink{l.z, l.z_ld, a.scale, a.weights}, s));
+    if (!with_grad) return cudaSuccess;
     FewGradArgs g{a, l.z, l.z_ld, ceil_div(a.width, kN), l.head, l.hidden};
     if (!a.grad_head) g.head.parts = 0;
     if (!a.grad_hidden) g.hidden.parts = 0;
-    launch_chained(k_few_gradients<T>, dim3((unsigned)(g.head.tiles * g.head.parts + g.hidden.tiles * g.hidden.parts)), kFewThreads, 0, s, g);
+    A2_CUDA_TRY(launch_chained(k_few_gradients<T>, dim3((unsigned)(g.head.tiles * g.head.parts + g.hidden.tiles * g.hidden.parts)), kFewThreads, 0, s, g));
     auto join = [&](const Split& p, int64_t rows, void* out, int64_t pitch) {
-        if (p.parts > 1)
-            launch_chained(k_few_join<T>, dim3((unsigned)std::min<int64_t>(ceil_div(rows * a.width, 256), kCtas)), 256, 0, s, p.sums, p.parts, rows, a.width,
-                           static_cast<T*>(out), pitch);
+        if (p.parts <= 1) return cudaSuccess;
+        return launch_chained(k_few_join<T>, dim3((unsigned)std::min<int64_t>(ceil_div(rows * a.width, 256), kCtas)), 256, 0, s, p.sums, p.parts, rows,
+                              a.width, static_cast<T*>(out), pitch);
     };
-    join(g.head, a.vocab, a.grad_head, a.grad_head_pitch);
-    join(g.hidden, n, a.grad_hidden, a.grad_hidden_pitch);
-    return cudaGetLastError();
+    A2_CUDA_TRY(join(g.head, a.vocab, a.grad_head, a.grad_head_pitch));
+    return join(g.hidden, n, a.grad_hidden, a.grad_hidden_pitch);
 }
 
 }  // namespace
