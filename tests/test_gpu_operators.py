@@ -289,6 +289,91 @@ def test_vocab_loss_extreme_logits(storage):
     assert torch.equal(a[2], b[2] * 2.0**60) and torch.equal(a[3], b[3] * 2.0**-60)
 
 
+# A size of every form that the library picks by (tokens, width, vocabulary): without tensor cores; logits kept; kept, with few tiles and a long sum
+# over the tokens; made again for a P of the whole vocabulary; made again piece by piece, the last piece shorter
+FORMS = {"few": (70, 48, 300), "kept": (700, 264, 2000), "kept, long sums": (5000, 72, 600), "again": (1100, 72, 17003), "pieces": (2600, 136, 32003)}
+
+
+def loss_case(storage, form, seed=0):
+    n, width, vocab = FORMS[form]
+    g, dt = gen(n + seed), DT[storage]
+    hidden = torch.randn(n, width, generator=g, device=DEV).to(dt)
+    head = (torch.randn(vocab, width, generator=g, device=DEV) / math.sqrt(width)).to(dt)
+    targets = torch.randint(0, vocab, (n,), generator=g, device=DEV, dtype=torch.int32)
+    return g, dt, hidden, head, targets
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("form", list(FORMS)[1:])
+@pytest.mark.parametrize("weighted", [False, True])
+def test_vocab_loss_and_gradients_of_every_form(storage, form, weighted):
+    test_vocab_loss_and_gradients(storage, *FORMS[form], weighted)
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_masked_rows_that_are_not_finite(storage, form):
+    """NaN and infinity in hidden rows and weights without a target: no loss, no gradient, and every bit of the other tokens as if the rows were zero."""
+    g, dt, hidden, head, targets = loss_case(storage, form)
+    n = len(hidden)
+    off = torch.arange(n, device=DEV) % 7 == 3
+    weights = torch.rand(n, generator=g, device=DEV)
+    some = torch.where(off, -1, targets).to(torch.int32)
+    zeroed = torch.where(off[:, None], torch.zeros_like(hidden), hidden)
+    want = ops.vocab_loss_grad(zeroed, head, some, weights=torch.where(off, 0.0, weights), scale=0.5)
+    hidden[off, 0] = math.nan
+    hidden[off, 5] = math.inf
+    hidden[off, 6] = -math.inf
+    got = ops.vocab_loss_grad(hidden, head, some, weights=torch.where(off, math.nan, weights), scale=0.5)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2]) and torch.equal(got[3], want[3])
+    assert torch.equal(got[1][~off], want[1][~off]) and not torch.isfinite(got[1][off]).any()
+    assert not got[0][off].any() and not got[2][off].any()
+    none = torch.full_like(targets, 2**31 - 1)
+    loss, lse, gh, gw = ops.vocab_loss_grad(hidden, head, none, weights=torch.full((n,), math.inf, device=DEV))
+    assert not loss.any() and not gh.any() and not gw.any()
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_only_the_products_of_sizes_matter(storage, form):
+    _, _, hidden, head, targets = loss_case(storage, form)
+    a = ops.vocab_loss_grad(hidden, head, targets)
+    b = ops.vocab_loss_grad(hidden * 2.0**60, head * 2.0**-60, targets)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert torch.equal(a[2], b[2] * 2.0**60) and torch.equal(a[3], b[3] * 2.0**-60)
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_logits_in_the_thousands(storage, form):
+    n, width, vocab = FORMS[form]
+    dt = DT[storage]
+    head = torch.zeros(vocab, width, dtype=dt, device=DEV)
+    head[:, 0] = (torch.arange(vocab, device=DEV) % 128).to(dt)
+    hidden = torch.zeros(n, width, dtype=dt, device=DEV)
+    sizes = torch.tensor([64.0, -64.0, 0.0, 2.0**-40], device=DEV)
+    hidden[:, 0] = sizes[torch.arange(n, device=DEV) % 4].to(dt)
+    targets = ((torch.arange(n, device=DEV) * 13) % vocab).to(torch.int32)
+    loss, lse, gh, gw = ops.vocab_loss_grad(hidden, head, targets, scale=1.0 / n)
+    z = hidden[:, :1].double() * head[:, 0].double()[None]
+    want = torch.logsumexp(z, 1)
+    # products are exact; the logarithm, the exponentials and their sums (of up to `depth` terms in a row) are good to some units
+    depth = 256 + vocab / 256 + 16
+    tol = depth * 2.0**-23 + 2.0**-22 * (want.abs() + 4)
+    assert ((lse.double() - want).abs() <= tol).all()
+    at = z.gather(1, targets.long()[:, None])[:, 0]
+    assert ((loss.double() - (want - at)).abs() <= tol + 2.0**-23 * (want - at).abs()).all()
+    assert torch.isfinite(gh).all() and torch.isfinite(gw).all()
+    p = torch.exp(z - want[:, None])
+    p[torch.arange(n, device=DEV), targets.long()] -= 1.0
+    slope = (p @ head[:, 0].double()) / n
+    # of the first column: sums of numbers up to 127 that P's rounding and the exponentials' error (that of lse) leave good to this, and the result's
+    # rounding
+    rel = 2.0**-8 if storage == "bf16" else 2.0**-18
+    mags = (p.abs() @ head[:, 0].double()) / n
+    assert ((gh[:, 0].double() - slope).abs() <= (rel + torch.expm1(2 * tol)) * mags + 127 * 2.0**-30 / n + U[storage] * slope.abs()).all()
+
+
 def test_vocab_loss_gradients_are_difference_quotients():
     """Central differences of the operator's own loss along random directions, 32-bit rows."""
     g = gen(9)
@@ -314,6 +399,41 @@ def test_vocab_loss_gradients_are_difference_quotients():
         cut = 0.7 * move**3 * eps**2 / 6
         noise = 60 * 2.0**-20 / eps
         assert abs(quotient - slope) <= cut + noise, (other, quotient, slope, cut, noise)
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("of", ["hidden", "head"])
+def test_gradients_against_differences_along_themselves(form, of):
+    """The operator's own loss along the normalised gradient, where its slope is largest: the gradient's norm. Two steps and Richardson's
+    extrapolation; what the quotient may be off is a fiftieth of the slope, so a missing or turned gradient cannot pass."""
+    g, _, hidden, head, targets = loss_case("f32", form, 3)
+    n = len(hidden)
+    targets[::9] = -1
+    weights = torch.rand(n, generator=g, device=DEV)
+    out = ops.vocab_loss_grad(hidden, head, targets, weights=weights, scale=0.7)
+    grad, base = (out[2], hidden) if of == "hidden" else (out[3], head)
+    slope = float(grad.double().norm())
+    d = (grad.double() / slope).float()
+
+    def value(x):
+        h, w = (x, head) if of == "hidden" else (hidden, x)
+        return float((0.7 * weights.double() * ops.vocab_loss(h, w, targets)[0].double()).sum())
+
+    def quotient(eps):
+        return (value(base + eps * d) - value(base - eps * d)) / (2 * eps)
+
+    # a unit step moves token t's logits by at most m_t = |direction's share of it| |the other matrix|; the fifth derivative of its log-sum-exp is
+    # below 16 m_t^5 (cumulants of a variable within +-m_t). With steps e and e / 2 the extrapolation leaves e^4 / 480 of it at most.
+    eps = 2.0**-3
+    if of == "hidden":
+        move = d.double().norm(dim=1) * float(head.double().norm(dim=1).max())
+    else:
+        move = hidden.double().norm(dim=1) * float(d.double().norm(dim=1).max())
+    cut = float((0.7 * weights.double() * 16 * move**5).sum()) * eps**4 / 480
+    # every loss is good to 2^-20 of the logits' sizes, the errors of the tokens add up at worst
+    noise = 0.7 * n * 2.0**-20 / (eps / 2) * 5 / 3
+    got = (4 * quotient(eps / 2) - quotient(eps)) / 3
+    assert abs(got - slope) <= min(slope / 50, cut + noise), (got, slope, cut, noise)
 
 
 # ------------------------------------------------------------------------------------------------
