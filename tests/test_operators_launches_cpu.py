@@ -98,3 +98,23 @@ def test_a_call_ends_at_the_first_launch_that_fails(fake, name):
         fake.fake_reset(k)
         assert call(fake, *args) == B.A2_ECUDA, (k, launches)
         assert fake.fake_launches() == k + 1 and len(fake.fake_error_text()) > 10
+
+
+# Launches without gradients, with grad_head, with grad_hidden, with both. Few: logits, rows; both gradients in one; join. Else fp32 rows take a scan and
+# words first, bf16 rows a copy where a gradient needs hidden without its masked rows; then statistics and rows (kept) or finish; P where logits are made again;
+# the products of the gradients, in one launch where they do not fill the GPU; joins of split sums; in pieces, P and the products piece by piece.
+LAUNCHES = {F32: {"few": [2, 3, 4, 4], "kept": [4, 5, 6, 6], "kept, long sums": [4, 6, 5, 6], "again": [4, 6, 7, 7], "pieces": [4, 10, 11, 14]},
+            BF16: {"few": [2, 3, 4, 4], "kept": [2, 4, 5, 5], "kept, long sums": [2, 5, 4, 5], "again": [2, 5, 6, 6], "pieces": [2, 7, 8, 10]}}
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_the_sizes_of_the_gpu_tests_reach_every_form(fake, dtype):
+    from tests.test_gpu_operators import FORMS
+
+    for form, (n, width, vocab) in FORMS.items():
+        got = []
+        for grad in ((), ("head",), ("hidden",), BOTH):
+            fake.fake_reset(-1)
+            assert loss(fake, n, width, vocab, dtype, grad) == B.A2_OK
+            got.append(fake.fake_launches())
+        assert got == LAUNCHES[dtype][form], form
