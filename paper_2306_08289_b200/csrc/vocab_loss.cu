@@ -336,6 +336,10 @@ struct GradientScale {
     bool of_hidden;  // the other operand is head (grad_hidden) or hidden (grad_head)
     bool weighted;
     float scale;
+    // of grad_hidden's rows, else NULL: a token without a target has a zero row, also where the head holds what is not finite and 0 * NaN came in
+    const int32_t* targets;
+    int64_t vocab;
+    __device__ __forceinline__ bool zero_row(int64_t r) const { return targets && !is_token(targets[r], vocab); }
 };
 template <class T>
 struct GradientFactor {
@@ -397,8 +401,11 @@ struct GradientEpi {
     float* staging;
     float* kept;
     GradientFactor<T> factor;
+    unsigned zero;  // rows of zeros, a bit each
     __device__ __forceinline__ GradientEpi(const Args& args, const Tile& t, int row, int col, int lane_, float* staging_)
-        : a(args), row0(row), col0(col), lane(lane_), staging(staging_), kept(a.kept ? a.kept + t.split * a.rows * a.kept_ld : nullptr), factor(a.scale) {}
+        : a(args), row0(row), col0(col), lane(lane_), staging(staging_), kept(a.kept ? a.kept + t.split * a.rows * a.kept_ld : nullptr), factor(a.scale) {
+        zero = __ballot_sync(0xffffffffu, row0 + lane < a.rows && a.scale.zero_row(row0 + lane));
+    }
     __device__ __forceinline__ void chunk(int c, float (&v)[32]) {
         const int64_t col = col0 + c * 32 + lane;
         if (row0 >= a.rows || col0 + c * 32 >= a.cols) return;
@@ -417,7 +424,7 @@ struct GradientEpi {
 #pragma unroll
         for (int r = 0; r < 32; ++r)
             if (r < rows) {
-                if (a.out) to[r * a.pitch] = factor(v[r]);
+                if (a.out) to[r * a.pitch] = zero >> r & 1 ? narrow<T>(0.0f) : factor(v[r]);
                 else keep[r * a.kept_ld] = v[r];
             }
     }
@@ -435,7 +442,7 @@ __global__ void __launch_bounds__(256) k_join_parts(const float* __restrict__ ke
     float sum = 0.0f;
 #pragma unroll 4
     for (int p = 0; p < parts; ++p) sum += kept[(p * rows + r) * kept_ld + c];
-    out[r * pitch + c] = factor(sum);
+    out[r * pitch + c] = scale.zero_row(r) ? narrow<T>(0.0f) : factor(sum);
 }
 
 // ---- layout and launches ------------------------------------------------------------------------
@@ -580,9 +587,11 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
     }
     if (!with_grad) return cudaSuccess;
 
-    auto join = [&](const float* kept, int parts, int64_t rows, T* out, int64_t pitch, const GradientScale& scale) {
+    auto join = [&](const float* kept, int parts, int64_t rows, T* out, int64_t pitch, const GradientScale& of_all) {
         for (int64_t r = 0; r < rows; r += 65535) {  // the grid's second dimension ends there
             const int64_t some = std::min<int64_t>(65535, rows - r);
+            GradientScale scale = of_all;
+            if (scale.targets) scale.targets += r;
             A2_CUDA_TRY(launch_chained(k_join_parts<T>, dim3((unsigned)ceil_div(a.width, 256), (unsigned)some), 256, 0, s, kept + r * l.kept_ld, parts,
                                    l.kept_ld, some, rows, a.width, out + r * pitch, pitch, scale));
         }
@@ -598,7 +607,7 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
         }
         using Grad = GradientEpi<T>;
         GemmArgs of_head, of_hidden;
-        const GradientScale head_scale{l.scan, false, weighted, a.scale}, hidden_scale{l.scan, true, weighted, a.scale};
+        const GradientScale head_scale{l.scan, false, weighted, a.scale, nullptr, 0}, hidden_scale{l.scan, true, weighted, a.scale, a.targets, a.vocab};
         T* head_out = a.grad_head ? static_cast<T*>(a.grad_head) + v0 * a.grad_head_pitch : nullptr;
         T* hidden_out = static_cast<T*>(a.grad_hidden);
         const bool head_parts = l.head_parts > 1, hidden_parts = l.hidden_parts > 1;

@@ -335,6 +335,17 @@ def test_masked_rows_that_are_not_finite(storage, form):
 
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
 @pytest.mark.parametrize("form", list(FORMS))
+def test_tokens_without_a_target_have_zero_rows_whatever_the_head_holds(storage, form):
+    _, _, hidden, head, targets = loss_case(storage, form)
+    head[11, 3], head[-1, 0] = math.nan, math.inf
+    off = torch.arange(len(hidden), device=DEV) % 3 == 1
+    loss, lse, gh, gw = ops.vocab_loss_grad(hidden, head, torch.where(off, -5, targets).to(torch.int32))
+    assert not loss[off].any() and not gh[off].any()
+    assert not torch.isfinite(loss[~off]).any()
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("form", list(FORMS))
 def test_only_the_products_of_sizes_matter(storage, form):
     _, _, hidden, head, targets = loss_case(storage, form)
     a = ops.vocab_loss_grad(hidden, head, targets)
