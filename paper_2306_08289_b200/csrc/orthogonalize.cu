@@ -21,11 +21,13 @@ constexpr float kScale = 16384.0f;  // 2^14
 // 65504 / 2^14 = 3.998 bounds X, A = X X^T and B; the rest is for rounding
 constexpr double kMostSingular = 1.95, kMostPoly = 3.9;
 
-// What the kernels know of each matrix.
+// What the kernels know of each matrix. Powers of two are kept as exponents: when eps outweighs the norm they lie far below the
+// smallest float.
 struct MatScale {
-    float u;  // X0 = u * (the stored words)
-    int e;    // stored words = G * 2^e
-    int r;    // |X0|_F <= 2^r, r <= 0: far below zero when eps outweighs the norm
+    float u;  // X0 = u * 2^k * (the stored words)
+    int k;
+    int e;  // stored words = G * 2^e
+    int r;  // |X0|_F <= 2^r, r <= 0
 };
 
 // |X_k|_F <= 2^r(k): the scale of the stored words of X_k, k >= 1, is 2^(14 - r(k)), so that a matrix far smaller than eps
@@ -42,13 +44,33 @@ struct Poly {
     int step;  // 0 .. steps - 1
 };
 
-// Value of one stored unit of X at step `step`, and of the next X's stored unit.
-__device__ __forceinline__ void units(const MatScale& s, const Poly& p, float* now, float* next) {
-    int r = s.r;
-    for (int k = 0; k < p.step; ++k) r = next_bound(r, p.a, p.b, p.c);
-    *now = p.step == 0 ? s.u : ldexpf(1.0f, r - 14);
-    *next = ldexpf(1.0f, next_bound(r, p.a, p.b, p.c) - 14);
-}
+// A stored unit of X at step `step` is worth u * 2^k, one of the next X 2^next.
+struct Units {
+    float u;
+    int k, next;
+    __device__ __forceinline__ Units(const MatScale& s, const Poly& p) {
+        int r = s.r;
+        for (int i = 0; i < p.step; ++i) r = next_bound(r, p.a, p.b, p.c);
+        u = p.step == 0 ? s.u : 1.0f;
+        k = p.step == 0 ? s.k : r - 14;
+        next = next_bound(r, p.a, p.b, p.c) - 14;
+    }
+    // What sums of words of X times words of X become in A's words (2^14).
+    __device__ __forceinline__ float gram() const { return ldexpf(kScale * u * u, 2 * k); }
+};
+
+// v * scale * u * 2^k, in factors that leave the range only if the result does.
+struct Scaled {
+    float a, b;
+    __device__ __forceinline__ Scaled(float scale, float u, int k) {
+        int e = 0;
+        const float m = frexpf(scale, &e);
+        const PowerOfTwo up(e + k);
+        a = m * u * up.a;
+        b = up.b;
+    }
+    __device__ __forceinline__ float operator()(float v) const { return v * a * b; }
+};
 
 // ---- norm and first words ------------------------------------------------------------------------
 constexpr int kNormThreads = 256;
@@ -93,11 +115,12 @@ __global__ void __launch_bounds__(kNormThreads) k_norm(const T* __restrict__ in,
 }
 
 __device__ __forceinline__ MatScale mat_scale(double squares, double eps) {
-    const double norm = sqrt(squares), by = norm + eps;
-    if (!(norm <= 1e300)) return {NAN, 0, 0};
-    if (norm == 0.0) return {0.0f, 0, 0};
-    const int e = 13 - ilogb(norm);  // norm * 2^e in [2^13, 2^14)
-    return {(float)(1.0 / (ldexp(by, e))), e, min(0, ilogb(norm / by) + 1)};
+    const double norm = sqrt(squares), by = fmin(norm + eps, 1.7e308);
+    if (!(norm <= 1e300)) return {NAN, 0, 0, 0};
+    if (norm == 0.0) return {0.0f, 0, 0, 0};
+    const int n = ilogb(norm), d = ilogb(by), e = 13 - n;  // norm * 2^e in [2^13, 2^14)
+    const double norm1 = ldexp(norm, -n), by1 = ldexp(by, -d);  // in [1, 2)
+    return {(float)(1.0 / by1), -d - e, e, min(0, n - d + (norm1 >= by1 ? 1 : 0))};
 }
 
 // Words of G 2^e, [rows, ld].
@@ -138,13 +161,13 @@ template <class T>
 __global__ void __launch_bounds__(kNormThreads) k_normalized(const __half* hi, const __half* lo, int64_t ld, int64_t rows, int64_t cols,
                                                              const MatScale* scales, float scale, T* out, int64_t stride, int64_t pitch) {
     ptx::chained();
-    const float by = scales[blockIdx.y].u * scale;
+    const Scaled by(scale, scales[blockIdx.y].u, scales[blockIdx.y].k);
     const int64_t base = (int64_t)blockIdx.y * rows * ld;
     const int64_t warp = (int64_t)blockIdx.x * (kNormThreads / 32) + threadIdx.x / 32, warps = (int64_t)gridDim.x * (kNormThreads / 32);
     for (int64_t i = warp; i < rows; i += warps)
         for (int64_t j = threadIdx.x % 32; j < cols; j += 32) {
             const int64_t at = base + i * ld + j;
-            out[blockIdx.y * stride + i * pitch + j] = narrow<T>((__half2float(hi[at]) + (lo ? __half2float(lo[at]) : 0.0f)) * by);
+            out[blockIdx.y * stride + i * pitch + j] = narrow<T>(by(__half2float(hi[at]) + (lo ? __half2float(lo[at]) : 0.0f)));
         }
 }
 
@@ -188,9 +211,7 @@ struct SymmetricEpi {
         if (kQuadratic) {
             factor = a.poly.c / kScale;
         } else {
-            float now, next;
-            units(a.scales[mat], a.poly, &now, &next);
-            factor = kScale * now * now;
+            factor = Units(a.scales[mat], a.poly).gram();
         }
     }
     __device__ __forceinline__ void chunk(int c, float (&v)[32]) {
@@ -232,9 +253,7 @@ __global__ void __launch_bounds__(256) k_join_gram(const float* __restrict__ par
     ptx::chained();
     const int64_t row = blockIdx.y, mat = blockIdx.z, col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 2;
     if (col >= m || col / kTileN > row / kTileM) return;
-    float now, next;
-    units(scales[mat], poly, &now, &next);
-    const float factor = kScale * now * now;
+    const float factor = Units(scales[mat], poly).gram();
     const int64_t at = mat * to.stride + row * to.ld + col;  // ld is even: the second column may be padding
     float x = 0.0f, y = 0.0f;
 #pragma unroll 4
@@ -265,19 +284,16 @@ struct UpdateEpi {
     int64_t row0, col0, mat;
     int lane;
     float* staging;
-    float factor;
+    Scaled factor;
+    static __device__ __forceinline__ Scaled make(const Args& a, const Units& x) { return Scaled(a.out ? a.scale : 1.0f, x.u, x.k - 14 - (a.out ? 0 : x.next)); }
     __device__ __forceinline__ UpdateEpi(const Args& args, const Tile& t, int row, int col, int lane_, float* staging_)
-        : a(args), row0(row), col0(col), mat(t.b), lane(lane_), staging(staging_) {
-        float now, next;
-        units(a.scales[mat], a.poly, &now, &next);
-        factor = (a.out ? a.scale * now : now / next) / kScale;
-    }
+        : a(args), row0(row), col0(col), mat(t.b), lane(lane_), staging(staging_), factor(make(a, Units(a.scales[mat], a.poly))) {}
     __device__ __forceinline__ void chunk(int c, float (&v)[32]) {
         const int64_t col = col0 + c * 32;
         if (row0 >= a.rows || col >= a.cols) return;
         const int rows = (int)min((int64_t)32, a.rows - row0);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] *= factor;
+        for (int k = 0; k < 32; ++k) v[k] = factor(v[k]);
         if (!a.out) {
             write_words(a.to, mat * a.to.stride + row0 * a.to.ld + col, v, rows, lane, staging);
             return;
@@ -556,10 +572,9 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) k_narrow(const T* __restric
     };
     Poly poly = g.poly;
     for (poly.step = 0; poly.step < g.steps; ++poly.step) {
-        float now, next;
-        units(scale, poly, &now, &next);
+        const Units x(scale, poly);
         const bool last = poly.step + 1 == g.steps;
-        const float gram = kScale * now * now;
+        const float gram = x.gram();
         product(tmem, xs, xs, false, n16 / 16, to_square);
         float total[2][32];  // of A, this thread's columns half * 32 .. and half * 32 + 64 ..
         if (g.ctas > 1) {
@@ -641,13 +656,13 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) k_narrow(const T* __restric
                 if (col + k < m16) write8(aw, col + k, v + k);
         }
         product(tmem + 256, as, xs, true, m16 / 16, to_wide);
-        const float factor = (last ? g.scale * now : now / next) / kScale;
+        const Scaled factor(last ? g.scale : 1.0f, x.u, x.k - 14 - (last ? 0 : x.next));
         for (int col = half * 32; mine && col < n16; col += 64) {
             float v[32];
             ptx::tmem_load32(v, lanes + 256 + col);
             ptx::tmem_load_wait();
 #pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] *= factor;
+            for (int k = 0; k < 32; ++k) v[k] = factor(v[k]);
             if (!last) {  // rows of padding keep their zeros: what they hold in tensor memory is not a product of anything
 #pragma unroll
                 for (int k = 0; k < 32; k += 8)
@@ -669,9 +684,10 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) k_narrow(const T* __restric
         }
     }
     if (g.steps == 0) {
+        const Scaled by(g.scale, scale.u, scale.k);
         for (int i = warp; i < my_rows; i += kNarrowThreads / 32)
             for (int j = lane; j < my_cols; j += 32)
-                to[i * g.out_pitch + j] = narrow<T>(up(widen(from[i * g.in_pitch + j])) * (scale.u * g.scale));
+                to[i * g.out_pitch + j] = narrow<T>(by(up(widen(from[i * g.in_pitch + j]))));
     }
     ptx::fence_before();
     sync_matrix();  // no CTA leaves while another may read its shared memory

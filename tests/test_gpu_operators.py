@@ -540,6 +540,27 @@ def test_orthogonalize_special_values(storage, rows, cols):
     check_orthogonalize((u @ v)[None].to(dt), ops.orthogonalize((u @ v)[None].to(dt)), storage)
 
 
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(40, 40), (70, 900), (300, 200)])
+@pytest.mark.parametrize("steps", [0, 1, 5])
+def test_orthogonalize_where_eps_outweighs_the_matrix(storage, rows, cols, steps):
+    """X0 = G / (|G| + eps) far below the smallest float: the caller's scale brings the result back, with all its bits."""
+    g, dt = gen(12), DT[storage]
+    base = torch.randn(2, rows, cols, generator=g, device=DEV)
+    base[1] *= 2.0**-30  # another size in the same batch
+    x = (base * 2.0**-60).to(dt)
+    got = ops.orthogonalize(x, steps=steps, eps=1e30, scale=2.0**110)
+    check_orthogonalize(x, got, storage, steps=steps, eps=1e30, scale=2.0**110)
+    # without it the result is nothing
+    assert not ops.orthogonalize(x, steps=steps, eps=1e38 * 1e60).any()
+    # subnormal rows: G (a^steps) to a unit of the smallest float or the words' 2^-20
+    x = (base * 2.0**-135).to(dt)
+    got = ops.orthogonalize(x, steps=steps, eps=1.0, scale=1.0)
+    want = newton_schulz(x, steps, ops.NEWTON_SCHULZ, 1.0)
+    rel = 2.0**-20 if storage == "f32" else 2.0**-6
+    assert ((got.double() - want).abs() <= rel * want.abs().amax(dim=(1, 2), keepdim=True) + (2.0**-148 if storage == "f32" else 2.0**-132)).all()
+
+
 # ------------------------------------------------------------------------------------------------
 # streams, refusals, the operators together
 # ------------------------------------------------------------------------------------------------
