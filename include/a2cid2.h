@@ -436,8 +436,10 @@ int a2cid2_vocab_loss_workspace(int64_t n_tokens, int64_t width, int64_t vocab, 
  *   P_tv = scale * weights[t] * (exp(z_tv - lse[t]) - [v = targets[t]]), 0 where targets[t] is no token,
  *   grad_hidden_t = sum_v P_tv head_v,  grad_head_v = sum_t P_tv hidden_t.
  * A token without a target adds nothing to grad_head and has a zero row in grad_hidden, whatever its hidden row and weight
- * hold. With fp32 rows the products are formed from two 11-bit words an operand (22 bits, about what an fp32 sum keeps); with
- * bf16 rows P is rounded to bf16 before its products. n_tokens = 0 zeroes grad_head. */
+ * hold. With fp32 rows the products are formed from two 11-bit words an operand: 22 bits (about what an fp32 sum keeps) of every element
+ * down to 2^-28 of the largest one, 2^-50 of the largest one below; the largest of hidden's rows with a target, of head, and of P
+ * the largest weight. Small problems are summed in fp32 throughout. With bf16 rows P is rounded to bf16 before its products.
+ * n_tokens = 0 zeroes grad_head. */
 int a2cid2_vocab_loss(const void* hidden, int64_t hidden_pitch, const void* head, int64_t head_pitch, const int32_t* targets,
                       int64_t n_tokens, int64_t width, int64_t vocab, const float* weights, double scale, float* loss,
                       float* lse, void* grad_hidden, int64_t grad_hidden_pitch, void* grad_head, int64_t grad_head_pitch,

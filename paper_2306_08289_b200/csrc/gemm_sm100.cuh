@@ -10,13 +10,14 @@
 // index contiguous); the 128-byte swizzle of TMA is the one the MMA descriptors name. Everything outside a matrix is
 // read as zero, so any M, N and K work.
 //
-// Words: an fp32 operand x is held as two fp16 words, hi = fp16(s x), lo = fp16(s x - hi), s a power of two that puts the largest
-// element just below 2^15. That keeps 22 bits of every element down to 2^-18 of the largest one, and 2^-40 of the largest one
-// below. A product is then three passes over K, lo*hi + hi*lo + hi*hi (small terms first).
+// Words: an fp32 operand x is held as two fp16 words, hi = fp16(s x), lo = fp16((s x - hi) 2^11), s a power of two that puts the largest
+// element just below 2^15. That keeps 22 bits of every element down to 2^-28 of the largest one, and 2^-50 of the largest one
+// below (a low word without its 2^11 would run into fp16's smallest numbers 11 bits earlier). A product is then three passes over K,
+// lo*hi + hi*lo + hi*hi: the small terms first, in a stay of their own whose sums are taken times 2^-11 when they are read back.
 //
 // Sums: the tensor core cuts, rather than rounds, each addition to its fp32 sums, an error that adds up with one sign over
 // thousands of steps. With kPromote the sums leave tensor memory every `flush` K blocks and are added up in registers (the passes
-// of the small terms, 2^-11 of the others, make one stay).
+// of the small terms, 2^-11 of the others, make one stay). Products of two words are always promoted.
 //
 // What bounds it, measured: a block of 64 along K takes 610 cycles (560 with the loads left out): the tensor core; 1.40 PFLOP/s on 8,192
 // x 9,472 x 2,048 bf16, the rate of a sustained library product under the same power cap; 1.1 PFLOP/s of three-pass products at 2,048 x
@@ -190,6 +191,11 @@ __device__ __forceinline__ void tmem_load_pairs(uint64_t (&v)[16], uint32_t addr
 #pragma unroll
     for (int k = 0; k < 16; ++k) asm volatile("mov.b64 %0, {%1, %2};" : "=l"(v[k]) : "f"(f[2 * k]), "f"(f[2 * k + 1]));
 }
+__device__ __forceinline__ uint64_t pair(float v) {
+    uint64_t p;
+    asm("mov.b64 %0, {%1, %1};" : "=l"(p) : "f"(v));
+    return p;
+}
 __device__ __forceinline__ void tmem_store_pairs(uint32_t addr, const uint64_t* p) {
     uint32_t v[32];
 #pragma unroll
@@ -337,18 +343,31 @@ struct PowerOfTwo {
     __device__ __forceinline__ float operator()(float v) const { return v * a * b; }
 };
 
-// x as hi + lo.
+constexpr int kLowUp = 2048;  // low words are held times this
+
+// x as hi + lo / kUp.
+template <int kUp = kLowUp>
 __device__ __forceinline__ void split_words(float x, __half& hi, __half& lo) {
     hi = __float2half_rn(x);
     const float back = __half2float(hi);
-    lo = __float2half_rn(fabsf(back) <= 65504.0f ? x - back : 0.0f);
+    lo = __float2half_rn(fabsf(back) <= 65504.0f ? (x - back) * kUp : 0.0f);
 }
 
 // A pair of finite values in packed conversions, for the epilogues.
+template <int kUp = kLowUp>
 __device__ __forceinline__ void split_pair(float x, float y, __half& hx, __half& hy, __half& lx, __half& ly) {
     const __half2 h = __floats2half2_rn(x, y);
     const float2 back = __half22float2(h);
-    const __half2 l = __floats2half2_rn(x - back.x, y - back.y);
+    float2 low{x - back.x, y - back.y};
+    if constexpr (kUp != 1) {  // the difference times kUp in two packed instructions; exact, for kUp is a power of two
+        uint64_t both, rest;
+        asm("mov.b64 %0, {%1, %2};" : "=l"(both) : "f"(x), "f"(y));
+        asm("mov.b64 %0, {%1, %2};" : "=l"(rest) : "f"(back.x), "f"(back.y));
+        asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(rest) : "l"(ptx::pair(-kUp)));
+        asm("fma.rn.f32x2 %0, %0, %1, %2;" : "+l"(both) : "l"(ptx::pair(kUp)), "l"(rest));
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(low.x), "=f"(low.y) : "l"(both));
+    }
+    const __half2 l = __floats2half2_rn(low.x, low.y);
     hx = __low2half(h);
     hy = __high2half(h);
     lx = __low2half(l);
@@ -542,6 +561,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                     uint64_t sum[64];  // pairs of columns
 #pragma unroll
                     for (int k = 0; k < 64; ++k) sum[k] = 0;
+                    // what a stay's sums are worth: the first one of a product of words is that of the small terms
+                    uint64_t worth = g.passes == 1 ? ptx::pair(1.0f) : ptx::pair(1.0f / kLowUp);
 #pragma unroll 1
                     for (int done = 0;;) {
                         buf = chunk & 1;
@@ -555,8 +576,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
                             ptx::tmem_load_wait();
 #pragma unroll
                             for (int k = 0; k < 32; ++k)
-                                asm volatile("add.rn.f32x2 %0, %0, %1;" : "+l"(sum[c * 16 + k]) : "l"(v[k / 16][k % 16]));
+                                asm volatile("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(sum[c * 16 + k]) : "l"(v[k / 16][k % 16]), "l"(worth));
                         }
+                        worth = ptx::pair(1.0f);
                         done = stay_end<true>(g, done, blocks);
                         if (done == blocks) break;  // the last stay: the epilogue reads it below
                         ptx::fence_before();
@@ -601,6 +623,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) k_g
 template <class Epi, bool kPromote, int kJobs>
 [[nodiscard]] cudaError_t launch_jobs(const Jobs<Epi, kJobs>& jobs, cudaStream_t s) {
     int64_t tiles = 0;
+    for (const GemmArgs& g : jobs.g)
+        if (g.passes != 1 && !kPromote) return cudaErrorInvalidValue;  // the small terms need a stay of their own
     for (const GemmArgs& g : jobs.g)
         tiles += (int64_t)g.batch * g.splits * (g.lower ? (int64_t)g.tiles_m * (g.tiles_m + 1) / 2 : (int64_t)g.tiles_m * g.tiles_n);
     if (tiles == 0) return cudaSuccess;

@@ -44,6 +44,9 @@ struct Poly {
     int step;  // 0 .. steps - 1
 };
 
+// 2^e for e <= 127, zero below the normal numbers.
+__device__ __forceinline__ float power_of_two(int e) { return e < -126 ? 0.0f : __int_as_float((e + 127) << 23); }
+
 // A stored unit of X at step `step` is worth u * 2^k, one of the next X 2^next.
 struct Units {
     float u;
@@ -56,7 +59,7 @@ struct Units {
         next = next_bound(r, p.a, p.b, p.c) - 14;
     }
     // What sums of words of X times words of X become in A's words (2^14).
-    __device__ __forceinline__ float gram() const { return ldexpf(kScale * u * u, 2 * k); }
+    __device__ __forceinline__ float gram() const { return kScale * u * u * power_of_two(2 * k); }
 };
 
 // v * scale * u * 2^k, in factors that leave the range only if the result does.
@@ -167,7 +170,7 @@ __global__ void __launch_bounds__(kNormThreads) k_normalized(const __half* hi, c
     for (int64_t i = warp; i < rows; i += warps)
         for (int64_t j = threadIdx.x % 32; j < cols; j += 32) {
             const int64_t at = base + i * ld + j;
-            out[blockIdx.y * stride + i * pitch + j] = narrow<T>(by(__half2float(hi[at]) + (lo ? __half2float(lo[at]) : 0.0f)));
+            out[blockIdx.y * stride + i * pitch + j] = narrow<T>(by(__half2float(hi[at]) + (lo ? __half2float(lo[at]) / kLowUp : 0.0f)));
         }
 }
 
@@ -236,7 +239,7 @@ struct SymmetricEpi {
             if (a.from.lo) {
                 load_rows16(staging, x, a.from.lo + at, a.from.ld, rows, lane);
 #pragma unroll
-                for (int k = 0; k < 32; ++k) v[k] += a.poly.b * __half2float(x[k]);
+                for (int k = 0; k < 32; ++k) v[k] += a.poly.b / kLowUp * __half2float(x[k]);
             }
         } else {
 #pragma unroll
@@ -281,19 +284,27 @@ struct UpdateEpi {
         float scale;
     };
     const Args& a;
-    int64_t row0, col0, mat;
+    int row0, col0, mat;
     int lane;
     float* staging;
-    Scaled factor;
-    static __device__ __forceinline__ Scaled make(const Args& a, const Units& x) { return Scaled(a.out ? a.scale : 1.0f, x.u, x.k - 14 - (a.out ? 0 : x.next)); }
+    float factor, rest;  // rest: the caller's matrix alone
     __device__ __forceinline__ UpdateEpi(const Args& args, const Tile& t, int row, int col, int lane_, float* staging_)
-        : a(args), row0(row), col0(col), mat(t.b), lane(lane_), staging(staging_), factor(make(a, Units(a.scales[mat], a.poly))) {}
+        : a(args), row0(row), col0(col), mat(t.b), lane(lane_), staging(staging_), rest(1.0f) {
+        const Units x(a.scales[mat], a.poly);
+        if (a.out) {
+            const Scaled by(a.scale, x.u, x.k - 14);
+            factor = by.a;
+            rest = by.b;
+        } else {
+            factor = x.u * power_of_two(x.k - x.next - 14);  // both bound the same X: about 2^-14
+        }
+    }
     __device__ __forceinline__ void chunk(int c, float (&v)[32]) {
-        const int64_t col = col0 + c * 32;
+        const int col = col0 + c * 32;
         if (row0 >= a.rows || col >= a.cols) return;
         const int rows = (int)min((int64_t)32, a.rows - row0);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] = factor(v[k]);
+        for (int k = 0; k < 32; ++k) v[k] *= factor;
         if (!a.out) {
             write_words(a.to, mat * a.to.stride + row0 * a.to.ld + col, v, rows, lane, staging);
             return;
@@ -303,7 +314,7 @@ struct UpdateEpi {
             T* to = a.out + mat * a.stride + row0 * a.pitch + col + lane;
 #pragma unroll
             for (int r = 0; r < 32; ++r)
-                if (r < rows) to[r * a.pitch] = narrow<T>(v[r]);
+                if (r < rows) to[r * a.pitch] = narrow<T>(v[r] * rest);
         }
     }
     __device__ __forceinline__ void finish() {}
@@ -411,6 +422,7 @@ constexpr int kWordBytes = (kNarrowM / 64) * kBlockBytes;         // a word of A
 constexpr int kSquareBytes = kNarrowM * (kNarrowM + 4) * 4 + 64;  // two of them, or a part of A as floats (and what a last load reads past it)
 static_assert(2 * kWordBytes <= kSquareBytes, "A's words and its part share their place");
 constexpr int kNarrowSmem = 2 * (kNarrowN / 64) * kBlockBytes + kSquareBytes + 1024;
+constexpr int kNarrowLowUp = 1;  // all passes share one accumulator: tensor memory has no room for another, so low words keep their size
 static_assert(kNarrowSmem <= 227 * 1024 - 512, "shared memory of one CTA, with room for the static part");
 
 // Byte offset of columns col .. col + 7 of a row.
@@ -532,7 +544,7 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) k_narrow(const T* __restric
         for (int q = 0; q < 8; ++q) {
             const bool inside = i < m && j + q < n;
             const float v = inside ? widen(g.tall ? from[(j + q) * g.in_pitch + i] : from[i * g.in_pitch + j + q]) : 0.0f;
-            split_words(up(v), hi.v[q], lo.v[q]);
+            split_words<kNarrowLowUp>(up(v), hi.v[q], lo.v[q]);
         }
         const uint32_t at = swizzled(i, j);
         *reinterpret_cast<Pack<__half, 8>*>(xw[0] + at) = hi;
@@ -565,7 +577,7 @@ __global__ void __launch_bounds__(kNarrowThreads, 1) k_narrow(const T* __restric
     auto write8 = [&](char* const (&to)[2], int col, const float* v) {
         Pack<__half, 8> hi, lo;
 #pragma unroll
-        for (int q = 0; q < 8; q += 2) split_pair(v[q], v[q + 1], hi.v[q], hi.v[q + 1], lo.v[q], lo.v[q + 1]);
+        for (int q = 0; q < 8; q += 2) split_pair<kNarrowLowUp>(v[q], v[q + 1], hi.v[q], hi.v[q + 1], lo.v[q], lo.v[q + 1]);
         const uint32_t at = swizzled(row, col);
         *reinterpret_cast<Pack<__half, 8>*>(to[0] + at) = hi;
         *reinterpret_cast<Pack<__half, 8>*>(to[1] + at) = lo;

@@ -207,7 +207,7 @@ def test_vocab_loss_and_gradients(storage, n, width, vocab, weighted):
 
 
 @pytest.mark.parametrize("weighted", [False, True])
-@pytest.mark.parametrize("storage,n,width,vocab", [("f32", 100, 16, 163841), ("f32", 64, 72, 200064), ("bf16", 25, 264, 327681),
+@pytest.mark.parametrize("storage,n,width,vocab", [("f32", 100, 16, 163841), ("f32", 64, 72, 200064), ("f32", 1, 768, 200064), ("bf16", 25, 264, 327681),
                                                    ("bf16", 16, 64, 400003), ("bf16", 1, 300, 262144)])
 def test_few_tokens_of_a_large_vocabulary(storage, n, width, vocab, weighted):
     """Kept logits whose P is longer than a piece of large problems would be."""
@@ -410,6 +410,39 @@ def test_vocab_loss_gradients_are_difference_quotients():
         cut = 0.7 * move**3 * eps**2 / 6
         noise = 60 * 2.0**-20 / eps
         assert abs(quotient - slope) <= cut + noise, (other, quotient, slope, cut, noise)
+
+
+def check_gradients(hidden, head, targets, weights, scale, storage):
+    factor, lse, loss, P, dh, dw, clean, live = loss_reference(hidden, head, targets, weights, scale)
+    t_loss, t_lse, t_h, t_w = loss_bounds(hidden, head, targets, factor, lse, P, clean, live, storage)
+    got = ops.vocab_loss_grad(hidden, head, targets, weights=weights, scale=scale)
+    for name, value, want, tol in zip(("loss", "lse", "grad_hidden", "grad_head"), got, (loss, lse, dh, dw), (t_loss, t_lse, t_h, t_w)):
+        assert_within(value, want, tol, name)
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+def test_small_probabilities_keep_their_digits(form):
+    """A trained model's tokens: what the vocabulary rows that no token names get is a sum of P of 2^-32 and less, to the same relative bound."""
+    g, _, hidden, head, targets = loss_case("f32", form, 7)
+    hidden = 22.0 * head[targets.long()] / head[targets.long()].square().sum(1, keepdim=True) + 0.3 * hidden
+    few = torch.randperm(len(hidden), generator=g, device=DEV)[:8]
+    on = torch.full_like(targets, -1)
+    on[few] = targets[few]
+    check_gradients(hidden, head, on, None, 1.0, "f32")
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("of", ["hidden", "head", "weights"])
+def test_a_large_row_leaves_the_others_their_digits(form, of):
+    g, _, hidden, head, targets = loss_case("f32", form, 8)
+    weights = torch.rand(len(hidden), generator=g, device=DEV) + 0.5
+    if of == "hidden":
+        hidden[7, -1], head[:, -1] = 2.0**30, 0.0
+    elif of == "head":
+        head[9, 0], hidden[:, 0] = -(2.0**30), 0.0
+    else:
+        weights[3::2] *= 2.0**-14
+    check_gradients(hidden, head, targets, weights, 1.0, "f32")
 
 
 @pytest.mark.parametrize("form", list(FORMS))
