@@ -399,7 +399,7 @@ int a2cid2_prescribe(double chi1, double chi2, int32_t accelerated, double* eta,
  *     are multiples of 16 bytes take faster accesses). Buffers of one call must not overlap
  *     unless stated otherwise.
  *   - Work is queued on cuda_stream (a cudaStream_t, NULL = default stream) and not waited for. Nothing is
- *     allocated: workspace is device memory of at least the size that the operator's _workspace call
+ *     allocated (but 256 bytes of pinned host memory at the first product of a process): workspace is device memory of at least the size that the operator's _workspace call
  *     gives for the same sizes, 256-byte aligned, used by the queued work only. Calls whose work may
  *     overlap need workspaces of their own.
  *   - Token ids and targets are int32; an id outside [0, vocab) means "no token" (padding, a masked prompt).
@@ -461,8 +461,9 @@ int a2cid2_orthogonalize(const void* in, int64_t in_stride, int64_t in_pitch, in
                          void* cuda_stream);
 
 /* Waits for the stream. The kernels of the products wait on one another's copies inside the GPU; each such wait has a limit in
- * time, after which the kernel returns with its result incomplete. A2_ECUDA if that has happened on the current device since the
- * process began, else A2_OK. */
+ * time, after which the kernel returns with its result incomplete. Every operator called after that on the same device returns
+ * A2_ECUDA and queues nothing, until this call has reported it: A2_ECUDA if it has happened on the current device since this call last
+ * said so, else A2_OK. */
 int a2cid2_operators_check(void* cuda_stream);
 
 /* Library version string. */

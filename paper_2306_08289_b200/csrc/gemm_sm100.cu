@@ -1,11 +1,11 @@
 // Host side of the tensor-core products: tensor maps, launch shape, the flag of kernels that gave up a wait.
+#include <mutex>
+
 #include "gemm_sm100.cuh"
 
 namespace a2 {
 
 namespace {
-
-__device__ int g_gave_up;
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -54,19 +54,38 @@ cudaError_t operand_maps(const Operand& o, bool bf16, int64_t mats, CUtensorMap 
 // What the launches ask of a device, looked up at its first product.
 namespace {
 constexpr int kMaxDevices = 64;
-std::atomic<int*> g_flags[kMaxDevices];
 std::atomic<int> g_clusters[kMaxDevices];
+std::mutex g_flags_mutex;
+std::atomic<int*> g_flags;  // one a device (the last one for all further), in pinned host memory that every device can write; never freed
 }  // namespace
 
 cudaError_t gave_up_flag(int** out) {
     int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    if (e != cudaSuccess) return e;
-    *out = device < kMaxDevices ? g_flags[device].load() : nullptr;
-    if (*out) return cudaSuccess;
-    e = cudaGetSymbolAddress(reinterpret_cast<void**>(out), g_gave_up);
-    if (e == cudaSuccess && device < kMaxDevices) g_flags[device].store(*out);
-    return e;
+    A2_CUDA_TRY(cudaGetDevice(&device));
+    if (!g_flags.load()) {
+        std::lock_guard<std::mutex> lock(g_flags_mutex);
+        if (!g_flags.load()) {
+            // the caller's stream may be under capture: this allocation is no part of it
+            cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+            A2_CUDA_TRY(cudaThreadExchangeStreamCaptureMode(&mode));
+            void* p = nullptr;
+            const cudaError_t e = cudaHostAlloc(&p, kMaxDevices * sizeof(int), cudaHostAllocPortable | cudaHostAllocMapped);
+            A2_CUDA_TRY(cudaThreadExchangeStreamCaptureMode(&mode));
+            if (e != cudaSuccess) return e;
+            for (int k = 0; k < kMaxDevices; ++k) static_cast<int*>(p)[k] = 0;
+            g_flags.store(static_cast<int*>(p));
+        }
+    }
+    // with unified addressing the devices know the memory by its host address
+    *out = g_flags.load() + std::min(device, kMaxDevices - 1);
+    return cudaSuccess;
+}
+
+bool products_gave_up() {
+    int device = 0;
+    const int* flags = g_flags.load();
+    if (!flags || cudaGetDevice(&device) != cudaSuccess) return false;
+    return *static_cast<const volatile int*>(flags + std::min(device, kMaxDevices - 1)) != 0;
 }
 
 int gemm_clusters() {
@@ -128,12 +147,14 @@ cudaError_t make_gemm(const Operand& a, const Operand& b, int64_t mats, bool bf1
     return cudaSuccess;
 }
 
-cudaError_t products_gave_up(cudaStream_t s, bool* out) {
-    int v = 0;
-    cudaError_t e = cudaStreamSynchronize(s);
-    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&v, g_gave_up, sizeof v);
-    *out = v != 0;
-    return e;
+cudaError_t check_products(cudaStream_t s, bool* gave_up) {
+    A2_CUDA_TRY(cudaStreamSynchronize(s));
+    *gave_up = products_gave_up();
+    if (!*gave_up) return cudaSuccess;
+    int* flag = nullptr;
+    A2_CUDA_TRY(gave_up_flag(&flag));
+    *static_cast<volatile int*>(flag) = 0;
+    return cudaSuccess;
 }
 
 }  // namespace a2

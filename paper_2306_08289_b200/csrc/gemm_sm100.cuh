@@ -24,8 +24,8 @@
 // 32,000 x 512, where reading the sums back takes the accumulators' port for 700 cycles a stay. A launch costs about 8 us beside its blocks (first
 // loads 1.6, epilogue 3 to 5, end 1.2, start of the next 1.7), which is what bounds small ones.
 //
-// Every wait has a limit in time (kWaitNs); a kernel that runs into it sets *gave_up, waits for its copies, frees its
-// tensor memory and returns.
+// Every wait has a limit in time (kWaitNs); a kernel that runs into it sets *gave_up (pinned host memory: the next call sees it without
+// waiting for the GPU), waits for its copies, frees its tensor memory and returns.
 #pragma once
 
 #include <cuda.h>
@@ -77,7 +77,7 @@ struct Operand {  // a 16-bit matrix, K-major [rows, k] or MN-major [k, rows], `
     bool symmetric = false;  // rows == k, K-major
 };
 [[nodiscard]] cudaError_t make_gemm(const Operand& a, const Operand& b, int64_t mats, bool bf16, bool lower, int flush, int splits, GemmArgs* out);
-[[nodiscard]] cudaError_t gave_up_flag(int** out);  // where kernels note a wait that ran out, on the current device
+[[nodiscard]] cudaError_t gave_up_flag(int** out);  // where kernels note a wait that ran out on the current device
 // Lets a kernel use `bytes` of dynamic shared memory on the current device; `done` remembers the devices it was asked on.
 [[nodiscard]] cudaError_t allow_large_clusters(const void* kernel, std::atomic<uint64_t>& done);  // more than 8 CTAs
 [[nodiscard]] cudaError_t allow_shared_memory(const void* kernel, int bytes, std::atomic<uint64_t>& done);
@@ -131,7 +131,8 @@ __device__ __forceinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, int
     const unsigned long long start = now_ns();
     while (!bar_try(bar, parity))
         if (now_ns() - start > kWaitNs) {
-            atomicExch(gave_up, 1);
+            *static_cast<volatile int*>(gave_up) = 1;
+            __threadfence_system();
             return false;
         }
     return true;

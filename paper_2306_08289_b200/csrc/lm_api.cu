@@ -83,8 +83,14 @@ int check_table_sizes(int64_t vocab, int64_t width, int64_t n_ids) {
     return A2_OK;
 }
 
+// A product that gave up a wait has left a result incomplete: nothing more is queued until the caller has been told.
+int check_complete() {
+    A2_CHECK(!a2::products_gave_up(), A2_ECUDA, "a product of an earlier call gave up a wait: its results are incomplete (a2cid2_operators_check)");
+    return A2_OK;
+}
+
 // The products count their tiles in 32 bits.
-int check_products(int64_t n_tokens, int64_t vocab) {
+int check_tiles(int64_t n_tokens, int64_t vocab) {
     A2_CHECK(a2::ceil_div(n_tokens, 256) * a2::ceil_div(vocab, 256) < (int64_t(1) << 30), A2_ERANGE, "n_tokens * vocab beyond 2^46");
     return A2_OK;
 }
@@ -114,6 +120,7 @@ int a2cid2_embed(const void* table, int64_t vocab, int64_t width, int64_t table_
     A2_TRY(check_matrix("table", table, vocab, width, table_pitch, storage_dtype));
     A2_TRY(check_ids("ids", ids, n_ids));
     A2_TRY(check_matrix("out", out, n_ids, width, out_pitch, storage_dtype));
+    A2_TRY(check_complete());
     const a2::EmbedArgs a{table, vocab, width, table_pitch, ids, n_ids, (float)scale, out, out_pitch, storage_dtype};
     return status(a2::run_embed(a, (cudaStream_t)cuda_stream), "embedding lookup");
 }
@@ -137,6 +144,7 @@ int a2cid2_embed_grad(const void* grad_out, int64_t grad_out_pitch, const int32_
     A2_TRY(check_ids("ids", ids, n_ids));
     A2_TRY(check_matrix("grad_table", grad_table, vocab, width, grad_table_pitch, storage_dtype));
     A2_TRY(check_workspace(workspace, workspace_bytes, a2::embed_grad_workspace(vocab, width, n_ids)));
+    A2_TRY(check_complete());
     const a2::EmbedGradArgs a{grad_out, grad_out_pitch, ids, n_ids, vocab, width, (float)scale, accumulate != 0, grad_table, grad_table_pitch,
                               storage_dtype};
     return status(a2::run_embed_grad(a, workspace, (cudaStream_t)cuda_stream), "embedding gradient");
@@ -147,7 +155,7 @@ int a2cid2_vocab_loss_workspace(int64_t n_tokens, int64_t width, int64_t vocab, 
     A2_CHECK(bytes, A2_EINVAL, "bytes is NULL");
     A2_TRY(check_type(storage_dtype));
     A2_TRY(check_table_sizes(vocab, width, n_tokens));
-    A2_TRY(check_products(n_tokens, vocab));
+    A2_TRY(check_tiles(n_tokens, vocab));
     *bytes = a2::vocab_loss_workspace(n_tokens, width, vocab, with_grad != 0, storage_dtype);
     return A2_OK;
 }
@@ -158,7 +166,7 @@ int a2cid2_vocab_loss(const void* hidden, int64_t hidden_pitch, const void* head
                       int32_t storage_dtype, void* workspace, int64_t workspace_bytes, void* cuda_stream) {
     A2_TRY(check_type(storage_dtype));
     A2_TRY(check_table_sizes(vocab, width, n_tokens));
-    A2_TRY(check_products(n_tokens, vocab));
+    A2_TRY(check_tiles(n_tokens, vocab));
     A2_TRY(check_number("scale", scale));
     A2_TRY(check_matrix("hidden", hidden, n_tokens, width, hidden_pitch, storage_dtype));
     A2_TRY(check_matrix("head", head, vocab, width, head_pitch, storage_dtype));
@@ -171,6 +179,7 @@ int a2cid2_vocab_loss(const void* hidden, int64_t hidden_pitch, const void* head
     if (grad_head) A2_TRY(check_matrix("grad_head", grad_head, vocab, width, grad_head_pitch, storage_dtype));
     const bool with_grad = grad_hidden || grad_head;
     A2_TRY(check_workspace(workspace, workspace_bytes, a2::vocab_loss_workspace(n_tokens, width, vocab, with_grad, storage_dtype)));
+    A2_TRY(check_complete());
     const a2::VocabLossArgs a{hidden, hidden_pitch, head, head_pitch, targets, n_tokens, width, vocab, weights, (float)scale, loss, lse,
                               grad_hidden, grad_hidden_pitch, grad_head, grad_head_pitch, storage_dtype};
     return status(a2::run_vocab_loss(a, workspace, (cudaStream_t)cuda_stream), "vocabulary loss");
@@ -208,6 +217,7 @@ int a2cid2_orthogonalize(const void* in, int64_t in_stride, int64_t in_pitch, in
              "in place needs the same stride and pitch on both sides");
     A2_TRY(check_workspace(workspace, workspace_bytes, a2::orthogonalize_workspace(n_mats, rows, cols, storage_dtype)));
     if (n_mats == 0) return A2_OK;
+    A2_TRY(check_complete());
     const a2::OrthogonalizeArgs args{in, in_stride, in_pitch, n_mats, rows, cols, steps, (float)a, (float)b, (float)c, eps, (float)scale, out,
                                      out_stride, out_pitch, storage_dtype};
     return status(a2::run_orthogonalize(args, workspace, (cudaStream_t)cuda_stream), "orthogonalisation");
@@ -215,8 +225,8 @@ int a2cid2_orthogonalize(const void* in, int64_t in_stride, int64_t in_pitch, in
 
 int a2cid2_operators_check(void* cuda_stream) {
     bool gave_up = false;
-    A2_TRY(status(a2::products_gave_up((cudaStream_t)cuda_stream, &gave_up), "operators check"));
-    A2_CHECK(!gave_up, A2_ECUDA, "a product gave up waiting for its operands: results since the start of the process may be incomplete");
+    A2_TRY(status(a2::check_products((cudaStream_t)cuda_stream, &gave_up), "operators check"));
+    A2_CHECK(!gave_up, A2_ECUDA, "a product gave up waiting for its operands: results since the last check may be incomplete");
     return A2_OK;
 }
 

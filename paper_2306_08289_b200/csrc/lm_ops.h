@@ -98,7 +98,9 @@ cudaError_t run_orthogonalize(const OrthogonalizeArgs& a, void* workspace, cudaS
         if (e__ != cudaSuccess) return e__;          \
     } while (0)
 
-cudaError_t products_gave_up(cudaStream_t s, bool* out);  // waits for the stream; whether a product ever gave up on this device
+// Whether a product gave up a wait on the current device since the last check that said so. Waits for nothing.
+bool products_gave_up();
+[[nodiscard]] cudaError_t check_products(cudaStream_t s, bool* gave_up);  // waits for the stream, and forgets what it reports
 
 #ifdef __CUDACC__
 __device__ __forceinline__ float widen(float v) { return v; }

@@ -177,6 +177,8 @@ def orthogonalize(mats, steps=5, coeffs=NEWTON_SCHULZ, eps=1e-7, scale=1.0, out=
 
 
 def check(stream=None):
-    """Waits for the stream (torch's current one if None) and raises `binding.A2Error` if a kernel of the products ever gave up a wait
-    on the current device."""
-    B._check(B.lib().a2cid2_operators_check((torch.cuda.current_stream() if stream is None else stream).cuda_stream))
+    """Waits for the stream (torch's current one if None) and raises `binding.A2Error` if a kernel of the products gave up a wait on its device
+    since this was last raised. Until then every operator on that device raises it too."""
+    stream = torch.cuda.current_stream() if stream is None else stream
+    with torch.cuda.device(stream.device):
+        B._check(B.lib().a2cid2_operators_check(stream.cuda_stream))

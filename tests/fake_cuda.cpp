@@ -3,11 +3,12 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <cstdlib>
 #include <string>
 
 namespace {
 int g_launches = 0, g_fail_at = -1, g_bad_maps = 0;
-int g_symbol[64];
+void* g_host = nullptr;
 std::string g_text;
 
 cudaError_t queue() { return g_launches++ == g_fail_at ? cudaErrorLaunchOutOfResources : cudaSuccess; }
@@ -51,10 +52,13 @@ cudaError_t __wrap_cudaDeviceGetAttribute(int* value, cudaDeviceAttr, int) {
     return cudaSuccess;
 }
 cudaError_t __wrap_cudaFuncSetAttribute(const void*, cudaFuncAttribute, int) { return cudaSuccess; }
-cudaError_t __wrap_cudaGetSymbolAddress(void** p, const void*) {
-    *p = g_symbol;
+cudaError_t __wrap_cudaHostAlloc(void** p, size_t bytes, unsigned int) {
+    *p = g_host = std::calloc(1, bytes);
     return cudaSuccess;
 }
+int* fake_host_memory() { return static_cast<int*>(g_host); }
+cudaError_t __wrap_cudaThreadExchangeStreamCaptureMode(cudaStreamCaptureMode*) { return cudaSuccess; }
+cudaError_t __wrap_cudaStreamSynchronize(cudaStream_t) { return cudaSuccess; }
 cudaError_t __wrap_cudaGetDriverEntryPointByVersion(const char*, void** p, unsigned int, unsigned long long, cudaDriverEntryPointQueryResult* found) {
     *p = reinterpret_cast<void*>(encode);
     *found = cudaDriverEntryPointSuccess;

@@ -3,6 +3,7 @@
 Tolerances are bounds derived from the arithmetic the header promises, written at each test: u = unit roundoff of the
 storage type (2^-24 fp32, 2^-8 bf16), sums of k terms in fp32 at most k * 2^-23 of the sum of magnitudes (each addition rounded
 or cut), operands of fp32 products kept to 22 bits."""
+import ctypes as C
 import math
 
 import pytest
@@ -621,6 +622,48 @@ def test_operators_on_another_stream():
     s.synchronize()
     assert torch.equal(y, want_y) and torch.equal(e, want_e) and torch.equal(o, want_o)
     assert all(torch.equal(a, b) for a, b in zip(l, want_l))
+
+
+def test_a_note_of_a_wait_that_ran_out_stops_the_next_call():
+    """The note lies in memory that the GPU writes and the host reads without waiting. The lookup writes it here, as a kernel that gives up would."""
+    t = torch.ones(1, 1, device=DEV)
+    ids = torch.zeros(1, dtype=torch.int32, device=DEV)
+    ops.orthogonalize(torch.ones(4, 4, device=DEV))
+    find = B.lib()._ZN2a212gave_up_flagEPPi
+    note = C.c_void_p()
+    find.argtypes = [C.POINTER(C.c_void_p)]
+    assert find(C.byref(note)) == 0
+    ops.check()
+    s = torch.cuda.current_stream().cuda_stream
+    assert B.lib().a2cid2_embed(t.data_ptr(), 1, 1, 1, ids.data_ptr(), 1, 1.0, note, 1, B.A2_F32, s) == B.A2_OK
+    torch.cuda.synchronize()
+    for call in (lambda: ops.embed(t, ids), lambda: ops.embed_grad(t, ids, 1), lambda: ops.vocab_loss(t, t, ids), lambda: ops.orthogonalize(t), ops.check):
+        with pytest.raises(B.A2Error, match="incomplete") as e:
+            call()
+        assert e.value.code == B.A2_ECUDA
+    ops.check()
+    assert float(ops.embed(t, ids)) == 1.0
+
+
+def test_operators_in_a_cuda_graph():
+    g = gen(16)
+    table = torch.randn(700, 136, generator=g, device=DEV)
+    ids = torch.randint(-1, 700, (6000,), generator=g, device=DEV, dtype=torch.int32)
+
+    def step():
+        y = ops.embed(table, ids)
+        loss, lse, gh, gw = ops.vocab_loss_grad(y, table, ids)
+        return loss, lse, gh, gw, ops.embed_grad(gh, ids, 700), ops.orthogonalize(gw)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    table.mul_(0.7)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, step()))
 
 
 def test_refusals():

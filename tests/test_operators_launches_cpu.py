@@ -11,8 +11,8 @@ from paper_2306_08289_b200 import build as build_mod
 
 SOURCES = ["lm_api.cu", "embed.cu", "gemm_sm100.cu", "vocab_loss.cu", "vocab_loss_few.cu", "orthogonalize.cu"]
 HERE = os.path.dirname(os.path.abspath(__file__))
-FAKED = ["cudaLaunchKernelExC", "cudaMemset2DAsync", "cudaGetDevice", "cudaDeviceGetAttribute", "cudaFuncSetAttribute", "cudaGetSymbolAddress",
-         "cudaGetDriverEntryPointByVersion", "cudaGetLastError"]
+FAKED = ["cudaLaunchKernelExC", "cudaMemset2DAsync", "cudaGetDevice", "cudaDeviceGetAttribute", "cudaFuncSetAttribute", "cudaHostAlloc", "cudaStreamSynchronize",
+         "cudaThreadExchangeStreamCaptureMode", "cudaGetDriverEntryPointByVersion", "cudaGetLastError"]
 
 
 @pytest.fixture(scope="module")
@@ -35,10 +35,11 @@ def fake(tmp_path_factory):
     assert r.returncode == 0, r.stdout + r.stderr
     L = C.CDLL(lib)
     for name, (restype, argtypes) in B.SIGNATURES.items():
-        if name.startswith(("a2cid2_embed", "a2cid2_vocab", "a2cid2_orthogonalize")):
+        if name.startswith(("a2cid2_embed", "a2cid2_vocab", "a2cid2_orthogonalize", "a2cid2_operators")):
             f = getattr(L, name)
             f.restype, f.argtypes = restype, argtypes
     L.fake_error_text.restype = C.c_char_p
+    L.fake_host_memory.restype = C.POINTER(C.c_int)
     return L
 
 
@@ -98,6 +99,20 @@ def test_a_call_ends_at_the_first_launch_that_fails(fake, name):
         fake.fake_reset(k)
         assert call(fake, *args) == B.A2_ECUDA, (k, launches)
         assert fake.fake_launches() == k + 1 and len(fake.fake_error_text()) > 10
+
+
+def test_a_wait_that_ran_out_is_reported_before_more_is_queued(fake):
+    fake.fake_reset(-1)
+    assert loss(fake, 333, 201, 5003, F32) == B.A2_OK and fake.a2cid2_operators_check(None) == B.A2_OK
+    fake.fake_host_memory()[0] = 1  # as a kernel that gives up does
+    fake.fake_reset(-1)
+    for call, args in CALLS.values():
+        assert call(fake, *args) == B.A2_ECUDA and b"incomplete" in fake.fake_error_text()
+    assert fake.fake_launches() == 0
+    assert fake.a2cid2_operators_check(None) == B.A2_ECUDA and b"incomplete" in fake.fake_error_text()
+    assert fake.a2cid2_operators_check(None) == B.A2_OK  # reported once
+    for call, args in CALLS.values():
+        assert call(fake, *args) == B.A2_OK
 
 
 # Launches without gradients, with grad_head, with grad_hidden, with both. Few: logits, rows; both gradients in one; join. Else fp32 rows take a scan and
