@@ -7,6 +7,9 @@ view into an engine's rows, e.g. `eng.x[w, off:off + v * h].view(v, h)` for work
 gradient, so that gradients land where the event kernels read them. Work is queued on torch's current stream of the tensors' device,
 or on `stream`; results and workspaces are allocated through torch on that stream. An argument the library cannot take raises
 `binding.A2Error`.
+
+The operators are no part of torch's autograd: gradients are calls of their own here. A tensor that requires a gradient is refused while torch
+records (call under `torch.no_grad()`, or pass it detached), for its result would have no gradient.
 """
 from __future__ import annotations
 
@@ -27,12 +30,18 @@ def _refuse(text):
     raise B.A2Error(B.A2_EINVAL, text)
 
 
+def _refuse_recorded(name, t):
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse(f"{name} requires a gradient, which these operators do not record: call under torch.no_grad() or pass {name}.detach()")
+
+
 def _matrix(name, t, like=None, shape=None, ndim=2):
     """Checks a matrix (or a batch of them) and returns its row pitch."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         _refuse(f"{name} must be a CUDA tensor")
     if t.dtype not in _DTYPES:
         _refuse(f"{name} must be float32 or bfloat16")
+    _refuse_recorded(name, t)
     if like is not None and (t.dtype != like.dtype or t.device != like.device):
         _refuse(f"{name} must have the type and device of the other matrices")
     dims, strides = t.shape, t.stride()
@@ -46,6 +55,7 @@ def _matrix(name, t, like=None, shape=None, ndim=2):
 def _vector(name, t, n, dtype, device):
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
         _refuse(f"{name} must be a contiguous {dtype} vector of {n} elements on {device}")
+    _refuse_recorded(name, t)
     return t.data_ptr()
 
 

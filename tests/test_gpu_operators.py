@@ -624,6 +624,23 @@ def test_operators_on_another_stream():
     assert all(torch.equal(a, b) for a, b in zip(l, want_l))
 
 
+def test_tensors_that_require_a_gradient_are_refused_while_torch_records():
+    t = torch.randn(10, 8, device=DEV)
+    p = t.clone().requires_grad_()
+    ids = torch.arange(10, dtype=torch.int32, device=DEV)
+    w = torch.ones(10, device=DEV, requires_grad=True)
+    calls = (lambda a, v: ops.embed(a, ids), lambda a, v: ops.embed(t, ids, out=a), lambda a, v: ops.embed_grad(a, ids, 10), lambda a, v: ops.vocab_loss(a, t, ids),
+             lambda a, v: ops.vocab_loss(t, a, ids), lambda a, v: ops.vocab_loss_grad(t, t, ids, weights=v), lambda a, v: ops.vocab_loss_grad(t, t, ids, grad_head=a),
+             lambda a, v: ops.orthogonalize(a))
+    for call in calls:
+        with pytest.raises(B.A2Error, match="requires a gradient") as e:
+            call(p, w)
+        assert e.value.code == B.A2_EINVAL
+        call(p.detach(), w.detach())
+        with torch.no_grad():
+            call(p, w)
+
+
 def test_a_note_of_a_wait_that_ran_out_stops_the_next_call():
     """The note lies in memory that the GPU writes and the host reads without waiting. The lookup writes it here, as a kernel that gives up would."""
     t = torch.ones(1, 1, device=DEV)
