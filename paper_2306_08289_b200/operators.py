@@ -60,16 +60,20 @@ def _vector(name, t, n, dtype, device):
 
 
 class _Queue:
-    """The context in which a call allocates and queues: the tensors' device and the stream. Entering it gives the raw stream."""
+    """The context in which a call allocates and queues: the tensors' device and the stream. Entering it gives the raw stream. `given` are the
+    caller's tensors (or None), `made` collects results allocated here: with a stream of the caller's, torch's allocator is told that the
+    former are used on it and that the latter are used on the caller's current one, so that neither is handed out again too early."""
 
-    __slots__ = ("device", "stream", "inner")
+    __slots__ = ("device", "stream", "given", "made", "inner")
 
-    def __init__(self, device, stream):
-        self.device, self.stream, self.inner = device, stream, None
+    def __init__(self, device, stream, *given):
+        self.device, self.stream, self.given, self.made, self.inner = device, stream, given, [], None
 
     def __enter__(self):
         if self.stream is None and torch._C._cuda_getDevice() == self.device.index:
             return torch._C._cuda_getCurrentRawStream(self.device.index)  # nothing to switch: the usual case, kept short
+        if self.stream is not None and self.stream.device != self.device:
+            _refuse(f"the stream is one of {self.stream.device}, the tensors are on {self.device}")
         self.inner = contextlib.ExitStack()
         self.inner.enter_context(torch.cuda.device(self.device))
         stream = torch.cuda.current_stream(self.device) if self.stream is None else self.stream
@@ -77,8 +81,16 @@ class _Queue:
         return stream.cuda_stream
 
     def __exit__(self, *exc):
-        if self.inner is not None:
-            return self.inner.__exit__(*exc)
+        if self.inner is None:
+            return False
+        self.inner.__exit__(*exc)
+        if self.stream is not None:
+            caller = torch.cuda.current_stream(self.device)
+            for t in self.given:
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(self.stream)
+            for t in self.made:
+                t.record_stream(caller)
         return False
 
 
@@ -103,9 +115,11 @@ def embed(table, ids, scale=1.0, out=None, stream=None):
     pitch = _matrix("table", table)
     n, (vocab, width) = ids.numel(), table.shape
     ids_p = _vector("ids", ids, n, torch.int32, table.device)
-    with _Queue(table.device, stream) as s:
+    queue = _Queue(table.device, stream, table, ids, out)
+    with queue as s:
         if out is None:
             out, out_pitch = torch.empty(n, width, dtype=table.dtype, device=table.device), width
+            queue.made.append(out)
         else:
             out_pitch = _matrix("out", out, table, (n, width))
         B._check(B.lib().a2cid2_embed(table.data_ptr(), vocab, width, pitch, ids_p, n, scale, out.data_ptr(), out_pitch,
@@ -121,9 +135,11 @@ def embed_grad(grad_out, ids, vocab, scale=1.0, out=None, accumulate=False, stre
     ids_p = _vector("ids", ids, n, torch.int32, grad_out.device)
     if accumulate and out is None:
         _refuse("accumulate needs out")
-    with _Queue(grad_out.device, stream) as s:
+    queue = _Queue(grad_out.device, stream, grad_out, ids, out)
+    with queue as s:
         if out is None:
             out = torch.empty(int(vocab), width, dtype=grad_out.dtype, device=grad_out.device)
+            queue.made.append(out)
         out_pitch = _matrix("out", out, grad_out, (int(vocab), width))
         ws, ws_p, size = _workspace(grad_out, "a2cid2_embed_grad_workspace", vocab, width, n)
         B._check(B.lib().a2cid2_embed_grad(grad_out.data_ptr(), pitch, ids_p, n, vocab, width, scale, int(accumulate), out.data_ptr(),
@@ -139,15 +155,18 @@ def _vocab_loss(hidden, head, targets, weights, scale, grad_hidden, grad_head, s
         _refuse(f"hidden has {width} columns, head {head.shape[1]}")
     targets_p = _vector("targets", targets, n, torch.int32, device)
     weights_p = None if weights is None else _vector("weights", weights, n, torch.float32, device)
-    with _Queue(device, stream) as s:
+    queue = _Queue(device, stream, hidden, head, targets, weights, grad_hidden, grad_head)
+    with queue as s:
         grads = []
         for name, g, like in (("grad_hidden", grad_hidden, hidden), ("grad_head", grad_head, head)):
             if g is True:
                 g = torch.empty(like.shape, dtype=like.dtype, device=device)
+                queue.made.append(g)
             grads += [None, None, 0] if g is None else [g, g.data_ptr(), _matrix(name, g, like, like.shape)]
         gh, gh_p, gh_pitch, gw, gw_p, gw_pitch = grads
         loss = torch.empty(n, dtype=torch.float32, device=device)
         lse = torch.empty(n, dtype=torch.float32, device=device)
+        queue.made += (loss, lse)
         dtype = _DTYPES[hidden.dtype]
         ws, ws_p, size = _workspace(hidden, "a2cid2_vocab_loss_workspace", n, width, vocab, int(gh is not None or gw is not None), dtype)
         B._check(B.lib().a2cid2_vocab_loss(hidden.data_ptr(), hidden_pitch, head.data_ptr(), head_pitch, targets_p, n, width, vocab,
@@ -175,9 +194,11 @@ def orthogonalize(mats, steps=5, coeffs=NEWTON_SCHULZ, eps=1e-7, scale=1.0, out=
         return orthogonalize(mats[None], steps, coeffs, eps, scale, None if out is None else out[None], stream)[0]
     pitch = _matrix("mats", mats, ndim=3)
     n, rows, cols = mats.shape
-    with _Queue(mats.device, stream) as s:
+    queue = _Queue(mats.device, stream, mats, out)
+    with queue as s:
         if out is None:
             out = torch.empty(mats.shape, dtype=mats.dtype, device=mats.device)
+            queue.made.append(out)
         out_pitch = _matrix("out", out, mats, mats.shape, ndim=3)
         dtype = _DTYPES[mats.dtype]
         ws, ws_p, size = _workspace(mats, "a2cid2_orthogonalize_workspace", n, rows, cols, dtype)

@@ -624,6 +624,65 @@ def test_operators_on_another_stream():
     assert all(torch.equal(a, b) for a, b in zip(l, want_l))
 
 
+def slow(stream):
+    with torch.cuda.stream(stream):
+        big = torch.ones(4096, 4096, device=DEV)
+        for _ in range(40):
+            big = big @ big * 1e-4
+
+
+def test_memory_of_a_call_on_another_stream_is_not_handed_out_too_early():
+    """Tensors that the caller drops right after a call on another stream, and results dropped while the caller's own stream still reads them."""
+    s = torch.cuda.Stream()
+    n, width, vocab = 4099, 136, 701
+    ids = torch.randint(0, vocab, (n,), device=DEV, dtype=torch.int32)
+
+    def calls():
+        t = torch.randn(vocab, width, device=DEV)
+        h = torch.randn(n, width, device=DEV)
+        w = torch.rand(n, device=DEV)
+        gh, gw, y = torch.empty_like(h), torch.empty_like(t), torch.empty_like(h)
+        yield [t, y], lambda: ops.embed(t, ids, out=y, stream=s)
+        yield [h, gw], lambda: ops.embed_grad(h, ids, vocab, out=gw, stream=s)
+        yield [h, t, w, gh, gw], lambda: ops.vocab_loss_grad(h, t, ids, weights=w, grad_hidden=gh, grad_head=gw, stream=s)
+        yield [t], lambda: ops.orthogonalize(t, stream=s)
+
+    slow(s)  # kernels, libraries and pools are set up before what is looked at
+    for _, call in calls():
+        call()
+    for which in range(4):
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        made = list(calls())[which]
+        sizes, addresses = [x.shape for x in made[0]], {x.data_ptr() for x in made[0]}
+        s.wait_stream(torch.cuda.current_stream())
+        slow(s)
+        made[1]()
+        del made
+        again = [torch.empty(size, device=DEV) for size in sizes for _ in range(3)]
+        assert not s.query(), "too little work in front of the call for this test to mean anything"
+        assert not addresses & {x.data_ptr() for x in again}, which
+    # results: the caller's stream is the slow one
+    t = torch.randn(vocab, width, device=DEV)
+    h = torch.randn(n, width, device=DEV)
+    for call in (lambda: [ops.embed(t, ids, stream=s)], lambda: [ops.embed_grad(h, ids, vocab, stream=s)], lambda: list(ops.vocab_loss_grad(h, t, ids, stream=s)),
+                 lambda: [ops.orthogonalize(t, stream=s)]):
+        torch.cuda.synchronize()
+        out = call()
+        addresses = {x.data_ptr() for x in out}
+        torch.cuda.current_stream().wait_stream(s)
+        slow(torch.cuda.current_stream())
+        for x in out:
+            x.add_(1.0)
+        del out, x
+        s.synchronize()
+        with torch.cuda.stream(s):
+            again = [torch.empty(size, device=DEV) for size in ((n,), (n,), (n, width), (vocab, width)) for _ in range(3)]
+        assert not torch.cuda.current_stream().query()
+        assert not addresses & {x.data_ptr() for x in again}
+    torch.cuda.synchronize()
+
+
 def test_tensors_that_require_a_gradient_are_refused_while_torch_records():
     t = torch.randn(10, 8, device=DEV)
     p = t.clone().requires_grad_()

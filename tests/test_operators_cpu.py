@@ -139,6 +139,19 @@ def test_the_range_of_coefficients_is_what_a_grid_search_finds():
     assert accepted > 30 and refused > 30
 
 
+def test_a_stream_of_another_device_is_refused():
+    import types
+
+    import torch
+
+    from paper_2306_08289_b200 import operators as ops
+
+    queue = ops._Queue(torch.device("cuda", 0), types.SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=0))
+    with pytest.raises(B.A2Error, match="cuda:1") as e:
+        queue.__enter__()
+    assert e.value.code == B.A2_EINVAL
+
+
 def test_markov_text():
     text = LM.MarkovText(50, 4, seed=1)
     rng = np.random.default_rng(0)
