@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import operator
 
 import torch
 
@@ -113,7 +114,7 @@ def _workspace(like, size_of, *args):
 def embed(table, ids, scale=1.0, out=None, stream=None):
     """out[t] = scale * table[ids[t]]; a row of zeros where ids[t] lies outside the table. table [vocab, width], ids int32 [n]."""
     pitch = _matrix("table", table)
-    n, (vocab, width) = ids.numel(), table.shape
+    n, (vocab, width) = ids.numel() if isinstance(ids, torch.Tensor) else 0, table.shape
     ids_p = _vector("ids", ids, n, torch.int32, table.device)
     queue = _Queue(table.device, stream, table, ids, out)
     with queue as s:
@@ -135,13 +136,17 @@ def embed_grad(grad_out, ids, vocab, scale=1.0, out=None, accumulate=False, stre
     ids_p = _vector("ids", ids, n, torch.int32, grad_out.device)
     if accumulate and out is None:
         _refuse("accumulate needs out")
+    try:
+        vocab = operator.index(vocab)
+    except TypeError:
+        _refuse("vocab must be a whole number")
     queue = _Queue(grad_out.device, stream, grad_out, ids, out)
     with queue as s:
+        ws, ws_p, size = _workspace(grad_out, "a2cid2_embed_grad_workspace", vocab, width, n)  # checks the sizes
         if out is None:
-            out = torch.empty(int(vocab), width, dtype=grad_out.dtype, device=grad_out.device)
+            out = torch.empty(vocab, width, dtype=grad_out.dtype, device=grad_out.device)
             queue.made.append(out)
-        out_pitch = _matrix("out", out, grad_out, (int(vocab), width))
-        ws, ws_p, size = _workspace(grad_out, "a2cid2_embed_grad_workspace", vocab, width, n)
+        out_pitch = _matrix("out", out, grad_out, (vocab, width))
         B._check(B.lib().a2cid2_embed_grad(grad_out.data_ptr(), pitch, ids_p, n, vocab, width, scale, int(accumulate), out.data_ptr(),
                                            out_pitch, _DTYPES[grad_out.dtype], ws_p, size, s))
     return out
@@ -162,7 +167,8 @@ def _vocab_loss(hidden, head, targets, weights, scale, grad_hidden, grad_head, s
             if g is True:
                 g = torch.empty(like.shape, dtype=like.dtype, device=device)
                 queue.made.append(g)
-            grads += [None, None, 0] if g is None else [g, g.data_ptr(), _matrix(name, g, like, like.shape)]
+            pitch = 0 if g is None else _matrix(name, g, like, like.shape)
+            grads += [g, None if g is None else g.data_ptr(), pitch]
         gh, gh_p, gh_pitch, gw, gw_p, gw_pitch = grads
         loss = torch.empty(n, dtype=torch.float32, device=device)
         lse = torch.empty(n, dtype=torch.float32, device=device)
@@ -191,8 +197,12 @@ def orthogonalize(mats, steps=5, coeffs=NEWTON_SCHULZ, eps=1e-7, scale=1.0, out=
     """Newton-Schulz orthogonalisation of a matrix [rows, cols] or a batch [mats, rows, cols] (e.g. one matrix of every worker's row:
     `eng.g[:, off:off + r * c].view(-1, r, c)`). out may be `mats` itself."""
     if isinstance(mats, torch.Tensor) and mats.dim() == 2:
+        if out is not None:
+            _matrix("out", out, mats, mats.shape)
         return orthogonalize(mats[None], steps, coeffs, eps, scale, None if out is None else out[None], stream)[0]
     pitch = _matrix("mats", mats, ndim=3)
+    if len(coeffs) != 3:
+        _refuse("coeffs are three numbers")
     n, rows, cols = mats.shape
     queue = _Queue(mats.device, stream, mats, out)
     with queue as s:

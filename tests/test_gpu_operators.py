@@ -624,6 +624,18 @@ def test_operators_on_another_stream():
     assert all(torch.equal(a, b) for a, b in zip(l, want_l))
 
 
+def test_refusals_of_arguments_of_another_kind():
+    t = torch.randn(10, 8, device=DEV)
+    ids = torch.zeros(10, dtype=torch.int32, device=DEV)
+    for call, code in ((lambda: ops.embed(t, [0, 1]), B.A2_EINVAL), (lambda: ops.embed(t, None), B.A2_EINVAL), (lambda: ops.embed_grad(t, ids, -1), B.A2_EINVAL),
+                       (lambda: ops.embed_grad(t, ids, 10.5), B.A2_EINVAL), (lambda: ops.embed_grad(t, ids, 1 << 40), B.A2_ERANGE),
+                       (lambda: ops.vocab_loss_grad(t, t, ids, grad_head=False), B.A2_EINVAL), (lambda: ops.orthogonalize(t, coeffs=(1.0, -0.5)), B.A2_EINVAL),
+                       (lambda: ops.orthogonalize(t, out=t.tolist()), B.A2_EINVAL), (lambda: ops.orthogonalize(t, out=t[None]), B.A2_EINVAL)):
+        with pytest.raises(B.A2Error) as e:
+            call()
+        assert e.value.code == code, str(e.value)
+
+
 def slow(stream):
     with torch.cuda.stream(stream):
         big = torch.ones(4096, 4096, device=DEV)
