@@ -22,8 +22,8 @@ bool aligned16(const void* p, int64_t pitch, int64_t elem) {
 
 // ---------------------------------------------------------------------------------------------
 // Lookup. Bound by memory: a token's row is read once and written once. A group of threads owns kRows
-// tokens, so that every thread has that many loads of 16 bytes in flight. 65,536 ids of 50,003 x 1,024 fp32: 57 us, 6.0 TB/s of what
-// crosses DRAM (frequent rows are read from L2).
+// tokens, so that every thread has that many loads of 16 bytes in flight. 65,536 ids of 50,003 x 1,024 fp32: 56 us, in which 87 MB are read
+// from DRAM and 209 MB written to it (5.3 TB/s): frequent rows are read from L2, and 60 MB of the writes are still there at the end.
 // ---------------------------------------------------------------------------------------------
 constexpr int kRows = 4;
 
@@ -449,9 +449,12 @@ int columns_a_thread(const EmbedGradArgs& a) {
     constexpr int kVec = 16 / sizeof(T);
     return a.width % kVec == 0 && aligned16(a.grad_out, a.grad_out_pitch, sizeof(T)) && aligned16(a.grad_table, a.grad_table_pitch, sizeof(T)) ? kVec : 1;
 }
-// bf16 rows, us, direct / sorted: 500 ids of 32,000 x 512 14 / 33; 2,000 ids 27 / 31; 4,096 ids with the frequencies of text, the
-// most frequent in 4 % of the places, 22 / 34, but with one in 18 % of them, as a small vocabulary has, 50 / 38: its warp adds its rows
-// up alone. 4,096 ids of 8,000 x 2,048 (more comparisons than allowed) 72 / 50.
+// The two forms cross at 4,000 to 5,000 positions, where no id holds many of them; us, direct / sorted, 512 columns, ids spread over 32,000
+// rows, the same with one id in 4 % and in 18 % of the places:
+//   bf16  2,000 12 / 32, 13 / 31, 26 / 32; 4,096 23 / 28, 23 / 30, 48 / 38; 5,000 29 / 29, 29 / 32, 54 / 42; 8,192 59 / 32, 59 / 36, 90 / 53
+//   fp32  2,000 20 / 33, 20 / 34, 28 / 35; 4,096 39 / 36, 39 / 37, 52 / 42; 5,000 51 / 36, 50 / 38, 70 / 44; 8,192 101 / 37, 99 / 40, 126 / 52
+// An id in 18 % of the places is what a small vocabulary has: its warp adds its rows up alone, so there half as many positions go without a
+// sort. 4,096 ids of 8,000 x 2,048 (more comparisons than allowed) 72 / 50.
 bool is_direct(int64_t n_ids, int64_t vocab, int64_t width, int vec) {
     const int64_t most = vocab >= 4 * n_ids ? kDirectMost : kDirectMost / 2;
     return n_ids <= most && n_ids * n_ids * ceil_div(width, 32 * vec) <= kDirectSearch;

@@ -322,8 +322,8 @@ struct UpdateEpi {
 
 // ---- layout and launches ---------------------------------------------------------------------------
 constexpr int64_t kPairs = 74, kLeastBlocks = 6;  // pairs of CTAs; fewest blocks of K worth a part (of three passes; four times that of one)
-// K blocks a sum stays in tensor memory with fp32 rows: 8 steps of the tensor core. 16 x 1,001 x 512: 470 us and 2.5e-6 from the 64-bit
-// result (a plain fp32 form is 2.4e-6 from it); with 4 blocks 455 us and 4.6e-6, with 8 448 us and 6.1e-6.
+// K blocks a sum stays in tensor memory with fp32 rows: 8 steps of the tensor core. 16 x 1,001 x 512: 475 us and 2.5e-6 from the 64-bit
+// result (a plain fp32 form is 2.4e-6 from it); with 4 blocks 459 us and 4.6e-6, with 8 452 us and 8.6e-6.
 constexpr int kFlush = 2;
 
 struct Layout {
@@ -413,8 +413,10 @@ cudaError_t typed(const OrthogonalizeArgs& a, Layout l, cudaStream_t s) {
 // tensor memory. X is kept [m, 256] in 64-column blocks of 128-byte swizzled rows, which the tensor core reads K-major for X X^T and
 // MN-major for B X. Every CTA makes its columns' part of A = X X^T; the parts are added up in CTA order, a share of the rows by each
 // CTA, and every CTA takes the whole of A from the shares and forms B by itself. Bound by that chain: three products, their
-// epilogues and two exchanges a step. Five steps, fp32, this form / the products below: 16 x 64 x 64 29 / 154 us; 3 x 21 x 2,579 54 / 195; 14 x
-// 3,802 x 42 159 / 291; 8 x 282 x 97 98 / 211.
+// epilogues and two exchanges a step. Five steps, fp32, us, this form / the products above: 16 x 64 x 64 30 / 149; 512 x 64 x 64 116 / 600; 3 x 21 x
+// 2,579 54 / 192; 14 x 3,802 x 42 164 / 295; 8 x 282 x 97 97 / 209; 64 x 100 x 1,000 213 / 417; 16 x 128 x 4,096 382 / 484; 64 x 128 x 4,096 1,326 /
+// 1,240: only many matrices of the widest kind, which fill the GPU either way, would be a little faster above. Its errors: 16 x 64 x 64 1.4e-6,
+// where a plain fp32 form has 1.1e-6 (sums are not promoted: K is 256 columns a CTA, added up in registers).
 constexpr int kNarrowM = 128, kNarrowN = 256, kNarrowCtas = 16;
 constexpr int kNarrowThreads = 256;
 constexpr int kBlockBytes = kNarrowM * 128;  // 128 rows of 64 fp16 columns

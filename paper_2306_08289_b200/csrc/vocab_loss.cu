@@ -18,8 +18,8 @@ namespace {
 constexpr int kPScale = 14;  // P / max |P| <= 1 is held at this power of two with fp32 rows
 
 // Largest finite magnitudes, as bits of non-negative floats (their order is that of the bits): of a CTA of k_scan, or of all.
-struct Scan {
-    uint32_t hidden, head, weight, unused;  // hidden: of the tokens with a target
+struct alignas(16) Scan {
+    uint32_t hidden, head, weight;  // hidden: of the tokens with a target
 };
 constexpr int kScanCtas = 148, kScanThreads = 1024;
 
@@ -466,9 +466,11 @@ struct Layout {
 constexpr int64_t kPieceBytes = 160ll << 20;
 constexpr int64_t kPairs = 74;
 // Few logits (64 MB as floats, half of that with bf16 rows, whose products cost a third) are kept: P then costs a pass over them and not
-// another product. Loss and gradients, us, kept / made again: fp32 rows, tokens x vocabulary x width: 333 x 5,003 x 201 71 / 97; 2,000 x 4,000 x
-// 512 139 / 179; 1,000 x 16,000 x 1,024 375 / 426; 200 x 60,000 x 80 199 / 192. bf16: 333 x 5,003 x 201 47 / 58; 2,000 x 4,000 x 512 78 / 92;
-// 128 x 50,000 x 512 149 / 143; 1,024 x 10,000 x 768 120 / 116; 200 x 60,000 x 80 127 / 102. (Part of the gain is the gradients' common launch.)
+// another product. Loss and gradients, us, kept / made again, tokens x vocabulary x width. fp32 rows: 333 x 5,003 x 201 76 / 87; 2,000 x 4,000 x
+// 512 137 / 162; 1,000 x 16,000 x 1,024 387 / 449; 200 x 60,000 x 80 211 / 212; 1 x 200,064 x 768 1,178 / 1,432; 64 x 200,064 x 512 881 / 1,010;
+// 64 x 262,144 x 2,048 4,042 / 4,808. bf16: 333 x 5,003 x 201 47 / 47; 2,000 x 4,000 x 512 78 / 74; 128 x 50,000 x 512 147 / 140; 200 x 40,000 x 80
+// 99 / 82; 1 x 262,144 x 768 612 / 703; 16 x 400,003 x 768 923 / 1,026; 25 x 327,681 x 2,048 1,772 / 2,037: with bf16 rows it pays for few tokens
+// against a large vocabulary, where a product pads them to 256, and costs up to a fifth where width is small against that.
 // A vocabulary of a few tiles would leave the pass mostly launch.
 constexpr int64_t kKeepLogits = int64_t(1) << 24, kKeepVocab = 512;
 constexpr int64_t kLeastBlocks = 8;  // of K in a part: less would leave its tile mostly epilogue
