@@ -421,6 +421,20 @@ def check_gradients(hidden, head, targets, weights, scale, storage):
         assert_within(value, want, tol, name)
 
 
+@pytest.mark.parametrize("vocab", [1, 3])
+def test_long_rows_of_small_losses_are_summed_in_parts(vocab):
+    """fp32 rows without tensor cores: 65,536 equal terms, where one chain of additions rounds each to the size of the whole sum. Parts of 128 leave chains
+    of 128 and of 512 additions, each good to 2^-24 of the sum."""
+    width = 65536
+    for h in (0.1, 0.37, 0.713, 1.9):
+        hidden = torch.full((2, width), h, device=DEV)
+        head = torch.full((vocab, width), 0.1 / 1280, device=DEV) * (1 + torch.arange(vocab, device=DEV)[:, None] / 7)
+        lse = ops.vocab_loss(hidden, head, torch.zeros(2, dtype=torch.int32, device=DEV))[1]
+        z = hidden.double() @ head.double().T
+        tol = (128 + width / 128 + 8) * 2.0**-24 * z.amax() + 2.0**-21
+        assert ((lse.double() - torch.logsumexp(z, 1)).abs() <= tol).all()
+
+
 @pytest.mark.parametrize("form", list(FORMS))
 def test_small_probabilities_keep_their_digits(form):
     """A trained model's tokens: what the vocabulary rows that no token names get is a sum of P of 2^-32 and less, to the same relative bound."""
