@@ -322,9 +322,13 @@ struct UpdateEpi {
 
 // ---- layout and launches ---------------------------------------------------------------------------
 constexpr int64_t kPairs = 74, kLeastBlocks = 6;  // pairs of CTAs; fewest blocks of K worth a part (of three passes; four times that of one)
-// K blocks a sum stays in tensor memory with fp32 rows: 8 steps of the tensor core. 16 x 1,001 x 512: 475 us and 2.5e-6 from the 64-bit
-// result (a plain fp32 form is 2.4e-6 from it); with 4 blocks 459 us and 4.6e-6, with 8 452 us and 8.6e-6.
-constexpr int kFlush = 2;
+// K blocks a sum stays in tensor memory with fp32 rows, in the products of A, A^2 and B X. What A^2's sums lose goes into every singular value and is what
+// the result's error follows; A's hardly show. 16 x 1,001 x 512, us, and 80 to 120 matrices of 129 to 1,200 a side, how many are over 1.5 times as far
+// from 64 bits as a plain fp32 form and the median of that ratio: stays of 2, 2, 2 477 us, 47 of 80, 1.61; 1, 2, 2 494, 48 of 80, 1.64; 2, 1, 2 490, 1 of 80,
+// 1.07; 4, 1, 2 483, 1 of 120, 1.05; 4, 1, 1 497, none, 0.96; 8, 1, 1 495, none, 1.17. The worst ratios are those of m up to 256, where a block more or
+// less of B X costs little: one block there.
+constexpr int kFlushGram = 4, kFlushPoly = 1, kFlushUpdate = 2;
+int update_flush(int64_t m) { return m <= kTileM ? 1 : kFlushUpdate; }
 
 struct Layout {
     double* partial;
@@ -364,7 +368,7 @@ int64_t layout(int64_t mats, int64_t rows, int64_t cols, int32_t dtype, void* ws
 template <class T>
 cudaError_t typed(const OrthogonalizeArgs& a, Layout l, cudaStream_t s) {
     constexpr bool kWords = sizeof(T) == 4;
-    const int flush = kWords ? kFlush : 0;
+    auto flush = [](int blocks) { return kWords ? blocks : 0; };
     const bool tall = a.rows > a.cols;
     const int64_t m = std::min(a.rows, a.cols), n = std::max(a.rows, a.cols);
     const dim3 grid((unsigned)l.parts, (unsigned)a.n_mats);
@@ -383,12 +387,12 @@ cudaError_t typed(const OrthogonalizeArgs& a, Layout l, cudaStream_t s) {
     gram.symmetric = b.symmetric = true;
     const Words x[2] = {l.x, l.y};
     GemmArgs make_gram[2], make_poly, update[2];
-    A2_CUDA_TRY(make_gemm(gram, gram, a.n_mats, false, true, flush, 1, &make_poly));
+    A2_CUDA_TRY(make_gemm(gram, gram, a.n_mats, false, true, flush(kFlushPoly), 1, &make_poly));
     for (int k = 0; k < 2 && k < a.steps; ++k) {
         const Operand side = operand(x[k], m, n, tall);
-        A2_CUDA_TRY(make_gemm(side, side, a.n_mats, false, true, flush, l.gram_parts, &make_gram[k]));
-        A2_CUDA_TRY(tall ? make_gemm(operand(x[k], a.rows, m, false), b, a.n_mats, false, false, flush, 1, &update[k])
-                     : make_gemm(b, operand(x[k], n, m, true), a.n_mats, false, false, flush, 1, &update[k]));
+        A2_CUDA_TRY(make_gemm(side, side, a.n_mats, false, true, flush(kFlushGram), l.gram_parts, &make_gram[k]));
+        A2_CUDA_TRY(tall ? make_gemm(operand(x[k], a.rows, m, false), b, a.n_mats, false, false, flush(update_flush(m)), 1, &update[k])
+                         : make_gemm(b, operand(x[k], n, m, true), a.n_mats, false, false, flush(update_flush(m)), 1, &update[k]));
     }
     const int64_t part_stride = a.n_mats * l.gram.stride;
     for (int step = 0; step < a.steps; ++step) {

@@ -588,6 +588,27 @@ def test_orthogonalize_special_values(storage, rows, cols):
     check_orthogonalize((u @ v)[None].to(dt), ops.orthogonalize((u @ v)[None].to(dt)), storage)
 
 
+@pytest.mark.parametrize("mats,rows,cols", [(1, 152, 890), (5, 130, 348), (3, 246, 135), (2, 371, 136), (2, 1001, 512)])
+def test_orthogonalize_is_as_exact_as_fp32_up_to_the_words(mats, rows, cols):
+    """fp32 rows, matrices like momenta (a few common directions over noise): two words an operand have twice fp32's unit roundoff, so the error may be twice
+    that of the same products in fp32."""
+    g = gen(rows)
+    r = min(rows, cols) // 8
+    x = torch.randn(mats, rows, r, generator=g, device=DEV) @ torch.randn(mats, r, cols, generator=g, device=DEV) / math.sqrt(r)
+    x = x + torch.randn(mats, rows, cols, generator=g, device=DEV)
+    want = newton_schulz(x, 5, ops.NEWTON_SCHULZ, 1e-7)
+    y = x.transpose(1, 2) if rows > cols else x
+    y = y / (torch.linalg.matrix_norm(y, keepdim=True) + 1e-7)
+    a, b, c = ops.NEWTON_SCHULZ
+    for _ in range(5):
+        s = y @ y.transpose(1, 2)
+        y = a * y + (b * s + c * (s @ s)) @ y
+    y = y.transpose(1, 2) if rows > cols else y
+    plain = float((y.double() - want).norm() / want.norm())
+    err = float((ops.orthogonalize(x).double() - want).norm() / want.norm())
+    assert err <= 2.0 * plain, (err, plain)
+
+
 @pytest.mark.parametrize("storage", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,cols", [(40, 40), (70, 900), (300, 200)])
 @pytest.mark.parametrize("steps", [0, 1, 5])
