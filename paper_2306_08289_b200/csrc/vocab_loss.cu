@@ -446,8 +446,14 @@ __global__ void __launch_bounds__(256) k_join_parts(const float* __restrict__ ke
 }
 
 // ---- layout and launches ------------------------------------------------------------------------
-// K blocks a promoted sum stays in tensor memory: 16 steps of the tensor core with fp32 rows, 64 for the loss of bf16 rows
-constexpr int kFlush = 4, kFlushLoss = 16;
+// K blocks a promoted sum stays in tensor memory: 16 steps of the tensor core with fp32 rows, for the loss of bf16 rows 32, or 16 where
+// reading the sums back more often costs little: all tiles have a pair of CTAs at once, or one tile holds all tokens and reading the head
+// bounds the product. The loss of bf16 rows, stays of 16 / 8 / 4 blocks: us and the error (root mean square over the tokens, of loss and
+// lse) as a multiple of a plain fp32 form's: 4,096 x 50,003 x 1,024 316 (2.8, 3.0) / 332 (1.4, 1.8) / 341 (0.7, 1.3); 256 x 50,003 x 1,024
+// 35.1 (2.7, 3.1) / 37.6 (1.2, 1.9) / 37.8 (0.7, 1.4); 64 x 20,000 x 768 22.8 (2.7, 2.6) / 24.1 (1.7, 2.1) / 21.7 (1.1, 1.2); 2,000 x 5,003
+// x 1,024 30.1 (2.9, 3.5) / 31.5 (1.4, 1.9) / 32.8 (0.7, 1.2); 2,000 x 356 x 1,753 28.8 (1.7, 2.4) / 28.6 (0.9, 1.2) / 28.1 (0.5, 0.6); 300
+// x 300 x 512, the product alone, 12.2 (1.9, 3.1) / 12.2 / 13.0 (0.9, 1.7).
+constexpr int kFlush = 4, kFlushLoss = 8, kFlushLossFewTiles = 4;
 
 struct Layout {
     Scan *scan, *scan_parts;
@@ -572,7 +578,9 @@ cudaError_t typed(const VocabLossArgs& a, Layout l, cudaStream_t s) {
 
     GemmArgs g;
     // the loss is fp32 with either storage type, so its sums are promoted with both
-    A2_CUDA_TRY(make_gemm(hidden(false), head(0, a.vocab, false), 1, !kWords, false, kWords ? kFlush : kFlushLoss, 1, &g));
+    const int64_t tiles_m = ceil_div(n, kTileM), tiles = tiles_m * ceil_div(a.vocab, kTileN);
+    const int flush_loss = kWords ? kFlush : tiles_m == 1 || tiles <= kPairs ? kFlushLossFewTiles : kFlushLoss;
+    A2_CUDA_TRY(make_gemm(hidden(false), head(0, a.vocab, false), 1, !kWords, false, flush_loss, 1, &g));
     const int parts = (int)(2 * ceil_div(a.vocab, kTileN));
     auto statistics = [&](auto keep) {
         using Epi = StatisticsEpi<kWords, decltype(keep)::value>;

@@ -435,6 +435,27 @@ def test_long_rows_of_small_losses_are_summed_in_parts(vocab):
         assert ((lse.double() - torch.logsumexp(z, 1)).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("n,width,vocab", [(2000, 1753, 356), (2000, 1024, 5003), (300, 512, 300), (256, 1024, 50003), (2500, 768, 9000), (64, 768, 20000)])
+def test_the_bf16_loss_is_as_exact_as_fp32(n, width, vocab):
+    """Products of bf16 values are exact in fp32, so loss and lse of bf16 rows may be as far from 64 bits as twice what the same logits in fp32 leave (root
+    mean square over the tokens; hidden states that lean towards their target, as in training)."""
+    g = gen(width)
+    head = (torch.randn(vocab, width, generator=g, device=DEV) / math.sqrt(width)).bfloat16()
+    targets = torch.randint(0, vocab, (n,), generator=g, device=DEV, dtype=torch.int32)
+    lean = 8.0 * torch.rand(n, 1, generator=g, device=DEV)
+    hidden = (torch.randn(n, width, generator=g, device=DEV) + lean * head[targets.long()].float()).bfloat16()
+    got = ops.vocab_loss(hidden, head, targets)
+
+    def form(h, w):
+        z = h @ w.T
+        lse = torch.logsumexp(z, 1)
+        return lse - z.gather(1, targets.long()[:, None])[:, 0], lse
+
+    for name, here, plain, want in zip(("loss", "lse"), got, form(hidden.float(), head.float()), form(hidden.double(), head.double())):
+        err, may = (float((x.double() - want).square().mean().sqrt()) for x in (here, plain))
+        assert err <= 2.0 * may, (name, err, may)
+
+
 @pytest.mark.parametrize("form", list(FORMS))
 def test_small_probabilities_keep_their_digits(form):
     """A trained model's tokens: what the vocabulary rows that no token names get is a sum of P of 2^-32 and less, to the same relative bound."""
