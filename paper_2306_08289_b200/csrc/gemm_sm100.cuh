@@ -20,7 +20,7 @@
 // of the small terms, 2^-11 of the others, make one stay). Products of two words are always promoted.
 //
 // What bounds it, measured: a block of 64 along K takes 610 cycles (560 with the loads left out): the tensor core. Launch by launch (no power cap)
-// the products of the loss of 8,192 x 65,536 x 2,048 bf16 run at 1.41 PFLOP/s (statistics), 1.29 (P, which is written), 1.38 (head's gradient) and
+// the products of the loss of 8,192 x 65,536 x 2,048 bf16 run at 1.41 PFLOP/s (statistics, in stays of 16 blocks), 1.29 (P, which is written), 1.38 (head's gradient) and
 // 1.22 (hidden's, added to kept sums); the call as a whole, eight of T V H, at 1.13 to 1.15 under the cap. Three-pass products: 1.1 PFLOP/s at
 // 2,048 x 32,000 x 512, where reading the sums back takes the accumulators' port for 700 cycles a stay. A launch costs about 8 us beside its blocks (first
 // loads 1.6, epilogue 3 to 5, end 1.2, start of the next 1.7), which is what bounds small ones.

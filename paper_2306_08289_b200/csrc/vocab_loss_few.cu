@@ -258,7 +258,7 @@ cudaError_t typed(const VocabLossArgs& a, const Layout& l, cudaStream_t s) {
 }  // namespace
 
 // Where this form is the faster one, by T V H and the head's size, gradients included (measured, us, this form / tensor cores):
-// fp32 rows, T V H = 2^25 8 x 8,000 x 512: 84 / 98; 2^25.4 300 x 500 x 300: 48 / 89; 2^27 64 x 16,000 x 128: 78 / 86; 2^28 128 x 4,000 x
+// fp32 rows, T V H = 2^25 8 x 8,000 x 512: 82 / 98; 2^25.4 300 x 500 x 300: 45 / 89; 2^27 64 x 16,000 x 128: 79 / 86; 2^28 128 x 4,000 x
 // 512: 122 / 99. bf16 rows need no words there, so less is gained: 2^22 32 x 1,000 x 128: 33 / 49; 2^24.6 100 x 1,000 x 256: 52 / 54; 2^25.4
 // 300 x 500 x 300: 72 / 55; a large head is read faster by the copies of that form: 2^24 1 x 32,000 x 512: 304 / 101; and a wide row is a
 // long chain of steps of 32 columns here, 2 us each: 2^21 64 x 64 x 512: 54 / 40.
