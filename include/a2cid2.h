@@ -389,8 +389,9 @@ int a2cid2_prescribe(double chi1, double chi2, int32_t accelerated, double* eta,
  *
  * The engine applies gradients that the user's model writes into rows of the gradient buffer. When the
  * rows are the parameters of a language model, these calls make such a row: the embedding lookup and
- * its gradient, the loss over the vocabulary with its gradients, and the orthogonalisation of a
- * matrix's gradient or momentum for all workers at once. They need no handle.
+ * its gradient, the loss over the vocabulary with its gradients, the orthogonalisation of a
+ * matrix's gradient or momentum for all workers at once, the root-mean-square norm and the routing to experts with their
+ * gradients, and the clipping of a gradient by its norm. They need no handle.
  *
  *   - All buffers are device memory of the current device, of the storage type (A2_F32 or A2_BF16;
  *     sums, softmax statistics and norms are held in fp32 or more) unless stated otherwise. A matrix is
@@ -459,6 +460,90 @@ int a2cid2_orthogonalize(const void* in, int64_t in_stride, int64_t in_pitch, in
                          int32_t steps, double a, double b, double c, double eps, double scale, void* out, int64_t out_stride,
                          int64_t out_pitch, int32_t storage_dtype, void* workspace, int64_t workspace_bytes,
                          void* cuda_stream);
+
+/* Root-mean-square norm of every row of s = x + residual (s = x where residual is NULL):
+ *   out = s / sqrt(mean over the row of s^2 + eps) * weight        (weight [width], NULL for ones)
+ * and, where sum is not NULL, sum = s in the storage type (the residual stream of the next layer). out is formed from s before that
+ * rounding. x, residual, sum, out [n, width], width <= 32768 (A2_ERANGE beyond). out may be x or residual, sum may be x or residual (each with the same
+ * pitch), but not both the same. eps >= 0; with eps = 0 a row of zeros gives zeros. A row whose elements' squares leave the range of fp32 is
+ * scaled first. A row that holds a NaN or an infinity has NaN in its results, the other rows do not. n = 0 does nothing. */
+int a2cid2_rms_norm(const void* x, int64_t x_pitch, const void* residual, int64_t residual_pitch, const void* weight, int64_t n,
+                    int64_t width, double eps, void* sum, int64_t sum_pitch, void* out, int64_t out_pitch, int32_t storage_dtype,
+                    void* cuda_stream);
+
+/* The same with the result in 8 bits (e4m3: 4 exponent and 3 mantissa bits, largest value 448): for every `block` columns of a row (32, 64 or 128;
+ * 0: the whole row; the last block of a row may be shorter) scale = max(largest magnitude / 448, 2^-126) and values = result / scale,
+ * rounded to nearest even. values [n, width] bytes with a pitch in bytes, scales float [n, blocks] without gaps. NaN stays NaN. values overlaps
+ * no other buffer. */
+int a2cid2_rms_norm_e4m3(const void* x, int64_t x_pitch, const void* residual, int64_t residual_pitch, const void* weight, int64_t n,
+                         int64_t width, double eps, void* sum, int64_t sum_pitch, int64_t block, void* values, int64_t values_pitch,
+                         float* scales, int32_t storage_dtype, void* cuda_stream);
+
+/* out = values * scales, rounded once to the storage type: reads back what the call above has written. */
+int a2cid2_dequantize_e4m3(const void* values, int64_t values_pitch, const float* scales, int64_t n, int64_t width, int64_t block,
+                           void* out, int64_t out_pitch, int32_t storage_dtype, void* cuda_stream);
+
+int a2cid2_rms_norm_grad_workspace(int64_t n, int64_t width, int32_t with_weight, int32_t storage_dtype, int64_t* bytes);
+
+/* The gradients of the norm for its rows x (the stored sum, where there was a residual): with r = 1 / sqrt(mean x^2 + eps), h = x r,
+ * c = mean over the row of h * weight * grad_out,
+ *   grad_x = r (weight * grad_out - c h) + grad_sum,     grad_weight = sum over rows of grad_out * h.
+ * grad_sum [n, width] (NULL for zeros) is the gradient that reaches the sum by its other use; grad_x is then the gradient of both x and the
+ * residual. grad_x may be grad_out, grad_sum or x with the same pitch. grad_x or grad_weight [width] may be NULL. with_weight of the workspace's size: whether grad_weight is asked
+ * for. n = 0 zeroes grad_weight. */
+int a2cid2_rms_norm_grad(const void* grad_out, int64_t grad_out_pitch, const void* x, int64_t x_pitch, const void* weight,
+                         const void* grad_sum, int64_t grad_sum_pitch, int64_t n, int64_t width, double eps, void* grad_x,
+                         int64_t grad_x_pitch, void* grad_weight, int32_t storage_dtype, void* workspace, int64_t workspace_bytes,
+                         void* cuda_stream);
+
+enum { A2_SCORE_SOFTMAX = 0, A2_SCORE_SIGMOID = 1 };
+enum { A2_GROUP_BEST = 0, A2_GROUP_TWO_BEST = 1 };
+
+/* Routing of tokens to experts. logits [n, n_experts]; s = softmax over a token's experts, or sigmoid of each; key = s + bias (bias float [n_experts], for the
+ * balance of the experts: it takes part in the choice alone), or the logit itself without a bias. The experts lie in `groups` groups of
+ * equal size, one after the other; the `top_groups` groups of the best score are open (score: the best key of a group, or the sum
+ * of its two best, where without a bias keys are s; the lowest group first where scores are equal).
+ *   ids[t][j], j < k:  the open experts of the k best keys, best first, the lowest expert first where keys are equal;
+ *   weights[t][j] = scale * s of that expert, with renormalize divided by the sum of the chosen ones' s;
+ *   counts[e] = tokens that have chosen e (int32 [n_experts], or NULL).
+ * ids int32 and weights float, [n, k] without gaps. The choice is that of keys in 64 bits (rows that fp32 cannot decide are chosen again). An expert whose logit is
+ * NaN, -inf or the lowest value of the storage type, or whose bias is NaN or -inf, is not available: where fewer than k are, ids are -1 and weights 0. Logits of +inf
+ * count as the largest float. n_experts <= 1024, k <= 32, groups <= 32 (A2_ERANGE beyond), k at most the experts of the open groups. n = 0 zeroes
+ * counts. */
+int a2cid2_route(const void* logits, int64_t logits_pitch, int64_t n, int64_t n_experts, int64_t k, int32_t score, const float* bias,
+                 int64_t groups, int64_t top_groups, int32_t group_score, int32_t renormalize, double scale, int32_t* ids, float* weights,
+                 int32_t* counts, int32_t storage_dtype, void* cuda_stream);
+
+/* The gradient of sum over t, j of grad_weights[t][j] * weights[t][j] for the logits, the choice held fixed: grad_logits [n, n_experts], zeros where
+ * there is none. Positions whose id is outside [0, n_experts), or whose expert is not available by its logit, have no part in it and
+ * their grad_weights do not matter. An id that a token has twice counts twice. grad_logits may be logits with the same pitch. */
+int a2cid2_route_grad(const void* logits, int64_t logits_pitch, const int32_t* ids, const float* grad_weights, int64_t n, int64_t n_experts,
+                      int64_t k, int32_t score, int32_t renormalize, double scale, void* grad_logits, int64_t grad_logits_pitch,
+                      int32_t storage_dtype, void* cuda_stream);
+
+/* A tensor of a gradient, for every worker: `rows` rows of `cols` elements, `pitch` elements apart; worker w's begin w * worker_stride elements
+ * after the first worker's. out is where the clipped ones go; it may be in, with the same pitch and stride. in and out are device memory, the struct is host memory. */
+typedef struct {
+    const void* in;
+    void* out;
+    int64_t worker_stride, out_worker_stride;
+    int64_t rows, cols, pitch, out_pitch;
+    int64_t storage_dtype; /* of this tensor */
+} a2cid2_gradient_t;
+
+int a2cid2_clip_gradients_workspace(int64_t n_tensors, int64_t workers, int64_t* bytes);
+
+/* norms[w] (float [workers], device) = the square root of the sum of squares of all elements of worker w's part of all tensors. One gradient that is
+ * spread over tensors has workers = 1. Squares neither overflow nor vanish (sums are held in 64 bits); elements are counted as often as tensors hold them.
+ * out of the tensors is not used. n_tensors <= 65536, workers <= 65535 (A2_ERANGE beyond). */
+int a2cid2_gradient_norms(const a2cid2_gradient_t* tensors, int64_t n_tensors, int64_t workers, float* norms, void* workspace,
+                          int64_t workspace_bytes, void* cuda_stream);
+
+/* The norms, and out = in * min(1, max_norm / norm) for every worker by its norm (max_norm >= 0, may be infinite). Where a norm is not finite, because an
+ * element is not, the worker's elements are left as they are, or with zero_nonfinite become zeros, so that the event that applies them brings nothing that is not
+ * finite to the other workers. No element of any out may belong to another tensor of the call. */
+int a2cid2_clip_gradients(const a2cid2_gradient_t* tensors, int64_t n_tensors, int64_t workers, double max_norm, int32_t zero_nonfinite,
+                          float* norms, void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
 /* Waits for the stream. The kernels of the products wait on one another's copies inside the GPU; each such wait has a limit in
  * time, after which the kernel returns with its result incomplete. Every operator called after that on the same device returns

@@ -27,6 +27,8 @@ A2_OP_GRAD_D, A2_OP_COMM_AD, A2_OP_COMM_BD, A2_OP_COMM_CD = 7, 8, 9, 10
 A2_MSG_AFTER_MIX, A2_MSG_BEFORE_MIX, A2_NO_MOMENTUM = 0, 1, 2
 A2_LAUNCH_AUTO, A2_LAUNCH_PER_BATCH, A2_LAUNCH_COLUMN_SLICES = 0, 1, 2
 A2_ROUND_PER_EVENT, A2_ROUND_PER_STORE = 0, 1
+A2_SCORE_SOFTMAX, A2_SCORE_SIGMOID = 0, 1
+A2_GROUP_BEST, A2_GROUP_TWO_BEST = 0, 1
 
 ERROR_NAMES = {A2_EINVAL: "A2_EINVAL", A2_EORDER: "A2_EORDER", A2_ERANGE: "A2_ERANGE", A2_ENOMEM: "A2_ENOMEM",
                A2_ECUDA: "A2_ECUDA", A2_ESTATE: "A2_ESTATE"}
@@ -109,6 +111,17 @@ SIGNATURES = {
     "a2cid2_orthogonalize_workspace": (C.c_int, [_i64, _i64, _i64, C.c_int32, _lp]),
     "a2cid2_orthogonalize": (C.c_int, [_vp, _i64, _i64, _i64, _i64, _i64, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double,
                                        C.c_double, _vp, _i64, _i64, C.c_int32, _vp, _i64, _vp]),
+    "a2cid2_rms_norm": (C.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i64, C.c_double, _vp, _i64, _vp, _i64, C.c_int32, _vp]),
+    "a2cid2_rms_norm_e4m3": (C.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i64, C.c_double, _vp, _i64, _i64, _vp, _i64, _vp, C.c_int32, _vp]),
+    "a2cid2_dequantize_e4m3": (C.c_int, [_vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, C.c_int32, _vp]),
+    "a2cid2_rms_norm_grad_workspace": (C.c_int, [_i64, _i64, C.c_int32, C.c_int32, _lp]),
+    "a2cid2_rms_norm_grad": (C.c_int, [_vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i64, C.c_double, _vp, _i64, _vp, C.c_int32, _vp, _i64, _vp]),
+    "a2cid2_route": (C.c_int, [_vp, _i64, _i64, _i64, _i64, C.c_int32, _vp, _i64, _i64, C.c_int32, C.c_int32, C.c_double, _vp, _vp, _vp, C.c_int32, _vp]),
+    "a2cid2_route_grad": (C.c_int, [_vp, _i64, _vp, _vp, _i64, _i64, _i64, C.c_int32, C.c_int32, C.c_double, _vp, _i64, C.c_int32, _vp]),
+    # a2cid2_gradient_t is nine words of 64 bits: in, out, worker strides of both, rows, cols, pitches of both, type
+    "a2cid2_clip_gradients_workspace": (C.c_int, [_i64, _i64, _lp]),
+    "a2cid2_gradient_norms": (C.c_int, [_vp, _i64, _i64, _vp, _vp, _i64, _vp]),
+    "a2cid2_clip_gradients": (C.c_int, [_vp, _i64, _i64, C.c_double, C.c_int32, _vp, _vp, _i64, _vp]),
     "a2cid2_operators_check": (C.c_int, [_vp]),
     "a2cid2_version": (C.c_char_p, []),
 }

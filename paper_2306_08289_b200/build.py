@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "liba2cid2.so")
 SOURCES = ["api.cu", "kernels.cu", "scheduler.cpp", "spectral.cpp",
-           "lm_api.cu", "embed.cu", "gemm_sm100.cu", "vocab_loss.cu", "vocab_loss_few.cu", "orthogonalize.cu"]
+           "lm_api.cu", "embed.cu", "gemm_sm100.cu", "vocab_loss.cu", "vocab_loss_few.cu", "orthogonalize.cu",
+           "lm_train_api.cu", "rms_norm.cu", "route.cu", "clip.cu"]
 
 
 def _nvcc() -> str:
@@ -40,7 +41,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
-           "-Xcompiler", "-fPIC,-O2,-Wall", "-shared", "-cudart", "static",
+           "-Xcompiler", "-fPIC,-O2,-Wall", "-shared", "-cudart", "static", "--threads", "0",  # sources side by side
            "--diag-error", "2809",  # a launch whose status is dropped ([[nodiscard]])
            "-I", INCLUDE, "-I", CSRC, "-o", tmp]
     cmd += os.environ.get("A2CID2_NVCC_FLAGS", "").split()  # extra flags for experiments, e.g. -DA2_EVENT_THREADS=512

@@ -1,0 +1,352 @@
+// Norm of a gradient that is spread over many tensors, and its clipping: norm = sqrt(sum of squares of all elements of all tensors), out = in * min(1, max_norm / norm); for
+// each worker's part of the tensors by itself.
+#include <algorithm>
+
+#include "lm_ops.h"
+
+namespace a2 {
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------
+// Bound by memory: read once for the norm, read again and written once for the clipping, the second reading against the direction of the first so that
+// what was read last comes from L2. A worker's elements are cut into chunks of kChunk, tensor after tensor; every CTA has a run of consecutive
+// chunks, over all workers, and leaves a sum for each worker it meets: CTA b and worker w at place b + w, which no other pair
+// has, since runs follow one another. Sums are joined in order.
+// ---------------------------------------------------------------------------------------------
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kChunk = 8192;         // elements
+constexpr int kCtas = 6;             // a multiprocessor
+constexpr int kFew = 48;             // tensors that are described in a kernel's parameters; more in the workspace
+constexpr int kStored = 240;         // tensors that a launch brings there
+constexpr int64_t kSmallChunks = 4;  // chunks of a worker that one CTA takes alone
+
+struct Tensor {
+    const void* in;
+    void* out;
+    int64_t worker_stride, out_worker_stride, rows, cols, pitch, out_pitch;
+    int64_t first_chunk;  // of the worker's
+    int32_t bf16;
+    int32_t wide;  // rows may be read 16 bytes at a time: one row (from the boundary before it), or all rows on boundaries
+};
+
+struct Few {
+    Tensor tensor[kFew];
+};
+struct Stored {
+    Tensor tensor[kStored];
+};
+
+struct ClipKernelArgs {
+    int64_t n_tensors, workers, worker_chunks, chunks;
+    double* sums;
+    float* norms;
+    double max_norm;
+    bool zero_nonfinite, clip;
+};
+
+__global__ void __launch_bounds__(kStored) k_store(const __grid_constant__ Stored from, Tensor* to, int n) {
+    ptx::chained();
+    if ((int)threadIdx.x < n) to[threadIdx.x] = from.tensor[threadIdx.x];
+}
+
+__device__ __forceinline__ int64_t run_start(const ClipKernelArgs& a, int64_t cta, int64_t ctas) { return cta * a.chunks / ctas; }
+__device__ __forceinline__ int64_t run_of(const ClipKernelArgs& a, int64_t chunk, int64_t ctas) { return ((chunk + 1) * ctas - 1) / a.chunks; }
+
+template <int THREADS>
+__device__ __forceinline__ double cta_sum(double v, double* shared) {
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
+    __syncthreads();
+    if (threadIdx.x % 32 == 0) shared[threadIdx.x / 32] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) v += shared[w];
+    return v;
+}
+
+// The sum of a vector's squares. In fp32 where that neither overflows nor loses what lies below its range, as it hardly ever does; else in 64 bits.
+template <class T, int V>
+__device__ __forceinline__ double squares(const Pack<T, V>& p) {
+    float q = 0.0f;
+#pragma unroll
+    for (int k = 0; k < V; ++k) q = fmaf(widen(p.v[k]), widen(p.v[k]), q);
+    if (q > 0x1p-80f && q < 0x1p120f) return q;
+    double d = 0.0;
+#pragma unroll
+    for (int k = 0; k < V; ++k) d += (double)widen(p.v[k]) * (double)widen(p.v[k]);
+    return d;
+}
+
+// Calls `vector(in, out)` and `element(in, out)` for the calling thread's share of a chunk.
+template <class T, int THREADS, class Vector, class Element>
+__device__ __forceinline__ void over_chunk(const Tensor& t, int64_t worker, int64_t chunk, const Vector& vector, const Element& element) {
+    constexpr int V = 16 / sizeof(T);
+    const T* in = static_cast<const T*>(t.in) + worker * t.worker_stride;
+    T* out = static_cast<T*>(t.out) + worker * t.out_worker_stride;
+    const int64_t all = t.rows * t.cols;
+    if (t.wide && t.rows == 1) {
+        const int64_t start = chunk * kChunk - (int64_t)(reinterpret_cast<uintptr_t>(in) % 16 / sizeof(T));
+        if (start >= 0 && start + kChunk <= all) {
+#pragma unroll 4
+            for (int i = threadIdx.x; i < kChunk / V; i += THREADS) vector(in + start + i * V, out + start + i * V);
+            return;
+        }
+        for (int i = threadIdx.x; i < kChunk / V; i += THREADS) {
+            const int64_t e = start + i * V;
+            if (e >= 0 && e + V <= all) {
+                vector(in + e, out + e);
+            } else {
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    if (e + k >= 0 && e + k < all) element(in + e + k, out + e + k);
+            }
+        }
+        return;
+    }
+    // rows: the chunk's first element, from which the others are found in 32 bits
+    const int64_t first = chunk * kChunk;
+    const int64_t row0 = first / t.cols, col0 = first % t.cols;
+    const int count = (int)(all - first < kChunk ? all - first : kChunk);
+    auto at = [&](int i, int64_t& row, int64_t& col) {
+        col = col0 + i;
+        row = row0;
+        if (t.cols >= kChunk) {
+            if (col >= t.cols) ++row, col -= t.cols;
+        } else {
+            const unsigned r = (unsigned)col / (unsigned)t.cols;
+            row += r;
+            col -= (int64_t)r * t.cols;
+        }
+    };
+    int64_t row, col;
+    if (t.wide) {
+#pragma unroll 4
+        for (int i = threadIdx.x * V; i < count; i += THREADS * V) {
+            at(i, row, col);
+            vector(in + row * t.pitch + col, out + row * t.out_pitch + col);
+        }
+    } else {
+#pragma unroll 4
+        for (int i = threadIdx.x; i < count; i += THREADS) {
+            at(i, row, col);
+            element(in + row * t.pitch + col, out + row * t.out_pitch + col);
+        }
+    }
+}
+
+template <class T, int THREADS>
+__device__ __forceinline__ double chunk_squares(const Tensor& t, int64_t worker, int64_t chunk) {
+    constexpr int V = 16 / sizeof(T);
+    double sum = 0.0;
+    over_chunk<T, THREADS>(
+        t, worker, chunk, [&](const T* in, T*) { sum += squares<T, V>(*reinterpret_cast<const Pack<T, V>*>(in)); },
+        [&](const T* in, T*) {
+            const double v = widen(*in);
+            sum += v * v;
+        });
+    return sum;
+}
+
+template <class T, int THREADS>
+__device__ __forceinline__ void scale_chunk(const Tensor& t, int64_t worker, int64_t chunk, float factor, bool zero) {
+    constexpr int V = 16 / sizeof(T);
+    over_chunk<T, THREADS>(
+        t, worker, chunk,
+        [&](const T* in, T* out) {
+            Pack<T, V> p = *reinterpret_cast<const Pack<T, V>*>(in);
+#pragma unroll
+            for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(zero ? 0.0f : widen(p.v[k]) * factor);
+            *reinterpret_cast<Pack<T, V>*>(out) = p;
+        },
+        [&](const T* in, T* out) { *out = narrow<T>(zero ? 0.0f : widen(*in) * factor); });
+}
+
+struct Factor {
+    float by;
+    bool zero, nothing;  // nothing: by one
+};
+__device__ __forceinline__ Factor factor_of(const ClipKernelArgs& a, double norm) {
+    if (!isfinite(norm)) return {1.0f, a.zero_nonfinite, !a.zero_nonfinite};
+    if (norm <= a.max_norm) return {1.0f, false, true};
+    return {(float)(a.max_norm / norm), false, false};
+}
+
+template <int THREADS>
+__device__ __forceinline__ void scale(const Tensor& t, int64_t worker, int64_t chunk, const Factor& f) {
+    if (f.nothing && t.in == t.out) return;
+    if (t.bf16)
+        scale_chunk<__nv_bfloat16, THREADS>(t, worker, chunk, f.by, f.zero);
+    else
+        scale_chunk<float, THREADS>(t, worker, chunk, f.by, f.zero);
+}
+
+// The tensor that a worker's chunk belongs to: the last one that begins at it or before.
+__device__ __forceinline__ int tensor_of(const Tensor* table, int64_t n, int64_t chunk) {
+    int low = 0, high = (int)n - 1;
+    while (low < high) {
+        const int mid = (low + high + 1) / 2;
+        if (table[mid].first_chunk <= chunk)
+            low = mid;
+        else
+            high = mid - 1;
+    }
+    return low;
+}
+
+template <bool FEW>
+__global__ void __launch_bounds__(kThreads) k_squares(const ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored) {
+    __shared__ double shared[kWarps];
+    ptx::chained();
+    const Tensor* table = FEW ? few.tensor : stored;
+    const int64_t cta = blockIdx.x, ctas = gridDim.x, end = run_start(a, cta + 1, ctas);
+    int64_t chunk = run_start(a, cta, ctas);
+    while (chunk < end) {
+        const int64_t worker = chunk / a.worker_chunks, worker_end = min(end, (worker + 1) * a.worker_chunks);
+        int64_t c = chunk - worker * a.worker_chunks;
+        int t = tensor_of(table, a.n_tensors, c);
+        double sum = 0.0;
+        for (; chunk < worker_end; ++chunk, ++c) {
+            while (t + 1 < a.n_tensors && table[t + 1].first_chunk <= c) ++t;
+            const Tensor& tensor = table[t];
+            sum += tensor.bf16 ? chunk_squares<__nv_bfloat16, kThreads>(tensor, worker, c - tensor.first_chunk)
+                               : chunk_squares<float, kThreads>(tensor, worker, c - tensor.first_chunk);
+        }
+        sum = cta_sum<kThreads>(sum, shared);
+        if (threadIdx.x == 0) a.sums[cta + worker] = sum;
+    }
+}
+
+__device__ __forceinline__ double norm_of(const ClipKernelArgs& a, int64_t worker, int64_t ctas, double* shared) {
+    const int64_t from = run_of(a, worker * a.worker_chunks, ctas), to = run_of(a, (worker + 1) * a.worker_chunks - 1, ctas);
+    double sum = 0.0;
+    for (int64_t b = from + threadIdx.x; b <= to; b += kThreads) sum += a.sums[b + worker];
+    return sqrt(cta_sum<kThreads>(sum, shared));
+}
+
+template <bool FEW>
+__global__ void __launch_bounds__(kThreads) k_scale(const ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored) {
+    __shared__ double shared[kWarps];
+    ptx::chained();
+    const Tensor* table = FEW ? few.tensor : stored;
+    const int64_t cta = blockIdx.x, ctas = gridDim.x, start = run_start(a, cta, ctas);
+    int64_t chunk = run_start(a, cta + 1, ctas);
+    while (chunk > start) {
+        const int64_t worker = (chunk - 1) / a.worker_chunks, worker_start = max(start, worker * a.worker_chunks);
+        const double norm = norm_of(a, worker, ctas, shared);
+        if (worker_start == worker * a.worker_chunks && threadIdx.x == 0) a.norms[worker] = (float)norm;
+        const Factor f = factor_of(a, norm);
+        int64_t c = chunk - 1 - worker * a.worker_chunks;
+        int t = tensor_of(table, a.n_tensors, c);
+        for (; chunk > worker_start; --chunk, --c) {
+            while (table[t].first_chunk > c) --t;
+            scale<kThreads>(table[t], worker, c - table[t].first_chunk, f);
+        }
+    }
+}
+
+// Norms alone, of a CTA each.
+__global__ void __launch_bounds__(kThreads) k_norms(const ClipKernelArgs a, int64_t ctas) {
+    __shared__ double shared[kWarps];
+    ptx::chained();
+    const double norm = a.chunks ? norm_of(a, blockIdx.x, ctas, shared) : 0.0;
+    if (threadIdx.x == 0) a.norms[blockIdx.x] = (float)norm;
+}
+
+// Few elements a worker: both steps in one launch, a CTA a worker.
+constexpr int kSmallThreads = 1024;
+
+template <bool FEW>
+__global__ void __launch_bounds__(kSmallThreads) k_small(const ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored) {
+    __shared__ double shared[kSmallThreads / 32];
+    ptx::chained();
+    const Tensor* table = FEW ? few.tensor : stored;
+    const int64_t worker = blockIdx.x;
+    double sum = 0.0;
+    for (int64_t c = 0, t = 0; c < a.worker_chunks; ++c) {
+        while (t + 1 < a.n_tensors && table[t + 1].first_chunk <= c) ++t;
+        const Tensor& tensor = table[t];
+        sum += tensor.bf16 ? chunk_squares<__nv_bfloat16, kSmallThreads>(tensor, worker, c - tensor.first_chunk)
+                           : chunk_squares<float, kSmallThreads>(tensor, worker, c - tensor.first_chunk);
+    }
+    const double norm = sqrt(cta_sum<kSmallThreads>(sum, shared));
+    if (threadIdx.x == 0) a.norms[worker] = (float)norm;
+    if (!a.clip) return;
+    const Factor f = factor_of(a, norm);
+    for (int64_t c = a.worker_chunks - 1, t = a.n_tensors - 1; c >= 0; --c) {
+        while (table[t].first_chunk > c) --t;
+        scale<kSmallThreads>(table[t], worker, c - table[t].first_chunk, f);
+    }
+}
+
+int64_t most_ctas() { return (int64_t)multiprocessors() * kCtas; }
+
+bool on_boundaries(const void* p, int64_t pitch, int64_t size) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && pitch * size % 16 == 0; }
+
+// How a tensor is read, and its chunks.
+int64_t describe(const a2cid2_gradient_t& g, bool clip, int64_t workers, Tensor& t) {
+    const int64_t size = g.storage_dtype == A2_BF16 ? 2 : 4;
+    t = {g.in, clip ? g.out : const_cast<void*>(g.in), g.worker_stride, clip ? g.out_worker_stride : g.worker_stride, g.rows, g.cols, g.pitch,
+         clip ? g.out_pitch : g.pitch, 0, g.storage_dtype == A2_BF16, 0};
+    if (t.rows > 1 && t.pitch == t.cols && t.out_pitch == t.cols) t.cols *= t.rows, t.rows = 1;
+    const int64_t all = t.rows * t.cols;
+    if (all == 0) return 0;
+    if (t.rows == 1) {
+        const uintptr_t apart = reinterpret_cast<uintptr_t>(t.in) - reinterpret_cast<uintptr_t>(t.out);
+        t.wide = apart % 16 == 0 && (workers == 1 || (t.worker_stride - t.out_worker_stride) * size % 16 == 0);
+    } else {
+        t.wide = on_boundaries(t.in, t.pitch, size) && on_boundaries(t.out, t.out_pitch, size) && t.cols * size % 16 == 0 &&
+                 (workers == 1 || (t.worker_stride * size % 16 == 0 && t.out_worker_stride * size % 16 == 0));
+    }
+    // a row that starts behind a boundary may take a part of a chunk more
+    return ceil_div(all + (t.wide && t.rows == 1 ? 16 / size - 1 : 0), kChunk);
+}
+
+}  // namespace
+
+int64_t clip_workspace(int64_t n_tensors, int64_t workers) {
+    Carver c(nullptr);
+    c.take<double>(most_ctas() + workers);
+    if (n_tensors > kFew) c.take<Tensor>(n_tensors);
+    return c.used;
+}
+
+cudaError_t run_clip(const ClipArgs& r, void* workspace, cudaStream_t s) {
+    if (r.workers == 0) return cudaSuccess;
+    Carver carver(workspace);
+    ClipKernelArgs a{0, r.workers, 0, 0, carver.take<double>(most_ctas() + r.workers), r.norms, r.max_norm, r.zero_nonfinite, r.clip};
+    Few few{};
+    Stored part{};
+    Tensor* table = r.n_tensors > kFew ? carver.take<Tensor>(r.n_tensors) : nullptr;
+    int held = 0;
+    int64_t stored = 0;
+    auto bring = [&]() -> cudaError_t {
+        A2_CUDA_TRY(launch_chained(k_store, dim3(1), kStored, 0, s, part, table + stored, held));
+        stored += held;
+        held = 0;
+        return cudaSuccess;
+    };
+    for (int64_t i = 0; i < r.n_tensors; ++i) {
+        Tensor t;
+        const int64_t chunks = describe(r.tensors[i], r.clip, r.workers, t);
+        if (chunks == 0) continue;
+        t.first_chunk = a.worker_chunks;
+        a.worker_chunks += chunks;
+        ++a.n_tensors;
+        (table ? part.tensor : few.tensor)[held++] = t;
+        if (table && held == kStored) A2_CUDA_TRY(bring());
+    }
+    if (table && held) A2_CUDA_TRY(bring());
+    a.chunks = a.worker_chunks * a.workers;
+    const unsigned workers = (unsigned)a.workers;
+    if (a.chunks == 0) return launch_chained(k_norms, dim3(workers), kThreads, 0, s, a, (int64_t)1);
+    if (a.worker_chunks <= kSmallChunks) return launch_chained(table ? k_small<false> : k_small<true>, dim3(workers), kSmallThreads, 0, s, a, few, table);
+    const int64_t ctas = std::min(a.chunks, most_ctas());
+    A2_CUDA_TRY(launch_chained(table ? k_squares<false> : k_squares<true>, dim3((unsigned)ctas), kThreads, 0, s, a, few, table));
+    if (!r.clip) return launch_chained(k_norms, dim3(workers), kThreads, 0, s, a, ctas);
+    return launch_chained(table ? k_scale<false> : k_scale<true>, dim3((unsigned)ctas), kThreads, 0, s, a, few, table);
+}
+
+}  // namespace a2

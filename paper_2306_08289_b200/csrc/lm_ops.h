@@ -91,6 +91,104 @@ bool orthogonalize_range(double a, double b, double c, int steps);
 int64_t orthogonalize_workspace(int64_t n_mats, int64_t rows, int64_t cols, int32_t dtype);
 cudaError_t run_orthogonalize(const OrthogonalizeArgs& a, void* workspace, cudaStream_t s);
 
+int multiprocessors();  // of the current device
+
+constexpr int64_t kMaxNormWidth = 32768;  // columns of a normalised row: it is held in the registers of a CTA
+
+struct NormArgs {
+    const void* x;
+    int64_t x_pitch;
+    const void* residual;  // or NULL
+    int64_t residual_pitch;
+    const void* weight;  // or NULL
+    int64_t n, width;
+    float eps;
+    void* sum;  // or NULL
+    int64_t sum_pitch;
+    void* out;  // rows of the storage type; with `scales` of 8 bits
+    int64_t out_pitch;
+    float* scales;  // [n][blocks], or NULL
+    int64_t block;  // columns of a scale, 0: a row
+    int32_t dtype;
+};
+cudaError_t run_norm(const NormArgs& a, cudaStream_t s);
+
+struct DequantizeArgs {
+    const uint8_t* values;
+    int64_t values_pitch;
+    const float* scales;
+    int64_t n, width, block;
+    void* out;
+    int64_t out_pitch;
+    int32_t dtype;
+};
+cudaError_t run_dequantize(const DequantizeArgs& a, cudaStream_t s);
+
+struct NormGradArgs {
+    const void* grad_out;
+    int64_t grad_out_pitch;
+    const void* x;
+    int64_t x_pitch;
+    const void* weight;    // or NULL
+    const void* grad_sum;  // or NULL
+    int64_t grad_sum_pitch;
+    int64_t n, width;
+    float eps;
+    void* grad_x;  // or NULL
+    int64_t grad_x_pitch;
+    void* grad_weight;  // or NULL
+    int32_t dtype;
+};
+int64_t norm_grad_workspace(int64_t n, int64_t width, bool with_weight, int32_t dtype);
+cudaError_t run_norm_grad(const NormGradArgs& a, void* workspace, cudaStream_t s);
+
+constexpr int64_t kMaxExperts = 1024;  // a lane of a warp holds 32 of them
+constexpr int64_t kMaxChosen = 32;     // one a lane
+constexpr int64_t kMaxGroups = 32;
+
+struct RouteArgs {
+    const void* logits;
+    int64_t logits_pitch, n;
+    int experts, k;
+    int score;          // A2_SCORE_*
+    const float* bias;  // or NULL
+    int groups, top_groups, group_score;
+    bool renormalize;
+    float scale;
+    int32_t* ids;
+    float* weights;
+    int32_t* counts;  // or NULL
+    int32_t dtype;
+};
+cudaError_t run_route(const RouteArgs& a, cudaStream_t s);
+
+struct RouteGradArgs {
+    const void* logits;
+    int64_t logits_pitch;
+    const int32_t* ids;
+    const float* grad_weights;
+    int64_t n;
+    int experts, k;
+    int score;
+    bool renormalize;
+    float scale;
+    void* grad_logits;
+    int64_t grad_logits_pitch;
+    int32_t dtype;
+};
+cudaError_t run_route_grad(const RouteGradArgs& a, cudaStream_t s);
+
+struct ClipArgs {
+    const a2cid2_gradient_t* tensors;  // host
+    int64_t n_tensors, workers;
+    bool clip;  // else the norms alone
+    double max_norm;
+    bool zero_nonfinite;
+    float* norms;
+};
+int64_t clip_workspace(int64_t n_tensors, int64_t workers);
+cudaError_t run_clip(const ClipArgs& a, void* workspace, cudaStream_t s);
+
 // Ends a function at the first launch that fails: what would follow reads what that launch was to write.
 #define A2_CUDA_TRY(call)                            \
     do {                                             \

@@ -1,8 +1,9 @@
 """Operators of a language model's gradient event, on torch tensors: embedding lookup and its gradient, the vocabulary
-loss with its gradients, orthogonalisation of matrix updates.
+loss with its gradients, orthogonalisation of matrix updates, the root-mean-square norm (also to 8 bits) and its gradient, routing to
+experts and its gradient, the norm of a gradient and its clipping.
 
-Thin wrappers of the a2cid2_embed*, a2cid2_vocab_loss* and a2cid2_orthogonalize* entry points of include/a2cid2.h (formulas
-and conventions there). A matrix argument is a CUDA tensor of float32 or bfloat16 whose last dimension is contiguous; it may be a
+Thin wrappers of the a2cid2_embed*, a2cid2_vocab_loss*, a2cid2_orthogonalize*, a2cid2_rms_norm*, a2cid2_dequantize_e4m3, a2cid2_route* and
+a2cid2_*_gradient* entry points of include/a2cid2.h (formulas and conventions there). A matrix argument is a CUDA tensor of float32 or bfloat16 whose last dimension is contiguous; it may be a
 view into an engine's rows, e.g. `eng.x[w, off:off + v * h].view(v, h)` for worker w's table and the same slice of `eng.g` for its
 gradient, so that gradients land where the event kernels read them. Work is queued on torch's current stream of the tensors' device,
 or on `stream`; results and workspaces are allocated through torch on that stream. An argument the library cannot take raises
@@ -13,6 +14,7 @@ records (call under `torch.no_grad()`, or pass it detached), for its result woul
 """
 from __future__ import annotations
 
+import array
 import contextlib
 import ctypes as C
 import operator
@@ -136,10 +138,7 @@ def embed_grad(grad_out, ids, vocab, scale=1.0, out=None, accumulate=False, stre
     ids_p = _vector("ids", ids, n, torch.int32, grad_out.device)
     if accumulate and out is None:
         _refuse("accumulate needs out")
-    try:
-        vocab = operator.index(vocab)
-    except TypeError:
-        _refuse("vocab must be a whole number")
+    vocab = _whole("vocab", vocab)
     queue = _Queue(grad_out.device, stream, grad_out, ids, out)
     with queue as s:
         ws, ws_p, size = _workspace(grad_out, "a2cid2_embed_grad_workspace", vocab, width, n)  # checks the sizes
@@ -215,6 +214,287 @@ def orthogonalize(mats, steps=5, coeffs=NEWTON_SCHULZ, eps=1e-7, scale=1.0, out=
         B._check(B.lib().a2cid2_orthogonalize(mats.data_ptr(), mats.stride(0), pitch, n, rows, cols, steps, *coeffs, eps, scale, out.data_ptr(),
                                               out.stride(0), out_pitch, dtype, ws_p, size, s))
     return out
+
+
+def _whole(name, v):
+    try:
+        return operator.index(v)
+    except TypeError:
+        _refuse(f"{name} must be a whole number")
+
+
+def _norm_inputs(x, weight, residual, sum_out):
+    """(pitches of x, residual and sum_out, address of weight) after their checks."""
+    x_pitch = _matrix("x", x)
+    shape = x.shape
+    weight_p = None if weight is None else _vector("weight", weight, shape[1], x.dtype, x.device)
+    r_pitch = 0 if residual is None else _matrix("residual", residual, x, shape)
+    if sum_out is not None and residual is None:
+        _refuse("sum_out needs a residual")
+    s_pitch = shape[1] if sum_out is None else _matrix("sum_out", sum_out, x, shape)
+    return x_pitch, r_pitch, s_pitch, weight_p
+
+
+def rms_norm(x, weight=None, residual=None, eps=1e-6, out=None, sum_out=None, stream=None):
+    """s / sqrt(mean(s^2) + eps) * weight for every row of s = x + residual; x, residual [n, width], weight [width] of their type. Without a residual
+    returns the result, with one (result, s). out may be x or residual, sum_out x or residual."""
+    x_pitch, r_pitch, s_pitch, weight_p = _norm_inputs(x, weight, residual, sum_out)
+    n, width = x.shape
+    queue = _Queue(x.device, stream, x, weight, residual, out, sum_out)
+    with queue as s:
+        if out is None:
+            out, out_pitch = torch.empty(n, width, dtype=x.dtype, device=x.device), width
+            queue.made.append(out)
+        else:
+            out_pitch = _matrix("out", out, x, x.shape)
+        if residual is not None and sum_out is None:
+            sum_out = torch.empty(n, width, dtype=x.dtype, device=x.device)
+            queue.made.append(sum_out)
+        B._check(B.lib().a2cid2_rms_norm(x.data_ptr(), x_pitch, None if residual is None else residual.data_ptr(), r_pitch, weight_p, n, width, eps,
+                                         None if sum_out is None else sum_out.data_ptr(), s_pitch, out.data_ptr(), out_pitch, _DTYPES[x.dtype], s))
+    return out if residual is None else (out, sum_out)
+
+
+def rms_norm_quantized(x, weight=None, residual=None, eps=1e-6, block=128, sum_out=None, stream=None):
+    """As `rms_norm` with the result in 8 bits: (values float8_e4m3fn [n, width], scales float32 [n, blocks]), and s where there is a residual. A scale
+    is that of `block` columns (32, 64, 128, or 0 for a whole row): the result is values * scale (`dequantize`)."""
+    x_pitch, r_pitch, s_pitch, weight_p = _norm_inputs(x, weight, residual, sum_out)
+    n, width = x.shape
+    block = _whole("block", block)
+    if block not in (0, 32, 64, 128):
+        _refuse("block is 32, 64, 128 or 0 for whole rows")
+    queue = _Queue(x.device, stream, x, weight, residual, sum_out)
+    with queue as s:
+        values = torch.empty(n, width, dtype=torch.float8_e4m3fn, device=x.device)
+        scales = torch.empty(n, -(-width // block) if block else 1, dtype=torch.float32, device=x.device)
+        queue.made += (values, scales)
+        if residual is not None and sum_out is None:
+            sum_out = torch.empty(n, width, dtype=x.dtype, device=x.device)
+            queue.made.append(sum_out)
+        B._check(B.lib().a2cid2_rms_norm_e4m3(x.data_ptr(), x_pitch, None if residual is None else residual.data_ptr(), r_pitch, weight_p, n, width, eps,
+                                              None if sum_out is None else sum_out.data_ptr(), s_pitch, block, values.data_ptr(), width, scales.data_ptr(),
+                                              _DTYPES[x.dtype], s))
+    return (values, scales) if residual is None else (values, scales, sum_out)
+
+
+def dequantize(values, scales, dtype=torch.bfloat16, out=None, stream=None):
+    """values * scales in float32 or bfloat16, for what `rms_norm_quantized` returns. The columns of a scale follow from the shapes: the whole row for
+    one scale a row of more than 128 columns, else 32, 64 or 128."""
+    if not isinstance(values, torch.Tensor) or not values.is_cuda or values.dtype != torch.float8_e4m3fn or values.dim() != 2:
+        _refuse("values must be a CUDA matrix of float8_e4m3fn")
+    n, width = values.shape
+    if width != 1 and values.stride(1) != 1:
+        _refuse("the last dimension of values must be contiguous")
+    if not isinstance(scales, torch.Tensor) or scales.dtype != torch.float32 or scales.device != values.device or scales.dim() != 2 \
+            or scales.shape[0] != n or not scales.is_contiguous():
+        _refuse(f"scales must be a contiguous torch.float32 matrix of {n} rows on {values.device}")
+    _refuse_recorded("scales", scales)
+    if dtype not in _DTYPES:
+        _refuse("dtype must be float32 or bfloat16")
+    blocks = scales.shape[1]
+    block = 0 if blocks == 1 else next((b for b in (32, 64, 128) if -(-width // b) == blocks), None)
+    if block is None:
+        _refuse(f"{blocks} scales a row for {width} columns")
+    queue = _Queue(values.device, stream, values, scales, out)
+    with queue as s:
+        if out is None:
+            out, out_pitch = torch.empty(n, width, dtype=dtype, device=values.device), width
+            queue.made.append(out)
+        else:
+            out_pitch = _matrix("out", out, None, (n, width))
+            if out.dtype != dtype or out.device != values.device:
+                _refuse(f"out must be {dtype} on {values.device}")
+        B._check(B.lib().a2cid2_dequantize_e4m3(values.data_ptr(), values.stride(0) if n > 1 else width, scales.data_ptr(), n, width, block, out.data_ptr(), out_pitch,
+                                                _DTYPES[dtype], s))
+    return out
+
+
+def rms_norm_grad(grad_out, x, weight=None, eps=1e-6, grad_sum=None, grad_x=True, grad_weight=True, stream=None):
+    """(grad_x, grad_weight): the gradients of `rms_norm` for its rows x (with a residual: the s it returned; grad_sum is then the gradient that reaches s
+    by its other use, and grad_x that of both x and the residual). grad_x and grad_weight are True (allocate), None (leave out) or
+    the tensor to write; without a weight grad_weight is None. grad_x may be grad_out, grad_sum or x."""
+    g_pitch = _matrix("grad_out", grad_out)
+    x_pitch = _matrix("x", x, grad_out, grad_out.shape)
+    (n, width), dtype, device = x.shape, x.dtype, x.device
+    weight_p = None if weight is None else _vector("weight", weight, width, dtype, device)
+    s_pitch = 0 if grad_sum is None else _matrix("grad_sum", grad_sum, x, x.shape)
+    if weight is None and grad_weight is True:
+        grad_weight = None
+    if grad_x is not None and grad_x is not True:
+        gx_pitch = _matrix("grad_x", grad_x, x, x.shape)
+    else:
+        gx_pitch = width
+    if grad_weight is not None and grad_weight is not True:
+        _vector("grad_weight", grad_weight, width, dtype, device)
+    queue = _Queue(device, stream, grad_out, x, weight, grad_sum, grad_x, grad_weight)
+    with queue as s:
+        if grad_x is True:
+            grad_x = torch.empty(n, width, dtype=dtype, device=device)
+            queue.made.append(grad_x)
+        if grad_weight is True:
+            grad_weight = torch.empty(width, dtype=dtype, device=device)
+            queue.made.append(grad_weight)
+        code = _DTYPES[dtype]
+        ws, ws_p, size = _workspace(x, "a2cid2_rms_norm_grad_workspace", n, width, int(grad_weight is not None), code)
+        B._check(B.lib().a2cid2_rms_norm_grad(grad_out.data_ptr(), g_pitch, x.data_ptr(), x_pitch, weight_p, None if grad_sum is None else grad_sum.data_ptr(), s_pitch,
+                                              n, width, eps, None if grad_x is None else grad_x.data_ptr(), gx_pitch,
+                                              None if grad_weight is None else grad_weight.data_ptr(), code, ws_p, size, s))
+    return grad_x, grad_weight
+
+
+_SCORES = {"softmax": B.A2_SCORE_SOFTMAX, "sigmoid": B.A2_SCORE_SIGMOID}
+_GROUP_SCORES = {"max": B.A2_GROUP_BEST, "top2": B.A2_GROUP_TWO_BEST}
+
+
+def _named(name, v, known):
+    code = known.get(v) if isinstance(v, str) else None
+    if code is None:
+        _refuse(f"{name} must be one of {', '.join(known)}")
+    return code
+
+
+def route(logits, k, score="softmax", bias=None, groups=1, top_groups=1, group_score="max", renormalize=True, scale=1.0, stream=None):
+    """(ids int32 [n, k], weights float32 [n, k], counts int32 [n_experts]): the k experts of every token of logits [n, n_experts], best first, their weights
+    and how many tokens have chosen each. score "softmax" or "sigmoid"; bias float32 [n_experts] is added to the scores for the choice alone; of `groups` groups of
+    experts the `top_groups` best are open (group_score "max": by their best expert, "top2": by the sum of their two best). Weights are scale * score, divided by
+    the chosen scores' sum with renormalize. Logits of -inf or the type's lowest value are experts that are not available; ids are -1 where too few are."""
+    pitch = _matrix("logits", logits)
+    n, experts = logits.shape
+    device = logits.device
+    bias_p = None if bias is None else _vector("bias", bias, experts, torch.float32, device)
+    k = _whole("k", k)
+    score, group_score = _named("score", score, _SCORES), _named("group_score", group_score, _GROUP_SCORES)
+    if not 1 <= k <= experts:
+        _refuse(f"need 1 <= k <= {experts}")
+    queue = _Queue(device, stream, logits, bias)
+    with queue as s:
+        ids = torch.empty(n, k, dtype=torch.int32, device=device)
+        weights = torch.empty(n, k, dtype=torch.float32, device=device)
+        counts = torch.empty(experts, dtype=torch.int32, device=device)
+        queue.made += (ids, weights, counts)
+        B._check(B.lib().a2cid2_route(logits.data_ptr(), pitch, n, experts, k, score, bias_p, _whole("groups", groups), _whole("top_groups", top_groups), group_score,
+                                      int(bool(renormalize)), scale, ids.data_ptr(), weights.data_ptr(), counts.data_ptr(), _DTYPES[logits.dtype], s))
+    return ids, weights, counts
+
+
+def route_grad(logits, ids, grad_weights, score="softmax", renormalize=True, scale=1.0, out=None, stream=None):
+    """The gradient of `route`'s weights for its logits, the choice held fixed: ids are what it returned, grad_weights float32 [n, k] the gradient of its weights; score,
+    renormalize and scale as given to it. Entries whose id is -1 do not matter. out may be logits."""
+    pitch = _matrix("logits", logits)
+    n, experts = logits.shape
+    device = logits.device
+    for name, t, dtype in (("ids", ids, torch.int32), ("grad_weights", grad_weights, torch.float32)):
+        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or t.dim() != 2 or t.shape[0] != n or not t.is_contiguous():
+            _refuse(f"{name} must be a contiguous {dtype} matrix of {n} rows on {device}")
+        _refuse_recorded(name, t)
+    if ids.shape != grad_weights.shape:
+        _refuse("ids and grad_weights differ in shape")
+    score = _named("score", score, _SCORES)
+    queue = _Queue(device, stream, logits, ids, grad_weights, out)
+    with queue as s:
+        if out is None:
+            out, out_pitch = torch.empty(n, experts, dtype=logits.dtype, device=device), experts
+            queue.made.append(out)
+        else:
+            out_pitch = _matrix("out", out, logits, logits.shape)
+        B._check(B.lib().a2cid2_route_grad(logits.data_ptr(), pitch, ids.data_ptr(), grad_weights.data_ptr(), n, experts, ids.shape[1], score, int(bool(renormalize)),
+                                           scale, out.data_ptr(), out_pitch, _DTYPES[logits.dtype], s))
+    return out
+
+
+def _rows_of(name, shape, strides, out_strides):
+    """(rows, cols, pitch, out_pitch) of a tensor whose elements may be visited in any order, the same one on both sides."""
+    dims = sorted(((a, b, n) for n, a, b in zip(shape, strides, out_strides) if n != 1), reverse=True)
+    merged = []
+    for a, b, n in dims:
+        if merged and merged[-1][0] == a * n and merged[-1][1] == b * n:
+            merged[-1] = (a, b, n * merged[-1][2])
+        else:
+            merged.append((a, b, n))
+    if merged and merged[-1][:2] == (1, 1):
+        cols = merged.pop()[2]
+    else:
+        cols = 1
+    if len(merged) > 1 or any(a < cols or b < cols for a, b, _ in merged):
+        _refuse(f"{name} has strides {tuple(strides)}: rows at one distance from each other are needed")
+    return (merged[0][2], cols, merged[0][0], merged[0][1]) if merged else (1, cols, cols, cols)
+
+
+def _gradients(tensors, per_worker, out):
+    """(descriptions for the library, number of workers, device) of a list of tensors."""
+    if isinstance(tensors, torch.Tensor) or isinstance(out, torch.Tensor):
+        _refuse("tensors and out are lists of tensors")
+    tensors = list(tensors)
+    if not tensors:
+        _refuse("no tensors")
+    out = tensors if out is None else list(out)
+    if len(out) != len(tensors):
+        _refuse(f"{len(tensors)} tensors, but {len(out)} to write to")
+    device, workers, words = None, None, []
+    for t, o in zip(tensors, out):
+        for v in (t,) if o is t else (t, o):
+            if not isinstance(v, torch.Tensor) or not v.is_cuda:
+                _refuse("a gradient's tensors must be CUDA tensors")
+            if v.dtype not in _DTYPES:
+                _refuse("a gradient's tensors must be float32 or bfloat16")
+            _refuse_recorded("a gradient's tensor", v)
+            if device is None:
+                device = v.device
+            elif v.device != device:
+                _refuse("a gradient's tensors must be on one device")
+        shape = t.shape
+        if o is not t and (o.shape != shape or o.dtype != t.dtype):
+            _refuse(f"a tensor of shape {tuple(shape)} and type {t.dtype} has an output of shape {tuple(o.shape)} and type {o.dtype}")
+        numel = t.numel()
+        if per_worker:
+            if not shape:
+                _refuse("a worker's tensors have a first dimension of workers")
+            if workers is None:
+                workers = shape[0]
+            elif shape[0] != workers:
+                _refuse(f"tensors of {workers} and of {shape[0]} workers")
+            strides, out_strides = t.stride(), o.stride()
+            ws, out_ws = (strides[0], out_strides[0]) if workers > 1 else (0, 0)
+            shape, strides, out_strides = shape[1:], strides[1:], out_strides[1:]
+            numel = numel // workers if workers else 0
+        elif t.is_contiguous() and (o is t or o.is_contiguous()):
+            words += (t.data_ptr(), o.data_ptr(), 0, 0, 1, numel, numel, numel, _DTYPES[t.dtype])
+            continue
+        else:
+            ws = out_ws = 0
+            strides, out_strides = t.stride(), o.stride()
+        rows, cols, pitch, out_pitch = _rows_of("a gradient's tensor", shape, strides, out_strides) if numel else (0, 0, 0, 0)
+        words += (t.data_ptr(), o.data_ptr(), ws, out_ws, rows, cols, pitch, out_pitch, _DTYPES[t.dtype])
+    return tensors, out, array.array("q", words), workers if per_worker else 1, device
+
+
+def _clip(tensors, max_norm, zero_nonfinite, per_worker, out, stream):
+    tensors, out, words, workers, device = _gradients(tensors, per_worker, out)
+    queue = _Queue(device, stream, *tensors, *out)
+    with queue as s:
+        norms = torch.empty((workers,) if per_worker else (), dtype=torch.float32, device=device)
+        queue.made.append(norms)
+        ws, ws_p, size = _workspace(norms, "a2cid2_clip_gradients_workspace", len(tensors), workers)
+        table = words.buffer_info()[0]
+        if max_norm is None:
+            B._check(B.lib().a2cid2_gradient_norms(table, len(tensors), workers, norms.data_ptr(), ws_p, size, s))
+        else:
+            B._check(B.lib().a2cid2_clip_gradients(table, len(tensors), workers, max_norm, int(bool(zero_nonfinite)), norms.data_ptr(), ws_p, size, s))
+    return norms
+
+
+def gradient_norms(tensors, per_worker=False, stream=None):
+    """The 2-norm of all elements of a list of tensors (float32 or bfloat16, also mixed), a float32 scalar on their device. With per_worker all have the workers as their first
+    dimension (e.g. parts of the engine's rows, `eng.g[:, off:off + r * c].view(-1, r, c)`) and a norm is that of a worker: float32 [workers]."""
+    return _clip(tensors, None, False, per_worker, None, stream)
+
+
+def clip_gradients(tensors, max_norm, per_worker=False, zero_nonfinite=False, out=None, stream=None):
+    """Multiplies the tensors by min(1, max_norm / norm), in place or into the list `out` of tensors of the same shapes and types, and returns the norms before that
+    (as `gradient_norms`). Tensors whose norm is not finite are left as they are, or with zero_nonfinite become zeros."""
+    if max_norm is None:
+        _refuse("max_norm must be a number")
+    return _clip(tensors, max_norm, zero_nonfinite, per_worker, out, stream)
 
 
 def check(stream=None):
