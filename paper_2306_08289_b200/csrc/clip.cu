@@ -1,6 +1,7 @@
 // Norm of a gradient that is spread over many tensors, and its clipping: norm = sqrt(sum of squares of all elements of all tensors), out = in * min(1, max_norm / norm); for
 // each worker's part of the tensors by itself.
 #include <algorithm>
+#include <type_traits>
 
 #include "lm_ops.h"
 
@@ -10,14 +11,14 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------
 // Bound by memory: read once for the norm, read again and written once for the clipping, the second reading against the direction of the first so that
-// what was read last comes from L2. A worker's elements are cut into chunks of kChunk, tensor after tensor; every CTA has a run of consecutive
+// what was read last comes from L2. A worker's elements are cut into chunks of kChunkBytes, tensor after tensor; every CTA has a run of consecutive
 // chunks, over all workers, and leaves a sum for each worker it meets: CTA b and worker w at place b + w, which no other pair
 // has, since runs follow one another. Sums are joined in order.
 // ---------------------------------------------------------------------------------------------
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kChunk = 8192;         // elements
-constexpr int kCtas = 6;             // a multiprocessor
+constexpr int kChunkBytes = 32768;   // eight loads of 16 bytes in flight for each of 256 threads
+constexpr int kCtas = 4;             // a multiprocessor
 constexpr int kFew = 48;             // tensors that are described in a kernel's parameters; more in the workspace
 constexpr int kStored = 240;         // tensors that a launch brings there
 constexpr int64_t kSmallChunks = 4;  // chunks of a worker that one CTA takes alone
@@ -67,37 +68,50 @@ __device__ __forceinline__ double cta_sum(double v, double* shared) {
     return v;
 }
 
-// The sum of a vector's squares. In fp32 where that neither overflows nor loses what lies below its range, as it hardly ever does; else in 64 bits.
-template <class T, int V>
-__device__ __forceinline__ double squares(const Pack<T, V>& p) {
-    float q = 0.0f;
+// The sum of the squares of vectors. In fp32 where that neither overflows nor loses what lies below its range, as it hardly ever does; else in 64 bits.
+template <class T, int V, int COUNT>
+__device__ __forceinline__ double squares(const Pack<T, V> (&p)[COUNT]) {
+    float q[COUNT];
 #pragma unroll
-    for (int k = 0; k < V; ++k) q = fmaf(widen(p.v[k]), widen(p.v[k]), q);
-    if (q > 0x1p-80f && q < 0x1p120f) return q;
+    for (int i = 0; i < COUNT; ++i) {
+        q[i] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < V; ++k) q[i] = fmaf(widen(p[i].v[k]), widen(p[i].v[k]), q[i]);
+    }
+#pragma unroll
+    for (int n = COUNT / 2; n > 0; n /= 2)
+#pragma unroll
+        for (int i = 0; i < n; ++i) q[i] += q[i + n];
+    if (q[0] > 0x1p-60f && q[0] < 0x1p120f) return q[0];
     double d = 0.0;
 #pragma unroll
-    for (int k = 0; k < V; ++k) d += (double)widen(p.v[k]) * (double)widen(p.v[k]);
+    for (int i = 0; i < COUNT; ++i)
+#pragma unroll
+        for (int k = 0; k < V; ++k) d += (double)widen(p[i].v[k]) * (double)widen(p[i].v[k]);
     return d;
 }
 
-// Calls `vector(in, out)` and `element(in, out)` for the calling thread's share of a chunk.
-template <class T, int THREADS, class Vector, class Element>
-__device__ __forceinline__ void over_chunk(const Tensor& t, int64_t worker, int64_t chunk, const Vector& vector, const Element& element) {
-    constexpr int V = 16 / sizeof(T);
+// Walks over a chunk: `vectors(in, out)` gets the addresses of COUNT vectors of the calling thread, `element(in, out)` of single elements.
+constexpr int kBatch = 4;
+
+template <class T, int THREADS, class Vectors, class Element>
+__device__ __forceinline__ void over_chunk(const Tensor& t, int64_t worker, int64_t chunk, const Vectors& vectors, const Element& element) {
+    constexpr int V = 16 / sizeof(T), kChunk = kChunkBytes / sizeof(T);
     const T* in = static_cast<const T*>(t.in) + worker * t.worker_stride;
     T* out = static_cast<T*>(t.out) + worker * t.out_worker_stride;
     const int64_t all = t.rows * t.cols;
     if (t.wide && t.rows == 1) {
         const int64_t start = chunk * kChunk - (int64_t)(reinterpret_cast<uintptr_t>(in) % 16 / sizeof(T));
+        constexpr int kCount = kChunk / V / THREADS;
         if (start >= 0 && start + kChunk <= all) {
-#pragma unroll 4
-            for (int i = threadIdx.x; i < kChunk / V; i += THREADS) vector(in + start + i * V, out + start + i * V);
+            vectors(std::integral_constant<int, kCount>{}, [&](int i) { return start + (int64_t)(i * THREADS + (int)threadIdx.x) * V; }, in, [&](int i) { return start + (int64_t)(i * THREADS + (int)threadIdx.x) * V; }, out);
             return;
         }
         for (int i = threadIdx.x; i < kChunk / V; i += THREADS) {
             const int64_t e = start + i * V;
+            if (e >= all) break;
             if (e >= 0 && e + V <= all) {
-                vector(in + e, out + e);
+                vectors(std::integral_constant<int, 1>{}, [&](int) { return e; }, in, [&](int) { return e; }, out);
             } else {
 #pragma unroll
                 for (int k = 0; k < V; ++k)
@@ -110,9 +124,8 @@ __device__ __forceinline__ void over_chunk(const Tensor& t, int64_t worker, int6
     const int64_t first = chunk * kChunk;
     const int64_t row0 = first / t.cols, col0 = first % t.cols;
     const int count = (int)(all - first < kChunk ? all - first : kChunk);
-    auto at = [&](int i, int64_t& row, int64_t& col) {
-        col = col0 + i;
-        row = row0;
+    auto at = [&](int i, int64_t pitch) {
+        int64_t row = row0, col = col0 + i;
         if (t.cols >= kChunk) {
             if (col >= t.cols) ++row, col -= t.cols;
         } else {
@@ -120,20 +133,17 @@ __device__ __forceinline__ void over_chunk(const Tensor& t, int64_t worker, int6
             row += r;
             col -= (int64_t)r * t.cols;
         }
+        return row * pitch + col;
     };
-    int64_t row, col;
     if (t.wide) {
-#pragma unroll 4
-        for (int i = threadIdx.x * V; i < count; i += THREADS * V) {
-            at(i, row, col);
-            vector(in + row * t.pitch + col, out + row * t.out_pitch + col);
-        }
+        int i = threadIdx.x * V;
+        for (; i + (kBatch - 1) * THREADS * V < count; i += kBatch * THREADS * V)
+            vectors(std::integral_constant<int, kBatch>{}, [&](int k) { return at(i + k * THREADS * V, t.pitch); }, in, [&](int k) { return at(i + k * THREADS * V, t.out_pitch); }, out);
+        for (; i < count; i += THREADS * V)
+            vectors(std::integral_constant<int, 1>{}, [&](int) { return at(i, t.pitch); }, in, [&](int) { return at(i, t.out_pitch); }, out);
     } else {
 #pragma unroll 4
-        for (int i = threadIdx.x; i < count; i += THREADS) {
-            at(i, row, col);
-            element(in + row * t.pitch + col, out + row * t.out_pitch + col);
-        }
+        for (int i = threadIdx.x; i < count; i += THREADS) element(in + at(i, t.pitch), out + at(i, t.out_pitch));
     }
 }
 
@@ -142,7 +152,14 @@ __device__ __forceinline__ double chunk_squares(const Tensor& t, int64_t worker,
     constexpr int V = 16 / sizeof(T);
     double sum = 0.0;
     over_chunk<T, THREADS>(
-        t, worker, chunk, [&](const T* in, T*) { sum += squares<T, V>(*reinterpret_cast<const Pack<T, V>*>(in)); },
+        t, worker, chunk,
+        [&](auto count, auto from, const T* in, auto, T*) {
+            constexpr int kCount = decltype(count)::value;
+            Pack<T, V> p[kCount];
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) p[i] = *reinterpret_cast<const Pack<T, V>*>(in + from(i));
+            sum += squares<T, V, kCount>(p);
+        },
         [&](const T* in, T*) {
             const double v = widen(*in);
             sum += v * v;
@@ -155,11 +172,17 @@ __device__ __forceinline__ void scale_chunk(const Tensor& t, int64_t worker, int
     constexpr int V = 16 / sizeof(T);
     over_chunk<T, THREADS>(
         t, worker, chunk,
-        [&](const T* in, T* out) {
-            Pack<T, V> p = *reinterpret_cast<const Pack<T, V>*>(in);
+        [&](auto count, auto from, const T* in, auto to, T* out) {
+            constexpr int kCount = decltype(count)::value;
+            Pack<T, V> p[kCount];
 #pragma unroll
-            for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(zero ? 0.0f : widen(p.v[k]) * factor);
-            *reinterpret_cast<Pack<T, V>*>(out) = p;
+            for (int i = 0; i < kCount; ++i) p[i] = *reinterpret_cast<const Pack<T, V>*>(in + from(i));
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) p[i].v[k] = narrow<T>(zero ? 0.0f : widen(p[i].v[k]) * factor);
+                *reinterpret_cast<Pack<T, V>*>(out + to(i)) = p[i];
+            }
         },
         [&](const T* in, T* out) { *out = narrow<T>(zero ? 0.0f : widen(*in) * factor); });
 }
@@ -197,7 +220,7 @@ __device__ __forceinline__ int tensor_of(const Tensor* table, int64_t n, int64_t
 }
 
 template <bool FEW>
-__global__ void __launch_bounds__(kThreads) k_squares(const ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored) {
+__global__ void __launch_bounds__(kThreads, kCtas) k_squares(const __grid_constant__ ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored) {
     __shared__ double shared[kWarps];
     ptx::chained();
     const Tensor* table = FEW ? few.tensor : stored;
@@ -227,7 +250,7 @@ __device__ __forceinline__ double norm_of(const ClipKernelArgs& a, int64_t worke
 }
 
 template <bool FEW>
-__global__ void __launch_bounds__(kThreads) k_scale(const ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored) {
+__global__ void __launch_bounds__(kThreads, kCtas) k_scale(const __grid_constant__ ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored) {
     __shared__ double shared[kWarps];
     ptx::chained();
     const Tensor* table = FEW ? few.tensor : stored;
@@ -259,7 +282,7 @@ __global__ void __launch_bounds__(kThreads) k_norms(const ClipKernelArgs a, int6
 constexpr int kSmallThreads = 1024;
 
 template <bool FEW>
-__global__ void __launch_bounds__(kSmallThreads) k_small(const ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored) {
+__global__ void __launch_bounds__(kSmallThreads) k_small(const __grid_constant__ ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored) {
     __shared__ double shared[kSmallThreads / 32];
     ptx::chained();
     const Tensor* table = FEW ? few.tensor : stored;
@@ -287,7 +310,7 @@ bool on_boundaries(const void* p, int64_t pitch, int64_t size) { return reinterp
 
 // How a tensor is read, and its chunks.
 int64_t describe(const a2cid2_gradient_t& g, bool clip, int64_t workers, Tensor& t) {
-    const int64_t size = g.storage_dtype == A2_BF16 ? 2 : 4;
+    const int64_t size = g.storage_dtype == A2_BF16 ? 2 : 4, chunk = kChunkBytes / size;
     t = {g.in, clip ? g.out : const_cast<void*>(g.in), g.worker_stride, clip ? g.out_worker_stride : g.worker_stride, g.rows, g.cols, g.pitch,
          clip ? g.out_pitch : g.pitch, 0, g.storage_dtype == A2_BF16, 0};
     if (t.rows > 1 && t.pitch == t.cols && t.out_pitch == t.cols) t.cols *= t.rows, t.rows = 1;
@@ -301,7 +324,7 @@ int64_t describe(const a2cid2_gradient_t& g, bool clip, int64_t workers, Tensor&
                  (workers == 1 || (t.worker_stride * size % 16 == 0 && t.out_worker_stride * size % 16 == 0));
     }
     // a row that starts behind a boundary may take a part of a chunk more
-    return ceil_div(all + (t.wide && t.rows == 1 ? 16 / size - 1 : 0), kChunk);
+    return ceil_div(all + (t.wide && t.rows == 1 ? 16 / size - 1 : 0), chunk);
 }
 
 }  // namespace

@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 #include <utility>
 
@@ -92,6 +93,9 @@ int64_t orthogonalize_workspace(int64_t n_mats, int64_t rows, int64_t cols, int3
 cudaError_t run_orthogonalize(const OrthogonalizeArgs& a, void* workspace, cudaStream_t s);
 
 int multiprocessors();  // of the current device
+
+// Allows a kernel its dynamic shared memory, once for each device (`done`: which of them).
+cudaError_t allow_shared_memory(const void* kernel, int bytes, std::atomic<uint64_t>& done);
 
 constexpr int64_t kMaxNormWidth = 32768;  // columns of a normalised row: it is held in the registers of a CTA
 

@@ -34,7 +34,7 @@ template <class T>
 constexpr int kVec = 16 / sizeof(T);
 
 template <class T, bool WIDE>
-__device__ __forceinline__ void load(Pack<T, kVec<T>>& to, const T* row, int64_t c, int64_t width) {
+__device__ __forceinline__ void load(Pack<T, kVec<T>>& to, const T* row, int c, int width) {
     if (WIDE && c >= 0 && c + kVec<T> <= width) {
         to = *reinterpret_cast<const Pack<T, kVec<T>>*>(row + c);
     } else {
@@ -43,7 +43,7 @@ __device__ __forceinline__ void load(Pack<T, kVec<T>>& to, const T* row, int64_t
     }
 }
 template <class T, bool WIDE>
-__device__ __forceinline__ void store(T* row, int64_t c, int64_t width, const Pack<T, kVec<T>>& from) {
+__device__ __forceinline__ void store(T* row, int c, int width, const Pack<T, kVec<T>>& from) {
     if (WIDE && c >= 0 && c + kVec<T> <= width) {
         *reinterpret_cast<Pack<T, kVec<T>>*>(row + c) = from;
     } else {
@@ -53,34 +53,50 @@ __device__ __forceinline__ void store(T* row, int64_t c, int64_t width, const Pa
     }
 }
 
-// Sums (or maxima) of two values over a group, the same bits in every thread. Groups of more than a warp are whole CTAs; `slot` changes from
-// one such reduction to the next (0, 1, 0, ...), so that one barrier each is enough.
-template <bool MAX>
-__device__ __forceinline__ float2 over_group(float2 v, int group, int slot, float2 (*shared)[32]) {
+// A thread's place in its group: groups are a power of two up to a warp, or a whole CTA.
+__device__ __forceinline__ int place_in(int group) { return group > 32 ? (int)threadIdx.x : (int)threadIdx.x & (group - 1); }
+
+__device__ __forceinline__ unsigned mask_of(int group) {  // of the lanes of this thread's group
     const int lane = threadIdx.x % 32;
-    const int span = group < 32 ? group : 32;
-    const unsigned mask = span == 32 ? 0xffffffffu : ((1u << span) - 1u) << (lane & ~(span - 1));
-    auto join = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
-    for (int d = span / 2; d > 0; d /= 2) {
-        v.x = join(v.x, __shfl_xor_sync(mask, v.x, d));
-        v.y = join(v.y, __shfl_xor_sync(mask, v.y, d));
-    }
-    if (group <= 32) return v;
-    const int warps = group / 32;
-    if (lane == 0) shared[slot][threadIdx.x / 32] = v;
-    __syncthreads();
-    v = lane < warps ? shared[slot][lane] : make_float2(0.0f, 0.0f);  // zero is neutral for both: maxima are of magnitudes
-    for (int d = 16; d > 0; d /= 2) {
-        v.x = join(v.x, __shfl_xor_sync(0xffffffffu, v.x, d));
-        v.y = join(v.y, __shfl_xor_sync(0xffffffffu, v.y, d));
-    }
-    return v;
+    return group >= 32 ? 0xffffffffu : ((1u << group) - 1u) << (lane & ~(group - 1));
 }
 
-// rstd as a product of two factors, `by` a power of two: values whose squares leave the range of floats are scaled first.
-struct Rstd {
-    float by, r;
-};
+// Sums (or maxima of magnitudes) of COUNT values over a group, the same bits in every thread. `slot` changes from one such reduction to the
+// next (0, 1, 0, ...), so that one barrier each is enough.
+template <bool MAX, int COUNT>
+__device__ __forceinline__ void over_group(float (&v)[COUNT], int group, int slot, float (*shared)[32 * 2]) {
+    const unsigned mask = mask_of(group);
+    auto join = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2)
+        if (d < group)
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) v[i] = join(v[i], __shfl_xor_sync(mask, v[i], d));
+    if (group <= 32) return;
+    const int warps = group / 32, lane = threadIdx.x % 32;
+    if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) shared[slot][threadIdx.x / 32 * COUNT + i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) v[i] = lane < warps ? shared[slot][lane * COUNT + i] : 0.0f;  // zero is neutral for both
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2)
+        if (d < warps)
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) v[i] = join(v[i], __shfl_xor_sync(0xffffffffu, v[i], d));
+    // warps that are no power of two: lanes past them hold other sums
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
+}
+template <bool MAX>
+__device__ __forceinline__ float over_group(float v, int group, int slot, float (*shared)[32 * 2]) {
+    float one[1] = {v};
+    over_group<MAX, 1>(one, group, slot, shared);
+    return one[0];
+}
+
+// Rows whose squares leave the range of floats are multiplied by a power of two first, and rstd is that of the scaled row.
 __device__ __forceinline__ bool in_range(float squares, float eps_sum) { return squares < 0x1p120f && squares + eps_sum > 0x1p-90f; }
 __device__ __forceinline__ float power_below(float most) {  // 2^-e for most in [2^e, 2^(e+1))
     if (!(most > 0.0f) || isinf(most)) return 1.0f;
@@ -88,72 +104,70 @@ __device__ __forceinline__ float power_below(float most) {  // 2^-e for most in 
     frexpf(most, &e);
     return ldexpf(1.0f, max(-126, min(126, 1 - e)));
 }
-__device__ __forceinline__ Rstd scaled_rstd(float by, float squares, int64_t width, float eps) {
+__device__ __forceinline__ float scaled_rstd(float by, float squares, int width, float eps) {
     const double mean = (double)squares / (double)width + (double)eps * by * by;
-    return {by, mean > 0.0 ? (float)(1.0 / sqrt(mean)) : (isnan(mean) ? (float)mean : 0.0f)};  // a row of zeros with eps = 0 gives zeros
+    return mean > 0.0 ? (float)(1.0 / sqrt(mean)) : isnan(mean) ? (float)mean : 0.0f;  // a row of zeros with eps = 0 gives zeros
 }
+
+__device__ __forceinline__ float scale_of(float most) { return fmaxf(most / kE4m3Most, kScaleLeast); }
 
 struct NormKernelArgs {
     const void *x, *residual, *weight;
-    int64_t x_pitch, residual_pitch, n, width;
+    int64_t x_pitch, residual_pitch, n;
+    int width;
     float eps;
     void *sum, *out;
     int64_t sum_pitch, out_pitch;
     float* scales;
-    int64_t block, blocks;
-    int group;
+    int block_log, blocks, group;
     bool wide_weight, wide_out;
 };
 
 // ---------------------------------------------------------------------------------------------
 // Forward. Bound by memory: x and r are read once, s and y written once, the row stays in registers as floats in between. A group holds one
-// row. MODE 0: y in the rows' type. 1: e4m3 with a scale for every `block` columns, whose vectors lie in neighbouring lanes. 2: e4m3 with one
+// row. MODE 0: y in the rows' type. 1: e4m3 with a scale for every 2^block_log columns, whose vectors lie in neighbouring lanes. 2: e4m3 with one
 // scale a row. Sums are in fp32; s is rounded only where it is stored, y is formed from what it was before.
 // ---------------------------------------------------------------------------------------------
 template <class T, bool WIDE, int K, int MODE, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_norm(const NormKernelArgs a) {
+__global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ NormKernelArgs a) {
     constexpr int V = kVec<T>;
-    __shared__ float2 shared[2][32];
+    __shared__ float shared[2][32 * 2];
     ptx::chained();
-    const int group = a.group;
-    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / group) + threadIdx.x / group;
+    const int group = a.group, width = a.width, t = place_in(group);
+    const int64_t row = group > 32 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (blockDim.x / group) + threadIdx.x / group;
     if (row >= a.n) return;  // whole groups, and whole CTAs where a group is one
-    const int t = threadIdx.x % group;
     const T* x = static_cast<const T*>(a.x) + row * a.x_pitch;
     const T* r = static_cast<const T*>(a.residual) + row * a.residual_pitch;
     T* sum = static_cast<T*>(a.sum) + row * a.sum_pitch;
     const T* w = static_cast<const T*>(a.weight);
     const int shift = WIDE ? (int)(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T)) : 0;
+    auto column = [&](int j) { return (j * group + t) * V - shift; };
 
     float v[K][V];
     {
         Pack<T, V> px[K], pr[K];
 #pragma unroll
-        for (int j = 0; j < K; ++j) {
-            const int64_t c = (int64_t)(j * group + t) * V - shift;
-            if (c < a.width) load<T, WIDE>(px[j], x, c, a.width);
-        }
+        for (int j = 0; j < K; ++j)
+            if (column(j) < width) load<T, WIDE>(px[j], x, column(j), width);
         if (a.residual) {
 #pragma unroll
-            for (int j = 0; j < K; ++j) {
-                const int64_t c = (int64_t)(j * group + t) * V - shift;
-                if (c < a.width) load<T, WIDE>(pr[j], r, c, a.width);
-            }
+            for (int j = 0; j < K; ++j)
+                if (column(j) < width) load<T, WIDE>(pr[j], r, column(j), width);
         }
 #pragma unroll
         for (int j = 0; j < K; ++j) {
-            const int64_t c = (int64_t)(j * group + t) * V - shift;
+            const int c = column(j);
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[j][k] = c < a.width ? widen(px[j].v[k]) : 0.0f;
-            if (a.residual && c < a.width) {
+            for (int k = 0; k < V; ++k) v[j][k] = c < width ? widen(px[j].v[k]) : 0.0f;
+            if (a.residual && c < width) {
 #pragma unroll
                 for (int k = 0; k < V; ++k) v[j][k] += widen(pr[j].v[k]);
             }
-            if (a.sum && c < a.width) {
+            if (a.sum && c < width) {
                 Pack<T, V> p;
 #pragma unroll
                 for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(v[j][k]);
-                store<T, WIDE>(sum, c, a.width, p);
+                store<T, WIDE>(sum, c, width, p);
             }
         }
     }
@@ -162,84 +176,91 @@ __global__ void __launch_bounds__(THREADS) k_norm(const NormKernelArgs a) {
     for (int j = 0; j < K; ++j)
 #pragma unroll
         for (int k = 0; k < V; ++k) squares = fmaf(v[j][k], v[j][k], squares);
-    squares = over_group<false>(make_float2(squares, 0.0f), group, 0, shared).x;
-    int slot = 1;
-    Rstd rstd{1.0f, 0.0f};
-    if (in_range(squares, a.eps * (float)a.width)) {
-        rstd.r = 1.0f / sqrtf(squares / (float)a.width + a.eps);
+    squares = over_group<false>(squares, group, 0, shared);
+    float by = 1.0f, rstd;
+    if (in_range(squares, a.eps * (float)width)) {
+        rstd = 1.0f / sqrtf(squares / (float)width + a.eps);
     } else {
         float most = 0.0f;
 #pragma unroll
         for (int j = 0; j < K; ++j)
 #pragma unroll
             for (int k = 0; k < V; ++k) most = fmaxf(most, fabsf(v[j][k]));
-        const float by = power_below(over_group<true>(make_float2(most, 0.0f), group, 1, shared).x);
+        by = power_below(over_group<true>(most, group, 1, shared));
         float again = 0.0f;
 #pragma unroll
         for (int j = 0; j < K; ++j)
 #pragma unroll
-            for (int k = 0; k < V; ++k) again = fmaf(v[j][k] * by, v[j][k] * by, again);
-        rstd = scaled_rstd(by, over_group<false>(make_float2(again, 0.0f), group, 0, shared).x, a.width, a.eps);
+            for (int k = 0; k < V; ++k) {
+                v[j][k] *= by;
+                again = fmaf(v[j][k], v[j][k], again);
+            }
+        rstd = scaled_rstd(by, over_group<false>(again, group, 0, shared), width, a.eps);
     }
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-        const int64_t c = (int64_t)(j * group + t) * V - shift;
-        if (c >= a.width) continue;
-        Pack<T, V> pw;
-        if (w) {
-            if (a.wide_weight && shift == 0)
-                load<T, true>(pw, w, c, a.width);
-            else
-                load<T, false>(pw, w, c, a.width);
-        }
+        const int c = column(j);
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            v[j][k] = v[j][k] * rstd.by * rstd.r;
-            if (w) v[j][k] *= widen(pw.v[k]);
+        for (int k = 0; k < V; ++k) v[j][k] *= rstd;
+        if (c >= width) continue;
+        if (w) {
+            Pack<T, V> p;
+            if (a.wide_weight && shift == 0)
+                load<T, true>(p, w, c, width);
+            else
+                load<T, false>(p, w, c, width);
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[j][k] *= widen(p.v[k]);
         }
         if (MODE == 0) {
             Pack<T, V> p;
 #pragma unroll
             for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(v[j][k]);
-            store<T, WIDE>(static_cast<T*>(a.out) + row * a.out_pitch, c, a.width, p);
+            store<T, WIDE>(static_cast<T*>(a.out) + row * a.out_pitch, c, width, p);
         }
     }
     if constexpr (MODE != 0) {
         uint8_t* out = static_cast<uint8_t*>(a.out) + row * a.out_pitch;
-        float most_of_row = 0.0f;
+        float* scales = a.scales + row * a.blocks;
+        float most = 0.0f;
         if (MODE == 2) {
 #pragma unroll
             for (int j = 0; j < K; ++j)
 #pragma unroll
-                for (int k = 0; k < V; ++k) most_of_row = fmaxf(most_of_row, fabsf(v[j][k]));
-            most_of_row = over_group<true>(make_float2(most_of_row, 0.0f), group, slot, shared).x;
+                for (int k = 0; k < V; ++k) most = fmaxf(most, fabsf(v[j][k]));
+            most = over_group<true>(most, group, 1, shared);
+            if (t == 0) scales[0] = scale_of(most);
         }
+        const unsigned mask = mask_of(group);
+        const int lanes = (1 << a.block_log) / V;
 #pragma unroll
         for (int j = 0; j < K; ++j) {
-            const int64_t c = (int64_t)(j * group + t) * V - shift;
-            float most = most_of_row;
-            if (MODE == 1) {  // vectors past the row's end hold zeros
-                const int lanes = (int)a.block / V;
-                const int span = group < 32 ? group : 32, lane = threadIdx.x % 32;
-                const unsigned mask = span == 32 ? 0xffffffffu : ((1u << span) - 1u) << (lane & ~(span - 1));
+            const int c = column(j);
+            if (MODE == 1) {  // vectors past the row's end hold zeros (or NaN, which maxima pass over)
+                most = 0.0f;
 #pragma unroll
                 for (int k = 0; k < V; ++k) most = fmaxf(most, fabsf(v[j][k]));
-                for (int d = lanes / 2; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(mask, most, d));
+#pragma unroll
+                for (int d = 16; d > 0; d /= 2)
+                    if (d < lanes) most = fmaxf(most, __shfl_xor_sync(mask, most, d));
             }
-            if (c >= a.width) continue;
-            const float scale = fmaxf(most / kE4m3Most, kScaleLeast);
+            if (c >= width) continue;
+            const float scale = scale_of(most);
             const float inverse = 1.0f / scale;
-            const int64_t block = MODE == 1 ? c / a.block : 0;
-            if (MODE == 1 ? c % a.block == 0 : (j == 0 && t == 0)) a.scales[row * a.blocks + block] = scale;
+            if (MODE == 1 && t % lanes == 0) scales[c >> a.block_log] = scale;
             Pack<uint8_t, V> q;
 #pragma unroll
-            for (int k = 0; k < V; ++k) q.v[k] = __nv_cvt_float_to_fp8(v[j][k] * inverse, __NV_SATFINITE, __NV_E4M3);
-            if (a.wide_out && shift == 0 && c + V <= a.width) {
+            for (int k = 0; k < V; k += 2) {
+                const __nv_fp8x2_storage_t two = __nv_cvt_float2_to_fp8x2(make_float2(v[j][k] * inverse, v[j][k + 1] * inverse), __NV_SATFINITE, __NV_E4M3);
+                q.v[k] = (uint8_t)(two & 0xff);
+                q.v[k + 1] = (uint8_t)(two >> 8);
+            }
+            if (a.wide_out && shift == 0 && c + V <= width) {
                 *reinterpret_cast<Pack<uint8_t, V>*>(out + c) = q;
             } else {
 #pragma unroll
                 for (int k = 0; k < V; ++k)
-                    if (c + k >= 0 && c + k < a.width) out[c + k] = q.v[k];
+                    if (c + k >= 0 && c + k < width) out[c + k] = q.v[k];
             }
         }
     }
@@ -291,8 +312,9 @@ cudaError_t launch_norm(NormKernelArgs& a, const Shape& shape, cudaStream_t s) {
 template <class T>
 cudaError_t norm_typed(const NormArgs& n, cudaStream_t s) {
     constexpr int V = kVec<T>;
-    NormKernelArgs a{n.x, n.residual, n.weight, n.x_pitch, n.residual_pitch, n.n, n.width, n.eps, n.sum, n.out, n.sum_pitch, n.out_pitch, n.scales, n.block,
-                     n.block ? ceil_div(n.width, n.block) : 1, 0, reinterpret_cast<uintptr_t>(n.weight) % 16 == 0, false};
+    const int block_log = n.block == 128 ? 7 : n.block == 64 ? 6 : 5;
+    NormKernelArgs a{n.x, n.residual, n.weight, n.x_pitch, n.residual_pitch, n.n, (int)n.width, n.eps, n.sum, n.out, n.sum_pitch, n.out_pitch, n.scales, block_log,
+                     n.block ? (int)ceil_div(n.width, n.block) : 1, 0, reinterpret_cast<uintptr_t>(n.weight) % 16 == 0, false};
     bool wide = (!n.residual || alike<T>(n.x, n.x_pitch, n.residual, n.residual_pitch, n.n)) && (!n.sum || alike<T>(n.x, n.x_pitch, n.sum, n.sum_pitch, n.n));
     if (n.scales)
         a.wide_out = reinterpret_cast<uintptr_t>(n.out) % V == 0 && n.out_pitch % V == 0;
@@ -316,54 +338,77 @@ cudaError_t norm_typed(const NormArgs& n, cudaStream_t s) {
 // ---------------------------------------------------------------------------------------------
 // Values from their 8 bits and scales. Bound by memory.
 // ---------------------------------------------------------------------------------------------
-constexpr int kBack = 8;  // values a thread
+constexpr int kBack = 16;  // values a thread takes at a time; blocks are multiples of it
 
 template <class T, bool WIDE>
 __global__ void __launch_bounds__(256) k_dequantize(const uint8_t* __restrict__ values, int64_t values_pitch, const float* __restrict__ scales, int64_t n,
-                                                    int64_t width, int64_t block, int64_t blocks, int64_t pieces, T* __restrict__ out, int64_t out_pitch) {
+                                                    int width, int block_log, int blocks, T* __restrict__ out, int64_t out_pitch, int group) {
     ptx::chained();
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t row = at / pieces, c = at % pieces * kBack;
+    const int64_t row = (int64_t)blockIdx.x * (256 / group) + threadIdx.x / group;
     if (row >= n) return;
-    const float scale = scales[row * blocks + (block ? c / block : 0)];  // blocks are multiples of a thread's values
-    const uint8_t* q = values + row * values_pitch + c;
-    T* o = out + row * out_pitch + c;
-    auto value = [&](uint8_t b) {
-        const __half_raw h = __nv_cvt_fp8_to_halfraw(b, __NV_E4M3);
-        return narrow<T>(__half2float(__half(h)) * scale);
-    };
-    if (WIDE && c + kBack <= width) {
-        const Pack<uint8_t, kBack> p = *reinterpret_cast<const Pack<uint8_t, kBack>*>(q);
-        constexpr int V = kVec<T>;
+    auto value = [](uint8_t b) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(b, __NV_E4M3))); };
+    for (int c = (int)threadIdx.x % group * kBack; c < width; c += group * kBack) {
+        const float scale = scales[row * blocks + (blocks > 1 ? c >> block_log : 0)];
+        const uint8_t* q = values + row * values_pitch + c;
+        T* o = out + row * out_pitch + c;
+        if (WIDE && c + kBack <= width) {
+            const Pack<uint8_t, kBack> p = *reinterpret_cast<const Pack<uint8_t, kBack>*>(q);
+            constexpr int V = kVec<T>;
 #pragma unroll
-        for (int k = 0; k < kBack; k += V) {
-            Pack<T, V> y;
+            for (int k = 0; k < kBack; k += V) {
+                Pack<T, V> y;
 #pragma unroll
-            for (int e = 0; e < V; ++e) y.v[e] = value(p.v[k + e]);
-            *reinterpret_cast<Pack<T, V>*>(o + k) = y;
+                for (int e = 0; e < V; ++e) y.v[e] = narrow<T>(value(p.v[k + e]) * scale);
+                *reinterpret_cast<Pack<T, V>*>(o + k) = y;
+            }
+        } else {
+            for (int k = 0; k < kBack && c + k < width; ++k) o[k] = narrow<T>(value(q[k]) * scale);
         }
-    } else {
-        for (int k = 0; k < kBack && c + k < width; ++k) o[k] = value(q[k]);
     }
 }
 
 template <class T>
 cudaError_t dequantize_typed(const DequantizeArgs& a, cudaStream_t s) {
-    const int64_t pieces = ceil_div(a.width, kBack), blocks = a.block ? ceil_div(a.width, a.block) : 1;
+    const int blocks = a.block ? (int)ceil_div(a.width, a.block) : 1, block_log = a.block == 128 ? 7 : a.block == 64 ? 6 : 5;
     const bool wide = reinterpret_cast<uintptr_t>(a.values) % kBack == 0 && a.values_pitch % kBack == 0 && aligned16<T>(a.out, a.out_pitch);
-    return launch_chained(wide ? k_dequantize<T, true> : k_dequantize<T, false>, dim3((unsigned)ceil_div(a.n * pieces, 256)), 256, 0, s, a.values, a.values_pitch,
-                          a.scales, a.n, a.width, a.block, blocks, pieces, static_cast<T*>(a.out), a.out_pitch);
+    int group = 1;
+    while (group < 256 && group * kBack < a.width) group *= 2;
+    return launch_chained(wide ? k_dequantize<T, true> : k_dequantize<T, false>, dim3((unsigned)ceil_div(a.n, 256 / group)), 256, 0, s, a.values, a.values_pitch,
+                          a.scales, a.n, (int)a.width, block_log, blocks, static_cast<T*>(a.out), a.out_pitch, group);
 }
 
 // ---------------------------------------------------------------------------------------------
 // Gradient. Bound by memory: g, s and ds are read once, dx written once. CTAs walk over rows a fixed number apart and keep their part of dw for the
-// columns of each thread, in registers (in shared memory for long rows, LEAN); the parts go to the workspace and a second kernel adds
-// them up in order. A slot (a group's sequence of rows) has rows a multiple of 8 apart, so that all of them start equally far from a
-// 16-byte boundary and a thread's columns stay the same.
+// columns of each thread in registers; the parts go to the workspace and a second kernel adds them up in order. A slot (a group's sequence of rows)
+// has rows a multiple of 8 apart, so that all of them start equally far from a 16-byte boundary and a thread's columns stay the same.
+// The reductions over a row leave the loads idle, so the rows to come are brought to shared memory meanwhile: every thread copies the vectors that
+// it will itself read, kStages rows deep, and waits for its own copies alone.
+// Long rows (LEAN) are one vector of four or more a thread: those keep x and g in registers and dw in shared memory, and bring nothing ahead.
 // ---------------------------------------------------------------------------------------------
+constexpr int kStages = 3;
+
+__device__ __forceinline__ void copy_ahead(void* to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void close_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void wait_copies() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+}
+
+// A vector to shared memory, for the calling thread.
+template <class T, bool WIDE>
+__device__ __forceinline__ void bring(Pack<T, kVec<T>>* to, const T* row, int c, int width) {
+    if (WIDE && c >= 0 && c + kVec<T> <= width)
+        copy_ahead(to, row + c);
+    else
+        load<T, false>(*to, row, c, width);
+}
+
 struct NormGradKernelArgs {
     const void *g, *x, *weight, *ds;
-    int64_t g_pitch, x_pitch, ds_pitch, n, width;
+    int64_t g_pitch, x_pitch, ds_pitch, n;
+    int width;
     float eps;
     void* dx;
     int64_t dx_pitch;
@@ -372,133 +417,165 @@ struct NormGradKernelArgs {
     int group;
 };
 
-template <class T, bool WIDE, int K, bool LEAN, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_norm_grad(const NormGradKernelArgs a) {
+template <class T, bool WIDE, int K, bool LEAN, int THREADS, int CTAS>
+__global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_constant__ NormGradKernelArgs a) {
     constexpr int V = kVec<T>;
-    __shared__ float2 shared[2][32];
-    extern __shared__ float columns[];  // LEAN: this CTA's dw. Else, with several groups a CTA: one row of dw for each
+    __shared__ float shared[2][32 * 2];
+    extern __shared__ uint4 memory[];  // LEAN: this CTA's dw. Else rows to come, and at the end, with several groups a CTA, a row of dw for each
+    float* columns = reinterpret_cast<float*>(memory);
     ptx::chained();
-    const int group = a.group, groups = blockDim.x / group, t = threadIdx.x % group, mine = threadIdx.x / group;
+    const int group = a.group, width = a.width, t = place_in(group);
+    const int groups = group > 32 ? 1 : blockDim.x / group, mine = group > 32 ? 0 : threadIdx.x / group;
     const int64_t first = (int64_t)blockIdx.x * groups + mine;
     const T* w = static_cast<const T*>(a.weight);
     const int shift = WIDE ? (int)(reinterpret_cast<uintptr_t>(static_cast<const T*>(a.x) + first * a.x_pitch) % 16 / sizeof(T)) : 0;
-    Pack<T, V> pw[LEAN ? 1 : K];
-    float dw[LEAN ? 1 : K][V];
-    if (!LEAN) {
-#pragma unroll
-        for (int j = 0; j < K; ++j) {
-            const int64_t c = (int64_t)(j * group + t) * V - shift;
-            if (w && c < a.width) load<T, false>(pw[LEAN ? 0 : j], w, c, a.width);
-#pragma unroll
-            for (int k = 0; k < V; ++k) dw[LEAN ? 0 : j][k] = 0.0f;
-        }
-    } else if (a.parts) {
-        for (int64_t c = threadIdx.x; c < a.width; c += blockDim.x) columns[c] = 0.0f;
-        __syncthreads();
-    }
-    int slot = 0;
-    for (int64_t row = first; row < a.n; row += a.slots) {
-        const T* x = static_cast<const T*>(a.x) + row * a.x_pitch;
-        const T* g = static_cast<const T*>(a.g) + row * a.g_pitch;
-        const T* ds = static_cast<const T*>(a.ds) + row * a.ds_pitch;
-        T* dx = static_cast<T*>(a.dx) + row * a.dx_pitch;
-        Pack<T, V> px[K], pg[K];
-#pragma unroll
-        for (int j = 0; j < K; ++j) {
-            const int64_t c = (int64_t)(j * group + t) * V - shift;
-            if (c < a.width) {
-                load<T, WIDE>(px[j], x, c, a.width);
-                load<T, WIDE>(pg[j], g, c, a.width);
-            } else {
-#pragma unroll
-                for (int k = 0; k < V; ++k) px[j].v[k] = pg[j].v[k] = narrow<T>(0.0f);
-            }
-        }
-        auto weights = [&](int j, int64_t c) {
-            Pack<T, V> p;
-            if (!LEAN) return pw[LEAN ? 0 : j];
-            if (w && c < a.width)
-                load<T, false>(p, w, c, a.width);
-            return p;
-        };
-        auto sums = [&](float by) {
-            float2 v = make_float2(0.0f, 0.0f);
+    auto column = [&](int j) { return (j * group + t) * V - shift; };
+    // the vectors of one row: [stage][matrix][j][thread]
+    auto ahead = [&](int stage, int matrix, int j) {
+        return reinterpret_cast<Pack<T, V>*>(memory) + ((stage * 3 + matrix) * K + j) * blockDim.x + threadIdx.x;
+    };
+    auto bring_row = [&](int stage, int64_t row) {
+        if (row < a.n) {
 #pragma unroll
             for (int j = 0; j < K; ++j) {
-                const int64_t c = (int64_t)(j * group + t) * V - shift;
-                if (c >= a.width) continue;
-                const Pack<T, V> p = weights(j, c);
+                if (column(j) >= width) continue;
+                bring<T, WIDE>(ahead(stage, 0, j), static_cast<const T*>(a.x) + row * a.x_pitch, column(j), width);
+                bring<T, WIDE>(ahead(stage, 1, j), static_cast<const T*>(a.g) + row * a.g_pitch, column(j), width);
+                if (a.ds) bring<T, WIDE>(ahead(stage, 2, j), static_cast<const T*>(a.ds) + row * a.ds_pitch, column(j), width);
+            }
+        }
+        close_copies();
+    };
+    Pack<T, V> pw[LEAN ? 1 : K];
+    float dw[LEAN ? 1 : K][V];
+    if constexpr (!LEAN) {
+#pragma unroll
+        for (int s = 0; s + 1 < kStages; ++s) bring_row(s, first + s * a.slots);
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) dw[j][k] = 0.0f, pw[j].v[k] = narrow<T>(1.0f);
+            if (w && column(j) < width) load<T, false>(pw[j], w, column(j), width);
+        }
+    } else if (a.parts) {
+        for (int c = threadIdx.x; c < width; c += blockDim.x) columns[c] = 0.0f;
+        __syncthreads();
+    }
+    int slot = 0, stage = 0;
+    for (int64_t row = first; row < a.n; row += a.slots) {
+        T* dx = static_cast<T*>(a.dx) + row * a.dx_pitch;
+        Pack<T, V> px[K], pg[K], pd[LEAN ? 1 : K];
+        if constexpr (LEAN) {
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) px[j].v[k] = pg[j].v[k] = narrow<T>(0.0f);
+                if (column(j) >= width) continue;
+                load<T, WIDE>(px[j], static_cast<const T*>(a.x) + row * a.x_pitch, column(j), width);
+                load<T, WIDE>(pg[j], static_cast<const T*>(a.g) + row * a.g_pitch, column(j), width);
+            }
+        } else {
+            bring_row(stage == 0 ? kStages - 1 : stage - 1, row + (kStages - 1) * a.slots);
+            wait_copies<kStages - 1>();
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                const bool in = column(j) < width;
+#pragma unroll
+                for (int k = 0; k < V; ++k) px[j].v[k] = pg[j].v[k] = narrow<T>(0.0f);
+                if (in) px[j] = *ahead(stage, 0, j), pg[j] = *ahead(stage, 1, j);
+                if (in && a.ds) pd[j] = *ahead(stage, 2, j);
+            }
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+        }
+        auto weights = [&](int j) {
+            if constexpr (!LEAN) {
+                return pw[j];
+            } else {
+                Pack<T, V> p;
+#pragma unroll
+                for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(1.0f);
+                if (w && column(j) < width) load<T, false>(p, w, column(j), width);
+                return p;
+            }
+        };
+        float v[2];
+        auto sums = [&](float by) {
+            v[0] = v[1] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                const Pack<T, V> p = weights(j);
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
                     const float s = widen(px[j].v[k]) * by;
-                    const float wg = widen(pg[j].v[k]) * (w ? widen(p.v[k]) : 1.0f);
-                    v.x = fmaf(s, s, v.x);
-                    v.y = fmaf(s, wg, v.y);
+                    v[0] = fmaf(s, s, v[0]);
+                    v[1] = fmaf(s, widen(pg[j].v[k]) * widen(p.v[k]), v[1]);
                 }
             }
-            v = over_group<false>(v, group, slot, shared);
+            over_group<false, 2>(v, group, slot, shared);
             slot ^= 1;
-            return v;
         };
-        float2 v = sums(1.0f);
-        Rstd rstd{1.0f, 0.0f};
-        if (in_range(v.x, a.eps * (float)a.width)) {
-            rstd.r = 1.0f / sqrtf(v.x / (float)a.width + a.eps);
+        sums(1.0f);
+        float by = 1.0f, rstd;
+        if (in_range(v[0], a.eps * (float)width)) {
+            rstd = 1.0f / sqrtf(v[0] / (float)width + a.eps);
         } else {
             float most = 0.0f;
 #pragma unroll
             for (int j = 0; j < K; ++j)
 #pragma unroll
                 for (int k = 0; k < V; ++k) most = fmaxf(most, fabsf(widen(px[j].v[k])));
-            most = over_group<true>(make_float2(most, 0.0f), group, slot, shared).x;
+            by = power_below(over_group<true>(most, group, slot, shared));
             slot ^= 1;
-            const float by = power_below(most);
-            v = sums(by);
-            rstd = scaled_rstd(by, v.x, a.width, a.eps);
+            sums(by);
+            rstd = scaled_rstd(by, v[0], width, a.eps);
         }
-        const float c_mean = v.y * rstd.r / (float)a.width;
+        const float c_mean = v[1] * rstd / (float)width;
 #pragma unroll
         for (int j = 0; j < K; ++j) {
-            const int64_t c = (int64_t)(j * group + t) * V - shift;
-            if (c >= a.width) continue;
-            const Pack<T, V> p = weights(j, c);
-            Pack<T, V> pd, o;
-            if (a.ds) load<T, WIDE>(pd, ds, c, a.width);
+            const int c = column(j);
+            if (c >= width) continue;
+            const Pack<T, V> p = weights(j);
+            Pack<T, V> d, o;
+            if constexpr (LEAN) {
+                if (a.ds) load<T, WIDE>(d, static_cast<const T*>(a.ds) + row * a.ds_pitch, c, width);
+            } else {
+                d = pd[j];
+            }
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                const float hat = widen(px[j].v[k]) * rstd.by * rstd.r, gk = widen(pg[j].v[k]);
-                const float wg = w ? gk * widen(p.v[k]) : gk;
-                float d = (wg - hat * c_mean) * rstd.r * rstd.by;
-                if (a.ds) d += widen(pd.v[k]);
-                o.v[k] = narrow<T>(d);
-                if (!LEAN)
-                    dw[LEAN ? 0 : j][k] = fmaf(gk, hat, dw[LEAN ? 0 : j][k]);
-                else if (a.parts && c + k >= 0 && c + k < a.width)
+                const float hat = widen(px[j].v[k]) * by * rstd, gk = widen(pg[j].v[k]);
+                float y = (gk * widen(p.v[k]) - hat * c_mean) * rstd * by;
+                if (a.ds) y += widen(d.v[k]);
+                o.v[k] = narrow<T>(y);
+                if constexpr (!LEAN)
+                    dw[j][k] = fmaf(gk, hat, dw[j][k]);
+                else if (a.parts && c + k >= 0 && c + k < width)
                     columns[c + k] = fmaf(gk, hat, columns[c + k]);
             }
-            if (a.dx) store<T, WIDE>(dx, c, a.width, o);
+            if (a.dx) store<T, WIDE>(dx, c, width, o);
         }
     }
     if (!a.parts) return;
-    float* part = a.parts + (int64_t)blockIdx.x * a.width;
-    if (LEAN) {
+    float* part = a.parts + (int64_t)blockIdx.x * width;
+    if constexpr (LEAN) {
         __syncthreads();
-        for (int64_t c = threadIdx.x; c < a.width; c += blockDim.x) part[c] = columns[c];
-        return;
-    }
-    float* to = groups > 1 ? columns + mine * a.width : part;
+        for (int c = threadIdx.x; c < width; c += blockDim.x) part[c] = columns[c];
+    } else {
+        if (groups > 1) {
+            wait_copies<0>();
+            __syncthreads();  // the rows' place is free
+        }
+        float* to = groups > 1 ? columns + mine * width : part;
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-        const int64_t c = (int64_t)(j * group + t) * V - shift;
+        for (int j = 0; j < K; ++j)
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-            if (c + k >= 0 && c + k < a.width) to[c + k] = dw[LEAN ? 0 : j][k];
-    }
-    if (groups > 1) {
+            for (int k = 0; k < V; ++k)
+                if (column(j) + k >= 0 && column(j) + k < width) to[column(j) + k] = dw[j][k];
+        if (groups == 1) return;
         __syncthreads();
-        for (int64_t c = threadIdx.x; c < a.width; c += blockDim.x) {
+        for (int c = threadIdx.x; c < width; c += blockDim.x) {
             float sum = 0.0f;
-            for (int q = 0; q < groups; ++q) sum += columns[q * a.width + c];
+            for (int q = 0; q < groups; ++q) sum += columns[q * width + c];
             part[c] = sum;
         }
     }
@@ -524,48 +601,52 @@ __global__ void __launch_bounds__(1024) k_norm_join(const float* __restrict__ pa
     if (lane == 0 && to < width) dw[to] = narrow<T>(sum);
 }
 
-constexpr int kGradThreads = 2048 / 2;  // threads of a multiprocessor's CTAs
-
 template <class T>
 Shape grad_shape(int64_t width) {
     return shape_of(ceil_div(width + (width + kVec<T> <= kMaxNormWidth ? kVec<T> - 1 : 0), kVec<T>), 512, 1024, 2048, 8);
 }
 
-// CTAs of the first kernel: enough to fill the GPU, at most one row for each group, a multiple of 8 where a group has several rows.
+// CTAs of the first kernel: those that are resident at once (1,024 threads a multiprocessor with one vector each, 512 with more), at most one row
+// for each group, a multiple of 8 where a group has several rows.
 int64_t grad_ctas(int64_t n, const Shape& shape) {
     const int threads = cta_threads(shape), groups = threads / shape.group;
-    const int64_t full = (int64_t)multiprocessors() * std::max(1, kGradThreads / threads);
+    const int64_t full = (int64_t)multiprocessors() * std::max(1, (shape.k == 1 ? 1024 : 512) / threads);
     const int64_t needed = ceil_div(n, groups);
-    return needed <= full ? std::max<int64_t>(needed, 1) : round_up(full, 8);
+    return needed <= full ? std::max<int64_t>(needed, 1) : std::max<int64_t>(full / 8, 1) * 8;
+}
+
+template <class T, bool WIDE, int K, bool LEAN, int THREADS>
+cudaError_t launch_grad_kernel(const NormGradKernelArgs& a, unsigned ctas, unsigned threads, cudaStream_t s) {
+    constexpr int kCtas = !LEAN && K == 1 ? 2 : 1;
+    constexpr size_t most = LEAN ? (size_t)kMaxNormWidth * 4 : (size_t)THREADS * kStages * 3 * K * 16;
+    static std::atomic<uint64_t> allowed{0};
+    auto* kernel = k_norm_grad<T, WIDE, K, LEAN, THREADS, kCtas>;
+    A2_CUDA_TRY(allow_shared_memory(reinterpret_cast<const void*>(kernel), (int)most, allowed));
+    // rows to come take more than the rows of dw of several groups: kStages * 3 times 16 bytes a thread against V floats
+    const size_t smem = LEAN ? (a.parts ? (size_t)a.width * 4 : 0) : (size_t)threads * kStages * 3 * K * 16;
+    return launch_chained(kernel, dim3(ctas), threads, smem, s, a);
 }
 
 template <class T, bool WIDE>
 cudaError_t launch_norm_grad(NormGradKernelArgs& a, const Shape& shape, int64_t ctas, cudaStream_t s) {
     const unsigned threads = cta_threads(shape);
-    const int groups = threads / shape.group;
     a.group = shape.group;
-    a.slots = ctas * groups;
-    const dim3 grid((unsigned)ctas);
-    const size_t several = groups > 1 && a.parts ? (size_t)groups * a.width * 4 : 0, whole = a.parts ? (size_t)a.width * 4 : 0;
-    auto lean = [&](auto* kernel) -> cudaError_t {
-        A2_CUDA_TRY(cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxNormWidth * 4));
-        return launch_chained(kernel, grid, threads, whole, s, a);
-    };
+    a.slots = ctas * (threads / shape.group);
     switch (shape.k) {
-        case 1: return launch_chained(k_norm_grad<T, WIDE, 1, false, 512>, grid, threads, several, s, a);
-        case 2: return launch_chained(k_norm_grad<T, WIDE, 2, false, 512>, grid, threads, several, s, a);
-        case 4: return lean(k_norm_grad<T, WIDE, 4, true, 512>);
+        case 1: return launch_grad_kernel<T, WIDE, 1, false, 512>(a, (unsigned)ctas, threads, s);
+        case 2: return launch_grad_kernel<T, WIDE, 2, false, 512>(a, (unsigned)ctas, threads, s);
+        case 4: return launch_grad_kernel<T, WIDE, 4, true, 512>(a, (unsigned)ctas, threads, s);
         default: break;
     }
-    if (threads <= 512) return lean(k_norm_grad<T, WIDE, 8, true, 512>);
-    return lean(k_norm_grad<float, WIDE, 8, true, 1024>);  // rows of fp32 alone are that long
+    if (threads <= 512) return launch_grad_kernel<T, WIDE, 8, true, 512>(a, (unsigned)ctas, threads, s);
+    return launch_grad_kernel<float, WIDE, 8, true, 1024>(a, (unsigned)ctas, threads, s);  // rows of fp32 alone are that long
 }
 
 template <class T>
 cudaError_t norm_grad_typed(const NormGradArgs& n, void* workspace, cudaStream_t s) {
     const Shape shape = grad_shape<T>(n.width);
     const int64_t ctas = grad_ctas(n.n, shape);
-    NormGradKernelArgs a{n.grad_out, n.x, n.weight, n.grad_sum, n.grad_out_pitch, n.x_pitch, n.grad_sum_pitch, n.n, n.width, n.eps, n.grad_x, n.grad_x_pitch,
+    NormGradKernelArgs a{n.grad_out, n.x, n.weight, n.grad_sum, n.grad_out_pitch, n.x_pitch, n.grad_sum_pitch, n.n, (int)n.width, n.eps, n.grad_x, n.grad_x_pitch,
                          n.grad_weight ? Carver(workspace).take<float>(ctas * n.width) : nullptr, 0, 0};
     const bool wide = alike<T>(n.x, n.x_pitch, n.grad_out, n.grad_out_pitch, n.n) && (!n.grad_sum || alike<T>(n.x, n.x_pitch, n.grad_sum, n.grad_sum_pitch, n.n)) &&
                       (!n.grad_x || alike<T>(n.x, n.x_pitch, n.grad_x, n.grad_x_pitch, n.n)) && (aligned16<T>(n.x, n.x_pitch) || n.width + kVec<T> <= kMaxNormWidth);

@@ -5,6 +5,7 @@
 //   weights = scale * s (divided by the chosen scores' sum: renormalised).
 #include <algorithm>
 #include <cfloat>
+#include <climits>
 
 #include "lm_ops.h"
 
@@ -16,24 +17,14 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr unsigned kAll = 0xffffffffu;
 
-// Numbers as unsigned integers in the same order, above zero: zero stands for an expert that cannot be chosen.
+// Floats as unsigned integers in the same order, above zero: zero stands for an expert that cannot be chosen.
 __device__ __forceinline__ uint32_t ordered(float v) {
     const uint32_t b = __float_as_uint(v + 0.0f);  // -0 is 0
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ uint64_t ordered(double v) {
-    const uint64_t b = (uint64_t)__double_as_longlong(v + 0.0);
-    return b >> 63 ? ~b : b | 0x8000000000000000ull;
-}
 __device__ __forceinline__ float number(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
-__device__ __forceinline__ double number(uint64_t u) { return __longlong_as_double((long long)(u >> 63 ? u & 0x7fffffffffffffffull : ~u)); }
 
 __device__ __forceinline__ uint32_t warp_max(uint32_t v) { return __reduce_max_sync(kAll, v); }
-__device__ __forceinline__ uint64_t warp_max(uint64_t v) {
-    const uint32_t high = __reduce_max_sync(kAll, (uint32_t)(v >> 32));
-    const uint32_t low = __reduce_max_sync(kAll, (uint32_t)(v >> 32) == high ? (uint32_t)v : 0u);
-    return (uint64_t)high << 32 | low;
-}
 template <class F>
 __device__ __forceinline__ F warp_sum(F v) {
 #pragma unroll
@@ -41,17 +32,6 @@ __device__ __forceinline__ F warp_sum(F v) {
     return v;
 }
 __device__ __forceinline__ float warp_most(float v) { return number(warp_max(ordered(v))); }
-
-template <class F>
-struct Ordered;
-template <>
-struct Ordered<float> {
-    using Type = uint32_t;
-};
-template <>
-struct Ordered<double> {
-    using Type = uint64_t;
-};
 
 // A logit as the kernels use it: -inf (no expert) for NaN and what is at or below the type's lowest value, as masks are written.
 template <class T>
@@ -67,186 +47,156 @@ struct RouteKernelArgs {
     bool sigmoid, renormalize;
     const float* bias;
     int groups, group_size, top_groups;
-    bool two_best;  // a group's score is the sum of its two best keys
+    int share, per;  // lanes of a group (a power of two), experts of a lane
+    bool two_best;   // a group's score is the sum of its two best keys
+    bool wide;       // a lane's logits may be read 16 bytes at a time
     float scale;
     int32_t* ids;
     float* weights;
     int32_t* counts;
 };
 
-// The choice among a warp's experts: groups by their keys, experts by `rank` (the keys, or without a bias the logits). Lane j gets the j-th expert
-// (or -1). Expert e lies in lane e % 32, place e / 32. `off_key` and `off_rank` bound the errors (0: exact). Returns whether a decision is
-// closer than they allow.
-template <class F, int N, class Same>
-__device__ __forceinline__ bool choose(const RouteKernelArgs& a, const F (&key)[N], F off_key, const F (&rank_by)[N], F off_rank, const bool (&live)[N], F* staged,
-                                       int& mine, const Same& same) {
-    using U = typename Ordered<F>::Type;
-    const int lane = threadIdx.x % 32;
-    bool doubt = false;
-    U u[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) u[j] = live[j] ? ordered(rank_by[j]) : U(0);
-    if (a.groups > 1) {
-        // keys through shared memory (a word in 33 left out against bank conflicts): `share` lanes look through a group
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (j * 32 + lane < a.experts) staged[j * 33 + lane] = live[j] ? key[j] : -(F)INFINITY;
-        __syncwarp();
-        int share = 1;
-        while (share * 2 * a.groups <= 32) share *= 2;
-        const int group = lane / share;
-        F first = -(F)INFINITY, second = -(F)INFINITY;
-        if (group < a.groups)
-            for (int i = lane % share; i < a.group_size; i += share) {
-                const int e = group * a.group_size + i;
-                const F v = staged[e + e / 32];
-                second = v > first ? first : (v > second ? v : second);
-                first = v > first ? v : first;
-            }
-        for (int d = share / 2; d > 0; d /= 2) {
-            const F f = __shfl_xor_sync(kAll, first, d), s = __shfl_xor_sync(kAll, second, d);
-            const F low = f > first ? first : f;
-            second = second > s ? second : s;
-            second = low > second ? low : second;
-            first = f > first ? f : first;
-        }
-        const F score = a.two_best && a.group_size > 1 ? first + second : first;
-        int rank = 0;
-        for (int g = 0; g < a.groups; ++g) {
-            const F other = __shfl_sync(kAll, score, g * share);
-            rank += other > score || (other == score && g < group);
-        }
-        const bool leads = group < a.groups && lane % share == 0;
-        const unsigned open = __ballot_sync(kAll, leads && rank < a.top_groups);
-        if (off_key > 0 && a.top_groups < a.groups) {
-            const int last = __ffs(__ballot_sync(kAll, leads && rank == a.top_groups - 1)) - 1, next = __ffs(__ballot_sync(kAll, leads && rank == a.top_groups)) - 1;
-            const F in = __shfl_sync(kAll, score, last), out = __shfl_sync(kAll, score, next);
-            if (out > -(F)INFINITY) doubt = !(in - out > 4 * off_key + fabs(in) * (F)0x1p-21);
-        }
-        const uint32_t magic = (1u << 20) / a.group_size + 1;  // e / group_size for e * group_size < 2^20
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int g = (int)(((uint32_t)(j * 32 + lane) * magic) >> 20);
-            if (j * 32 + lane < a.experts && !(open >> (g * share) & 1)) u[j] = 0;
-        }
-    }
-    mine = -1;
-    U best = 0;
-    int at = 0;
-    auto look = [&] {
-        best = 0;
-#pragma unroll
-        for (int j = N - 1; j >= 0; --j)
-            if (u[j] >= best) best = u[j], at = j;
-    };
-    look();
-    F before = 0;
-    int expert_before = -1;
-    const int rounds = off_rank > 0 ? a.k + 1 : a.k;
-    for (int r = 0; r < rounds; ++r) {
-        const U top = warp_max(best);
-        if (top == 0) break;
-        const int expert = (int)__reduce_min_sync(kAll, best == top ? (unsigned)(at * 32 + lane) : 0xffffffffu);
-        if (off_rank > 0) {
-            const F now = number(top);
-            if (r > 0 && !(before - now > 2 * off_rank + fabs(now) * (F)0x1p-22) && !same(expert_before, expert)) doubt = true;
-            before = now;
-            expert_before = expert;
-        }
-        if (r < a.k && lane == r) mine = expert;
-        if (lane == expert % 32) {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (j == expert / 32) u[j] = 0;
-            look();
-        }
-    }
-    return doubt;
-}
-
 __device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
 
-// Keys closer to one another than fp32 scores can tell apart: the whole choice again in 64 bits. Rare.
+// Better of two experts by key; the lower one where keys are equal.
+__device__ __forceinline__ bool before(double key, int expert, double key2, int expert2) { return key > key2 || (key == key2 && expert < expert2); }
+
+// Keys closer to one another than fp32 scores can tell apart: the whole choice again in 64 bits. Rare, so short rather than fast. `first` and `count` are
+// this lane's experts. Lane j gets the j-th expert (or -1).
 template <class T, int N>
-__device__ __noinline__ int choose_in_doubt(const RouteKernelArgs& a, const T* row, double* staged) {
+__device__ __noinline__ int choose_in_doubt(const RouteKernelArgs& a, const T* row, int first, int count) {
     const int lane = threadIdx.x % 32;
-    double z[N], key[N];
-    bool live[N];
-    double most = -INFINITY;
-#pragma unroll
+    double key[N], rank[N];  // of groups and of experts
+    double most = -(double)INFINITY;
     for (int j = 0; j < N; ++j) {
-        const int e = j * 32 + lane;
-        z[j] = e < a.experts ? (double)logit(row[e]) : -(double)INFINITY;
-        live[j] = z[j] > -(double)INFINITY;
-        most = fmax(most, z[j]);
+        rank[j] = j < count ? (double)logit(row[first + j]) : -(double)INFINITY;
+        most = fmax(most, rank[j]);
     }
-    if (a.sigmoid) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) key[j] = 1.0 / (1.0 + exp(-z[j]));
-    } else {
-#pragma unroll
-        for (int d = 16; d > 0; d /= 2) most = fmax(most, __shfl_xor_sync(kAll, most, d));
-        double total = 0.0;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            key[j] = live[j] ? exp(z[j] - most) : 0.0;
-            total += key[j];
+    for (int d = 16; d > 0; d /= 2) most = fmax(most, __shfl_xor_sync(kAll, most, d));
+    double total = 0.0;
+    for (int j = 0; j < N; ++j) {
+        const bool live = rank[j] > -(double)INFINITY;
+        key[j] = !live ? 0.0 : a.sigmoid ? 1.0 / (1.0 + exp(-rank[j])) : exp(rank[j] - most);
+        total += key[j];
+    }
+    total = warp_sum(total);
+    for (int j = 0; j < N; ++j) {
+        if (!(rank[j] > -(double)INFINITY)) {
+            key[j] = -(double)INFINITY;
+            continue;
         }
-        total = warp_sum(total);
-#pragma unroll
-        for (int j = 0; j < N; ++j) key[j] = key[j] / total;
+        if (!a.sigmoid) key[j] /= total;
+        if (a.bias) {
+            key[j] += (double)a.bias[first + j];
+            key[j] = key[j] > -(double)INFINITY ? fmin(key[j], DBL_MAX) : -(double)INFINITY;  // NaN: not available
+            rank[j] = key[j];
+        }
+        if (!a.bias && !a.two_best) key[j] = rank[j];
     }
-    if (a.bias) {
-#pragma unroll
+    if (a.groups > 1) {
+        double best = -(double)INFINITY, second = best;
+        for (int j = 0; j < N; ++j) {
+            second = fmax(second, fmin(best, key[j]));
+            best = fmax(best, key[j]);
+        }
+        for (int d = a.share / 2; d > 0; d /= 2) {
+            const double b = __shfl_xor_sync(kAll, best, d), s = __shfl_xor_sync(kAll, second, d);
+            second = fmax(fmin(best, b), fmax(second, s));
+            best = fmax(best, b);
+        }
+        const double score = a.two_best && a.group_size > 1 ? best + second : best;
+        int place = 0;
+        for (int g = 0; g < a.groups; ++g) place += before(__shfl_sync(kAll, score, g * a.share), g, score, lane / a.share);
+        if (place >= a.top_groups)
+            for (int j = 0; j < N; ++j) rank[j] = -(double)INFINITY;
+    }
+    int mine = -1;
+    for (int r = 0; r < a.k; ++r) {
+        double best = -(double)INFINITY;
+        int expert = INT_MAX;
         for (int j = 0; j < N; ++j)
-            if (live[j]) {
-                key[j] += (double)a.bias[j * 32 + lane];
-                live[j] = key[j] > -(double)INFINITY;
-                key[j] = fmin(key[j], DBL_MAX);
-            }
+            if (rank[j] > best) best = rank[j], expert = first + j;
+        for (int d = 16; d > 0; d /= 2) {
+            const double b = __shfl_xor_sync(kAll, best, d);
+            const int e = __shfl_xor_sync(kAll, expert, d);
+            if (before(b, e, best, expert)) best = b, expert = e;
+        }
+        if (expert == INT_MAX) break;
+        if (lane == r) mine = expert;
+        if (expert >= first && expert < first + count) rank[expert - first] = -(double)INFINITY;
     }
-    int mine;
-    const auto never = [](int, int) { return false; };
-    if (a.bias)
-        choose<double, N>(a, key, 0.0, key, 0.0, live, staged, mine, never);
-    else
-        choose<double, N>(a, key, 0.0, z, 0.0, live, staged, mine, never);
     return mine;
 }
 
+// Sorts descending: Batcher's odd-even merges.
+template <int N>
+__device__ __forceinline__ void sort(uint32_t (&u)[N]) {
+#pragma unroll
+    for (int p = 1; p < N; p *= 2)
+#pragma unroll
+        for (int q = p; q >= 1; q /= 2)
+#pragma unroll
+            for (int j = q % p; j + q < N; j += 2 * q)
+#pragma unroll
+                for (int i = 0; i < q; ++i)
+                    if (j + i + q < N && (j + i) / (2 * p) == (j + i + q) / (2 * p)) {
+                        const uint32_t x = u[j + i], y = u[j + i + q];
+                        u[j + i] = max(x, y);
+                        u[j + i + q] = min(x, y);
+                    }
+}
+
 // ---------------------------------------------------------------------------------------------
-// A warp takes a token: its logits lie in registers, a round of the choice is a maximum over the warp and the lowest expert that has
-// it. Scores are fp32; where a decision is closer than their errors, the row is chosen again in 64 bits, so that the choice is that of
-// exact scores. Experts are counted in shared memory and added to `counts`, which an earlier kernel has cleared (ALONE: one CTA writes them).
+// A warp takes a token. Lane l has the experts first .. first + count of group l / share in registers, as keys in 32 bits whose lowest bits are replaced by the
+// expert's place in the lane (lower places larger), sorted; a round of the choice is a maximum over the heads of the lanes' lists, and the lowest lane that has
+// it, which is the lowest expert. Keys are fp32 scores less those bits. Where a decision is closer than their errors, the row is chosen
+// again in 64 bits, so that the choice is that of exact scores; without a bias keys are the logits, and only what is equal but for the lost bits is in
+// doubt. Experts are counted in shared memory and added to `counts`, which an earlier kernel has cleared (ALONE: one CTA writes them).
+// Bound by instructions: scores (two special functions an element), sorting, and about 20 for each round.
 // ---------------------------------------------------------------------------------------------
+constexpr int ctas_of(int n) { return n <= 8 ? 4 : n <= 16 ? 3 : 2; }  // a multiprocessor, of kThreads
+
 template <class T, int N, bool ALONE, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_route(const RouteKernelArgs a) {
-    extern __shared__ double memory[];  // groups: a row of keys for every warp; then the counts
+__global__ void __launch_bounds__(THREADS, ALONE ? 1 : ctas_of(N)) k_route(const __grid_constant__ RouteKernelArgs a) {
+    constexpr uint32_t kPlace = N - 1;
+    constexpr bool kSorted = N <= 16;  // longer lists: the maximum is looked for again in each round
+    constexpr float kLost = N * 0x1p-23f;
+    constexpr int V = 16 / sizeof(T);
+    extern __shared__ int counts[];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int staged_words = a.groups > 1 ? N * 33 : 0;
-    double* staged = memory + warp * staged_words;
-    int* counts = reinterpret_cast<int*>(memory + THREADS / 32 * staged_words);
-    if (ALONE) {
-        ptx::chained();
-    } else if (!a.counts) {
-        ptx::chained();
-    }  // else k_clear before it has waited for all that came before
+    if (ALONE || !a.counts) ptx::chained();  // else k_clear before it has waited for all that came before
     if (a.counts) {
         for (int e = threadIdx.x; e < a.experts; e += THREADS) counts[e] = 0;
         __syncthreads();
     }
-    const float off = a.bias || a.two_best ? (a.sigmoid ? 0x1p-22f : (N + 16) * 0x1p-24f) : 0.0f;
+    const int group = lane / a.share, skip = lane % a.share * a.per;
+    const int first = group * a.group_size + skip;
+    const int count = group < a.groups ? max(0, min(a.per, a.group_size - skip)) : 0;
+    float bias[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) bias[j] = a.bias && j < count ? a.bias[first + j] : 0.0f;
+    const bool scored = a.bias || a.two_best;
+    const float off = a.sigmoid ? 0x1p-21f : (N + 24) * 0x1p-24f;  // of a score: approximate exponential and reciprocal, sums of N + 5 terms
+    const bool exact = !a.bias;                                   // experts are ranked by their logits
+    const int rounds = exact && sizeof(T) == 2 ? a.k : a.k + 1;   // bf16 logits have no bits to lose
     for (int64_t token = (int64_t)blockIdx.x * (THREADS / 32) + warp; token < a.n; token += (int64_t)gridDim.x * (THREADS / 32)) {
         const T* row = static_cast<const T*>(a.logits) + token * a.pitch;
         float z[N];
+        if (N % V == 0 && a.wide) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int e = j * 32 + lane;
-            z[j] = e < a.experts ? logit(row[e]) : -INFINITY;
+            for (int j = 0; j < N; j += V) {
+                Pack<T, V> p;
+                if (j < count) p = *reinterpret_cast<const Pack<T, V>*>(row + first + j);
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (j + i < N) z[j + i] = j < count ? logit(p.v[i]) : -INFINITY;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) z[j] = j < count ? logit(row[first + j]) : -INFINITY;
         }
         float most = 0.0f, total = 1.0f;
-        if (!a.sigmoid && (off > 0.0f || !a.renormalize)) {
+        if (!a.sigmoid && (scored || !a.renormalize)) {
             most = z[0];
 #pragma unroll
             for (int j = 1; j < N; ++j) most = fmaxf(most, z[j]);
@@ -257,40 +207,88 @@ __global__ void __launch_bounds__(THREADS) k_route(const RouteKernelArgs a) {
             for (int j = 0; j < N; ++j) total += expf(z[j] - most);
             total = warp_sum(total);
         }
-        bool live[N];
-#pragma unroll
-        for (int j = 0; j < N; ++j) live[j] = z[j] > -INFINITY;
-        int mine;
-        auto same = [&](int p, int q) {  // equal in every respect: no rounding has made them so
-            return logit(row[p]) == logit(row[q]) && (!a.bias || a.bias[p] == a.bias[q]);
-        };
         bool doubt = false;
-        if (off > 0.0f) {
-            float key[N], rank_by[N];
+        uint32_t u[N];
+        float best = -INFINITY, second = -INFINITY;
+        if (scored) {
+            const float one = 1.0f / total;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                key[j] = a.sigmoid ? sigmoid(z[j]) : expf(z[j] - most) / total;
-                if (a.bias && live[j]) {
-                    key[j] += a.bias[j * 32 + lane];
-                    live[j] = key[j] > -INFINITY;  // a bias of -inf or NaN switches an expert off
-                    key[j] = fminf(key[j], FLT_MAX);
-                }
+                float key = (a.sigmoid ? __fdividef(1.0f, 1.0f + __expf(-z[j])) : __expf(z[j] - most) * one) + bias[j];
+                // a bias of -inf or NaN switches an expert off
+                const bool live = z[j] > -INFINITY && key > -INFINITY;
+                key = live ? fminf(key, FLT_MAX) : -INFINITY;
+                second = fmaxf(second, fminf(best, key));
+                best = fmaxf(best, key);
+                u[j] = !live ? 0u : (ordered(exact ? z[j] : key) & ~kPlace) | (kPlace - j);
             }
-            if (!a.bias) {
-#pragma unroll
-                for (int j = 0; j < N; ++j) rank_by[j] = z[j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j) rank_by[j] = key[j];
-            }
-            doubt = choose<float, N>(a, key, off, rank_by, a.bias ? off : 0.0f, live, reinterpret_cast<float*>(staged), mine, same);
         } else {
-            choose<float, N>(a, z, 0.0f, z, 0.0f, live, reinterpret_cast<float*>(staged), mine, same);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                best = fmaxf(best, z[j]);
+                u[j] = z[j] > -INFINITY ? (ordered(z[j]) & ~kPlace) | (kPlace - j) : 0u;
+            }
         }
-        if (doubt) {
-            __syncwarp();
-            mine = choose_in_doubt<T, N>(a, row, staged);
+        if (a.groups > 1) {
+            for (int d = a.share / 2; d > 0; d /= 2) {
+                const float b = __shfl_xor_sync(kAll, best, d), s = __shfl_xor_sync(kAll, second, d);
+                second = fmaxf(fminf(best, b), fmaxf(second, s));
+                best = fmaxf(best, b);
+            }
+            const float score = a.two_best && a.group_size > 1 ? best + second : best;
+            int place = 0;
+            for (int g = 0; g < a.groups; ++g) {
+                const float other = __shfl_sync(kAll, score, g * a.share);
+                place += other > score || (other == score && g < group);
+            }
+            if (scored && a.top_groups < a.groups) {
+                const unsigned in = __ballot_sync(kAll, group < a.groups && place == a.top_groups - 1), out = __ballot_sync(kAll, group < a.groups && place == a.top_groups);
+                const float last = __shfl_sync(kAll, score, __ffs(in) - 1), next = __shfl_sync(kAll, score, __ffs(out) - 1);
+                doubt = next > -INFINITY && !(last - next > 4.0f * off + fabsf(last) * 0x1p-21f);
+            }
+            if (place >= a.top_groups) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) u[j] = 0;
+            }
         }
+        if constexpr (kSorted) sort<N>(u);
+        auto head_of = [&] {
+            if constexpr (kSorted) return u[0];
+            uint32_t h = u[0];
+#pragma unroll
+            for (int j = 1; j < N; ++j) h = max(h, u[j]);
+            return h;
+        };
+        int mine = -1, last_expert = -1;
+        uint32_t head = head_of(), last = 0;
+        for (int r = 0; r < rounds; ++r) {
+            const uint32_t here = head & ~kPlace;
+            const uint32_t top = warp_max(here);
+            if (top == 0) break;
+            const int winner = __ffs(__ballot_sync(kAll, here == top)) - 1;
+            const int expert = __shfl_sync(kAll, first + (int)(kPlace - (head & kPlace)), winner);
+            if (r > 0) {
+                const float now = number(top);
+                const bool close = exact ? sizeof(T) == 4 && top == last : !(number(last) - now > 2.0f * off + fabsf(now) * (2.0f * kLost + 0x1p-22f));
+                // equal in every respect: no rounding has made them so
+                if (close && !(logit(row[last_expert]) == logit(row[expert]) && (!a.bias || a.bias[last_expert] == a.bias[expert]))) doubt = true;
+            }
+            last = top;
+            last_expert = expert;
+            if (r < a.k && lane == r) mine = expert;
+            if (lane == winner) {
+                if constexpr (kSorted) {
+#pragma unroll
+                    for (int j = 0; j + 1 < N; ++j) u[j] = u[j + 1];
+                    u[N - 1] = 0;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < N; ++j) u[j] = u[j] == head ? 0u : u[j];
+                }
+                head = head_of();
+            }
+        }
+        if (__any_sync(kAll, doubt)) mine = choose_in_doubt<T, N>(a, row, first, count);
         // lane j < k: the j-th expert's weight
         const bool chosen = mine >= 0;
         const float x = chosen ? logit(row[mine]) : -INFINITY;
@@ -337,34 +335,35 @@ __global__ void __launch_bounds__(1024) k_clear(int32_t* counts, int n) {
     if ((int)threadIdx.x < n) counts[threadIdx.x] = 0;
 }
 
+constexpr int64_t kAlone = 64;  // tokens of one CTA: four rounds of its 16 warps are as long as the launch that it saves
+
 template <class T, int N>
 cudaError_t launch_route(const RouteKernelArgs& a, cudaStream_t s) {
-    const size_t staged = a.groups > 1 ? (size_t)N * 33 * 8 : 0, counted = a.counts ? (size_t)a.experts * 4 : 0;
-    constexpr int64_t kAlone = N <= 8 ? 64 : 32;  // tokens of one CTA
-    if (a.n <= kAlone && N <= 8) {
-        constexpr int kMost = N <= 8 ? 512 : kThreads;
-        return launch_chained(k_route<T, N, true, kMost>, dim3(1), kMost, staged * (kMost / 32) + counted, s, a);
-    }
+    const size_t counted = a.counts ? (size_t)a.experts * 4 : 0;
+    if constexpr (N <= 8)
+        if (a.n <= kAlone) return launch_chained(k_route<T, N, true, 512>, dim3(1), 512, counted, s, a);
     if (a.counts) A2_CUDA_TRY(launch_chained(k_clear, dim3(1), 1024, 0, s, a.counts, a.experts));
-    const int64_t ctas = std::min<int64_t>(ceil_div(a.n, kWarps), (int64_t)multiprocessors() * (N <= 8 ? 8 : N <= 16 ? 4 : 2));
-    auto* kernel = k_route<T, N, false, kThreads>;
-    const size_t smem = staged * kWarps + counted;
-    if (smem > 48 * 1024)
-        A2_CUDA_TRY(cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    return launch_chained(kernel, dim3((unsigned)ctas), kThreads, smem, s, a);
+    const int64_t ctas = std::min<int64_t>(ceil_div(a.n, kWarps), (int64_t)multiprocessors() * ctas_of(N));
+    return launch_chained(k_route<T, N, false, kThreads>, dim3((unsigned)ctas), kThreads, counted, s, a);
 }
 
 template <class T>
 cudaError_t route_typed(const RouteArgs& r, cudaStream_t s) {
-    const RouteKernelArgs a{r.logits, r.logits_pitch, r.n, r.experts, r.k, r.score == A2_SCORE_SIGMOID, r.renormalize, r.bias, r.groups, r.experts / r.groups,
-                            r.top_groups, r.group_score == A2_GROUP_TWO_BEST && r.groups > 1, r.scale, r.ids, r.weights, r.counts};
-    const int places = (r.experts + 31) / 32;
-    if (places <= 1) return launch_route<T, 1>(a, s);
-    if (places <= 2) return launch_route<T, 2>(a, s);
-    if (places <= 4) return launch_route<T, 4>(a, s);
-    if (places <= 8) return launch_route<T, 8>(a, s);
-    if (places <= 16) return launch_route<T, 16>(a, s);
-    return launch_route<T, 32>(a, s);
+    const int size = r.experts / r.groups;
+    int share = 1;
+    while (share * 2 * r.groups <= 32) share *= 2;
+    const int per = (int)ceil_div(size, share);
+    constexpr int V = 16 / sizeof(T);
+    const bool wide = per % V == 0 && size % V == 0 && reinterpret_cast<uintptr_t>(r.logits) % 16 == 0 && r.logits_pitch % V == 0;
+    const RouteKernelArgs a{r.logits, r.logits_pitch, r.n, r.experts, r.k, r.score == A2_SCORE_SIGMOID, r.renormalize, r.bias, r.groups, size, r.top_groups, share, per,
+                            r.group_score == A2_GROUP_TWO_BEST && r.groups > 1, wide, r.scale, r.ids, r.weights, r.counts};
+    if (per <= 1) return launch_route<T, 1>(a, s);
+    if (per <= 2) return launch_route<T, 2>(a, s);
+    if (per <= 4) return launch_route<T, 4>(a, s);
+    if (per <= 8) return launch_route<T, 8>(a, s);
+    if (per <= 16) return launch_route<T, 16>(a, s);
+    if (per <= 32) return launch_route<T, 32>(a, s);
+    return launch_route<T, 64>(a, s);  // groups that leave up to half of the lanes idle
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -387,7 +386,7 @@ struct RouteGradKernelArgs {
 };
 
 template <class T, int N>
-__global__ void __launch_bounds__(kThreads) k_route_grad(const RouteGradKernelArgs a) {
+__global__ void __launch_bounds__(kThreads) k_route_grad(const __grid_constant__ RouteGradKernelArgs a) {
     ptx::chained();
     const int lane = threadIdx.x % 32;
     for (int64_t token = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; token < a.n; token += (int64_t)gridDim.x * kWarps) {
@@ -442,11 +441,9 @@ __global__ void __launch_bounds__(kThreads) k_route_grad(const RouteGradKernelAr
         for (int c = 0; c < a.k; ++c) {
             const int e = __shfl_sync(kAll, mine, c);
             const float v = __shfl_sync(kAll, h, c);
-            if (e >= 0 && e % 32 == lane) {
+            const int place = e >= 0 && e % 32 == lane ? e / 32 : N;
 #pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (j == e / 32) d[j] += v;
-            }
+            for (int j = 0; j < N; ++j) d[j] += j == place ? v : 0.0f;
         }
 #pragma unroll
         for (int j = 0; j < N; ++j) {
