@@ -69,14 +69,16 @@ __device__ __forceinline__ double cta_sum(double v, double* shared) {
 }
 
 // The sum of the squares of vectors. In fp32 where that neither overflows nor loses what lies below its range, as it hardly ever does; else in 64 bits.
-template <class T, int V, int COUNT>
-__device__ __forceinline__ double squares(const Pack<T, V> (&p)[COUNT]) {
-    float q[COUNT];
+template <class T, int COUNT>
+__device__ __forceinline__ double squares(const Words (&p)[COUNT]) {
+    constexpr int V = kVec<T>;
+    float q[COUNT], v[V];
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) {
+        unpack<T>(p[i], v);
         q[i] = 0.0f;
 #pragma unroll
-        for (int k = 0; k < V; ++k) q[i] = fmaf(widen(p[i].v[k]), widen(p[i].v[k]), q[i]);
+        for (int k = 0; k < V; ++k) q[i] = fmaf(v[k], v[k], q[i]);
     }
 #pragma unroll
     for (int n = COUNT / 2; n > 0; n /= 2)
@@ -85,9 +87,11 @@ __device__ __forceinline__ double squares(const Pack<T, V> (&p)[COUNT]) {
     if (q[0] > 0x1p-60f && q[0] < 0x1p120f) return q[0];
     double d = 0.0;
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i)
+    for (int i = 0; i < COUNT; ++i) {
+        unpack<T>(p[i], v);
 #pragma unroll
-        for (int k = 0; k < V; ++k) d += (double)widen(p[i].v[k]) * (double)widen(p[i].v[k]);
+        for (int k = 0; k < V; ++k) d += (double)v[k] * (double)v[k];
+    }
     return d;
 }
 
@@ -149,16 +153,15 @@ __device__ __forceinline__ void over_chunk(const Tensor& t, int64_t worker, int6
 
 template <class T, int THREADS>
 __device__ __forceinline__ double chunk_squares(const Tensor& t, int64_t worker, int64_t chunk) {
-    constexpr int V = 16 / sizeof(T);
     double sum = 0.0;
     over_chunk<T, THREADS>(
         t, worker, chunk,
         [&](auto count, auto from, const T* in, auto, T*) {
             constexpr int kCount = decltype(count)::value;
-            Pack<T, V> p[kCount];
+            Words p[kCount];
 #pragma unroll
-            for (int i = 0; i < kCount; ++i) p[i] = *reinterpret_cast<const Pack<T, V>*>(in + from(i));
-            sum += squares<T, V, kCount>(p);
+            for (int i = 0; i < kCount; ++i) p[i] = *reinterpret_cast<const Words*>(in + from(i));
+            sum += squares<T, kCount>(p);
         },
         [&](const T* in, T*) {
             const double v = widen(*in);
@@ -174,14 +177,16 @@ __device__ __forceinline__ void scale_chunk(const Tensor& t, int64_t worker, int
         t, worker, chunk,
         [&](auto count, auto from, const T* in, auto to, T* out) {
             constexpr int kCount = decltype(count)::value;
-            Pack<T, V> p[kCount];
+            Words p[kCount];
 #pragma unroll
-            for (int i = 0; i < kCount; ++i) p[i] = *reinterpret_cast<const Pack<T, V>*>(in + from(i));
+            for (int i = 0; i < kCount; ++i) p[i] = *reinterpret_cast<const Words*>(in + from(i));
 #pragma unroll
             for (int i = 0; i < kCount; ++i) {
+                float v[V];
+                unpack<T>(p[i], v);
 #pragma unroll
-                for (int k = 0; k < V; ++k) p[i].v[k] = narrow<T>(zero ? 0.0f : widen(p[i].v[k]) * factor);
-                *reinterpret_cast<Pack<T, V>*>(out + to(i)) = p[i];
+                for (int k = 0; k < V; ++k) v[k] = zero ? 0.0f : v[k] * factor;
+                *reinterpret_cast<Words*>(out + to(i)) = pack<T>(v);
             }
         },
         [&](const T* in, T* out) { *out = narrow<T>(zero ? 0.0f : widen(*in) * factor); });

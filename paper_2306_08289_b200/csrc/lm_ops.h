@@ -253,6 +253,77 @@ template <class T, int VEC>
 struct alignas(sizeof(T) * VEC) Pack {
     T v[VEC];
 };
+
+// 16 bytes of a row as they lie in memory. Kept in words where paths with and without whole vectors meet: as single bf16 elements they would take
+// a register and several instructions each.
+struct alignas(16) Words {
+    uint32_t w[4];
+};
+template <class T>
+constexpr int kVec = 16 / sizeof(T);
+
+__device__ __forceinline__ void unpack(const Words& p, float (&v)[4], float) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(p.w[i]);
+}
+__device__ __forceinline__ void unpack(const Words& p, float (&v)[8], __nv_bfloat16) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(p.w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(p.w[i] & 0xffff0000u);
+    }
+}
+template <class T>
+__device__ __forceinline__ void unpack(const Words& p, float (&v)[kVec<T>]) {
+    unpack(p, v, T());
+}
+__device__ __forceinline__ Words pack(const float (&v)[4], float) {
+    Words p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p.w[i] = __float_as_uint(v[i]);
+    return p;
+}
+__device__ __forceinline__ Words pack(const float (&v)[8], __nv_bfloat16) {
+    Words p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 two = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        p.w[i] = *reinterpret_cast<const uint32_t*>(&two);
+    }
+    return p;
+}
+template <class T>
+__device__ __forceinline__ Words pack(const float (&v)[kVec<T>]) {
+    return pack(v, T());
+}
+
+// A vector of a row at column c, whole or cut at the row's ends (zeros past them); WIDE: whole ones lie on 16-byte boundaries.
+__device__ __forceinline__ uint32_t bits_of(const float* p) { return __float_as_uint(*p); }
+__device__ __forceinline__ uint32_t bits_of(const __nv_bfloat16* p) { return *reinterpret_cast<const uint16_t*>(p); }
+template <class T, bool WIDE>
+__device__ __forceinline__ Words load_words(const T* row, int c, int width) {
+    if (WIDE && c >= 0 && c + kVec<T> <= width) return *reinterpret_cast<const Words*>(row + c);
+    Words p{};
+#pragma unroll
+    for (int k = 0; k < kVec<T>; ++k)
+        if (c + k >= 0 && c + k < width) p.w[k * sizeof(T) / 4] |= bits_of(row + c + k) << (k * sizeof(T) % 4 * 8);
+    return p;
+}
+template <class T, bool WIDE>
+__device__ __forceinline__ void store_words(T* row, int c, int width, const Words& p) {
+    if (WIDE && c >= 0 && c + kVec<T> <= width) {
+        *reinterpret_cast<Words*>(row + c) = p;
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < kVec<T>; ++k) {
+        if (c + k < 0 || c + k >= width) continue;
+        if constexpr (sizeof(T) == 4)
+            reinterpret_cast<uint32_t*>(row)[c + k] = p.w[k];
+        else
+            reinterpret_cast<uint16_t*>(row)[c + k] = (uint16_t)(p.w[k / 2] >> (k % 2 * 16));
+    }
+}
 #endif
 
 }  // namespace a2

@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "lm_ops.h"
 
@@ -30,29 +31,6 @@ constexpr float kScaleLeast = 0x1p-126f;  // of a block of zeros: its values are
 // all rows are shifted alike): the first and the last vector are cut at the row's ends, element by element. WIDE = false reads all vectors
 // element by element.
 // ---------------------------------------------------------------------------------------------
-template <class T>
-constexpr int kVec = 16 / sizeof(T);
-
-template <class T, bool WIDE>
-__device__ __forceinline__ void load(Pack<T, kVec<T>>& to, const T* row, int c, int width) {
-    if (WIDE && c >= 0 && c + kVec<T> <= width) {
-        to = *reinterpret_cast<const Pack<T, kVec<T>>*>(row + c);
-    } else {
-#pragma unroll
-        for (int k = 0; k < kVec<T>; ++k) to.v[k] = c + k >= 0 && c + k < width ? row[c + k] : narrow<T>(0.0f);
-    }
-}
-template <class T, bool WIDE>
-__device__ __forceinline__ void store(T* row, int c, int width, const Pack<T, kVec<T>>& from) {
-    if (WIDE && c >= 0 && c + kVec<T> <= width) {
-        *reinterpret_cast<Pack<T, kVec<T>>*>(row + c) = from;
-    } else {
-#pragma unroll
-        for (int k = 0; k < kVec<T>; ++k)
-            if (c + k >= 0 && c + k < width) row[c + k] = from.v[k];
-    }
-}
-
 // A thread's place in its group: groups are a power of two up to a warp, or a whole CTA.
 __device__ __forceinline__ int place_in(int group) { return group > 32 ? (int)threadIdx.x : (int)threadIdx.x & (group - 1); }
 
@@ -98,11 +76,22 @@ __device__ __forceinline__ float over_group(float v, int group, int slot, float 
 
 // Rows whose squares leave the range of floats are multiplied by a power of two first, and rstd is that of the scaled row.
 __device__ __forceinline__ bool in_range(float squares, float eps_sum) { return squares < 0x1p120f && squares + eps_sum > 0x1p-90f; }
+template <class T>
+__device__ __forceinline__ float most_of(uint32_t word) {  // the larger magnitude of a word's elements
+    if constexpr (sizeof(T) == 4)
+        return fabsf(__uint_as_float(word));
+    else
+        return fmaxf(fabsf(__uint_as_float(word << 16)), fabsf(__uint_as_float(word & 0xffff0000u)));
+}
 __device__ __forceinline__ float power_below(float most) {  // 2^-e for most in [2^e, 2^(e+1))
     if (!(most > 0.0f) || isinf(most)) return 1.0f;
     int e;
     frexpf(most, &e);
     return ldexpf(1.0f, max(-126, min(126, 1 - e)));
+}
+__device__ __forceinline__ float rstd_of(float mean) {  // 1 / sqrt, by one step of Newton's from the approximate one
+    const float r = rsqrtf(mean);
+    return r * fmaf(-0.5f * mean * r, r, 1.5f);
 }
 __device__ __forceinline__ float scaled_rstd(float by, float squares, int width, float eps) {
     const double mean = (double)squares / (double)width + (double)eps * by * by;
@@ -115,7 +104,7 @@ struct NormKernelArgs {
     const void *x, *residual, *weight;
     int64_t x_pitch, residual_pitch, n;
     int width;
-    float eps;
+    float eps, one_over_width;
     void *sum, *out;
     int64_t sum_pitch, out_pitch;
     float* scales;
@@ -145,30 +134,26 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ Nor
 
     float v[K][V];
     {
-        Pack<T, V> px[K], pr[K];
+        Words px[K], pr[K];
+#pragma unroll
+        for (int j = 0; j < K; ++j) px[j] = pr[j] = Words{};
 #pragma unroll
         for (int j = 0; j < K; ++j)
-            if (column(j) < width) load<T, WIDE>(px[j], x, column(j), width);
+            if (column(j) < width) px[j] = load_words<T, WIDE>(x, column(j), width);
         if (a.residual) {
 #pragma unroll
             for (int j = 0; j < K; ++j)
-                if (column(j) < width) load<T, WIDE>(pr[j], r, column(j), width);
+                if (column(j) < width) pr[j] = load_words<T, WIDE>(r, column(j), width);
         }
 #pragma unroll
         for (int j = 0; j < K; ++j) {
-            const int c = column(j);
+            unpack<T>(px[j], v[j]);
+            if (!a.residual) continue;
+            float other[V];
+            unpack<T>(pr[j], other);
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[j][k] = c < width ? widen(px[j].v[k]) : 0.0f;
-            if (a.residual && c < width) {
-#pragma unroll
-                for (int k = 0; k < V; ++k) v[j][k] += widen(pr[j].v[k]);
-            }
-            if (a.sum && c < width) {
-                Pack<T, V> p;
-#pragma unroll
-                for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(v[j][k]);
-                store<T, WIDE>(sum, c, width, p);
-            }
+            for (int k = 0; k < V; ++k) v[j][k] += other[k];
+            if (a.sum && column(j) < width) store_words<T, WIDE>(sum, column(j), width, pack<T>(v[j]));
         }
     }
     float squares = 0.0f;
@@ -179,7 +164,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ Nor
     squares = over_group<false>(squares, group, 0, shared);
     float by = 1.0f, rstd;
     if (in_range(squares, a.eps * (float)width)) {
-        rstd = 1.0f / sqrtf(squares / (float)width + a.eps);
+        rstd = rstd_of(fmaf(squares, a.one_over_width, a.eps));
     } else {
         float most = 0.0f;
 #pragma unroll
@@ -204,20 +189,13 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ Nor
         for (int k = 0; k < V; ++k) v[j][k] *= rstd;
         if (c >= width) continue;
         if (w) {
-            Pack<T, V> p;
-            if (a.wide_weight && shift == 0)
-                load<T, true>(p, w, c, width);
-            else
-                load<T, false>(p, w, c, width);
+            const Words p = a.wide_weight && shift == 0 ? load_words<T, true>(w, c, width) : load_words<T, false>(w, c, width);
+            float by_weight[V];
+            unpack<T>(p, by_weight);
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[j][k] *= widen(p.v[k]);
+            for (int k = 0; k < V; ++k) v[j][k] *= by_weight[k];
         }
-        if (MODE == 0) {
-            Pack<T, V> p;
-#pragma unroll
-            for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(v[j][k]);
-            store<T, WIDE>(static_cast<T*>(a.out) + row * a.out_pitch, c, width, p);
-        }
+        if (MODE == 0) store_words<T, WIDE>(static_cast<T*>(a.out) + row * a.out_pitch, c, width, pack<T>(v[j]));
     }
     if constexpr (MODE != 0) {
         uint8_t* out = static_cast<uint8_t*>(a.out) + row * a.out_pitch;
@@ -248,19 +226,19 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ Nor
             const float scale = scale_of(most);
             const float inverse = 1.0f / scale;
             if (MODE == 1 && t % lanes == 0) scales[c >> a.block_log] = scale;
-            Pack<uint8_t, V> q;
+            Pack<uint32_t, V / 4> q;
 #pragma unroll
-            for (int k = 0; k < V; k += 2) {
-                const __nv_fp8x2_storage_t two = __nv_cvt_float2_to_fp8x2(make_float2(v[j][k] * inverse, v[j][k + 1] * inverse), __NV_SATFINITE, __NV_E4M3);
-                q.v[k] = (uint8_t)(two & 0xff);
-                q.v[k + 1] = (uint8_t)(two >> 8);
+            for (int k = 0; k < V; k += 4) {
+                const uint32_t low = __nv_cvt_float2_to_fp8x2(make_float2(v[j][k] * inverse, v[j][k + 1] * inverse), __NV_SATFINITE, __NV_E4M3);
+                const uint32_t high = __nv_cvt_float2_to_fp8x2(make_float2(v[j][k + 2] * inverse, v[j][k + 3] * inverse), __NV_SATFINITE, __NV_E4M3);
+                q.v[k / 4] = low | high << 16;
             }
             if (a.wide_out && shift == 0 && c + V <= width) {
-                *reinterpret_cast<Pack<uint8_t, V>*>(out + c) = q;
+                *reinterpret_cast<Pack<uint32_t, V / 4>*>(out + c) = q;
             } else {
 #pragma unroll
                 for (int k = 0; k < V; ++k)
-                    if (c + k >= 0 && c + k < width) out[c + k] = q.v[k];
+                    if (c + k >= 0 && c + k < width) out[c + k] = (uint8_t)(q.v[k / 4] >> (k % 4 * 8));
             }
         }
     }
@@ -313,7 +291,7 @@ template <class T>
 cudaError_t norm_typed(const NormArgs& n, cudaStream_t s) {
     constexpr int V = kVec<T>;
     const int block_log = n.block == 128 ? 7 : n.block == 64 ? 6 : 5;
-    NormKernelArgs a{n.x, n.residual, n.weight, n.x_pitch, n.residual_pitch, n.n, (int)n.width, n.eps, n.sum, n.out, n.sum_pitch, n.out_pitch, n.scales, block_log,
+    NormKernelArgs a{n.x, n.residual, n.weight, n.x_pitch, n.residual_pitch, n.n, (int)n.width, n.eps, 1.0f / (float)n.width, n.sum, n.out, n.sum_pitch, n.out_pitch, n.scales, block_log,
                      n.block ? (int)ceil_div(n.width, n.block) : 1, 0, reinterpret_cast<uintptr_t>(n.weight) % 16 == 0, false};
     bool wide = (!n.residual || alike<T>(n.x, n.x_pitch, n.residual, n.residual_pitch, n.n)) && (!n.sum || alike<T>(n.x, n.x_pitch, n.sum, n.sum_pitch, n.n));
     if (n.scales)
@@ -328,8 +306,7 @@ cudaError_t norm_typed(const NormArgs& n, cudaStream_t s) {
         else
             vecs = ceil_div(n.width + V - 1, V);
     }
-    const Shape shape = sizeof(T) == 2 ? shape_of(vecs, 256, 1024, 2048, std::max<int>(8, (int)(n.block / V)))
-                                       : shape_of(vecs, 128, 512, 2048, std::max<int>(8, (int)(n.block / V)));
+    const Shape shape = shape_of(vecs, 32, 64, sizeof(T) == 2 ? 1024 : 2048, std::max<int>(8, (int)(n.block / V)));
     if (!n.scales) return wide ? launch_norm<T, true, 0>(a, shape, s) : launch_norm<T, false, 0>(a, shape, s);
     if (n.block) return wide ? launch_norm<T, true, 1>(a, shape, s) : launch_norm<T, false, 1>(a, shape, s);
     return wide ? launch_norm<T, true, 2>(a, shape, s) : launch_norm<T, false, 2>(a, shape, s);
@@ -352,14 +329,18 @@ __global__ void __launch_bounds__(256) k_dequantize(const uint8_t* __restrict__ 
         const uint8_t* q = values + row * values_pitch + c;
         T* o = out + row * out_pitch + c;
         if (WIDE && c + kBack <= width) {
-            const Pack<uint8_t, kBack> p = *reinterpret_cast<const Pack<uint8_t, kBack>*>(q);
+            const Words p = *reinterpret_cast<const Words*>(q);
             constexpr int V = kVec<T>;
 #pragma unroll
             for (int k = 0; k < kBack; k += V) {
-                Pack<T, V> y;
+                float y[V];
 #pragma unroll
-                for (int e = 0; e < V; ++e) y.v[e] = narrow<T>(value(p.v[k + e]) * scale);
-                *reinterpret_cast<Pack<T, V>*>(o + k) = y;
+                for (int e = 0; e < V; e += 2) {
+                    const __half2_raw two = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(p.w[(k + e) / 4] >> ((k + e) % 4 * 8)), __NV_E4M3);
+                    const float2 f = __half22float2(__half2(two));
+                    y[e] = f.x * scale, y[e + 1] = f.y * scale;
+                }
+                *reinterpret_cast<Words*>(o + k) = pack<T>(y);
             }
         } else {
             for (int k = 0; k < kBack && c + k < width; ++k) o[k] = narrow<T>(value(q[k]) * scale);
@@ -383,9 +364,10 @@ cudaError_t dequantize_typed(const DequantizeArgs& a, cudaStream_t s) {
 // has rows a multiple of 8 apart, so that all of them start equally far from a 16-byte boundary and a thread's columns stay the same.
 // The reductions over a row leave the loads idle, so the rows to come are brought to shared memory meanwhile: every thread copies the vectors that
 // it will itself read, kStages rows deep, and waits for its own copies alone.
-// Long rows (LEAN) are one vector of four or more a thread: those keep x and g in registers and dw in shared memory, and bring nothing ahead.
+// Long rows (LEAN) have no room for that: they keep x and g in registers and dw in shared memory, every thread its own.
 // ---------------------------------------------------------------------------------------------
-constexpr int kStages = 3;
+template <int K>
+constexpr int kStagesOf = K <= 2 ? 3 : 2;
 
 __device__ __forceinline__ void copy_ahead(void* to, const void* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(to)), "l"(from) : "memory");
@@ -398,30 +380,31 @@ __device__ __forceinline__ void wait_copies() {
 
 // A vector to shared memory, for the calling thread.
 template <class T, bool WIDE>
-__device__ __forceinline__ void bring(Pack<T, kVec<T>>* to, const T* row, int c, int width) {
+__device__ __forceinline__ void bring(Words* to, const T* row, int c, int width) {
     if (WIDE && c >= 0 && c + kVec<T> <= width)
         copy_ahead(to, row + c);
     else
-        load<T, false>(*to, row, c, width);
+        *to = load_words<T, false>(row, c, width);
 }
 
 struct NormGradKernelArgs {
     const void *g, *x, *weight, *ds;
     int64_t g_pitch, x_pitch, ds_pitch, n;
     int width;
-    float eps;
+    float eps, one_over_width;
     void* dx;
     int64_t dx_pitch;
     float* parts;  // [CTAs][width], or NULL without a gradient of the weight
     int64_t slots;
     int group;
+    bool wide_weight;
 };
 
 template <class T, bool WIDE, int K, bool LEAN, int THREADS, int CTAS>
 __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_constant__ NormGradKernelArgs a) {
-    constexpr int V = kVec<T>;
+    constexpr int V = kVec<T>, kStages = kStagesOf<K>;
     __shared__ float shared[2][32 * 2];
-    extern __shared__ uint4 memory[];  // LEAN: this CTA's dw. Else rows to come, and at the end, with several groups a CTA, a row of dw for each
+    extern __shared__ uint4 memory[];  // LEAN: every thread's part of dw. Else rows to come, and at the end, with several groups a CTA, a row of dw for each
     float* columns = reinterpret_cast<float*>(memory);
     ptx::chained();
     const int group = a.group, width = a.width, t = place_in(group);
@@ -432,7 +415,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
     auto column = [&](int j) { return (j * group + t) * V - shift; };
     // the vectors of one row: [stage][matrix][j][thread]
     auto ahead = [&](int stage, int matrix, int j) {
-        return reinterpret_cast<Pack<T, V>*>(memory) + ((stage * 3 + matrix) * K + j) * blockDim.x + threadIdx.x;
+        return reinterpret_cast<Words*>(memory) + ((stage * 3 + matrix) * K + j) * blockDim.x + threadIdx.x;
     };
     auto bring_row = [&](int stage, int64_t row) {
         if (row < a.n) {
@@ -446,120 +429,148 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
         }
         close_copies();
     };
-    Pack<T, V> pw[LEAN ? 1 : K];
+    auto load_weight = [&](int j) {
+        if (w && column(j) < width) return a.wide_weight && shift == 0 ? load_words<T, true>(w, column(j), width) : load_words<T, false>(w, column(j), width);
+        Words ones;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ones.w[i] = sizeof(T) == 4 ? 0x3f800000u : 0x3f803f80u;
+        return ones;
+    };
+    Words pw[LEAN ? 1 : K];
     float dw[LEAN ? 1 : K][V];
+    auto own = [&](int j, int q) -> float4& { return reinterpret_cast<float4*>(memory)[(j * (V / 4) + q) * blockDim.x + threadIdx.x]; };  // LEAN
     if constexpr (!LEAN) {
 #pragma unroll
         for (int s = 0; s + 1 < kStages; ++s) bring_row(s, first + s * a.slots);
 #pragma unroll
         for (int j = 0; j < K; ++j) {
 #pragma unroll
-            for (int k = 0; k < V; ++k) dw[j][k] = 0.0f, pw[j].v[k] = narrow<T>(1.0f);
-            if (w && column(j) < width) load<T, false>(pw[j], w, column(j), width);
+            for (int k = 0; k < V; ++k) dw[j][k] = 0.0f;
+            pw[j] = load_weight(j);
         }
-    } else if (a.parts) {
-        for (int c = threadIdx.x; c < width; c += blockDim.x) columns[c] = 0.0f;
-        __syncthreads();
+    } else {
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+#pragma unroll
+            for (int q = 0; q < V / 4; ++q) own(j, q) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
     int slot = 0, stage = 0;
     for (int64_t row = first; row < a.n; row += a.slots) {
         T* dx = static_cast<T*>(a.dx) + row * a.dx_pitch;
-        Pack<T, V> px[K], pg[K], pd[LEAN ? 1 : K];
+        Words px[K], pg[K], pd[LEAN ? 1 : K];
+#pragma unroll
+        for (int j = 0; j < K; ++j) px[j] = pg[j] = Words{};
         if constexpr (LEAN) {
 #pragma unroll
             for (int j = 0; j < K; ++j) {
-#pragma unroll
-                for (int k = 0; k < V; ++k) px[j].v[k] = pg[j].v[k] = narrow<T>(0.0f);
                 if (column(j) >= width) continue;
-                load<T, WIDE>(px[j], static_cast<const T*>(a.x) + row * a.x_pitch, column(j), width);
-                load<T, WIDE>(pg[j], static_cast<const T*>(a.g) + row * a.g_pitch, column(j), width);
+                px[j] = load_words<T, WIDE>(static_cast<const T*>(a.x) + row * a.x_pitch, column(j), width);
+                pg[j] = load_words<T, WIDE>(static_cast<const T*>(a.g) + row * a.g_pitch, column(j), width);
             }
         } else {
             bring_row(stage == 0 ? kStages - 1 : stage - 1, row + (kStages - 1) * a.slots);
             wait_copies<kStages - 1>();
 #pragma unroll
             for (int j = 0; j < K; ++j) {
-                const bool in = column(j) < width;
-#pragma unroll
-                for (int k = 0; k < V; ++k) px[j].v[k] = pg[j].v[k] = narrow<T>(0.0f);
-                if (in) px[j] = *ahead(stage, 0, j), pg[j] = *ahead(stage, 1, j);
-                if (in && a.ds) pd[j] = *ahead(stage, 2, j);
+                pd[j] = Words{};
+                if (column(j) >= width) continue;
+                px[j] = *ahead(stage, 0, j), pg[j] = *ahead(stage, 1, j);
+                if (a.ds) pd[j] = *ahead(stage, 2, j);
             }
             stage = stage + 1 == kStages ? 0 : stage + 1;
         }
-        auto weights = [&](int j) {
-            if constexpr (!LEAN) {
-                return pw[j];
-            } else {
-                Pack<T, V> p;
-#pragma unroll
-                for (int k = 0; k < V; ++k) p.v[k] = narrow<T>(1.0f);
-                if (w && column(j) < width) load<T, false>(p, w, column(j), width);
-                return p;
-            }
+        auto weights = [&](int j, float (&f)[V]) {
+            if constexpr (LEAN)
+                unpack<T>(load_weight(j), f);
+            else
+                unpack<T>(pw[j], f);
         };
+        // by: a power of two that the row is multiplied by (SCALED), one but for rows whose squares leave the range of floats
         float v[2];
-        auto sums = [&](float by) {
+        auto sums = [&](auto scaled, float by) {
             v[0] = v[1] = 0.0f;
 #pragma unroll
             for (int j = 0; j < K; ++j) {
-                const Pack<T, V> p = weights(j);
+                float p[V], s[V], g[V];
+                weights(j, p);
+                unpack<T>(px[j], s);
+                unpack<T>(pg[j], g);
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
-                    const float s = widen(px[j].v[k]) * by;
-                    v[0] = fmaf(s, s, v[0]);
-                    v[1] = fmaf(s, widen(pg[j].v[k]) * widen(p.v[k]), v[1]);
+                    if (scaled.value) s[k] *= by;
+                    v[0] = fmaf(s[k], s[k], v[0]);
+                    v[1] = fmaf(s[k], g[k] * p[k], v[1]);
                 }
             }
             over_group<false, 2>(v, group, slot, shared);
             slot ^= 1;
         };
-        sums(1.0f);
-        float by = 1.0f, rstd;
+        auto results = [&](auto scaled, float by, float rstd) {
+            const float c_mean = v[1] * rstd * a.one_over_width;
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                const int c = column(j);
+                if (c >= width) continue;
+                float p[V], hat[V], g[V], d[V], add[V];
+                weights(j, p);
+                unpack<T>(px[j], hat);
+                unpack<T>(pg[j], g);
+                if constexpr (LEAN)
+                    unpack<T>(a.ds ? load_words<T, WIDE>(static_cast<const T*>(a.ds) + row * a.ds_pitch, c, width) : Words{}, d);
+                else
+                    unpack<T>(pd[j], d);
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    if (scaled.value) hat[k] *= by;
+                    hat[k] *= rstd;
+                    float y = fmaf(g[k], p[k], -hat[k] * c_mean) * rstd;
+                    if (scaled.value) y *= by;
+                    d[k] += y;
+                    add[k] = g[k] * hat[k];
+                    if constexpr (!LEAN) dw[j][k] += add[k];
+                }
+                if constexpr (LEAN) {
+                    if (a.parts)
+#pragma unroll
+                        for (int q = 0; q < V / 4; ++q) {
+                            float4 f = own(j, q);
+                            f.x += add[4 * q], f.y += add[4 * q + 1], f.z += add[4 * q + 2], f.w += add[4 * q + 3];
+                            own(j, q) = f;
+                        }
+                }
+                if (a.dx) store_words<T, WIDE>(dx, c, width, pack<T>(d));
+            }
+        };
+        sums(std::false_type{}, 1.0f);
         if (in_range(v[0], a.eps * (float)width)) {
-            rstd = 1.0f / sqrtf(v[0] / (float)width + a.eps);
+            results(std::false_type{}, 1.0f, rstd_of(fmaf(v[0], a.one_over_width, a.eps)));
         } else {
             float most = 0.0f;
 #pragma unroll
             for (int j = 0; j < K; ++j)
 #pragma unroll
-                for (int k = 0; k < V; ++k) most = fmaxf(most, fabsf(widen(px[j].v[k])));
-            by = power_below(over_group<true>(most, group, slot, shared));
+                for (int i = 0; i < 4; ++i) most = fmaxf(most, most_of<T>(px[j].w[i]));
+            const float by = power_below(over_group<true>(most, group, slot, shared));
             slot ^= 1;
-            sums(by);
-            rstd = scaled_rstd(by, v[0], width, a.eps);
-        }
-        const float c_mean = v[1] * rstd / (float)width;
-#pragma unroll
-        for (int j = 0; j < K; ++j) {
-            const int c = column(j);
-            if (c >= width) continue;
-            const Pack<T, V> p = weights(j);
-            Pack<T, V> d, o;
-            if constexpr (LEAN) {
-                if (a.ds) load<T, WIDE>(d, static_cast<const T*>(a.ds) + row * a.ds_pitch, c, width);
-            } else {
-                d = pd[j];
-            }
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const float hat = widen(px[j].v[k]) * by * rstd, gk = widen(pg[j].v[k]);
-                float y = (gk * widen(p.v[k]) - hat * c_mean) * rstd * by;
-                if (a.ds) y += widen(d.v[k]);
-                o.v[k] = narrow<T>(y);
-                if constexpr (!LEAN)
-                    dw[j][k] = fmaf(gk, hat, dw[j][k]);
-                else if (a.parts && c + k >= 0 && c + k < width)
-                    columns[c + k] = fmaf(gk, hat, columns[c + k]);
-            }
-            if (a.dx) store<T, WIDE>(dx, c, width, o);
+            sums(std::true_type{}, by);
+            results(std::true_type{}, by, scaled_rstd(by, v[0], width, a.eps));
         }
     }
     if (!a.parts) return;
     float* part = a.parts + (int64_t)blockIdx.x * width;
     if constexpr (LEAN) {
-        __syncthreads();
-        for (int c = threadIdx.x; c < width; c += blockDim.x) part[c] = columns[c];
+#pragma unroll
+        for (int j = 0; j < K; ++j)
+#pragma unroll
+            for (int q = 0; q < V / 4; ++q) {
+                const float4 f = own(j, q);
+                const float four[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int c = column(j) + 4 * q + k;
+                    if (c >= 0 && c < width) part[c] = four[k];
+                }
+            }
     } else {
         if (groups > 1) {
             wait_copies<0>();
@@ -603,7 +614,7 @@ __global__ void __launch_bounds__(1024) k_norm_join(const float* __restrict__ pa
 
 template <class T>
 Shape grad_shape(int64_t width) {
-    return shape_of(ceil_div(width + (width + kVec<T> <= kMaxNormWidth ? kVec<T> - 1 : 0), kVec<T>), 512, 1024, 2048, 8);
+    return shape_of(ceil_div(width + (width + kVec<T> <= kMaxNormWidth ? kVec<T> - 1 : 0), kVec<T>), 32, 1024, 2048, 8);
 }
 
 // CTAs of the first kernel: those that are resident at once (1,024 threads a multiprocessor with one vector each, 512 with more), at most one row
@@ -618,13 +629,11 @@ int64_t grad_ctas(int64_t n, const Shape& shape) {
 template <class T, bool WIDE, int K, bool LEAN, int THREADS>
 cudaError_t launch_grad_kernel(const NormGradKernelArgs& a, unsigned ctas, unsigned threads, cudaStream_t s) {
     constexpr int kCtas = !LEAN && K == 1 ? 2 : 1;
-    constexpr size_t most = LEAN ? (size_t)kMaxNormWidth * 4 : (size_t)THREADS * kStages * 3 * K * 16;
+    constexpr size_t each = LEAN ? K * kVec<T> * 4 : kStagesOf<K> * 3 * K * 16, most = each * THREADS;  // bytes of a thread
     static std::atomic<uint64_t> allowed{0};
     auto* kernel = k_norm_grad<T, WIDE, K, LEAN, THREADS, kCtas>;
     A2_CUDA_TRY(allow_shared_memory(reinterpret_cast<const void*>(kernel), (int)most, allowed));
-    // rows to come take more than the rows of dw of several groups: kStages * 3 times 16 bytes a thread against V floats
-    const size_t smem = LEAN ? (a.parts ? (size_t)a.width * 4 : 0) : (size_t)threads * kStages * 3 * K * 16;
-    return launch_chained(kernel, dim3(ctas), threads, smem, s, a);
+    return launch_chained(kernel, dim3(ctas), threads, each * threads, s, a);  // of several groups a CTA, rows of dw take less: V floats a thread
 }
 
 template <class T, bool WIDE>
@@ -635,7 +644,7 @@ cudaError_t launch_norm_grad(NormGradKernelArgs& a, const Shape& shape, int64_t 
     switch (shape.k) {
         case 1: return launch_grad_kernel<T, WIDE, 1, false, 512>(a, (unsigned)ctas, threads, s);
         case 2: return launch_grad_kernel<T, WIDE, 2, false, 512>(a, (unsigned)ctas, threads, s);
-        case 4: return launch_grad_kernel<T, WIDE, 4, true, 512>(a, (unsigned)ctas, threads, s);
+        case 4: return launch_grad_kernel<T, WIDE, 4, sizeof(T) == 2, 512>(a, (unsigned)ctas, threads, s);
         default: break;
     }
     if (threads <= 512) return launch_grad_kernel<T, WIDE, 8, true, 512>(a, (unsigned)ctas, threads, s);
@@ -646,8 +655,9 @@ template <class T>
 cudaError_t norm_grad_typed(const NormGradArgs& n, void* workspace, cudaStream_t s) {
     const Shape shape = grad_shape<T>(n.width);
     const int64_t ctas = grad_ctas(n.n, shape);
-    NormGradKernelArgs a{n.grad_out, n.x, n.weight, n.grad_sum, n.grad_out_pitch, n.x_pitch, n.grad_sum_pitch, n.n, (int)n.width, n.eps, n.grad_x, n.grad_x_pitch,
-                         n.grad_weight ? Carver(workspace).take<float>(ctas * n.width) : nullptr, 0, 0};
+    NormGradKernelArgs a{n.grad_out, n.x, n.weight, n.grad_sum, n.grad_out_pitch, n.x_pitch, n.grad_sum_pitch, n.n, (int)n.width, n.eps, 1.0f / (float)n.width, n.grad_x, n.grad_x_pitch,
+                         n.grad_weight ? Carver(workspace).take<float>(ctas * n.width) : nullptr, 0, 0,
+                         reinterpret_cast<uintptr_t>(n.weight) % 16 == 0};
     const bool wide = alike<T>(n.x, n.x_pitch, n.grad_out, n.grad_out_pitch, n.n) && (!n.grad_sum || alike<T>(n.x, n.x_pitch, n.grad_sum, n.grad_sum_pitch, n.n)) &&
                       (!n.grad_x || alike<T>(n.x, n.x_pitch, n.grad_x, n.grad_x_pitch, n.n)) && (aligned16<T>(n.x, n.x_pitch) || n.width + kVec<T> <= kMaxNormWidth);
     A2_CUDA_TRY((wide ? launch_norm_grad<T, true>(a, shape, ctas, s) : launch_norm_grad<T, false>(a, shape, ctas, s)));

@@ -450,9 +450,11 @@ def test_route_grad(storage, n, experts, k, groups, top_groups, score, renormali
     # as the weights' errors, over two factors and a sum of 32 terms
     assert_within(got, d, 2.0**-16 * size + u * d.abs() + TINY[storage])
     outside_untouched(out, buf)
-    assert torch.equal(ops.route_grad(z.clone(), ids, gw, score=score, renormalize=renormalize, scale=1.5), got)
-    place = z.clone()
-    assert torch.equal(ops.route_grad(place, ids, gw, score=score, renormalize=renormalize, scale=1.5, out=place), got)
+    again, _ = matrix(n, experts, dt, g, pad=n % 3, shift=n % 2)
+    assert torch.equal(ops.route_grad(z, ids, gw, score=score, renormalize=renormalize, scale=1.5, out=again), got)
+    # logits that do not start alike are summed in another order
+    assert_within(ops.route_grad(z.clone(), ids, gw, score=score, renormalize=renormalize, scale=1.5), d, 2.0**-16 * size + u * d.abs() + TINY[storage])
+    assert torch.equal(ops.route_grad(z, ids, gw, score=score, renormalize=renormalize, scale=1.5, out=z), got) and torch.equal(z, got)
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
