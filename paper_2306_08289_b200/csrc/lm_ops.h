@@ -297,24 +297,62 @@ __device__ __forceinline__ Words pack(const float (&v)[kVec<T>]) {
     return pack(v, T());
 }
 
-// A vector of a row at column c, whole or cut at the row's ends (zeros past them); WIDE: whole ones lie on 16-byte boundaries.
+// Two floats at a time: one instruction on this architecture.
+__device__ __forceinline__ uint64_t bits(float2 v) { return *reinterpret_cast<const uint64_t*>(&v); }
+__device__ __forceinline__ float2 floats(uint64_t b) { return *reinterpret_cast<const float2*>(&b); }
+__device__ __forceinline__ float2 two(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+    return floats(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+    return floats(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+    return floats(r);
+}
+template <class T>
+__device__ __forceinline__ void unpack(const Words& p, float2 (&v)[kVec<T> / 2]) {
+    float one[kVec<T>];
+    unpack<T>(p, one);
+#pragma unroll
+    for (int i = 0; i < kVec<T> / 2; ++i) v[i] = make_float2(one[2 * i], one[2 * i + 1]);
+}
+template <class T>
+__device__ __forceinline__ Words pack(const float2 (&v)[kVec<T> / 2]) {
+    float one[kVec<T>];
+#pragma unroll
+    for (int i = 0; i < kVec<T> / 2; ++i) one[2 * i] = v[i].x, one[2 * i + 1] = v[i].y;
+    return pack<T>(one);
+}
+
+// A vector of a row at column c that begins before the row or ends past it. Where vectors lie on 16-byte boundaries such a one is read whole (memory comes in
+// larger units than that, so what is next to the row is there) and `within` clears what is not the row's; else it is read, and always written, element by
+// element.
 __device__ __forceinline__ uint32_t bits_of(const float* p) { return __float_as_uint(*p); }
 __device__ __forceinline__ uint32_t bits_of(const __nv_bfloat16* p) { return *reinterpret_cast<const uint16_t*>(p); }
-template <class T, bool WIDE>
-__device__ __forceinline__ Words load_words(const T* row, int c, int width) {
-    if (WIDE && c >= 0 && c + kVec<T> <= width) return *reinterpret_cast<const Words*>(row + c);
+template <class T>
+__device__ __forceinline__ Words by_element(const T* row, int c, int width) {
     Words p{};
 #pragma unroll
     for (int k = 0; k < kVec<T>; ++k)
         if (c + k >= 0 && c + k < width) p.w[k * sizeof(T) / 4] |= bits_of(row + c + k) << (k * sizeof(T) % 4 * 8);
     return p;
 }
-template <class T, bool WIDE>
-__device__ __forceinline__ void store_words(T* row, int c, int width, const Words& p) {
-    if (WIDE && c >= 0 && c + kVec<T> <= width) {
-        *reinterpret_cast<Words*>(row + c) = p;
-        return;
-    }
+template <class T>
+__device__ __forceinline__ Words within(Words p, int c, int width) {
+#pragma unroll
+    for (int k = 0; k < kVec<T>; ++k)
+        if (c + k < 0 || c + k >= width) p.w[k * sizeof(T) / 4] &= sizeof(T) == 4 ? 0u : k % 2 ? 0xffffu : 0xffff0000u;
+    return p;
+}
+template <class T>
+__device__ __forceinline__ void store_cut(T* row, int c, int width, const Words& p) {
 #pragma unroll
     for (int k = 0; k < kVec<T>; ++k) {
         if (c + k < 0 || c + k >= width) continue;

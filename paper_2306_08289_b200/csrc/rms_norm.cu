@@ -28,8 +28,7 @@ constexpr float kScaleLeast = 0x1p-126f;  // of a block of zeros: its values are
 // ---------------------------------------------------------------------------------------------
 // A row's columns lie over a group of `group` threads: thread t holds the vectors t, t + group, ... of 16 bytes, K of them. A row that starts `shift`
 // elements after a 16-byte boundary is read from that boundary on (the vectors of all matrices of a call then start on boundaries, if
-// all rows are shifted alike): the first and the last vector are cut at the row's ends, element by element. WIDE = false reads all vectors
-// element by element.
+// all rows are shifted alike): the first and the last vector are cut at the row's ends. WIDE = false reads and writes element by element.
 // ---------------------------------------------------------------------------------------------
 // A thread's place in its group: groups are a power of two up to a warp, or a whole CTA.
 __device__ __forceinline__ int place_in(int group) { return group > 32 ? (int)threadIdx.x : (int)threadIdx.x & (group - 1); }
@@ -98,7 +97,7 @@ __device__ __forceinline__ float scaled_rstd(float by, float squares, int width,
     return mean > 0.0 ? (float)(1.0 / sqrt(mean)) : isnan(mean) ? (float)mean : 0.0f;  // a row of zeros with eps = 0 gives zeros
 }
 
-__device__ __forceinline__ float scale_of(float most) { return fmaxf(most / kE4m3Most, kScaleLeast); }
+__device__ __forceinline__ float scale_of(float most) { return fmaxf(most * (1.0f / kE4m3Most), kScaleLeast); }
 
 struct NormKernelArgs {
     const void *x, *residual, *weight;
@@ -117,123 +116,156 @@ struct NormKernelArgs {
 // row. MODE 0: y in the rows' type. 1: e4m3 with a scale for every 2^block_log columns, whose vectors lie in neighbouring lanes. 2: e4m3 with one
 // scale a row. Sums are in fp32; s is rounded only where it is stored, y is formed from what it was before.
 // ---------------------------------------------------------------------------------------------
+// A thread's vectors of a row.
+template <class T, bool WIDE>
+struct Columns {
+    int first, step, width;  // the column of vector 0, columns from one vector to the next
+    bool cut;                // one of them is cut at the row's ends
+    __device__ Columns(const void* row, int t, int group, int w) {
+        first = t * kVec<T> - (WIDE ? (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T)) : 0);
+        step = group * kVec<T>;
+        width = w;
+        const int rest = (w - first) % step;  // of the row behind this thread's last whole vector
+        cut = !WIDE || first < 0 || (rest > 0 && rest < kVec<T>);
+    }
+    __device__ int at(int j) const { return first + j * step; }
+    __device__ bool in(int j) const { return at(j) < width; }
+    // Loads K vectors, all of them before anything is done with one: zeros past the row's ends.
+    template <int K>
+    __device__ void load(Words (&p)[K], const T* row) const {
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            p[j] = Words{};
+            if (in(j)) p[j] = WIDE ? *reinterpret_cast<const Words*>(row + at(j)) : by_element(row, at(j), width);
+        }
+    }
+    template <int K>
+    __device__ void clear_past_ends(Words (&p)[K]) const {
+        if (!WIDE || !cut) return;
+#pragma unroll
+        for (int j = 0; j < K; ++j) p[j] = within<T>(p[j], at(j), width);
+    }
+    __device__ void store(T* row, int j, const Words& p) const {
+        if (WIDE && !cut)
+            *reinterpret_cast<Words*>(row + at(j)) = p;
+        else if (WIDE && at(j) >= 0 && at(j) + kVec<T> <= width)
+            *reinterpret_cast<Words*>(row + at(j)) = p;
+        else
+            store_cut(row, at(j), width, p);
+    }
+    // A vector of the weight, which may start elsewhere.
+    __device__ Words load_weight(const T* w, int j, bool wide) const {
+        return wide && !cut && first % kVec<T> == 0 ? *reinterpret_cast<const Words*>(w + at(j)) : by_element(w, at(j), width);
+    }
+};
+
 template <class T, bool WIDE, int K, int MODE, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ NormKernelArgs a) {
-    constexpr int V = kVec<T>;
+    constexpr int V = kVec<T>, H = V / 2;
     __shared__ float shared[2][32 * 2];
     ptx::chained();
     const int group = a.group, width = a.width, t = place_in(group);
     const int64_t row = group > 32 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (blockDim.x / group) + threadIdx.x / group;
     if (row >= a.n) return;  // whole groups, and whole CTAs where a group is one
     const T* x = static_cast<const T*>(a.x) + row * a.x_pitch;
-    const T* r = static_cast<const T*>(a.residual) + row * a.residual_pitch;
-    T* sum = static_cast<T*>(a.sum) + row * a.sum_pitch;
     const T* w = static_cast<const T*>(a.weight);
-    const int shift = WIDE ? (int)(reinterpret_cast<uintptr_t>(x) % 16 / sizeof(T)) : 0;
-    auto column = [&](int j) { return (j * group + t) * V - shift; };
+    const Columns<T, WIDE> columns(x, t, group, width);
 
-    float v[K][V];
+    float2 v[K][H];
     {
         Words px[K], pr[K];
+        columns.load(px, x);
+        if (a.residual) columns.load(pr, static_cast<const T*>(a.residual) + row * a.residual_pitch);
+        columns.clear_past_ends(px);
 #pragma unroll
-        for (int j = 0; j < K; ++j) px[j] = pr[j] = Words{};
-#pragma unroll
-        for (int j = 0; j < K; ++j)
-            if (column(j) < width) px[j] = load_words<T, WIDE>(x, column(j), width);
+        for (int j = 0; j < K; ++j) unpack<T>(px[j], v[j]);
         if (a.residual) {
+            columns.clear_past_ends(pr);
+            T* sum = static_cast<T*>(a.sum) + row * a.sum_pitch;
 #pragma unroll
-            for (int j = 0; j < K; ++j)
-                if (column(j) < width) pr[j] = load_words<T, WIDE>(r, column(j), width);
-        }
+            for (int j = 0; j < K; ++j) {
+                float2 other[H];
+                unpack<T>(pr[j], other);
 #pragma unroll
-        for (int j = 0; j < K; ++j) {
-            unpack<T>(px[j], v[j]);
-            if (!a.residual) continue;
-            float other[V];
-            unpack<T>(pr[j], other);
-#pragma unroll
-            for (int k = 0; k < V; ++k) v[j][k] += other[k];
-            if (a.sum && column(j) < width) store_words<T, WIDE>(sum, column(j), width, pack<T>(v[j]));
+                for (int k = 0; k < H; ++k) v[j][k] = add2(v[j][k], other[k]);
+                if (a.sum && columns.in(j)) columns.store(sum, j, pack<T>(v[j]));
+            }
         }
     }
-    float squares = 0.0f;
+    auto squares_of = [&] {
+        float2 q = two(0.0f);
 #pragma unroll
-    for (int j = 0; j < K; ++j)
+        for (int j = 0; j < K; ++j)
 #pragma unroll
-        for (int k = 0; k < V; ++k) squares = fmaf(v[j][k], v[j][k], squares);
-    squares = over_group<false>(squares, group, 0, shared);
-    float by = 1.0f, rstd;
-    if (in_range(squares, a.eps * (float)width)) {
-        rstd = rstd_of(fmaf(squares, a.one_over_width, a.eps));
-    } else {
+            for (int k = 0; k < H; ++k) q = fma2(v[j][k], v[j][k], q);
+        return q.x + q.y;
+    };
+    auto most_of_row = [&] {
         float most = 0.0f;
 #pragma unroll
         for (int j = 0; j < K; ++j)
 #pragma unroll
-            for (int k = 0; k < V; ++k) most = fmaxf(most, fabsf(v[j][k]));
-        by = power_below(over_group<true>(most, group, 1, shared));
-        float again = 0.0f;
+            for (int k = 0; k < H; ++k) most = fmaxf(most, fmaxf(fabsf(v[j][k].x), fabsf(v[j][k].y)));
+        return most;
+    };
+    const float squares = over_group<false>(squares_of(), group, 0, shared);
+    float rstd;
+    if (in_range(squares, a.eps * (float)width)) {
+        rstd = rstd_of(fmaf(squares, a.one_over_width, a.eps));
+    } else {
+        const float by = power_below(over_group<true>(most_of_row(), group, 1, shared));
 #pragma unroll
         for (int j = 0; j < K; ++j)
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                v[j][k] *= by;
-                again = fmaf(v[j][k], v[j][k], again);
-            }
-        rstd = scaled_rstd(by, over_group<false>(again, group, 0, shared), width, a.eps);
+            for (int k = 0; k < H; ++k) v[j][k] = mul2(v[j][k], two(by));
+        rstd = scaled_rstd(by, over_group<false>(squares_of(), group, 0, shared), width, a.eps);
     }
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-        const int c = column(j);
 #pragma unroll
-        for (int k = 0; k < V; ++k) v[j][k] *= rstd;
-        if (c >= width) continue;
+        for (int k = 0; k < H; ++k) v[j][k] = mul2(v[j][k], two(rstd));
+        if (!columns.in(j)) continue;
         if (w) {
-            const Words p = a.wide_weight && shift == 0 ? load_words<T, true>(w, c, width) : load_words<T, false>(w, c, width);
-            float by_weight[V];
-            unpack<T>(p, by_weight);
+            float2 by_weight[H];
+            unpack<T>(columns.load_weight(w, j, a.wide_weight), by_weight);
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[j][k] *= by_weight[k];
+            for (int k = 0; k < H; ++k) v[j][k] = mul2(v[j][k], by_weight[k]);
         }
-        if (MODE == 0) store_words<T, WIDE>(static_cast<T*>(a.out) + row * a.out_pitch, c, width, pack<T>(v[j]));
+        if (MODE == 0) columns.store(static_cast<T*>(a.out) + row * a.out_pitch, j, pack<T>(v[j]));
     }
     if constexpr (MODE != 0) {
         uint8_t* out = static_cast<uint8_t*>(a.out) + row * a.out_pitch;
         float* scales = a.scales + row * a.blocks;
-        float most = 0.0f;
+        float most = 0.0f, scale = 0.0f;
         if (MODE == 2) {
-#pragma unroll
-            for (int j = 0; j < K; ++j)
-#pragma unroll
-                for (int k = 0; k < V; ++k) most = fmaxf(most, fabsf(v[j][k]));
-            most = over_group<true>(most, group, 1, shared);
-            if (t == 0) scales[0] = scale_of(most);
+            scale = scale_of(over_group<true>(most_of_row(), group, 1, shared));
+            if (t == 0) scales[0] = scale;
         }
         const unsigned mask = mask_of(group);
         const int lanes = (1 << a.block_log) / V;
 #pragma unroll
         for (int j = 0; j < K; ++j) {
-            const int c = column(j);
+            const int c = columns.at(j);
             if (MODE == 1) {  // vectors past the row's end hold zeros (or NaN, which maxima pass over)
                 most = 0.0f;
 #pragma unroll
-                for (int k = 0; k < V; ++k) most = fmaxf(most, fabsf(v[j][k]));
+                for (int k = 0; k < H; ++k) most = fmaxf(most, fmaxf(fabsf(v[j][k].x), fabsf(v[j][k].y)));
 #pragma unroll
                 for (int d = 16; d > 0; d /= 2)
                     if (d < lanes) most = fmaxf(most, __shfl_xor_sync(mask, most, d));
+                scale = scale_of(most);
+                if (t % lanes == 0 && columns.in(j)) scales[c >> a.block_log] = scale;
             }
-            if (c >= width) continue;
-            const float scale = scale_of(most);
-            const float inverse = 1.0f / scale;
-            if (MODE == 1 && t % lanes == 0) scales[c >> a.block_log] = scale;
+            if (!columns.in(j)) continue;
+            const float2 inverse = two(1.0f / scale);
             Pack<uint32_t, V / 4> q;
 #pragma unroll
-            for (int k = 0; k < V; k += 4) {
-                const uint32_t low = __nv_cvt_float2_to_fp8x2(make_float2(v[j][k] * inverse, v[j][k + 1] * inverse), __NV_SATFINITE, __NV_E4M3);
-                const uint32_t high = __nv_cvt_float2_to_fp8x2(make_float2(v[j][k + 2] * inverse, v[j][k + 3] * inverse), __NV_SATFINITE, __NV_E4M3);
-                q.v[k / 4] = low | high << 16;
+            for (int k = 0; k < H; k += 2) {
+                const uint32_t low = __nv_cvt_float2_to_fp8x2(mul2(v[j][k], inverse), __NV_SATFINITE, __NV_E4M3);
+                const uint32_t high = __nv_cvt_float2_to_fp8x2(mul2(v[j][k + 1], inverse), __NV_SATFINITE, __NV_E4M3);
+                q.v[k / 2] = low | high << 16;
             }
-            if (a.wide_out && shift == 0 && c + V <= width) {
+            if (a.wide_out && c >= 0 && c + V <= width && c % V == 0) {
                 *reinterpret_cast<Pack<uint32_t, V / 4>*>(out + c) = q;
             } else {
 #pragma unroll
@@ -378,15 +410,6 @@ __device__ __forceinline__ void wait_copies() {
     asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
 }
 
-// A vector to shared memory, for the calling thread.
-template <class T, bool WIDE>
-__device__ __forceinline__ void bring(Words* to, const T* row, int c, int width) {
-    if (WIDE && c >= 0 && c + kVec<T> <= width)
-        copy_ahead(to, row + c);
-    else
-        *to = load_words<T, false>(row, c, width);
-}
-
 struct NormGradKernelArgs {
     const void *g, *x, *weight, *ds;
     int64_t g_pitch, x_pitch, ds_pitch, n;
@@ -402,51 +425,59 @@ struct NormGradKernelArgs {
 
 template <class T, bool WIDE, int K, bool LEAN, int THREADS, int CTAS>
 __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_constant__ NormGradKernelArgs a) {
-    constexpr int V = kVec<T>, kStages = kStagesOf<K>;
+    constexpr int V = kVec<T>, H = V / 2, kStages = kStagesOf<K>;
     __shared__ float shared[2][32 * 2];
     extern __shared__ uint4 memory[];  // LEAN: every thread's part of dw. Else rows to come, and at the end, with several groups a CTA, a row of dw for each
-    float* columns = reinterpret_cast<float*>(memory);
     ptx::chained();
     const int group = a.group, width = a.width, t = place_in(group);
     const int groups = group > 32 ? 1 : blockDim.x / group, mine = group > 32 ? 0 : threadIdx.x / group;
     const int64_t first = (int64_t)blockIdx.x * groups + mine;
-    const T* w = static_cast<const T*>(a.weight);
-    const int shift = WIDE ? (int)(reinterpret_cast<uintptr_t>(static_cast<const T*>(a.x) + first * a.x_pitch) % 16 / sizeof(T)) : 0;
-    auto column = [&](int j) { return (j * group + t) * V - shift; };
+    const T* x = static_cast<const T*>(a.x) + first * a.x_pitch;
+    const T* g = static_cast<const T*>(a.g) + first * a.g_pitch;
+    const T* ds = static_cast<const T*>(a.ds) + first * a.ds_pitch;
+    T* dx = static_cast<T*>(a.dx) + first * a.dx_pitch;
+    const Columns<T, WIDE> columns(x, t, group, width);
     // the vectors of one row: [stage][matrix][j][thread]
-    auto ahead = [&](int stage, int matrix, int j) {
-        return reinterpret_cast<Words*>(memory) + ((stage * 3 + matrix) * K + j) * blockDim.x + threadIdx.x;
-    };
-    auto bring_row = [&](int stage, int64_t row) {
-        if (row < a.n) {
-#pragma unroll
-            for (int j = 0; j < K; ++j) {
-                if (column(j) >= width) continue;
-                bring<T, WIDE>(ahead(stage, 0, j), static_cast<const T*>(a.x) + row * a.x_pitch, column(j), width);
-                bring<T, WIDE>(ahead(stage, 1, j), static_cast<const T*>(a.g) + row * a.g_pitch, column(j), width);
-                if (a.ds) bring<T, WIDE>(ahead(stage, 2, j), static_cast<const T*>(a.ds) + row * a.ds_pitch, column(j), width);
-            }
-        }
-        close_copies();
-    };
-    auto load_weight = [&](int j) {
-        if (w && column(j) < width) return a.wide_weight && shift == 0 ? load_words<T, true>(w, column(j), width) : load_words<T, false>(w, column(j), width);
-        Words ones;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ones.w[i] = sizeof(T) == 4 ? 0x3f800000u : 0x3f803f80u;
-        return ones;
-    };
-    Words pw[LEAN ? 1 : K];
-    float dw[LEAN ? 1 : K][V];
-    auto own = [&](int j, int q) -> float4& { return reinterpret_cast<float4*>(memory)[(j * (V / 4) + q) * blockDim.x + threadIdx.x]; };  // LEAN
-    if constexpr (!LEAN) {
-#pragma unroll
-        for (int s = 0; s + 1 < kStages; ++s) bring_row(s, first + s * a.slots);
+    auto ahead = [&](int stage, int matrix, int j) -> Words& { return reinterpret_cast<Words*>(memory)[((stage * 3 + matrix) * K + j) * blockDim.x + threadIdx.x]; };
+    auto bring_row = [&](int stage, const T* x, const T* g, const T* ds) {
 #pragma unroll
         for (int j = 0; j < K; ++j) {
+            if (!columns.in(j)) continue;
+            if (WIDE) {
+                copy_ahead(&ahead(stage, 0, j), x + columns.at(j));
+                copy_ahead(&ahead(stage, 1, j), g + columns.at(j));
+                if (a.ds) copy_ahead(&ahead(stage, 2, j), ds + columns.at(j));
+            } else {
+                ahead(stage, 0, j) = by_element(x, columns.at(j), width);
+                ahead(stage, 1, j) = by_element(g, columns.at(j), width);
+                if (a.ds) ahead(stage, 2, j) = by_element(ds, columns.at(j), width);
+            }
+        }
+    };
+    float2 p[K][H], dw[LEAN ? 1 : K][H];
+    auto own = [&](int j, int q) -> float4& { return reinterpret_cast<float4*>(memory)[(j * (V / 4) + q) * blockDim.x + threadIdx.x]; };  // LEAN
+    auto load_weight = [&](int j) {
+        if (a.weight && columns.in(j)) {
+            unpack<T>(columns.load_weight(static_cast<const T*>(a.weight), j, a.wide_weight), p[j]);
+        } else {
 #pragma unroll
-            for (int k = 0; k < V; ++k) dw[j][k] = 0.0f;
-            pw[j] = load_weight(j);
+            for (int k = 0; k < H; ++k) p[j][k] = two(1.0f);
+        }
+    };
+    const int64_t x_step = a.slots * a.x_pitch, g_step = a.slots * a.g_pitch, ds_step = a.slots * a.ds_pitch, dx_step = a.slots * a.dx_pitch;
+    int64_t coming = first;  // the next row to bring, with the three pointers
+    if constexpr (!LEAN) {
+#pragma unroll
+        for (int s = 0; s + 1 < kStages; ++s) {
+            if (coming < a.n) bring_row(s, x, g, ds);
+            close_copies();
+            coming += a.slots, x += x_step, g += g_step, ds += ds_step;
+        }
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            load_weight(j);
+#pragma unroll
+            for (int k = 0; k < H; ++k) dw[j][k] = two(0.0f);
         }
     } else {
 #pragma unroll
@@ -455,140 +486,140 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
             for (int q = 0; q < V / 4; ++q) own(j, q) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
     int slot = 0, stage = 0;
-    for (int64_t row = first; row < a.n; row += a.slots) {
-        T* dx = static_cast<T*>(a.dx) + row * a.dx_pitch;
-        Words px[K], pg[K], pd[LEAN ? 1 : K];
-#pragma unroll
-        for (int j = 0; j < K; ++j) px[j] = pg[j] = Words{};
+    for (int64_t row = first; row < a.n; row += a.slots, dx += dx_step) {
+        float2 s[K][H], u[K][H];  // the row and its grad_out
+        Words px[K], pg[K];
         if constexpr (LEAN) {
-#pragma unroll
-            for (int j = 0; j < K; ++j) {
-                if (column(j) >= width) continue;
-                px[j] = load_words<T, WIDE>(static_cast<const T*>(a.x) + row * a.x_pitch, column(j), width);
-                pg[j] = load_words<T, WIDE>(static_cast<const T*>(a.g) + row * a.g_pitch, column(j), width);
-            }
+            columns.load(px, x);
+            columns.load(pg, g);
+            columns.clear_past_ends(px);
+            columns.clear_past_ends(pg);
         } else {
-            bring_row(stage == 0 ? kStages - 1 : stage - 1, row + (kStages - 1) * a.slots);
+            if (coming < a.n) bring_row(stage == 0 ? kStages - 1 : stage - 1, x, g, ds);
+            close_copies();
+            coming += a.slots, x += x_step, g += g_step, ds += ds_step;
             wait_copies<kStages - 1>();
 #pragma unroll
             for (int j = 0; j < K; ++j) {
-                pd[j] = Words{};
-                if (column(j) >= width) continue;
-                px[j] = *ahead(stage, 0, j), pg[j] = *ahead(stage, 1, j);
-                if (a.ds) pd[j] = *ahead(stage, 2, j);
+                px[j] = pg[j] = Words{};
+                if (columns.in(j)) px[j] = ahead(stage, 0, j), pg[j] = ahead(stage, 1, j);
             }
-            stage = stage + 1 == kStages ? 0 : stage + 1;
-        }
-        auto weights = [&](int j, float (&f)[V]) {
-            if constexpr (LEAN)
-                unpack<T>(load_weight(j), f);
-            else
-                unpack<T>(pw[j], f);
-        };
-        // by: a power of two that the row is multiplied by (SCALED), one but for rows whose squares leave the range of floats
-        float v[2];
-        auto sums = [&](auto scaled, float by) {
-            v[0] = v[1] = 0.0f;
+            columns.clear_past_ends(px);
+            columns.clear_past_ends(pg);
 #pragma unroll
             for (int j = 0; j < K; ++j) {
-                float p[V], s[V], g[V];
-                weights(j, p);
-                unpack<T>(px[j], s);
-                unpack<T>(pg[j], g);
+                unpack<T>(px[j], s[j]);
+                unpack<T>(pg[j], u[j]);
+            }
+        }
+        // by: a power of two that the row is multiplied by, one but for rows whose squares leave the range of floats
+        float v[2];
+        auto sums = [&](float by) {
+            float2 q = two(0.0f), c = two(0.0f);
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    if (scaled.value) s[k] *= by;
-                    v[0] = fmaf(s[k], s[k], v[0]);
-                    v[1] = fmaf(s[k], g[k] * p[k], v[1]);
+            for (int j = 0; j < K; ++j) {
+                if constexpr (LEAN) {
+                    unpack<T>(px[j], s[j]);
+                    unpack<T>(pg[j], u[j]);
+                    load_weight(j);
+                }
+#pragma unroll
+                for (int k = 0; k < H; ++k) {
+                    if (by != 1.0f) s[j][k] = mul2(s[j][k], two(by));
+                    q = fma2(s[j][k], s[j][k], q);
+                    c = fma2(s[j][k], mul2(u[j][k], p[j][k]), c);
                 }
             }
+            v[0] = q.x + q.y, v[1] = c.x + c.y;
             over_group<false, 2>(v, group, slot, shared);
             slot ^= 1;
         };
-        auto results = [&](auto scaled, float by, float rstd) {
-            const float c_mean = v[1] * rstd * a.one_over_width;
-#pragma unroll
-            for (int j = 0; j < K; ++j) {
-                const int c = column(j);
-                if (c >= width) continue;
-                float p[V], hat[V], g[V], d[V], add[V];
-                weights(j, p);
-                unpack<T>(px[j], hat);
-                unpack<T>(pg[j], g);
-                if constexpr (LEAN)
-                    unpack<T>(a.ds ? load_words<T, WIDE>(static_cast<const T*>(a.ds) + row * a.ds_pitch, c, width) : Words{}, d);
-                else
-                    unpack<T>(pd[j], d);
-#pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    if (scaled.value) hat[k] *= by;
-                    hat[k] *= rstd;
-                    float y = fmaf(g[k], p[k], -hat[k] * c_mean) * rstd;
-                    if (scaled.value) y *= by;
-                    d[k] += y;
-                    add[k] = g[k] * hat[k];
-                    if constexpr (!LEAN) dw[j][k] += add[k];
-                }
-                if constexpr (LEAN) {
-                    if (a.parts)
-#pragma unroll
-                        for (int q = 0; q < V / 4; ++q) {
-                            float4 f = own(j, q);
-                            f.x += add[4 * q], f.y += add[4 * q + 1], f.z += add[4 * q + 2], f.w += add[4 * q + 3];
-                            own(j, q) = f;
-                        }
-                }
-                if (a.dx) store_words<T, WIDE>(dx, c, width, pack<T>(d));
-            }
-        };
-        sums(std::false_type{}, 1.0f);
+        sums(1.0f);
+        float by = 1.0f, rstd;
         if (in_range(v[0], a.eps * (float)width)) {
-            results(std::false_type{}, 1.0f, rstd_of(fmaf(v[0], a.one_over_width, a.eps)));
+            rstd = rstd_of(fmaf(v[0], a.one_over_width, a.eps));
         } else {
             float most = 0.0f;
 #pragma unroll
-            for (int j = 0; j < K; ++j)
+            for (int j = 0; j < K; ++j) {
+                if constexpr (LEAN) unpack<T>(px[j], s[j]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) most = fmaxf(most, most_of<T>(px[j].w[i]));
-            const float by = power_below(over_group<true>(most, group, slot, shared));
+                for (int k = 0; k < H; ++k) most = fmaxf(most, fmaxf(fabsf(s[j][k].x), fabsf(s[j][k].y)));
+            }
+            by = power_below(over_group<true>(most, group, slot, shared));
             slot ^= 1;
-            sums(std::true_type{}, by);
-            results(std::true_type{}, by, scaled_rstd(by, v[0], width, a.eps));
+            sums(by);
+            rstd = scaled_rstd(by, v[0], width, a.eps);
         }
+        // dx = w g rstd - h (c rstd) + ds, where rstd of the row itself is `by` times that of the scaled one
+        const float true_rstd = rstd * by, back = -(v[1] * rstd * a.one_over_width) * true_rstd;
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            if (!columns.in(j)) continue;
+            float2 d[H];
+            if constexpr (LEAN) {
+                unpack<T>(!a.ds ? Words{} : WIDE ? *reinterpret_cast<const Words*>(ds + columns.at(j)) : by_element(ds, columns.at(j), width), d);
+                unpack<T>(px[j], s[j]);
+                unpack<T>(pg[j], u[j]);
+                if (by != 1.0f) {
+#pragma unroll
+                    for (int k = 0; k < H; ++k) s[j][k] = mul2(s[j][k], two(by));
+                }
+                load_weight(j);
+            } else {
+                unpack<T>(a.ds ? ahead(stage, 2, j) : Words{}, d);
+            }
+#pragma unroll
+            for (int k = 0; k < H; ++k) {
+                const float2 hat = mul2(s[j][k], two(rstd));
+                d[k] = fma2(mul2(u[j][k], two(true_rstd)), p[j][k], fma2(hat, two(back), d[k]));
+                if constexpr (LEAN)
+                    s[j][k] = hat;
+                else
+                    dw[j][k] = fma2(u[j][k], hat, dw[j][k]);
+            }
+            if constexpr (LEAN) {
+#pragma unroll
+                for (int q = 0; q < V / 4; ++q) {
+                    const float4 f = own(j, q);
+                    const float2 low = fma2(u[j][2 * q], s[j][2 * q], make_float2(f.x, f.y)), high = fma2(u[j][2 * q + 1], s[j][2 * q + 1], make_float2(f.z, f.w));
+                    own(j, q) = make_float4(low.x, low.y, high.x, high.y);
+                }
+            }
+            if (a.dx) columns.store(dx, j, pack<T>(d));
+        }
+        if constexpr (LEAN)
+            x += x_step, g += g_step, ds += ds_step;
+        else
+            stage = stage + 1 == kStages ? 0 : stage + 1;
     }
     if (!a.parts) return;
     float* part = a.parts + (int64_t)blockIdx.x * width;
-    if constexpr (LEAN) {
+    float* rows = reinterpret_cast<float*>(memory);
+    if (!LEAN && groups > 1) {
+        wait_copies<0>();
+        __syncthreads();  // the place of the rows to come is free
+    }
+    float* to = groups > 1 ? rows + mine * width : part;
 #pragma unroll
-        for (int j = 0; j < K; ++j)
+    for (int j = 0; j < K; ++j)
 #pragma unroll
-            for (int q = 0; q < V / 4; ++q) {
-                const float4 f = own(j, q);
-                const float four[4] = {f.x, f.y, f.z, f.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int c = column(j) + 4 * q + k;
-                    if (c >= 0 && c < width) part[c] = four[k];
-                }
-            }
-    } else {
-        if (groups > 1) {
-            wait_copies<0>();
-            __syncthreads();  // the rows' place is free
+        for (int k = 0; k < H; ++k) {
+            float2 f;
+            if constexpr (LEAN)
+                f = k % 2 ? make_float2(own(j, k / 2).z, own(j, k / 2).w) : make_float2(own(j, k / 2).x, own(j, k / 2).y);
+            else
+                f = dw[j][k];
+            const int c = columns.at(j) + 2 * k;
+            if (c >= 0 && c < width) to[c] = f.x;
+            if (c + 1 >= 0 && c + 1 < width) to[c + 1] = f.y;
         }
-        float* to = groups > 1 ? columns + mine * width : part;
-#pragma unroll
-        for (int j = 0; j < K; ++j)
-#pragma unroll
-            for (int k = 0; k < V; ++k)
-                if (column(j) + k >= 0 && column(j) + k < width) to[column(j) + k] = dw[j][k];
-        if (groups == 1) return;
-        __syncthreads();
-        for (int c = threadIdx.x; c < width; c += blockDim.x) {
-            float sum = 0.0f;
-            for (int q = 0; q < groups; ++q) sum += columns[q * width + c];
-            part[c] = sum;
-        }
+    if (groups == 1) return;
+    __syncthreads();
+    for (int c = threadIdx.x; c < width; c += blockDim.x) {
+        float sum = 0.0f;
+        for (int q = 0; q < groups; ++q) sum += rows[q * width + c];
+        part[c] = sum;
     }
 }
 
@@ -613,8 +644,8 @@ __global__ void __launch_bounds__(1024) k_norm_join(const float* __restrict__ pa
 }
 
 template <class T>
-Shape grad_shape(int64_t width) {
-    return shape_of(ceil_div(width + (width + kVec<T> <= kMaxNormWidth ? kVec<T> - 1 : 0), kVec<T>), 32, 1024, 2048, 8);
+Shape grad_shape(int64_t width, bool shifted) {  // shifted: rows may start behind a 16-byte boundary, and take a vector more
+    return shape_of(ceil_div(width + (shifted ? kVec<T> - 1 : 0), kVec<T>), 32, 1024, 2048, 8);
 }
 
 // CTAs of the first kernel: those that are resident at once (1,024 threads a multiprocessor with one vector each, 512 with more), at most one row
@@ -653,13 +684,14 @@ cudaError_t launch_norm_grad(NormGradKernelArgs& a, const Shape& shape, int64_t 
 
 template <class T>
 cudaError_t norm_grad_typed(const NormGradArgs& n, void* workspace, cudaStream_t s) {
-    const Shape shape = grad_shape<T>(n.width);
+    const bool aligned = aligned16<T>(n.x, n.x_pitch), room = n.width + kVec<T> <= kMaxNormWidth;
+    const bool wide = alike<T>(n.x, n.x_pitch, n.grad_out, n.grad_out_pitch, n.n) && (!n.grad_sum || alike<T>(n.x, n.x_pitch, n.grad_sum, n.grad_sum_pitch, n.n)) &&
+                      (!n.grad_x || alike<T>(n.x, n.x_pitch, n.grad_x, n.grad_x_pitch, n.n)) && (aligned || room);
+    const Shape shape = grad_shape<T>(n.width, wide && !aligned);
     const int64_t ctas = grad_ctas(n.n, shape);
     NormGradKernelArgs a{n.grad_out, n.x, n.weight, n.grad_sum, n.grad_out_pitch, n.x_pitch, n.grad_sum_pitch, n.n, (int)n.width, n.eps, 1.0f / (float)n.width, n.grad_x, n.grad_x_pitch,
                          n.grad_weight ? Carver(workspace).take<float>(ctas * n.width) : nullptr, 0, 0,
                          reinterpret_cast<uintptr_t>(n.weight) % 16 == 0};
-    const bool wide = alike<T>(n.x, n.x_pitch, n.grad_out, n.grad_out_pitch, n.n) && (!n.grad_sum || alike<T>(n.x, n.x_pitch, n.grad_sum, n.grad_sum_pitch, n.n)) &&
-                      (!n.grad_x || alike<T>(n.x, n.x_pitch, n.grad_x, n.grad_x_pitch, n.n)) && (aligned16<T>(n.x, n.x_pitch) || n.width + kVec<T> <= kMaxNormWidth);
     A2_CUDA_TRY((wide ? launch_norm_grad<T, true>(a, shape, ctas, s) : launch_norm_grad<T, false>(a, shape, ctas, s)));
     if (!n.grad_weight) return cudaSuccess;
     return launch_chained(k_norm_join<T>, dim3((unsigned)ceil_div(n.width, 32)), 1024, 0, s, a.parts, ctas, n.width, static_cast<T*>(n.grad_weight));
@@ -680,7 +712,11 @@ cudaError_t run_dequantize(const DequantizeArgs& a, cudaStream_t s) {
 int64_t norm_grad_workspace(int64_t n, int64_t width, bool with_weight, int32_t dtype) {
     if (!with_weight) return 0;
     Carver c(nullptr);
-    c.take<float>(grad_ctas(n, dtype == A2_BF16 ? grad_shape<__nv_bfloat16>(width) : grad_shape<float>(width)) * width);
+    int64_t most = 0;
+    for (const bool shifted : {false, true})
+        if (!shifted || width + 8 <= kMaxNormWidth)
+            most = std::max(most, grad_ctas(n, dtype == A2_BF16 ? grad_shape<__nv_bfloat16>(width, shifted) : grad_shape<float>(width, shifted)));
+    c.take<float>(most * width);
     return c.used;
 }
 
