@@ -331,25 +331,33 @@ __device__ __forceinline__ Words pack(const float2 (&v)[kVec<T> / 2]) {
     return pack<T>(one);
 }
 
-// A vector of a row at column c that begins before the row or ends past it. Where vectors lie on 16-byte boundaries such a one is read whole (memory comes in
-// larger units than that, so what is next to the row is there) and `within` clears what is not the row's; else it is read, and always written, element by
-// element.
-__device__ __forceinline__ uint32_t bits_of(const float* p) { return __float_as_uint(*p); }
-__device__ __forceinline__ uint32_t bits_of(const __nv_bfloat16* p) { return *reinterpret_cast<const uint16_t*>(p); }
-template <class T>
-__device__ __forceinline__ Words by_element(const T* row, int c, int width) {
-    Words p{};
-#pragma unroll
-    for (int k = 0; k < kVec<T>; ++k)
-        if (c + k >= 0 && c + k < width) p.w[k * sizeof(T) / 4] |= bits_of(row + c + k) << (k * sizeof(T) % 4 * 8);
-    return p;
-}
+// What of a vector at column c lies in a row. Vectors that begin before the row or end past it, and such as do not lie on a 16-byte boundary, are read in whole
+// units of 16 bytes that hold an element of the row (memory comes in larger units than that, so what is next to the row is there) and cleared of
+// what is not the row's; they are written element by element.
 template <class T>
 __device__ __forceinline__ Words within(Words p, int c, int width) {
 #pragma unroll
     for (int k = 0; k < kVec<T>; ++k)
         if (c + k < 0 || c + k >= width) p.w[k * sizeof(T) / 4] &= sizeof(T) == 4 ? 0u : k % 2 ? 0xffffu : 0xffff0000u;
     return p;
+}
+// A vector at column c >= 0 of a row, wherever it lies.
+template <class T>
+__device__ __forceinline__ Words load_anywhere(const T* row, int c, int width) {
+    const uintptr_t from = reinterpret_cast<uintptr_t>(row + c), unit = from & ~(uintptr_t)15;
+    const int skip = (int)(from - unit);  // bytes
+    const int last = min(c + kVec<T>, width) - 1;
+    const Words low = *reinterpret_cast<const Words*>(unit);
+    const Words high = reinterpret_cast<uintptr_t>(row + last) >= unit + 16 ? *reinterpret_cast<const Words*>(unit + 16) : Words{};
+    uint32_t w[8] = {low.w[0], low.w[1], low.w[2], low.w[3], high.w[0], high.w[1], high.w[2], high.w[3]};
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = skip & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = skip & 4 ? w[i + 1] : w[i];
+    Words p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p.w[i] = sizeof(T) == 4 ? w[i] : __funnelshift_r(w[i], w[i + 1], skip % 4 * 8);
+    return within<T>(p, c, width);
 }
 template <class T>
 __device__ __forceinline__ void store_cut(T* row, int c, int width, const Words& p) {

@@ -28,10 +28,17 @@ constexpr float kScaleLeast = 0x1p-126f;  // of a block of zeros: its values are
 // ---------------------------------------------------------------------------------------------
 // A row's columns lie over a group of `group` threads: thread t holds the vectors t, t + group, ... of 16 bytes, K of them. A row that starts `shift`
 // elements after a 16-byte boundary is read from that boundary on (the vectors of all matrices of a call then start on boundaries, if
-// all rows are shifted alike): the first and the last vector are cut at the row's ends. WIDE = false reads and writes element by element.
+// all rows are shifted alike): the first and the last vector are cut at the row's ends. WIDE = false finds a vector in two units of 16 bytes and writes element by
+// element.
 // ---------------------------------------------------------------------------------------------
-// A thread's place in its group: groups are a power of two up to a warp, or a whole CTA.
-__device__ __forceinline__ int place_in(int group) { return group > 32 ? (int)threadIdx.x : (int)threadIdx.x & (group - 1); }
+// Groups are a power of two up to a warp, or whole warps. A thread's group in its CTA, its place in it:
+struct Place {
+    int mine, t;
+    __device__ explicit Place(unsigned group) {
+        mine = blockDim.x == group ? 0 : threadIdx.x / group;
+        t = threadIdx.x - mine * group;
+    }
+};
 
 __device__ __forceinline__ unsigned mask_of(int group) {  // of the lanes of this thread's group
     const int lane = threadIdx.x % 32;
@@ -39,9 +46,10 @@ __device__ __forceinline__ unsigned mask_of(int group) {  // of the lanes of thi
 }
 
 // Sums (or maxima of magnitudes) of COUNT values over a group, the same bits in every thread. `slot` changes from one such reduction to the
-// next (0, 1, 0, ...), so that one barrier each is enough.
-template <bool MAX, int COUNT>
-__device__ __forceinline__ void over_group(float (&v)[COUNT], int group, int slot, float (*shared)[32 * 2]) {
+// next (0, 1, 0, ...), so that one barrier each is enough: that of the CTA, or with SEVERAL groups of more than a warp in it (at most 15) that of the
+// group's warps. A kernel that does not know its barriers' numbers reserves all of a CTA's, which only few CTAs a multiprocessor can have.
+template <bool MAX, bool SEVERAL, int COUNT>
+__device__ __forceinline__ void over_group(float (&v)[COUNT], int group, int mine, int slot, float (*shared)[32 * 2]) {
     const unsigned mask = mask_of(group);
     auto join = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
 #pragma unroll
@@ -54,9 +62,13 @@ __device__ __forceinline__ void over_group(float (&v)[COUNT], int group, int slo
     if (lane == 0)
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) shared[slot][threadIdx.x / 32 * COUNT + i] = v[i];
-    __syncthreads();
+    if constexpr (SEVERAL)
+        asm volatile("bar.sync %0, %1;" ::"r"(mine + 1), "r"(group) : "memory");
+    else
+        __syncthreads();
+    const int first = SEVERAL ? mine * warps : 0;
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) v[i] = lane < warps ? shared[slot][lane * COUNT + i] : 0.0f;  // zero is neutral for both
+    for (int i = 0; i < COUNT; ++i) v[i] = lane < warps ? shared[slot][(first + lane) * COUNT + i] : 0.0f;  // zero is neutral for both
 #pragma unroll
     for (int d = 16; d > 0; d /= 2)
         if (d < warps)
@@ -66,10 +78,10 @@ __device__ __forceinline__ void over_group(float (&v)[COUNT], int group, int slo
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
 }
-template <bool MAX>
-__device__ __forceinline__ float over_group(float v, int group, int slot, float (*shared)[32 * 2]) {
+template <bool MAX, bool SEVERAL>
+__device__ __forceinline__ float over_group(float v, int group, int mine, int slot, float (*shared)[32 * 2]) {
     float one[1] = {v};
-    over_group<MAX, 1>(one, group, slot, shared);
+    over_group<MAX, SEVERAL, 1>(one, group, mine, slot, shared);
     return one[0];
 }
 
@@ -116,6 +128,9 @@ struct NormKernelArgs {
 // row. MODE 0: y in the rows' type. 1: e4m3 with a scale for every 2^block_log columns, whose vectors lie in neighbouring lanes. 2: e4m3 with one
 // scale a row. Sums are in fp32; s is rounded only where it is stored, y is formed from what it was before.
 // ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t bits_of(const float* p) { return __float_as_uint(*p); }
+__device__ __forceinline__ uint32_t bits_of(const __nv_bfloat16* p) { return *reinterpret_cast<const uint16_t*>(p); }
+
 // A thread's vectors of a row.
 template <class T, bool WIDE>
 struct Columns {
@@ -136,7 +151,7 @@ struct Columns {
 #pragma unroll
         for (int j = 0; j < K; ++j) {
             p[j] = Words{};
-            if (in(j)) p[j] = WIDE ? *reinterpret_cast<const Words*>(row + at(j)) : by_element(row, at(j), width);
+            if (in(j)) p[j] = WIDE ? *reinterpret_cast<const Words*>(row + at(j)) : load_anywhere(row, at(j), width);
         }
     }
     template <int K>
@@ -155,7 +170,13 @@ struct Columns {
     }
     // A vector of the weight, which may start elsewhere.
     __device__ Words load_weight(const T* w, int j, bool wide) const {
-        return wide && !cut && first % kVec<T> == 0 ? *reinterpret_cast<const Words*>(w + at(j)) : by_element(w, at(j), width);
+        if (wide && !cut && first % kVec<T> == 0) return *reinterpret_cast<const Words*>(w + at(j));
+        if (at(j) >= 0) return load_anywhere(w, at(j), width);
+        Words p{};  // the vector that begins before the row
+#pragma unroll
+        for (int k = 0; k < kVec<T>; ++k)
+            if (at(j) + k >= 0 && at(j) + k < width) p.w[k * sizeof(T) / 4] |= bits_of(w + at(j) + k) << (k * sizeof(T) % 4 * 8);
+        return p;
     }
 };
 
@@ -164,9 +185,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ Nor
     constexpr int V = kVec<T>, H = V / 2;
     __shared__ float shared[2][32 * 2];
     ptx::chained();
-    const int group = a.group, width = a.width, t = place_in(group);
-    const int64_t row = group > 32 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (blockDim.x / group) + threadIdx.x / group;
-    if (row >= a.n) return;  // whole groups, and whole CTAs where a group is one
+    const int group = a.group, width = a.width;
+    const Place place(group);
+    const int t = place.t, mine = place.mine;
+    const int64_t row = group > 32 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (blockDim.x / group) + mine;
+    if (row >= a.n) return;  // whole groups, which are CTAs where they are more than a warp
     const T* x = static_cast<const T*>(a.x) + row * a.x_pitch;
     const T* w = static_cast<const T*>(a.weight);
     const Columns<T, WIDE> columns(x, t, group, width);
@@ -208,17 +231,17 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ Nor
             for (int k = 0; k < H; ++k) most = fmaxf(most, fmaxf(fabsf(v[j][k].x), fabsf(v[j][k].y)));
         return most;
     };
-    const float squares = over_group<false>(squares_of(), group, 0, shared);
+    const float squares = over_group<false, false>(squares_of(), group, mine, 0, shared);
     float rstd;
     if (in_range(squares, a.eps * (float)width)) {
         rstd = rstd_of(fmaf(squares, a.one_over_width, a.eps));
     } else {
-        const float by = power_below(over_group<true>(most_of_row(), group, 1, shared));
+        const float by = power_below(over_group<true, false>(most_of_row(), group, mine, 1, shared));
 #pragma unroll
         for (int j = 0; j < K; ++j)
 #pragma unroll
             for (int k = 0; k < H; ++k) v[j][k] = mul2(v[j][k], two(by));
-        rstd = scaled_rstd(by, over_group<false>(squares_of(), group, 0, shared), width, a.eps);
+        rstd = scaled_rstd(by, over_group<false, false>(squares_of(), group, mine, 0, shared), width, a.eps);
     }
 #pragma unroll
     for (int j = 0; j < K; ++j) {
@@ -238,7 +261,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ Nor
         float* scales = a.scales + row * a.blocks;
         float most = 0.0f, scale = 0.0f;
         if (MODE == 2) {
-            scale = scale_of(over_group<true>(most_of_row(), group, 1, shared));
+            scale = scale_of(over_group<true, false>(most_of_row(), group, mine, 1, shared));
             if (t == 0) scales[0] = scale;
         }
         const unsigned mask = mask_of(group);
@@ -338,7 +361,7 @@ cudaError_t norm_typed(const NormArgs& n, cudaStream_t s) {
         else
             vecs = ceil_div(n.width + V - 1, V);
     }
-    const Shape shape = shape_of(vecs, 32, 64, sizeof(T) == 2 ? 1024 : 2048, std::max<int>(8, (int)(n.block / V)));
+    const Shape shape = shape_of(vecs, 32, sizeof(T) == 2 ? 1024 : 64, 2048, std::max<int>(8, (int)(n.block / V)));
     if (!n.scales) return wide ? launch_norm<T, true, 0>(a, shape, s) : launch_norm<T, false, 0>(a, shape, s);
     if (n.block) return wide ? launch_norm<T, true, 1>(a, shape, s) : launch_norm<T, false, 1>(a, shape, s);
     return wide ? launch_norm<T, true, 2>(a, shape, s) : launch_norm<T, false, 2>(a, shape, s);
@@ -349,7 +372,7 @@ cudaError_t norm_typed(const NormArgs& n, cudaStream_t s) {
 // ---------------------------------------------------------------------------------------------
 constexpr int kBack = 16;  // values a thread takes at a time; blocks are multiples of it
 
-template <class T, bool WIDE>
+template <class T>
 __global__ void __launch_bounds__(256) k_dequantize(const uint8_t* __restrict__ values, int64_t values_pitch, const float* __restrict__ scales, int64_t n,
                                                     int width, int block_log, int blocks, T* __restrict__ out, int64_t out_pitch, int group) {
     ptx::chained();
@@ -360,7 +383,7 @@ __global__ void __launch_bounds__(256) k_dequantize(const uint8_t* __restrict__ 
         const float scale = scales[row * blocks + (blocks > 1 ? c >> block_log : 0)];
         const uint8_t* q = values + row * values_pitch + c;
         T* o = out + row * out_pitch + c;
-        if (WIDE && c + kBack <= width) {
+        if (c + kBack <= width) {
             const Words p = *reinterpret_cast<const Words*>(q);
             constexpr int V = kVec<T>;
 #pragma unroll
@@ -380,13 +403,27 @@ __global__ void __launch_bounds__(256) k_dequantize(const uint8_t* __restrict__ 
     }
 }
 
+// Rows anywhere: neighbouring threads take neighbouring values.
+template <class T>
+__global__ void __launch_bounds__(256) k_dequantize_single(const uint8_t* __restrict__ values, int64_t values_pitch, const float* __restrict__ scales, int64_t n,
+                                                           int width, int block_log, int blocks, T* __restrict__ out, int64_t out_pitch, int group) {
+    ptx::chained();
+    const int64_t row = (int64_t)blockIdx.x * (256 / group) + threadIdx.x / group;
+    if (row >= n) return;
+#pragma unroll 8
+    for (int c = (int)threadIdx.x % group; c < width; c += group) {
+        const float f = __half2float(__half(__nv_cvt_fp8_to_halfraw(values[row * values_pitch + c], __NV_E4M3)));
+        out[row * out_pitch + c] = narrow<T>(f * scales[row * blocks + (blocks > 1 ? c >> block_log : 0)]);
+    }
+}
+
 template <class T>
 cudaError_t dequantize_typed(const DequantizeArgs& a, cudaStream_t s) {
     const int blocks = a.block ? (int)ceil_div(a.width, a.block) : 1, block_log = a.block == 128 ? 7 : a.block == 64 ? 6 : 5;
     const bool wide = reinterpret_cast<uintptr_t>(a.values) % kBack == 0 && a.values_pitch % kBack == 0 && aligned16<T>(a.out, a.out_pitch);
     int group = 1;
-    while (group < 256 && group * kBack < a.width) group *= 2;
-    return launch_chained(wide ? k_dequantize<T, true> : k_dequantize<T, false>, dim3((unsigned)ceil_div(a.n, 256 / group)), 256, 0, s, a.values, a.values_pitch,
+    while (group < 256 && group * (wide ? kBack : 8) < a.width) group *= 2;
+    return launch_chained(wide ? k_dequantize<T> : k_dequantize_single<T>, dim3((unsigned)ceil_div(a.n, 256 / group)), 256, 0, s, a.values, a.values_pitch,
                           a.scales, a.n, (int)a.width, block_log, blocks, static_cast<T*>(a.out), a.out_pitch, group);
 }
 
@@ -418,7 +455,7 @@ struct NormGradKernelArgs {
     void* dx;
     int64_t dx_pitch;
     float* parts;  // [CTAs][width], or NULL without a gradient of the weight
-    int64_t slots;
+    int64_t slots, x_step, g_step, ds_step, dx_step;  // elements from one row of a slot to the next
     int group;
     bool wide_weight;
 };
@@ -429,8 +466,9 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
     __shared__ float shared[2][32 * 2];
     extern __shared__ uint4 memory[];  // LEAN: every thread's part of dw. Else rows to come, and at the end, with several groups a CTA, a row of dw for each
     ptx::chained();
-    const int group = a.group, width = a.width, t = place_in(group);
-    const int groups = group > 32 ? 1 : blockDim.x / group, mine = group > 32 ? 0 : threadIdx.x / group;
+    const int group = a.group, width = a.width, groups = blockDim.x / group;
+    const Place place(group);
+    const int t = place.t, mine = place.mine;
     const int64_t first = (int64_t)blockIdx.x * groups + mine;
     const T* x = static_cast<const T*>(a.x) + first * a.x_pitch;
     const T* g = static_cast<const T*>(a.g) + first * a.g_pitch;
@@ -448,9 +486,9 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
                 copy_ahead(&ahead(stage, 1, j), g + columns.at(j));
                 if (a.ds) copy_ahead(&ahead(stage, 2, j), ds + columns.at(j));
             } else {
-                ahead(stage, 0, j) = by_element(x, columns.at(j), width);
-                ahead(stage, 1, j) = by_element(g, columns.at(j), width);
-                if (a.ds) ahead(stage, 2, j) = by_element(ds, columns.at(j), width);
+                ahead(stage, 0, j) = load_anywhere(x, columns.at(j), width);
+                ahead(stage, 1, j) = load_anywhere(g, columns.at(j), width);
+                if (a.ds) ahead(stage, 2, j) = load_anywhere(ds, columns.at(j), width);
             }
         }
     };
@@ -464,14 +502,13 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
             for (int k = 0; k < H; ++k) p[j][k] = two(1.0f);
         }
     };
-    const int64_t x_step = a.slots * a.x_pitch, g_step = a.slots * a.g_pitch, ds_step = a.slots * a.ds_pitch, dx_step = a.slots * a.dx_pitch;
     int64_t coming = first;  // the next row to bring, with the three pointers
     if constexpr (!LEAN) {
 #pragma unroll
         for (int s = 0; s + 1 < kStages; ++s) {
             if (coming < a.n) bring_row(s, x, g, ds);
             close_copies();
-            coming += a.slots, x += x_step, g += g_step, ds += ds_step;
+            coming += a.slots, x += a.x_step, g += a.g_step, ds += a.ds_step;
         }
 #pragma unroll
         for (int j = 0; j < K; ++j) {
@@ -486,7 +523,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
             for (int q = 0; q < V / 4; ++q) own(j, q) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
     int slot = 0, stage = 0;
-    for (int64_t row = first; row < a.n; row += a.slots, dx += dx_step) {
+    for (int64_t row = first; row < a.n; row += a.slots, dx += a.dx_step) {
         float2 s[K][H], u[K][H];  // the row and its grad_out
         Words px[K], pg[K];
         if constexpr (LEAN) {
@@ -497,7 +534,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
         } else {
             if (coming < a.n) bring_row(stage == 0 ? kStages - 1 : stage - 1, x, g, ds);
             close_copies();
-            coming += a.slots, x += x_step, g += g_step, ds += ds_step;
+            coming += a.slots, x += a.x_step, g += a.g_step, ds += a.ds_step;
             wait_copies<kStages - 1>();
 #pragma unroll
             for (int j = 0; j < K; ++j) {
@@ -531,7 +568,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
                 }
             }
             v[0] = q.x + q.y, v[1] = c.x + c.y;
-            over_group<false, 2>(v, group, slot, shared);
+            over_group<false, true, 2>(v, group, mine, slot, shared);
             slot ^= 1;
         };
         sums(1.0f);
@@ -546,7 +583,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
 #pragma unroll
                 for (int k = 0; k < H; ++k) most = fmaxf(most, fmaxf(fabsf(s[j][k].x), fabsf(s[j][k].y)));
             }
-            by = power_below(over_group<true>(most, group, slot, shared));
+            by = power_below(over_group<true, true>(most, group, mine, slot, shared));
             slot ^= 1;
             sums(by);
             rstd = scaled_rstd(by, v[0], width, a.eps);
@@ -558,7 +595,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
             if (!columns.in(j)) continue;
             float2 d[H];
             if constexpr (LEAN) {
-                unpack<T>(!a.ds ? Words{} : WIDE ? *reinterpret_cast<const Words*>(ds + columns.at(j)) : by_element(ds, columns.at(j), width), d);
+                unpack<T>(!a.ds ? Words{} : WIDE ? *reinterpret_cast<const Words*>(ds + columns.at(j)) : load_anywhere(ds, columns.at(j), width), d);
                 unpack<T>(px[j], s[j]);
                 unpack<T>(pg[j], u[j]);
                 if (by != 1.0f) {
@@ -589,7 +626,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
             if (a.dx) columns.store(dx, j, pack<T>(d));
         }
         if constexpr (LEAN)
-            x += x_step, g += g_step, ds += ds_step;
+            x += a.x_step, g += a.g_step, ds += a.ds_step;
         else
             stage = stage + 1 == kStages ? 0 : stage + 1;
     }
@@ -648,13 +685,22 @@ Shape grad_shape(int64_t width, bool shifted) {  // shifted: rows may start behi
     return shape_of(ceil_div(width + (shifted ? kVec<T> - 1 : 0), kVec<T>), 32, 1024, 2048, 8);
 }
 
-// CTAs of the first kernel: those that are resident at once (1,024 threads a multiprocessor with one vector each, 512 with more), at most one row
-// for each group, a multiple of 8 where a group has several rows.
-int64_t grad_ctas(int64_t n, const Shape& shape) {
-    const int threads = cta_threads(shape), groups = threads / shape.group;
-    const int64_t full = (int64_t)multiprocessors() * std::max(1, (shape.k == 1 ? 1024 : 512) / threads);
-    const int64_t needed = ceil_div(n, groups);
-    return needed <= full ? std::max<int64_t>(needed, 1) : std::max<int64_t>(full / 8, 1) * 8;
+// The first kernel's launch. A CTA has as many groups as make 512 threads, for a part of dw each CTA is written and read again; fewer where there are not rows
+// enough to give each multiprocessor some. At most as many CTAs as are resident at once (two a multiprocessor with one vector a thread, else one); where a
+// group has several rows, so many that the slots are a multiple of 8.
+struct GradLaunch {
+    int groups;
+    int64_t ctas;
+};
+GradLaunch grad_launch(int64_t n, const Shape& shape) {
+    const int64_t sms = multiprocessors(), resident = sms * (shape.k == 1 ? 2 : 1);
+    const int whole = std::max(1, 32 / shape.group);  // groups of a warp
+    int groups = (int)std::min<int64_t>(std::max(1, 512 / shape.group), round_up(std::max<int64_t>(ceil_div(n, sms), 1), whole));
+    const int64_t ctas = ceil_div(n, groups);
+    if (ctas <= resident) return {groups, std::max<int64_t>(ctas, 1)};
+    int64_t most = resident;
+    while (most * groups % 8) --most;
+    return {groups, std::max<int64_t>(most, 1)};
 }
 
 template <class T, bool WIDE, int K, bool LEAN, int THREADS>
@@ -664,22 +710,23 @@ cudaError_t launch_grad_kernel(const NormGradKernelArgs& a, unsigned ctas, unsig
     static std::atomic<uint64_t> allowed{0};
     auto* kernel = k_norm_grad<T, WIDE, K, LEAN, THREADS, kCtas>;
     A2_CUDA_TRY(allow_shared_memory(reinterpret_cast<const void*>(kernel), (int)most, allowed));
-    return launch_chained(kernel, dim3(ctas), threads, each * threads, s, a);  // of several groups a CTA, rows of dw take less: V floats a thread
+    return launch_chained(kernel, dim3(ctas), threads, each * threads, s, a);  // rows of dw of several groups take less: K vectors of floats a thread
 }
 
 template <class T, bool WIDE>
-cudaError_t launch_norm_grad(NormGradKernelArgs& a, const Shape& shape, int64_t ctas, cudaStream_t s) {
-    const unsigned threads = cta_threads(shape);
+cudaError_t launch_norm_grad(NormGradKernelArgs& a, const Shape& shape, const GradLaunch& launch, cudaStream_t s) {
+    const unsigned threads = launch.groups * shape.group, ctas = (unsigned)launch.ctas;
     a.group = shape.group;
-    a.slots = ctas * (threads / shape.group);
+    a.slots = launch.ctas * launch.groups;
+    a.x_step = a.slots * a.x_pitch, a.g_step = a.slots * a.g_pitch, a.ds_step = a.slots * a.ds_pitch, a.dx_step = a.slots * a.dx_pitch;
     switch (shape.k) {
-        case 1: return launch_grad_kernel<T, WIDE, 1, false, 512>(a, (unsigned)ctas, threads, s);
-        case 2: return launch_grad_kernel<T, WIDE, 2, false, 512>(a, (unsigned)ctas, threads, s);
-        case 4: return launch_grad_kernel<T, WIDE, 4, sizeof(T) == 2, 512>(a, (unsigned)ctas, threads, s);
+        case 1: return launch_grad_kernel<T, WIDE, 1, false, 512>(a, ctas, threads, s);
+        case 2: return launch_grad_kernel<T, WIDE, 2, false, 512>(a, ctas, threads, s);
+        case 4: return launch_grad_kernel<T, WIDE, 4, sizeof(T) == 2, 512>(a, ctas, threads, s);
         default: break;
     }
-    if (threads <= 512) return launch_grad_kernel<T, WIDE, 8, true, 512>(a, (unsigned)ctas, threads, s);
-    return launch_grad_kernel<float, WIDE, 8, true, 1024>(a, (unsigned)ctas, threads, s);  // rows of fp32 alone are that long
+    if (threads <= 512) return launch_grad_kernel<T, WIDE, 8, true, 512>(a, ctas, threads, s);
+    return launch_grad_kernel<float, WIDE, 8, true, 1024>(a, ctas, threads, s);  // rows of fp32 alone are that long
 }
 
 template <class T>
@@ -688,13 +735,13 @@ cudaError_t norm_grad_typed(const NormGradArgs& n, void* workspace, cudaStream_t
     const bool wide = alike<T>(n.x, n.x_pitch, n.grad_out, n.grad_out_pitch, n.n) && (!n.grad_sum || alike<T>(n.x, n.x_pitch, n.grad_sum, n.grad_sum_pitch, n.n)) &&
                       (!n.grad_x || alike<T>(n.x, n.x_pitch, n.grad_x, n.grad_x_pitch, n.n)) && (aligned || room);
     const Shape shape = grad_shape<T>(n.width, wide && !aligned);
-    const int64_t ctas = grad_ctas(n.n, shape);
+    const GradLaunch launch = grad_launch(n.n, shape);
     NormGradKernelArgs a{n.grad_out, n.x, n.weight, n.grad_sum, n.grad_out_pitch, n.x_pitch, n.grad_sum_pitch, n.n, (int)n.width, n.eps, 1.0f / (float)n.width, n.grad_x, n.grad_x_pitch,
-                         n.grad_weight ? Carver(workspace).take<float>(ctas * n.width) : nullptr, 0, 0,
+                         n.grad_weight ? Carver(workspace).take<float>(launch.ctas * n.width) : nullptr, 0, 0, 0, 0, 0, 0,
                          reinterpret_cast<uintptr_t>(n.weight) % 16 == 0};
-    A2_CUDA_TRY((wide ? launch_norm_grad<T, true>(a, shape, ctas, s) : launch_norm_grad<T, false>(a, shape, ctas, s)));
+    A2_CUDA_TRY((wide ? launch_norm_grad<T, true>(a, shape, launch, s) : launch_norm_grad<T, false>(a, shape, launch, s)));
     if (!n.grad_weight) return cudaSuccess;
-    return launch_chained(k_norm_join<T>, dim3((unsigned)ceil_div(n.width, 32)), 1024, 0, s, a.parts, ctas, n.width, static_cast<T*>(n.grad_weight));
+    return launch_chained(k_norm_join<T>, dim3((unsigned)ceil_div(n.width, 32)), 1024, 0, s, a.parts, launch.ctas, n.width, static_cast<T*>(n.grad_weight));
 }
 
 }  // namespace
@@ -715,7 +762,7 @@ int64_t norm_grad_workspace(int64_t n, int64_t width, bool with_weight, int32_t 
     int64_t most = 0;
     for (const bool shifted : {false, true})
         if (!shifted || width + 8 <= kMaxNormWidth)
-            most = std::max(most, grad_ctas(n, dtype == A2_BF16 ? grad_shape<__nv_bfloat16>(width, shifted) : grad_shape<float>(width, shifted)));
+            most = std::max(most, grad_launch(n, dtype == A2_BF16 ? grad_shape<__nv_bfloat16>(width, shifted) : grad_shape<float>(width, shifted)).ctas);
     c.take<float>(most * width);
     return c.used;
 }
