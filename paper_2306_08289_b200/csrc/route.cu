@@ -16,10 +16,13 @@ namespace {
 constexpr int kThreads = 256;
 constexpr unsigned kAll = 0xffffffffu;
 
-// Floats as unsigned integers in the same order, above zero: zero stands for an expert that cannot be chosen.
+// Floats as unsigned integers in the same order. The sign is spread by a product rather than a shift: the pipe of shifts, comparisons and selections
+// is what these kernels are short of.
 __device__ __forceinline__ uint32_t ordered(float v) {
     const uint32_t b = __float_as_uint(v + 0.0f);  // -0 is 0
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
+    int sign;
+    asm("mul.hi.s32 %0, %1, 2;" : "=r"(sign) : "r"(b));
+    return b ^ ((uint32_t)sign | 0x80000000u);
 }
 __device__ __forceinline__ float number(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
 
@@ -49,11 +52,27 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
 
 // A logit (widened) as the kernels use it: -inf (no expert) for NaN and what is at or below the type's lowest value, as masks are written.
 template <class T>
+__device__ __forceinline__ float lowest_of() {
+    return sizeof(T) == 2 ? -0x1.fep127f : -FLT_MAX;
+}
+template <class T>
 __device__ __forceinline__ float logit(float x) {
-    return x > (sizeof(T) == 2 ? -0x1.fep127f : -FLT_MAX) ? fminf(x, FLT_MAX) : -INFINITY;
+    return x > lowest_of<T>() ? fminf(x, FLT_MAX) : -INFINITY;
 }
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
+
+// Approximate ones, of single instructions: off by 2^-22 of their results and by what rounding x * log2(e) does.
+__device__ __forceinline__ float near_exp(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * 1.4426950408889634f));
+    return y;
+}
+__device__ __forceinline__ float near_reciprocal(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
 struct RouteKernelArgs {
     const void* logits;
@@ -175,20 +194,24 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
     constexpr int kTokens = 32 / LANES, kThreadCount = ALONE ? kAloneThreads : kThreads;  // tokens of a warp
     constexpr unsigned kSegment = LANES == 32 ? kAll : (1u << (LANES % 32)) - 1u;
     constexpr uint32_t kPlace = N - 1;
+    constexpr uint32_t kNone = sizeof(T) == 4 ? 0x00800000u | kPlace : 0x0080ffffu;  // what a key is above, if its expert is available: ordered(lowest_of<T>())
     constexpr bool kSorted = N <= 16;  // longer lists: the maximum is looked for again in each round
     constexpr float kLost = N * 0x1p-23f;
     constexpr int V = 16 / sizeof(T);
+    __shared__ alignas(16) float biases[LANES * N];
     extern __shared__ int counts[];
     const int lane = threadIdx.x % LANES, base = threadIdx.x % 32 - lane;
     if (ALONE || !a.counts) ptx::chained();  // else k_clear before it has waited for all that came before
-    if (a.counts) {
+    if (a.counts)
         for (int e = threadIdx.x; e < a.experts; e += kThreadCount) counts[e] = 0;
-        __syncthreads();
-    }
     auto first_of = [&](int l) { return (l >> a.share_log) * a.group_size + (l & ((1 << a.share_log) - 1)) * a.per; };
     const int group = lane >> a.share_log, first = first_of(lane);
     const int count = group < a.groups ? max(0, min(a.per, (group + 1) * a.group_size - first)) : 0;
     const bool scored = a.bias || a.two_best;
+    if (threadIdx.x < LANES)  // a bias of -inf or NaN switches an expert off
+#pragma unroll
+        for (int j = 0; j < N; ++j) biases[lane * N + j] = !a.bias || j >= count ? 0.0f : a.bias[first + j] > -INFINITY ? fminf(a.bias[first + j], FLT_MAX) : -INFINITY;
+    __syncthreads();
     const float off = a.sigmoid ? 0x1p-21f : (N + 24) * 0x1p-24f;  // of a score: approximate exponential and reciprocal, sums of N + 5 terms
     const bool exact = !a.bias;                                   // experts are ranked by their logits
     const bool checked = !exact || sizeof(T) == 4;                // bf16 logits have no bits to lose
@@ -199,23 +222,29 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
         const int64_t token = wanted < a.n ? wanted : a.n - 1;   // a warp's last ones work along
         const T* row = static_cast<const T*>(a.logits) + token * a.pitch;
         float z[N];
+        constexpr uint32_t kNothing = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;  // -inf
         if (N % V == 0 && a.wide) {
 #pragma unroll
             for (int j = 0; j < N; j += V) {
-                Words p{};
+                Words p{kNothing, kNothing, kNothing, kNothing};
                 if (j < count) p = *reinterpret_cast<const Words*>(row + first + j);
                 float f[V];
                 unpack<T>(p, f);
 #pragma unroll
                 for (int i = 0; i < V; ++i)
-                    if (j + i < N) z[j + i] = j < count ? logit<T>(f[i]) : -INFINITY;
+                    if (j + i < N) z[j + i] = f[i];
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < N; ++j) z[j] = j < count ? logit<T>(widen(row[first + j])) : -INFINITY;
+            for (int j = 0; j < N; ++j) {
+                z[j] = -INFINITY;
+                if (j < count) z[j] = widen(row[first + j]);
+            }
         }
         float most = 0.0f, total = 1.0f;
         if (!a.sigmoid && (scored || !a.renormalize)) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) z[j] = logit<T>(z[j]);
             most = z[0];
 #pragma unroll
             for (int j = 1; j < N; ++j) most = fmaxf(most, z[j]);
@@ -228,45 +257,17 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
         }
         bool doubt = false;
         uint32_t u[N];
-        float best = -INFINITY, second = -INFINITY;
-        if (scored) {
+        auto place = [&](int j, float key) { u[j] = (ordered(key) & ~kPlace) | (kPlace - j); };
+        if (a.bias) {
             const float one = 1.0f / total;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const float bias = a.bias && j < count ? a.bias[first + j] : 0.0f;
-                float key = (a.sigmoid ? __fdividef(1.0f, 1.0f + __expf(-z[j])) : __expf(z[j] - most) * one) + bias;
-                // a bias of -inf or NaN switches an expert off
-                key = z[j] > -INFINITY && key > -INFINITY ? fminf(key, FLT_MAX) : -INFINITY;
-                second = fmaxf(second, fminf(best, key));
-                best = fmaxf(best, key);
-                u[j] = key == -INFINITY ? 0u : (ordered(exact ? z[j] : key) & ~kPlace) | (kPlace - j);
+                const float score = a.sigmoid ? near_reciprocal(1.0f + near_exp(-z[j])) : near_exp(z[j] - most) * one;
+                place(j, z[j] > lowest_of<T>() ? score + biases[lane * N + j] : -INFINITY);
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                best = fmaxf(best, z[j]);
-                u[j] = z[j] == -INFINITY ? 0u : (ordered(z[j]) & ~kPlace) | (kPlace - j);
-            }
-        }
-        if (a.groups > 1) {
-            for (int d = (1 << a.share_log) / 2; d > 0; d /= 2) {
-                const float b = __shfl_xor_sync(kAll, best, d), s = __shfl_xor_sync(kAll, second, d);
-                second = fmaxf(fminf(best, b), fmaxf(second, s));
-                best = fmaxf(best, b);
-            }
-            const float score = a.two_best && a.group_size > 1 ? best + second : best;
-            int place = 0;
-            float next = -INFINITY;  // the best score behind this group's
-            for (int g = 0; g < a.groups; ++g) {
-                const float other = __shfl_sync(kAll, score, base + (g << a.share_log));
-                const bool ahead = other > score || (other == score && g < group);
-                place += ahead;
-                if (!ahead && g != group) next = fmaxf(next, other);
-            }
-            const bool open = place < a.top_groups;
-            if (scored) doubt = group < a.groups && place == a.top_groups - 1 && next > -INFINITY && !(score - next > 4.0f * off + fabsf(score) * 0x1p-21f);
-#pragma unroll
-            for (int j = 0; j < N; ++j) u[j] = open ? u[j] : 0u;
+            for (int j = 0; j < N; ++j) place(j, fmaxf(z[j], -INFINITY));  // NaN is -inf
         }
         if constexpr (kSorted) sort<N>(u);
         auto head_of = [&] {
@@ -277,6 +278,52 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
             }
             return h;
         };
+        if (a.groups > 1) {
+            // a lane's two best keys, less the lost bits; -inf for what is not available
+            auto value = [&](uint32_t v) { return v > kNone ? fminf(number(v & ~kPlace), FLT_MAX) : -INFINITY; };
+            uint32_t u0 = head_of(), u1 = kSorted && N > 1 ? u[N > 1 ? 1 : 0] : 0;
+            if constexpr (!kSorted) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) u1 = u[j] == u0 ? u1 : max(u1, u[j]);
+            }
+            float best = value(u0), second = value(u1);
+            if (scored && !a.bias) {  // lists of logits, but groups by scores
+                best = second = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float v = logit<T>(z[j]);
+                    second = fmaxf(second, fminf(best, v));
+                    best = fmaxf(best, v);
+                }
+                auto score = [&](float v) { return v == -INFINITY ? v : a.sigmoid ? near_reciprocal(1.0f + near_exp(-v)) : near_exp(v - most) / total; };
+                best = score(best), second = score(second);
+            }
+            for (int d = (1 << a.share_log) / 2; d > 0; d /= 2) {
+                const float b = __shfl_xor_sync(kAll, best, d);
+                if (a.two_best) {
+                    const float s = __shfl_xor_sync(kAll, second, d);
+                    second = fmaxf(fminf(best, b), fmaxf(second, s));
+                }
+                best = fmaxf(best, b);
+            }
+            const float score = a.two_best && a.group_size > 1 ? best + second : best;
+            // the best groups one after the other; a group's number in the lowest bits, so that no two are equal and the lowest is first
+            uint32_t mine = group < a.groups ? (ordered(score) & ~31u) | (31 - group) : 0u, last = 0;
+            bool open = false;
+            for (int r = 0; r < a.top_groups; ++r) {
+                last = lanes_max<LANES>(mine);
+                if (mine == last) open = true, mine = 0;
+            }
+            const uint32_t next = lanes_max<LANES>(mine);
+            if (a.top_groups < a.groups && (next | 31u) != (ordered(-INFINITY) | 31u)) {
+                // the border's scores without 5 bits (unscored ones of bf16 have none there), of keys without those of their places
+                const float in = number(last & ~31u), out = number(next & ~31u);
+                doubt = !scored ? sizeof(T) == 4 && !(in - out > fabsf(in) * (2.0f * kLost + 0x1p-17f))
+                                : !(in - out > 4.0f * off + fabsf(in) * (4.0f * kLost + 0x1p-17f));
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) u[j] = open ? u[j] : 0u;
+        }
         // lane r keeps the r-th round's key and lane; all keep those of the round after the last, for the check of what was left out
         uint32_t head = head_of(), key = 0, key_next = 0;
         int from = 0, from_next = 0;
@@ -300,11 +347,11 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
             head = head_of();
         }
         auto expert_of = [&](uint32_t key, int from) { return first_of(from) + (int)(kPlace - (key & kPlace)); };
-        int mine = lane < a.k && key != 0 ? expert_of(key, from) : -1;
+        int mine = lane < a.k && key > kNone ? expert_of(key, from) : -1;
         if (checked) {
             const uint32_t after = __shfl_down_sync(kAll, key, 1), behind = lane + 1 < a.k ? after : key_next;
             const int after_from = __shfl_down_sync(kAll, from, 1);
-            if (mine >= 0 && behind != 0) {
+            if (mine >= 0 && behind > kNone) {
                 const uint32_t k0 = key & ~kPlace, k1 = behind & ~kPlace;
                 const float low = number(k1);
                 if (exact ? k0 == k1 : !(number(k0) - low > 2.0f * off + fabsf(low) * (2.0f * kLost + 0x1p-22f))) {
