@@ -17,8 +17,10 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kChunkBytes = 32768;   // eight loads of 16 bytes in flight for each of 256 threads
-constexpr int kCtas = 4;             // a multiprocessor
+constexpr int kChunkBytes = 16384;   // four loads of 16 bytes in flight for each of 256 threads
+constexpr int kCtas = 6;             // a multiprocessor
+constexpr int64_t kMany = 2;           // chunks of a run from which on the scaling is a launch of its own shape, after one that joins the norms
+constexpr int kKept = 5;             // chunks at the end of a run that should stay in the L2 cache: 73 MB of its 126
 constexpr int kFew = 48;             // tensors that are described in a kernel's parameters; more in the workspace
 constexpr int kStored = 240;         // tensors that a launch brings there
 constexpr int64_t kSmallChunks = 4;  // chunks of a worker that one CTA takes alone
@@ -41,10 +43,10 @@ struct Stored {
 
 struct ClipKernelArgs {
     int64_t n_tensors, workers, worker_chunks, chunks;
-    double* sums;
+    double *sums, *wide_norms;
     float* norms;
     double max_norm;
-    bool zero_nonfinite, clip;
+    bool zero_nonfinite, clip, in_place;
 };
 
 __global__ void __launch_bounds__(kStored) k_store(const __grid_constant__ Stored from, Tensor* to, int n) {
@@ -72,13 +74,14 @@ __device__ __forceinline__ double cta_sum(double v, double* shared) {
 template <class T, int COUNT>
 __device__ __forceinline__ double squares(const Words (&p)[COUNT]) {
     constexpr int V = kVec<T>;
-    float q[COUNT], v[V];
+    float q[COUNT];
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) {
+        float2 v[V / 2], sum = two(0.0f);
         unpack<T>(p[i], v);
-        q[i] = 0.0f;
 #pragma unroll
-        for (int k = 0; k < V; ++k) q[i] = fmaf(v[k], v[k], q[i]);
+        for (int k = 0; k < V / 2; ++k) sum = fma2(v[k], v[k], sum);
+        q[i] = sum.x + sum.y;
     }
 #pragma unroll
     for (int n = COUNT / 2; n > 0; n /= 2)
@@ -88,6 +91,7 @@ __device__ __forceinline__ double squares(const Words (&p)[COUNT]) {
     double d = 0.0;
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) {
+        float v[V];
         unpack<T>(p[i], v);
 #pragma unroll
         for (int k = 0; k < V; ++k) d += (double)v[k] * (double)v[k];
@@ -151,8 +155,15 @@ __device__ __forceinline__ void over_chunk(const Tensor& t, int64_t worker, int6
     }
 }
 
+// Words that nobody reads again soon leave the L2 cache first.
+__device__ __forceinline__ Words load_once(const void* p) {
+    const uint4 v = __ldcs(static_cast<const uint4*>(p));
+    return {v.x, v.y, v.z, v.w};
+}
+__device__ __forceinline__ void store_once(void* p, const Words& v) { __stcs(static_cast<uint4*>(p), make_uint4(v.w[0], v.w[1], v.w[2], v.w[3])); }
+
 template <class T, int THREADS>
-__device__ __forceinline__ double chunk_squares(const Tensor& t, int64_t worker, int64_t chunk) {
+__device__ __forceinline__ double chunk_squares(const Tensor& t, int64_t worker, int64_t chunk, bool keep) {
     double sum = 0.0;
     over_chunk<T, THREADS>(
         t, worker, chunk,
@@ -160,7 +171,7 @@ __device__ __forceinline__ double chunk_squares(const Tensor& t, int64_t worker,
             constexpr int kCount = decltype(count)::value;
             Words p[kCount];
 #pragma unroll
-            for (int i = 0; i < kCount; ++i) p[i] = *reinterpret_cast<const Words*>(in + from(i));
+            for (int i = 0; i < kCount; ++i) p[i] = keep ? *reinterpret_cast<const Words*>(in + from(i)) : load_once(in + from(i));
             sum += squares<T, kCount>(p);
         },
         [&](const T* in, T*) {
@@ -179,14 +190,14 @@ __device__ __forceinline__ void scale_chunk(const Tensor& t, int64_t worker, int
             constexpr int kCount = decltype(count)::value;
             Words p[kCount];
 #pragma unroll
-            for (int i = 0; i < kCount; ++i) p[i] = *reinterpret_cast<const Words*>(in + from(i));
+            for (int i = 0; i < kCount; ++i) p[i] = load_once(in + from(i));
 #pragma unroll
             for (int i = 0; i < kCount; ++i) {
                 float v[V];
                 unpack<T>(p[i], v);
 #pragma unroll
                 for (int k = 0; k < V; ++k) v[k] = zero ? 0.0f : v[k] * factor;
-                *reinterpret_cast<Words*>(out + to(i)) = pack<T>(v);
+                store_once(out + to(i), pack<T>(v));
             }
         },
         [&](const T* in, T* out) { *out = narrow<T>(zero ? 0.0f : widen(*in) * factor); });
@@ -239,8 +250,9 @@ __global__ void __launch_bounds__(kThreads, kCtas) k_squares(const __grid_consta
         for (; chunk < worker_end; ++chunk, ++c) {
             while (t + 1 < a.n_tensors && table[t + 1].first_chunk <= c) ++t;
             const Tensor& tensor = table[t];
-            sum += tensor.bf16 ? chunk_squares<__nv_bfloat16, kThreads>(tensor, worker, c - tensor.first_chunk)
-                               : chunk_squares<float, kThreads>(tensor, worker, c - tensor.first_chunk);
+            const bool keep = end - chunk <= kKept;
+            sum += tensor.bf16 ? chunk_squares<__nv_bfloat16, kThreads>(tensor, worker, c - tensor.first_chunk, keep)
+                               : chunk_squares<float, kThreads>(tensor, worker, c - tensor.first_chunk, keep);
         }
         sum = cta_sum<kThreads>(sum, shared);
         if (threadIdx.x == 0) a.sums[cta + worker] = sum;
@@ -275,12 +287,33 @@ __global__ void __launch_bounds__(kThreads, kCtas) k_scale(const __grid_constant
     }
 }
 
-// Norms alone, of a CTA each.
-__global__ void __launch_bounds__(kThreads) k_norms(const ClipKernelArgs a, int64_t ctas) {
+// Norms alone, of a CTA each; in 64 bits too where a kernel that scales follows.
+__global__ void __launch_bounds__(kThreads) k_norms(const __grid_constant__ ClipKernelArgs a, int64_t ctas) {
     __shared__ double shared[kWarps];
     ptx::chained();
     const double norm = a.chunks ? norm_of(a, blockIdx.x, ctas, shared) : 0.0;
-    if (threadIdx.x == 0) a.norms[blockIdx.x] = (float)norm;
+    if (threadIdx.x != 0) return;
+    a.norms[blockIdx.x] = (float)norm;
+    if (a.clip) a.wide_norms[blockIdx.x] = norm;
+}
+
+// Chunks in the order of first the last ones of all runs, then those before them: what was read last comes from L2. A chunk a CTA: while one waits for its
+// loads, others write (134 M bf16: 128 us with the norm, 133 with a few chunks each). In place, where mostly nothing has to be done, a few chunks each, which
+// are sooner over then.
+template <bool FEW>
+__global__ void __launch_bounds__(kThreads) k_scale_chunks(const __grid_constant__ ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored, unsigned ctas) {
+    ptx::chained();
+    const Tensor* table = FEW ? few.tensor : stored;
+    if (a.in_place && a.workers == 1 && factor_of(a, a.wide_norms[0]).nothing) return;
+    const unsigned most = (unsigned)((a.chunks + ctas - 1) / ctas) * ctas;
+    for (unsigned i = blockIdx.x; i < most; i += gridDim.x) {
+        const int64_t run = i % ctas, chunk = run_start(a, run + 1, ctas) - 1 - i / ctas;
+        if (chunk < run_start(a, run, ctas)) continue;
+        const int64_t worker = a.workers == 1 ? 0 : chunk / a.worker_chunks, c = chunk - worker * a.worker_chunks;
+        const Factor f = factor_of(a, a.wide_norms[worker]);
+        const Tensor& t = table[tensor_of(table, a.n_tensors, c)];
+        scale<kThreads>(t, worker, c - t.first_chunk, f);
+    }
 }
 
 // Few elements a worker: both steps in one launch, a CTA a worker.
@@ -296,8 +329,8 @@ __global__ void __launch_bounds__(kSmallThreads) k_small(const __grid_constant__
     for (int64_t c = 0, t = 0; c < a.worker_chunks; ++c) {
         while (t + 1 < a.n_tensors && table[t + 1].first_chunk <= c) ++t;
         const Tensor& tensor = table[t];
-        sum += tensor.bf16 ? chunk_squares<__nv_bfloat16, kSmallThreads>(tensor, worker, c - tensor.first_chunk)
-                           : chunk_squares<float, kSmallThreads>(tensor, worker, c - tensor.first_chunk);
+        sum += tensor.bf16 ? chunk_squares<__nv_bfloat16, kSmallThreads>(tensor, worker, c - tensor.first_chunk, true)
+                           : chunk_squares<float, kSmallThreads>(tensor, worker, c - tensor.first_chunk, true);
     }
     const double norm = sqrt(cta_sum<kSmallThreads>(sum, shared));
     if (threadIdx.x == 0) a.norms[worker] = (float)norm;
@@ -337,6 +370,7 @@ int64_t describe(const a2cid2_gradient_t& g, bool clip, int64_t workers, Tensor&
 int64_t clip_workspace(int64_t n_tensors, int64_t workers) {
     Carver c(nullptr);
     c.take<double>(most_ctas() + workers);
+    c.take<double>(workers);
     if (n_tensors > kFew) c.take<Tensor>(n_tensors);
     return c.used;
 }
@@ -344,7 +378,7 @@ int64_t clip_workspace(int64_t n_tensors, int64_t workers) {
 cudaError_t run_clip(const ClipArgs& r, void* workspace, cudaStream_t s) {
     if (r.workers == 0) return cudaSuccess;
     Carver carver(workspace);
-    ClipKernelArgs a{0, r.workers, 0, 0, carver.take<double>(most_ctas() + r.workers), r.norms, r.max_norm, r.zero_nonfinite, r.clip};
+    ClipKernelArgs a{0, r.workers, 0, 0, carver.take<double>(most_ctas() + r.workers), carver.take<double>(r.workers), r.norms, r.max_norm, r.zero_nonfinite, r.clip, true};
     Few few{};
     Stored part{};
     Tensor* table = r.n_tensors > kFew ? carver.take<Tensor>(r.n_tensors) : nullptr;
@@ -363,6 +397,7 @@ cudaError_t run_clip(const ClipArgs& r, void* workspace, cudaStream_t s) {
         t.first_chunk = a.worker_chunks;
         a.worker_chunks += chunks;
         ++a.n_tensors;
+        a.in_place = a.in_place && t.in == t.out;
         (table ? part.tensor : few.tensor)[held++] = t;
         if (table && held == kStored) A2_CUDA_TRY(bring());
     }
@@ -373,7 +408,10 @@ cudaError_t run_clip(const ClipArgs& r, void* workspace, cudaStream_t s) {
     if (a.worker_chunks <= kSmallChunks) return launch_chained(table ? k_small<false> : k_small<true>, dim3(workers), kSmallThreads, 0, s, a, few, table);
     const int64_t ctas = std::min(a.chunks, most_ctas());
     A2_CUDA_TRY(launch_chained(table ? k_squares<false> : k_squares<true>, dim3((unsigned)ctas), kThreads, 0, s, a, few, table));
-    if (!r.clip) return launch_chained(k_norms, dim3(workers), kThreads, 0, s, a, ctas);
+    const bool many = a.chunks > kMany * ctas && a.chunks < (int64_t(1) << 30);
+    if (!r.clip || many) A2_CUDA_TRY(launch_chained(k_norms, dim3(workers), kThreads, 0, s, a, ctas));
+    if (!r.clip) return cudaSuccess;
+    if (many) return launch_chained(table ? k_scale_chunks<false> : k_scale_chunks<true>, dim3((unsigned)(a.in_place ? std::min(a.chunks, 4 * ctas) : ceil_div(a.chunks, ctas) * ctas)), kThreads, 0, s, a, few, table, (unsigned)ctas);
     return launch_chained(table ? k_scale<false> : k_scale<true>, dim3((unsigned)ctas), kThreads, 0, s, a, few, table);
 }
 
