@@ -46,7 +46,7 @@ struct ClipKernelArgs {
     double *sums, *wide_norms;
     float* norms;
     double max_norm;
-    bool zero_nonfinite, clip, in_place;
+    bool zero_nonfinite, clip;
 };
 
 __global__ void __launch_bounds__(kStored) k_store(const __grid_constant__ Stored from, Tensor* to, int n) {
@@ -300,20 +300,27 @@ __global__ void __launch_bounds__(kThreads) k_norms(const __grid_constant__ Clip
 // Chunks in the order of first the last ones of all runs, then those before them: what was read last comes from L2. A chunk a CTA: while one waits for its
 // loads, others write (134 M bf16: 128 us with the norm, 133 with a few chunks each). In place, where mostly nothing has to be done, a few chunks each, which
 // are sooner over then.
+__device__ __forceinline__ void scale_in_order(const ClipKernelArgs& a, const Tensor* table, unsigned i, unsigned ctas) {
+    const int64_t run = i % ctas, chunk = run_start(a, run + 1, ctas) - 1 - i / ctas;
+    if (chunk < run_start(a, run, ctas)) return;
+    const int64_t worker = a.workers == 1 ? 0 : chunk / a.worker_chunks, c = chunk - worker * a.worker_chunks;
+    const Factor f = factor_of(a, a.wide_norms[worker]);
+    const Tensor& t = table[tensor_of(table, a.n_tensors, c)];
+    scale<kThreads>(t, worker, c - t.first_chunk, f);
+}
+
 template <bool FEW>
 __global__ void __launch_bounds__(kThreads) k_scale_chunks(const __grid_constant__ ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored, unsigned ctas) {
     ptx::chained();
-    const Tensor* table = FEW ? few.tensor : stored;
-    if (a.in_place && a.workers == 1 && factor_of(a, a.wide_norms[0]).nothing) return;
+    scale_in_order(a, FEW ? few.tensor : stored, blockIdx.x, ctas);
+}
+
+template <bool FEW>
+__global__ void __launch_bounds__(kThreads) k_scale_in_place(const __grid_constant__ ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored, unsigned ctas) {
+    ptx::chained();
+    if (a.workers == 1 && factor_of(a, a.wide_norms[0]).nothing) return;
     const unsigned most = (unsigned)((a.chunks + ctas - 1) / ctas) * ctas;
-    for (unsigned i = blockIdx.x; i < most; i += gridDim.x) {
-        const int64_t run = i % ctas, chunk = run_start(a, run + 1, ctas) - 1 - i / ctas;
-        if (chunk < run_start(a, run, ctas)) continue;
-        const int64_t worker = a.workers == 1 ? 0 : chunk / a.worker_chunks, c = chunk - worker * a.worker_chunks;
-        const Factor f = factor_of(a, a.wide_norms[worker]);
-        const Tensor& t = table[tensor_of(table, a.n_tensors, c)];
-        scale<kThreads>(t, worker, c - t.first_chunk, f);
-    }
+    for (unsigned i = blockIdx.x; i < most; i += gridDim.x) scale_in_order(a, FEW ? few.tensor : stored, i, ctas);
 }
 
 // Few elements a worker: both steps in one launch, a CTA a worker.
@@ -378,12 +385,13 @@ int64_t clip_workspace(int64_t n_tensors, int64_t workers) {
 cudaError_t run_clip(const ClipArgs& r, void* workspace, cudaStream_t s) {
     if (r.workers == 0) return cudaSuccess;
     Carver carver(workspace);
-    ClipKernelArgs a{0, r.workers, 0, 0, carver.take<double>(most_ctas() + r.workers), carver.take<double>(r.workers), r.norms, r.max_norm, r.zero_nonfinite, r.clip, true};
+    ClipKernelArgs a{0, r.workers, 0, 0, carver.take<double>(most_ctas() + r.workers), carver.take<double>(r.workers), r.norms, r.max_norm, r.zero_nonfinite, r.clip};
     Few few{};
     Stored part{};
     Tensor* table = r.n_tensors > kFew ? carver.take<Tensor>(r.n_tensors) : nullptr;
     int held = 0;
     int64_t stored = 0;
+    bool in_place = true;
     auto bring = [&]() -> cudaError_t {
         A2_CUDA_TRY(launch_chained(k_store, dim3(1), kStored, 0, s, part, table + stored, held));
         stored += held;
@@ -397,7 +405,7 @@ cudaError_t run_clip(const ClipArgs& r, void* workspace, cudaStream_t s) {
         t.first_chunk = a.worker_chunks;
         a.worker_chunks += chunks;
         ++a.n_tensors;
-        a.in_place = a.in_place && t.in == t.out;
+        in_place = in_place && t.in == t.out;
         (table ? part.tensor : few.tensor)[held++] = t;
         if (table && held == kStored) A2_CUDA_TRY(bring());
     }
@@ -411,7 +419,12 @@ cudaError_t run_clip(const ClipArgs& r, void* workspace, cudaStream_t s) {
     const bool many = a.chunks > kMany * ctas && a.chunks < (int64_t(1) << 30);
     if (!r.clip || many) A2_CUDA_TRY(launch_chained(k_norms, dim3(workers), kThreads, 0, s, a, ctas));
     if (!r.clip) return cudaSuccess;
-    if (many) return launch_chained(table ? k_scale_chunks<false> : k_scale_chunks<true>, dim3((unsigned)(a.in_place ? std::min(a.chunks, 4 * ctas) : ceil_div(a.chunks, ctas) * ctas)), kThreads, 0, s, a, few, table, (unsigned)ctas);
+    if (many && in_place)
+        return launch_chained(table ? k_scale_in_place<false> : k_scale_in_place<true>, dim3((unsigned)std::min(a.chunks, 4 * ctas)), kThreads, 0, s, a, few, table,
+                              (unsigned)ctas);
+    if (many)
+        return launch_chained(table ? k_scale_chunks<false> : k_scale_chunks<true>, dim3((unsigned)(ceil_div(a.chunks, ctas) * ctas)), kThreads, 0, s, a, few, table,
+                              (unsigned)ctas);
     return launch_chained(table ? k_scale<false> : k_scale<true>, dim3((unsigned)ctas), kThreads, 0, s, a, few, table);
 }
 
