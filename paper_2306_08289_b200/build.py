@@ -1,4 +1,4 @@
-"""Compile the CUDA library for sm_100a into paper_2306_08289_b200/liba2cid2.so (in-tree).
+"""Compile the CUDA library for sm_100a into paper_2306_08289_b200/liba2cid2.so, and the host side of the operators' usual calls into _calls.so (in-tree).
 
 Extra nvcc flags for experiments may be given in the environment variable A2CID2_NVCC_FLAGS, e.g.
 "-DA2_EVENT_THREADS=512" (threads per CTA of the event kernel) or "-DA2_TUNING_KNOBS=1" (a build whose
@@ -10,12 +10,14 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "liba2cid2.so")
+CALLS = os.path.join(HERE, "_calls.so")
 SOURCES = ["api.cu", "kernels.cu", "scheduler.cpp", "spectral.cpp",
            "lm_api.cu", "embed.cu", "gemm_sm100.cu", "vocab_loss.cu", "vocab_loss_few.cu", "orthogonalize.cu",
            "lm_train_api.cu", "rms_norm.cu", "route.cu", "clip.cu"]
@@ -29,11 +31,26 @@ def _nvcc() -> str:
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALLS):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(INCLUDE, "a2cid2.h")]
     return any(os.path.getmtime(p) > t for p in deps)
+
+
+def _build_calls(tmp: str) -> subprocess.Popen:
+    """Starts the build of the host side of the usual operator calls (csrc/torch_calls.cpp), which is linked to torch and to LIB."""
+    import torch
+
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    include = os.path.join(os.path.dirname(torch.__file__), "include")
+    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-o", tmp,
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", INCLUDE, "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
+           "-isystem", os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include"), "-isystem", sysconfig.get_paths()["include"],
+           os.path.join(CSRC, "torch_calls.cpp"), "-L", HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN",
+           "-L", lib, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -55,6 +72,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if verbose:
         sys.stderr.write(r.stdout + r.stderr)
     os.replace(tmp, LIB)
+    tmp = CALLS + f".tmp{os.getpid()}"
+    calls = _build_calls(tmp)
+    text = calls.communicate()[0]
+    if calls.returncode != 0:
+        sys.stderr.write(text)
+        raise RuntimeError("g++ failed")
+    os.replace(tmp, CALLS)
     return LIB
 
 

@@ -62,6 +62,23 @@ def _vector(name, t, n, dtype, device):
     return t.data_ptr()
 
 
+_calls = None
+
+
+def _usual():
+    """The module that takes the usual calls (csrc/torch_calls.cpp): its functions return None for what they leave to the code below them."""
+    global _calls
+    if _calls is None:
+        B.lib()  # says so if nothing has been built
+        try:
+            from . import _calls as module
+        except ImportError as e:
+            raise ImportError(f"the host side of the operators' calls cannot be loaded ({e}): build it with `python -m paper_2306_08289_b200.build`") from e
+        module.set_error(B.A2Error)
+        _calls = module
+    return _calls
+
+
 class _Queue:
     """The context in which a call allocates and queues: the tensors' device and the stream. Entering it gives the raw stream. `given` are the
     caller's tensors (or None), `made` collects results allocated here: with a stream of the caller's, torch's allocator is told that the
@@ -238,6 +255,10 @@ def _norm_inputs(x, weight, residual, sum_out):
 def rms_norm(x, weight=None, residual=None, eps=1e-6, out=None, sum_out=None, stream=None):
     """s / sqrt(mean(s^2) + eps) * weight for every row of s = x + residual; x, residual [n, width], weight [width] of their type. Without a residual
     returns the result, with one (result, s). out may be x or residual, sum_out x or residual."""
+    if stream is None and out is None and sum_out is None:
+        done = _usual().rms_norm(x, weight, residual, eps)
+        if done is not None:
+            return done
     x_pitch, r_pitch, s_pitch, weight_p = _norm_inputs(x, weight, residual, sum_out)
     n, width = x.shape
     queue = _Queue(x.device, stream, x, weight, residual, out, sum_out)
@@ -258,6 +279,10 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, out=None, sum_out=None, st
 def rms_norm_quantized(x, weight=None, residual=None, eps=1e-6, block=128, sum_out=None, stream=None):
     """As `rms_norm` with the result in 8 bits: (values float8_e4m3fn [n, width], scales float32 [n, blocks]), and s where there is a residual. A scale
     is that of `block` columns (32, 64, 128, or 0 for a whole row): the result is values * scale (`dequantize`)."""
+    if stream is None and sum_out is None:
+        done = _usual().rms_norm_quantized(x, weight, residual, eps, block)
+        if done is not None:
+            return done
     x_pitch, r_pitch, s_pitch, weight_p = _norm_inputs(x, weight, residual, sum_out)
     n, width = x.shape
     block = _whole("block", block)
@@ -280,6 +305,10 @@ def rms_norm_quantized(x, weight=None, residual=None, eps=1e-6, block=128, sum_o
 def dequantize(values, scales, dtype=torch.bfloat16, out=None, stream=None):
     """values * scales in float32 or bfloat16, for what `rms_norm_quantized` returns. The columns of a scale follow from the shapes: the whole row for
     one scale a row of more than 128 columns, else 32, 64 or 128."""
+    if stream is None and out is None and dtype in _DTYPES:
+        done = _usual().dequantize(values, scales, _DTYPES[dtype])
+        if done is not None:
+            return done
     if not isinstance(values, torch.Tensor) or not values.is_cuda or values.dtype != torch.float8_e4m3fn or values.dim() != 2:
         _refuse("values must be a CUDA matrix of float8_e4m3fn")
     n, width = values.shape
@@ -313,6 +342,10 @@ def rms_norm_grad(grad_out, x, weight=None, eps=1e-6, grad_sum=None, grad_x=True
     """(grad_x, grad_weight): the gradients of `rms_norm` for its rows x (with a residual: the s it returned; grad_sum is then the gradient that reaches s
     by its other use, and grad_x that of both x and the residual). grad_x and grad_weight are True (allocate), None (leave out) or
     the tensor to write; without a weight grad_weight is None. grad_x may be grad_out, grad_sum or x."""
+    if stream is None and (grad_x is True or grad_x is None) and (grad_weight is True or grad_weight is None):
+        done = _usual().rms_norm_grad(grad_out, x, weight, eps, grad_sum, grad_x, grad_weight)
+        if done is not None:
+            return done
     g_pitch = _matrix("grad_out", grad_out)
     x_pitch = _matrix("x", x, grad_out, grad_out.shape)
     (n, width), dtype, device = x.shape, x.dtype, x.device
@@ -358,6 +391,10 @@ def route(logits, k, score="softmax", bias=None, groups=1, top_groups=1, group_s
     and how many tokens have chosen each. score "softmax" or "sigmoid"; bias float32 [n_experts] is added to the scores for the choice alone; of `groups` groups of
     experts the `top_groups` best are open (group_score "max": by their best expert, "top2": by the sum of their two best). Weights are scale * score, divided by
     the chosen scores' sum with renormalize. Logits of -inf or the type's lowest value are experts that are not available; ids are -1 where too few are."""
+    if stream is None and isinstance(score, str) and isinstance(group_score, str):
+        done = _usual().route(logits, k, _SCORES.get(score), bias, groups, top_groups, _GROUP_SCORES.get(group_score), bool(renormalize), scale)
+        if done is not None:
+            return done
     pitch = _matrix("logits", logits)
     n, experts = logits.shape
     device = logits.device
@@ -380,6 +417,10 @@ def route(logits, k, score="softmax", bias=None, groups=1, top_groups=1, group_s
 def route_grad(logits, ids, grad_weights, score="softmax", renormalize=True, scale=1.0, out=None, stream=None):
     """The gradient of `route`'s weights for its logits, the choice held fixed: ids are what it returned, grad_weights float32 [n, k] the gradient of its weights; score,
     renormalize and scale as given to it. Entries whose id is -1 do not matter. out may be logits."""
+    if stream is None and out is None and isinstance(score, str):
+        done = _usual().route_grad(logits, ids, grad_weights, _SCORES.get(score), bool(renormalize), scale)
+        if done is not None:
+            return done
     pitch = _matrix("logits", logits)
     n, experts = logits.shape
     device = logits.device
@@ -469,6 +510,10 @@ def _gradients(tensors, per_worker, out):
 
 
 def _clip(tensors, max_norm, zero_nonfinite, per_worker, out, stream):
+    if stream is None:
+        done = _usual().clip(tensors, out, bool(per_worker), max_norm, bool(zero_nonfinite))
+        if done is not None:
+            return done
     tensors, out, words, workers, device = _gradients(tensors, per_worker, out)
     queue = _Queue(device, stream, *tensors, *out)
     with queue as s:
