@@ -79,8 +79,6 @@ struct Operand {  // a 16-bit matrix, K-major [rows, k] or MN-major [k, rows], `
 };
 [[nodiscard]] cudaError_t make_gemm(const Operand& a, const Operand& b, int64_t mats, bool bf16, bool lower, int flush, int splits, GemmArgs* out);
 [[nodiscard]] cudaError_t gave_up_flag(int** out);  // where kernels note a wait that ran out on the current device
-// Lets a kernel use `bytes` of dynamic shared memory on the current device; `done` remembers the devices it was asked on.
-[[nodiscard]] cudaError_t allow_large_clusters(const void* kernel, std::atomic<uint64_t>& done);  // more than 8 CTAs
 int gemm_clusters();  // CTA pairs that run at once on the current device
 
 #ifdef __CUDACC__

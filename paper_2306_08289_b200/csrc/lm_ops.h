@@ -95,7 +95,8 @@ cudaError_t run_orthogonalize(const OrthogonalizeArgs& a, void* workspace, cudaS
 int multiprocessors();  // of the current device
 
 // Allows a kernel its dynamic shared memory, once for each device (`done`: which of them).
-cudaError_t allow_shared_memory(const void* kernel, int bytes, std::atomic<uint64_t>& done);
+[[nodiscard]] cudaError_t allow_shared_memory(const void* kernel, int bytes, std::atomic<uint64_t>& done);
+[[nodiscard]] cudaError_t allow_large_clusters(const void* kernel, std::atomic<uint64_t>& done);  // more than 8 CTAs
 
 constexpr int64_t kMaxNormWidth = 32768;  // columns of a normalised row: it is held in the registers of a CTA
 

@@ -447,6 +447,17 @@ __device__ __forceinline__ void wait_copies() {
     asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
 }
 
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float load_of_cta(const float* p, unsigned cta) {  // from the place p of another CTA's shared memory
+    uint32_t at;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(cta));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+
 struct NormGradKernelArgs {
     const void *g, *x, *weight, *ds;
     int64_t g_pitch, x_pitch, ds_pitch, n;
@@ -454,7 +465,8 @@ struct NormGradKernelArgs {
     float eps, one_over_width;
     void* dx;
     int64_t dx_pitch;
-    float* parts;  // [CTAs][width], or NULL without a gradient of the weight
+    float* parts;  // [CTAs][width], or NULL without a gradient of the weight, or if the CTAs are one cluster and join their parts themselves:
+    void* dw;      // the gradient of the weight then, else NULL
     int64_t slots, x_step, g_step, ds_step, dx_step;  // elements from one row of a slot to the next
     int group;
     bool wide_weight;
@@ -630,13 +642,14 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
         else
             stage = stage + 1 == kStages ? 0 : stage + 1;
     }
-    if (!a.parts) return;
-    float* part = a.parts + (int64_t)blockIdx.x * width;
+    if (!a.parts && !a.dw) return;
     float* rows = reinterpret_cast<float*>(memory);
-    if (!LEAN && groups > 1) {
+    const bool one_cluster = !LEAN && a.dw;
+    if (!LEAN && (groups > 1 || one_cluster)) {
         wait_copies<0>();
         __syncthreads();  // the place of the rows to come is free
     }
+    float* part = one_cluster ? rows + (groups > 1 ? groups * width : 0) : a.parts + (int64_t)blockIdx.x * width;
     float* to = groups > 1 ? rows + mine * width : part;
 #pragma unroll
     for (int j = 0; j < K; ++j)
@@ -651,13 +664,26 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
             if (c >= 0 && c < width) to[c] = f.x;
             if (c + 1 >= 0 && c + 1 < width) to[c + 1] = f.y;
         }
-    if (groups == 1) return;
-    __syncthreads();
-    for (int c = threadIdx.x; c < width; c += blockDim.x) {
-        float sum = 0.0f;
-        for (int q = 0; q < groups; ++q) sum += rows[q * width + c];
-        part[c] = sum;
+    if (groups > 1) {
+        __syncthreads();
+        for (int c = threadIdx.x; c < width; c += blockDim.x) {
+            float sum = 0.0f;
+            for (int q = 0; q < groups; ++q) sum += rows[q * width + c];
+            part[c] = sum;
+        }
     }
+    if (!one_cluster) return;
+    // the columns are shared out over the CTAs of the cluster; sixteen lanes take a column, each the part of one CTA
+    cluster_barrier();
+    const int q = threadIdx.x % 16, columns_at_once = blockDim.x / 16;
+    for (int i = 0; i * (int)gridDim.x < width; i += columns_at_once) {
+        const int c = (i + (int)threadIdx.x / 16) * gridDim.x + blockIdx.x;
+        float sum = c < width && q < (int)gridDim.x ? load_of_cta(part + c, q) : 0.0f;
+#pragma unroll
+        for (int d = 8; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (q == 0 && c < width) static_cast<T*>(a.dw)[c] = narrow<T>(sum);
+    }
+    cluster_barrier();  // no CTA ends while another reads its memory
 }
 
 // dw from the CTAs' parts: 32 columns a CTA, every warp a share of the parts, joined in order.
@@ -688,19 +714,30 @@ Shape grad_shape(int64_t width, bool shifted) {  // shifted: rows may start behi
 // The first kernel's launch. A CTA has as many groups as make 512 threads, for a part of dw each CTA is written and read again; fewer where there are not rows
 // enough to give each multiprocessor some. At most as many CTAs as are resident at once (two a multiprocessor with one vector a thread, else one); where a
 // group has several rows, so many that the slots are a multiple of 8.
+// With few rows they are one cluster of up to 16 CTAs, which joins its parts of dw itself: no workspace, and no second launch.
+constexpr int kClusterRows = 4;  // of a group, at most: four rows one after the other are as long as the second launch
+
 struct GradLaunch {
     int groups;
     int64_t ctas;
+    bool one_cluster;
 };
-GradLaunch grad_launch(int64_t n, const Shape& shape) {
+GradLaunch grad_launch(int64_t n, const Shape& shape, bool lean, bool with_weight) {
+    const int most_groups = std::max(1, 512 / shape.group);
+    if (!lean && with_weight && n <= (int64_t)16 * most_groups * kClusterRows)
+        return {most_groups, std::min<int64_t>(16, std::max<int64_t>(1, ceil_div(n, most_groups))), true};
     const int64_t sms = multiprocessors(), resident = sms * (shape.k == 1 ? 2 : 1);
     const int whole = std::max(1, 32 / shape.group);  // groups of a warp
-    int groups = (int)std::min<int64_t>(std::max(1, 512 / shape.group), round_up(std::max<int64_t>(ceil_div(n, sms), 1), whole));
+    int groups = (int)std::min<int64_t>(most_groups, round_up(std::max<int64_t>(ceil_div(n, sms), 1), whole));
     const int64_t ctas = ceil_div(n, groups);
-    if (ctas <= resident) return {groups, std::max<int64_t>(ctas, 1)};
+    if (ctas <= resident) return {groups, std::max<int64_t>(ctas, 1), false};
     int64_t most = resident;
     while (most * groups % 8) --most;
-    return {groups, std::max<int64_t>(most, 1)};
+    return {groups, std::max<int64_t>(most, 1), false};
+}
+template <class T>
+bool is_lean(const Shape& shape) {
+    return shape.k > (sizeof(T) == 2 ? 2 : 4);
 }
 
 template <class T, bool WIDE, int K, bool LEAN, int THREADS>
@@ -710,7 +747,12 @@ cudaError_t launch_grad_kernel(const NormGradKernelArgs& a, unsigned ctas, unsig
     static std::atomic<uint64_t> allowed{0};
     auto* kernel = k_norm_grad<T, WIDE, K, LEAN, THREADS, kCtas>;
     A2_CUDA_TRY(allow_shared_memory(reinterpret_cast<const void*>(kernel), (int)most, allowed));
-    return launch_chained(kernel, dim3(ctas), threads, each * threads, s, a);  // rows of dw of several groups take less: K vectors of floats a thread
+    if (a.dw) {
+        static std::atomic<uint64_t> clusters{0};
+        if (ctas > 8) A2_CUDA_TRY(allow_large_clusters(reinterpret_cast<const void*>(kernel), clusters));
+        return launch_clusters(kernel, dim3(ctas), threads, each * threads, ctas, s, a);
+    }
+    return launch_chained(kernel, dim3(ctas), threads, each * threads, s, a);  // rows of dw of several groups, and their sum, take less: K vectors of floats a thread
 }
 
 template <class T, bool WIDE>
@@ -735,12 +777,13 @@ cudaError_t norm_grad_typed(const NormGradArgs& n, void* workspace, cudaStream_t
     const bool wide = alike<T>(n.x, n.x_pitch, n.grad_out, n.grad_out_pitch, n.n) && (!n.grad_sum || alike<T>(n.x, n.x_pitch, n.grad_sum, n.grad_sum_pitch, n.n)) &&
                       (!n.grad_x || alike<T>(n.x, n.x_pitch, n.grad_x, n.grad_x_pitch, n.n)) && (aligned || room);
     const Shape shape = grad_shape<T>(n.width, wide && !aligned);
-    const GradLaunch launch = grad_launch(n.n, shape);
+    const GradLaunch launch = grad_launch(n.n, shape, is_lean<T>(shape), n.grad_weight != nullptr);
+    const bool parts = n.grad_weight && !launch.one_cluster;
     NormGradKernelArgs a{n.grad_out, n.x, n.weight, n.grad_sum, n.grad_out_pitch, n.x_pitch, n.grad_sum_pitch, n.n, (int)n.width, n.eps, 1.0f / (float)n.width, n.grad_x, n.grad_x_pitch,
-                         n.grad_weight ? Carver(workspace).take<float>(launch.ctas * n.width) : nullptr, 0, 0, 0, 0, 0, 0,
+                         parts ? Carver(workspace).take<float>(launch.ctas * n.width) : nullptr, launch.one_cluster ? n.grad_weight : nullptr, 0, 0, 0, 0, 0, 0,
                          reinterpret_cast<uintptr_t>(n.weight) % 16 == 0};
     A2_CUDA_TRY((wide ? launch_norm_grad<T, true>(a, shape, launch, s) : launch_norm_grad<T, false>(a, shape, launch, s)));
-    if (!n.grad_weight) return cudaSuccess;
+    if (!parts) return cudaSuccess;
     return launch_chained(k_norm_join<T>, dim3((unsigned)ceil_div(n.width, 32)), 1024, 0, s, a.parts, launch.ctas, n.width, static_cast<T*>(n.grad_weight));
 }
 
@@ -760,9 +803,13 @@ int64_t norm_grad_workspace(int64_t n, int64_t width, bool with_weight, int32_t 
     if (!with_weight) return 0;
     Carver c(nullptr);
     int64_t most = 0;
-    for (const bool shifted : {false, true})
-        if (!shifted || width + 8 <= kMaxNormWidth)
-            most = std::max(most, grad_launch(n, dtype == A2_BF16 ? grad_shape<__nv_bfloat16>(width, shifted) : grad_shape<float>(width, shifted)).ctas);
+    for (const bool shifted : {false, true}) {
+        if (shifted && width + 8 > kMaxNormWidth) continue;
+        const Shape shape = dtype == A2_BF16 ? grad_shape<__nv_bfloat16>(width, shifted) : grad_shape<float>(width, shifted);
+        const GradLaunch launch = grad_launch(n, shape, dtype == A2_BF16 ? is_lean<__nv_bfloat16>(shape) : is_lean<float>(shape), true);
+        if (!launch.one_cluster) most = std::max(most, launch.ctas);
+    }
+    if (most == 0) return 0;
     c.take<float>(most * width);
     return c.used;
 }

@@ -452,7 +452,8 @@ cudaError_t route_typed(const RouteArgs& r, cudaStream_t s) {
 //                  that (softmax) or that times 1 - s_j (sigmoid);
 //   sigmoid        dz_j = h_j (1 - s_j);      softmax  dz_e = [e chosen] h_e - s_e sum_m h_m for every expert.
 // LANES lanes take a token, lane j its j-th chosen expert, and all of them the row of the gradient, in vectors of 16 bytes (WIDE) or element by
-// element, side by side. Bound by memory for few chosen experts, by the 3 N + 2 instructions that each of them takes for more.
+// element, side by side; then each chosen expert's lane writes that element once more, with the expert's own part. (Handing every expert to the lane that has
+// its element takes 2 N + 2 instructions each.) In place: a warp has read all that it needs of a token's row before it writes.
 // ---------------------------------------------------------------------------------------------
 struct RouteGradKernelArgs {
     const void* logits;
@@ -486,7 +487,7 @@ __global__ void __launch_bounds__(kThreads) k_route_grad(const __grid_constant__
         const float x = named ? logit<T>(widen(row[mine])) : -INFINITY;
         const bool chosen = x > -INFINITY;
         if (!chosen) mine = -1, g = 0.0f;
-        float d[N], h;
+        float d[N], h, rest = 0.0f;  // the row without the chosen experts' own part; that, and what the row has at this lane's expert
 #pragma unroll
         for (int j = 0; j < N; ++j) d[j] = 0.0f;
         if (a.renormalize) {
@@ -523,30 +524,32 @@ __global__ void __launch_bounds__(kThreads) k_route_grad(const __grid_constant__
             float total = 0.0f;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                d[j] = expf(d[j] - most);
+                d[j] = near_exp(d[j] - most);
                 total += d[j];
             }
             total = lanes_sum<LANES>(total);
-            const float one = total > 0.0f ? 1.0f / total : 0.0f;
-            h = chosen ? g * expf(x - most) * one : 0.0f;
-            const float all = lanes_sum<LANES>(h) * one;
+            const float one = total > 0.0f ? 1.0f / total : 0.0f, s = chosen ? near_exp(x - most) : 0.0f;
+            h = g * s * one;
+            const float all = lanes_sum<LANES>(h) * -one;
 #pragma unroll
-            for (int j = 0; j < N; ++j) d[j] *= -all;
+            for (int j = 0; j < N; ++j) d[j] *= all;
+            rest = s * all;
         }
-        // the chosen experts' places: -1 but for the lane that has the expert
-        const int vector = mine / V;
-        const int holder = mine >= 0 ? vector % LANES : LANES, place = vector / LANES * V + mine % V;
-        for (int c = 0; c < a.k; ++c) {
-            const int at = __shfl_sync(kAll, holder << 8 | place, base + c);
-            const float v = __shfl_sync(kAll, h, base + c);
-            const int j0 = at >> 8 == lane ? at & 255 : -1;
-#pragma unroll
-            for (int j = 0; j < N; ++j) d[j] += j == j0 ? v : 0.0f;
+        // an expert that a token has twice: the first of the two lanes has their sum, in order
+        const unsigned alike = __match_any_sync(kAll, chosen ? base << 16 | mine : -1 - (int)(threadIdx.x % 32));
+        bool writes = chosen && wanted < a.n;
+        if (__any_sync(kAll, __popc(alike) > 1)) {
+            float sum = 0.0f;
+            for (int c = 0; c < 32; ++c) {
+                const float v = __shfl_sync(kAll, h, c);
+                if (alike >> c & 1) sum += v;
+            }
+            h = sum;
+            writes = writes && __ffs(alike) - 1 == (int)(threadIdx.x % 32);
         }
-        if (wanted >= a.n) continue;
 #pragma unroll
         for (int j = 0; j < N; j += V) {
-            if (column(j) >= a.experts) continue;
+            if (column(j) >= a.experts || wanted >= a.n) continue;
             if constexpr (WIDE) {
                 float f[V];
 #pragma unroll
@@ -556,6 +559,9 @@ __global__ void __launch_bounds__(kThreads) k_route_grad(const __grid_constant__
                 out[column(j)] = narrow<T>(d[j]);
             }
         }
+        __syncwarp();  // orders the warp's writes: the chosen experts' come second
+        if (writes) out[mine] = narrow<T>(rest + h);
+        __syncwarp();  // and before what the next token's lanes read, where it is in place
     }
 }
 
