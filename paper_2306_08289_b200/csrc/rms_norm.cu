@@ -131,22 +131,27 @@ struct NormKernelArgs {
 __device__ __forceinline__ uint32_t bits_of(const float* p) { return __float_as_uint(*p); }
 __device__ __forceinline__ uint32_t bits_of(const __nv_bfloat16* p) { return *reinterpret_cast<const uint16_t*>(p); }
 
+// How rows lie: vectors are found in two units each; on boundaries, the ends cut; or on boundaries and all K vectors of all threads whole.
+enum Lie { kAnywhere, kWide, kFull };
+
 // A thread's vectors of a row.
-template <class T, bool WIDE>
+template <class T, Lie LIE, int K>
 struct Columns {
+    static constexpr bool WIDE = LIE != kAnywhere;
     int first, step, width;  // the column of vector 0, columns from one vector to the next
     bool cut;                // one of them is cut at the row's ends
     __device__ Columns(const void* row, int t, int group, int w) {
-        first = t * kVec<T> - (WIDE ? (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T)) : 0);
+        first = t * kVec<T> - (LIE == kWide ? (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T)) : 0);
         step = group * kVec<T>;
         width = w;
-        const int rest = (w - first) % step;  // of the row behind this thread's last whole vector
-        cut = !WIDE || first < 0 || (rest > 0 && rest < kVec<T>);
+        cut = LIE == kAnywhere || (LIE == kWide && first < 0);
+        if (LIE == kWide)
+#pragma unroll
+            for (int j = 0; j < K; ++j) cut = cut || (at(j) < w && at(j) + kVec<T> > w);
     }
     __device__ int at(int j) const { return first + j * step; }
-    __device__ bool in(int j) const { return at(j) < width; }
+    __device__ bool in(int j) const { return LIE == kFull || at(j) < width; }
     // Loads K vectors, all of them before anything is done with one: zeros past the row's ends.
-    template <int K>
     __device__ void load(Words (&p)[K], const T* row) const {
 #pragma unroll
         for (int j = 0; j < K; ++j) {
@@ -154,7 +159,6 @@ struct Columns {
             if (in(j)) p[j] = WIDE ? *reinterpret_cast<const Words*>(row + at(j)) : load_anywhere(row, at(j), width);
         }
     }
-    template <int K>
     __device__ void clear_past_ends(Words (&p)[K]) const {
         if (!WIDE || !cut) return;
 #pragma unroll
@@ -170,7 +174,7 @@ struct Columns {
     }
     // A vector of the weight, which may start elsewhere.
     __device__ Words load_weight(const T* w, int j, bool wide) const {
-        if (wide && !cut && first % kVec<T> == 0) return *reinterpret_cast<const Words*>(w + at(j));
+        if (wide && !cut && (LIE == kFull || first % kVec<T> == 0)) return *reinterpret_cast<const Words*>(w + at(j));
         if (at(j) >= 0) return load_anywhere(w, at(j), width);
         Words p{};  // the vector that begins before the row
 #pragma unroll
@@ -180,19 +184,18 @@ struct Columns {
     }
 };
 
-template <class T, bool WIDE, int K, int MODE, int THREADS>
+template <class T, Lie LIE, int K, int MODE, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ NormKernelArgs a) {
     constexpr int V = kVec<T>, H = V / 2;
     __shared__ float shared[2][32 * 2];
     ptx::chained();
     const int group = a.group, width = a.width;
-    const Place place(group);
-    const int t = place.t, mine = place.mine;
+    const int mine = group > 32 ? 0 : threadIdx.x >> (31 - __clz(group)), t = group > 32 ? threadIdx.x : threadIdx.x & (group - 1);
     const int64_t row = group > 32 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (blockDim.x / group) + mine;
     if (row >= a.n) return;  // whole groups, which are CTAs where they are more than a warp
     const T* x = static_cast<const T*>(a.x) + row * a.x_pitch;
     const T* w = static_cast<const T*>(a.weight);
-    const Columns<T, WIDE> columns(x, t, group, width);
+    const Columns<T, LIE, K> columns(x, t, group, width);
 
     float2 v[K][H];
     {
@@ -329,16 +332,22 @@ Shape shape_of(int64_t vecs, int64_t one, int64_t two, int64_t four, int least) 
     return {k, group};
 }
 
-template <class T, bool WIDE, int MODE>
+template <class T>
+bool is_full(const void* x, int64_t pitch, int64_t width, const Shape& shape) {
+    return aligned16<T>(x, pitch) && width == (int64_t)shape.k * shape.group * kVec<T>;
+}
+
+template <class T, Lie LIE, int MODE>
 cudaError_t launch_norm(NormKernelArgs& a, const Shape& shape, cudaStream_t s) {
     const unsigned threads = cta_threads(shape);
     const dim3 grid((unsigned)ceil_div(a.n, threads / shape.group));
     a.group = shape.group;
+    constexpr Lie kLong = LIE == kFull ? kWide : LIE;  // the longest rows are not told apart
     switch (shape.k) {
-        case 1: return launch_chained(k_norm<T, WIDE, 1, MODE, 512>, grid, threads, 0, s, a);
-        case 2: return launch_chained(k_norm<T, WIDE, 2, MODE, 512>, grid, threads, 0, s, a);
-        case 4: return launch_chained(k_norm<T, WIDE, 4, MODE, 512>, grid, threads, 0, s, a);
-        default: return launch_chained(k_norm<T, WIDE, 8, MODE, (sizeof(T) == 2 ? 512 : 1024)>, grid, threads, 0, s, a);
+        case 1: return launch_chained(k_norm<T, LIE, 1, MODE, 512>, grid, threads, 0, s, a);
+        case 2: return launch_chained(k_norm<T, LIE, 2, MODE, 512>, grid, threads, 0, s, a);
+        case 4: return launch_chained(k_norm<T, LIE, 4, MODE, 512>, grid, threads, 0, s, a);
+        default: return launch_chained(k_norm<T, kLong, 8, MODE, (sizeof(T) == 2 ? 512 : 1024)>, grid, threads, 0, s, a);
     }
 }
 
@@ -362,9 +371,13 @@ cudaError_t norm_typed(const NormArgs& n, cudaStream_t s) {
             vecs = ceil_div(n.width + V - 1, V);
     }
     const Shape shape = shape_of(vecs, 32, sizeof(T) == 2 ? 1024 : 64, 2048, std::max<int>(8, (int)(n.block / V)));
-    if (!n.scales) return wide ? launch_norm<T, true, 0>(a, shape, s) : launch_norm<T, false, 0>(a, shape, s);
-    if (n.block) return wide ? launch_norm<T, true, 1>(a, shape, s) : launch_norm<T, false, 1>(a, shape, s);
-    return wide ? launch_norm<T, true, 2>(a, shape, s) : launch_norm<T, false, 2>(a, shape, s);
+    const Lie lie = !wide ? kAnywhere : is_full<T>(n.x, n.x_pitch, n.width, shape) ? kFull : kWide;
+    auto launch = [&](auto mode) {
+        constexpr int kMode = decltype(mode)::value;
+        return lie == kFull ? launch_norm<T, kFull, kMode>(a, shape, s) : lie == kWide ? launch_norm<T, kWide, kMode>(a, shape, s) : launch_norm<T, kAnywhere, kMode>(a, shape, s);
+    };
+    if (!n.scales) return launch(std::integral_constant<int, 0>{});
+    return n.block ? launch(std::integral_constant<int, 1>{}) : launch(std::integral_constant<int, 2>{});
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -379,6 +392,7 @@ __global__ void __launch_bounds__(256) k_dequantize(const uint8_t* __restrict__ 
     const int64_t row = (int64_t)blockIdx.x * (256 / group) + threadIdx.x / group;
     if (row >= n) return;
     auto value = [](uint8_t b) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(b, __NV_E4M3))); };
+#pragma unroll 2
     for (int c = (int)threadIdx.x % group * kBack; c < width; c += group * kBack) {
         const float scale = scales[row * blocks + (blocks > 1 ? c >> block_log : 0)];
         const uint8_t* q = values + row * values_pitch + c;
@@ -422,7 +436,7 @@ cudaError_t dequantize_typed(const DequantizeArgs& a, cudaStream_t s) {
     const int blocks = a.block ? (int)ceil_div(a.width, a.block) : 1, block_log = a.block == 128 ? 7 : a.block == 64 ? 6 : 5;
     const bool wide = reinterpret_cast<uintptr_t>(a.values) % kBack == 0 && a.values_pitch % kBack == 0 && aligned16<T>(a.out, a.out_pitch);
     int group = 1;
-    while (group < 256 && group * (wide ? kBack : 8) < a.width) group *= 2;
+    while (group < 256 && group * (wide ? 2 * kBack : 8) < a.width) group *= 2;
     return launch_chained(wide ? k_dequantize<T> : k_dequantize_single<T>, dim3((unsigned)ceil_div(a.n, 256 / group)), 256, 0, s, a.values, a.values_pitch,
                           a.scales, a.n, (int)a.width, block_log, blocks, static_cast<T*>(a.out), a.out_pitch, group);
 }
@@ -472,9 +486,10 @@ struct NormGradKernelArgs {
     bool wide_weight;
 };
 
-template <class T, bool WIDE, int K, bool LEAN, int THREADS, int CTAS>
+template <class T, Lie LIE, int K, bool LEAN, int THREADS, int CTAS>
 __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_constant__ NormGradKernelArgs a) {
     constexpr int V = kVec<T>, H = V / 2, kStages = kStagesOf<K>;
+    constexpr bool WIDE = LIE != kAnywhere;
     __shared__ float shared[2][32 * 2];
     extern __shared__ uint4 memory[];  // LEAN: every thread's part of dw. Else rows to come, and at the end, with several groups a CTA, a row of dw for each
     ptx::chained();
@@ -486,7 +501,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
     const T* g = static_cast<const T*>(a.g) + first * a.g_pitch;
     const T* ds = static_cast<const T*>(a.ds) + first * a.ds_pitch;
     T* dx = static_cast<T*>(a.dx) + first * a.dx_pitch;
-    const Columns<T, WIDE> columns(x, t, group, width);
+    const Columns<T, LIE, K> columns(x, t, group, width);
     // the vectors of one row: [stage][matrix][j][thread]
     auto ahead = [&](int stage, int matrix, int j) -> Words& { return reinterpret_cast<Words*>(memory)[((stage * 3 + matrix) * K + j) * blockDim.x + threadIdx.x]; };
     auto bring_row = [&](int stage, const T* x, const T* g, const T* ds) {
@@ -715,7 +730,7 @@ Shape grad_shape(int64_t width, bool shifted) {  // shifted: rows may start behi
 // enough to give each multiprocessor some. At most as many CTAs as are resident at once (two a multiprocessor with one vector a thread, else one); where a
 // group has several rows, so many that the slots are a multiple of 8.
 // With few rows they are one cluster of up to 16 CTAs, which joins its parts of dw itself: no workspace, and no second launch.
-constexpr int kClusterRows = 4;  // of a group, at most: four rows one after the other are as long as the second launch
+constexpr int kClusterRows = 2;  // of a group, at most: 1,001 x 201 fp32 (four rows each) 9.5 us in one launch, 6.7 in two
 
 struct GradLaunch {
     int groups;
@@ -740,12 +755,12 @@ bool is_lean(const Shape& shape) {
     return shape.k > (sizeof(T) == 2 ? 2 : 4);
 }
 
-template <class T, bool WIDE, int K, bool LEAN, int THREADS>
+template <class T, Lie LIE, int K, bool LEAN, int THREADS>
 cudaError_t launch_grad_kernel(const NormGradKernelArgs& a, unsigned ctas, unsigned threads, cudaStream_t s) {
     constexpr int kCtas = !LEAN && K == 1 ? 2 : 1;
     constexpr size_t each = LEAN ? K * kVec<T> * 4 : kStagesOf<K> * 3 * K * 16, most = each * THREADS;  // bytes of a thread
     static std::atomic<uint64_t> allowed{0};
-    auto* kernel = k_norm_grad<T, WIDE, K, LEAN, THREADS, kCtas>;
+    auto* kernel = k_norm_grad<T, LIE, K, LEAN, THREADS, kCtas>;
     A2_CUDA_TRY(allow_shared_memory(reinterpret_cast<const void*>(kernel), (int)most, allowed));
     if (a.dw) {
         static std::atomic<uint64_t> clusters{0};
@@ -755,20 +770,21 @@ cudaError_t launch_grad_kernel(const NormGradKernelArgs& a, unsigned ctas, unsig
     return launch_chained(kernel, dim3(ctas), threads, each * threads, s, a);  // rows of dw of several groups, and their sum, take less: K vectors of floats a thread
 }
 
-template <class T, bool WIDE>
+template <class T, Lie LIE>
 cudaError_t launch_norm_grad(NormGradKernelArgs& a, const Shape& shape, const GradLaunch& launch, cudaStream_t s) {
     const unsigned threads = launch.groups * shape.group, ctas = (unsigned)launch.ctas;
     a.group = shape.group;
     a.slots = launch.ctas * launch.groups;
     a.x_step = a.slots * a.x_pitch, a.g_step = a.slots * a.g_pitch, a.ds_step = a.slots * a.ds_pitch, a.dx_step = a.slots * a.dx_pitch;
+    constexpr Lie kLong = LIE == kFull ? kWide : LIE;
     switch (shape.k) {
-        case 1: return launch_grad_kernel<T, WIDE, 1, false, 512>(a, ctas, threads, s);
-        case 2: return launch_grad_kernel<T, WIDE, 2, false, 512>(a, ctas, threads, s);
-        case 4: return launch_grad_kernel<T, WIDE, 4, sizeof(T) == 2, 512>(a, ctas, threads, s);
+        case 1: return launch_grad_kernel<T, LIE, 1, false, 512>(a, ctas, threads, s);
+        case 2: return launch_grad_kernel<T, LIE, 2, false, 512>(a, ctas, threads, s);
+        case 4: return launch_grad_kernel<T, LIE, 4, sizeof(T) == 2, 512>(a, ctas, threads, s);
         default: break;
     }
-    if (threads <= 512) return launch_grad_kernel<T, WIDE, 8, true, 512>(a, ctas, threads, s);
-    return launch_grad_kernel<float, WIDE, 8, true, 1024>(a, ctas, threads, s);  // rows of fp32 alone are that long
+    if (threads <= 512) return launch_grad_kernel<T, kLong, 8, true, 512>(a, ctas, threads, s);
+    return launch_grad_kernel<float, kLong, 8, true, 1024>(a, ctas, threads, s);  // rows of fp32 alone are that long
 }
 
 template <class T>
@@ -782,7 +798,9 @@ cudaError_t norm_grad_typed(const NormGradArgs& n, void* workspace, cudaStream_t
     NormGradKernelArgs a{n.grad_out, n.x, n.weight, n.grad_sum, n.grad_out_pitch, n.x_pitch, n.grad_sum_pitch, n.n, (int)n.width, n.eps, 1.0f / (float)n.width, n.grad_x, n.grad_x_pitch,
                          parts ? Carver(workspace).take<float>(launch.ctas * n.width) : nullptr, launch.one_cluster ? n.grad_weight : nullptr, 0, 0, 0, 0, 0, 0,
                          reinterpret_cast<uintptr_t>(n.weight) % 16 == 0};
-    A2_CUDA_TRY((wide ? launch_norm_grad<T, true>(a, shape, launch, s) : launch_norm_grad<T, false>(a, shape, launch, s)));
+    const cudaError_t e = !wide ? launch_norm_grad<T, kAnywhere>(a, shape, launch, s)
+                          : is_full<T>(n.x, n.x_pitch, n.width, shape) ? launch_norm_grad<T, kFull>(a, shape, launch, s) : launch_norm_grad<T, kWide>(a, shape, launch, s);
+    A2_CUDA_TRY(e);
     if (!parts) return cudaSuccess;
     return launch_chained(k_norm_join<T>, dim3((unsigned)ceil_div(n.width, 32)), 1024, 0, s, a.parts, launch.ctas, n.width, static_cast<T*>(n.grad_weight));
 }
