@@ -764,3 +764,60 @@ def test_a_backward_graph_beside_an_eager_one():
     graph.replay()
     eager.backward()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(leaf.grad, torch.full_like(leaf, 2.0))
+
+
+def reference_loss(model, row, ids, targets, scale, chosen):
+    """The example's loss in torch, whose autograd gives its gradient; `chosen` are the experts that the model has taken."""
+    w = model.width
+    y = model.part(row, "E")[ids.long()] * math.sqrt(w)
+    rms = lambda v, g: v / torch.sqrt((v * v).mean(1, keepdim=True) + 1e-6) * g  # noqa: E731
+    u = rms(y, model.part(row, "N")) if model.norm else y
+    if model.experts:
+        s = torch.softmax(u @ model.part(row, "R").T, 1).gather(1, chosen)
+        s = s / s.sum(1, keepdim=True)
+        each = torch.tanh(torch.einsum("ti,eoi->teo", u, model.hidden(row)))
+        a = (s[:, :, None] * each.gather(1, chosen[:, :, None].expand(-1, -1, w))).sum(1)
+    else:
+        a = torch.tanh(u @ model.part(row, "M").T)
+    h = rms(y + a, model.part(row, "F")) if model.norm else y + a
+    live = targets >= 0
+    z = h @ model.part(row, "W").T
+    return scale * (torch.logsumexp(z, 1) - z.gather(1, targets.long().clamp(min=0)[:, None])[:, 0])[live].sum()
+
+
+@pytest.mark.parametrize("norm,experts", [(False, 0), (True, 0), (False, 5), (True, 8)])
+def test_gradients_of_the_example(norm, experts):
+    """Norm, routing, embedding and loss forward and backward in a model, against autograd in 64 bits."""
+    from paper_2306_08289_b200 import language_model as LM
+
+    text = LM.MarkovText(40, 4, 1)
+    model = LM.Model(40, 24, norm=norm, experts=experts)
+    row = torch.from_numpy(model.initial_row(5)).to(DEV)
+    row += 0.05 * torch.randn(model.d, generator=gen(1), device=DEV)
+    ids, targets = (torch.from_numpy(v).to(DEV) for v in text.draw(np.random.default_rng(2), 6, 11))
+    out = torch.full((model.d,), math.nan, device=DEV)
+    model.gradient(row, ids, targets, 0.1, out)
+    chosen = None
+    if experts:
+        *_, kept, _, _ = model.forward(row, ids)
+        chosen = kept[1].long()
+    wide = row.double().requires_grad_()
+    reference_loss(model, wide, ids, targets, 0.1, chosen).backward()
+    want = wide.grad
+    # a chain of fp32 products of up to 66 terms each: some hundred roundings of a part's own size
+    for name in model.shape:
+        g, d = model.part(out, name).double(), model.part(want, name)
+        assert (g - d).norm() <= 1e-5 * d.norm(), name
+    model.gradient(row.bfloat16(), ids, targets, 0.1, out.bfloat16())
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+def test_rows_of_an_engine_train_a_model_with_norms_and_experts(storage):
+    """The operators together as a user runs them: norms, experts and clipping in the closed loop."""
+    from paper_2306_08289_b200 import language_model
+
+    trace, entropy = language_model.train(n=4, vocab=64, width=32, T=6.0, storage=storage, sequences=4, length=16, samples=2, norm=True, experts=4, clip=1.0)
+    assert len(trace) >= 3 and all(len(row) == 4 and all(math.isfinite(v) for v in row) for row in trace)
+    trace, _ = language_model.train(n=4, vocab=64, width=32, T=6.0, storage=storage, sequences=4, length=16, samples=2, clip=0.5)
+    assert all(len(row) == 3 and all(math.isfinite(v) for v in row) for row in trace)
+    ops.check()
