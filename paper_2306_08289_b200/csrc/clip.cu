@@ -181,8 +181,20 @@ __device__ __forceinline__ double chunk_squares(const Tensor& t, int64_t worker,
     return sum;
 }
 
+struct Factor {
+    float by, then;      // two factors: one alone may lie below the range of floats where the result does not
+    bool zero, nothing;  // nothing: by one
+};
+__device__ __forceinline__ Factor factor_of(const ClipKernelArgs& a, double norm) {
+    if (!isfinite(norm)) return {1.0f, 1.0f, a.zero_nonfinite, !a.zero_nonfinite};
+    if (norm <= a.max_norm) return {1.0f, 1.0f, false, true};
+    const double factor = a.max_norm / norm;
+    if (factor < 0x1p-100) return {(float)(factor * 0x1p100), 0x1p-100f, false, false};
+    return {(float)factor, 1.0f, false, false};
+}
+
 template <class T, int THREADS>
-__device__ __forceinline__ void scale_chunk(const Tensor& t, int64_t worker, int64_t chunk, float factor, bool zero) {
+__device__ __forceinline__ void scale_chunk(const Tensor& t, int64_t worker, int64_t chunk, const Factor& f) {
     constexpr int V = 16 / sizeof(T);
     over_chunk<T, THREADS>(
         t, worker, chunk,
@@ -196,30 +208,20 @@ __device__ __forceinline__ void scale_chunk(const Tensor& t, int64_t worker, int
                 float v[V];
                 unpack<T>(p[i], v);
 #pragma unroll
-                for (int k = 0; k < V; ++k) v[k] = zero ? 0.0f : v[k] * factor;
+                for (int k = 0; k < V; ++k) v[k] = f.zero ? 0.0f : v[k] * f.by * f.then;
                 store_once(out + to(i), pack<T>(v));
             }
         },
-        [&](const T* in, T* out) { *out = narrow<T>(zero ? 0.0f : widen(*in) * factor); });
-}
-
-struct Factor {
-    float by;
-    bool zero, nothing;  // nothing: by one
-};
-__device__ __forceinline__ Factor factor_of(const ClipKernelArgs& a, double norm) {
-    if (!isfinite(norm)) return {1.0f, a.zero_nonfinite, !a.zero_nonfinite};
-    if (norm <= a.max_norm) return {1.0f, false, true};
-    return {(float)(a.max_norm / norm), false, false};
+        [&](const T* in, T* out) { *out = narrow<T>(f.zero ? 0.0f : widen(*in) * f.by * f.then); });
 }
 
 template <int THREADS>
 __device__ __forceinline__ void scale(const Tensor& t, int64_t worker, int64_t chunk, const Factor& f) {
     if (f.nothing && t.in == t.out) return;
     if (t.bf16)
-        scale_chunk<__nv_bfloat16, THREADS>(t, worker, chunk, f.by, f.zero);
+        scale_chunk<__nv_bfloat16, THREADS>(t, worker, chunk, f);
     else
-        scale_chunk<float, THREADS>(t, worker, chunk, f.by, f.zero);
+        scale_chunk<float, THREADS>(t, worker, chunk, f);
 }
 
 // The tensor that a worker's chunk belongs to: the last one that begins at it or before.

@@ -207,15 +207,19 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ Nor
         for (int j = 0; j < K; ++j) unpack<T>(px[j], v[j]);
         if (a.residual) {
             columns.clear_past_ends(pr);
-            T* sum = static_cast<T*>(a.sum) + row * a.sum_pitch;
 #pragma unroll
             for (int j = 0; j < K; ++j) {
                 float2 other[H];
                 unpack<T>(pr[j], other);
 #pragma unroll
                 for (int k = 0; k < H; ++k) v[j][k] = add2(v[j][k], other[k]);
-                if (a.sum && columns.in(j)) columns.store(sum, j, pack<T>(v[j]));
             }
+        }
+        if (a.sum) {
+            T* sum = static_cast<T*>(a.sum) + row * a.sum_pitch;
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+                if (columns.in(j)) columns.store(sum, j, pack<T>(v[j]));
         }
     }
     auto squares_of = [&] {

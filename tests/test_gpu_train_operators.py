@@ -113,6 +113,35 @@ def test_rms_norm_special_rows(storage, width):
         assert not torch.isnan(gx[3]).any() or eps == 0.0
 
 
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+def test_rms_norm_sum_without_a_residual(storage):
+    """The library's own call writes the sum also where nothing is added: a copy of the rows."""
+    dt = DT[storage]
+    x = torch.randn(5, 72, generator=gen(1), device=DEV).to(dt)
+    out, total = torch.empty_like(x), torch.empty_like(x)
+    s = torch.cuda.current_stream().cuda_stream
+    assert B.lib().a2cid2_rms_norm(x.data_ptr(), 72, None, 0, None, 5, 72, 1e-6, total.data_ptr(), 72, out.data_ptr(), 72, ops._DTYPES[dt], s) == B.A2_OK
+    assert torch.equal(total, x) and torch.equal(out, ops.rms_norm(x))
+
+
+def test_rms_norm_offsets_past_32_bits():
+    """Rows of more than 2^31 elements in all: the last ones against a copy of them."""
+    n, width = 67000, 32768
+    x = torch.zeros(n, width, dtype=torch.bfloat16, device=DEV)
+    x[-3:] = torch.randn(3, width, generator=gen(2), device=DEV).bfloat16()
+    w = torch.ones(width, dtype=torch.bfloat16, device=DEV)
+    y = ops.rms_norm(x, w)
+    assert torch.equal(y[-3:], ops.rms_norm(x[-3:].clone(), w)) and not y[:3].any()
+    gx, gw = ops.rms_norm_grad(x, x, w, grad_x=y)
+    small = ops.rms_norm_grad(x[-3:].clone(), x[-3:].clone(), w)
+    assert torch.equal(gx[-3:], small[0]) and torch.allclose(gw.float(), small[1].float(), rtol=2.0**-7)
+    del y, gx
+    values, scales = ops.rms_norm_quantized(x, w, block=128)
+    small = ops.rms_norm_quantized(x[-3:].clone(), w, block=128)
+    assert torch.equal(values[-3:].view(torch.uint8), small[0].view(torch.uint8)) and torch.equal(scales[-3:], small[1])
+    assert torch.equal(ops.dequantize(values, scales, out=x)[-3:], ops.dequantize(*small))
+
+
 E4M3 = [0.0] + sorted({(1 + m / 8) * 2.0**e for e in range(-6, 9) for m in range(8) if (1 + m / 8) * 2.0**e <= 448} | {m * 2.0**-9 for m in range(1, 8)})
 
 
@@ -610,6 +639,14 @@ def test_clip_of_extreme_values(storage, n):
         assert torch.isfinite(norms[[0, 2]]).all() and t[0].double().norm() < 0.101
         ops.clip_gradients([t], 0.1, per_worker=True, zero_nonfinite=True)
         assert not t[1].any() and t[2].any()
+
+
+def test_clip_by_a_factor_below_the_range_of_floats():
+    for n in (100, 300000):
+        t = torch.full((n,), 2.0**120, device=DEV)
+        out = [torch.empty_like(t)]
+        ops.clip_gradients([t], 2.0**-30, out=out)
+        assert torch.allclose(out[0].double() * math.sqrt(n), torch.full((n,), 2.0**-30, device=DEV, dtype=torch.float64), rtol=2.0**-20)
 
 
 def test_clip_offsets_past_32_bits():
