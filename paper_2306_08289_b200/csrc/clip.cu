@@ -41,9 +41,16 @@ struct Stored {
     Tensor tensor[kStored];
 };
 
+struct alignas(16) Factor {
+    float by, then;      // two factors: one alone may lie below the range of floats where the result does not
+    int32_t zero, nothing;  // nothing: by one
+};
+
 struct ClipKernelArgs {
     int64_t n_tensors, workers, worker_chunks, chunks;
-    double *sums, *wide_norms;
+    int64_t run, longer_runs;  // chunks of a CTA's run, and how many runs have one more
+    double* sums;
+    Factor* factors;  // of the workers, where the scaling is a launch of its own shape
     float* norms;
     double max_norm;
     bool zero_nonfinite, clip;
@@ -54,8 +61,12 @@ __global__ void __launch_bounds__(kStored) k_store(const __grid_constant__ Store
     if ((int)threadIdx.x < n) to[threadIdx.x] = from.tensor[threadIdx.x];
 }
 
-__device__ __forceinline__ int64_t run_start(const ClipKernelArgs& a, int64_t cta, int64_t ctas) { return cta * a.chunks / ctas; }
-__device__ __forceinline__ int64_t run_of(const ClipKernelArgs& a, int64_t chunk, int64_t ctas) { return ((chunk + 1) * ctas - 1) / a.chunks; }
+// The first runs have a chunk more than the others.
+__device__ __forceinline__ int64_t run_start(const ClipKernelArgs& a, int64_t cta) { return cta * a.run + min(cta, a.longer_runs); }
+__device__ __forceinline__ int64_t run_of(const ClipKernelArgs& a, int64_t chunk) {
+    const int64_t longer = a.longer_runs * (a.run + 1);
+    return chunk < longer ? chunk / (a.run + 1) : a.longer_runs + (chunk - longer) / a.run;
+}
 
 template <int THREADS>
 __device__ __forceinline__ double cta_sum(double v, double* shared) {
@@ -181,10 +192,6 @@ __device__ __forceinline__ double chunk_squares(const Tensor& t, int64_t worker,
     return sum;
 }
 
-struct Factor {
-    float by, then;      // two factors: one alone may lie below the range of floats where the result does not
-    bool zero, nothing;  // nothing: by one
-};
 __device__ __forceinline__ Factor factor_of(const ClipKernelArgs& a, double norm) {
     if (!isfinite(norm)) return {1.0f, 1.0f, a.zero_nonfinite, !a.zero_nonfinite};
     if (norm <= a.max_norm) return {1.0f, 1.0f, false, true};
@@ -193,8 +200,8 @@ __device__ __forceinline__ Factor factor_of(const ClipKernelArgs& a, double norm
     return {(float)factor, 1.0f, false, false};
 }
 
-template <class T, int THREADS>
-__device__ __forceinline__ void scale_chunk(const Tensor& t, int64_t worker, int64_t chunk, const Factor& f) {
+template <class T, int THREADS, class F>
+__device__ __forceinline__ void scale_chunk(const Tensor& t, int64_t worker, int64_t chunk, const F& factor) {
     constexpr int V = 16 / sizeof(T);
     over_chunk<T, THREADS>(
         t, worker, chunk,
@@ -203,6 +210,7 @@ __device__ __forceinline__ void scale_chunk(const Tensor& t, int64_t worker, int
             Words p[kCount];
 #pragma unroll
             for (int i = 0; i < kCount; ++i) p[i] = load_once(in + from(i));
+            const Factor f = factor();
 #pragma unroll
             for (int i = 0; i < kCount; ++i) {
                 float v[V];
@@ -212,19 +220,23 @@ __device__ __forceinline__ void scale_chunk(const Tensor& t, int64_t worker, int
                 store_once(out + to(i), pack<T>(v));
             }
         },
-        [&](const T* in, T* out) { *out = narrow<T>(f.zero ? 0.0f : widen(*in) * f.by * f.then); });
+        [&](const T* in, T* out) {
+            const Factor f = factor();
+            *out = narrow<T>(f.zero ? 0.0f : widen(*in) * f.by * f.then);
+        });
 }
 
-template <int THREADS>
-__device__ __forceinline__ void scale(const Tensor& t, int64_t worker, int64_t chunk, const Factor& f) {
-    if (f.nothing && t.in == t.out) return;
+// `factor()` gives the factor: it is asked for after the loads that do not need it.
+template <int THREADS, class F>
+__device__ __forceinline__ void scale(const Tensor& t, int64_t worker, int64_t chunk, const F& factor) {
     if (t.bf16)
-        scale_chunk<__nv_bfloat16, THREADS>(t, worker, chunk, f);
+        scale_chunk<__nv_bfloat16, THREADS>(t, worker, chunk, factor);
     else
-        scale_chunk<float, THREADS>(t, worker, chunk, f);
+        scale_chunk<float, THREADS>(t, worker, chunk, factor);
 }
 
-// The tensor that a worker's chunk belongs to: the last one that begins at it or before.
+// The tensor that a worker's chunk belongs to: the last one that begins at it or before. (Each lane with an entry of its own would read a kernel's
+// parameters one lane after the other.)
 __device__ __forceinline__ int tensor_of(const Tensor* table, int64_t n, int64_t chunk) {
     int low = 0, high = (int)n - 1;
     while (low < high) {
@@ -242,8 +254,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) k_squares(const __grid_consta
     __shared__ double shared[kWarps];
     ptx::chained();
     const Tensor* table = FEW ? few.tensor : stored;
-    const int64_t cta = blockIdx.x, ctas = gridDim.x, end = run_start(a, cta + 1, ctas);
-    int64_t chunk = run_start(a, cta, ctas);
+    const int64_t cta = blockIdx.x, end = run_start(a, cta + 1);
+    int64_t chunk = run_start(a, cta);
     while (chunk < end) {
         const int64_t worker = chunk / a.worker_chunks, worker_end = min(end, (worker + 1) * a.worker_chunks);
         int64_t c = chunk - worker * a.worker_chunks;
@@ -261,8 +273,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) k_squares(const __grid_consta
     }
 }
 
-__device__ __forceinline__ double norm_of(const ClipKernelArgs& a, int64_t worker, int64_t ctas, double* shared) {
-    const int64_t from = run_of(a, worker * a.worker_chunks, ctas), to = run_of(a, (worker + 1) * a.worker_chunks - 1, ctas);
+__device__ __forceinline__ double norm_of(const ClipKernelArgs& a, int64_t worker, double* shared) {
+    const int64_t from = run_of(a, worker * a.worker_chunks), to = run_of(a, (worker + 1) * a.worker_chunks - 1);
     double sum = 0.0;
     for (int64_t b = from + threadIdx.x; b <= to; b += kThreads) sum += a.sums[b + worker];
     return sqrt(cta_sum<kThreads>(sum, shared));
@@ -273,56 +285,55 @@ __global__ void __launch_bounds__(kThreads, kCtas) k_scale(const __grid_constant
     __shared__ double shared[kWarps];
     ptx::chained();
     const Tensor* table = FEW ? few.tensor : stored;
-    const int64_t cta = blockIdx.x, ctas = gridDim.x, start = run_start(a, cta, ctas);
-    int64_t chunk = run_start(a, cta + 1, ctas);
+    const int64_t cta = blockIdx.x, start = run_start(a, cta);
+    int64_t chunk = run_start(a, cta + 1);
     while (chunk > start) {
         const int64_t worker = (chunk - 1) / a.worker_chunks, worker_start = max(start, worker * a.worker_chunks);
-        const double norm = norm_of(a, worker, ctas, shared);
+        const double norm = norm_of(a, worker, shared);
         if (worker_start == worker * a.worker_chunks && threadIdx.x == 0) a.norms[worker] = (float)norm;
         const Factor f = factor_of(a, norm);
         int64_t c = chunk - 1 - worker * a.worker_chunks;
         int t = tensor_of(table, a.n_tensors, c);
         for (; chunk > worker_start; --chunk, --c) {
             while (table[t].first_chunk > c) --t;
-            scale<kThreads>(table[t], worker, c - table[t].first_chunk, f);
+            if (!f.nothing || table[t].in != table[t].out) scale<kThreads>(table[t], worker, c - table[t].first_chunk, [&] { return f; });
         }
     }
 }
 
-// Norms alone, of a CTA each; in 64 bits too where a kernel that scales follows.
-__global__ void __launch_bounds__(kThreads) k_norms(const __grid_constant__ ClipKernelArgs a, int64_t ctas) {
+// Norms alone, of a CTA each; with the factors where a kernel that scales follows.
+__global__ void __launch_bounds__(kThreads) k_norms(const __grid_constant__ ClipKernelArgs a) {
     __shared__ double shared[kWarps];
     ptx::chained();
-    const double norm = a.chunks ? norm_of(a, blockIdx.x, ctas, shared) : 0.0;
+    const double norm = a.chunks ? norm_of(a, blockIdx.x, shared) : 0.0;
     if (threadIdx.x != 0) return;
     a.norms[blockIdx.x] = (float)norm;
-    if (a.clip) a.wide_norms[blockIdx.x] = norm;
+    if (a.clip) a.factors[blockIdx.x] = factor_of(a, norm);
 }
 
 // Chunks in the order of first the last ones of all runs, then those before them: what was read last comes from L2. A chunk a CTA: while one waits for its
 // loads, others write (134 M bf16: 128 us with the norm, 133 with a few chunks each). In place, where mostly nothing has to be done, a few chunks each, which
 // are sooner over then.
-__device__ __forceinline__ void scale_in_order(const ClipKernelArgs& a, const Tensor* table, unsigned i, unsigned ctas) {
-    const int64_t run = i % ctas, chunk = run_start(a, run + 1, ctas) - 1 - i / ctas;
-    if (chunk < run_start(a, run, ctas)) return;
+__device__ __forceinline__ void scale_in_order(const ClipKernelArgs& a, const Tensor* table, unsigned run, unsigned back) {
+    const int64_t chunk = run_start(a, run + 1) - 1 - back;
+    if (chunk < run_start(a, run)) return;
     const int64_t worker = a.workers == 1 ? 0 : chunk / a.worker_chunks, c = chunk - worker * a.worker_chunks;
-    const Factor f = factor_of(a, a.wide_norms[worker]);
+    const uint4 factor = *reinterpret_cast<const uint4*>(a.factors + worker);
     const Tensor& t = table[tensor_of(table, a.n_tensors, c)];
-    scale<kThreads>(t, worker, c - t.first_chunk, f);
+    scale<kThreads>(t, worker, c - t.first_chunk, [&] { return *reinterpret_cast<const Factor*>(&factor); });
 }
 
 template <bool FEW>
-__global__ void __launch_bounds__(kThreads) k_scale_chunks(const __grid_constant__ ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored, unsigned ctas) {
+__global__ void __launch_bounds__(kThreads, 5) k_scale_chunks(const __grid_constant__ ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored) {
     ptx::chained();
-    scale_in_order(a, FEW ? few.tensor : stored, blockIdx.x, ctas);
+    scale_in_order(a, FEW ? few.tensor : stored, blockIdx.x, blockIdx.y);
 }
 
 template <bool FEW>
-__global__ void __launch_bounds__(kThreads) k_scale_in_place(const __grid_constant__ ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored, unsigned ctas) {
+__global__ void __launch_bounds__(kThreads) k_scale_in_place(const __grid_constant__ ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored) {
     ptx::chained();
-    if (a.workers == 1 && factor_of(a, a.wide_norms[0]).nothing) return;
-    const unsigned most = (unsigned)((a.chunks + ctas - 1) / ctas) * ctas;
-    for (unsigned i = blockIdx.x; i < most; i += gridDim.x) scale_in_order(a, FEW ? few.tensor : stored, i, ctas);
+    if (a.workers == 1 && a.factors[0].nothing) return;
+    for (unsigned back = blockIdx.y; back <= a.run; back += gridDim.y) scale_in_order(a, FEW ? few.tensor : stored, blockIdx.x, back);
 }
 
 // Few elements a worker: both steps in one launch, a CTA a worker.
@@ -347,7 +358,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_small(const __grid_constant__
     const Factor f = factor_of(a, norm);
     for (int64_t c = a.worker_chunks - 1, t = a.n_tensors - 1; c >= 0; --c) {
         while (table[t].first_chunk > c) --t;
-        scale<kSmallThreads>(table[t], worker, c - table[t].first_chunk, f);
+        if (!f.nothing || table[t].in != table[t].out) scale<kSmallThreads>(table[t], worker, c - table[t].first_chunk, [&] { return f; });
     }
 }
 
@@ -379,7 +390,7 @@ int64_t describe(const a2cid2_gradient_t& g, bool clip, int64_t workers, Tensor&
 int64_t clip_workspace(int64_t n_tensors, int64_t workers) {
     Carver c(nullptr);
     c.take<double>(most_ctas() + workers);
-    c.take<double>(workers);
+    c.take<Factor>(workers);
     if (n_tensors > kFew) c.take<Tensor>(n_tensors);
     return c.used;
 }
@@ -387,7 +398,7 @@ int64_t clip_workspace(int64_t n_tensors, int64_t workers) {
 cudaError_t run_clip(const ClipArgs& r, void* workspace, cudaStream_t s) {
     if (r.workers == 0) return cudaSuccess;
     Carver carver(workspace);
-    ClipKernelArgs a{0, r.workers, 0, 0, carver.take<double>(most_ctas() + r.workers), carver.take<double>(r.workers), r.norms, r.max_norm, r.zero_nonfinite, r.clip};
+    ClipKernelArgs a{0, r.workers, 0, 0, 1, 0, carver.take<double>(most_ctas() + r.workers), carver.take<Factor>(r.workers), r.norms, r.max_norm, r.zero_nonfinite, r.clip};
     Few few{};
     Stored part{};
     Tensor* table = r.n_tensors > kFew ? carver.take<Tensor>(r.n_tensors) : nullptr;
@@ -414,19 +425,20 @@ cudaError_t run_clip(const ClipArgs& r, void* workspace, cudaStream_t s) {
     if (table && held) A2_CUDA_TRY(bring());
     a.chunks = a.worker_chunks * a.workers;
     const unsigned workers = (unsigned)a.workers;
-    if (a.chunks == 0) return launch_chained(k_norms, dim3(workers), kThreads, 0, s, a, (int64_t)1);
+    if (a.chunks == 0) return launch_chained(k_norms, dim3(workers), kThreads, 0, s, a);
     if (a.worker_chunks <= kSmallChunks) return launch_chained(table ? k_small<false> : k_small<true>, dim3(workers), kSmallThreads, 0, s, a, few, table);
     const int64_t ctas = std::min(a.chunks, most_ctas());
+    a.run = a.chunks / ctas, a.longer_runs = a.chunks % ctas;
     A2_CUDA_TRY(launch_chained(table ? k_squares<false> : k_squares<true>, dim3((unsigned)ctas), kThreads, 0, s, a, few, table));
-    const bool many = a.chunks > kMany * ctas && a.chunks < (int64_t(1) << 30);
-    if (!r.clip || many) A2_CUDA_TRY(launch_chained(k_norms, dim3(workers), kThreads, 0, s, a, ctas));
+    const bool many = a.run >= kMany && a.run < 65535;
+    if (!r.clip || many) A2_CUDA_TRY(launch_chained(k_norms, dim3(workers), kThreads, 0, s, a));
     if (!r.clip) return cudaSuccess;
     if (many && in_place)
-        return launch_chained(table ? k_scale_in_place<false> : k_scale_in_place<true>, dim3((unsigned)std::min(a.chunks, 4 * ctas)), kThreads, 0, s, a, few, table,
-                              (unsigned)ctas);
+        return launch_chained(table ? k_scale_in_place<false> : k_scale_in_place<true>, dim3((unsigned)ctas, (unsigned)std::min<int64_t>(a.run + 1, 4)), kThreads, 0, s, a, few,
+                              table);
     if (many)
-        return launch_chained(table ? k_scale_chunks<false> : k_scale_chunks<true>, dim3((unsigned)(ceil_div(a.chunks, ctas) * ctas)), kThreads, 0, s, a, few, table,
-                              (unsigned)ctas);
+        return launch_chained(table ? k_scale_chunks<false> : k_scale_chunks<true>, dim3((unsigned)ctas, (unsigned)(a.run + (a.longer_runs > 0))), kThreads, 0, s, a, few,
+                              table);
     return launch_chained(table ? k_scale<false> : k_scale<true>, dim3((unsigned)ctas), kThreads, 0, s, a, few, table);
 }
 
