@@ -321,21 +321,22 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
                 doubt = !scored ? sizeof(T) == 4 && !(in - out > fabsf(in) * (2.0f * kLost + 0x1p-17f))
                                 : !(in - out > 4.0f * off + fabsf(in) * (4.0f * kLost + 0x1p-17f));
             }
+            // a lane whose group is closed never wins a round, so of its sorted list the head alone is looked at
 #pragma unroll
-            for (int j = 0; j < N; ++j) u[j] = open ? u[j] : 0u;
+            for (int j = 0; j < (kSorted ? 1 : N); ++j) u[j] = open ? u[j] : 0u;
         }
-        // lane r keeps the r-th round's key and lane; all keep those of the round after the last, for the check of what was left out
-        uint32_t head = head_of(), key = 0, key_next = 0;
-        int from = 0, from_next = 0;
-        const int rounds = checked ? a.k + 1 : a.k;
-        for (int r = 0; r < rounds; ++r) {
-            uint32_t top = lanes_max<LANES>(head);
+        // lane r keeps the r-th round's key and lane; all keep those of the best that is left, for the check of what was left out
+        uint32_t head = head_of(), key = 0, top = 0;
+        int from = 0, winner = 0;
+        auto best_of_lanes = [&] {
+            top = lanes_max<LANES>(head);
             const unsigned hits = __ballot_sync(kAll, (head ^ top) <= kPlace) >> base & kSegment;  // equal but for the places
-            const int winner = __ffs(hits) - 1;
+            winner = __ffs(hits) - 1;
             top = __shfl_sync(kAll, head, base + winner);
+        };
+        for (int r = 0; r < a.k; ++r) {
+            best_of_lanes();
             if (lane == r) key = top, from = winner;
-            key_next = top;
-            from_next = winner;
             const bool won = lane == winner;
             if constexpr (kSorted) {
 #pragma unroll
@@ -346,6 +347,9 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
             }
             head = head_of();
         }
+        if (checked) best_of_lanes();
+        const uint32_t key_next = top;
+        const int from_next = winner;
         auto expert_of = [&](uint32_t key, int from) { return first_of(from) + (int)(kPlace - (key & kPlace)); };
         int mine = lane < a.k && key > kNone ? expert_of(key, from) : -1;
         if (checked) {
