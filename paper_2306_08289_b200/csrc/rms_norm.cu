@@ -111,6 +111,13 @@ __device__ __forceinline__ float scaled_rstd(float by, float squares, int width,
 
 __device__ __forceinline__ float scale_of(float most) { return fmaxf(most * (1.0f / kE4m3Most), kScaleLeast); }
 
+// Off by a unit in the last place; a scale and its reciprocal are both in the range of floats.
+__device__ __forceinline__ float reciprocal_of_scale(float scale) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(scale));
+    return r;
+}
+
 struct NormKernelArgs {
     const void *x, *residual, *weight;
     int64_t x_pitch, residual_pitch, n;
@@ -272,7 +279,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ Nor
             if (t == 0) scales[0] = scale;
         }
         const unsigned mask = mask_of(group);
-        const int lanes = (1 << a.block_log) / V;
+        const int lanes = (1 << a.block_log) / V;  // a power of two
 #pragma unroll
         for (int j = 0; j < K; ++j) {
             const int c = columns.at(j);
@@ -284,10 +291,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ Nor
                 for (int d = 16; d > 0; d /= 2)
                     if (d < lanes) most = fmaxf(most, __shfl_xor_sync(mask, most, d));
                 scale = scale_of(most);
-                if (t % lanes == 0 && columns.in(j)) scales[c >> a.block_log] = scale;
+                if ((t & (lanes - 1)) == 0 && columns.in(j)) scales[c >> a.block_log] = scale;
             }
             if (!columns.in(j)) continue;
-            const float2 inverse = two(1.0f / scale);
+            const float2 inverse = two(reciprocal_of_scale(scale));
             Pack<uint32_t, V / 4> q;
 #pragma unroll
             for (int k = 0; k < H; k += 2) {
