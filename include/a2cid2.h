@@ -398,7 +398,8 @@ int a2cid2_prescribe(double chi1, double chi2, int32_t accelerated, double* eta,
  *     row-major; its pitch counts elements from one row to the next and is at least its width. A matrix
  *     may start anywhere inside a worker's row (element alignment suffices; matrices whose start and pitch
  *     are multiples of 16 bytes take faster accesses). Buffers of one call must not overlap
- *     unless stated otherwise.
+ *     unless stated otherwise. The norm and its gradient read rows in whole units of 16 bytes, on 16-byte boundaries, that hold an element
+ *     of the row: what else lies in a unit is read and not used.
  *   - Work is queued on cuda_stream (a cudaStream_t, NULL = default stream) and not waited for. Nothing is
  *     allocated (but 256 bytes of pinned host memory at the first product of a process): workspace is device memory of at least the size that the operator's _workspace call
  *     gives for the same sizes, 256-byte aligned, used by the queued work only. Calls whose work may

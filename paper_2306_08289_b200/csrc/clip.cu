@@ -14,6 +14,8 @@ namespace {
 // what was read last comes from L2. A worker's elements are cut into chunks of kChunkBytes, tensor after tensor; every CTA has a run of consecutive
 // chunks, over all workers, and leaves a sum for each worker it meets: CTA b and worker w at place b + w, which no other pair
 // has, since runs follow one another. Sums are joined in order.
+// 134 M elements, two thirds bf16 (340 MB), to other tensors: 164 us, 58 for the norm (5.9 TB/s) and 103 for the scaling (6.5 TB/s, a copy's rate); 134 M fp32
+// 77 and 171. In place and not clipped 80. The second reading finds 60 MB in L2 at most, which does not shorten it. 16 workers of 4.5 MB: 36 us.
 // ---------------------------------------------------------------------------------------------
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;

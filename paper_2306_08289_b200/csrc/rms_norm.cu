@@ -134,6 +134,10 @@ struct NormKernelArgs {
 // Forward. Bound by memory: x and r are read once, s and y written once, the row stays in registers as floats in between. A group holds one
 // row. MODE 0: y in the rows' type. 1: e4m3 with a scale for every 2^block_log columns, whose vectors lie in neighbouring lanes. 2: e4m3 with one
 // scale a row. Sums are in fp32; s is rounded only where it is stored, y is formed from what it was before.
+// With residual, 16,384 x 4,096 fp32: 158 us (6.8 TB/s); 16,384 x 2,048 bf16: 41 us (6.5 TB/s); 8,192 x 2,048 bf16 to 8 bits in blocks of 128: 26 us (4.5 TB/s:
+// instructions, two thirds of the issue slots; in one read and one write for every two elements there are 8 of the norm and 10 of the 8 bits).
+// Few threads a row (two to four vectors each) because what a row costs besides its vectors is paid by every warp: 2,048 columns of bf16 over 256 threads
+// 64 us, over 128 threads 45.
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t bits_of(const float* p) { return __float_as_uint(*p); }
 __device__ __forceinline__ uint32_t bits_of(const __nv_bfloat16* p) { return *reinterpret_cast<const uint16_t*>(p); }
@@ -392,7 +396,7 @@ cudaError_t norm_typed(const NormArgs& n, cudaStream_t s) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// Values from their 8 bits and scales. Bound by memory.
+// Values from their 8 bits and scales. Bound by memory: 8,192 x 2,048 to bf16 12.5 us behind the kernel that has written them (4.0 TB/s).
 // ---------------------------------------------------------------------------------------------
 constexpr int kBack = 16;  // values a thread takes at a time; blocks are multiples of it
 
@@ -459,6 +463,9 @@ cudaError_t dequantize_typed(const DequantizeArgs& a, cudaStream_t s) {
 // The reductions over a row leave the loads idle, so the rows to come are brought to shared memory meanwhile: every thread copies the vectors that
 // it will itself read, kStages rows deep, and waits for its own copies alone.
 // Long rows (LEAN) have no room for that: they keep x and g in registers and dw in shared memory, every thread its own.
+// 16,384 x 2,048 bf16 with ds: 50 us (5.4 TB/s), 16,384 x 1,024 fp32: 46 us (5.8 TB/s), of which the second kernel is 4 to 6; without the copies ahead the
+// first took 108 us. What holds bf16 back is one CTA of 16 warps a multiprocessor (124 registers: the row, its gradient, the weight and dw as floats), whose
+// issue slots are 60 % busy. 2,000 x 16,384 fp32 (LEAN): 149 us (3.5 TB/s).
 // ---------------------------------------------------------------------------------------------
 template <int K>
 constexpr int kStagesOf = K <= 2 ? 3 : 2;
