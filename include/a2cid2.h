@@ -507,9 +507,9 @@ enum { A2_GROUP_BEST = 0, A2_GROUP_TWO_BEST = 1 };
  *   ids[t][j], j < k:  the open experts of the k best keys, best first, the lowest expert first where keys are equal;
  *   weights[t][j] = scale * s of that expert, with renormalize divided by the sum of the chosen ones' s;
  *   counts[e] = tokens that have chosen e (int32 [n_experts], or NULL).
- * ids int32 and weights float, [n, k] without gaps. The choice is that of keys in 64 bits (rows that fp32 cannot decide are chosen again). An expert whose logit is
- * NaN, -inf or the lowest value of the storage type (of fp32: within 2^-17 of it), or whose bias is NaN or -inf, is not available: where fewer than k are, ids are -1 and weights 0. Logits of +inf
- * count as the largest float. n_experts <= 1024, k <= 32, groups <= 32 (A2_ERANGE beyond), k at most the experts of the open groups. n = 0 zeroes
+ * ids int32 and weights float, [n, k] without gaps. The choice is that of keys in 64 bits (rows that fp32 cannot decide are chosen again). An expert whose logit or bias is
+ * NaN, -inf or the lowest value of the storage type (of fp32: within 2^-16 of it) is not available: where fewer than k are, ids are -1 and weights 0. Logits of +inf
+ * (and biases) count as the largest float. n_experts <= 1024, k <= 32, groups <= 32 (A2_ERANGE beyond), k at most the experts of the open groups. n = 0 zeroes
  * counts. */
 int a2cid2_route(const void* logits, int64_t logits_pitch, int64_t n, int64_t n_experts, int64_t k, int32_t score, const float* bias,
                  int64_t groups, int64_t top_groups, int32_t group_score, int32_t renormalize, double scale, int32_t* ids, float* weights,

@@ -50,10 +50,11 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
     }
 }
 
-// A logit (widened) as the kernels use it: -inf (no expert) for NaN and what is at or below the type's lowest value, as masks are written.
+// A logit (widened) as the kernels use it: -inf (no expert) for NaN and what is at or below the type's lowest value, as masks are written; of fp32 that is what its
+// lowest 8 bits do not tell from it, for keys lose up to 6 of them.
 template <class T>
 __device__ __forceinline__ float lowest_of() {
-    return sizeof(T) == 2 ? -0x1.fep127f : -FLT_MAX;
+    return sizeof(T) == 2 ? -0x1.fep127f : -0x1.fffep127f;
 }
 template <class T>
 __device__ __forceinline__ float logit(float x) {
@@ -119,8 +120,8 @@ __device__ __noinline__ int choose_in_doubt(const RouteKernelArgs& a, const T* r
         }
         if (!a.sigmoid) key[j] /= total;
         if (a.bias) {
-            key[j] += (double)a.bias[first + j];
-            key[j] = key[j] > -(double)INFINITY ? fmin(key[j], DBL_MAX) : -(double)INFINITY;  // NaN: not available
+            const float bias = a.bias[first + j];
+            key[j] = bias > lowest_of<T>() ? key[j] + (double)fminf(bias, FLT_MAX) : -(double)INFINITY;
             rank[j] = key[j];
         }
         if (!a.bias && !a.two_best) key[j] = rank[j];
@@ -196,7 +197,7 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
     constexpr int kTokens = 32 / LANES, kThreadCount = ALONE ? kAloneThreads : kThreads;  // tokens of a warp
     constexpr unsigned kSegment = LANES == 32 ? kAll : (1u << (LANES % 32)) - 1u;
     constexpr uint32_t kPlace = N - 1;
-    constexpr uint32_t kNone = sizeof(T) == 4 ? 0x00800000u | kPlace : 0x0080ffffu;  // what a key is above, if its expert is available: ordered(lowest_of<T>())
+    constexpr uint32_t kNone = sizeof(T) == 4 ? 0x008000ffu : 0x0080ffffu;  // what a key is above, if its expert is available: ordered(lowest_of<T>())
     constexpr bool kSorted = N <= 16;  // longer lists: the maximum is looked for again in each round
     constexpr float kLost = N * 0x1p-23f;
     constexpr int V = 16 / sizeof(T);
@@ -210,9 +211,9 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
     const int group = lane >> a.share_log, first = first_of(lane);
     const int count = group < a.groups ? max(0, min(a.per, (group + 1) * a.group_size - first)) : 0;
     const bool scored = a.bias || a.two_best;
-    if (threadIdx.x < LANES)  // a bias of -inf or NaN switches an expert off
+    if (threadIdx.x < LANES)  // a bias may switch an expert off like a logit
 #pragma unroll
-        for (int j = 0; j < N; ++j) biases[lane * N + j] = !a.bias || j >= count ? 0.0f : a.bias[first + j] > -INFINITY ? fminf(a.bias[first + j], FLT_MAX) : -INFINITY;
+        for (int j = 0; j < N; ++j) biases[lane * N + j] = !a.bias || j >= count ? 0.0f : a.bias[first + j] > lowest_of<T>() ? fminf(a.bias[first + j], FLT_MAX) : -INFINITY;
     __syncthreads();
     const float off = a.sigmoid ? 0x1p-21f : (N + 24) * 0x1p-24f;  // of a score: approximate exponential and reciprocal, sums of N + 5 terms
     const bool exact = !a.bias;                                   // experts are ranked by their logits

@@ -740,6 +740,39 @@ def test_on_a_given_stream():
     del y, total, values, scales, back, ids, weights, counts, dz, gx, gw, norms, again, got
 
 
+def test_two_calls_at_once():
+    """The same operators on two streams at a time, each with inputs of its own."""
+    inputs = [step_inputs(seed) for seed in (11, 12)]
+    want = [step(*v) for v in inputs]
+    streams = [torch.cuda.Stream() for _ in inputs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[k].append(step(*inputs[k]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for result in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(result, want[k]))
+
+
+def test_route_biases_that_switch_experts_off():
+    """-inf, NaN and the lowest value, in choices that fp32 makes and in those that 64 bits have to make (all logits alike)."""
+    for dt in (torch.float32, torch.bfloat16):
+        z = torch.randn(200, 64, generator=gen(4), device=DEV).to(dt)
+        z[100:] = 0.0
+        bias = 1e-12 * torch.randn(64, generator=gen(5), device=DEV)
+        off = [3, 17, 40]
+        bias[off[0]], bias[off[1]], bias[off[2]] = -math.inf, math.nan, torch.finfo(torch.float32).min
+        for score in ("softmax", "sigmoid"):
+            for groups in (1, 8):
+                ids, _, counts = ops.route(z, 8, score=score, bias=bias, groups=groups, top_groups=max(groups // 2, 1), group_score="top2")
+                assert not counts[off].any() and (ids >= 0).all() and int(counts.sum()) == 1600
+                best = bias.nan_to_num(-1.0).clamp(min=-1.0).sort(descending=True, stable=True).indices[:8].to(torch.int32)
+                assert groups > 1 or (ids[100:] == best).all()
+
+
 def test_refusals_of_the_wrappers():
     x = torch.randn(10, 64, device=DEV)
     w = torch.ones(64, device=DEV)
