@@ -21,7 +21,7 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kChunkBytes = 16384;   // four loads of 16 bytes in flight for each of 256 threads
 constexpr int kCtas = 6;             // a multiprocessor
-constexpr int64_t kMany = 2;           // chunks of a run from which on the scaling is a launch of its own shape, after one that joins the norms
+constexpr int64_t kMany = 2;         // chunks of a run from which on the scaling is a launch of its own shape, after one that joins the norms
 constexpr int kKept = 5;             // chunks at the end of a run that should stay in the L2 cache: 73 MB of its 126
 constexpr int kFew = 48;             // tensors that are described in a kernel's parameters; more in the workspace
 constexpr int kStored = 240;         // tensors that a launch brings there
@@ -322,6 +322,7 @@ __device__ __forceinline__ void scale_in_order(const ClipKernelArgs& a, const Te
     const int64_t worker = a.workers == 1 ? 0 : chunk / a.worker_chunks, c = chunk - worker * a.worker_chunks;
     const uint4 factor = *reinterpret_cast<const uint4*>(a.factors + worker);
     const Tensor& t = table[tensor_of(table, a.n_tensors, c)];
+    if (t.in == t.out && reinterpret_cast<const Factor*>(&factor)->nothing) return;
     scale<kThreads>(t, worker, c - t.first_chunk, [&] { return *reinterpret_cast<const Factor*>(&factor); });
 }
 

@@ -641,6 +641,25 @@ def test_clip_of_extreme_values(storage, n):
         assert not t[1].any() and t[2].any()
 
 
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [100, 200000, 12000000])
+def test_what_need_not_be_clipped_keeps_its_bits_in_place(storage, n):
+    """Workers within the norm, and such with elements that are not finite, beside one that is clipped: in every form of the scaling."""
+    dt, bits = (torch.float32, torch.int32) if storage == "f32" else (torch.bfloat16, torch.int16)
+    t = torch.randn(3, n, generator=gen(n), device=DEV).to(dt)
+    t[0] *= 1e-3 / math.sqrt(n)
+    t[1, 7:9] = math.inf
+    t.view(bits)[1, 11] = 0x7f812345 if storage == "f32" else 0x7f91  # a NaN of its own
+    keep = t.clone()
+    ops.clip_gradients([t], 0.5, per_worker=True)
+    assert torch.equal(t[:2].view(bits), keep[:2].view(bits))
+    assert abs(float(t[2].double().norm()) - 0.5) < 1e-2
+    other = keep.clone()
+    apart = torch.empty(3, n + 5, dtype=dt, device=DEV)[:, 5:]
+    ops.clip_gradients([other, other.clone()], 0.5, per_worker=True, out=[other, apart])  # one in place, one not
+    assert torch.equal(other[:2].view(bits), keep[:2].view(bits)) and torch.equal(apart[0], keep[0])
+
+
 def test_clip_by_a_factor_below_the_range_of_floats():
     for n in (100, 300000):
         t = torch.full((n,), 2.0**120, device=DEV)
