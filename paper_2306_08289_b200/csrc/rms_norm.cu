@@ -100,10 +100,7 @@ __device__ __forceinline__ float power_below(float most) {  // 2^-e for most in 
     frexpf(most, &e);
     return ldexpf(1.0f, max(-126, min(126, 1 - e)));
 }
-__device__ __forceinline__ float rstd_of(float mean) {  // 1 / sqrt, by one step of Newton's from the approximate one
-    const float r = rsqrtf(mean);
-    return r * fmaf(-0.5f * mean * r, r, 1.5f);
-}
+__device__ __forceinline__ float rstd_of(float mean) { return __frsqrt_rn(mean); }  // 1 / sqrt, rounded once
 __device__ __forceinline__ float scaled_rstd(float by, float squares, int width, float eps) {
     const double mean = (double)squares / (double)width + (double)eps * by * by;
     return mean > 0.0 ? (float)(1.0 / sqrt(mean)) : isnan(mean) ? (float)mean : 0.0f;  // a row of zeros with eps = 0 gives zeros
