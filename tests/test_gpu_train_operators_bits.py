@@ -1,0 +1,53 @@
+"""Norm, routing and clipping where single bits, neighbouring rows or ties decide: beside the bounds of test_gpu_train_operators.py."""
+import math
+
+import pytest
+import torch
+
+from paper_2306_08289_b200 import operators as ops
+from tests.test_gpu_operators import DEV, DT, assert_within, gen
+
+pytestmark = pytest.mark.gpu
+
+
+def quotients(y, block):
+    """(values, scales) of a result in fp32, by the definition: scale = max(largest magnitude / 448, 2^-126), values = result / scale to the nearest of 8 bits, ties to even. Both
+    quotients are of two tensors, which torch divides by the IEEE rule (a number it would multiply by its reciprocal)."""
+    n, width = y.shape
+    b = block or width
+    blocks = -(-width // b)
+    most = torch.nn.functional.pad(y, (0, blocks * b - width)).view(n, blocks, b).abs().amax(2)
+    scales = (most / torch.full_like(most, 448.0)).clamp(min=2.0**-126)
+    return (y / scales.repeat_interleave(b, 1)[:, :width]).to(torch.float8_e4m3fn), scales
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("block", [0, 32, 64, 128])
+@pytest.mark.parametrize("n,width", [(4096, 2048), (3000, 200), (1, 8192)])
+def test_values_in_8_bits_are_the_nearest_of_the_quotients(storage, block, n, width):
+    """Bit for bit. Rows are whole numbers up to 15, whose squares' sums fp32 holds exactly in any order, so that the result before the 8 bits is that of `rms_norm` on the
+    same rows in fp32; a weight of 24 bits (8 of bf16) spreads the quotients over all fractions. 2^23 of them have some 50 within an approximate reciprocal's error of the middle
+    of two values."""
+    g, dt = gen(width + block), DT[storage]
+    x = torch.randint(-15, 16, (n, width), generator=g, device=DEV).to(dt)
+    x[0, : width // 2] = 0
+    w = torch.randn(width, generator=g, device=DEV).to(dt)
+    w[3] *= 2.0**-12  # results below the 8 bits' normal range
+    values, scales = ops.rms_norm_quantized(x, w, block=block)
+    y = ops.rms_norm(x.float(), w.float())
+    want, want_scales = quotients(y, block)
+    assert torch.equal(scales, want_scales)
+    assert torch.equal(values.view(torch.uint8), want.view(torch.uint8))
+
+
+def test_values_in_8_bits_of_extreme_results():
+    """Results from the end of fp32's range to its other end, in one block and over several, beside the largest and the smallest scale."""
+    g = gen(3)
+    x = torch.randint(-15, 16, (64, 256), generator=g, device=DEV).float()
+    for low, high in ((-140, -100), (-20, 20), (90, 123)):
+        w = torch.randn(256, generator=g, device=DEV) * torch.exp2(torch.randint(low, high + 1, (256,), generator=g, device=DEV).float())
+        for block in (0, 32, 128):
+            values, scales = ops.rms_norm_quantized(x, w, block=block)
+            want, want_scales = quotients(ops.rms_norm(x, w), block)
+            assert torch.equal(scales, want_scales)
+            assert torch.equal(values.view(torch.uint8), want.view(torch.uint8)), (low, block)
