@@ -28,8 +28,8 @@ bool aligned16(const void* p, int64_t pitch, int64_t elem) {
 constexpr int kRows = 4;
 
 template <class T, int VEC>
-__global__ void __launch_bounds__(kThreads) k_embed(const T* __restrict__ table, int64_t vocab, int64_t width, int64_t table_pitch,
-                                                    const int32_t* __restrict__ ids, int64_t n_ids, float scale,
+__global__ void __launch_bounds__(kThreads) k_embed(const T* table, int64_t vocab, int64_t width, int64_t table_pitch,
+                                                    const int32_t* ids, int64_t n_ids, float scale,
                                                     T* __restrict__ out, int64_t out_pitch, int group) {
     ptx::chained();
     const int lane = threadIdx.x % group;
@@ -161,7 +161,7 @@ __device__ __forceinline__ void zero_rows(const ZeroFill& z, int64_t cta, int64_
 }
 
 // Counts of the first digit, per tile of kTile positions.
-__global__ void __launch_bounds__(kSortThreads) k_sort_count(const int32_t* __restrict__ ids, int64_t n, int64_t vocab, int passes, int n_tiles, int* __restrict__ counts,
+__global__ void __launch_bounds__(kSortThreads) k_sort_count(const int32_t* ids, int64_t n, int64_t vocab, int passes, int n_tiles, int* __restrict__ counts,
                                                              const ZeroFill zero) {
     ptx::chained();
     if ((int)blockIdx.x >= n_tiles) return zero_rows(zero, blockIdx.x - n_tiles, gridDim.x - n_tiles);
@@ -177,8 +177,8 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(const int32_t* __re
 
 // One pass: every tile adds up where its items go from the counts of all tiles, moves them, and counts the next
 // digit of the tiles they land in (integer sums: the order of the atomics does not show).
-__global__ void __launch_bounds__(kSortThreads) k_sort_pass(const int32_t* __restrict__ ids, const Pair* __restrict__ in, int64_t n, int64_t vocab,
-                                                            int pass, bool last, const int* __restrict__ counts, int n_tiles,
+__global__ void __launch_bounds__(kSortThreads) k_sort_pass(const int32_t* ids, const Pair* in, int64_t n, int64_t vocab,
+                                                            int pass, bool last, const int* counts, int n_tiles,
                                                             Pair* __restrict__ out, int* __restrict__ next_counts, const ZeroFill zero) {
     ptx::chained();
     if ((int)blockIdx.x >= n_tiles) return zero_rows(zero, blockIdx.x - n_tiles, gridDim.x - n_tiles);
@@ -238,7 +238,7 @@ constexpr unsigned kZeroCtas = 148 * 2;
 constexpr int64_t kZeroBytes = 16 << 20;
 
 template <class T, int VEC>
-__global__ void __launch_bounds__(kThreads) k_segments(const T* __restrict__ grad_out, int64_t grad_pitch, const Pair* __restrict__ sorted, int64_t n,
+__global__ void __launch_bounds__(kThreads) k_segments(const T* grad_out, int64_t grad_pitch, const Pair* sorted, int64_t n,
                                                        int64_t vocab, int64_t width, float scale, bool accumulate, T* __restrict__ table,
                                                        int64_t table_pitch, float* __restrict__ partial, int span, int group, int64_t sum_ctas, int64_t zero_first) {
     ptx::chained();
@@ -314,9 +314,9 @@ __global__ void __launch_bounds__(kThreads) k_segments(const T* __restrict__ gra
 // The ids that lie in more than one block: the group of the block where such an id begins adds up its parts in
 // block order.
 template <class T, int VEC>
-__global__ void __launch_bounds__(kThreads) k_join(const Pair* __restrict__ sorted, int64_t n, int64_t vocab, int64_t width, float scale,
+__global__ void __launch_bounds__(kThreads) k_join(const Pair* sorted, int64_t n, int64_t vocab, int64_t width, float scale,
                                                    bool accumulate, T* __restrict__ table, int64_t table_pitch,
-                                                   const float* __restrict__ partial, int span, int group) {
+                                                   const float* partial, int span, int group) {
     ptx::chained();
     const int64_t block = (int64_t)blockIdx.x * (kThreads / group) + threadIdx.x / group;
     const int64_t c = ((int64_t)blockIdx.y * group + threadIdx.x % group) * VEC;
@@ -360,7 +360,7 @@ constexpr int kDirectWarps = kDirectThreads / 32;
 constexpr int kFound = 128 + 32;  // positions a warp holds before it adds their rows up: one round of 128 ids, and a remainder
 
 template <class T, int VEC>
-__global__ void __launch_bounds__(kDirectThreads, 4) k_direct(const T* __restrict__ grad_out, int64_t grad_pitch, const int32_t* __restrict__ ids, int n,
+__global__ void __launch_bounds__(kDirectThreads, 4) k_direct(const T* grad_out, int64_t grad_pitch, const int32_t* ids, int n,
                                                            int64_t vocab, int64_t width, float scale, bool accumulate, T* __restrict__ table,
                                                            int64_t table_pitch, int64_t sum_ctas) {
     ptx::chained();

@@ -241,7 +241,9 @@ template <class... P, class... A>
 
 namespace ptx {
 // Kernels of one operator are launched so that one may start while its predecessor ends: it sets itself up, lets its own
-// successor do the same, and waits until everything before it is done and visible.
+// successor do the same, and waits until everything before it is done and visible. Such a kernel's inputs are no `const T* __restrict__`: that lets the
+// compiler read them through the read-only cache and before the wait, which is right only for what nobody writes while the kernel lives, and its life begins before the
+// predecessor's writes end. (Results may be __restrict__.)
 __device__ __forceinline__ void release_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void chained() {

@@ -89,7 +89,7 @@ __device__ __forceinline__ Pack<T, VEC> read_columns(const T* row, int64_t j, in
 }
 
 template <class T, int VEC>
-__global__ void __launch_bounds__(kNormThreads) k_norm(const T* __restrict__ in, int64_t stride, int64_t pitch, int64_t rows, int64_t cols,
+__global__ void __launch_bounds__(kNormThreads) k_norm(const T* in, int64_t stride, int64_t pitch, int64_t rows, int64_t cols,
                                                        double* __restrict__ partial) {
     ptx::chained();
     __shared__ double part[kNormThreads / 32];
@@ -128,8 +128,8 @@ __device__ __forceinline__ MatScale mat_scale(double squares, double eps) {
 
 // Words of G 2^e, [rows, ld].
 template <class T, int VEC>
-__global__ void __launch_bounds__(kNormThreads) k_first_words(const T* __restrict__ in, int64_t stride, int64_t pitch, int64_t rows, int64_t cols,
-                                                              const double* __restrict__ partial, int parts, double eps, __half* __restrict__ hi, __half* __restrict__ lo, int64_t ld,
+__global__ void __launch_bounds__(kNormThreads) k_first_words(const T* in, int64_t stride, int64_t pitch, int64_t rows, int64_t cols,
+                                                              const double* partial, int parts, double eps, __half* __restrict__ hi, __half* __restrict__ lo, int64_t ld,
                                                               MatScale* __restrict__ scales) {
     ptx::chained();
     __shared__ MatScale shared;
@@ -251,8 +251,8 @@ struct SymmetricEpi {
 };
 
 // Adds up the parts of A = X X^T, in order, on and below the diagonal tiles. Two columns a thread.
-__global__ void __launch_bounds__(256) k_join_gram(const float* __restrict__ parts, int n_parts, int64_t part_stride, Words to, int64_t m,
-                                                   const MatScale* __restrict__ scales, Poly poly) {
+__global__ void __launch_bounds__(256) k_join_gram(const float* parts, int n_parts, int64_t part_stride, Words to, int64_t m,
+                                                   const MatScale* scales, Poly poly) {
     ptx::chained();
     const int64_t row = blockIdx.y, mat = blockIdx.z, col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 2;
     if (col >= m || col / kTileN > row / kTileM) return;
@@ -477,7 +477,7 @@ __device__ __forceinline__ void narrow_product(uint32_t d, const uint32_t (&a)[2
 }
 
 template <class T>
-__global__ void __launch_bounds__(kNarrowThreads, 1) k_narrow(const T* __restrict__ in, T* out, const NarrowArgs g) {
+__global__ void __launch_bounds__(kNarrowThreads, 1) k_narrow(const T* in, T* out, const NarrowArgs g) {
     extern __shared__ char raw[];
     __shared__ double part[kNarrowThreads / 32];
     __shared__ double squares;

@@ -429,7 +429,7 @@ cudaError_t norm_typed(const NormArgs& n, cudaStream_t s) {
 constexpr int kBack = 16;  // values a thread takes at a time; blocks are multiples of it
 
 template <class T>
-__global__ void __launch_bounds__(256) k_dequantize(const uint8_t* __restrict__ values, int64_t values_pitch, const float* __restrict__ scales, int64_t n,
+__global__ void __launch_bounds__(256) k_dequantize(const uint8_t* values, int64_t values_pitch, const float* scales, int64_t n,
                                                     int width, int block_log, int blocks, T* __restrict__ out, int64_t out_pitch, int group) {
     ptx::chained();
     const int64_t row = (int64_t)blockIdx.x * (256 / group) + threadIdx.x / group;
@@ -462,15 +462,22 @@ __global__ void __launch_bounds__(256) k_dequantize(const uint8_t* __restrict__ 
 
 // Rows anywhere: neighbouring threads take neighbouring values.
 template <class T>
-__global__ void __launch_bounds__(256) k_dequantize_single(const uint8_t* __restrict__ values, int64_t values_pitch, const float* __restrict__ scales, int64_t n,
+__global__ void __launch_bounds__(256) k_dequantize_single(const uint8_t* values, int64_t values_pitch, const float* scales, int64_t n,
                                                            int width, int block_log, int blocks, T* __restrict__ out, int64_t out_pitch, int group) {
     ptx::chained();
     const int64_t row = (int64_t)blockIdx.x * (256 / group) + threadIdx.x / group;
     if (row >= n) return;
-#pragma unroll 8
-    for (int c = (int)threadIdx.x % group; c < width; c += group) {
-        const float f = __half2float(__half(__nv_cvt_fp8_to_halfraw(values[row * values_pitch + c], __NV_E4M3)));
-        out[row * out_pitch + c] = narrow<T>(f * scales[row * blocks + (blocks > 1 ? c >> block_log : 0)]);
+    constexpr int kAtOnce = 8;
+    for (int c = (int)threadIdx.x % group; c < width; c += kAtOnce * group) {
+        float f[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {  // all loads before the first store
+            const int at = c + k * group;
+            if (at < width) f[k] = __half2float(__half(__nv_cvt_fp8_to_halfraw(values[row * values_pitch + at], __NV_E4M3))) * scales[row * blocks + (blocks > 1 ? at >> block_log : 0)];
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+            if (c + k * group < width) out[row * out_pitch + c + k * group] = narrow<T>(f[k]);
     }
 }
 
@@ -749,7 +756,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_consta
 
 // dw from the CTAs' parts: 32 columns a CTA, every warp a share of the parts, joined in order.
 template <class T>
-__global__ void __launch_bounds__(1024) k_norm_join(const float* __restrict__ parts, int64_t count, int64_t width, T* __restrict__ dw) {
+__global__ void __launch_bounds__(1024) k_norm_join(const float* parts, int64_t count, int64_t width, T* __restrict__ dw) {
     __shared__ float sums[32][33];
     ptx::chained();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;

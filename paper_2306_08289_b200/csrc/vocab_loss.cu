@@ -433,7 +433,7 @@ struct GradientEpi {
 
 // Adds up the parts of K of a gradient, in order.
 template <class T>
-__global__ void __launch_bounds__(256) k_join_parts(const float* __restrict__ kept, int parts, int64_t kept_ld, int64_t some, int64_t rows, int64_t cols, T* __restrict__ out,
+__global__ void __launch_bounds__(256) k_join_parts(const float* kept, int parts, int64_t kept_ld, int64_t some, int64_t rows, int64_t cols, T* __restrict__ out,
                                                     int64_t pitch, GradientScale scale) {
     ptx::chained();
     const GradientFactor<T> factor(scale);

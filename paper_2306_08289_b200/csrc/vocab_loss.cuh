@@ -26,8 +26,8 @@ __device__ __forceinline__ bool is_token(int32_t y, int64_t vocab) { return y >=
 
 // Joins the statistics of the parts: 32 tokens a CTA, its warps over the parts.
 constexpr int kFinishWarps = 16;
-__global__ void __launch_bounds__(kFinishWarps * 32) k_finish(const float2* __restrict__ partial, int parts, const float* __restrict__ at_target,
-                                                const int32_t* __restrict__ targets, const int32_t* __restrict__ poisoned, int64_t n, int64_t vocab,
+__global__ void __launch_bounds__(kFinishWarps * 32) k_finish(const float2* partial, int parts, const float* at_target,
+                                                const int32_t* targets, const int32_t* poisoned, int64_t n, int64_t vocab,
                                                 float* __restrict__ loss, float* __restrict__ lse) {
     ptx::chained();
     __shared__ float2 joined[kFinishWarps][32];
@@ -81,8 +81,8 @@ __device__ __forceinline__ float block_reduce(float v, bool sum, float* shared) 
 }
 
 template <class Sink>
-__global__ void __launch_bounds__(kRowThreads) k_rows(const VocabLossArgs a, const float2* __restrict__ partial, int parts, const float* __restrict__ at_target,
-                                                      const int32_t* __restrict__ poisoned, bool probabilities, const float* z, int64_t z_ld, Sink sink) {
+__global__ void __launch_bounds__(kRowThreads) k_rows(const VocabLossArgs a, const float2* partial, int parts, const float* at_target,
+                                                      const int32_t* poisoned, bool probabilities, const float* z, int64_t z_ld, Sink sink) {
     ptx::chained();
     __shared__ float shared[kRowThreads / 32];
     const int64_t t = blockIdx.x;

@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kFewThreads) k_few_gradients(const FewGradArgs
 }
 
 template <class T>
-__global__ void __launch_bounds__(256) k_few_join(const float* __restrict__ sums, int parts, int64_t n, int64_t width, T* __restrict__ out, int64_t pitch) {
+__global__ void __launch_bounds__(256) k_few_join(const float* sums, int parts, int64_t n, int64_t width, T* __restrict__ out, int64_t pitch) {
     ptx::chained();
     for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < n * width; e += (int64_t)gridDim.x * 256) {
         float sum = 0.0f;
