@@ -47,9 +47,12 @@ __device__ __forceinline__ unsigned mask_of(int group) {  // of the lanes of thi
 
 // Sums (or maxima of magnitudes) of COUNT values over a group, the same bits in every thread. `slot` changes from one such reduction to the
 // next (0, 1, 0, ...), so that one barrier each is enough: that of the CTA, or with SEVERAL groups of more than a warp in it (at most 15) that of the
-// group's warps. A kernel that does not know its barriers' numbers reserves all of a CTA's, which only few CTAs a multiprocessor can have.
+// group's warps. Those groups do not wait for one another: a warp has two places of its own in a slot, whatever COUNT is, so that one group's maximum never lies where
+// another's sums do. A kernel that does not know its barriers' numbers reserves all of a CTA's, which only few CTAs a multiprocessor can have.
+constexpr int kPlaces = 2;  // of a warp, in a slot
 template <bool MAX, bool SEVERAL, int COUNT>
-__device__ __forceinline__ void over_group(float (&v)[COUNT], int group, int mine, int slot, float (*shared)[32 * 2]) {
+__device__ __forceinline__ void over_group(float (&v)[COUNT], int group, int mine, int slot, float (*shared)[32 * kPlaces]) {
+    static_assert(COUNT <= kPlaces, "places of a warp");
     const unsigned mask = mask_of(group);
     auto join = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
 #pragma unroll
@@ -61,14 +64,14 @@ __device__ __forceinline__ void over_group(float (&v)[COUNT], int group, int min
     const int warps = group / 32, lane = threadIdx.x % 32;
     if (lane == 0)
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) shared[slot][threadIdx.x / 32 * COUNT + i] = v[i];
+        for (int i = 0; i < COUNT; ++i) shared[slot][threadIdx.x / 32 * kPlaces + i] = v[i];
     if constexpr (SEVERAL)
         asm volatile("bar.sync %0, %1;" ::"r"(mine + 1), "r"(group) : "memory");
     else
         __syncthreads();
     const int first = SEVERAL ? mine * warps : 0;
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) v[i] = lane < warps ? shared[slot][(first + lane) * COUNT + i] : 0.0f;  // zero is neutral for both
+    for (int i = 0; i < COUNT; ++i) v[i] = lane < warps ? shared[slot][(first + lane) * kPlaces + i] : 0.0f;  // zero is neutral for both
 #pragma unroll
     for (int d = 16; d > 0; d /= 2)
         if (d < warps)
@@ -79,7 +82,7 @@ __device__ __forceinline__ void over_group(float (&v)[COUNT], int group, int min
     for (int i = 0; i < COUNT; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
 }
 template <bool MAX, bool SEVERAL>
-__device__ __forceinline__ float over_group(float v, int group, int mine, int slot, float (*shared)[32 * 2]) {
+__device__ __forceinline__ float over_group(float v, int group, int mine, int slot, float (*shared)[32 * kPlaces]) {
     float one[1] = {v};
     over_group<MAX, SEVERAL, 1>(one, group, mine, slot, shared);
     return one[0];
@@ -233,7 +236,7 @@ struct Columns {
 template <class T, Lie LIE, int K, int MODE, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1) k_norm(const __grid_constant__ NormKernelArgs a) {
     constexpr int V = kVec<T>, H = V / 2;
-    __shared__ float shared[2][32 * 2];
+    __shared__ float shared[2][32 * kPlaces];
     ptx::chained();
     const int group = a.group, width = a.width;
     const int mine = group > 32 ? 0 : threadIdx.x >> (31 - __clz(group)), t = group > 32 ? threadIdx.x : threadIdx.x & (group - 1);
@@ -543,7 +546,7 @@ template <class T, Lie LIE, int K, bool LEAN, int THREADS, int CTAS>
 __global__ void __launch_bounds__(THREADS, CTAS) k_norm_grad(const __grid_constant__ NormGradKernelArgs a) {
     constexpr int V = kVec<T>, H = V / 2, kStages = kStagesOf<K>;
     constexpr bool WIDE = LIE != kAnywhere;
-    __shared__ float shared[2][32 * 2];
+    __shared__ float shared[2][32 * kPlaces];
     extern __shared__ uint4 memory[];  // LEAN: every thread's part of dw. Else rows to come, and at the end, with several groups a CTA, a row of dw for each
     ptx::chained();
     const int group = a.group, width = a.width, groups = blockDim.x / group;

@@ -51,3 +51,43 @@ def test_values_in_8_bits_of_extreme_results():
             want, want_scales = quotients(ops.rms_norm(x, w), block)
             assert torch.equal(scales, want_scales)
             assert torch.equal(values.view(torch.uint8), want.view(torch.uint8)), (low, block)
+
+
+# groups of 2, 4 and 3 warps, 8 warps alone in bf16 and fp32: (type, rows, columns)
+@pytest.mark.parametrize("storage,n,width", [("bf16", 16384, 2048), ("f32", 16384, 1024), ("bf16", 9001, 520), ("f32", 9001, 260), ("bf16", 6000, 1030), ("f32", 6000, 2047), ("bf16", 6000, 4096)])
+@pytest.mark.parametrize("special", ["nan", "inf", "zeros", "large", "small"])
+def test_rows_out_of_range_leave_the_gradient_of_the_others_alone(storage, n, width, special):
+    """Every seventh row needs the scaled way; all other rows have the bits that they have without such rows, in every one of many calls, and so has the weight's gradient from call to
+    call."""
+    g, dt = gen(n + width), DT[storage]
+    x, go = (torch.randn(n, width, generator=g, device=DEV).to(dt) for _ in range(2))
+    w = (1.0 + 0.3 * torch.randn(width, generator=g, device=DEV)).to(dt)
+    want, _ = ops.rms_norm_grad(go, x, w, eps=0.0)
+    odd = x.clone()
+    rows = odd[3::7]
+    if special == "nan":
+        rows[:, width // 2] = math.nan
+    elif special == "inf":
+        rows[:, width - 1] = math.inf
+    elif special == "zeros":
+        rows.zero_()
+    else:
+        rows.mul_(2.0**80 if special == "large" else 2.0**-80)
+    others = torch.arange(n, device=DEV) % 7 != 3
+    first = None
+    for _ in range(50):
+        gx, gw = ops.rms_norm_grad(go, odd, w, eps=0.0)
+        assert torch.equal(gx[others], want[others])
+        first = (gx, gw) if first is None else first
+        assert torch.equal(gw.view(torch.int8), first[1].view(torch.int8)) and torch.equal(gx.view(torch.int8), first[0].view(torch.int8))
+    if special in ("nan", "inf"):
+        assert torch.isnan(gx[3::7]).any(1).all()
+    elif special == "zeros":
+        assert not gx[3::7].any()
+    if special in ("zeros", "large", "small"):
+        # of the columns: a zero row adds nothing, a scaled one what it adds unscaled. At most 16384 / 148 additions in a slot's column, 2048 in the join, and a term's 2^-17
+        keep = others if special == "zeros" else torch.ones_like(others)
+        terms = go.double() * x.double() / torch.sqrt((x.double() ** 2).mean(1, keepdim=True))
+        terms[~keep] = 0.0
+        u = 2.0**-8 if storage == "bf16" else 2.0**-24
+        assert_within(gw, terms.sum(0), ((n / 148 + 2048) * 2.0**-24 + 2.0**-17) * terms.abs().sum(0) + u * terms.sum(0).abs())
