@@ -273,6 +273,7 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
             for (int j = 0; j < N; ++j) place(j, fmaxf(z[j], -INFINITY));  // NaN is -inf
         }
         if constexpr (kSorted) sort<N>(u);
+        bool open = true;  // this lane's group
         auto head_of = [&] {
             uint32_t h = u[0];
             if constexpr (!kSorted) {
@@ -312,7 +313,7 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
             const float score = a.two_best && a.group_size > 1 ? best + second : best;
             // the best groups one after the other; a group's number in the lowest bits, so that no two are equal and the lowest is first
             uint32_t mine = group < a.groups ? (ordered(score) & ~31u) | (31 - group) : 0u, last = 0;
-            bool open = false;
+            open = false;
             for (int r = 0; r < a.top_groups; ++r) {
                 last = lanes_max<LANES>(mine);
                 if (mine == last) open = true, mine = 0;
@@ -356,16 +357,29 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
         auto expert_of = [&](uint32_t key, int from) { return first_of(from) + (int)(kPlace - (key & kPlace)); };
         int mine = lane < a.k && key > kNone ? expert_of(key, from) : -1;
         if (checked) {
+            // whether the better of two keys, less the lost bits, may not be so; what is equal in every respect has not been made so by rounding
+            auto close = [&](uint32_t better, uint32_t worse) {
+                const float low = number(worse);
+                return exact ? better == worse : !(number(better) - low > 2.0f * off + fabsf(low) * (2.0f * kLost + 0x1p-22f));
+            };
+            auto same = [&](int x, int y) { return logit<T>(widen(row[x])) == logit<T>(widen(row[y])) && (!a.bias || a.bias[x] == a.bias[y]); };
             const uint32_t after = __shfl_down_sync(kAll, key, 1), behind = lane + 1 < a.k ? after : key_next;
             const int after_from = __shfl_down_sync(kAll, from, 1);
-            if (mine >= 0 && behind > kNone) {
-                const uint32_t k0 = key & ~kPlace, k1 = behind & ~kPlace;
-                const float low = number(k1);
-                if (exact ? k0 == k1 : !(number(k0) - low > 2.0f * off + fabsf(low) * (2.0f * kLost + 0x1p-22f))) {
-                    // close; what is equal in every respect has not been made so by rounding
-                    const int other = expert_of(behind, lane + 1 < a.k ? after_from : from_next);
-                    if (!(logit<T>(widen(row[mine])) == logit<T>(widen(row[other])) && (!a.bias || a.bias[mine] == a.bias[other]))) doubt = true;
-                }
+            bool tied = false;  // the last one that is chosen, with the first that is not
+            if (mine >= 0 && behind > kNone && close(key & ~kPlace, behind & ~kPlace)) {
+                const bool equal = same(mine, expert_of(behind, lane + 1 < a.k ? after_from : from_next));
+                doubt = doubt || !equal;
+                tied = equal && lane + 1 == a.k;
+            }
+            // such a tie says nothing about the others that are not chosen: those in it may hide a better one
+            if (__any_sync(kAll, tied)) {
+                const int last = base + a.k - 1;
+                const uint32_t chosen_key = __shfl_sync(kAll, key, last) & ~kPlace;
+                const int chosen = __shfl_sync(kAll, mine, last);
+                if (__shfl_sync(kAll, (int)tied, last) && open)
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        if (u[j] > kNone && close(chosen_key, u[j] & ~kPlace) && !same(chosen, first + (int)(kPlace - (u[j] & kPlace)))) doubt = true;
             }
         }
         const unsigned doubts = __ballot_sync(kAll, doubt);

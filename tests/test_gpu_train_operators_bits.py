@@ -6,6 +6,7 @@ import torch
 
 from paper_2306_08289_b200 import operators as ops
 from tests.test_gpu_operators import DEV, DT, assert_within, gen
+from tests.test_gpu_train_operators import route_of
 
 pytestmark = pytest.mark.gpu
 
@@ -91,3 +92,50 @@ def test_rows_out_of_range_leave_the_gradient_of_the_others_alone(storage, n, wi
         terms[~keep] = 0.0
         u = 2.0**-8 if storage == "bf16" else 2.0**-24
         assert_within(gw, terms.sum(0), ((n / 148 + 2048) * 2.0**-24 + 2.0**-17) * terms.abs().sum(0) + u * terms.sum(0).abs())
+
+
+# ------------------------------------------------------------------------------------------------
+# routing
+# ------------------------------------------------------------------------------------------------
+def tied_tokens(n, experts, k, dt, score, with_bias, g):
+    """(logits, bias): k - 1 or k - 2 experts of every token are sure to be chosen; for the places that are left there are some with the same logit and bias, and one or two with a
+    slightly larger key that fp32 scores (without a bias: the keys' upper bits) cannot tell from theirs."""
+    z = torch.full((n, experts), -45.0, device=DEV)
+    bias = torch.zeros(experts, device=DEV) if with_bias else None
+    base, more = 30.0, 31.0  # of a sigmoid: 1 - 9e-14 and 1 - 3e-14
+    if not with_bias:
+        base, more = 1.5, 1.5 + 2.0**-23
+    elif score == "softmax":  # beside an expert that has almost all of the sum, and is out by its bias: 1 + 2e-9 and 1 + 3e-9, or less
+        base, more = 10.0, 10.5
+    for t in range(n):
+        order = torch.randperm(experts - 1, generator=g, device=DEV) + 1
+        sure = max(0, k - 1 - t % 2)
+        equal, larger = 2 + t % 5, 1 + t // 5 % 2
+        at = order[: sure + equal + larger].cpu()
+        tied = at[sure:].sort().values if t % 3 else at[sure:]  # the larger ones behind the others, or anywhere
+        z[t, at[:sure]] = 2.0 if not with_bias else 40.0 + torch.arange(sure, device=DEV) if score == "sigmoid" else 20.0 + 0.5 * torch.arange(sure, device=DEV)
+        z[t, tied[:equal]] = base
+        z[t, tied[equal:]] = more
+    if with_bias and score == "softmax":
+        z[:, 0] = 30.0
+        bias += 1.0
+        bias[0] = -4.0
+    return z.to(dt), bias
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("experts,k", [(16, 1), (16, 3), (32, 2), (64, 1), (64, 8), (128, 4), (256, 1), (256, 8), (500, 2), (1024, 8), (1024, 31)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("groups,top_groups", [(1, 1), (4, 4), (4, 3)])
+def test_route_where_the_last_choice_is_tied_with_one_and_beaten_by_another(storage, experts, k, score, with_bias, groups, top_groups):
+    """The tie says nothing about the third expert, which has the larger key."""
+    n = 60
+    z, bias = tied_tokens(n, experts, k, DT[storage], score, with_bias, gen(experts + k))
+    k = min(k, experts // groups * top_groups)
+    args = dict(score=score, bias=bias, groups=groups, top_groups=top_groups, group_score="max", renormalize=True, scale=1.0)
+    ids = ops.route(z, k, **args)[0].cpu().numpy()
+    want = route_of(z, k, **args)[0]
+    assert (ids == want).all(), (ids[(ids != want).any(1)][:3], want[(ids != want).any(1)][:3])
+    many = ops.route(z.repeat(50, 1), k, **args)[0].view(50, n, k)
+    assert (many == many[0]).all() and (many[0].cpu().numpy() == want).all()
