@@ -270,7 +270,10 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < N; ++j) place(j, fmaxf(z[j], -INFINITY));  // NaN is -inf
+            for (int j = 0; j < N; ++j) {
+                const float known = fmaxf(z[j], -INFINITY);                     // NaN is -inf
+                place(j, sizeof(T) == 4 ? fminf(known, FLT_MAX) : known);  // +inf the largest float, which bf16 does not have beside it
+            }
         }
         if constexpr (kSorted) sort<N>(u);
         bool open = true;  // this lane's group

@@ -139,3 +139,27 @@ def test_route_where_the_last_choice_is_tied_with_one_and_beaten_by_another(stor
     assert (ids == want).all(), (ids[(ids != want).any(1)][:3], want[(ids != want).any(1)][:3])
     many = ops.route(z.repeat(50, 1), k, **args)[0].view(50, n, k)
     assert (many == many[0]).all() and (many[0].cpu().numpy() == want).all()
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalize", [False, True])
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("groups,top_groups", [(1, 1), (4, 2)])
+def test_route_of_infinite_logits_beside_the_largest_float(score, renormalize, with_bias, groups, top_groups):
+    """A logit of +inf counts as the largest float, so the lower expert comes first, whatever is asked for beside the choice."""
+    big = torch.finfo(torch.float32).max
+    for experts in (8, 64, 256, 1024):
+        z = torch.randn(40, experts, generator=gen(experts), device=DEV)
+        low, high = experts // 4, experts // 2 - 1  # of one group of two
+        low, high = (low, high) if groups == 1 else (experts // 4, experts // 4 + 1)
+        z[:, low] = big
+        z[:, high] = math.inf
+        z[20:, low], z[20:, high] = math.inf, big
+        z[30:, experts - 1] = math.inf
+        bias = torch.zeros(experts, device=DEV) if with_bias else None
+        args = dict(score=score, bias=bias, groups=groups, top_groups=top_groups, group_score="max", renormalize=renormalize, scale=1.0)
+        ids, weights, _ = ops.route(z, 2, **args)
+        want = torch.tensor([low, high], dtype=torch.int32, device=DEV)
+        assert (ids == want).all(), (ids[0], ids[-1])
+        share = 0.5 if renormalize or score == "softmax" else 1.0
+        assert (weights[:30] == share).all() and torch.isfinite(weights).all()
