@@ -69,6 +69,12 @@ __device__ __forceinline__ float near_exp(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * 1.4426950408889634f));
     return y;
 }
+// Of the dense gradient: rows of fp32 take the accurate one, whose error does not grow with the distance from the largest logit (30,011 x 161: 14.3 us, 12.8 with the
+// other); rows of bf16 keep 8 bits of it, and the approximate one is right to 2^-17 wherever it is above 2^-126 (13.5 us, 15.1 with the accurate one).
+template <class T>
+__device__ __forceinline__ float row_exp(float x) {
+    return sizeof(T) == 4 ? expf(x) : near_exp(x);
+}
 __device__ __forceinline__ float near_reciprocal(float x) {
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -550,11 +556,11 @@ __global__ void __launch_bounds__(kThreads) k_route_grad(const __grid_constant__
             float total = 0.0f;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                d[j] = near_exp(d[j] - most);
+                d[j] = row_exp<T>(d[j] - most);
                 total += d[j];
             }
             total = lanes_sum<LANES>(total);
-            const float one = total > 0.0f ? 1.0f / total : 0.0f, s = chosen ? near_exp(x - most) : 0.0f;
+            const float one = total > 0.0f ? 1.0f / total : 0.0f, s = chosen ? row_exp<T>(x - most) : 0.0f;
             h = g * s * one;
             const float all = lanes_sum<LANES>(h) * -one;
 #pragma unroll

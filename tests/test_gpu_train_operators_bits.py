@@ -163,3 +163,20 @@ def test_route_of_infinite_logits_beside_the_largest_float(score, renormalize, w
         assert (ids == want).all(), (ids[0], ids[-1])
         share = 0.5 if renormalize or score == "softmax" else 1.0
         assert (weights[:30] == share).all() and torch.isfinite(weights).all()
+
+
+@pytest.mark.parametrize("experts", [8, 64, 65, 128, 256, 500, 1024])
+def test_dense_gradient_of_experts_far_below_the_best(experts):
+    """Softmax, not renormalised, one expert chosen that has the whole sum: the others' gradients are -s_e g s. Differences of logits are whole multiples of 2^-8, so no error comes from
+    them; the exponential is off by a unit in the last place (2^-23), and there are at most six roundings beside it: 2^-21 in all, however small s_e."""
+    g = gen(experts)
+    z = -50.0 - torch.randint(0, 37 * 256 + 1, (300, experts), generator=g, device=DEV) / 256.0  # down to e^-87, above the smallest normal float
+    best = torch.randint(0, experts, (300, 1), generator=g, device=DEV)
+    z.scatter_(1, best, 0.0)
+    gw = torch.randn(300, 1, generator=g, device=DEV) * 100.0
+    got = ops.route_grad(z, best.to(torch.int32), gw, score="softmax", renormalize=False)
+    s = torch.softmax(z.double(), 1)
+    chosen = torch.zeros_like(s).scatter_(1, best, 1.0)
+    # the chosen expert's own is g s (1 - s), a difference of nearly equal numbers
+    want = s * (chosen - s.gather(1, best)) * gw.double()
+    assert_within(got, want, 2.0**-21 * (want.abs() + chosen * gw.double().abs()))
