@@ -17,11 +17,14 @@ from __future__ import annotations
 import array
 import contextlib
 import ctypes as C
+import importlib
 import operator
+import warnings
 
 import torch
 
 from . import binding as B
+from . import build
 
 NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)  # a quintic whose iterates send every singular value into about [0.7, 1.2]
 
@@ -65,16 +68,27 @@ def _vector(name, t, n, dtype, device):
 _calls = None
 
 
+class _NoCalls:
+    """In the place of the module below where that cannot be loaded: every call is left to the code in Python."""
+
+    def __getattr__(self, name):
+        return lambda *arguments: None
+
+
 def _usual():
     """The module that takes the usual calls (csrc/torch_calls.cpp): its functions return None for what they leave to the code below them."""
     global _calls
     if _calls is None:
         B.lib()  # says so if nothing has been built
         try:
-            from . import _calls as module
+            if build.calls_version() != torch.__version__:
+                raise ImportError(f"it was built for torch {build.calls_version()}, this is {torch.__version__}")
+            module = importlib.import_module(__package__ + "._calls")
+            module.set_error(B.A2Error)
         except ImportError as e:
-            raise ImportError(f"the host side of the operators' calls cannot be loaded ({e}): build it with `python -m paper_2306_08289_b200.build`") from e
-        module.set_error(B.A2Error)
+            warnings.warn(f"the host side of the operators' usual calls cannot be loaded ({e}), so small calls take some 5 to 25 us longer: "
+                          "build it with `python -m paper_2306_08289_b200.build`", RuntimeWarning, stacklevel=3)
+            module = _NoCalls()
         _calls = module
     return _calls
 
