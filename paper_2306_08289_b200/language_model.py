@@ -105,6 +105,11 @@ class Model:
         return a, (logits, ids, weights, each, picked)
 
     def forward(self, row, ids):
+        """(y, a, h); of a model with norms or experts (y, u, a, what the gradient needs of the hidden layer, s or None, h)."""
+        y, u, a, kept, s, h = self._layers(row, ids)
+        return (y, u, a, kept, s, h) if self.norm or self.experts else (y, a, h)
+
+    def _layers(self, row, ids):
         from . import operators as ops
 
         y = ops.embed(self.part(row, "E"), ids, scale=math.sqrt(self.width))
@@ -119,7 +124,7 @@ class Model:
         """Mean loss over the tokens that have a target; quantized: with the last hidden states held in 8 bits."""
         from . import operators as ops
 
-        *_, s, h = self.forward(row, ids)
+        *_, s, h = self._layers(row, ids)
         if quantized:
             h = ops.dequantize(*ops.rms_norm_quantized(s, self.part(row, "F")[0], block=32 if self.width > 32 else 0), h.dtype)
         loss, _ = ops.vocab_loss(h, self.part(row, "W"), targets)
@@ -131,7 +136,7 @@ class Model:
 
         from . import operators as ops
 
-        y, u, a, kept, s, h = self.forward(row, ids)
+        y, u, a, kept, s, h = self._layers(row, ids)
         _, _, dh, _ = ops.vocab_loss_grad(h, self.part(row, "W"), targets, scale=scale, grad_head=self.part(out, "W"))
         if self.norm:  # dh of the sum from here on
             dh, _ = ops.rms_norm_grad(dh, s, self.part(row, "F")[0], grad_weight=self.part(out, "F")[0])

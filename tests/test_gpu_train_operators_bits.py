@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+from paper_2306_08289_b200 import language_model as LM
 from paper_2306_08289_b200 import operators as ops
 from tests.test_gpu_operators import DEV, DT, assert_within, gen
 from tests.test_gpu_train_operators import route_of
@@ -180,3 +181,18 @@ def test_dense_gradient_of_experts_far_below_the_best(experts):
     # the chosen expert's own is g s (1 - s), a difference of nearly equal numbers
     want = s * (chosen - s.gather(1, best)) * gw.double()
     assert_within(got, want, 2.0**-21 * (want.abs() + chosen * gw.double().abs()))
+
+
+# ------------------------------------------------------------------------------------------------
+# the example
+# ------------------------------------------------------------------------------------------------
+def test_forward_of_a_model_without_norms_and_experts_gives_three_tensors():
+    model = LM.Model(40, 24)
+    row = torch.from_numpy(model.initial_row(5)).to(DEV)
+    ids = torch.arange(30, dtype=torch.int32, device=DEV)
+    y, a, h = model.forward(row, ids)
+    assert y.shape == a.shape == h.shape == (30, 24) and torch.equal(h, y + a)
+    assert torch.equal(a, torch.tanh(y @ model.part(row, "M").T))
+    for more in (dict(norm=True), dict(experts=4), dict(norm=True, experts=4)):
+        model = LM.Model(40, 24, **more)
+        assert len(model.forward(torch.from_numpy(model.initial_row(5)).to(DEV), ids)) == 6
