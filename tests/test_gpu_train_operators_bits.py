@@ -1,13 +1,15 @@
 """Norm, routing and clipping where single bits, neighbouring rows or ties decide: beside the bounds of test_gpu_train_operators.py."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
+from paper_2306_08289_b200 import binding as B
 from paper_2306_08289_b200 import language_model as LM
 from paper_2306_08289_b200 import operators as ops
 from tests.test_gpu_operators import DEV, DT, assert_within, gen
-from tests.test_gpu_train_operators import route_of
+from tests.test_gpu_train_operators import TINY, grad_of, reference_loss, route_of
 
 pytestmark = pytest.mark.gpu
 
@@ -93,6 +95,36 @@ def test_rows_out_of_range_leave_the_gradient_of_the_others_alone(storage, n, wi
         terms[~keep] = 0.0
         u = 2.0**-8 if storage == "bf16" else 2.0**-24
         assert_within(gw, terms.sum(0), ((n / 148 + 2048) * 2.0**-24 + 2.0**-17) * terms.abs().sum(0) + u * terms.sum(0).abs())
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+@pytest.mark.parametrize("width", [48, 1000, 2048, 9000])
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+@pytest.mark.parametrize("with_sum", [False, True])
+def test_gradients_of_zero_rows_and_of_rows_out_of_range(storage, width, eps, with_sum):
+    """A row of zeros without eps has zeros for its own part and adds none to the weight's gradient, one with eps has r w g; rows beyond fp32's squares as the formula says."""
+    g, dt = gen(width), DT[storage]
+    u = 2.0**-8 if storage == "bf16" else 2.0**-24
+    x = torch.randn(40, width, generator=g, device=DEV, dtype=torch.float64)
+    x[1::8] *= 2.0**90
+    x[2::8] *= 2.0**-90
+    x[3::8] = 0.0
+    x[5::8] = 0.0
+    x[5::8, width - 1] = 2.0**100
+    x = x.to(dt)
+    go, ds = (torch.randn(40, width, generator=g, device=DEV).to(dt) for _ in range(2))
+    w = (1.0 + 0.3 * torch.randn(width, generator=g, device=DEV)).to(dt)
+    gx, gw = ops.rms_norm_grad(go, x, w, eps=eps, grad_sum=ds if with_sum else None)
+    zero = ~x.any(1)
+    assert int(zero.sum()) == 5
+    if eps == 0.0:
+        assert torch.equal(gx[zero], ds[zero] if with_sum else torch.zeros_like(gx[zero]))
+    d, size = grad_of(go.double(), x.double(), w, eps, ds.double() if with_sum else None)
+    rows = ~zero if eps == 0.0 else torch.ones_like(zero)
+    assert_within(gx[rows], d[rows], 2.0**-16 * size[rows] + u * d[rows].abs() + TINY[storage])  # as in test_rms_norm_grad
+    hat = x.double() / torch.sqrt((x.double() ** 2).mean(1, keepdim=True) + eps)
+    terms = (go.double() * hat).nan_to_num(0.0)
+    assert_within(gw, terms.sum(0), (40 * 2.0**-24 + 2.0**-17) * terms.abs().sum(0) + u * terms.sum(0).abs() + TINY[storage])
 
 
 # ------------------------------------------------------------------------------------------------
@@ -196,3 +228,100 @@ def test_forward_of_a_model_without_norms_and_experts_gives_three_tensors():
     for more in (dict(norm=True), dict(experts=4), dict(norm=True, experts=4)):
         model = LM.Model(40, 24, **more)
         assert len(model.forward(torch.from_numpy(model.initial_row(5)).to(DEV), ids)) == 6
+
+
+@pytest.mark.parametrize("norm,experts", [(False, 0), (True, 0), (False, 5), (True, 8)])
+def test_gradients_of_the_example_in_bf16(norm, experts):
+    """Against autograd in 64 bits at the same row. Some 16 tensors on the way are rounded to bf16 (2^-8 each), and 1 - a^2 of an ordinary tanh doubles what a was off by: 2^-3 of a part. The
+    router's part is a difference of the chosen experts' gradients, whose errors are relative to their magnitudes."""
+    text = LM.MarkovText(40, 4, 1)
+    model = LM.Model(40, 24, norm=norm, experts=experts)
+    row = torch.from_numpy(model.initial_row(5)).to(DEV)
+    row = (row + 0.05 * torch.randn(model.d, generator=gen(1), device=DEV)).bfloat16()
+    ids, targets = (torch.from_numpy(v).to(DEV) for v in text.draw(np.random.default_rng(2), 6, 11))
+    out = torch.full((model.d,), math.nan, device=DEV, dtype=torch.bfloat16)
+    model.gradient(row, ids, targets, 0.1, out)
+    chosen = model.forward(row, ids)[3][1].long() if experts else None
+    wide = row.double().requires_grad_()
+    reference_loss(model, wide, ids, targets, 0.1, chosen).backward()
+    for name in model.shape:
+        got, want = model.part(out, name).double(), model.part(wide.grad, name)
+        bound = 2.0**-3 * float(want.norm())
+        if name == "R":
+            _, u, _, (_, _, weights, _, picked), _, _ = model.forward(row, ids)
+            _, _, dh, _ = ops.vocab_loss_grad(model.forward(row, ids)[5], model.part(row, "W"), targets, scale=0.1)
+            if norm:
+                dh, _ = ops.rms_norm_grad(dh, model.forward(row, ids)[4], model.part(row, "F")[0])
+            each = weights.double() * (picked.double() * dh.double()[:, None]).abs().sum(2)
+            size = torch.zeros(len(ids), experts, dtype=torch.float64, device=DEV).scatter_add_(1, chosen, each)
+            bound = 2.0**-3 * float((size.T @ u.double().abs()).norm())
+        assert torch.isfinite(got).all() and float((got - want).norm()) <= bound, name
+
+
+# ------------------------------------------------------------------------------------------------
+# the two ways to the library
+# ------------------------------------------------------------------------------------------------
+def calls_of_every_kind(storage):
+    g, dt = gen(7), DT[storage]
+    x, r, go = (torch.randn(70, 200, generator=g, device=DEV).to(dt) for _ in range(3))
+    w = torch.randn(200, generator=g, device=DEV).to(dt)
+    z, bias = torch.randn(70, 64, generator=g, device=DEV).to(dt), torch.randn(64, generator=g, device=DEV) * 0.1
+    inside = torch.randn(70, 211, generator=g, device=DEV).to(dt)[:, 3:203]
+    values, scales = ops.rms_norm_quantized(x, w, block=64)
+    ids, weights, _ = ops.route(z, 4)
+    workers = torch.randn(6, 5000, generator=g, device=DEV).to(dt)
+    parts = [workers[:, :3000].view(6, 50, 60), workers[:, 3000:3007], workers[:, 4000:]]
+    return {
+        "norm": lambda: ops.rms_norm(x, w), "norm, residual": lambda: ops.rms_norm(x, None, residual=r, eps=1e-3), "norm inside rows": lambda: ops.rms_norm(inside, w, residual=x),
+        "norm of no rows": lambda: ops.rms_norm(x[:0], w, residual=x[:0]), "norm of one row": lambda: ops.rms_norm(x[3:4], w), "eps whole": lambda: ops.rms_norm(x, w, eps=1),
+        "8 bits": lambda: ops.rms_norm_quantized(x, w, block=64), "8 bits a row, residual": lambda: ops.rms_norm_quantized(inside, w, residual=r, block=0),
+        "back": lambda: ops.dequantize(values, scales), "back to fp32": lambda: ops.dequantize(values, scales, torch.float32), "back, inside": lambda: ops.dequantize(values[:, :192], scales[:, :3].contiguous()),
+        "gradient": lambda: ops.rms_norm_grad(go, x, w), "gradient, sum": lambda: ops.rms_norm_grad(go, inside, w, grad_sum=r), "gradient of rows": lambda: ops.rms_norm_grad(go, x, w, grad_weight=None),
+        "gradient of the weight": lambda: ops.rms_norm_grad(go, x, w, grad_x=None), "gradient without a weight": lambda: ops.rms_norm_grad(go, x), "gradient of no rows": lambda: ops.rms_norm_grad(go[:0], x[:0], w),
+        "route": lambda: ops.route(z, 4), "route, groups": lambda: ops.route(z, 6, "sigmoid", bias, 8, 3, "top2", False, 2.5), "route of one": lambda: ops.route(z[5:6], 1, renormalize=False),
+        "route of none": lambda: ops.route(z[:0], 3), "route gradient": lambda: ops.route_grad(z, ids, weights), "route gradient, sigmoid": lambda: ops.route_grad(z, ids, weights, "sigmoid", False, 2),
+        "norms": lambda: ops.gradient_norms([x, w, z]), "norms of workers": lambda: ops.gradient_norms(parts, per_worker=True), "norms of a tuple": lambda: ops.gradient_norms((x, r)),
+        "clipped": lambda: [t := [x.clone(), w.clone()], ops.clip_gradients(t, 1.0)], "clipped workers": lambda: [t := workers.clone(), ops.clip_gradients([t[:, 9:3009], t[:, 3100:]], 2.0, per_worker=True, zero_nonfinite=True)],
+        "clipped elsewhere": lambda: [o := [torch.empty_like(x), torch.empty_like(w)], ops.clip_gradients([x, w], 0.5, out=o)], "not clipped": lambda: [t := [x.clone()], ops.clip_gradients(t, math.inf)],
+    }
+
+
+def refused_of_every_kind(storage):
+    dt = DT[storage]
+    x, w = torch.randn(10, 64, device=DEV).to(dt), torch.ones(64, device=DEV).to(dt)
+    wide = torch.zeros(2, 32769, device=DEV).to(dt)
+    ids, weights, _ = ops.route(x, 2)
+    return [lambda: ops.rms_norm(x, eps=-1.0), lambda: ops.rms_norm(x, w[:5]), lambda: ops.rms_norm(wide), lambda: ops.rms_norm(x.T), lambda: ops.rms_norm_quantized(x, block=3), lambda: ops.rms_norm_grad(x, x[:4]),
+            lambda: ops.rms_norm_grad(x, x, eps=math.inf), lambda: ops.route(x, 0), lambda: ops.route(x, 65), lambda: ops.route(x, 40), lambda: ops.route(x, 2, groups=7), lambda: ops.route(x, 2, scale=math.inf),
+            lambda: ops.route_grad(x, ids.long(), weights), lambda: ops.route_grad(x, ids, weights, scale=math.nan), lambda: ops.clip_gradients([x, x], 1.0), lambda: ops.clip_gradients([x], -1.0),
+            lambda: ops.gradient_norms([x.half()]), lambda: ops.gradient_norms([x, w], per_worker=True), lambda: ops.gradient_norms([x[:1].expand(10, 64)])]
+
+
+def flat(v):
+    return [t for x in v for t in flat(x)] if isinstance(v, (list, tuple)) else [v]
+
+
+@pytest.mark.parametrize("storage", ["f32", "bf16"])
+def test_both_ways_to_the_library_give_the_same(storage, monkeypatch):
+    """The calls that go to it from C++ and the ones that go from Python: results bit for bit, refusals by their codes."""
+    usual = ops._usual()
+    assert not isinstance(usual, ops._NoCalls)
+    calls, refused = calls_of_every_kind(storage), refused_of_every_kind(storage)
+
+    def code(call):
+        with pytest.raises(B.A2Error) as e:
+            call()
+        return e.value.code
+
+    first, codes = {name: flat(call()) for name, call in calls.items()}, [code(call) for call in refused]
+    monkeypatch.setattr(ops, "_calls", ops._NoCalls())
+    for name, call in calls.items():
+        again = flat(call())
+        assert len(again) == len(first[name])
+        for a, b in zip(first[name], again):
+            if a is None or b is None:
+                assert a is b, name
+                continue
+            assert a.shape == b.shape and a.dtype == b.dtype and a.device == b.device and a.stride() == b.stride(), name
+            assert torch.equal(a.contiguous().view(torch.uint8) if a.dim() else a, b.contiguous().view(torch.uint8) if b.dim() else b), name
+    assert codes == [code(call) for call in refused]
