@@ -10,19 +10,19 @@ namespace a2 {
 namespace {
 
 // ---------------------------------------------------------------------------------------------
-// Bound by memory: read once for the norm, read again and written once for the clipping, the second reading against the direction of the first so that
-// what was read last comes from L2. A worker's elements are cut into chunks of kChunkBytes, tensor after tensor; every CTA has a run of consecutive
-// chunks, over all workers, and leaves a sum for each worker it meets: CTA b and worker w at place b + w, which no other pair
+// Bound by memory: read once for the norm, read again and written once for the clipping. A worker's elements are cut into chunks of kChunkBytes, tensor after tensor;
+// every CTA has a run of consecutive chunks, over all workers, and leaves a sum for each worker it meets: CTA b and worker w at place b + w, which no other pair
 // has, since runs follow one another. Sums are joined in order.
-// 134 M elements, two thirds bf16 (340 MB), to other tensors: 164 us, 58 for the norm (5.9 TB/s) and 103 for the scaling (6.5 TB/s, a copy's rate); 134 M fp32
-// 77 and 171. In place and not clipped 80. The second reading finds 60 MB in L2 at most, which does not shorten it. 16 workers of 4.5 MB: 36 us.
+// 134 M elements, two thirds bf16 (340 MB), to other tensors: 165 us, 58 for the norm (5.9 TB/s) and 103 for the scaling (6.5 TB/s, a copy's rate); 135 M fp32
+// 81 and 170. In place and not clipped 87. 16 workers of 4.5 MB: 35 us. The first reading leaves what it reads in the L2 cache where a second one follows (10 M fp32 clipped
+// 17.8 us, 20.3 without), and not where the norms are all (135 M fp32: 80.6 us, 82.6 with it). The second reading goes in the order of the first: against it, with
+// what was read last kept in the cache by hints, took the same (60 M fp32 113.3 us both ways) or more (16 workers of 34 MB 264 us, 258 in order).
 // ---------------------------------------------------------------------------------------------
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kChunkBytes = 16384;   // four loads of 16 bytes in flight for each of 256 threads
 constexpr int kCtas = 6;             // a multiprocessor
 constexpr int64_t kMany = 2;         // chunks of a run from which on the scaling is a launch of its own shape, after one that joins the norms
-constexpr int kKept = 5;             // chunks at the end of a run that should stay in the L2 cache: 73 MB of its 126
 constexpr int kFew = 48;             // tensors that are described in a kernel's parameters; more in the workspace
 constexpr int kStored = 240;         // tensors that a launch brings there
 constexpr int64_t kSmallChunks = 4;  // chunks of a worker that one CTA takes alone
@@ -266,9 +266,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) k_squares(const __grid_consta
         for (; chunk < worker_end; ++chunk, ++c) {
             while (t + 1 < a.n_tensors && table[t + 1].first_chunk <= c) ++t;
             const Tensor& tensor = table[t];
-            const bool keep = end - chunk <= kKept;
-            sum += tensor.bf16 ? chunk_squares<__nv_bfloat16, kThreads>(tensor, worker, c - tensor.first_chunk, keep)
-                               : chunk_squares<float, kThreads>(tensor, worker, c - tensor.first_chunk, keep);
+            sum += tensor.bf16 ? chunk_squares<__nv_bfloat16, kThreads>(tensor, worker, c - tensor.first_chunk, a.clip)
+                               : chunk_squares<float, kThreads>(tensor, worker, c - tensor.first_chunk, a.clip);
         }
         sum = cta_sum<kThreads>(sum, shared);
         if (threadIdx.x == 0) a.sums[cta + worker] = sum;
@@ -287,17 +286,17 @@ __global__ void __launch_bounds__(kThreads, kCtas) k_scale(const __grid_constant
     __shared__ double shared[kWarps];
     ptx::chained();
     const Tensor* table = FEW ? few.tensor : stored;
-    const int64_t cta = blockIdx.x, start = run_start(a, cta);
-    int64_t chunk = run_start(a, cta + 1);
-    while (chunk > start) {
-        const int64_t worker = (chunk - 1) / a.worker_chunks, worker_start = max(start, worker * a.worker_chunks);
+    const int64_t cta = blockIdx.x, end = run_start(a, cta + 1);
+    int64_t chunk = run_start(a, cta);
+    while (chunk < end) {
+        const int64_t worker = chunk / a.worker_chunks, worker_end = min(end, (worker + 1) * a.worker_chunks);
         const double norm = norm_of(a, worker, shared);
-        if (worker_start == worker * a.worker_chunks && threadIdx.x == 0) a.norms[worker] = (float)norm;
+        if (chunk == worker * a.worker_chunks && threadIdx.x == 0) a.norms[worker] = (float)norm;
         const Factor f = factor_of(a, norm);
-        int64_t c = chunk - 1 - worker * a.worker_chunks;
+        int64_t c = chunk - worker * a.worker_chunks;
         int t = tensor_of(table, a.n_tensors, c);
-        for (; chunk > worker_start; --chunk, --c) {
-            while (table[t].first_chunk > c) --t;
+        for (; chunk < worker_end; ++chunk, ++c) {
+            while (t + 1 < a.n_tensors && table[t + 1].first_chunk <= c) ++t;
             if (!f.nothing || table[t].in != table[t].out) scale<kThreads>(table[t], worker, c - table[t].first_chunk, [&] { return f; });
         }
     }
@@ -313,12 +312,9 @@ __global__ void __launch_bounds__(kThreads) k_norms(const __grid_constant__ Clip
     if (a.clip) a.factors[blockIdx.x] = factor_of(a, norm);
 }
 
-// Chunks in the order of first the last ones of all runs, then those before them: what was read last comes from L2. A chunk a CTA: while one waits for its
-// loads, others write (134 M bf16: 128 us with the norm, 133 with a few chunks each). In place, where mostly nothing has to be done, a few chunks each, which
-// are sooner over then.
-__device__ __forceinline__ void scale_in_order(const ClipKernelArgs& a, const Tensor* table, unsigned run, unsigned back) {
-    const int64_t chunk = run_start(a, run + 1) - 1 - back;
-    if (chunk < run_start(a, run)) return;
+// A chunk a CTA: while one waits for its loads, others write (134 M bf16: 128 us with the norm, 133 with a few chunks each). In place, where mostly nothing has to be done, a
+// few chunks each, which are sooner over then.
+__device__ __forceinline__ void scale_one(const ClipKernelArgs& a, const Tensor* table, int64_t chunk) {
     const int64_t worker = a.workers == 1 ? 0 : chunk / a.worker_chunks, c = chunk - worker * a.worker_chunks;
     const uint4 factor = *reinterpret_cast<const uint4*>(a.factors + worker);
     const Tensor& t = table[tensor_of(table, a.n_tensors, c)];
@@ -329,14 +325,14 @@ __device__ __forceinline__ void scale_in_order(const ClipKernelArgs& a, const Te
 template <bool FEW>
 __global__ void __launch_bounds__(kThreads, 5) k_scale_chunks(const __grid_constant__ ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored) {
     ptx::chained();
-    scale_in_order(a, FEW ? few.tensor : stored, blockIdx.x, blockIdx.y);
+    scale_one(a, FEW ? few.tensor : stored, blockIdx.x);
 }
 
 template <bool FEW>
 __global__ void __launch_bounds__(kThreads) k_scale_in_place(const __grid_constant__ ClipKernelArgs a, const __grid_constant__ Few few, const Tensor* stored) {
     ptx::chained();
     if (a.workers == 1 && a.factors[0].nothing) return;
-    for (unsigned back = blockIdx.y; back <= a.run; back += gridDim.y) scale_in_order(a, FEW ? few.tensor : stored, blockIdx.x, back);
+    for (int64_t chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) scale_one(a, FEW ? few.tensor : stored, chunk);
 }
 
 // Few elements a worker: both steps in one launch, a CTA a worker.
@@ -359,8 +355,8 @@ __global__ void __launch_bounds__(kSmallThreads) k_small(const __grid_constant__
     if (threadIdx.x == 0) a.norms[worker] = (float)norm;
     if (!a.clip) return;
     const Factor f = factor_of(a, norm);
-    for (int64_t c = a.worker_chunks - 1, t = a.n_tensors - 1; c >= 0; --c) {
-        while (table[t].first_chunk > c) --t;
+    for (int64_t c = 0, t = 0; c < a.worker_chunks; ++c) {
+        while (t + 1 < a.n_tensors && table[t + 1].first_chunk <= c) ++t;
         if (!f.nothing || table[t].in != table[t].out) scale<kSmallThreads>(table[t], worker, c - table[t].first_chunk, [&] { return f; });
     }
 }
@@ -433,15 +429,12 @@ cudaError_t run_clip(const ClipArgs& r, void* workspace, cudaStream_t s) {
     const int64_t ctas = std::min(a.chunks, most_ctas());
     a.run = a.chunks / ctas, a.longer_runs = a.chunks % ctas;
     A2_CUDA_TRY(launch_chained(table ? k_squares<false> : k_squares<true>, dim3((unsigned)ctas), kThreads, 0, s, a, few, table));
-    const bool many = a.run >= kMany && a.run < 65535;
+    const bool many = a.run >= kMany && a.chunks < (int64_t(1) << 31);  // CTAs of a launch
     if (!r.clip || many) A2_CUDA_TRY(launch_chained(k_norms, dim3(workers), kThreads, 0, s, a));
     if (!r.clip) return cudaSuccess;
     if (many && in_place)
-        return launch_chained(table ? k_scale_in_place<false> : k_scale_in_place<true>, dim3((unsigned)ctas, (unsigned)std::min<int64_t>(a.run + 1, 4)), kThreads, 0, s, a, few,
-                              table);
-    if (many)
-        return launch_chained(table ? k_scale_chunks<false> : k_scale_chunks<true>, dim3((unsigned)ctas, (unsigned)(a.run + (a.longer_runs > 0))), kThreads, 0, s, a, few,
-                              table);
+        return launch_chained(table ? k_scale_in_place<false> : k_scale_in_place<true>, dim3((unsigned)std::min(a.chunks, 4 * ctas)), kThreads, 0, s, a, few, table);
+    if (many) return launch_chained(table ? k_scale_chunks<false> : k_scale_chunks<true>, dim3((unsigned)a.chunks), kThreads, 0, s, a, few, table);
     return launch_chained(table ? k_scale<false> : k_scale<true>, dim3((unsigned)ctas), kThreads, 0, s, a, few, table);
 }
 
