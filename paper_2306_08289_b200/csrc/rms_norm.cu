@@ -172,8 +172,8 @@ struct NormKernelArgs {
 // Forward. Bound by memory: x and r are read once, s and y written once, the row stays in registers as floats in between. A group holds one
 // row. MODE 0: y in the rows' type. 1: e4m3 with a scale for every 2^block_log columns, whose vectors lie in neighbouring lanes. 2: e4m3 with one
 // scale a row. Sums are in fp32; s is rounded only where it is stored, y is formed from what it was before.
-// With residual, 16,384 x 4,096 fp32: 158 us (6.8 TB/s); 16,384 x 2,048 bf16: 41 us (6.5 TB/s); 8,192 x 2,048 bf16 to 8 bits in blocks of 128: 26 us (4.5 TB/s:
-// instructions, two thirds of the issue slots; in one read and one write for every two elements there are 8 of the norm and 10 of the 8 bits).
+// With residual, 16,384 x 4,096 fp32: 158 us (6.8 TB/s); 16,384 x 2,048 bf16: 41 us (6.5 TB/s). To 8 bits in blocks of 128, with residual: 8,192 x 2,048 bf16 26 us (4.5 TB/s;
+// instructions and what one waits for another: two thirds of the issue slots), fp32 39 us (5.6 TB/s); with a scale a row 25 and 35.
 // Few threads a row (two to four vectors each) because what a row costs besides its vectors is paid by every warp: 2,048 columns of bf16 over 256 threads
 // 64 us, over 128 threads 45.
 // ---------------------------------------------------------------------------------------------
@@ -416,6 +416,8 @@ cudaError_t norm_typed(const NormArgs& n, cudaStream_t s) {
         else
             vecs = ceil_div(n.width + V - 1, V);
     }
+    // Rows of more than 32 vectors have two a thread (65,536 x 512 bf16 with a residual 41 us, 69 with one, which takes two warps a row). Rows of fp32 have four from 65 vectors on: 33.5 M elements in rows of 1,024 without a residual 41 us, 45 with two, in rows of 260 60 and 134, to 8 bits 70 and 79, with a residual 80 both ways. Rows of bf16 stay with
+    // two: one row of 2,048 takes 2.5 us, 2.9 with four, and 16,384 with a residual 41 both ways; many rows without a residual would be faster with four (24 us, 27 with two).
     const Shape shape = shape_of(vecs, 32, sizeof(T) == 2 ? 1024 : 64, 2048, std::max<int>(8, (int)(n.block / V)));
     const Lie lie = !wide ? kAnywhere : is_full<T>(n.x, n.x_pitch, n.width, shape) ? kFull : kWide;
     auto launch = [&](auto mode) {
