@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
     __shared__ alignas(16) float biases[LANES * N];
     extern __shared__ int counts[];
     const int lane = threadIdx.x % LANES, base = threadIdx.x % 32 - lane;
-    if (ALONE || !a.counts) ptx::chained();  // else k_clear before it has waited for all that came before
+    ptx::chained();
     if (a.counts)
         for (int e = threadIdx.x; e < a.experts; e += kThreadCount) counts[e] = 0;
     auto first_of = [&](int l) { return (l >> a.share_log) * a.group_size + (l & ((1 << a.share_log) - 1)) * a.per; };
@@ -428,7 +428,6 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
     }
     if (!a.counts) return;
     __syncthreads();
-    if (!ALONE) ptx::chained();
     for (int e = threadIdx.x; e < a.experts; e += kThreadCount) {
         if (ALONE)
             a.counts[e] = counts[e];
@@ -438,8 +437,7 @@ __global__ void __launch_bounds__(ALONE ? kAloneThreads : kThreads, ALONE ? 1 : 
 }
 
 __global__ void __launch_bounds__(1024) k_clear(int32_t* counts, int n) {
-    ptx::wait_previous();
-    ptx::release_next();  // the next kernel does not wait before it reads: all it reads was done before this one
+    ptx::chained();
     if ((int)threadIdx.x < n) counts[threadIdx.x] = 0;
 }
 

@@ -30,3 +30,15 @@ def test_kernels_that_begin_before_their_predecessor_ends_do_not_promise_the_com
     for file, name, parameters, _ in chained:
         assert not re.search(r"const [\w:]+\* *__restrict__", parameters), (file, name)
         assert "__ldg" not in _ and "ld.global.nc" not in _, (file, name)
+
+
+def test_kernels_that_begin_before_their_predecessor_ends_wait_for_it_whatever_their_arguments():
+    """What earlier kernels have written is visible behind a kernel's own wait alone, so none is on a condition, and nothing of memory is touched before it."""
+    for file, name, _, body in kernels():
+        waits = list(re.finditer(r"^.*(?:chained\(\)|wait_previous\(\)).*$", body, re.M))
+        if not waits:
+            continue
+        assert len(waits) == 1, (file, name)
+        assert re.fullmatch(r" {4}ptx::(chained|wait_previous)\(\);", waits[0].group()), (file, name)
+        before = body[body.index("{") + 1:waits[0].start()]
+        assert not re.search(r"\bload|\bstore|atomic|__ld|__st", before), (file, name)
