@@ -474,13 +474,13 @@ int a2cid2_rms_norm(const void* x, int64_t x_pitch, const void* residual, int64_
 
 /* The same with the result in 8 bits (e4m3: 4 exponent and 3 mantissa bits, largest value 448): for every `block` columns of a row (32, 64 or 128;
  * 0: the whole row; the last block of a row may be shorter) scale = max(largest magnitude / 448, 2^-126) and values = result / scale,
- * rounded to nearest even. values [n, width] bytes with a pitch in bytes, scales float [n, blocks] without gaps. NaN stays NaN. values overlaps
+ * both of the result in fp32 and as fp32 quotients, the second rounded to the nearest of the 8 bits, ties to even. values [n, width] bytes with a pitch in bytes, scales float [n, blocks] without gaps. NaN stays NaN. values overlaps
  * no other buffer. */
 int a2cid2_rms_norm_e4m3(const void* x, int64_t x_pitch, const void* residual, int64_t residual_pitch, const void* weight, int64_t n,
                          int64_t width, double eps, void* sum, int64_t sum_pitch, int64_t block, void* values, int64_t values_pitch,
                          float* scales, int32_t storage_dtype, void* cuda_stream);
 
-/* out = values * scales, rounded once to the storage type: reads back what the call above has written. */
+/* out = values * scales, a product in fp32 that is rounded to the storage type: reads back what the call above has written. */
 int a2cid2_dequantize_e4m3(const void* values, int64_t values_pitch, const float* scales, int64_t n, int64_t width, int64_t block,
                            void* out, int64_t out_pitch, int32_t storage_dtype, void* cuda_stream);
 
@@ -503,7 +503,7 @@ enum { A2_GROUP_BEST = 0, A2_GROUP_TWO_BEST = 1 };
 /* Routing of tokens to experts. logits [n, n_experts]; s = softmax over a token's experts, or sigmoid of each; key = s + bias (bias float [n_experts], for the
  * balance of the experts: it takes part in the choice alone), or the logit itself without a bias. The experts lie in `groups` groups of
  * equal size, one after the other; the `top_groups` groups of the best score are open (score: the best key of a group, or the sum
- * of its two best, where without a bias keys are s; the lowest group first where scores are equal).
+ * of its two best, where without a bias keys are s, and -inf for a group that has two experts or more and fewer than two available; the lowest group first where scores are equal).
  *   ids[t][j], j < k:  the open experts of the k best keys, best first, the lowest expert first where keys are equal;
  *   weights[t][j] = scale * s of that expert, with renormalize divided by the sum of the chosen ones' s;
  *   counts[e] = tokens that have chosen e (int32 [n_experts], or NULL).

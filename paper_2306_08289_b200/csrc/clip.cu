@@ -13,7 +13,7 @@ namespace {
 // Bound by memory: read once for the norm, read again and written once for the clipping. A worker's elements are cut into chunks of kChunkBytes, tensor after tensor;
 // every CTA has a run of consecutive chunks, over all workers, and leaves a sum for each worker it meets: CTA b and worker w at place b + w, which no other pair
 // has, since runs follow one another. Sums are joined in order.
-// 134 M elements, two thirds bf16 (340 MB), to other tensors: 165 us, 58 for the norm (5.9 TB/s) and 103 for the scaling (6.5 TB/s, a copy's rate); 135 M fp32
+// 134 M elements, two thirds bf16 (340 MB), to other tensors: 165 us, 58 for the norm (5.9 TB/s) and 98 to 103 for the scaling (6.5 TB/s, a copy's rate); 135 M fp32
 // 81 and 170. In place and not clipped 87. 16 workers of 4.5 MB: 35 us. The first reading leaves what it reads in the L2 cache where a second one follows (10 M fp32 clipped
 // 17.8 us, 20.3 without), and not where the norms are all (135 M fp32: 80.6 us, 82.6 with it). The second reading goes in the order of the first: against it, with
 // what was read last kept in the cache by hints, took the same (60 M fp32 113.3 us both ways) or more (16 workers of 34 MB 264 us, 258 in order).

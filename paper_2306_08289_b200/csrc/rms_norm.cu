@@ -174,8 +174,8 @@ struct NormKernelArgs {
 // scale a row. Sums are in fp32; s is rounded only where it is stored, y is formed from what it was before.
 // With residual, 16,384 x 4,096 fp32: 158 us (6.8 TB/s); 16,384 x 2,048 bf16: 41 us (6.5 TB/s). To 8 bits in blocks of 128, with residual: 8,192 x 2,048 bf16 26 us (4.5 TB/s;
 // instructions and what one waits for another: two thirds of the issue slots), fp32 39 us (5.6 TB/s); with a scale a row 25 and 35.
-// Few threads a row (two to four vectors each) because what a row costs besides its vectors is paid by every warp: 2,048 columns of bf16 over 256 threads
-// 64 us, over 128 threads 45.
+// Few threads a row (two to four vectors each) because what a row costs besides its vectors is paid by every warp; the
+// figures stand at the choice. Times here and below are of launches replayed from a graph, one behind the other.
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t bits_of(const float* p) { return __float_as_uint(*p); }
 __device__ __forceinline__ uint32_t bits_of(const __nv_bfloat16* p) { return *reinterpret_cast<const uint16_t*>(p); }
@@ -429,7 +429,8 @@ cudaError_t norm_typed(const NormArgs& n, cudaStream_t s) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// Values from their 8 bits and scales. Bound by memory: 8,192 x 2,048 to bf16 12.5 us behind the kernel that has written them (4.0 TB/s).
+// Values from their 8 bits and scales. Bound by memory's latency, one load of 16 bytes a thread before the conversions: 8,192 x 2,048 to bf16 8.9 us where the values lie in L2, 13.5 from
+// DRAM (3.7 TB/s); to fp32 20.5 us. Rows off boundaries go value by value: 8,192 x 2,049 28.8 us.
 // ---------------------------------------------------------------------------------------------
 constexpr int kBack = 16;  // values a thread takes at a time; blocks are multiples of it
 
@@ -503,7 +504,7 @@ cudaError_t dequantize_typed(const DequantizeArgs& a, cudaStream_t s) {
 // The reductions over a row leave the loads idle, so the rows to come are brought to shared memory meanwhile: every thread copies the vectors that
 // it will itself read, kStages rows deep, and waits for its own copies alone.
 // Long rows (LEAN) have no room for that: they keep x and g in registers and dw in shared memory, every thread its own.
-// 16,384 x 2,048 bf16 with ds: 50 us (5.4 TB/s), 16,384 x 1,024 fp32: 46 us (5.8 TB/s), of which the second kernel is 4 to 6; without the copies ahead the
+// 16,384 x 2,048 bf16 with ds: 51 us (5.3 TB/s), 16,384 x 1,024 fp32: 46 us (5.8 TB/s), of which the second kernel is 4 to 6; without the copies ahead the
 // first took 108 us. What holds bf16 back is one CTA of 16 warps a multiprocessor (124 registers: the row, its gradient, the weight and dw as floats), whose
 // issue slots are 60 % busy. 2,000 x 16,384 fp32 (LEAN): 149 us (3.5 TB/s).
 // ---------------------------------------------------------------------------------------------

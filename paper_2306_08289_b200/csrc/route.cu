@@ -190,9 +190,10 @@ __device__ __forceinline__ void sort(uint32_t (&u)[N]) {
 // lowest lane that has it, which is the lowest expert. Keys are fp32 scores less those bits. Where a decision is closer than their errors, the token's experts are
 // chosen again in 64 bits, so that the choice is that of exact scores; without a bias keys are the logits, and only what is equal but
 // for the lost bits is in doubt. Experts are counted in shared memory and added to `counts`, which an earlier kernel has cleared (ALONE: one CTA writes
-// them). Bound by instructions, nearly half of them comparisons, selections and logic, of which a multiprocessor takes two warps' a cycle: 815 a token of 256 experts
-// with sigmoid scores, a bias, 8 groups and 8 choices (362 of that kind): 32,768 tokens 45 us, for 6 us of memory. Without groups 38 us, by softmax without a bias 28, one
-// choice 20. LANES: 64 experts over 8 lanes, four tokens a warp, 10 us; over 32 lanes 26. 256 experts over 16 lanes 58 us (lists of 16 to sort and to move).
+// them). Bound by instructions, nearly half of them comparisons, selections and logic, of which a multiprocessor takes two warps' a cycle: 823 a token of 256 experts
+// with sigmoid scores, a bias, 8 groups and 8 choices (367 of that kind), which is 24 us of issue slots and 21 of that pipe; and by the rounds, each a chain of a reduction, a ballot and a shuffle
+// with one token a warp (issue slots 63 % busy): 32,768 tokens of fp32 44 us, for 6 us of memory. Without groups 38 us, by softmax without a bias 30, one
+// choice of those 20. LANES: 65,536 tokens of 64 experts, 2 chosen, over 8 lanes, four tokens a warp, 13 us; over 32 lanes 26. 256 experts over 16 lanes 58 us (lists of 16 to sort and to move).
 // ---------------------------------------------------------------------------------------------
 constexpr int kAloneThreads = 512;
 template <int N>
@@ -481,8 +482,8 @@ cudaError_t route_typed(const RouteArgs& r, cudaStream_t s) {
 //   sigmoid        dz_j = h_j (1 - s_j);      softmax  dz_e = [e chosen] h_e - s_e sum_m h_m for every expert.
 // LANES lanes take a token, lane j its j-th chosen expert, and all of them the row of the gradient, in vectors of 16 bytes (WIDE) or element by
 // element, side by side; then each chosen expert's lane writes that element once more, with the expert's own part. (Handing every expert to the lane that has
-// its element takes 2 N + 2 instructions each: 30,011 x 161, softmax not renormalised, 6 chosen, 24 us that way, 14 so.) In place: a warp has read all that it needs of a
-// token's row before it writes. Those 14 us are 2.9 TB/s: rows of 161 are read and written element by element; 128 experts in whole vectors, 8 chosen and
+// its element takes 2 N + 2 instructions each: 30,011 x 161, softmax not renormalised, 6 chosen, 24 us that way, 13 so, both with the approximate exponential.) In place: a warp has read all that it needs of a
+// token's row before it writes. With the accurate one it is 14.3 us (2.8 TB/s): rows of 161 are read and written element by element; 128 experts in whole vectors, 8 chosen and
 // renormalised, 8,192 tokens: 4 us, as long as a small kernel takes.
 // ---------------------------------------------------------------------------------------------
 struct RouteGradKernelArgs {
