@@ -114,8 +114,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
             sys.stderr.write(text)
             raise RuntimeError("g++ failed")
         os.replace(tmp, CALLS)
-        with open(CALLS + ".torch", "w") as f:
+        with open(tmp + ".torch", "w") as f:
             f.write(version + "\n")
+        os.replace(tmp + ".torch", CALLS + ".torch")  # others may be reading it
     return LIB
 
 

@@ -46,6 +46,7 @@ def test_what_is_built_is_not_built_again(made):
     assert made.names == ["lib.so", "_calls.so"] and build_mod.calls_version() == torch.__version__
     build_mod.build(force=True)
     assert made.names == ["lib.so", "_calls.so"] * 2
+    assert sorted(os.listdir(os.path.dirname(build_mod.LIB))) == ["_calls.so", "_calls.so.torch", "lib.so"]
 
 
 @pytest.mark.parametrize("how", ["no torch", "no CUDA in it"])
